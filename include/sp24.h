@@ -341,6 +341,48 @@ sp24_status sp24_apply_mask(sp24_dtype t, int64_t M, int64_t K, const void* w, i
 sp24_status sp24_prune_2d(sp24_dtype t, int64_t M, int64_t K, const void* x, int64_t ldx,
                           void* y, int64_t ldy, void* stream);
 
+/* Activations of sp24_linear and the operators around it: the identity, max(z, 0) (NaN stays), z Phi(z) with the normal
+ * distribution's Phi, z / (1 + exp(-z)), and the approximation of the second by tanh,
+ * z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2.  Evaluated in FP32. */
+typedef enum {
+  SP24_ACT_NONE = 0, SP24_ACT_RELU = 1, SP24_ACT_GELU = 2, SP24_ACT_SILU = 3, SP24_ACT_GELU_TANH = 4
+} sp24_act;
+
+/* (No counterpart in the paper: the operators that stand before, between and behind the sparse products of a
+ * feed-forward layer, and make their 8-bit operands.)
+ *
+ * Root-mean-square norm of rows, with the residual's addition before it:
+ *   h = x + residual, rounded to t (h = x without residual);
+ *   n = h / sqrt(mean(h^2) + eps) * weight, in FP32 from h as rounded;
+ *   y = n rounded to t (out_type == t), or 8-bit codes with a scale for each row (SP24_I8, SP24_E4M3, SP24_E5M2):
+ *   scale[i] = max |n[i, .]| / L with L = 127, 448, 57344, y = n / scale[i] rounded to the nearest code (ties to even).
+ *   A row of zeros, or of |n| all below about 1e-36, has scale 0 and codes 0.  A row with a NaN or an infinity in h has scale NaN and
+ *   codes 0 (SP24_I8) or NaN.
+ * The codes and scales are what the products with 8-bit operands take (the scales as sp24_linear's col_scale).
+ *   t: SP24_F16, SP24_BF16 or SP24_F32.  rows >= 0, 1 <= K <= 2^30; any leading dimensions >= K, any alignment that the
+ *   types have; fastest where rows start at 16-byte boundaries.
+ *   residual: rows x K of type t, or NULL.  h: where x + residual goes, or NULL; without residual it has to be NULL.
+ *   weight: K values of weight_type (t or SP24_F32), or NULL for ones.
+ *   scale: rows floats for 8-bit results, else ignored.  rstd: rows floats that receive 1 / sqrt(mean(h^2) + eps), or NULL.
+ *   h and y may each be the same buffer, with the same leading dimension, as x or residual (y: if out_type == t), but not
+ *   each other.  Else outputs overlap neither inputs nor each other. */
+sp24_status sp24_rms_norm(sp24_dtype t, int64_t rows, int64_t K, const void* x, int64_t ldx, const void* residual,
+                          int64_t ldr, const void* weight, sp24_dtype weight_type, float eps, void* h, int64_t ldh,
+                          sp24_dtype out_type, void* y, int64_t ldy, float* scale, float* rstd, void* stream);
+
+/* Gradient of sp24_rms_norm (out_type == t) from dy, the h it normalised (x without residual) and its rstd:
+ *   v = dy * weight;  dx = rstd v - rstd^3 h mean(v h) + dh;  dweight[k] = sum over rows of dy h rstd.
+ * dh (or NULL): the gradient that arrives at h itself along the residual stream.  With a residual, dx is the gradient of
+ * both x and the residual.  Everything in FP32, dx rounded once to t.  dweight: K floats, or NULL if it is not wanted.
+ *   dx may be the same buffer as dy, h or dh (same leading dimension).
+ *   workspace: sp24_rms_norm_backward_workspace_bytes(rows, K) bytes (0 for NULL dweight), 16-byte aligned, contents of no
+ *   matter before or after.  The rows' sums are added in an order that rows and K fix: the same call gives the same bits. */
+size_t sp24_rms_norm_backward_workspace_bytes(int64_t rows, int64_t K);
+sp24_status sp24_rms_norm_backward(sp24_dtype t, int64_t rows, int64_t K, const void* dy, int64_t lddy, const void* h,
+                                   int64_t ldh, const void* weight, sp24_dtype weight_type, const float* rstd,
+                                   const void* dh, int64_t lddh, void* dx, int64_t lddx, float* dweight, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
 /* End-to-end convenience for callers whose data lives in HOST memory (pinned for speed):
  * copies dense A (M x K, row-major, packed), B (N rows of K, packed) and, if beta != 0, C
  * (M x N packed) to the device buffers the caller provides, runs sp24_compress (TCGEN05

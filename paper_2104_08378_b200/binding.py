@@ -35,7 +35,7 @@ EXPORTS = [
     "sp24_im2col_nhwc_3x3", "sp24_pipeline_host", "sp24_gemm_static_ws", "sp24_gemm_i8_dequant",
     "sp24_conv3x3_nhwc", "sp24_kept_magnitude", "sp24_apply_mask", "sp24_prune_2d",
     "sp24_gemm_static_ws_status", "sp24_set_tile_override", "sp24_test_set_fault_hooks", "sp24_gemm_f16acc",
-    "sp24_gemm_plan",
+    "sp24_gemm_plan", "sp24_rms_norm", "sp24_rms_norm_backward_workspace_bytes", "sp24_rms_norm_backward",
 ]
 
 
@@ -98,6 +98,12 @@ def _load() -> ctypes.CDLL:
     lib.sp24_test_set_fault_hooks.restype = ci
     lib.sp24_im2col_nhwc_3x3.argtypes = [ci, i64, i64, i64, i64, vp, vp, i64, vp]
     lib.sp24_pipeline_host.argtypes = [ctypes.POINTER(GemmDesc)] + [vp] * 13 + [sz, vp]
+    lib.sp24_rms_norm.argtypes = [ci, i64, i64, vp, i64, vp, i64, vp, ci, ctypes.c_float, vp, i64, ci, vp, i64, vp, vp, vp]
+    lib.sp24_rms_norm_backward_workspace_bytes.argtypes = [i64, i64]
+    lib.sp24_rms_norm_backward_workspace_bytes.restype = sz
+    lib.sp24_rms_norm_backward.argtypes = [ci, i64, i64, vp, i64, vp, i64, vp, ci, vp, vp, i64, vp, i64, vp, vp, sz, vp]
+    for name in ("sp24_rms_norm", "sp24_rms_norm_backward"):
+        getattr(lib, name).restype = ci
     for name in ("sp24_prune", "sp24_compress", "sp24_decompress", "sp24_gemm", "sp24_gemm_status",
                  "sp24_im2col_nhwc_3x3", "sp24_pipeline_host"):
         getattr(lib, name).restype = ci
@@ -439,3 +445,115 @@ def prune_2d(x: torch.Tensor, out: torch.Tensor | None = None, dtype: str | None
     _check(lib.sp24_prune_2d(DTYPE_CODE[dt], M, K, _ptr(x), x.stride(0) if M > 1 else K, _ptr(out),
                              out.stride(0) if M > 1 else K, _stream()), "sp24_prune_2d")
     return out
+
+
+# ---- the operators around the products -----------------------------------------------------------------------------------
+# Their tensors may be on another device than the current one (all on the same): the call is then made with that one current,
+# on its current stream.  What torch knows about the tensors is checked here, the rest by the library.
+ERR_DTYPE, ERR_SHAPE, ERR_STRIDE, ERR_UNSUPPORTED = 2, 3, 4, 6
+_QUANT = ("i8", "e4m3", "e5m2")
+
+
+def _refuse(condition, status: int, where: str):
+    if condition:
+        raise Sp24Error(status, where)
+
+
+def _matrix(t: torch.Tensor, where: str, like: torch.Tensor | None = None, shape=None, dtype=None) -> int:
+    """The leading dimension of a CUDA matrix whose rows are contiguous; refused if it is not one, on another device than
+    `like`, or not of the shape or type given."""
+    _refuse(t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)), ERR_SHAPE, where)
+    _refuse(not t.is_cuda or (like is not None and t.device != like.device), ERR_UNSUPPORTED, where)
+    _refuse(dtype is not None and t.dtype != dtype, ERR_DTYPE, where)
+    _refuse(t.shape[1] > 1 and t.stride(1) != 1, ERR_STRIDE, where)
+    return t.stride(0) if t.shape[0] > 1 else max(1, t.shape[1])
+
+
+def _vector(t: torch.Tensor | None, n: int, where: str, like: torch.Tensor, dtypes=(torch.float32,)):
+    """The same for a contiguous vector of n values, or None."""
+    if t is None:
+        return
+    _refuse(t.dim() != 1 or t.shape[0] != n, ERR_SHAPE, where)
+    _refuse(not t.is_cuda or t.device != like.device, ERR_UNSUPPORTED, where)
+    _refuse(t.dtype not in dtypes, ERR_DTYPE, where)
+    _refuse(n > 1 and t.stride(0) != 1, ERR_STRIDE, where)
+
+
+def _on_device_of(name: str):
+    """Makes the device of the first argument, `name`, current for the call where it is not."""
+    def wrap(fn):
+        @functools.wraps(fn)
+        def call(*args, **kwargs):
+            t = args[0] if args else kwargs[name]
+            if not t.is_cuda or t.get_device() == torch.cuda.current_device():
+                return fn(*args, **kwargs)
+            with torch.cuda.device(t.device):
+                return fn(*args, **kwargs)
+        return call
+    return wrap
+
+
+def _float_code(t: torch.Tensor, where: str) -> int:
+    code = _FROM_TORCH.get(t.dtype)
+    _refuse(code not in ("f16", "bf16", "f32"), ERR_DTYPE, where)
+    return DTYPE_CODE[code]
+
+
+@_on_device_of("x")
+def rms_norm(x: torch.Tensor, weight: torch.Tensor | None = None, *, eps: float = 1e-6, residual: torch.Tensor | None = None,
+             quant: str | None = None, with_rstd: bool = False, h_out: torch.Tensor | None = None,
+             out: torch.Tensor | None = None):
+    """sp24_rms_norm on the rows of x [rows, K]: returns (y, h, scale, rstd).  h = x + residual (None without residual), y its
+    norm times weight [K] (x's type or float32; None: ones).  quant = "i8", "e4m3" or "e5m2": y in 8 bits and scale [rows],
+    else scale is None.  rstd [rows] with with_rstd, else None.  h_out and out may be x or residual themselves."""
+    where = "sp24_rms_norm"
+    t = _float_code(x, where)
+    ldx = _matrix(x, where)
+    rows, K = x.shape
+    _refuse(quant is not None and quant not in _QUANT, ERR_DTYPE, where)
+    _refuse(residual is None and h_out is not None, ERR_UNSUPPORTED, where)
+    ldr = ldh = ldx
+    h = None
+    if residual is not None:
+        ldr = _matrix(residual, where, x, x.shape, x.dtype)
+        h = x.new_empty((rows, K)) if h_out is None else h_out
+        ldh = _matrix(h, where, x, x.shape, x.dtype)
+    _vector(weight, K, where, x, (x.dtype, torch.float32))
+    out_dtype = x.dtype if quant is None else TORCH_DTYPE[quant]
+    y = x.new_empty((rows, K), dtype=out_dtype) if out is None else out
+    ldy = _matrix(y, where, x, x.shape, out_dtype)
+    scale = x.new_empty(rows, dtype=torch.float32) if quant is not None else None
+    rstd = x.new_empty(rows, dtype=torch.float32) if with_rstd else None
+    _check(lib.sp24_rms_norm(t, rows, K, _ptr(x), ldx, _ptr(residual), ldr, _ptr(weight),
+                             F32 if weight is None else DTYPE_CODE[_FROM_TORCH[weight.dtype]], eps, _ptr(h), ldh,
+                             t if quant is None else DTYPE_CODE[quant], _ptr(y), ldy, _ptr(scale), _ptr(rstd), _stream()), where)
+    return y, h, scale, rstd
+
+
+@_on_device_of("dy")
+def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor | None, rstd: torch.Tensor, *,
+                      dh: torch.Tensor | None = None, out: torch.Tensor | None = None):
+    """sp24_rms_norm_backward: (dx, dweight) from the gradient of y, the h that rms_norm normalised (x without residual), its
+    weight and its rstd; dh is the gradient that arrives at h along the residual.  dweight is float32, None without weight.
+    out may be dy, h or dh."""
+    where = "sp24_rms_norm_backward"
+    t = _float_code(dy, where)
+    lddy = _matrix(dy, where)
+    rows, K = dy.shape
+    ldh = _matrix(h, where, dy, dy.shape, dy.dtype)
+    lddh = lddy if dh is None else _matrix(dh, where, dy, dy.shape, dy.dtype)
+    _vector(weight, K, where, dy, (dy.dtype, torch.float32))
+    _refuse(rstd is None, 1, where)
+    _vector(rstd, rows, where, dy)
+    dx = dy.new_empty((rows, K)) if out is None else out
+    lddx = _matrix(dx, where, dy, dy.shape, dy.dtype)
+    dweight = ws = None
+    ws_bytes = 0
+    if weight is not None:
+        dweight = dy.new_empty(K, dtype=torch.float32)
+        ws_bytes = lib.sp24_rms_norm_backward_workspace_bytes(rows, K)
+        ws = dy.new_empty(ws_bytes, dtype=torch.uint8)
+    _check(lib.sp24_rms_norm_backward(t, rows, K, _ptr(dy), lddy, _ptr(h), ldh, _ptr(weight),
+                                      F32 if weight is None else DTYPE_CODE[_FROM_TORCH[weight.dtype]], _ptr(rstd), _ptr(dh),
+                                      lddh, _ptr(dx), lddx, _ptr(dweight), _ptr(ws), ws_bytes, _stream()), where)
+    return dx, dweight

@@ -1,0 +1,61 @@
+"""What the operators around the products refuse, before any device work: by the library's entry points and by the binding."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2104_08378_b200 import binding as sp
+
+ONE = ctypes.c_void_p(4096)
+F = ctypes.c_float
+
+
+def norm(t=sp.BF16, rows=4, K=64, x=ONE, ldx=64, r=ONE, ldr=64, w=ONE, wt=sp.BF16, eps=1e-6, h=ONE, ldh=64, out=sp.BF16, y=ONE,
+         ldy=64, scale=ONE, rstd=ONE):
+    return sp.lib.sp24_rms_norm(t, rows, K, x, ldx, r, ldr, w, wt, F(eps), h, ldh, out, y, ldy, scale, rstd, None)
+
+
+@pytest.mark.parametrize("status,args", [
+    (2, {"t": sp.I8}), (2, {"t": sp.I32}), (2, {"out": sp.F16}), (2, {"out": sp.I32}), (2, {"wt": sp.F16}), (2, {"t": 99}),
+    (3, {"rows": -1}), (3, {"K": 0}), (3, {"K": 2 ** 30 + 1}),
+    (6, {"eps": -1.0}), (6, {"eps": float("nan")}), (6, {"r": None}),
+    (1, {"x": None}), (1, {"y": None}), (1, {"out": sp.I8, "scale": None}),
+    (4, {"ldx": 63}), (4, {"ldr": 63}), (4, {"ldh": 0}), (4, {"ldy": -64}),
+    (5, {"x": ctypes.c_void_p(4097)}), (5, {"w": ctypes.c_void_p(4098), "wt": sp.F32}), (5, {"rstd": ctypes.c_void_p(4098)}),
+    (0, {"rows": 0, "x": None, "y": None})])
+def test_norm(status, args):
+    assert norm(**args) == status
+
+
+def norm_backward(t=sp.BF16, rows=4, K=64, dy=ONE, lddy=64, h=ONE, ldh=64, w=ONE, wt=sp.BF16, rstd=ONE, dh=ONE, lddh=64, dx=ONE,
+                  lddx=64, dw=ONE, ws=ONE, ws_bytes=1 << 20):
+    return sp.lib.sp24_rms_norm_backward(t, rows, K, dy, lddy, h, ldh, w, wt, rstd, dh, lddh, dx, lddx, dw, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("status,args", [
+    (2, {"t": sp.E4M3}), (2, {"wt": sp.F16}), (3, {"rows": -1}), (3, {"K": 0}), (1, {"dy": None}), (1, {"h": None}),
+    (1, {"rstd": None}), (1, {"dx": None}), (4, {"lddy": 63}), (4, {"ldh": 63}), (4, {"lddh": 63}), (4, {"lddx": 63}),
+    (5, {"dx": ctypes.c_void_p(4097)}), (7, {"ws": None}), (7, {"ws_bytes": 4 * 64 * 4 - 1}), (7, {"ws": ctypes.c_void_p(4100)}),
+    (0, {"rows": 0, "dw": None})])
+def test_norm_backward(status, args):
+    assert norm_backward(**args) == status
+
+
+def test_workspace_of_the_norms_gradient():
+    size = sp.lib.sp24_rms_norm_backward_workspace_bytes
+    assert size(4, 64) == 4 * 64 * 4 and size(10 ** 6, 64) == size(2 * 10 ** 6, 64) and size(0, 64) == size(4, 0) == 0
+
+
+def refused(status, fn, *args, **kwargs):
+    with pytest.raises(sp.Sp24Error) as e:
+        fn(*args, **kwargs)
+    assert e.value.status == status
+
+
+def test_the_binding_takes_cuda_tensors_only():
+    x, w, r = torch.zeros(4, 64), torch.zeros(64), torch.zeros(4)
+    refused(6, sp.rms_norm, x, w)
+    refused(6, sp.rms_norm_backward, x, x, w, r)
+    refused(2, sp.rms_norm, x.to(torch.int8))
+    refused(2, sp.rms_norm, x.double())
+    refused(3, sp.rms_norm, x[0])
