@@ -383,6 +383,33 @@ sp24_status sp24_rms_norm_backward(sp24_dtype t, int64_t rows, int64_t K, const 
                                    const void* dh, int64_t lddh, void* dx, int64_t lddx, float* dweight, void* workspace,
                                    size_t workspace_bytes, void* stream);
 
+/* Gated activation y = act(g) * u of rows (u == NULL: act(g) alone; with SP24_ACT_NONE then the rows themselves, quantised),
+ * in FP32, rounded once to t or to 8-bit codes with a scale for each row, as sp24_rms_norm has them (a NaN or an infinity in
+ * act(g) * u gives scale NaN).  g and u may be the two halves of one product's result (leading dimensions >= F, any
+ * alignment that the types have).  y may be the same buffer as g or u (out_type == t, same leading dimension). */
+sp24_status sp24_gated_act(sp24_dtype t, sp24_act act, int64_t rows, int64_t F, const void* g, int64_t ldg, const void* u,
+                           int64_t ldu, sp24_dtype out_type, void* y, int64_t ldy, float* scale, void* stream);
+
+/* Its gradient (out_type == t):  dg = dy * u * act'(g),  du = dy * act(g), in FP32, rounded once to t.  u and du are both
+ * given or both NULL.  dg may be the same buffer as g, u or dy, du too, each with its leading dimension, but not both the
+ * same. */
+sp24_status sp24_gated_act_backward(sp24_dtype t, sp24_act act, int64_t rows, int64_t F, const void* dy, int64_t lddy,
+                                    const void* g, int64_t ldg, const void* u, int64_t ldu, void* dg, int64_t lddg,
+                                    void* du, int64_t lddu, void* stream);
+
+/* Gradient of the activation of sp24_linear: dz = dy * act'(z), a rows x cols matrix in the order of dy and z (row-major
+ * here: rows are tokens if the product's D was column-major, features if it was row-major), in FP32 and rounded once to t.
+ *   dz, or NULL; dzt: dz transposed (cols x rows, leading dimension lddzt >= rows), or NULL.  The gradients of a layer's
+ *   input and of its weights contract dz over different axes, and each product wants its own contiguous.
+ *   dbias: the sums of dz before its rounding over the rows (sum_over_rows != 0: cols floats) or the columns (rows floats),
+ *   in an order that the sizes fix, or NULL.  z is not read for SP24_ACT_NONE and may be NULL then.
+ *   dz may be the same buffer as dy or z (same leading dimension).
+ *   workspace: sp24_act_backward_workspace_bytes(...) bytes for dbias, 16-byte aligned, contents of no matter. */
+size_t sp24_act_backward_workspace_bytes(int64_t rows, int64_t cols, int sum_over_rows);
+sp24_status sp24_act_backward(sp24_dtype t, sp24_act act, int64_t rows, int64_t cols, const void* dy, int64_t lddy,
+                              const void* z, int64_t ldz, void* dz, int64_t lddz, void* dzt, int64_t lddzt, float* dbias,
+                              int sum_over_rows, void* workspace, size_t workspace_bytes, void* stream);
+
 /* End-to-end convenience for callers whose data lives in HOST memory (pinned for speed):
  * copies dense A (M x K, row-major, packed), B (N rows of K, packed) and, if beta != 0, C
  * (M x N packed) to the device buffers the caller provides, runs sp24_compress (TCGEN05

@@ -36,6 +36,7 @@ EXPORTS = [
     "sp24_conv3x3_nhwc", "sp24_kept_magnitude", "sp24_apply_mask", "sp24_prune_2d",
     "sp24_gemm_static_ws_status", "sp24_set_tile_override", "sp24_test_set_fault_hooks", "sp24_gemm_f16acc",
     "sp24_gemm_plan", "sp24_rms_norm", "sp24_rms_norm_backward_workspace_bytes", "sp24_rms_norm_backward",
+    "sp24_gated_act", "sp24_gated_act_backward", "sp24_act_backward_workspace_bytes", "sp24_act_backward",
 ]
 
 
@@ -102,7 +103,12 @@ def _load() -> ctypes.CDLL:
     lib.sp24_rms_norm_backward_workspace_bytes.argtypes = [i64, i64]
     lib.sp24_rms_norm_backward_workspace_bytes.restype = sz
     lib.sp24_rms_norm_backward.argtypes = [ci, i64, i64, vp, i64, vp, i64, vp, ci, vp, vp, i64, vp, i64, vp, vp, sz, vp]
-    for name in ("sp24_rms_norm", "sp24_rms_norm_backward"):
+    lib.sp24_gated_act.argtypes = [ci, ci, i64, i64, vp, i64, vp, i64, ci, vp, i64, vp, vp]
+    lib.sp24_gated_act_backward.argtypes = [ci, ci, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    lib.sp24_act_backward_workspace_bytes.argtypes = [i64, i64, ci]
+    lib.sp24_act_backward_workspace_bytes.restype = sz
+    lib.sp24_act_backward.argtypes = [ci, ci, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, ci, vp, sz, vp]
+    for name in ("sp24_rms_norm", "sp24_rms_norm_backward", "sp24_gated_act", "sp24_gated_act_backward", "sp24_act_backward"):
         getattr(lib, name).restype = ci
     for name in ("sp24_prune", "sp24_compress", "sp24_decompress", "sp24_gemm", "sp24_gemm_status",
                  "sp24_im2col_nhwc_3x3", "sp24_pipeline_host"):
@@ -452,6 +458,7 @@ def prune_2d(x: torch.Tensor, out: torch.Tensor | None = None, dtype: str | None
 # on its current stream.  What torch knows about the tensors is checked here, the rest by the library.
 ERR_DTYPE, ERR_SHAPE, ERR_STRIDE, ERR_UNSUPPORTED = 2, 3, 4, 6
 _QUANT = ("i8", "e4m3", "e5m2")
+ACT = {None: 0, "relu": 1, "gelu": 2, "silu": 3, "gelu_tanh": 4}
 
 
 def _refuse(condition, status: int, where: str):
@@ -497,6 +504,11 @@ def _float_code(t: torch.Tensor, where: str) -> int:
     code = _FROM_TORCH.get(t.dtype)
     _refuse(code not in ("f16", "bf16", "f32"), ERR_DTYPE, where)
     return DTYPE_CODE[code]
+
+
+def _act_code(act: str | None, where: str) -> int:
+    _refuse(act not in ACT, ERR_UNSUPPORTED, where)
+    return ACT[act]
 
 
 @_on_device_of("x")
@@ -557,3 +569,74 @@ def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor | 
                                       F32 if weight is None else DTYPE_CODE[_FROM_TORCH[weight.dtype]], _ptr(rstd), _ptr(dh),
                                       lddh, _ptr(dx), lddx, _ptr(dweight), _ptr(ws), ws_bytes, _stream()), where)
     return dx, dweight
+
+
+@_on_device_of("g")
+def gated_act(g: torch.Tensor, u: torch.Tensor | None = None, *, act: str | None = "silu", quant: str | None = None,
+              out: torch.Tensor | None = None):
+    """sp24_gated_act: (y, scale) with y = act(g) * u on rows [rows, F] (act(g) without u; act: "relu", "gelu", "silu",
+    "gelu_tanh" or None).  quant = "i8", "e4m3" or "e5m2": y in 8 bits and scale [rows], else scale is None.  g and u may be
+    slices of one matrix; out may be g or u."""
+    where = "sp24_gated_act"
+    t, code = _float_code(g, where), _act_code(act, where)
+    ldg = _matrix(g, where)
+    rows, F = g.shape
+    ldu = ldg if u is None else _matrix(u, where, g, g.shape, g.dtype)
+    _refuse(quant is not None and quant not in _QUANT, ERR_DTYPE, where)
+    out_dtype = g.dtype if quant is None else TORCH_DTYPE[quant]
+    y = g.new_empty((rows, F), dtype=out_dtype) if out is None else out
+    ldy = _matrix(y, where, g, g.shape, out_dtype)
+    scale = g.new_empty(rows, dtype=torch.float32) if quant is not None else None
+    _check(lib.sp24_gated_act(t, code, rows, F, _ptr(g), ldg, _ptr(u), ldu, t if quant is None else DTYPE_CODE[quant], _ptr(y),
+                              ldy, _ptr(scale), _stream()), where)
+    return y, scale
+
+
+@_on_device_of("dy")
+def gated_act_backward(dy: torch.Tensor, g: torch.Tensor, u: torch.Tensor | None = None, *, act: str | None = "silu",
+                       dg: torch.Tensor | None = None, du: torch.Tensor | None = None):
+    """sp24_gated_act_backward: (dg, du) from the gradient of y = act(g) * u; du is None without u.  dg and du may be given,
+    as slices of one matrix for instance."""
+    where = "sp24_gated_act_backward"
+    t, code = _float_code(dy, where), _act_code(act, where)
+    lddy = _matrix(dy, where)
+    rows, F = dy.shape
+    ldg = _matrix(g, where, dy, dy.shape, dy.dtype)
+    dg = dy.new_empty((rows, F)) if dg is None else dg
+    lddg = _matrix(dg, where, dy, dy.shape, dy.dtype)
+    ldu = lddu = lddy
+    if u is not None:
+        ldu = _matrix(u, where, dy, dy.shape, dy.dtype)
+        du = dy.new_empty((rows, F)) if du is None else du
+        lddu = _matrix(du, where, dy, dy.shape, dy.dtype)
+    _check(lib.sp24_gated_act_backward(t, code, rows, F, _ptr(dy), lddy, _ptr(g), ldg, _ptr(u), ldu, _ptr(dg), lddg, _ptr(du),
+                                       lddu, _stream()), where)
+    return dg, du
+
+
+@_on_device_of("dy")
+def act_backward(dy: torch.Tensor, pre: torch.Tensor | None, *, act: str | None, cd_col_major: bool = False,
+                 transposed: bool = True, bias: bool = True, out: torch.Tensor | None = None):
+    """sp24_act_backward: (dz, dz transposed or None, dbias or None) from the gradient of act(pre).  cd_col_major as in the
+    product that made pre: True: dy and pre are [N, M], else [M, N]; dbias [M] sums over the N tokens.  Without an activation
+    dz is dy itself and pre is not read.  out may be dy or pre."""
+    where = "sp24_act_backward"
+    t, code = _float_code(dy, where), _act_code(act, where)
+    lddy = ldz = _matrix(dy, where)
+    rows, cols = dy.shape
+    dz = None
+    if code:
+        _refuse(pre is None, 1, where)
+        ldz = _matrix(pre, where, dy, dy.shape, dy.dtype)
+        dz = dy.new_empty((rows, cols)) if out is None else out
+    lddz = lddy if dz is None else _matrix(dz, where, dy, dy.shape, dy.dtype)
+    dzt = dy.new_empty((cols, rows)) if transposed else None
+    dbias = ws = None
+    ws_bytes = 0
+    if bias:
+        dbias = dy.new_empty(cols if cd_col_major else rows, dtype=torch.float32)
+        ws_bytes = lib.sp24_act_backward_workspace_bytes(rows, cols, 1 if cd_col_major else 0)
+        ws = dy.new_empty(ws_bytes, dtype=torch.uint8)
+    _check(lib.sp24_act_backward(t, code, rows, cols, _ptr(dy), lddy, _ptr(pre) if code else None, ldz, _ptr(dz), lddz, _ptr(dzt),
+                                 max(1, rows), _ptr(dbias), 1 if cd_col_major else 0, _ptr(ws), ws_bytes, _stream()), where)
+    return dy if dz is None else dz, dzt, dbias

@@ -62,7 +62,7 @@ __device__ __forceinline__ float act_and_slope(float z, float* slope) {
   }
   if (ACT == SP24_ACT_GELU_TANH) {
     const float p = logistic(tanh_argument(z));
-    *slope = p * fmaf(z * (1.f - p), fmaf(1.5957691f * 0.134145f, limited_square(z), 1.5957691f), 1.f);
+    *slope = fmaf(p * (1.f - p) * z, fmaf(1.5957691f * 0.134145f, limited_square(z), 1.5957691f), p);
     return z * p;
   }
   *slope = 1.f;
@@ -75,7 +75,7 @@ struct Act {
   static constexpr int value = ACT;
 };
 template <typename F>
-__host__ __device__ __forceinline__ auto with_act(int act, F&& f) {
+inline auto with_act(int act, F&& f) {
   switch (act) {
     case SP24_ACT_RELU: return f(Act<SP24_ACT_RELU>{});
     case SP24_ACT_GELU: return f(Act<SP24_ACT_GELU>{});

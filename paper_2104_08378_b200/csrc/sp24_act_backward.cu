@@ -1,0 +1,105 @@
+// Gradient of the activation between a product and what follows it: dz = dy * act'(z), in both orders (the two products of a linear
+// layer's gradient contract over different axes), and the bias's gradient, the sums of dz over tokens.
+#include "sp24_act.cuh"
+#include "sp24_rows.cuh"
+
+namespace sp24 {
+namespace {
+
+constexpr int kTile = 64;
+
+struct ActGradParams {
+  int64_t rows, cols;
+  const void *dy, *z;
+  void *dz, *dzt;
+  float* partial;  // sums over the rows of a tile (over_rows: [row tiles][cols]) or over its columns ([column tiles][rows]); or null
+  int64_t lddy, ldz, lddz, lddzt;
+  int32_t over_rows;
+};
+
+// A block to a tile of 64 x 64, transposed through shared memory.
+template <typename T, int ACT>
+__global__ void __launch_bounds__(256) act_grad_kernel(const ActGradParams p) {
+  __shared__ float tile[kTile][kTile + 1];
+  wait_for_stream();
+  const int64_t col_tiles = (p.cols + kTile - 1) / kTile;
+  const int64_t row0 = (int64_t)(blockIdx.x / col_tiles) * kTile, col0 = (int64_t)(blockIdx.x % col_tiles) * kTile;
+  const int x = threadIdx.x % kTile, y = threadIdx.x / kTile;
+  for (int i = y; i < kTile; i += 256 / kTile) {
+    const int64_t r = row0 + i, c = col0 + x;
+    float d = 0.f;
+    if (r < p.rows && c < p.cols) {
+      d = to_float(static_cast<const T*>(p.dy)[r * p.lddy + c]);
+      if (ACT != SP24_ACT_NONE) {
+        float slope;
+        act_and_slope<ACT>(to_float(static_cast<const T*>(p.z)[r * p.ldz + c]), &slope);
+        d *= slope;
+      }
+      if (p.dz) static_cast<T*>(p.dz)[r * p.lddz + c] = round_to<T>(d);
+    }
+    tile[i][x] = d;
+  }
+  __syncthreads();
+  if (p.dzt)
+    for (int i = y; i < kTile; i += 256 / kTile) {
+      const int64_t c = col0 + i, r = row0 + x;
+      if (r < p.rows && c < p.cols) static_cast<T*>(p.dzt)[c * p.lddzt + r] = round_to<T>(tile[x][i]);
+    }
+  if (p.partial && threadIdx.x < kTile) {
+    float sum = 0.f;
+    for (int i = 0; i < kTile; ++i) sum += p.over_rows ? tile[i][threadIdx.x] : tile[threadIdx.x][i];
+    const int64_t at = (p.over_rows ? col0 : row0) + threadIdx.x;
+    if (p.over_rows && at < p.cols) p.partial[row0 / kTile * p.cols + at] = sum;
+    if (!p.over_rows && at < p.rows) p.partial[col0 / kTile * p.rows + at] = sum;
+  }
+}
+
+}  // namespace
+}  // namespace sp24
+
+using namespace sp24;
+
+extern "C" size_t sp24_act_backward_workspace_bytes(int64_t rows, int64_t cols, int sum_over_rows) {
+  if (rows <= 0 || cols <= 0 || rows > kMostColumns || cols > kMostColumns) return 0;
+  const int64_t tiles = ((sum_over_rows ? rows : cols) + kTile - 1) / kTile;
+  return (size_t)tiles * (size_t)(sum_over_rows ? cols : rows) * sizeof(float);
+}
+
+extern "C" sp24_status sp24_act_backward(sp24_dtype t, sp24_act act, int64_t rows, int64_t cols, const void* dy, int64_t lddy, const void* z,
+                                         int64_t ldz, void* dz, int64_t lddz, void* dzt, int64_t lddzt, float* dbias, int sum_over_rows,
+                                         void* workspace, size_t workspace_bytes, void* stream) {
+  SP24_RETURN_IF(!is_float_type(t), SP24_ERR_DTYPE);
+  SP24_RETURN_IF(!is_act(act), SP24_ERR_UNSUPPORTED);
+  SP24_RETURN_IF(rows < 0 || cols < 0 || rows > kMostColumns || cols > kMostColumns, SP24_ERR_SHAPE);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const int64_t sums = sum_over_rows ? cols : rows;
+  SP24_RETURN_IF(!aligned(dbias, 4), SP24_ERR_ALIGN);
+  if (rows == 0 || cols == 0) {
+    if (!dbias || sums == 0) return SP24_OK;
+    const sp24_status st = check_arch();
+    return st != SP24_OK ? st : cuda_status(cudaMemsetAsync(dbias, 0, (size_t)sums * sizeof(float), s));
+  }
+  const bool reads_z = act != SP24_ACT_NONE;
+  SP24_RETURN_IF(!dy || (reads_z && !z), SP24_ERR_NULL);
+  SP24_RETURN_IF(!row_fits(rows, cols, lddy) || (reads_z && !row_fits(rows, cols, ldz)) || (dz && !row_fits(rows, cols, lddz)) ||
+                     (dzt && !row_fits(cols, rows, lddzt)),
+                 SP24_ERR_STRIDE);
+  const size_t es = elem_bytes(t);
+  SP24_RETURN_IF(!aligned(dy, es) || (reads_z && !aligned(z, es)) || !aligned(dz, es) || !aligned(dzt, es), SP24_ERR_ALIGN);
+  SP24_RETURN_IF(dbias && (!workspace || !aligned16(workspace) || workspace_bytes < sp24_act_backward_workspace_bytes(rows, cols, sum_over_rows)),
+                 SP24_ERR_WORKSPACE);
+  if (!dz && !dzt && !dbias) return SP24_OK;
+  const int64_t row_tiles = (rows + kTile - 1) / kTile, col_tiles = (cols + kTile - 1) / kTile;
+  SP24_RETURN_IF(row_tiles * col_tiles > 0x7fffffff, SP24_ERR_SHAPE);
+  sp24_status st = check_arch();
+  if (st != SP24_OK) return st;
+  const ActGradParams p = {rows, cols, dy, z, dz, dzt, dbias ? static_cast<float*>(workspace) : nullptr, lddy, ldz, lddz, lddzt, sum_over_rows != 0};
+  st = with_float_type(t, [&](auto type) {
+    using T = typename decltype(type)::type;
+    return with_act(act, [&](auto a) {
+      return launch_overlapped(act_grad_kernel<T, decltype(a)::value>, dim3((unsigned)(row_tiles * col_tiles)), dim3(256), 0, s, 1, p);
+    });
+  });
+  if (st != SP24_OK || !dbias) return st;
+  return column_sums(static_cast<const float*>(workspace), sum_over_rows ? row_tiles : col_tiles, sums, dbias, s);
+}

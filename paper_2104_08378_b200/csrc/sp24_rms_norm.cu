@@ -112,12 +112,6 @@ __global__ void __launch_bounds__(256) column_sums_kernel(const float* partial, 
 constexpr int64_t kMostPartials = 592;
 int64_t grad_blocks(int64_t rows) { return rows < kMostPartials ? rows : kMostPartials; }
 
-int row_threads(int64_t K) {
-  int threads = 32;
-  while (threads < 1024 && threads * 4 < K) threads *= 2;
-  return threads;
-}
-
 }  // namespace
 
 sp24_status column_sums(const float* partial, int64_t parts, int64_t K, float* out, cudaStream_t s) {

@@ -90,6 +90,9 @@ __device__ __forceinline__ OUT to_code(float v) {
   }
 }
 
+// an infinite maximum counts as NaN (where no factor of the row turns it into one)
+__device__ __forceinline__ float finite_or_nan(float top) { return top < __int_as_float(0x7f800000) ? top : __int_as_float(0x7fffffff); }
+
 // ---- a row's sum and maximum over a block ----------------------------------------------------------------------
 // Two buffers in turn, so that one barrier is enough: whoever writes a buffer again has passed the barrier of the one between,
 // which the readers reach behind their reads.
@@ -117,6 +120,13 @@ struct RowSums {
     t = __reduce_max_sync(~0u, t);
   }
 };
+
+// Threads of a block to a row of K elements.
+inline int row_threads(int64_t K) {
+  int threads = 32;
+  while (threads < 1024 && threads * 4 < K) threads *= 2;
+  return threads;
+}
 
 // out[k] = sum of partial[b * K + k] over b < parts, in an order that parts alone fixes (sp24_rms_norm.cu)
 sp24_status column_sums(const float* partial, int64_t parts, int64_t K, float* out, cudaStream_t s);

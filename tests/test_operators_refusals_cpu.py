@@ -59,3 +59,45 @@ def test_the_binding_takes_cuda_tensors_only():
     refused(2, sp.rms_norm, x.to(torch.int8))
     refused(2, sp.rms_norm, x.double())
     refused(3, sp.rms_norm, x[0])
+    refused(6, sp.gated_act, x, x)
+    refused(6, sp.gated_act, x, act="tanh")
+    refused(6, sp.gated_act_backward, x, x, x)
+    refused(6, sp.act_backward, x, x, act="gelu")
+
+
+def gated(t=sp.BF16, act=3, rows=4, F=64, g=ONE, ldg=64, u=ONE, ldu=64, out=sp.BF16, y=ONE, ldy=64, scale=ONE):
+    return sp.lib.sp24_gated_act(t, act, rows, F, g, ldg, u, ldu, out, y, ldy, scale, None)
+
+
+def gated_backward(t=sp.BF16, act=3, rows=4, F=64, dy=ONE, lddy=64, g=ONE, ldg=64, u=ONE, ldu=64, dg=ONE, lddg=64, du=ONE, lddu=64):
+    return sp.lib.sp24_gated_act_backward(t, act, rows, F, dy, lddy, g, ldg, u, ldu, dg, lddg, du, lddu, None)
+
+
+def act_backward(t=sp.BF16, act=3, rows=4, cols=64, dy=ONE, lddy=64, z=ONE, ldz=64, dz=ONE, lddz=64, dzt=ONE, lddzt=4, db=ONE, over_rows=1,
+                 ws=ONE, ws_bytes=1 << 20):
+    return sp.lib.sp24_act_backward(t, act, rows, cols, dy, lddy, z, ldz, dz, lddz, dzt, lddzt, db, over_rows, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("status,args", [
+    (2, {"t": sp.I8}), (2, {"out": sp.F32}), (6, {"act": 5}), (6, {"act": -1}), (3, {"rows": -1}), (3, {"F": 0}), (1, {"g": None}),
+    (1, {"y": None}), (1, {"out": sp.E4M3, "scale": None}), (4, {"ldg": 63}), (4, {"ldu": 63}), (4, {"ldy": 0}),
+    (5, {"u": ctypes.c_void_p(4097)}), (0, {"rows": 0})])
+def test_gated(status, args):
+    assert gated(**args) == status
+
+
+@pytest.mark.parametrize("status,args", [
+    (2, {"t": sp.I32}), (6, {"act": 9}), (6, {"u": None}), (3, {"F": 0}), (1, {"dy": None}), (1, {"g": None}), (1, {"dg": None}),
+    (1, {"du": None}), (4, {"lddy": 1}), (4, {"ldg": 1}), (4, {"ldu": 1}), (4, {"lddg": 1}), (4, {"lddu": 1}),
+    (5, {"dg": ctypes.c_void_p(4097)}), (0, {"rows": 0})])
+def test_gated_backward(status, args):
+    assert gated_backward(**args) == status
+
+
+@pytest.mark.parametrize("status,args", [
+    (2, {"t": sp.I8}), (6, {"act": 9}), (3, {"rows": -1}), (3, {"cols": 2 ** 30 + 1}), (1, {"dy": None}), (1, {"z": None}),
+    (4, {"lddy": 63}), (4, {"ldz": 63}), (4, {"lddz": 63}), (4, {"lddzt": 3}), (5, {"dzt": ctypes.c_void_p(4097)}),
+    (5, {"db": ctypes.c_void_p(4098)}), (7, {"ws": None}), (7, {"ws_bytes": 255}), (0, {"rows": 0, "db": None}),
+    (0, {"dz": None, "dzt": None, "db": None})])
+def test_act_backward(status, args):
+    assert act_backward(**args) == status
