@@ -235,6 +235,39 @@ sp24_status sp24_gemm_i8_dequant(const sp24_gemm_desc* d, const void* A, const v
                                  int relu, float out_scale, void* D, void* workspace,
                                  size_t workspace_bytes, void* stream);
 
+/* Activations of sp24_linear and the operators around it: the identity, max(z, 0) (NaN stays), z Phi(z) with the normal
+ * distribution's Phi, z / (1 + exp(-z)), and the approximation of the second by tanh,
+ * z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2.  Evaluated in FP32. */
+typedef enum {
+  SP24_ACT_NONE = 0, SP24_ACT_RELU = 1, SP24_ACT_GELU = 2, SP24_ACT_SILU = 3, SP24_ACT_GELU_TANH = 4
+} sp24_act;
+
+/* (No counterpart in the paper.)  A linear layer in one call: the product with scales, bias, activation and residual in its
+ * epilogue,
+ *   z[i,j] = row_scale[i] * col_scale[j] * acc[i,j] + bias[i],   D[i,j] = act(z[i,j]) + residual[i,j],
+ * acc = A * B as sp24_gemm accumulates it (FP32, INT32), everything after it in FP32 in the order written, D rounded once to
+ * cd_type.
+ *   row_scale, bias: device, M floats (a factor and an addend of each output feature), or NULL (1, 0).
+ *   col_scale: device, N floats (a factor of each token, as sp24_rms_norm and sp24_gated_act give with their 8-bit results),
+ *              or NULL (1); 8-bit operand types only.
+ *   residual:  device, M x N of cd_type in D's order with leading dimension d->ldc, 16-byte aligned, or NULL.  May be D.
+ *   pre:       device, receives z rounded to cd_type in D's order with leading dimension ld_pre (what the gradient of act
+ *              needs, see sp24_act_backward), 16-byte aligned, or NULL.  Must not overlap D or the residual. */
+typedef struct {
+  const float* row_scale;
+  const float* col_scale;
+  const float* bias;
+  sp24_act act;
+  const void* residual;
+  void* pre;
+  int64_t ld_pre;
+} sp24_linear_epilogue;
+
+/*   d: as for sp24_gemm; cd_type: F16/BF16 operands: their own type or SP24_F32; I8, E4M3, E5M2 operands: SP24_F16, SP24_BF16
+ *      or SP24_F32; F32 operands (TF32 mode): SP24_F32.  A, meta, B, D, workspace: as for sp24_gemm. */
+sp24_status sp24_linear(const sp24_gemm_desc* d, const sp24_linear_epilogue* e, const void* A, const void* meta,
+                        const void* B, void* D, void* workspace, size_t workspace_bytes, void* stream);
+
 /* 3x3, stride-1, pad-1 convolution of an NHWC activation with 2:4-sparse weights as an implicit
  * GEMM (Section 4.2: a convolution's reduction dimension is C*R*S): the same kernel as sp24_gemm,
  * but the B operand is read straight from the activation by im2col-mode TMA loads instead of
@@ -340,13 +373,6 @@ sp24_status sp24_apply_mask(sp24_dtype t, int64_t M, int64_t K, const void* w, i
  * lowest-numbered pattern with the largest score wins.  M % 4 == 0, K % 4 == 0; y may alias x. */
 sp24_status sp24_prune_2d(sp24_dtype t, int64_t M, int64_t K, const void* x, int64_t ldx,
                           void* y, int64_t ldy, void* stream);
-
-/* Activations of sp24_linear and the operators around it: the identity, max(z, 0) (NaN stays), z Phi(z) with the normal
- * distribution's Phi, z / (1 + exp(-z)), and the approximation of the second by tanh,
- * z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2.  Evaluated in FP32. */
-typedef enum {
-  SP24_ACT_NONE = 0, SP24_ACT_RELU = 1, SP24_ACT_GELU = 2, SP24_ACT_SILU = 3, SP24_ACT_GELU_TANH = 4
-} sp24_act;
 
 /* (No counterpart in the paper: the operators that stand before, between and behind the sparse products of a
  * feed-forward layer, and make their 8-bit operands.)

@@ -37,6 +37,7 @@ EXPORTS = [
     "sp24_gemm_static_ws_status", "sp24_set_tile_override", "sp24_test_set_fault_hooks", "sp24_gemm_f16acc",
     "sp24_gemm_plan", "sp24_rms_norm", "sp24_rms_norm_backward_workspace_bytes", "sp24_rms_norm_backward",
     "sp24_gated_act", "sp24_gated_act_backward", "sp24_act_backward_workspace_bytes", "sp24_act_backward",
+    "sp24_linear",
 ]
 
 
@@ -53,6 +54,11 @@ class GemmDesc(ctypes.Structure):
                 ("ldd", ctypes.c_int64),
                 ("order_b", ctypes.c_int), ("order_c", ctypes.c_int), ("order_d", ctypes.c_int),
                 ("a_is_dense", ctypes.c_int)]
+
+
+class LinearEpilogue(ctypes.Structure):
+    _fields_ = [("row_scale", ctypes.c_void_p), ("col_scale", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("act", ctypes.c_int),
+                ("residual", ctypes.c_void_p), ("pre", ctypes.c_void_p), ("ld_pre", ctypes.c_int64)]
 
 
 def _load() -> ctypes.CDLL:
@@ -108,7 +114,8 @@ def _load() -> ctypes.CDLL:
     lib.sp24_act_backward_workspace_bytes.argtypes = [i64, i64, ci]
     lib.sp24_act_backward_workspace_bytes.restype = sz
     lib.sp24_act_backward.argtypes = [ci, ci, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, ci, vp, sz, vp]
-    for name in ("sp24_rms_norm", "sp24_rms_norm_backward", "sp24_gated_act", "sp24_gated_act_backward", "sp24_act_backward"):
+    lib.sp24_linear.argtypes = [ctypes.POINTER(GemmDesc), ctypes.POINTER(LinearEpilogue), vp, vp, vp, vp, vp, sz, vp]
+    for name in ("sp24_linear", "sp24_rms_norm", "sp24_rms_norm_backward", "sp24_gated_act", "sp24_gated_act_backward", "sp24_act_backward"):
         getattr(lib, name).restype = ci
     for name in ("sp24_prune", "sp24_compress", "sp24_decompress", "sp24_gemm", "sp24_gemm_status",
                  "sp24_im2col_nhwc_3x3", "sp24_pipeline_host"):
@@ -640,3 +647,78 @@ def act_backward(dy: torch.Tensor, pre: torch.Tensor | None, *, act: str | None,
     _check(lib.sp24_act_backward(t, code, rows, cols, _ptr(dy), lddy, _ptr(pre) if code else None, ldz, _ptr(dz), lddz, _ptr(dzt),
                                  max(1, rows), _ptr(dbias), 1 if cd_col_major else 0, _ptr(ws), ws_bytes, _stream()), where)
     return dy if dz is None else dz, dzt, dbias
+
+
+@_on_device_of("A")
+def linear(A: torch.Tensor, meta: torch.Tensor | None, Bt: torch.Tensor, *, bias: torch.Tensor | None = None,
+           act: str | None = None, residual: torch.Tensor | None = None, row_scale: torch.Tensor | None = None,
+           col_scale: torch.Tensor | None = None, pre: bool | torch.Tensor = False, out: torch.Tensor | None = None,
+           cd: str | None = None, a_is_dense: bool = False, b_row_major: bool = False, cd_col_major: bool = False,
+           ws: torch.Tensor | None = None):
+    """sp24_linear: D = act(row_scale[i] * col_scale[j] * (A B)[i, j] + bias[i]) + residual[i, j].  A, meta, Bt, cd,
+    a_is_dense, b_row_major, cd_col_major as for gemm (cd defaults to A's type, bf16 for 8-bit operands); bias and row_scale
+    [M], col_scale [N] float32 (col_scale: 8-bit operands); residual in D's type and shape, and may be `out`.  Returns D, or
+    with pre=True (or a tensor for it) (D, what act was applied to)."""
+    where = "sp24_linear"
+    ab = _FROM_TORCH.get(A.dtype)
+    _refuse(ab is None or ab == "i32", ERR_DTYPE, where)
+    lda, ldb = _matrix(A, where), _matrix(Bt, where, A, None, A.dtype)
+    M, K = A.shape[0], A.shape[1] * (1 if a_is_dense else 2)
+    N = Bt.shape[1 if b_row_major else 0]
+    _refuse(Bt.shape[0 if b_row_major else 1] != K, ERR_SHAPE, where)
+    if not a_is_dense:
+        _refuse(meta is None, 1, where)
+        _vector(meta, meta_bytes(ab, M, K), where, A, (torch.uint8,))
+    cd = cd or ("bf16" if ab in _QUANT else ab)
+    _refuse(cd not in TORCH_DTYPE, ERR_DTYPE, where)
+    shape, dtype = ((N, M) if cd_col_major else (M, N)), TORCH_DTYPE[cd]
+    if out is None:
+        out = A.new_empty(shape, dtype=dtype)
+    ldd = ldc = _matrix(out, where, A, shape, dtype)
+    if residual is not None:
+        ldc = _matrix(residual, where, A, shape, dtype)
+    for v, n in ((bias, M), (row_scale, M), (col_scale, N)):
+        _vector(v, n, where, A)
+    z, ld_pre = None, 0
+    if pre is not False and pre is not None:
+        z = torch.empty_like(out) if pre is True else pre
+        ld_pre = _matrix(z, where, A, shape, dtype)
+    stream = _stream()
+    ws = ws if ws is not None else workspace(A.device, stream)
+    order = COL_MAJOR if cd_col_major else ROW_MAJOR
+    desc = GemmDesc(DTYPE_CODE[ab], DTYPE_CODE[cd], M, N, K, lda, ldb, ldc, ldd, ROW_MAJOR if b_row_major else COL_MAJOR, order,
+                    order, 1 if a_is_dense else 0)
+    epilogue = LinearEpilogue(_ptr(row_scale), _ptr(col_scale), _ptr(bias), _act_code(act, where), _ptr(residual), _ptr(z), ld_pre)
+    _check(lib.sp24_linear(byref(desc), byref(epilogue), _ptr(A), _ptr(meta), _ptr(Bt), _ptr(out), _ptr(ws), ws.numel(), stream),
+           where)
+    return out if z is None else (out, z)
+
+
+@_on_device_of("dy")
+def linear_backward(dy: torch.Tensor, pre: torch.Tensor | None, Bt: torch.Tensor, W: torch.Tensor, *, act: str | None = None,
+                    meta: torch.Tensor | None = None, b_row_major: bool = False, cd_col_major: bool = False,
+                    ws: torch.Tensor | None = None):
+    """Gradients of linear (16-bit operands, or float32 in the TF32 mode without meta) from dy, its `pre` (None without an activation) and Bt, and the pruned
+    weights W [M, K] themselves: (dBt, dW, dbias).  dy and pre are [N, M] with cd_col_major, else [M, N]; Bt [N, K], or [K, N]
+    with b_row_major; dBt has Bt's form.  With meta the entries of dW that the 2:4 pattern leaves out are zeros.  The
+    residual's gradient is dy.  sp24_act_backward, then two dense products (and sp24_apply_mask)."""
+    where = "sp24_linear_backward"
+    _float_code(dy, where)
+    _matrix(dy, where)
+    _matrix(W, where, dy, None, dy.dtype)
+    _matrix(Bt, where, dy, None, dy.dtype)
+    M, K = W.shape
+    N = Bt.shape[1 if b_row_major else 0]
+    _refuse(tuple(Bt.shape) != ((K, N) if b_row_major else (N, K)) or tuple(dy.shape) != ((N, M) if cd_col_major else (M, N)),
+            ERR_SHAPE, where)
+    _refuse(M % 16 or N % 16 or K % 16, ERR_SHAPE, where)
+    _refuse(meta is not None and dy.dtype == torch.float32, ERR_DTYPE, where)   # (apply_mask knows the 2:4 pattern only)
+    if meta is not None:
+        _vector(meta, meta_bytes(_FROM_TORCH[W.dtype], M, K), where, dy, (torch.uint8,))
+    dz, dzt, dbias = act_backward(dy, pre, act=act, cd_col_major=cd_col_major)
+    tokens, features = (dz, dzt) if cd_col_major else (dzt, dz)          # [N, M], [M, N]
+    dBt = gemm(tokens, None, W, a_is_dense=True, b_row_major=True, cd_col_major=b_row_major, ws=ws)
+    dW = gemm(features, None, Bt, a_is_dense=True, b_row_major=not b_row_major, ws=ws)
+    if meta is not None:
+        apply_mask(dW, meta, out=dW)
+    return dBt, dW, dbias

@@ -422,8 +422,9 @@ extern "C" sp24_status sp24_gemm_plan(const sp24_gemm_desc* d, int* ctas, int* b
 
 static sp24_status validate_gemm(const sp24_gemm_desc* d, const void* alpha, const void* A, const void* meta,
                                  const void* B, const void* beta, const void* C, void* D, void* ws, size_t ws_bytes,
-                                 bool& has_c, float& falpha, float& fbeta, bool dequant = false) {
-  SP24_RETURN_IF(d == nullptr || (!dequant && (alpha == nullptr || beta == nullptr)), SP24_ERR_NULL);
+                                 bool& has_c, float& falpha, float& fbeta, bool dequant = false,
+                                 const sp24_linear_epilogue* linear = nullptr) {
+  SP24_RETURN_IF(d == nullptr || (!dequant && !linear && (alpha == nullptr || beta == nullptr)), SP24_ERR_NULL);
   const bool tf32 = d->ab_type == SP24_F32;
   const bool f8 = is_fp8(d->ab_type);
   const bool fp = d->ab_type == SP24_F16 || d->ab_type == SP24_BF16 || tf32 || f8;
@@ -433,7 +434,7 @@ static sp24_status validate_gemm(const sp24_gemm_desc* d, const void* alpha, con
     SP24_RETURN_IF(fp || (d->cd_type != SP24_BF16 && d->cd_type != SP24_F16 && d->cd_type != SP24_F32 &&
                           d->cd_type != SP24_I8),
                    SP24_ERR_DTYPE);
-  else if (f8) SP24_RETURN_IF(d->cd_type != SP24_F16 && d->cd_type != SP24_BF16 && d->cd_type != SP24_F32, SP24_ERR_DTYPE);
+  else if (f8 || (linear && !fp)) SP24_RETURN_IF(d->cd_type != SP24_F16 && d->cd_type != SP24_BF16 && d->cd_type != SP24_F32, SP24_ERR_DTYPE);
   else if (fp) SP24_RETURN_IF(d->cd_type != d->ab_type && d->cd_type != SP24_F32, SP24_ERR_DTYPE);
   else SP24_RETURN_IF(d->cd_type != SP24_I32, SP24_ERR_DTYPE);
   const int64_t mult = elem_bytes(d->ab_type) == 1 ? 32 : 16;
@@ -442,9 +443,9 @@ static sp24_status validate_gemm(const sp24_gemm_desc* d, const void* alpha, con
   SP24_RETURN_IF(d->M > (int64_t(1) << 30) || d->N > (int64_t(1) << 30) || d->K > (int64_t(1) << 30), SP24_ERR_SHAPE);
   SP24_RETURN_IF(d->order_b != SP24_COL_MAJOR && d->order_b != SP24_ROW_MAJOR, SP24_ERR_UNSUPPORTED);
   SP24_RETURN_IF(d->order_d != SP24_ROW_MAJOR && d->order_d != SP24_COL_MAJOR, SP24_ERR_UNSUPPORTED);
-  if (dequant) {
+  if (dequant || linear) {
     falpha = 1.f;
-    fbeta = 0.f;
+    fbeta = linear && linear->residual ? 1.f : 0.f;
   } else if (fp) {
     falpha = *static_cast<const float*>(alpha);
     fbeta = *static_cast<const float*>(beta);
@@ -472,6 +473,12 @@ static sp24_status validate_gemm(const sp24_gemm_desc* d, const void* alpha, con
   SP24_RETURN_IF(!aligned16(A) || !aligned16(B) || !aligned16(D) || (has_c && !aligned16(C)) ||
                      (!d->a_is_dense && !aligned16(meta)),
                  SP24_ERR_ALIGN);
+  if (linear) {
+    SP24_RETURN_IF(linear->pre && (linear->ld_pre < cd_width || (linear->ld_pre * cs) % 16), SP24_ERR_STRIDE);
+    const uintptr_t vectors = reinterpret_cast<uintptr_t>(linear->row_scale) | reinterpret_cast<uintptr_t>(linear->col_scale) |
+                              reinterpret_cast<uintptr_t>(linear->bias);
+    SP24_RETURN_IF(!aligned16(linear->pre) || (vectors & 3), SP24_ERR_ALIGN);
+  }
   return SP24_OK;
 }
 
@@ -488,11 +495,12 @@ struct DequantArgs {
 
 static sp24_status run_gemm(const sp24_gemm_desc* d, const void* alpha, const void* A, const void* meta, const void* B,
                             const void* beta, const void* C, void* D, void* workspace, size_t workspace_bytes,
-                            void* stream, const DequantArgs* dq, const ConvArgs* cv = nullptr, bool acc_f16 = false) {
+                            void* stream, const DequantArgs* dq, const ConvArgs* cv = nullptr, bool acc_f16 = false,
+                            const sp24_linear_epilogue* linear = nullptr) {
   bool has_c = false;
   float falpha = 1.f, fbeta = 0.f;
   sp24_status st = validate_gemm(d, alpha, A, meta, B, beta, C, D, workspace, workspace_bytes, has_c, falpha, fbeta,
-                                 dq != nullptr);
+                                 dq != nullptr, linear);
   if (st != SP24_OK) return st;
   if (d->M == 0 || d->N == 0) return SP24_OK;
   if ((st = check_arch()) != SP24_OK) return st;
@@ -513,6 +521,15 @@ static sp24_status run_gemm(const sp24_gemm_desc* d, const void* alpha, const vo
     p.row_scale = dq->row_scale;
     p.bias = dq->bias;
     p.out_inv_scale = dq->out_inv_scale;
+  }
+  if (linear) {
+    p.linear = 1;
+    p.act = (int)linear->act;
+    p.row_scale = linear->row_scale;
+    p.col_scale = linear->col_scale;
+    p.bias = linear->bias;
+    p.pre = linear->pre;
+    p.ld_pre = linear->ld_pre;
   }
   p.M = d->M; p.N = d->N; p.K = d->K;
   p.ldc = d->ldc; p.ldd = d->ldd;
@@ -552,7 +569,7 @@ static sp24_status run_gemm(const sp24_gemm_desc* d, const void* alpha, const vo
   if (cfg.log.load(std::memory_order_relaxed))
     fprintf(stderr, "sp24_gemm: M=%lld N=%lld K=%lld ab=%d cd=%d %s%s tile=%dx%dx%d columns=%d split=%d band=%d beta=%g%s%s\n", (long long)d->M,
             (long long)d->N, (long long)d->K, (int)d->ab_type, (int)d->cd_type, sparse ? "sparse" : "dense",
-            b_mn ? " B:N-contiguous" : "", tile.ctas, tile.block_n, tile.mblk, tile.tile_n, 1 << tile.split_log, p.band, (double)fbeta, dq ? " dequant" : "",
+            b_mn ? " B:N-contiguous" : "", tile.ctas, tile.block_n, tile.mblk, tile.tile_n, 1 << tile.split_log, p.band, (double)fbeta, dq ? " dequant" : (linear ? " linear" : ""),
             cv ? " conv3x3" : (acc_f16 ? " fp16-accumulate" : ""));
   if (i8) return launch_gemm<1>(tile, sparse, b_mn, d, p, A, meta, B, s);
   if (tf32) return launch_gemm<2>(tile, sparse, b_mn, d, p, A, meta, B, s);
@@ -582,6 +599,14 @@ extern "C" sp24_status sp24_gemm_i8_dequant(const sp24_gemm_desc* d, const void*
   SP24_RETURN_IF(d->cd_type == SP24_I8 && !(out_scale > 0.f), SP24_ERR_UNSUPPORTED);
   DequantArgs dq = {row_scale, bias, relu ? 1 : 0, d->cd_type == SP24_I8 ? 1.0f / out_scale : 1.0f};
   return run_gemm(d, nullptr, A, meta, B, nullptr, nullptr, D, workspace, workspace_bytes, stream, &dq);
+}
+
+extern "C" sp24_status sp24_linear(const sp24_gemm_desc* d, const sp24_linear_epilogue* e, const void* A, const void* meta, const void* B,
+                                   void* D, void* workspace, size_t workspace_bytes, void* stream) {
+  SP24_RETURN_IF(d == nullptr || e == nullptr, SP24_ERR_NULL);
+  SP24_RETURN_IF((int)e->act < SP24_ACT_NONE || (int)e->act > SP24_ACT_GELU_TANH, SP24_ERR_UNSUPPORTED);
+  SP24_RETURN_IF(e->col_scale && elem_bytes(d->ab_type) != 1, SP24_ERR_UNSUPPORTED);
+  return run_gemm(d, nullptr, A, meta, B, nullptr, e->residual, D, workspace, workspace_bytes, stream, nullptr, nullptr, false, e);
 }
 
 extern "C" sp24_status sp24_conv3x3_nhwc(const sp24_gemm_desc* d, int64_t Nb, int64_t H, int64_t W, int64_t Cin,

@@ -77,6 +77,11 @@ struct GemmParams {
   const float* row_scale;
   const float* bias;
   float out_inv_scale;
+  // epilogue of sp24_linear (linear != 0; row_scale and bias above, C is the residual): pre, if not null, gets what act is applied to
+  int32_t linear, act;
+  const float* col_scale;
+  void* pre;
+  int64_t ld_pre;
 };
 
 constexpr int kSwizzle128Atom32 = 1280;
@@ -116,5 +121,11 @@ struct TileShape {
 template <int KIND>
 sp24_status launch_gemm(TileShape tile, bool sparse, bool b_mn, const sp24_gemm_desc* d, const GemmParams& p, const void* A,
                         const void* meta, const void* B, cudaStream_t s);
+
+// ---- in sp24_linear_{f16,i8,tf32,f8}.cu ------------------------------------------------------------
+// The same with the epilogue of sp24_linear (p.linear), which launch_gemm() passes on here.
+template <int KIND>
+sp24_status launch_linear(TileShape tile, bool sparse, bool b_mn, const sp24_gemm_desc* d, const GemmParams& p, const void* A,
+                          const void* meta, const void* B, cudaStream_t s);
 
 }  // namespace sp24

@@ -36,6 +36,7 @@
 
 #include <atomic>
 
+#include "sp24_act.cuh"
 #include "sp24_gemm.cuh"
 #include "sp24_ptx.cuh"
 
@@ -316,6 +317,63 @@ __device__ __forceinline__ void compute_row(const uint32_t (&r)[COLUMNS], const 
   }
 }
 
+// Epilogue of sp24_linear, one thread's row of a box: z = row_scale * col_scale * acc + bias in place of the accumulators, then the
+// activation, the residual and the rounding, all in FP32.  col_scale: that of column `lane` of the box; the columns are the same for all lanes of
+// the warp, their scales go round by shuffles.
+template <int KIND, int COLUMNS>
+__device__ __forceinline__ void scale_row(uint32_t (&r)[COLUMNS], float scale, float col_scale, float bias) {
+#pragma unroll
+  for (int e = 0; e < COLUMNS; ++e) {
+    const float a = KIND == 1 ? __int2float_rn((int)r[e]) : __uint_as_float(r[e]);
+    const float f = one_byte_operands(KIND) ? scale * __shfl_sync(~0u, col_scale, e) : scale;
+    r[e] = __float_as_uint(fmaf(a, f, bias));
+  }
+}
+template <int ACT, int COLUMNS>
+__device__ __forceinline__ void activate_row(uint32_t (&r)[COLUMNS]) {
+#pragma unroll
+  for (int e = 0; e < COLUMNS; ++e) r[e] = __float_as_uint(act_value<ACT>(__uint_as_float(r[e])));
+}
+template <int COLUMNS>
+__device__ __forceinline__ void activate_row(uint32_t (&r)[COLUMNS], int act) {
+  if (act == SP24_ACT_RELU) activate_row<SP24_ACT_RELU>(r);
+  else if (act == SP24_ACT_GELU) activate_row<SP24_ACT_GELU>(r);
+  else if (act == SP24_ACT_SILU) activate_row<SP24_ACT_SILU>(r);
+  else if (act == SP24_ACT_GELU_TANH) activate_row<SP24_ACT_GELU_TANH>(r);
+}
+template <int CS, int COLUMNS>
+__device__ __forceinline__ void pack_row(const uint32_t (&r)[COLUMNS], int cd_type, uint32_t (&o)[COLUMNS * CS / 4]) {
+  if constexpr (CS == 4) {
+#pragma unroll
+    for (int e = 0; e < COLUMNS; ++e) o[e] = r[e];
+  } else {
+    auto pack = [&](bool bf) {
+#pragma unroll
+      for (int e = 0; e < COLUMNS / 2; ++e) o[e] = pack_16bit(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1]), bf);
+    };
+    if (cd_type == SP24_BF16) pack(true);
+    else pack(false);
+  }
+}
+template <int CS, int COLUMNS>
+__device__ __forceinline__ void add_row(uint32_t (&r)[COLUMNS], const uint32_t (&c)[COLUMNS * CS / 4], int cd_type) {
+  if constexpr (CS == 4) {
+#pragma unroll
+    for (int e = 0; e < COLUMNS; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) + __uint_as_float(c[e]));
+  } else {
+    auto add = [&](bool bf) {
+#pragma unroll
+      for (int e = 0; e < COLUMNS / 2; ++e) {
+        const float2 f = unpack_16bit(c[e], bf);
+        r[2 * e] = __float_as_uint(__uint_as_float(r[2 * e]) + f.x);
+        r[2 * e + 1] = __float_as_uint(__uint_as_float(r[2 * e + 1]) + f.y);
+      }
+    };
+    if (cd_type == SP24_BF16) add(true);
+    else add(false);
+  }
+}
+
 // FP16 accumulation: every accumulator cell of tensor memory holds a binary16 value in its low half
 template <int COLUMNS>
 __device__ __forceinline__ void widen_f16_accumulators(uint32_t (&r)[COLUMNS]) {
@@ -367,13 +425,13 @@ __device__ __forceinline__ void convert_row_staged(const uint32_t (&r)[32], uint
 // half as wide, meet in pairs).
 // C is loaded in the order of the stores (whole 64-byte row segments as well) into registers, four boxes ahead, the
 // first four of a tile before its accumulators are complete, and goes to the rows' owners through the buffer.
-template <int KIND, int CS, bool COLS, bool HAS_C, int BLOCK_N, int CTAS, int MBLK, int ACC_STAGES, int WARPS, bool SPLIT>
+template <int KIND, int CS, bool COLS, bool HAS_C, int BLOCK_N, int CTAS, int MBLK, int ACC_STAGES, int WARPS, bool SPLIT, bool LINEAR>
 __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh, uint8_t* epi, uint32_t tmem_base,
                                               int cta_rank, int cluster_id, int num_clusters, int num_tiles, int warp,
                                               int lane, uint32_t parts, int split_rank) {
   constexpr int kCols = CS == 4 ? 16 : 32;  // columns of a box
   constexpr int W = kCols * CS / 4;         // 32-bit words of one box row
-  constexpr int P = 4;                      // boxes whose C values are held in registers
+  constexpr int P = LINEAR ? 2 : 4;         // boxes whose C values are held in registers (as many copies of the code of a box)
   constexpr int kUnits = W / 4;             // 16-byte units of a buffer row that hold data
   constexpr int kUnitElems = 16 / CS;       // elements per 16-byte unit
   constexpr int kRowsPerStore = 32 / kUnits;
@@ -465,8 +523,8 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
       for (int u = 0; u < kUnits; ++u)
         ptx::ld_shared_v4(own_row ^ (uint32_t)(u << 4), c[4 * u], c[4 * u + 1], c[4 * u + 2], c[4 * u + 3]);
     };
-    // packed output rows -> D
-    auto store = [&](const uint32_t (&o)[W], int row0, int col0) {
+    // packed output rows -> D (or what else has its form); `again`: the buffer has been stored from since this box's C came through it
+    auto store_to = [&](uint8_t* Db, size_t ldd_b, bool again, const uint32_t (&o)[W], int row0, int col0) {
       if constexpr (CS == 4 && COLS) {
         if (row0 + lane < M) {
           uint8_t* dst = Db + (size_t)col0 * ldd_b + (size_t)(row0 + lane) * CS;
@@ -475,7 +533,7 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
             if (col0 + e < col_end) *reinterpret_cast<uint32_t*>(dst + e * ldd_b) = o[e];
         }
       } else {
-        if (!has_c) __syncwarp();  // the reads of the box before are done (with C each lane writes what it alone has read)
+        if (!has_c || again) __syncwarp();  // the reads of the box before are done (with C each lane writes what it alone has read)
 #pragma unroll
         for (int u = 0; u < kUnits; ++u)
           ptx::st_shared_v4(own_row ^ (uint32_t)(u << 4), o[4 * u], o[4 * u + 1], o[4 * u + 2], o[4 * u + 3]);
@@ -515,6 +573,7 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
         }
       }
     };
+    auto store = [&](const uint32_t (&o)[W], int row0, int col0, bool again) { store_to(Db, ldd_b, again, o, row0, col0); };
     auto hand_back = [&] {  // this warp's part of the accumulators is in registers: the MMA issuer (CTA 0 of the pair) may go on
       ptx::tc_fence_before();
       __syncwarp();
@@ -525,9 +584,16 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
     };
     const uint32_t t_acc = tmem_base + (acc * MBLK) * BLOCK_N + ((uint32_t)(q * 32) << 16);
     uint32_t r[kCols], creg[P][W];
-    float scale = 1.f, bias = 0.f;
+    float scale = 1.f, bias = 0.f, col_scale = 1.f;
+    auto load_col_scale = [&](int col0) {  // lane e: that of column e of the box
+      if (LINEAR && one_byte_operands(KIND) && p.col_scale) col_scale = p.col_scale[min(col0 + lane, N - 1)];
+    };
     auto load_scale = [&](int row0) {
-      if (KIND == 1 && p.dequant) {
+      if (LINEAR) {
+        const int row = min(row0 + lane, M - 1);
+        if (p.row_scale) scale = p.row_scale[row];
+        if (p.bias) bias = p.bias[row];
+      } else if (KIND == 1 && p.dequant) {
         const int row = min(row0 + lane, M - 1);
         scale = p.row_scale[row];
         bias = p.bias ? p.bias[row] : 0.f;
@@ -560,17 +626,34 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
         }
       }
       if (KIND == 0 && p.acc_f16) widen_f16_accumulators(r);
-      compute_row<KIND, CS, kCols>(r, c, has_c, p, scale, bias, o);
+      bool again = false;
+      if constexpr (LINEAR) {
+        scale_row<KIND>(r, scale, col_scale, bias);
+        if (p.pre) {
+          pack_row<CS>(r, p.cd_type, o);
+          store_to(static_cast<uint8_t*>(p.pre), (size_t)p.ld_pre * CS, false, o, row0, col0);
+          again = true;
+        }
+        activate_row(r, p.act);
+        if (has_c) add_row<CS>(r, c, p.cd_type);
+        pack_row<CS>(r, p.cd_type, o);
+      } else {
+        compute_row<KIND, CS, kCols>(r, c, has_c, p, scale, bias, o);
+      }
       if (more) {
         ptx::tmem_ld_32x32b(t_acc + j * BLOCK_N + sc * kCols, r);
         if (j != j0) load_scale(row_q + j * kBlockM);
+        load_col_scale(tile_col + sc * kCols);
       }
       if (has_c) fetch_c(c);
-      store(o, row0, col0);
+      store(o, row0, col0, again);
       return more;
     };
     const bool any = mine && j < blocks;
-    if (any) load_scale(row_q + j * kBlockM);
+    if (any) {
+      load_scale(row_q + j * kBlockM);
+      load_col_scale(tile_col + sc * kCols);
+    }
     if (has_c && mine) {
 #pragma unroll
       for (int n = 0; n < P; ++n) fetch_c(creg[n]);
@@ -624,7 +707,8 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
 // the form (us, branches -> own kernels: bf16 24576 x 224 x 4096 with 512 x 224 tiles 39.8 -> 34.3, with C 43.6 -> 37.8).  With
 // and without C apart (the registers of four boxes of it): f16 256 x 256 x 512 3.29 -> 3.19, BERT FFN 12.48 -> 12.26, bf16
 // 8480 x 896 x 384 7.83 -> 7.46, with C 9920 x 544 x 1216 16.1 -> 15.6, f16 1184 x 736 x 1008 5.92 -> 5.82; none slower.
-template <int KIND, bool SPARSE, int BLOCK_N, int CTAS, int MBLK, bool B_MN, int CS, bool COLS, bool HAS_C, bool SPLIT = false, int WARPS = kEpiWarps>
+template <int KIND, bool SPARSE, int BLOCK_N, int CTAS, int MBLK, bool B_MN, int CS, bool COLS, bool HAS_C, bool SPLIT = false, int WARPS = kEpiWarps,
+          bool LINEAR = false>
 __global__ void __launch_bounds__(32 * (kFirstEpiWarp + WARPS), 1)
 gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
             const __grid_constant__ CUtensorMap map_e, const __grid_constant__ CUtensorMap map_c,
@@ -634,6 +718,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   // Operand atoms need 1024-byte alignment for the 128-byte swizzle.
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   constexpr bool kTall = is_tall<CTAS, MBLK>;
+  constexpr bool kStaged = !LINEAR && C::staged_epilogue(CS, COLS);
   static_assert(!kTall || (SPARSE && !B_MN && C::kABoxes == 1 && C::kBBoxes == 2), "tall tiles: sparse A, K-major B");
   // tall tiles: [slots of A and metadata | slots of B | epilogue staging]
   const int tile_n = p.tile_n, b_bytes = C::b_bytes(tile_n), b_slot_bytes = kTall ? b_bytes : 0;
@@ -645,7 +730,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t cta_rank = CTAS == 2 ? ptx::cluster_ctarank() : 0;
-  static_assert(WARPS == kEpiWarps || !(SPLIT || C::staged_epilogue(CS, COLS)), "these count on eight epilogue warps");
+  static_assert(WARPS == kEpiWarps || !(SPLIT || kStaged), "these count on eight epilogue warps");
   static_assert(!SPLIT || can_split<KIND, SPARSE, CTAS, MBLK, B_MN>, "only INT32 sums may be split");
   const int split_log = SPLIT ? p.split_log : 0, split_rank = SPLIT ? (int)ptx::cluster_ctarank() : 0;
   const int cluster_id = SPLIT ? blockIdx.x >> split_log : blockIdx.x / CTAS;
@@ -671,7 +756,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       ptx::mbar_init(&sh->tmem_full[lane], 1);
       ptx::mbar_init(&sh->tmem_empty[lane], WARPS * CTAS);  // one arrival per epilogue warp of the pair
     }
-    if (C::staged_epilogue(CS, COLS) && lane < 2 * kEpiWarps) ptx::mbar_init(&sh->c_full[lane >> 1][lane & 1], 1);
+    if (kStaged && lane < 2 * kEpiWarps) ptx::mbar_init(&sh->c_full[lane >> 1][lane & 1], 1);
     if (SPLIT && lane == 0) ptx::mbar_init(&sh->split_full, kEpiWarps >> split_log);
     if (lane == 0) sh->abort = 0;
     ptx::fence_barrier_init();
@@ -685,7 +770,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     ptx::prefetch_tensormap(&map_a);
     ptx::prefetch_tensormap(&map_b);
     if (SPARSE) ptx::prefetch_tensormap(&map_e);
-    if (C::staged_epilogue(CS, COLS)) {
+    if (kStaged) {
       if (HAS_C) ptx::prefetch_tensormap(&map_c);
       ptx::prefetch_tensormap(&map_d);
     }
@@ -996,10 +1081,10 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     }
   } else if (warp >= kFirstEpiWarp) {
     // ------------------------------ epilogue ------------------------------
-    if constexpr (!C::staged_epilogue(CS, COLS)) {
+    if constexpr (!kStaged) {
       // loads and stores by the epilogue warps themselves
       if (SPLIT) ptx::cluster_wait();  // (the set-up's: the other CTAs' barriers are there)
-      epilogue_direct<KIND, CS, COLS, HAS_C, BLOCK_N, CTAS, MBLK, C::kAccStages, WARPS, SPLIT>(p, sh, epi, tmem_base, (int)cta_rank, cluster_id,
+      epilogue_direct<KIND, CS, COLS, HAS_C, BLOCK_N, CTAS, MBLK, C::kAccStages, WARPS, SPLIT, LINEAR>(p, sh, epi, tmem_base, (int)cta_rank, cluster_id,
                                                                           num_clusters, num_tiles, warp, lane, ptx::smem_u32(b_ring), split_rank);
       // (all that this warp sends is on its way: the cluster may leave when every warp has come so far)
       if (SPLIT) {
@@ -1149,7 +1234,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   if (CTAS == 2 || SPLIT) settle();
 }
 
-template <int KIND, bool SPARSE, int BLOCK_N, int CTAS, int MBLK, bool B_MN>
+// LINEAR: with the epilogue of sp24_linear, in kernels of their own.
+template <int KIND, bool SPARSE, int BLOCK_N, int CTAS, int MBLK, bool B_MN, bool LINEAR>
 sp24_status launch(const TileShape& tile, const sp24_gemm_desc* d, const GemmParams& base, const void* A, const void* meta, const void* B,
                    cudaStream_t stream) {
   using C = Cfg<KIND, SPARSE, BLOCK_N, CTAS, MBLK, B_MN>;
@@ -1159,10 +1245,11 @@ sp24_status launch(const TileShape& tile, const sp24_gemm_desc* d, const GemmPar
   const int cs = elem_bytes(d->cd_type);
   // Shared-memory split.  The ring comes first (these kernels are bound by the operand feed: one
   // stage less cost the int8 configuration 9 %); a staged epilogue gets what is left.
-  constexpr bool kTwelve = twelve_warps<KIND, SPARSE, BLOCK_N, CTAS, MBLK, B_MN>;
+  constexpr bool kTwelve = !LINEAR && twelve_warps<KIND, SPARSE, BLOCK_N, CTAS, MBLK, B_MN>;
+  const bool staged = !LINEAR && C::staged_epilogue(cs, p.cd_col_major);
   int tile_m = kBlockM * CTAS * MBLK;
-  const int warps = epilogue_warps<KIND, SPARSE, BLOCK_N, CTAS, MBLK, B_MN>(d, tile_n);
-  p.epi_bytes = warps * (C::staged_epilogue(cs, p.cd_col_major) ? 4096 : 2048);
+  const int warps = LINEAR ? kEpiWarps : epilogue_warps<KIND, SPARSE, BLOCK_N, CTAS, MBLK, B_MN>(d, tile_n);
+  p.epi_bytes = warps * (staged ? 4096 : 2048);
   const int es = KIND == 0 ? 2 : (one_byte_operands(KIND) ? 1 : 4);
   const uint32_t atom_elems = kAtomBytes / es;
   const uint64_t a_cols = SPARSE ? d->K / 2 : d->K;
@@ -1232,7 +1319,7 @@ sp24_status launch(const TileShape& tile, const sp24_gemm_desc* d, const GemmPar
     map_e = map_a;
   }
   CUtensorMap map_c, map_d;
-  if (!C::staged_epilogue(cs, p.cd_col_major)) {
+  if (!staged) {
     map_c = map_d = map_a;  // not used
   } else {
     if (C::kSmemLimit - p.stages * ring_bytes >= 2 * p.epi_bytes) p.epi_bytes *= 2;
@@ -1248,12 +1335,12 @@ sp24_status launch(const TileShape& tile, const sp24_gemm_desc* d, const GemmPar
   constexpr bool kCanSplit = can_split<KIND, SPARSE, CTAS, MBLK, B_MN>;
   Kernel forms[24] = {}, twelve[2] = {};  // [split][with C][bytes][order]
 #define SP24_FORM(CS_, COLS_, C_)                                                                                                   \
-  forms[6 * C_ + 2 * (CS_ >> 1) + COLS_] = gemm_kernel<KIND, SPARSE, BLOCK_N, CTAS, MBLK, B_MN, CS_, COLS_, C_>;                     \
+  forms[6 * C_ + 2 * (CS_ >> 1) + COLS_] = gemm_kernel<KIND, SPARSE, BLOCK_N, CTAS, MBLK, B_MN, CS_, COLS_, C_, false, kEpiWarps, LINEAR>; \
   if constexpr (kTwelve && CS_ == 1) twelve[COLS_] = gemm_kernel<KIND, SPARSE, BLOCK_N, CTAS, MBLK, B_MN, CS_, COLS_, false, false, 12>; \
-  if constexpr (kCanSplit) forms[12 + 6 * C_ + 2 * (CS_ >> 1) + COLS_] = gemm_kernel<KIND, SPARSE, BLOCK_N, CTAS, MBLK, B_MN, CS_, COLS_, C_, true>;
-  if constexpr (KIND == 1) { SP24_FORM(1, false, false) SP24_FORM(1, true, false) }
+  if constexpr (kCanSplit) forms[12 + 6 * C_ + 2 * (CS_ >> 1) + COLS_] = gemm_kernel<KIND, SPARSE, BLOCK_N, CTAS, MBLK, B_MN, CS_, COLS_, C_, true, kEpiWarps, LINEAR>;
+  if constexpr (KIND == 1 && !LINEAR) { SP24_FORM(1, false, false) SP24_FORM(1, true, false) }
   if constexpr (KIND != 2) { SP24_FORM(2, false, false) SP24_FORM(2, true, false) }
-  if constexpr (KIND != 2 && KIND != 1) { SP24_FORM(2, false, true) SP24_FORM(2, true, true) }  // (int8: only INT32 results are added to)
+  if constexpr (KIND != 2 && (KIND != 1 || LINEAR)) { SP24_FORM(2, false, true) SP24_FORM(2, true, true) }  // (sp24_gemm, int8: only INT32 results are added to)
   if constexpr (BLOCK_N % 32 == 0) {  // 240-column tiles: 2-byte outputs only
     SP24_FORM(4, false, false) SP24_FORM(4, true, false) SP24_FORM(4, false, true) SP24_FORM(4, true, true)
   }
@@ -1282,16 +1369,14 @@ sp24_status launch(const TileShape& tile, const sp24_gemm_desc* d, const GemmPar
                            map_b, map_e, map_c, map_d, p);
 }
 
-}  // namespace
-
-template <int KIND>
-sp24_status launch_gemm(TileShape t, bool sparse, bool b_mn, const sp24_gemm_desc* d, const GemmParams& p, const void* A,
-                        const void* meta, const void* B, cudaStream_t s) {
+template <int KIND, bool LINEAR>
+sp24_status launch_shape(TileShape t, bool sparse, bool b_mn, const sp24_gemm_desc* d, const GemmParams& p, const void* A,
+                         const void* meta, const void* B, cudaStream_t s) {
   constexpr bool tf32 = KIND == 2;
   auto is = [&](int ctas, int block_n, int mblk) { return t.ctas == ctas && t.block_n == block_n && t.mblk == mblk; };
 #define SP24_SHAPE(CT, BN, MB, MN)                                     \
   if (is(CT, BN, MB) && b_mn == MN)                                    \
-    return sparse ? launch<KIND, true, BN, CT, MB, MN>(t, d, p, A, meta, B, s) : launch<KIND, false, BN, CT, MB, MN>(t, d, p, A, meta, B, s);
+    return sparse ? launch<KIND, true, BN, CT, MB, MN, LINEAR>(t, d, p, A, meta, B, s) : launch<KIND, false, BN, CT, MB, MN, LINEAR>(t, d, p, A, meta, B, s);
   SP24_SHAPE(1, 128, 1, false)
   SP24_SHAPE(2, 224, 1, false)
   SP24_SHAPE(2, 224, 2, false)
@@ -1306,11 +1391,20 @@ sp24_status launch_gemm(TileShape t, bool sparse, bool b_mn, const sp24_gemm_des
     SP24_SHAPE(2, 240, 1, false)  // 2-byte outputs only
   }
   if constexpr (!tf32)  // dense variant only
-    if (is(2, 256, 2) && !sparse && !b_mn) return launch<KIND, false, 256, 2, 2, false>(t, d, p, A, meta, B, s);
+    if (is(2, 256, 2) && !sparse && !b_mn) return launch<KIND, false, 256, 2, 2, false, LINEAR>(t, d, p, A, meta, B, s);
   if (t.ctas == 1 && t.block_n == 128 && (t.mblk == 2 || t.mblk == kTallBlocks) && sparse && !b_mn)
-    return launch<KIND, true, 128, 1, kTallBlocks, false>(t, d, p, A, meta, B, s);
+    return launch<KIND, true, 128, 1, kTallBlocks, false, LINEAR>(t, d, p, A, meta, B, s);
 #undef SP24_SHAPE
   return SP24_ERR_UNSUPPORTED;
+}
+
+}  // namespace
+
+template <int KIND>
+sp24_status launch_gemm(TileShape t, bool sparse, bool b_mn, const sp24_gemm_desc* d, const GemmParams& p, const void* A,
+                        const void* meta, const void* B, cudaStream_t s) {
+  if (p.linear) return launch_linear<KIND>(t, sparse, b_mn, d, p, A, meta, B, s);
+  return launch_shape<KIND, false>(t, sparse, b_mn, d, p, A, meta, B, s);
 }
 
 }  // namespace sp24

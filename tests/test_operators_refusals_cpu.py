@@ -101,3 +101,29 @@ def test_gated_backward(status, args):
     (0, {"dz": None, "dzt": None, "db": None})])
 def test_act_backward(status, args):
     assert act_backward(**args) == status
+
+
+def linear(ab=sp.BF16, cd=sp.BF16, M=64, N=32, K=64, lda=32, ldb=64, ldc=32, ldd=32, order=0, dense=0, act=1, row_scale=ONE, col_scale=None, bias=ONE,
+           residual=ONE, pre=ONE, ld_pre=32, A=ONE, meta=ONE, B=ONE, D=ONE, ws=ONE, ws_bytes=256):
+    d = sp.GemmDesc(ab, cd, M, N, K, lda, ldb, ldc, ldd, sp.COL_MAJOR, 0, order, dense)
+    e = sp.LinearEpilogue(row_scale, col_scale, bias, act, residual, pre, ld_pre)
+    return sp.lib.sp24_linear(ctypes.byref(d), ctypes.byref(e), A, meta, B, D, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("status,args", [
+    (2, {"ab": sp.I32}), (2, {"cd": sp.F16}), (2, {"ab": sp.I8, "cd": sp.I32}), (2, {"ab": sp.I8, "cd": sp.I8}), (2, {"ab": sp.E4M3, "cd": sp.I32}),
+    (6, {"ab": sp.F32, "cd": sp.F16}), (6, {"act": 7}), (6, {"act": -1}), (6, {"col_scale": ONE}), (6, {"order": 1, "ldd": 64}), (6, {"order": 3}),
+    (3, {"M": 40}), (3, {"N": 24}), (3, {"K": 72}), (3, {"ab": sp.I8, "M": 48}), (3, {"M": -16}),
+    (1, {"A": None}), (1, {"meta": None}), (1, {"B": None}), (1, {"D": None}), (7, {"ws": None}), (7, {"ws_bytes": 255}),
+    (4, {"lda": 24}), (4, {"ldb": 56}), (4, {"ldc": 24}), (4, {"ldd": 36}), (4, {"ld_pre": 24}), (4, {"ld_pre": 36}),
+    (5, {"residual": ctypes.c_void_p(4104)}), (5, {"pre": ctypes.c_void_p(4104)}), (5, {"bias": ctypes.c_void_p(4098)}),
+    (5, {"row_scale": ctypes.c_void_p(4098)}), (0, {"N": 0})])
+def test_linear(status, args):
+    assert linear(**args) == status
+
+
+def test_linear_without_a_problem():
+    assert sp.lib.sp24_linear(None, None, None, None, None, None, None, 0, None) == 1
+    x, w, m = torch.zeros(32, 64, dtype=torch.bfloat16), torch.zeros(64, 32, dtype=torch.bfloat16), torch.zeros(4096, dtype=torch.uint8)
+    refused(6, sp.linear, w, m, x)
+    refused(6, sp.linear_backward, x, x, x, w)
