@@ -382,7 +382,7 @@ sp24_status sp24_prune_2d(sp24_dtype t, int64_t M, int64_t K, const void* x, int
  *   n = h / sqrt(mean(h^2) + eps) * weight, in FP32 from h as rounded;
  *   y = n rounded to t (out_type == t), or 8-bit codes with a scale for each row (SP24_I8, SP24_E4M3, SP24_E5M2):
  *   scale[i] = max |n[i, .]| / L with L = 127, 448, 57344, y = n / scale[i] rounded to the nearest code (ties to even).
- *   A row of zeros, or of |n| all below about 1e-36, has scale 0 and codes 0.  A row with a NaN or an infinity in h has scale NaN and
+ *   A row of zeros, or of |h weight| all below 2^-110, has scale 0 and codes 0.  A row with a NaN or an infinity in h has scale NaN and
  *   codes 0 (SP24_I8) or NaN.
  * The codes and scales are what the products with 8-bit operands take (the scales as sp24_linear's col_scale).
  *   t: SP24_F16, SP24_BF16 or SP24_F32.  rows >= 0, 1 <= K <= 2^30; any leading dimensions >= K, any alignment that the

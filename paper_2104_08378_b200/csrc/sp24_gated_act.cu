@@ -26,11 +26,10 @@ __global__ void __launch_bounds__(1024) gated_act_kernel(const GatedParams p) {
     auto value = [&](int64_t k) { return act_value<ACT>(to_float(g[k])) * (u ? to_float(u[k]) : 1.f); };
     float inv = 0.f;
     if (is_code<OUT>) {
-      uint32_t top = 0;
-      float unused = 0.f;
-      for (int64_t k = threadIdx.x; k < p.F; k += blockDim.x) top = max(top, magnitude(value(k)));
+      float top = 0.f, unused = 0.f;
+      for (int64_t k = threadIdx.x; k < p.F; k += blockDim.x) top = max_abs(top, value(k), 0.f);
       sums.reduce(unused, top, turn);
-      const float scale = row_scale<OUT>(finite_or_nan(__uint_as_float(top)), 1.f, &inv);
+      const float scale = row_scale<OUT>(finite_or_nan(top), 1.f, &inv);
       if (threadIdx.x == 0) p.scale[row] = scale;
     }
     for (int64_t k = threadIdx.x; k < p.F; k += blockDim.x) {

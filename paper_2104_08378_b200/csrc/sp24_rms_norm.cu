@@ -12,7 +12,107 @@ struct NormParams {
   int64_t ldx, ldr, ldh, ldy;
   float eps;
   int32_t weight_f32;
+  bool whole_x, whole_r, whole_h, whole_y, whole_w;  // rows (the weight) at boundaries of vectors
 };
+
+// Rows of up to kMostTeamVectors vectors: a team of threads to a row, which holds it in registers, and the weight for all its rows.  One pass: the
+// team's next row (without a residual the next two, in as many registers) is on its way while this one is reduced, multiplied and
+// stored.
+template <typename T, typename OUT, typename W, int V, bool RESIDUAL, bool WHOLE>
+__global__ void __launch_bounds__(team_threads(V), 1) rms_norm_rows_kernel(const NormParams p) {
+  constexpr int N = kVector<T>, kWords = sizeof(W) / sizeof(T);  // 16-byte words of a vector's weights
+  __shared__ RowSums sums;
+  int turn = 0;
+  const int tx = threadIdx.x, team = blockDim.x;
+  const int64_t step = (int64_t)gridDim.x * blockDim.y;
+  wait_for_stream();
+  uint4 a[V], b[V], w[V][kWords];  // a row and its residual, or two rows
+  auto fetch = [&](const void* from, int64_t ld, bool whole, int64_t row, uint4 (&to)[V]) {
+    if (row >= p.rows) return;
+    const T* at = static_cast<const T*>(from) + row * ld;
+#pragma unroll
+    for (int v = 0; v < V; ++v) to[v] = load_vector<WHOLE>(at, tx + v * team, (int)p.K, whole);
+  };
+  int64_t base = (int64_t)blockIdx.x * blockDim.y;  // the first team's row: the warps of a block stay together
+  fetch(p.x, p.ldx, p.whole_x, base + threadIdx.y, a);
+  if (RESIDUAL) fetch(p.residual, p.ldr, p.whole_r, base + threadIdx.y, b);
+  else fetch(p.x, p.ldx, p.whole_x, base + step + threadIdx.y, b);
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      Pairs<W> one;
+#pragma unroll
+      for (int n = 0; n < kVector<W> / 2; ++n) one[n] = both(1.f);
+      w[v][i] = p.weight ? load_vector<WHOLE>(static_cast<const W*>(p.weight), (tx + v * team) * kWords + i, (int)p.K, p.whole_w) : pack<W>(one);
+    }
+  auto weighted = [&](int v, Pairs<T>& f) {  // f times the weights
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      Pairs<W> g;
+      unpack<W>(w[v][i], g);
+#pragma unroll
+      for (int n = 0; n < kVector<W> / 2; ++n) f[i * (kVector<W> / 2) + n] = mul2(f[i * (kVector<W> / 2) + n], g[n]);
+    }
+  };
+  // the row whose values are in x (and its residual in b), behind whose use the registers get the next ones
+  auto one_row = [&](int64_t row, uint4 (&x)[V]) {
+    const int K = row < p.rows ? (int)p.K : 0;
+    uint4 h[V];
+    float2 sum2 = both(0.f);
+    float top = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      h[v] = RESIDUAL ? add_packed<T>(x[v], b[v]) : x[v];
+      Pairs<T> f;
+      unpack<T>(h[v], f);
+#pragma unroll
+      for (int n = 0; n < N / 2; ++n) sum2 = fma2(f[n], f[n], sum2);
+      if (is_code<OUT>) {
+        weighted(v, f);
+#pragma unroll
+        for (int n = 0; n < N / 2; ++n) top = max_abs(top, f[n].x, f[n].y);
+      }
+    }
+    fetch(p.x, p.ldx, p.whole_x, row + (RESIDUAL ? step : 2 * step), x);
+    if (RESIDUAL) {
+      fetch(p.residual, p.ldr, p.whole_r, row + step, b);
+      if (p.h) {
+        T* ph = static_cast<T*>(p.h) + row * p.ldh;
+#pragma unroll
+        for (int v = 0; v < V; ++v) store_vector<WHOLE>(ph, tx + v * team, K, p.whole_h, h[v]);
+      }
+    }
+    float sum = sum2.x + sum2.y;
+    sums.reduce<true, is_code<OUT>>(sum, top, turn);
+    const float rstd = rsqrtf(sum / (float)p.K + p.eps);
+    if (tx == 0 && K && p.rstd) p.rstd[row] = rstd;
+    float factor = rstd;
+    if (is_code<OUT>) {
+      const float scale = row_scale<OUT>(top, rstd, &factor);
+      if (tx == 0 && K) p.scale[row] = scale;
+    }
+    OUT* py = static_cast<OUT*>(p.y) + row * p.ldy;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      Pairs<T> f;
+      unpack<T>(h[v], f);
+      if (is_code<OUT>) weighted(v, f);
+#pragma unroll
+      for (int n = 0; n < N / 2; ++n) f[n] = mul2(f[n], both(factor));
+      if (!is_code<OUT>) weighted(v, f);
+      if constexpr (is_code<OUT>) store_codes<WHOLE, OUT>(py, tx + v * team, K, p.whole_y, f);
+      else store_vector<WHOLE>(py, tx + v * team, K, p.whole_y, pack<T>(f));
+    }
+  };
+  for (; base < p.rows; base += step) {
+    one_row(base + threadIdx.y, a);
+    if (!RESIDUAL) {
+      base += step;
+      if (base < p.rows) one_row(base + threadIdx.y, b);
+    }
+  }
+}
 
 // Rows of any length and alignment: a block to a row, two passes over it (the second from the caches).  The scale of an 8-bit row needs no
 // pass of its own: max |n| = rstd max |h w|.
@@ -29,18 +129,18 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(const NormParams p) {
     auto weight = [&](int64_t k) { return p.weight ? load_weight<T>(p.weight, p.weight_f32, k) : 1.f; };
     auto value = [&](int64_t k) { return r ? to_float(round_to<T>(to_float(x[k]) + to_float(r[k]))) : to_float(x[k]); };
     float sum = 0.f;
-    uint32_t top = 0;
+    float top = 0.f;
     for (int64_t k = threadIdx.x; k < p.K; k += blockDim.x) {
       const float v = value(k);
       sum = fmaf(v, v, sum);
-      if (is_code<OUT>) top = max(top, magnitude(v * weight(k)));
+      if (is_code<OUT>) top = max_abs(top, v * weight(k), 0.f);
     }
     sums.reduce(sum, top, turn);
     const float rstd = rsqrtf(sum / (float)p.K + p.eps);
     if (threadIdx.x == 0 && p.rstd) p.rstd[row] = rstd;
     float inv = 0.f;
     if (is_code<OUT>) {
-      const float scale = row_scale<OUT>(__uint_as_float(top), rstd, &inv);
+      const float scale = row_scale<OUT>(top, rstd, &inv);
       if (threadIdx.x == 0) p.scale[row] = scale;
     }
     for (int64_t k = threadIdx.x; k < p.K; k += blockDim.x) {
@@ -76,7 +176,7 @@ __global__ void __launch_bounds__(1024) rms_norm_grad_kernel(const NormGradParam
     auto weight = [&](int64_t k) { return p.weight ? load_weight<T>(p.weight, p.weight_f32, k) : 1.f; };
     const float rstd = p.rstd[row];
     float sum = 0.f;
-    uint32_t unused = 0;
+    float unused = 0.f;
     for (int64_t k = threadIdx.x; k < p.K; k += blockDim.x) sum = fmaf(to_float(dy[k]) * weight(k), to_float(h[k]), sum);
     sums.reduce(sum, unused, turn);
     const float along = sum / (float)p.K * rstd * rstd;
@@ -138,11 +238,31 @@ extern "C" sp24_status sp24_rms_norm(sp24_dtype t, int64_t rows, int64_t K, cons
                  SP24_ERR_ALIGN);
   sp24_status st = check_arch();
   if (st != SP24_OK) return st;
-  const NormParams p = {rows, K, x, residual, weight, h, y, scale, rstd, ldx, ldr, ldh, ldy, eps, weight_type == SP24_F32};
+  NormParams p = {rows, K, x, residual, weight, h, y, scale, rstd, ldx, ldr, ldh, ldy, eps, weight_type == SP24_F32};
+  p.whole_x = whole_rows(x, rows, ldx, es, 16);
+  p.whole_r = !residual || whole_rows(residual, rows, ldr, es, 16);
+  p.whole_h = !h || whole_rows(h, rows, ldh, es, 16);
+  p.whole_y = whole_rows(y, rows, ldy, os, 16 / es * os);
+  p.whole_w = aligned(weight, 16);
+  const int64_t vectors = (K * (int64_t)es + 15) / 16;
+  const bool whole = p.whole_x && p.whole_r && p.whole_h && p.whole_y && p.whole_w && K * es % 16 == 0;
   return with_float_type(t, [&](auto type) {
     using T = typename decltype(type)::type;
     return with_out_type<T>(out_type, [&](auto out) {
       using OUT = typename decltype(out)::type;
+      if (vectors <= kMostTeamVectors) {
+        const TeamLaunch at(rows, vectors);
+        auto launch = [&](auto weight_t) {
+          using W = typename decltype(weight_t)::type;
+          const auto kernel = with_flags(
+              [](auto four, auto two, auto with_residual, auto whole) {
+                return rms_norm_rows_kernel<T, OUT, W, four.value ? 4 : two.value ? 2 : 1, with_residual.value, whole.value>;
+              },
+              at.v == 4, at.v >= 2, residual != nullptr, whole);
+          return launch_overlapped(kernel, at.grid, at.block, 0, static_cast<cudaStream_t>(stream), 1, p);
+        };
+        return weight && weight_type == SP24_F32 ? launch(TypeOf<float>{}) : launch(TypeOf<T>{});
+      }
       return launch_overlapped(rms_norm_kernel<T, OUT>, dim3((unsigned)(rows < 65535 ? rows : 65535)), dim3(row_threads(K)), 0,
                                static_cast<cudaStream_t>(stream), 1, p);
     });

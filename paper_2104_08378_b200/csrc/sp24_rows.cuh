@@ -5,6 +5,8 @@
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
+#include <type_traits>
+
 #include "sp24_common.cuh"
 
 namespace sp24 {
@@ -41,6 +43,15 @@ inline sp24_status with_out_type(sp24_dtype t, F&& f) {
   }
 }
 
+// f(flags as types...) with a member `value` each
+template <typename F>
+inline auto with_flags(F&& f) { return f(); }
+template <typename F, typename... Rest>
+inline auto with_flags(F&& f, bool first, Rest... rest) {
+  auto go = [&](auto flag) { return with_flags([&](auto... others) { return f(flag, others...); }, rest...); };
+  return first ? go(std::true_type{}) : go(std::false_type{});
+}
+
 __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
 __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
@@ -61,16 +72,19 @@ constexpr bool is_code = sizeof(OUT) == 1;
 template <typename OUT>
 constexpr float kLargestCode = std::is_same_v<OUT, int8_t> ? 127.f : std::is_same_v<OUT, __nv_fp8_e4m3> ? 448.f : 57344.f;
 
-// |v| as an integer that grows with it; NaN is above everything, so that a maximum keeps it.
-__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+// max(m, |a|, |b|) for m >= 0; NaN stays.
+__device__ __forceinline__ float max_abs(float m, float a, float b) {
+  asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(a), "f"(b));
+  return m;
+}
 
-// Scale of a row whose values are v * factor with max |v| = top, and what v is multiplied by to give codes.  Rows below 2^-120
-// count as zeros (L / top would pass the largest float).  NaN or an infinity anywhere (factor: rstd is NaN or 0 then) gives
+// Scale of a row whose values are v * factor with max |v| = top, and what v is multiplied by to give codes.  Rows below 2^-110
+// count as zeros (below 2^-112 L / top could pass the largest float).  NaN or an infinity anywhere (factor: rstd is NaN or 0 then) gives
 // scale NaN; v * NaN is then code 0 as an integer and NaN as a float.
 template <typename OUT>
 __device__ __forceinline__ float row_scale(float top, float factor, float* inv) {
   constexpr float L = kLargestCode<OUT>;
-  if (top < 7.52316385e-37f) {
+  if (top < 7.7037198e-34f) {
     *inv = 0.f;
     return 0.f;
   }
@@ -93,31 +107,206 @@ __device__ __forceinline__ OUT to_code(float v) {
 // an infinite maximum counts as NaN (where no factor of the row turns it into one)
 __device__ __forceinline__ float finite_or_nan(float top) { return top < __int_as_float(0x7f800000) ? top : __int_as_float(0x7fffffff); }
 
-// ---- a row's sum and maximum over a block ----------------------------------------------------------------------
-// Two buffers in turn, so that one barrier is enough: whoever writes a buffer again has passed the barrier of the one between,
-// which the readers reach behind their reads.
+// ---- a row's sum and maximum over its team -----------------------------------------------------------------------
+// A team is blockDim.x threads, a power of two below 32 or whole warps, one of blockDim.y; every thread of it gets the team's sum and
+// maximum (of values >= 0).  All threads of a block's warps call it together.  Two buffers in turn, so that one barrier is enough: whoever
+// writes a buffer again has passed the barrier of the one between, which the readers reach behind their reads.
+constexpr int kMostTeams = 15;  // of several warps: each has a hardware barrier of its own
 struct RowSums {
-  float sum[2][32];
-  uint32_t top[2][32];
-  // every thread of the block gets the block's sum and maximum
-  __device__ __forceinline__ void reduce(float& s, uint32_t& t, int& turn) {
+  float sum[2][32], top[2][32];
+  template <bool SUM = true, bool TOP = true>
+  __device__ __forceinline__ void reduce(float& s, float& t, int& turn) {
+    auto over = [&](int lanes) {
+      for (int i = lanes >> 1; i > 0; i >>= 1) {
+        if (SUM) s += __shfl_xor_sync(~0u, s, i);
+        if (TOP) t = max_abs(t, __shfl_xor_sync(~0u, t, i), 0.f);
+      }
+    };
+    auto over_warp = [&] {
+      if (SUM) {
 #pragma unroll
-    for (int i = 16; i > 0; i >>= 1) s += __shfl_xor_sync(~0u, s, i);
-    t = __reduce_max_sync(~0u, t);
+        for (int i = 16; i > 0; i >>= 1) s += __shfl_xor_sync(~0u, s, i);
+      }
+      if (TOP) asm volatile("redux.sync.max.abs.NaN.f32 %0, %0, 0xffffffff;" : "+f"(t));
+    };
+    if (blockDim.x < 32) return over(blockDim.x);
+    over_warp();
     const int warps = blockDim.x >> 5;
     if (warps == 1) return;
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, first = threadIdx.y * warps;
     if (lane == 0) {
-      sum[turn][threadIdx.x >> 5] = s;
-      top[turn][threadIdx.x >> 5] = t;
+      if (SUM) sum[turn][first + (threadIdx.x >> 5)] = s;
+      if (TOP) top[turn][first + (threadIdx.x >> 5)] = t;
     }
-    __syncthreads();
-    s = lane < warps ? sum[turn][lane] : 0.f;
-    t = lane < warps ? top[turn][lane] : 0u;
+    asm volatile("bar.sync %0, %1;" ::"r"(threadIdx.y + 1), "r"(blockDim.x) : "memory");
+    if (SUM) s = lane < warps ? sum[turn][first + lane] : 0.f;
+    if (TOP) t = lane < warps ? top[turn][first + lane] : 0.f;
     turn ^= 1;
+    over_warp();
+  }
+};
+
+// ---- pairs: two FP32 operations of one instruction, each rounded by itself --------------------------------------------------
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  asm("{ .reg .b64 x, y; mov.b64 x, {%0, %1}; mov.b64 y, {%2, %3}; mul.rn.f32x2 x, x, y; mov.b64 {%0, %1}, x; }" : "+f"(a.x), "+f"(a.y) : "f"(b.x), "f"(b.y));
+  return a;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  asm("{ .reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mov.b64 z, {%0, %1}; fma.rn.f32x2 z, x, y, z; mov.b64 {%0, %1}, z; }"
+      : "+f"(c.x), "+f"(c.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return c;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// ---- rows in registers --------------------------------------------------------------------------------------------
+// A thread has V vectors of a row, number threadIdx.x + v * blockDim.x: 16 bytes of the type T that the operator works on, N elements, N / 2
+// pairs.
+template <typename T>
+constexpr int kVector = 16 / sizeof(T);
+template <typename T>
+using Pairs = float2[kVector<T> / 2];
+
+template <typename T>
+__device__ __forceinline__ void unpack(const uint4& w, Pairs<T>& f) {
+  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+  if constexpr (sizeof(T) == 4) {
+    f[0] = make_float2(__uint_as_float(w.x), __uint_as_float(w.y));
+    f[1] = make_float2(__uint_as_float(w.z), __uint_as_float(w.w));
+  } else {
 #pragma unroll
-    for (int i = 16; i > 0; i >>= 1) s += __shfl_xor_sync(~0u, s, i);
-    t = __reduce_max_sync(~0u, t);
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (std::is_same_v<T, __half>) f[i] = __half22float2(*reinterpret_cast<const __half2*>(&x[i]));
+      else f[i] = make_float2(__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xffff0000u));
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack(const Pairs<T>& f) {
+  if constexpr (sizeof(T) == 4) {
+    return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y));
+  } else {
+    uint32_t x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (std::is_same_v<T, __half>) {
+        const __half2 v = __float22half2_rn(f[i]);
+        x[i] = *reinterpret_cast<const uint32_t*>(&v);
+      } else {
+        const __nv_bfloat162 v = __float22bfloat162_rn(f[i]);
+        x[i] = *reinterpret_cast<const uint32_t*>(&v);
+      }
+    }
+    return make_uint4(x[0], x[1], x[2], x[3]);
+  }
+}
+// a + b element by element, rounded to T
+template <typename T>
+__device__ __forceinline__ uint4 add_packed(const uint4& a, const uint4& b) {
+  const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+  uint32_t z[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      z[i] = __float_as_uint(__uint_as_float(x[i]) + __uint_as_float(y[i]));
+    } else if constexpr (std::is_same_v<T, __half>) {
+      const __half2 v = __hadd2(*reinterpret_cast<const __half2*>(&x[i]), *reinterpret_cast<const __half2*>(&y[i]));
+      z[i] = *reinterpret_cast<const uint32_t*>(&v);
+    } else {
+      const __nv_bfloat162 v = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&x[i]), *reinterpret_cast<const __nv_bfloat162*>(&y[i]));
+      z[i] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+  }
+  return make_uint4(z[0], z[1], z[2], z[3]);
+}
+
+// Vector i of a row of K elements; what lies behind the row's end is 0.  `whole`: its vectors lie at 16-byte boundaries.  WHOLE: those of
+// all rows do, and K is a number of vectors.
+template <bool WHOLE, typename T>
+__device__ __forceinline__ uint4 load_vector(const T* row, int i, int K, bool whole) {
+  constexpr int N = kVector<T>;
+  if (WHOLE) return i * N < K ? __ldcs(reinterpret_cast<const uint4*>(row) + i) : make_uint4(0, 0, 0, 0);
+  if (whole && (i + 1) * N <= K) return __ldcs(reinterpret_cast<const uint4*>(row) + i);
+  uint4 w = make_uint4(0, 0, 0, 0);
+  T* e = reinterpret_cast<T*>(&w);
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+    if (i * N + n < K) e[n] = row[i * N + n];
+  return w;
+}
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void store_vector(T* row, int i, int K, bool whole, const uint4& w) {
+  constexpr int N = kVector<T>;
+  if (WHOLE) {
+    if (i * N < K) reinterpret_cast<uint4*>(row)[i] = w;
+    return;
+  }
+  if (whole && (i + 1) * N <= K) {
+    reinterpret_cast<uint4*>(row)[i] = w;
+    return;
+  }
+  const T* e = reinterpret_cast<const T*>(&w);
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+    if (i * N + n < K) row[i * N + n] = e[n];
+}
+// N codes, in `whole` rows at boundaries of N bytes
+template <bool WHOLE, typename OUT, int PAIRS>
+__device__ __forceinline__ void store_codes(OUT* row, int i, int K, bool whole, const float2 (&f)[PAIRS]) {
+  constexpr int N = 2 * PAIRS;
+  uint32_t w[N / 4];
+#pragma unroll
+  for (int n = 0; n < N / 4; ++n) {
+    const float2 lo = f[2 * n], hi = f[2 * n + 1];
+    if constexpr (std::is_same_v<OUT, int8_t>) {  // (NaN: 0.  The lower end is -127, |v| <= 127 (1 + 2^-22): only its rounding has to be clamped, above.)
+      asm("cvt.pack.sat.s8.s32.b32 %0, %1, %2, 0;" : "=r"(w[n]) : "r"(__float2int_rn(hi.y)), "r"(__float2int_rn(hi.x)));
+      asm("cvt.pack.sat.s8.s32.b32 %0, %1, %2, %0;" : "+r"(w[n]) : "r"(__float2int_rn(lo.y)), "r"(__float2int_rn(lo.x)));
+    } else {
+      constexpr __nv_fp8_interpretation_t kind = std::is_same_v<OUT, __nv_fp8_e4m3> ? __NV_E4M3 : __NV_E5M2;
+      w[n] = __nv_cvt_float2_to_fp8x2(lo, __NV_SATFINITE, kind) | (uint32_t)__nv_cvt_float2_to_fp8x2(hi, __NV_SATFINITE, kind) << 16;
+    }
+  }
+  if (WHOLE ? i * N < K : whole && (i + 1) * N <= K) {
+    if constexpr (N == 8) reinterpret_cast<uint2*>(row)[i] = make_uint2(w[0], w[1]);
+    else reinterpret_cast<uint32_t*>(row)[i] = w[0];
+    return;
+  }
+  if (WHOLE) return;
+  const OUT* e = reinterpret_cast<const OUT*>(w);
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+    if (i * N + n < K) row[i * N + n] = e[n];
+}
+
+// Whether the rows start at `bytes` boundaries (an absent matrix does).
+inline bool whole_rows(const void* base, int64_t rows, int64_t ld, size_t es, size_t bytes) {
+  return aligned(base, bytes) && (rows <= 1 || (size_t)ld * es % bytes == 0);
+}
+
+// Teams, blocks and vectors to a thread for rows that a team holds in registers: a block to an SM, as many teams to a block as its threads
+// and the SM's rows allow.  Each thread has two vectors on their way where there are rows enough, one where most SMs have a row or two;
+// four in the longest rows.  (Registers: 1024 threads with one vector, 768 with two, 512 with four.)
+constexpr int team_threads(int v) { return v == 1 ? 1024 : v == 2 ? 768 : 512; }
+constexpr int64_t kMostTeamVectors = 4 * team_threads(4);
+struct TeamLaunch {
+  dim3 grid, block;
+  int v;
+  TeamLaunch(int64_t rows, int64_t vectors) {
+    const int64_t sms = sm_count();
+    v = vectors > 2 * team_threads(2) ? 4 : vectors > team_threads(1) || rows > 2 * sms ? 2 : 1;
+    const int64_t lanes = (vectors + v - 1) / v;
+    int64_t team = (lanes + 31) / 32 * 32;
+    if (lanes < 32)
+      for (team = 4; team < lanes; team *= 2) {
+      }
+    int64_t teams = team_threads(v) / team;
+    if (team > 32 && teams > kMostTeams) teams = kMostTeams;
+    const int64_t each = (rows + sms - 1) / sms, whole_warp = team < 32 ? 32 / team : 1;  // rows of an SM; teams of a warp
+    if (teams > each) teams = (each + whole_warp - 1) / whole_warp * whole_warp;
+    block = dim3((unsigned)team, (unsigned)teams);
+    int64_t blocks = (rows + teams - 1) / teams;
+    if (blocks > sms) blocks = sms;
+    grid = dim3((unsigned)blocks);
   }
 };
 
