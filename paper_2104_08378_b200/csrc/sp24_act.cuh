@@ -85,4 +85,14 @@ inline auto with_act(int act, F&& f) {
   }
 }
 
+// the same on the device, for an activation that all threads share
+template <typename F>
+__device__ __forceinline__ void device_with_act(int act, F&& f) {
+  if (act == SP24_ACT_SILU) f(Act<SP24_ACT_SILU>{});
+  else if (act == SP24_ACT_GELU) f(Act<SP24_ACT_GELU>{});
+  else if (act == SP24_ACT_GELU_TANH) f(Act<SP24_ACT_GELU_TANH>{});
+  else if (act == SP24_ACT_RELU) f(Act<SP24_ACT_RELU>{});
+  else f(Act<SP24_ACT_NONE>{});
+}
+
 }  // namespace sp24

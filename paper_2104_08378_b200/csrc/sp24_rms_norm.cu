@@ -114,40 +114,66 @@ __global__ void __launch_bounds__(team_threads(V), 1) rms_norm_rows_kernel(const
   }
 }
 
-// Rows of any length and alignment: a block to a row, two passes over it (the second from the caches).  The scale of an 8-bit row needs no
-// pass of its own: max |n| = rstd max |h w|.
+// Longer rows: a block to a row, two passes over it (the second from the caches).
 template <typename T, typename OUT>
-__global__ void __launch_bounds__(1024) rms_norm_kernel(const NormParams p) {
+__global__ void __launch_bounds__(1024, 1) rms_norm_kernel(const NormParams p) {
+  constexpr int P = kVector<T> / 2;
   __shared__ RowSums sums;
   int turn = 0;
+  const int K = (int)p.K, vectors = (K + kVector<T> - 1) / kVector<T>;
   wait_for_stream();
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     const T* x = static_cast<const T*>(p.x) + row * p.ldx;
     const T* r = p.residual ? static_cast<const T*>(p.residual) + row * p.ldr : nullptr;
     T* h = p.h ? static_cast<T*>(p.h) + row * p.ldh : nullptr;
     OUT* y = static_cast<OUT*>(p.y) + row * p.ldy;
-    auto weight = [&](int64_t k) { return p.weight ? load_weight<T>(p.weight, p.weight_f32, k) : 1.f; };
-    auto value = [&](int64_t k) { return r ? to_float(round_to<T>(to_float(x[k]) + to_float(r[k]))) : to_float(x[k]); };
-    float sum = 0.f;
+    auto value = [&](int i) {
+      const uint4 a = load_vector<false>(x, i, K, p.whole_x);
+      return r ? add_packed<T>(a, load_vector<false>(r, i, K, p.whole_r)) : a;
+    };
+    auto weighted = [&](int i, Pairs<T>& f) {
+#pragma unroll
+      for (int n = 0; n < P; ++n) {
+        const int k = i * kVector<T> + 2 * n;
+        if (p.weight && k < K) f[n].x *= load_weight<T>(p.weight, p.weight_f32, k);
+        if (p.weight && k + 1 < K) f[n].y *= load_weight<T>(p.weight, p.weight_f32, k + 1);
+      }
+    };
+    float2 sum2 = both(0.f);
     float top = 0.f;
-    for (int64_t k = threadIdx.x; k < p.K; k += blockDim.x) {
-      const float v = value(k);
-      sum = fmaf(v, v, sum);
-      if (is_code<OUT>) top = max_abs(top, v * weight(k), 0.f);
+#pragma unroll 2
+    for (int i = threadIdx.x; i < vectors; i += blockDim.x) {
+      Pairs<T> f;
+      unpack<T>(value(i), f);
+#pragma unroll
+      for (int n = 0; n < P; ++n) sum2 = fma2(f[n], f[n], sum2);
+      if (is_code<OUT>) {
+        weighted(i, f);
+#pragma unroll
+        for (int n = 0; n < P; ++n) top = max_abs(top, f[n].x, f[n].y);
+      }
     }
+    float sum = sum2.x + sum2.y;
     sums.reduce(sum, top, turn);
     const float rstd = rsqrtf(sum / (float)p.K + p.eps);
     if (threadIdx.x == 0 && p.rstd) p.rstd[row] = rstd;
-    float inv = 0.f;
+    float factor = rstd;
     if (is_code<OUT>) {
-      const float scale = row_scale<OUT>(top, rstd, &inv);
+      const float scale = row_scale<OUT>(top, rstd, &factor);
       if (threadIdx.x == 0) p.scale[row] = scale;
     }
-    for (int64_t k = threadIdx.x; k < p.K; k += blockDim.x) {
-      const float v = value(k);
-      if (h) h[k] = round_to<T>(v);
-      if constexpr (is_code<OUT>) y[k] = to_code<OUT>(v * weight(k) * inv);
-      else y[k] = round_to<OUT>(v * rstd * weight(k));
+#pragma unroll 2
+    for (int i = threadIdx.x; i < vectors; i += blockDim.x) {
+      const uint4 v = value(i);
+      Pairs<T> f;
+      unpack<T>(v, f);
+      if (is_code<OUT>) weighted(i, f);
+#pragma unroll
+      for (int n = 0; n < P; ++n) f[n] = mul2(f[n], both(factor));
+      if (!is_code<OUT>) weighted(i, f);
+      if (h) store_vector<false>(h, i, K, p.whole_h, v);
+      if constexpr (is_code<OUT>) store_codes<false, OUT>(y, i, K, p.whole_y, f);
+      else store_vector<false>(y, i, K, p.whole_y, pack<T>(f));
     }
   }
 }
@@ -160,7 +186,121 @@ struct NormGradParams {
   float* partial;  // gridDim.x rows of K: each block's part of dweight, or null
   int64_t lddy, ldh, lddh, lddx;
   int32_t weight_f32;
+  bool whole_dy, whole_h, whole_dh, whole_dx, whole_w;
 };
+
+// Rows of up to kMostTeamVectors vectors: a team of threads to a row, with the weight and the team's part of dweight in registers for all
+// its rows, the next one on its way.  At the end the teams of a block add their parts up in their order.
+template <typename T, typename W, int V, bool WHOLE>
+__global__ void __launch_bounds__(team_threads(V), 1) rms_norm_grad_rows_kernel(const NormGradParams p) {
+  constexpr int P = kVector<T> / 2, kWords = sizeof(W) / sizeof(T), PW = kVector<W> / 2;
+  __shared__ RowSums sums;
+  extern __shared__ float part[];  // K floats, if there is more than one team
+  int turn = 0;
+  const int tx = threadIdx.x, team = blockDim.x, K = (int)p.K;
+  const int64_t step = (int64_t)gridDim.x * blockDim.y;
+  const float over_k = 1.f / (float)p.K;
+  wait_for_stream();
+  uint4 dy[V] = {}, h[V] = {}, w[V][kWords];
+  float rstd = 0.f;
+  auto fetch = [&](const void* from, int64_t ld, bool whole, int64_t row, uint4 (&to)[V]) {
+    const T* at = static_cast<const T*>(from) + row * ld;
+#pragma unroll
+    for (int v = 0; v < V; ++v) to[v] = load_vector<WHOLE>(at, tx + v * team, K, whole);
+  };
+  auto fetch_row = [&](int64_t row) {
+    if (row >= p.rows) return;
+    fetch(p.dy, p.lddy, p.whole_dy, row, dy);
+    fetch(p.h, p.ldh, p.whole_h, row, h);
+    rstd = p.rstd[row];
+  };
+  int64_t base = (int64_t)blockIdx.x * blockDim.y;  // the first team's row: the warps of a block stay together
+  fetch_row(base + threadIdx.y);
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      Pairs<W> one;
+#pragma unroll
+      for (int n = 0; n < PW; ++n) one[n] = both(1.f);
+      w[v][i] = p.weight ? load_vector<WHOLE>(static_cast<const W*>(p.weight), (tx + v * team) * kWords + i, K, p.whole_w) : pack<W>(one);
+    }
+  auto weighted = [&](int v, Pairs<T>& f) {  // f times the weights
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      Pairs<W> g;
+      unpack<W>(w[v][i], g);
+#pragma unroll
+      for (int n = 0; n < PW; ++n) f[i * PW + n] = mul2(f[i * PW + n], g[n]);
+    }
+  };
+  Pairs<T> acc[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int n = 0; n < P; ++n) acc[v][n] = both(0.f);
+  for (; base < p.rows; base += step) {
+    const int64_t row = base + threadIdx.y;
+    const bool live = row < p.rows;
+    const float r = rstd;
+    uint4 dh[V] = {};
+    if (live && p.dh) fetch(p.dh, p.lddh, p.whole_dh, row, dh);
+    float2 sum2 = both(0.f);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      Pairs<T> g, f;
+      unpack<T>(dy[v], g);
+      unpack<T>(h[v], f);
+#pragma unroll
+      for (int n = 0; n < P; ++n) {
+        const float2 s = mul2(g[n], f[n]);
+        if (live) acc[v][n] = fma2(s, both(r), acc[v][n]);
+      }
+      weighted(v, g);
+#pragma unroll
+      for (int n = 0; n < P; ++n) sum2 = fma2(g[n], f[n], sum2);
+    }
+    float sum = sum2.x + sum2.y, unused = 0.f;
+    sums.reduce<true, false>(sum, unused, turn);
+    const float along = -sum * over_k * r * r;
+    T* dx = static_cast<T*>(p.dx) + row * p.lddx;
+    uint4 out[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      Pairs<T> g, f, d;
+      unpack<T>(dy[v], g);
+      unpack<T>(h[v], f);
+      unpack<T>(dh[v], d);
+      weighted(v, g);
+#pragma unroll
+      for (int n = 0; n < P; ++n) g[n] = fma2(fma2(f[n], both(along), g[n]), both(r), d[n]);
+      out[v] = pack<T>(g);
+    }
+    fetch_row(row + step);
+    if (live) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) store_vector<WHOLE>(dx, tx + v * team, K, p.whole_dx, out[v]);
+    }
+  }
+  if (!p.partial) return;
+  float* to = p.partial + (int64_t)blockIdx.x * p.K;
+  for (int t = 0; t < (int)blockDim.y; ++t) {
+    if (t == (int)threadIdx.y) {
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int n = 0; n < 2 * P; ++n) {
+          const int k = (tx + v * team) * 2 * P + n;
+          if (k >= K) continue;
+          float s = n & 1 ? acc[v][n / 2].y : acc[v][n / 2].x;
+          if (t) s += part[k];
+          if (t + 1 < (int)blockDim.y) part[k] = s;
+          else to[k] = s;
+        }
+    }
+    if (blockDim.y > 1) __syncthreads();
+  }
+}
 
 template <typename T>
 __global__ void __launch_bounds__(1024) rms_norm_grad_kernel(const NormGradParams p) {
@@ -263,7 +403,7 @@ extern "C" sp24_status sp24_rms_norm(sp24_dtype t, int64_t rows, int64_t K, cons
         };
         return weight && weight_type == SP24_F32 ? launch(TypeOf<float>{}) : launch(TypeOf<T>{});
       }
-      return launch_overlapped(rms_norm_kernel<T, OUT>, dim3((unsigned)(rows < 65535 ? rows : 65535)), dim3(row_threads(K)), 0,
+      return launch_overlapped(rms_norm_kernel<T, OUT>, dim3((unsigned)(rows < 65535 ? rows : 65535)), dim3(1024), 0,
                                static_cast<cudaStream_t>(stream), 1, p);
     });
   });
@@ -297,10 +437,26 @@ extern "C" sp24_status sp24_rms_norm_backward(sp24_dtype t, int64_t rows, int64_
                  SP24_ERR_WORKSPACE);
   sp24_status st = check_arch();
   if (st != SP24_OK) return st;
-  const int64_t blocks = grad_blocks(rows);
-  const NormGradParams p = {rows, K, dy, h, weight, dh, rstd, dx, dweight ? static_cast<float*>(workspace) : nullptr, lddy, ldh, lddh, lddx, weight_type == SP24_F32};
+  int64_t blocks = grad_blocks(rows);
+  const NormGradParams p = {rows, K, dy, h, weight, dh, rstd, dx, dweight ? static_cast<float*>(workspace) : nullptr, lddy, ldh, lddh, lddx, weight_type == SP24_F32,
+                            whole_rows(dy, rows, lddy, es, 16), whole_rows(h, rows, ldh, es, 16), !dh || whole_rows(dh, rows, lddh, es, 16),
+                            whole_rows(dx, rows, lddx, es, 16), aligned(weight, 16)};
+  const int64_t vectors = (K * (int64_t)es + 15) / 16;
+  const bool whole = p.whole_dy && p.whole_h && p.whole_dh && p.whole_dx && p.whole_w && K * es % 16 == 0;
   st = with_float_type(t, [&](auto type) {
     using T = typename decltype(type)::type;
+    if (vectors <= kMostTeamVectors) {
+      TeamLaunch at(rows, vectors);
+      if (at.grid.x > blocks) at.grid.x = (unsigned)blocks;
+      blocks = at.grid.x;
+      auto launch = [&](auto weight_t) {
+        using W = typename decltype(weight_t)::type;
+        const auto kernel = with_flags([](auto four, auto two, auto whole) { return rms_norm_grad_rows_kernel<T, W, four.value ? 4 : two.value ? 2 : 1, whole.value>; },
+                                       at.v == 4, at.v >= 2, whole);
+        return launch_overlapped(kernel, at.grid, at.block, at.block.y > 1 && dweight ? (size_t)K * sizeof(float) : 0, s, 1, p);
+      };
+      return weight && weight_type == SP24_F32 ? launch(TypeOf<float>{}) : launch(TypeOf<T>{});
+    }
     return launch_overlapped(rms_norm_grad_kernel<T>, dim3((unsigned)blocks), dim3(row_threads(K)), 0, s, 1, p);
   });
   if (st != SP24_OK || !dweight) return st;
