@@ -190,32 +190,39 @@ struct NormGradParams {
 };
 
 // Rows of up to kMostTeamVectors vectors: a team of threads to a row, with the weight and the team's part of dweight in registers for all
-// its rows, the next one on its way.  At the end the teams of a block add their parts up in their order.
-template <typename T, typename W, int V, bool WHOLE>
-__global__ void __launch_bounds__(team_threads(V), 1) rms_norm_grad_rows_kernel(const NormGradParams p) {
+// its rows.  AHEAD: the team's next row is on its way from before this one's work to the end of it, in registers of its own (two sets in
+// turn).  At the end the block adds its teams' parts up, in an order that their number fixes.
+constexpr int kAheadThreads = 512;
+template <typename T, typename W, int V, bool AHEAD, bool WHOLE>
+__global__ void __launch_bounds__(AHEAD ? kAheadThreads : team_threads(V), 1) rms_norm_grad_rows_kernel(const NormGradParams p) {
   constexpr int P = kVector<T> / 2, kWords = sizeof(W) / sizeof(T), PW = kVector<W> / 2;
   __shared__ RowSums sums;
-  extern __shared__ float part[];  // K floats, if there is more than one team
+  extern __shared__ float4 parts[];  // K rounded up to vectors, a row for each team of whole warps or for each warp
   int turn = 0;
   const int tx = threadIdx.x, team = blockDim.x, K = (int)p.K;
   const int64_t step = (int64_t)gridDim.x * blockDim.y;
   const float over_k = 1.f / (float)p.K;
   wait_for_stream();
-  uint4 dy[V] = {}, h[V] = {}, w[V][kWords];
-  float rstd = 0.f;
+  struct Row {
+    uint4 dy[V], h[V], dh[V];
+    float rstd;
+  };
   auto fetch = [&](const void* from, int64_t ld, bool whole, int64_t row, uint4 (&to)[V]) {
     const T* at = static_cast<const T*>(from) + row * ld;
 #pragma unroll
     for (int v = 0; v < V; ++v) to[v] = load_vector<WHOLE>(at, tx + v * team, K, whole);
   };
-  auto fetch_row = [&](int64_t row) {
+  auto fetch_row = [&](int64_t row, Row& to) {
     if (row >= p.rows) return;
-    fetch(p.dy, p.lddy, p.whole_dy, row, dy);
-    fetch(p.h, p.ldh, p.whole_h, row, h);
-    rstd = p.rstd[row];
+    to.rstd = p.rstd[row];
+    fetch(p.dy, p.lddy, p.whole_dy, row, to.dy);
+    fetch(p.h, p.ldh, p.whole_h, row, to.h);
+    if (p.dh) fetch(p.dh, p.lddh, p.whole_dh, row, to.dh);
   };
+  Row a = {}, b = {};
   int64_t base = (int64_t)blockIdx.x * blockDim.y;  // the first team's row: the warps of a block stay together
-  fetch_row(base + threadIdx.y);
+  fetch_row(base + threadIdx.y, a);
+  uint4 w[V][kWords];
 #pragma unroll
   for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -239,18 +246,16 @@ __global__ void __launch_bounds__(team_threads(V), 1) rms_norm_grad_rows_kernel(
   for (int v = 0; v < V; ++v)
 #pragma unroll
     for (int n = 0; n < P; ++n) acc[v][n] = both(0.f);
-  for (; base < p.rows; base += step) {
-    const int64_t row = base + threadIdx.y;
+  auto one_row = [&](int64_t row, Row& x, Row& next) {
     const bool live = row < p.rows;
-    const float r = rstd;
-    uint4 dh[V] = {};
-    if (live && p.dh) fetch(p.dh, p.lddh, p.whole_dh, row, dh);
+    if (AHEAD) fetch_row(row + step, next);
+    const float r = x.rstd;
     float2 sum2 = both(0.f);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       Pairs<T> g, f;
-      unpack<T>(dy[v], g);
-      unpack<T>(h[v], f);
+      unpack<T>(x.dy[v], g);
+      unpack<T>(x.h[v], f);
 #pragma unroll
       for (int n = 0; n < P; ++n) {
         const float2 s = mul2(g[n], f[n]);
@@ -268,37 +273,64 @@ __global__ void __launch_bounds__(team_threads(V), 1) rms_norm_grad_rows_kernel(
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       Pairs<T> g, f, d;
-      unpack<T>(dy[v], g);
-      unpack<T>(h[v], f);
-      unpack<T>(dh[v], d);
+      unpack<T>(x.dy[v], g);
+      unpack<T>(x.h[v], f);
+      unpack<T>(x.dh[v], d);
       weighted(v, g);
 #pragma unroll
       for (int n = 0; n < P; ++n) g[n] = fma2(fma2(f[n], both(along), g[n]), both(r), d[n]);
       out[v] = pack<T>(g);
     }
-    fetch_row(row + step);
+    if (!AHEAD) fetch_row(row + step, x);
     if (live) {
 #pragma unroll
       for (int v = 0; v < V; ++v) store_vector<WHOLE>(dx, tx + v * team, K, p.whole_dx, out[v]);
     }
+  };
+  for (; base < p.rows; base += step) {
+    one_row(base + threadIdx.y, a, b);
+    if (AHEAD) {
+      base += step;
+      if (base < p.rows) one_row(base + threadIdx.y, b, a);
+    }
   }
   if (!p.partial) return;
-  float* to = p.partial + (int64_t)blockIdx.x * p.K;
-  for (int t = 0; t < (int)blockDim.y; ++t) {
-    if (t == (int)threadIdx.y) {
+  const int vectors = (K + 2 * P - 1) / (2 * P), thread = threadIdx.y * team + tx;
+  if (team < 32) {  // the teams of a warp: lanes `team` apart have the same columns
 #pragma unroll
-      for (int v = 0; v < V; ++v)
+    for (int v = 0; v < V; ++v)
 #pragma unroll
-        for (int n = 0; n < 2 * P; ++n) {
-          const int k = (tx + v * team) * 2 * P + n;
-          if (k >= K) continue;
-          float s = n & 1 ? acc[v][n / 2].y : acc[v][n / 2].x;
-          if (t) s += part[k];
-          if (t + 1 < (int)blockDim.y) part[k] = s;
-          else to[k] = s;
+      for (int n = 0; n < P; ++n)
+        for (int i = 16; i >= team; i >>= 1) {
+          acc[v][n].x += __shfl_xor_sync(~0u, acc[v][n].x, i);
+          acc[v][n].y += __shfl_xor_sync(~0u, acc[v][n].y, i);
         }
+  }
+  const int slots = team < 32 ? (int)blockDim.y * team / 32 : (int)blockDim.y, slot = team < 32 ? thread / 32 : (int)threadIdx.y;
+  constexpr int kQuads = P / 2;  // 16-byte groups of a vector's sums
+  if (team >= 32 || (thread & 31) < team) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int i = tx + v * team;
+#pragma unroll
+      for (int q = 0; q < kQuads; ++q)
+        if (i < vectors) parts[(slot * kQuads + q) * vectors + i] = make_float4(acc[v][2 * q].x, acc[v][2 * q].y, acc[v][2 * q + 1].x, acc[v][2 * q + 1].y);
     }
-    if (blockDim.y > 1) __syncthreads();
+  }
+  __syncthreads();
+  float* to = p.partial + (int64_t)blockIdx.x * p.K;
+  for (int c = thread; c < vectors * kQuads; c += team * blockDim.y) {
+    const int i = c / kQuads, q = c % kQuads;
+    float4 s = parts[q * vectors + i];
+    for (int t = 1; t < slots; ++t) {
+      const float4 o = parts[(t * kQuads + q) * vectors + i];
+      s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
+    }
+    const int k = i * 2 * P + q * 4;
+    if (k < K) to[k] = s.x;
+    if (k + 1 < K) to[k + 1] = s.y;
+    if (k + 2 < K) to[k + 2] = s.z;
+    if (k + 3 < K) to[k + 3] = s.w;
   }
 }
 
@@ -446,14 +478,19 @@ extern "C" sp24_status sp24_rms_norm_backward(sp24_dtype t, int64_t rows, int64_
   st = with_float_type(t, [&](auto type) {
     using T = typename decltype(type)::type;
     if (vectors <= kMostTeamVectors) {
-      TeamLaunch at(rows, vectors);
+      TeamLaunch at(rows, vectors, kAheadThreads);
       if (at.grid.x > blocks) at.grid.x = (unsigned)blocks;
       blocks = at.grid.x;
+      const int slots = at.block.x < 32 ? (int)(at.block.x * at.block.y / 32) : (int)at.block.y;
+      const size_t smem = dweight ? (size_t)slots * vectors * kVector<T> * sizeof(float) : 0;  // (at most 64 KB: V vectors for each thread)
       auto launch = [&](auto weight_t) {
         using W = typename decltype(weight_t)::type;
-        const auto kernel = with_flags([](auto four, auto two, auto whole) { return rms_norm_grad_rows_kernel<T, W, four.value ? 4 : two.value ? 2 : 1, whole.value>; },
-                                       at.v == 4, at.v >= 2, whole);
-        return launch_overlapped(kernel, at.grid, at.block, at.block.y > 1 && dweight ? (size_t)K * sizeof(float) : 0, s, 1, p);
+        const auto kernel = at.v == 2 && vectors <= 2 * kAheadThreads
+                                ? (whole ? rms_norm_grad_rows_kernel<T, W, 2, true, true> : rms_norm_grad_rows_kernel<T, W, 2, true, false>)
+                                : with_flags([](auto four, auto two, auto whole) { return rms_norm_grad_rows_kernel<T, W, four.value ? 4 : two.value ? 2 : 1, false, whole.value>; },
+                                             at.v == 4, at.v >= 2, whole);
+        if (smem > 48 * 1024 - sizeof(RowSums)) SP24_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        return launch_overlapped(kernel, at.grid, at.block, smem, s, 1, p);
       };
       return weight && weight_type == SP24_F32 ? launch(TypeOf<float>{}) : launch(TypeOf<T>{});
     }

@@ -291,15 +291,17 @@ constexpr int64_t kMostTeamVectors = 4 * team_threads(4);
 struct TeamLaunch {
   dim3 grid, block;
   int v;
-  TeamLaunch(int64_t rows, int64_t vectors) {
+  // with_two: threads of a block with two vectors each, where they suffice
+  TeamLaunch(int64_t rows, int64_t vectors, int with_two = team_threads(2)) {
     const int64_t sms = sm_count();
     v = vectors > 2 * team_threads(2) ? 4 : vectors > team_threads(1) || rows > 2 * sms ? 2 : 1;
+    const int64_t most = v == 2 && vectors <= 2 * with_two ? with_two : team_threads(v);
     const int64_t lanes = (vectors + v - 1) / v;
     int64_t team = (lanes + 31) / 32 * 32;
     if (lanes < 32)
       for (team = 4; team < lanes; team *= 2) {
       }
-    int64_t teams = team_threads(v) / team;
+    int64_t teams = most / team;
     if (team > 32 && teams > kMostTeams) teams = kMostTeams;
     const int64_t each = (rows + sms - 1) / sms, whole_warp = team < 32 ? 32 / team : 1;  // rows of an SM; teams of a warp
     if (teams > each) teams = (each + whole_warp - 1) / whole_warp * whole_warp;
