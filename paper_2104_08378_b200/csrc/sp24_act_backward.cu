@@ -1,6 +1,7 @@
 // Gradient of the activation between a product and what follows it: dz = dy * act'(z), in both orders (the two products of a linear
 // layer's gradient contract over different axes), and the bias's gradient, the sums of dz over tokens.
 #include "sp24_act.cuh"
+#include "sp24_ptx.cuh"
 #include "sp24_rows.cuh"
 
 namespace sp24 {
@@ -17,7 +18,93 @@ struct ActGradParams {
   int32_t over_rows;
 };
 
-// A block to a tile of 64 x 64, transposed through shared memory.
+// 16-bit types, all rows (of dzt too) whole vectors at 16-byte boundaries.  A block to a tile of 64 x 64, transposed on its way out of
+// shared memory by ldmatrix.trans: the eight rows of matrix i are 8 j + 2 i + b (j = 0..3, b = 0, 1), which leaves lane 4 c + j with eight
+// consecutive rows of column c, so that a warp stores eight segments of 64 bytes.  Unit u (16 bytes) of row m lies at
+// u ^ (2 (m >> 3 & 3) + (m & 1)): the eight rows of a matrix are in different banks.
+template <typename T, int ACT>
+__global__ void __launch_bounds__(256) act_grad_tile_kernel(const ActGradParams p) {
+  __shared__ uint4 tile[kTile * kTile / 8];
+  __shared__ float over[8][kTile];  // sums over the rows of each warp
+  const int64_t col_tiles = (p.cols + kTile - 1) / kTile;
+  const int64_t row0 = (int64_t)(blockIdx.x / col_tiles) * kTile, col0 = (int64_t)(blockIdx.x % col_tiles) * kTile;
+  const int u = threadIdx.x % 8, m0 = threadIdx.x / 8, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const int64_t c = col0 + 8 * u;
+  wait_for_stream();
+  uint4 dy[2] = {}, z[2] = {};
+#pragma unroll
+  for (int v = 0; v < 2; ++v)
+    if (const int64_t r = row0 + m0 + 32 * v; r < p.rows && c < p.cols) dy[v] = ld_stream(static_cast<const T*>(p.dy) + r * p.lddy + c);
+  if (ACT != SP24_ACT_NONE) {
+#pragma unroll
+    for (int v = 0; v < 2; ++v)
+      if (const int64_t r = row0 + m0 + 32 * v; r < p.rows && c < p.cols) z[v] = ld_stream(static_cast<const T*>(p.z) + r * p.ldz + c);
+  }
+  Pairs<T> sums = {};
+#pragma unroll
+  for (int v = 0; v < 2; ++v) {
+    const int m = m0 + 32 * v;
+    const int64_t r = row0 + m;
+    Pairs<T> d, f;
+    unpack<T>(dy[v], d);
+    unpack<T>(z[v], f);
+    if (ACT != SP24_ACT_NONE) {
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        float2 slope;
+        act_and_slope<ACT>(f[n].x, &slope.x);
+        act_and_slope<ACT>(f[n].y, &slope.y);
+        d[n] = mul2(d[n], slope);
+      }
+    }
+    const uint4 packed = pack<T>(d);
+    if (p.dz && r < p.rows && c < p.cols) *reinterpret_cast<uint4*>(static_cast<T*>(p.dz) + r * p.lddz + c) = packed;
+    tile[m * 8 + (u ^ (2 * (m >> 3 & 3) + (m & 1)))] = packed;
+    if (p.partial && p.over_rows) {
+#pragma unroll
+      for (int n = 0; n < 4; ++n) sums[n] = make_float2(sums[n].x + d[n].x, sums[n].y + d[n].y);
+    } else if (p.partial) {
+      float s = ((d[0].x + d[0].y) + (d[1].x + d[1].y)) + ((d[2].x + d[2].y) + (d[3].x + d[3].y));
+#pragma unroll
+      for (int i = 1; i < 8; i *= 2) s += __shfl_xor_sync(~0u, s, i);
+      if (u == 0 && r < p.rows) p.partial[col0 / kTile * p.rows + r] = s;
+    }
+  }
+  if (p.partial && p.over_rows) {
+#pragma unroll
+    for (int i = 8; i < 32; i *= 2)
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        sums[n].x += __shfl_xor_sync(~0u, sums[n].x, i);
+        sums[n].y += __shfl_xor_sync(~0u, sums[n].y, i);
+      }
+    if (lane < 8) {
+#pragma unroll
+      for (int n = 0; n < 4; ++n) *reinterpret_cast<float2*>(&over[warp][8 * u + 2 * n]) = sums[n];
+    }
+  }
+  __syncthreads();
+  if (p.dzt) {
+    const int i = lane >> 3, j = (lane & 7) >> 1, b = lane & 1;  // this lane's row of matrix i for ldmatrix
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int m32 = 32 * k, unit = warp;  // rows m32..m32 + 31, columns 8 unit..8 unit + 7
+      const int m = m32 + 8 * j + 2 * i + b;
+      uint32_t x[4];
+      ptx::ldmatrix_x4_trans(ptx::smem_u32(&tile[m * 8 + (unit ^ (2 * (m >> 3 & 3) + (m & 1)))]), x[0], x[1], x[2], x[3]);
+      const int64_t col = col0 + 8 * unit + (lane >> 2), r = row0 + m32 + 8 * (lane & 3);
+      if (col < p.cols && r < p.rows) *reinterpret_cast<uint4*>(static_cast<T*>(p.dzt) + col * p.lddzt + r) = make_uint4(x[0], x[1], x[2], x[3]);
+    }
+  }
+  if (p.partial && p.over_rows && threadIdx.x < kTile) {
+    float s = over[0][threadIdx.x];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) s += over[w][threadIdx.x];
+    if (col0 + threadIdx.x < p.cols) p.partial[row0 / kTile * p.cols + col0 + threadIdx.x] = s;
+  }
+}
+
+// Any type, size and alignment, element by element through shared memory.
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256) act_grad_kernel(const ActGradParams p) {
   __shared__ float tile[kTile][kTile + 1];
@@ -94,9 +181,14 @@ extern "C" sp24_status sp24_act_backward(sp24_dtype t, sp24_act act, int64_t row
   sp24_status st = check_arch();
   if (st != SP24_OK) return st;
   const ActGradParams p = {rows, cols, dy, z, dz, dzt, dbias ? static_cast<float*>(workspace) : nullptr, lddy, ldz, lddz, lddzt, sum_over_rows != 0};
+  const bool whole = t != SP24_F32 && cols % 8 == 0 && (!dzt || rows % 8 == 0) && whole_rows(dy, rows, lddy, 2, 16) &&
+                     (!reads_z || whole_rows(z, rows, ldz, 2, 16)) && (!dz || whole_rows(dz, rows, lddz, 2, 16)) &&
+                     (!dzt || whole_rows(dzt, cols, lddzt, 2, 16));
   st = with_float_type(t, [&](auto type) {
     using T = typename decltype(type)::type;
     return with_act(act, [&](auto a) {
+      if constexpr (sizeof(T) == 2)
+        if (whole) return launch_overlapped(act_grad_tile_kernel<T, decltype(a)::value>, dim3((unsigned)(row_tiles * col_tiles)), dim3(256), 0, s, 1, p);
       return launch_overlapped(act_grad_kernel<T, decltype(a)::value>, dim3((unsigned)(row_tiles * col_tiles)), dim3(256), 0, s, 1, p);
     });
   });

@@ -12,7 +12,6 @@ struct GatedParams {
   float* scale;
   int64_t ldg, ldu, ldy;
   int32_t act;
-  bool whole_g, whole_u, whole_y;  // rows at boundaries of vectors
 };
 
 // act(g) * u of a vector
@@ -37,7 +36,7 @@ __device__ __forceinline__ void gated_vector(int act, const uint4& g, const uint
 // exponentials and reciprocals take half as long as the memory does.
 template <typename T, typename OUT, int V, bool WHOLE>
 __global__ void __launch_bounds__(team_threads(V), 1) gated_act_rows_kernel(const GatedParams p) {
-  constexpr int P = kVector<T> / 2;
+  constexpr int N = kVector<T>, P = N / 2;
   __shared__ RowSums sums;
   int turn = 0;
   const int tx = threadIdx.x, team = blockDim.x, F = (int)p.F;
@@ -47,19 +46,21 @@ __global__ void __launch_bounds__(team_threads(V), 1) gated_act_rows_kernel(cons
   struct Row {
     uint4 g[V], u[V];
   };
+  auto shift = [&](int64_t row) { return WHOLE ? 0 : shift_of<OUT, N>(static_cast<const OUT*>(p.y) + row * p.ldy); };
   auto fetch = [&](int64_t row, Row& to) {
     if (row >= p.rows) return;
+    const int s = shift(row);
     const T* pg = static_cast<const T*>(p.g) + row * p.ldg;
     const T* pu = static_cast<const T*>(p.u) + row * p.ldu;
 #pragma unroll
-    for (int v = 0; v < V; ++v) to.g[v] = load_vector<WHOLE>(pg, tx + v * team, F, p.whole_g);
+    for (int v = 0; v < V; ++v) to.g[v] = load_vector<WHOLE>(pg, tx + v * team, F, s);
     if (gated) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) to.u[v] = load_vector<WHOLE>(pu, tx + v * team, F, p.whole_u);
+      for (int v = 0; v < V; ++v) to.u[v] = load_vector<WHOLE>(pu, tx + v * team, F, s);
     }
   };
   auto one_row = [&](int64_t row, const Row& x, Row& next) {
-    const int K = row < p.rows ? F : 0;
+    const int K = row < p.rows ? F : 0, s = row < p.rows ? shift(row) : 0;
     fetch(row + step, next);
     Pairs<T> y[V];
     float top = 0.f, unused = 0.f, inv = 0.f;
@@ -82,9 +83,9 @@ __global__ void __launch_bounds__(team_threads(V), 1) gated_act_rows_kernel(cons
       if constexpr (is_code<OUT>) {
 #pragma unroll
         for (int n = 0; n < P; ++n) y[v][n] = mul2(y[v][n], both(inv));
-        store_codes<WHOLE, OUT>(py, tx + v * team, K, p.whole_y, y[v]);
+        store_codes<WHOLE, OUT>(py, tx + v * team, K, s, y[v]);
       } else {
-        store_vector<WHOLE>(py, tx + v * team, K, p.whole_y, pack<T>(y[v]));
+        store_vector<WHOLE>(py, tx + v * team, K, s, pack<T>(y[v]));
       }
     }
   };
@@ -103,15 +104,16 @@ __global__ void __launch_bounds__(1024, 1) gated_act_kernel(const GatedParams p)
   constexpr int P = kVector<T> / 2;
   __shared__ RowSums sums;
   int turn = 0;
-  const int K = (int)p.F, vectors = (K + kVector<T> - 1) / kVector<T>;
+  const int K = (int)p.F;
   wait_for_stream();
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     const T* g = static_cast<const T*>(p.g) + row * p.ldg;
     const T* u = p.u ? static_cast<const T*>(p.u) + row * p.ldu : nullptr;
     OUT* y = static_cast<OUT*>(p.y) + row * p.ldy;
+    const int shift = shift_of<OUT, kVector<T>>(y), vectors = (shift + K + kVector<T> - 1) / kVector<T>;
     auto value = [&](int i, Pairs<T>& f) {
-      const uint4 a = load_vector<false>(g, i, K, p.whole_g);
-      gated_vector<T>(p.act, a, u ? load_vector<false>(u, i, K, p.whole_u) : a, u != nullptr, f);
+      const uint4 a = load_vector<false>(g, i, K, shift);
+      gated_vector<T>(p.act, a, u ? load_vector<false>(u, i, K, shift) : a, u != nullptr, f);
     };
     float inv = 0.f;
     if (is_code<OUT>) {
@@ -134,9 +136,9 @@ __global__ void __launch_bounds__(1024, 1) gated_act_kernel(const GatedParams p)
       if constexpr (is_code<OUT>) {
 #pragma unroll
         for (int n = 0; n < P; ++n) f[n] = mul2(f[n], both(inv));
-        store_codes<false, OUT>(y, i, K, p.whole_y, f);
+        store_codes<false, OUT>(y, i, K, shift, f);
       } else {
-        store_vector<false>(y, i, K, p.whole_y, pack<T>(f));
+        store_vector<false>(y, i, K, shift, pack<T>(f));
       }
     }
   }
@@ -147,20 +149,48 @@ struct GatedGradParams {
   const void *dy, *g, *u;
   void *dg, *du;
   int64_t lddy, ldg, ldu, lddg, lddu;
+  int32_t act;
 };
 
-template <typename T, int ACT>
-__global__ void __launch_bounds__(256) gated_act_grad_kernel(const GatedGradParams p) {
+// Element by element: two vectors to a thread, all their loads before the first use.
+template <typename T, bool WHOLE>
+__global__ void __launch_bounds__(kThreads) gated_act_grad_kernel(const GatedGradParams p) {
+  constexpr int P = kVector<T> / 2, V = 2;
+  const int tx = threadIdx.x, F = (int)p.F, i0 = blockIdx.x * (V * blockDim.x) + tx;
+  const bool gated = p.u != nullptr;
   wait_for_stream();
-  for (int64_t row = blockIdx.y; row < p.rows; row += gridDim.y) {
-    const T* dy = static_cast<const T*>(p.dy) + row * p.lddy;
-    const T* g = static_cast<const T*>(p.g) + row * p.ldg;
-    for (int64_t k = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; k < p.F; k += (int64_t)gridDim.x * blockDim.x) {
-      float slope, d = to_float(dy[k]);
-      const float value = act_and_slope<ACT>(to_float(g[k]), &slope);
-      const float w = p.u ? to_float(static_cast<const T*>(p.u)[row * p.ldu + k]) : 1.f;
-      static_cast<T*>(p.dg)[row * p.lddg + k] = round_to<T>(d * w * slope);
-      if (p.du) static_cast<T*>(p.du)[row * p.lddu + k] = round_to<T>(d * value);
+  for (int64_t base = (int64_t)blockIdx.y * blockDim.y; base < p.rows; base += (int64_t)gridDim.y * blockDim.y) {
+    const int64_t row = base + threadIdx.y;
+    if (row >= p.rows) break;
+    const int s = WHOLE ? 0 : shift_of<T, kVector<T>>(static_cast<const T*>(p.dg) + row * p.lddg);
+    uint4 dy[V], g[V], u[V] = {};
+#pragma unroll
+    for (int v = 0; v < V; ++v) dy[v] = load_vector<WHOLE>(static_cast<const T*>(p.dy) + row * p.lddy, i0 + v * (int)blockDim.x, F, s);
+#pragma unroll
+    for (int v = 0; v < V; ++v) g[v] = load_vector<WHOLE>(static_cast<const T*>(p.g) + row * p.ldg, i0 + v * (int)blockDim.x, F, s);
+    if (gated) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) u[v] = load_vector<WHOLE>(static_cast<const T*>(p.u) + row * p.ldu, i0 + v * (int)blockDim.x, F, s);
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int i = i0 + v * (int)blockDim.x;
+      Pairs<T> d, f, w, dg, du;
+      unpack<T>(dy[v], d);
+      unpack<T>(g[v], f);
+      unpack<T>(u[v], w);
+      device_with_act(p.act, [&](auto a) {
+#pragma unroll
+        for (int n = 0; n < P; ++n) {
+          float2 slope;
+          du[n].x = act_and_slope<decltype(a)::value>(f[n].x, &slope.x);
+          du[n].y = act_and_slope<decltype(a)::value>(f[n].y, &slope.y);
+          dg[n] = mul2(gated ? mul2(d[n], w[n]) : d[n], slope);
+          du[n] = mul2(du[n], d[n]);
+        }
+      });
+      store_vector<WHOLE>(static_cast<T*>(p.dg) + row * p.lddg, i, F, s, pack<T>(dg));
+      if (gated) store_vector<WHOLE>(static_cast<T*>(p.du) + row * p.lddu, i, F, s, pack<T>(du));
     }
   }
 }
@@ -183,10 +213,9 @@ extern "C" sp24_status sp24_gated_act(sp24_dtype t, sp24_act act, int64_t rows, 
   const sp24_status st = check_arch();
   if (st != SP24_OK) return st;
   const size_t os = elem_bytes(out_type);
-  const GatedParams p = {rows, F, g, u, y, scale, ldg, ldu, ldy, (int)act, whole_rows(g, rows, ldg, es, 16), !u || whole_rows(u, rows, ldu, es, 16),
-                         whole_rows(y, rows, ldy, os, 16 / es * os)};
-  const int64_t vectors = (F * (int64_t)es + 15) / 16;
-  const bool whole = p.whole_g && p.whole_u && p.whole_y && F * es % 16 == 0;
+  const GatedParams p = {rows, F, g, u, y, scale, ldg, ldu, ldy, (int)act};
+  const bool whole = F * es % 16 == 0 && whole_rows(g, rows, ldg, es, 16) && whole_rows(u, rows, ldu, es, 16) && whole_rows(y, rows, ldy, os, 16 / es * os);
+  const int64_t vectors = row_vectors(F, es, whole);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   return with_float_type(t, [&](auto type) {
     using T = typename decltype(type)::type;
@@ -216,13 +245,12 @@ extern "C" sp24_status sp24_gated_act_backward(sp24_dtype t, sp24_act act, int64
   SP24_RETURN_IF(!aligned(dy, es) || !aligned(g, es) || !aligned(u, es) || !aligned(dg, es) || !aligned(du, es), SP24_ERR_ALIGN);
   const sp24_status st = check_arch();
   if (st != SP24_OK) return st;
-  const GatedGradParams p = {rows, F, dy, g, u, dg, du, lddy, ldg, ldu, lddg, lddu};
-  const int64_t across = (F + 255) / 256;
+  const GatedGradParams p = {rows, F, dy, g, u, dg, du, lddy, ldg, ldu, lddg, lddu, (int)act};
+  const bool whole = F * es % 16 == 0 && whole_rows(dy, rows, lddy, es, 16) && whole_rows(g, rows, ldg, es, 16) && whole_rows(u, rows, ldu, es, 16) &&
+                     whole_rows(dg, rows, lddg, es, 16) && whole_rows(du, rows, lddu, es, 16);
+  const RowLaunch at(row_vectors(F, es, whole), rows, 2);
   return with_float_type(t, [&](auto type) {
     using T = typename decltype(type)::type;
-    return with_act(act, [&](auto a) {
-      return launch_overlapped(gated_act_grad_kernel<T, decltype(a)::value>, dim3((unsigned)(across < 65535 ? across : 65535), (unsigned)(rows < 32768 ? rows : 32768)), dim3(256), 0,
-                               static_cast<cudaStream_t>(stream), 1, p);
-    });
+    return launch_overlapped(whole ? gated_act_grad_kernel<T, true> : gated_act_grad_kernel<T, false>, at.grid, at.block, 0, static_cast<cudaStream_t>(stream), 1, p);
   });
 }

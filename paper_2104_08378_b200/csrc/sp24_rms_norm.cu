@@ -12,7 +12,6 @@ struct NormParams {
   int64_t ldx, ldr, ldh, ldy;
   float eps;
   int32_t weight_f32;
-  bool whole_x, whole_r, whole_h, whole_y, whole_w;  // rows (the weight) at boundaries of vectors
 };
 
 // Rows of up to kMostTeamVectors vectors: a team of threads to a row, which holds it in registers, and the weight for all its rows.  One pass: the
@@ -27,25 +26,30 @@ __global__ void __launch_bounds__(team_threads(V), 1) rms_norm_rows_kernel(const
   const int64_t step = (int64_t)gridDim.x * blockDim.y;
   wait_for_stream();
   uint4 a[V], b[V], w[V][kWords];  // a row and its residual, or two rows
-  auto fetch = [&](const void* from, int64_t ld, bool whole, int64_t row, uint4 (&to)[V]) {
+  auto shift = [&](int64_t row) { return WHOLE ? 0 : shift_of<OUT, N>(static_cast<const OUT*>(p.y) + row * p.ldy); };
+  auto fetch = [&](const void* from, int64_t ld, int64_t row, uint4 (&to)[V]) {
     if (row >= p.rows) return;
     const T* at = static_cast<const T*>(from) + row * ld;
 #pragma unroll
-    for (int v = 0; v < V; ++v) to[v] = load_vector<WHOLE>(at, tx + v * team, (int)p.K, whole);
+    for (int v = 0; v < V; ++v) to[v] = load_vector<WHOLE>(at, tx + v * team, (int)p.K, shift(row));
+  };
+  // the weights of a row's vectors: those of all rows are the same if they are WHOLE
+  auto fetch_weights = [&](int shift) {
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) {
+        Pairs<W> one;
+#pragma unroll
+        for (int n = 0; n < kVector<W> / 2; ++n) one[n] = both(1.f);
+        w[v][i] = p.weight ? load_vector<WHOLE>(static_cast<const W*>(p.weight), (tx + v * team) * kWords + i, (int)p.K, shift) : pack<W>(one);
+      }
   };
   int64_t base = (int64_t)blockIdx.x * blockDim.y;  // the first team's row: the warps of a block stay together
-  fetch(p.x, p.ldx, p.whole_x, base + threadIdx.y, a);
-  if (RESIDUAL) fetch(p.residual, p.ldr, p.whole_r, base + threadIdx.y, b);
-  else fetch(p.x, p.ldx, p.whole_x, base + step + threadIdx.y, b);
-#pragma unroll
-  for (int v = 0; v < V; ++v)
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) {
-      Pairs<W> one;
-#pragma unroll
-      for (int n = 0; n < kVector<W> / 2; ++n) one[n] = both(1.f);
-      w[v][i] = p.weight ? load_vector<WHOLE>(static_cast<const W*>(p.weight), (tx + v * team) * kWords + i, (int)p.K, p.whole_w) : pack<W>(one);
-    }
+  fetch(p.x, p.ldx, base + threadIdx.y, a);
+  if (RESIDUAL) fetch(p.residual, p.ldr, base + threadIdx.y, b);
+  else fetch(p.x, p.ldx, base + step + threadIdx.y, b);
+  if (WHOLE) fetch_weights(0);
   auto weighted = [&](int v, Pairs<T>& f) {  // f times the weights
 #pragma unroll
     for (int i = 0; i < kWords; ++i) {
@@ -57,7 +61,8 @@ __global__ void __launch_bounds__(team_threads(V), 1) rms_norm_rows_kernel(const
   };
   // the row whose values are in x (and its residual in b), behind whose use the registers get the next ones
   auto one_row = [&](int64_t row, uint4 (&x)[V]) {
-    const int K = row < p.rows ? (int)p.K : 0;
+    const int K = row < p.rows ? (int)p.K : 0, s = row < p.rows ? shift(row) : 0;
+    if (!WHOLE) fetch_weights(s);
     uint4 h[V];
     float2 sum2 = both(0.f);
     float top = 0.f;
@@ -74,13 +79,13 @@ __global__ void __launch_bounds__(team_threads(V), 1) rms_norm_rows_kernel(const
         for (int n = 0; n < N / 2; ++n) top = max_abs(top, f[n].x, f[n].y);
       }
     }
-    fetch(p.x, p.ldx, p.whole_x, row + (RESIDUAL ? step : 2 * step), x);
+    fetch(p.x, p.ldx, row + (RESIDUAL ? step : 2 * step), x);
     if (RESIDUAL) {
-      fetch(p.residual, p.ldr, p.whole_r, row + step, b);
+      fetch(p.residual, p.ldr, row + step, b);
       if (p.h) {
         T* ph = static_cast<T*>(p.h) + row * p.ldh;
 #pragma unroll
-        for (int v = 0; v < V; ++v) store_vector<WHOLE>(ph, tx + v * team, K, p.whole_h, h[v]);
+        for (int v = 0; v < V; ++v) store_vector<WHOLE>(ph, tx + v * team, K, s, h[v]);
       }
     }
     float sum = sum2.x + sum2.y;
@@ -101,8 +106,8 @@ __global__ void __launch_bounds__(team_threads(V), 1) rms_norm_rows_kernel(const
 #pragma unroll
       for (int n = 0; n < N / 2; ++n) f[n] = mul2(f[n], both(factor));
       if (!is_code<OUT>) weighted(v, f);
-      if constexpr (is_code<OUT>) store_codes<WHOLE, OUT>(py, tx + v * team, K, p.whole_y, f);
-      else store_vector<WHOLE>(py, tx + v * team, K, p.whole_y, pack<T>(f));
+      if constexpr (is_code<OUT>) store_codes<WHOLE, OUT>(py, tx + v * team, K, s, f);
+      else store_vector<WHOLE>(py, tx + v * team, K, s, pack<T>(f));
     }
   };
   for (; base < p.rows; base += step) {
@@ -120,23 +125,24 @@ __global__ void __launch_bounds__(1024, 1) rms_norm_kernel(const NormParams p) {
   constexpr int P = kVector<T> / 2;
   __shared__ RowSums sums;
   int turn = 0;
-  const int K = (int)p.K, vectors = (K + kVector<T> - 1) / kVector<T>;
+  const int K = (int)p.K;
   wait_for_stream();
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     const T* x = static_cast<const T*>(p.x) + row * p.ldx;
     const T* r = p.residual ? static_cast<const T*>(p.residual) + row * p.ldr : nullptr;
     T* h = p.h ? static_cast<T*>(p.h) + row * p.ldh : nullptr;
     OUT* y = static_cast<OUT*>(p.y) + row * p.ldy;
+    const int shift = shift_of<OUT, kVector<T>>(y), vectors = (shift + K + kVector<T> - 1) / kVector<T>;
     auto value = [&](int i) {
-      const uint4 a = load_vector<false>(x, i, K, p.whole_x);
-      return r ? add_packed<T>(a, load_vector<false>(r, i, K, p.whole_r)) : a;
+      const uint4 a = load_vector<false>(x, i, K, shift);
+      return r ? add_packed<T>(a, load_vector<false>(r, i, K, shift)) : a;
     };
     auto weighted = [&](int i, Pairs<T>& f) {
 #pragma unroll
       for (int n = 0; n < P; ++n) {
-        const int k = i * kVector<T> + 2 * n;
-        if (p.weight && k < K) f[n].x *= load_weight<T>(p.weight, p.weight_f32, k);
-        if (p.weight && k + 1 < K) f[n].y *= load_weight<T>(p.weight, p.weight_f32, k + 1);
+        const int k = i * kVector<T> - shift + 2 * n;
+        if (p.weight && k >= 0 && k < K) f[n].x *= load_weight<T>(p.weight, p.weight_f32, k);
+        if (p.weight && k + 1 >= 0 && k + 1 < K) f[n].y *= load_weight<T>(p.weight, p.weight_f32, k + 1);
       }
     };
     float2 sum2 = both(0.f);
@@ -171,9 +177,9 @@ __global__ void __launch_bounds__(1024, 1) rms_norm_kernel(const NormParams p) {
 #pragma unroll
       for (int n = 0; n < P; ++n) f[n] = mul2(f[n], both(factor));
       if (!is_code<OUT>) weighted(i, f);
-      if (h) store_vector<false>(h, i, K, p.whole_h, v);
-      if constexpr (is_code<OUT>) store_codes<false, OUT>(y, i, K, p.whole_y, f);
-      else store_vector<false>(y, i, K, p.whole_y, pack<T>(f));
+      if (h) store_vector<false>(h, i, K, shift, v);
+      if constexpr (is_code<OUT>) store_codes<false, OUT>(y, i, K, shift, f);
+      else store_vector<false>(y, i, K, shift, pack<T>(f));
     }
   }
 }
@@ -186,7 +192,6 @@ struct NormGradParams {
   float* partial;  // gridDim.x rows of K: each block's part of dweight, or null
   int64_t lddy, ldh, lddh, lddx;
   int32_t weight_f32;
-  bool whole_dy, whole_h, whole_dh, whole_dx, whole_w;
 };
 
 // Rows of up to kMostTeamVectors vectors: a team of threads to a row, with the weight and the team's part of dweight in registers for all
@@ -207,17 +212,17 @@ __global__ void __launch_bounds__(AHEAD ? kAheadThreads : team_threads(V), 1) rm
     uint4 dy[V], h[V], dh[V];
     float rstd;
   };
-  auto fetch = [&](const void* from, int64_t ld, bool whole, int64_t row, uint4 (&to)[V]) {
+  auto fetch = [&](const void* from, int64_t ld, int64_t row, uint4 (&to)[V]) {
     const T* at = static_cast<const T*>(from) + row * ld;
 #pragma unroll
-    for (int v = 0; v < V; ++v) to[v] = load_vector<WHOLE>(at, tx + v * team, K, whole);
+    for (int v = 0; v < V; ++v) to[v] = load_vector<WHOLE>(at, tx + v * team, K, 0);  // (dweight's sums stay with their columns: no shift)
   };
   auto fetch_row = [&](int64_t row, Row& to) {
     if (row >= p.rows) return;
     to.rstd = p.rstd[row];
-    fetch(p.dy, p.lddy, p.whole_dy, row, to.dy);
-    fetch(p.h, p.ldh, p.whole_h, row, to.h);
-    if (p.dh) fetch(p.dh, p.lddh, p.whole_dh, row, to.dh);
+    fetch(p.dy, p.lddy, row, to.dy);
+    fetch(p.h, p.ldh, row, to.h);
+    if (p.dh) fetch(p.dh, p.lddh, row, to.dh);
   };
   Row a = {}, b = {};
   int64_t base = (int64_t)blockIdx.x * blockDim.y;  // the first team's row: the warps of a block stay together
@@ -230,7 +235,7 @@ __global__ void __launch_bounds__(AHEAD ? kAheadThreads : team_threads(V), 1) rm
       Pairs<W> one;
 #pragma unroll
       for (int n = 0; n < PW; ++n) one[n] = both(1.f);
-      w[v][i] = p.weight ? load_vector<WHOLE>(static_cast<const W*>(p.weight), (tx + v * team) * kWords + i, K, p.whole_w) : pack<W>(one);
+      w[v][i] = p.weight ? load_vector<WHOLE>(static_cast<const W*>(p.weight), (tx + v * team) * kWords + i, K, 0) : pack<W>(one);
     }
   auto weighted = [&](int v, Pairs<T>& f) {  // f times the weights
 #pragma unroll
@@ -282,10 +287,8 @@ __global__ void __launch_bounds__(AHEAD ? kAheadThreads : team_threads(V), 1) rm
       out[v] = pack<T>(g);
     }
     if (!AHEAD) fetch_row(row + step, x);
-    if (live) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) store_vector<WHOLE>(dx, tx + v * team, K, p.whole_dx, out[v]);
-    }
+    for (int v = 0; v < V; ++v) store_vector<WHOLE>(dx, tx + v * team, live ? K : 0, 0, out[v]);
   };
   for (; base < p.rows; base += step) {
     one_row(base + threadIdx.y, a, b);
@@ -334,31 +337,52 @@ __global__ void __launch_bounds__(AHEAD ? kAheadThreads : team_threads(V), 1) rm
   }
 }
 
+// Longer rows: a block to a row, two passes over it, the block's part of dweight in the workspace.
 template <typename T>
-__global__ void __launch_bounds__(1024) rms_norm_grad_kernel(const NormGradParams p) {
+__global__ void __launch_bounds__(1024, 1) rms_norm_grad_kernel(const NormGradParams p) {
+  constexpr int P = kVector<T> / 2;
   __shared__ RowSums sums;
   int turn = 0;
+  const int K = (int)p.K, vectors = (K + kVector<T> - 1) / kVector<T>;
   wait_for_stream();
+  float* part = p.partial ? p.partial + blockIdx.x * p.K : nullptr;
   bool first = true;
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, first = false) {
     const T* dy = static_cast<const T*>(p.dy) + row * p.lddy;
     const T* h = static_cast<const T*>(p.h) + row * p.ldh;
     const T* dh = p.dh ? static_cast<const T*>(p.dh) + row * p.lddh : nullptr;
     T* dx = static_cast<T*>(p.dx) + row * p.lddx;
-    auto weight = [&](int64_t k) { return p.weight ? load_weight<T>(p.weight, p.weight_f32, k) : 1.f; };
     const float rstd = p.rstd[row];
-    float sum = 0.f;
-    float unused = 0.f;
-    for (int64_t k = threadIdx.x; k < p.K; k += blockDim.x) sum = fmaf(to_float(dy[k]) * weight(k), to_float(h[k]), sum);
-    sums.reduce(sum, unused, turn);
-    const float along = sum / (float)p.K * rstd * rstd;
-    float* part = p.partial ? p.partial + blockIdx.x * p.K : nullptr;
-    for (int64_t k = threadIdx.x; k < p.K; k += blockDim.x) {
-      const float g = to_float(dy[k]), v = to_float(h[k]);
-      float d = rstd * fmaf(-v, along, g * weight(k));
-      if (dh) d += to_float(dh[k]);
-      dx[k] = round_to<T>(d);
-      if (part) part[k] = fmaf(g * v, rstd, first ? 0.f : part[k]);
+    auto weight = [&](int k) { return p.weight && k < K ? load_weight<T>(p.weight, p.weight_f32, k) : 1.f; };
+    auto load = [&](int i, Pairs<T>& g, Pairs<T>& f) {
+      unpack<T>(load_vector<false>(dy, i, K, 0), g);
+      unpack<T>(load_vector<false>(h, i, K, 0), f);
+    };
+    float2 sum2 = both(0.f);
+    for (int i = threadIdx.x; i < vectors; i += blockDim.x) {
+      Pairs<T> g, f;
+      load(i, g, f);
+#pragma unroll
+      for (int n = 0; n < P; ++n) {
+        const int k = i * kVector<T> + 2 * n;
+        sum2 = fma2(mul2(g[n], make_float2(weight(k), weight(k + 1))), f[n], sum2);
+      }
+    }
+    float sum = sum2.x + sum2.y, unused = 0.f;
+    sums.reduce<true, false>(sum, unused, turn);
+    const float along = -sum / (float)p.K * rstd * rstd;
+    for (int i = threadIdx.x; i < vectors; i += blockDim.x) {
+      Pairs<T> g, f, d = {};
+      load(i, g, f);
+      if (dh) unpack<T>(load_vector<false>(dh, i, K, 0), d);
+#pragma unroll
+      for (int n = 0; n < P; ++n) {
+        const int k = i * kVector<T> + 2 * n;
+        if (part && k < K) part[k] = fmaf(g[n].x * f[n].x, rstd, first ? 0.f : part[k]);
+        if (part && k + 1 < K) part[k + 1] = fmaf(g[n].y * f[n].y, rstd, first ? 0.f : part[k + 1]);
+        g[n] = fma2(fma2(f[n], both(along), mul2(g[n], make_float2(weight(k), weight(k + 1)))), both(rstd), d[n]);
+      }
+      store_vector<false>(dx, i, K, 0, pack<T>(g));
     }
   }
 }
@@ -410,14 +434,10 @@ extern "C" sp24_status sp24_rms_norm(sp24_dtype t, int64_t rows, int64_t K, cons
                  SP24_ERR_ALIGN);
   sp24_status st = check_arch();
   if (st != SP24_OK) return st;
-  NormParams p = {rows, K, x, residual, weight, h, y, scale, rstd, ldx, ldr, ldh, ldy, eps, weight_type == SP24_F32};
-  p.whole_x = whole_rows(x, rows, ldx, es, 16);
-  p.whole_r = !residual || whole_rows(residual, rows, ldr, es, 16);
-  p.whole_h = !h || whole_rows(h, rows, ldh, es, 16);
-  p.whole_y = whole_rows(y, rows, ldy, os, 16 / es * os);
-  p.whole_w = aligned(weight, 16);
-  const int64_t vectors = (K * (int64_t)es + 15) / 16;
-  const bool whole = p.whole_x && p.whole_r && p.whole_h && p.whole_y && p.whole_w && K * es % 16 == 0;
+  const NormParams p = {rows, K, x, residual, weight, h, y, scale, rstd, ldx, ldr, ldh, ldy, eps, weight_type == SP24_F32};
+  const bool whole = K * es % 16 == 0 && whole_rows(x, rows, ldx, es, 16) && whole_rows(residual, rows, ldr, es, 16) && whole_rows(h, rows, ldh, es, 16) &&
+                     whole_rows(y, rows, ldy, os, 16 / es * os) && aligned16(weight);
+  const int64_t vectors = row_vectors(K, es, whole);
   return with_float_type(t, [&](auto type) {
     using T = typename decltype(type)::type;
     return with_out_type<T>(out_type, [&](auto out) {
@@ -470,11 +490,10 @@ extern "C" sp24_status sp24_rms_norm_backward(sp24_dtype t, int64_t rows, int64_
   sp24_status st = check_arch();
   if (st != SP24_OK) return st;
   int64_t blocks = grad_blocks(rows);
-  const NormGradParams p = {rows, K, dy, h, weight, dh, rstd, dx, dweight ? static_cast<float*>(workspace) : nullptr, lddy, ldh, lddh, lddx, weight_type == SP24_F32,
-                            whole_rows(dy, rows, lddy, es, 16), whole_rows(h, rows, ldh, es, 16), !dh || whole_rows(dh, rows, lddh, es, 16),
-                            whole_rows(dx, rows, lddx, es, 16), aligned(weight, 16)};
-  const int64_t vectors = (K * (int64_t)es + 15) / 16;
-  const bool whole = p.whole_dy && p.whole_h && p.whole_dh && p.whole_dx && p.whole_w && K * es % 16 == 0;
+  const NormGradParams p = {rows, K, dy, h, weight, dh, rstd, dx, dweight ? static_cast<float*>(workspace) : nullptr, lddy, ldh, lddh, lddx, weight_type == SP24_F32};
+  const bool whole = K * es % 16 == 0 && whole_rows(dy, rows, lddy, es, 16) && whole_rows(h, rows, ldh, es, 16) && whole_rows(dh, rows, lddh, es, 16) &&
+                     whole_rows(dx, rows, lddx, es, 16) && aligned16(weight);
+  const int64_t vectors = row_vectors(K, es, true);
   st = with_float_type(t, [&](auto type) {
     using T = typename decltype(type)::type;
     if (vectors <= kMostTeamVectors) {
@@ -494,7 +513,7 @@ extern "C" sp24_status sp24_rms_norm_backward(sp24_dtype t, int64_t rows, int64_
       };
       return weight && weight_type == SP24_F32 ? launch(TypeOf<float>{}) : launch(TypeOf<T>{});
     }
-    return launch_overlapped(rms_norm_grad_kernel<T>, dim3((unsigned)blocks), dim3(row_threads(K)), 0, s, 1, p);
+    return launch_overlapped(rms_norm_grad_kernel<T>, dim3((unsigned)blocks), dim3(1024), 0, s, 1, p);
   });
   if (st != SP24_OK || !dweight) return st;
   return column_sums(static_cast<const float*>(workspace), blocks, K, dweight, s);

@@ -220,45 +220,94 @@ __device__ __forceinline__ uint4 add_packed(const uint4& a, const uint4& b) {
   return make_uint4(z[0], z[1], z[2], z[3]);
 }
 
-// Vector i of a row of K elements; what lies behind the row's end is 0.  `whole`: its vectors lie at 16-byte boundaries.  WHOLE: those of
-// all rows do, and K is a number of vectors.
+// ---- rows that start between 16-byte boundaries ----------------------------------------------------------------------------------
+// Bytes `o` (below 4 * WORDS) and on of the 8 * WORDS bytes {lo, hi}.
+template <int WORDS>
+__device__ __forceinline__ void from_byte(const uint32_t (&lo)[WORDS], const uint32_t (&hi)[WORDS], int o, uint32_t (&out)[WORDS]) {
+  uint32_t w[2 * WORDS];
+#pragma unroll
+  for (int i = 0; i < WORDS; ++i) {
+    w[i] = lo[i];
+    w[WORDS + i] = hi[i];
+  }
+#pragma unroll
+  for (int by = WORDS / 2; by > 0; by /= 2) {
+    const bool shift = o & (4 * by);
+#pragma unroll
+    for (int i = 0; i + by < 2 * WORDS; ++i) w[i] = shift ? w[i + by] : w[i];
+  }
+#pragma unroll
+  for (int i = 0; i < WORDS; ++i) out[i] = __funnelshift_r(w[i], w[i + 1], 8 * (o & 3));
+}
+
+// Where the vectors of a row lie: number i holds the elements from i * N - shift on, so that the words of a row whose first element lies
+// `shift` elements behind a boundary are whole vectors (WHOLE: all rows start at boundaries and end with a vector, shift is 0).
+template <typename E, int N>
+__device__ __forceinline__ int shift_of(const E* row) {
+  return (int)(reinterpret_cast<uintptr_t>(row) / sizeof(E) % N);
+}
+
+// Vector i of a row of K elements, zeros where the row has none.  If the vectors do not lie at boundaries, out of the two words that one lies in.  A word is
+// read if one of the row's elements is in it: the bytes beside them are in the same 16, and not used.
 template <bool WHOLE, typename T>
-__device__ __forceinline__ uint4 load_vector(const T* row, int i, int K, bool whole) {
+__device__ __forceinline__ uint4 load_vector(const T* row, int i, int K, int shift) {
   constexpr int N = kVector<T>;
   if (WHOLE) return i * N < K ? __ldcs(reinterpret_cast<const uint4*>(row) + i) : make_uint4(0, 0, 0, 0);
-  if (whole && (i + 1) * N <= K) return __ldcs(reinterpret_cast<const uint4*>(row) + i);
-  uint4 w = make_uint4(0, 0, 0, 0);
-  T* e = reinterpret_cast<T*>(&w);
+  const int first = i * N - shift;  // its first element's number
+  const int o = (int)(reinterpret_cast<uintptr_t>(row - shift) & 15), behind = o / (int)sizeof(T);  // the vectors lie so far behind the words
+  const uint4* words = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(row - shift) - o);
+  auto word = [&](int j) {
+    const int e = j * N - shift - behind;  // the word's first element
+    return e < K && e + N > 0 ? words[j] : make_uint4(0, 0, 0, 0);
+  };
+  uint4 a = word(i);
+  uint32_t w[4] = {a.x, a.y, a.z, a.w};
+  if (o) {
+    a = word(i + 1);
+    const uint32_t lo[4] = {w[0], w[1], w[2], w[3]}, hi[4] = {a.x, a.y, a.z, a.w};
+    from_byte(lo, hi, o, w);
+  }
+  if (first < 0 || first + N > K) {
+    T* e = reinterpret_cast<T*>(w);
+    const T zero = {};
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      if ((unsigned)(first + n) >= (unsigned)K) e[n] = zero;
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Vector i of a row of K elements, 4 * WORDS bytes of E, to the row: as one word if it lies at a boundary, else by elements.
+template <bool WHOLE, typename E, int WORDS>
+__device__ __forceinline__ void store_words(E* row, int i, int K, int shift, const uint32_t (&w)[WORDS]) {
+  constexpr int N = 4 * WORDS / sizeof(E);
+  const int first = i * N - (WHOLE ? 0 : shift);
+  if (WHOLE ? first < K : first >= 0 && first + N <= K && reinterpret_cast<uintptr_t>(row - shift) % (4 * WORDS) == 0) {
+    if constexpr (WORDS == 4) *reinterpret_cast<uint4*>(row + first) = make_uint4(w[0], w[1], w[2], w[3]);
+    else if constexpr (WORDS == 2) *reinterpret_cast<uint2*>(row + first) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint32_t*>(row + first) = w[0];
+    return;
+  }
+  if (WHOLE) return;
+  const E* e = reinterpret_cast<const E*>(w);
 #pragma unroll
   for (int n = 0; n < N; ++n)
-    if (i * N + n < K) e[n] = row[i * N + n];
-  return w;
+    if ((unsigned)(first + n) < (unsigned)K) row[first + n] = e[n];
 }
 template <bool WHOLE, typename T>
-__device__ __forceinline__ void store_vector(T* row, int i, int K, bool whole, const uint4& w) {
-  constexpr int N = kVector<T>;
-  if (WHOLE) {
-    if (i * N < K) reinterpret_cast<uint4*>(row)[i] = w;
-    return;
-  }
-  if (whole && (i + 1) * N <= K) {
-    reinterpret_cast<uint4*>(row)[i] = w;
-    return;
-  }
-  const T* e = reinterpret_cast<const T*>(&w);
-#pragma unroll
-  for (int n = 0; n < N; ++n)
-    if (i * N + n < K) row[i * N + n] = e[n];
+__device__ __forceinline__ void store_vector(T* row, int i, int K, int shift, const uint4& v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  store_words<WHOLE>(row, i, K, shift, w);
 }
-// N codes, in `whole` rows at boundaries of N bytes
+// ... as N codes
 template <bool WHOLE, typename OUT, int PAIRS>
-__device__ __forceinline__ void store_codes(OUT* row, int i, int K, bool whole, const float2 (&f)[PAIRS]) {
+__device__ __forceinline__ void store_codes(OUT* row, int i, int K, int shift, const float2 (&f)[PAIRS]) {
   constexpr int N = 2 * PAIRS;
   uint32_t w[N / 4];
 #pragma unroll
   for (int n = 0; n < N / 4; ++n) {
     const float2 lo = f[2 * n], hi = f[2 * n + 1];
-    if constexpr (std::is_same_v<OUT, int8_t>) {  // (NaN: 0.  The lower end is -127, |v| <= 127 (1 + 2^-22): only its rounding has to be clamped, above.)
+    if constexpr (std::is_same_v<OUT, int8_t>) {  // (NaN: 0.  |v| is at most 127 (1 + 2^-22), which rounds to no more than 127.)
       asm("cvt.pack.sat.s8.s32.b32 %0, %1, %2, 0;" : "=r"(w[n]) : "r"(__float2int_rn(hi.y)), "r"(__float2int_rn(hi.x)));
       asm("cvt.pack.sat.s8.s32.b32 %0, %1, %2, %0;" : "+r"(w[n]) : "r"(__float2int_rn(lo.y)), "r"(__float2int_rn(lo.x)));
     } else {
@@ -266,21 +315,15 @@ __device__ __forceinline__ void store_codes(OUT* row, int i, int K, bool whole, 
       w[n] = __nv_cvt_float2_to_fp8x2(lo, __NV_SATFINITE, kind) | (uint32_t)__nv_cvt_float2_to_fp8x2(hi, __NV_SATFINITE, kind) << 16;
     }
   }
-  if (WHOLE ? i * N < K : whole && (i + 1) * N <= K) {
-    if constexpr (N == 8) reinterpret_cast<uint2*>(row)[i] = make_uint2(w[0], w[1]);
-    else reinterpret_cast<uint32_t*>(row)[i] = w[0];
-    return;
-  }
-  if (WHOLE) return;
-  const OUT* e = reinterpret_cast<const OUT*>(w);
-#pragma unroll
-  for (int n = 0; n < N; ++n)
-    if (i * N + n < K) row[i * N + n] = e[n];
+  store_words<WHOLE>(row, i, K, shift, w);
 }
+
+// Vectors that hold a row of K elements wherever it starts.
+inline int64_t row_vectors(int64_t K, size_t es, bool whole) { return ((K + (whole ? 0 : 16 / (int64_t)es - 1)) * (int64_t)es + 15) / 16; }
 
 // Whether the rows start at `bytes` boundaries (an absent matrix does).
 inline bool whole_rows(const void* base, int64_t rows, int64_t ld, size_t es, size_t bytes) {
-  return aligned(base, bytes) && (rows <= 1 || (size_t)ld * es % bytes == 0);
+  return !base || (aligned(base, bytes) && (rows <= 1 || (size_t)ld * es % bytes == 0));
 }
 
 // Teams, blocks and vectors to a thread for rows that a team holds in registers: a block to an SM, as many teams to a block as its threads
@@ -311,13 +354,6 @@ struct TeamLaunch {
     grid = dim3((unsigned)blocks);
   }
 };
-
-// Threads of a block to a row of K elements.
-inline int row_threads(int64_t K) {
-  int threads = 32;
-  while (threads < 1024 && threads * 4 < K) threads *= 2;
-  return threads;
-}
 
 // out[k] = sum of partial[b * K + k] over b < parts, in an order that parts alone fixes (sp24_rms_norm.cu)
 sp24_status column_sums(const float* partial, int64_t parts, int64_t K, float* out, cudaStream_t s);
