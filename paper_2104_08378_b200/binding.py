@@ -130,12 +130,17 @@ if hasattr(torch._C, "_cuda_getCurrentRawStream"):
 else:                          # a CPU-only build of torch has no CUDA tensors: every call is for the functions below
     class _native:
         gemm = gemm_i8_dequant = conv3x3_nhwc = compress = apply_mask = staticmethod(lambda *args: None)
+        rms_norm = rms_norm_backward = gated_act = gated_act_backward = act_backward = linear = staticmethod(lambda *args: None)
 
 # Addresses for the native form of the short calls, which does what the functions below do if all arguments are of the
 # ordinary kind, and returns None if not (then they do it themselves) or the status of a call that was refused.
 _GEMM, _DEQUANT, _CONV, _COMPRESS, _META_BYTES, _APPLY_MASK = (
     ctypes.cast(getattr(lib, name), ctypes.c_void_p).value
     for name in ("sp24_gemm", "sp24_gemm_i8_dequant", "sp24_conv3x3_nhwc", "sp24_compress", "sp24_meta_bytes", "sp24_apply_mask"))
+_RMS_NORM, _RMS_NORM_BACKWARD, _RMS_NORM_BYTES, _GATED, _GATED_BACKWARD, _ACT_BACKWARD, _ACT_BYTES, _LINEAR = (
+    ctypes.cast(getattr(lib, name), ctypes.c_void_p).value
+    for name in ("sp24_rms_norm", "sp24_rms_norm_backward", "sp24_rms_norm_backward_workspace_bytes", "sp24_gated_act",
+                 "sp24_gated_act_backward", "sp24_act_backward", "sp24_act_backward_workspace_bytes", "sp24_linear"))
 
 
 def status_string(status: int) -> str:
@@ -518,13 +523,20 @@ def _act_code(act: str | None, where: str) -> int:
     return ACT[act]
 
 
-@_on_device_of("x")
 def rms_norm(x: torch.Tensor, weight: torch.Tensor | None = None, *, eps: float = 1e-6, residual: torch.Tensor | None = None,
              quant: str | None = None, with_rstd: bool = False, h_out: torch.Tensor | None = None,
              out: torch.Tensor | None = None):
     """sp24_rms_norm on the rows of x [rows, K]: returns (y, h, scale, rstd).  h = x + residual (None without residual), y its
     norm times weight [K] (x's type or float32; None: ones).  quant = "i8", "e4m3" or "e5m2": y in 8 bits and scale [rows],
     else scale is None.  rstd [rows] with with_rstd, else None.  h_out and out may be x or residual themselves."""
+    done = _native.rms_norm(_RMS_NORM, x, weight, eps, residual, quant, with_rstd, h_out, out)
+    if done is not None:
+        return done if type(done) is not int else _check(done, "sp24_rms_norm")
+    return _rms_norm(x, weight, eps=eps, residual=residual, quant=quant, with_rstd=with_rstd, h_out=h_out, out=out)
+
+
+@_on_device_of("x")
+def _rms_norm(x, weight, *, eps, residual, quant, with_rstd, h_out, out):
     where = "sp24_rms_norm"
     t = _float_code(x, where)
     ldx = _matrix(x, where)
@@ -549,12 +561,19 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor | None = None, *, eps: float 
     return y, h, scale, rstd
 
 
-@_on_device_of("dy")
 def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor | None, rstd: torch.Tensor, *,
                       dh: torch.Tensor | None = None, out: torch.Tensor | None = None):
     """sp24_rms_norm_backward: (dx, dweight) from the gradient of y, the h that rms_norm normalised (x without residual), its
     weight and its rstd; dh is the gradient that arrives at h along the residual.  dweight is float32, None without weight.
     out may be dy, h or dh."""
+    done = _native.rms_norm_backward(_RMS_NORM_BACKWARD, _RMS_NORM_BYTES, dy, h, weight, rstd, dh, out)
+    if done is not None:
+        return done if type(done) is not int else _check(done, "sp24_rms_norm_backward")
+    return _rms_norm_backward(dy, h, weight, rstd, dh=dh, out=out)
+
+
+@_on_device_of("dy")
+def _rms_norm_backward(dy, h, weight, rstd, *, dh, out):
     where = "sp24_rms_norm_backward"
     t = _float_code(dy, where)
     lddy = _matrix(dy, where)
@@ -578,12 +597,19 @@ def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor | 
     return dx, dweight
 
 
-@_on_device_of("g")
 def gated_act(g: torch.Tensor, u: torch.Tensor | None = None, *, act: str | None = "silu", quant: str | None = None,
               out: torch.Tensor | None = None):
     """sp24_gated_act: (y, scale) with y = act(g) * u on rows [rows, F] (act(g) without u; act: "relu", "gelu", "silu",
     "gelu_tanh" or None).  quant = "i8", "e4m3" or "e5m2": y in 8 bits and scale [rows], else scale is None.  g and u may be
     slices of one matrix; out may be g or u."""
+    done = _native.gated_act(_GATED, g, u, act, quant, out)
+    if done is not None:
+        return done if type(done) is not int else _check(done, "sp24_gated_act")
+    return _gated_act(g, u, act=act, quant=quant, out=out)
+
+
+@_on_device_of("g")
+def _gated_act(g, u, *, act, quant, out):
     where = "sp24_gated_act"
     t, code = _float_code(g, where), _act_code(act, where)
     ldg = _matrix(g, where)
@@ -599,11 +625,18 @@ def gated_act(g: torch.Tensor, u: torch.Tensor | None = None, *, act: str | None
     return y, scale
 
 
-@_on_device_of("dy")
 def gated_act_backward(dy: torch.Tensor, g: torch.Tensor, u: torch.Tensor | None = None, *, act: str | None = "silu",
                        dg: torch.Tensor | None = None, du: torch.Tensor | None = None):
     """sp24_gated_act_backward: (dg, du) from the gradient of y = act(g) * u; du is None without u.  dg and du may be given,
     as slices of one matrix for instance."""
+    done = _native.gated_act_backward(_GATED_BACKWARD, dy, g, u, act, dg, du)
+    if done is not None:
+        return done if type(done) is not int else _check(done, "sp24_gated_act_backward")
+    return _gated_act_backward(dy, g, u, act=act, dg=dg, du=du)
+
+
+@_on_device_of("dy")
+def _gated_act_backward(dy, g, u, *, act, dg, du):
     where = "sp24_gated_act_backward"
     t, code = _float_code(dy, where), _act_code(act, where)
     lddy = _matrix(dy, where)
@@ -621,12 +654,19 @@ def gated_act_backward(dy: torch.Tensor, g: torch.Tensor, u: torch.Tensor | None
     return dg, du
 
 
-@_on_device_of("dy")
 def act_backward(dy: torch.Tensor, pre: torch.Tensor | None, *, act: str | None, cd_col_major: bool = False,
                  transposed: bool = True, bias: bool = True, out: torch.Tensor | None = None):
     """sp24_act_backward: (dz, dz transposed or None, dbias or None) from the gradient of act(pre).  cd_col_major as in the
     product that made pre: True: dy and pre are [N, M], else [M, N]; dbias [M] sums over the N tokens.  Without an activation
     dz is dy itself and pre is not read.  out may be dy or pre."""
+    done = _native.act_backward(_ACT_BACKWARD, _ACT_BYTES, dy, pre, act, cd_col_major, transposed, bias, out)
+    if done is not None:
+        return done if type(done) is not int else _check(done, "sp24_act_backward")
+    return _act_backward(dy, pre, act=act, cd_col_major=cd_col_major, transposed=transposed, bias=bias, out=out)
+
+
+@_on_device_of("dy")
+def _act_backward(dy, pre, *, act, cd_col_major, transposed, bias, out):
     where = "sp24_act_backward"
     t, code = _float_code(dy, where), _act_code(act, where)
     lddy = ldz = _matrix(dy, where)
@@ -649,7 +689,6 @@ def act_backward(dy: torch.Tensor, pre: torch.Tensor | None, *, act: str | None,
     return dy if dz is None else dz, dzt, dbias
 
 
-@_on_device_of("A")
 def linear(A: torch.Tensor, meta: torch.Tensor | None, Bt: torch.Tensor, *, bias: torch.Tensor | None = None,
            act: str | None = None, residual: torch.Tensor | None = None, row_scale: torch.Tensor | None = None,
            col_scale: torch.Tensor | None = None, pre: bool | torch.Tensor = False, out: torch.Tensor | None = None,
@@ -659,6 +698,17 @@ def linear(A: torch.Tensor, meta: torch.Tensor | None, Bt: torch.Tensor, *, bias
     a_is_dense, b_row_major, cd_col_major as for gemm (cd defaults to A's type, bf16 for 8-bit operands); bias and row_scale
     [M], col_scale [N] float32 (col_scale: 8-bit operands); residual in D's type and shape, and may be `out`.  Returns D, or
     with pre=True (or a tensor for it) (D, what act was applied to)."""
+    done = _native.linear(_LINEAR, _workspaces, _META_BYTES, A, meta, Bt, bias, act, residual, row_scale, col_scale, pre,
+                          out, cd, a_is_dense, b_row_major, cd_col_major, ws)
+    if done is not None:
+        return done if type(done) is not int else _check(done, "sp24_linear")
+    return _linear(A, meta, Bt, bias=bias, act=act, residual=residual, row_scale=row_scale, col_scale=col_scale, pre=pre,
+                   out=out, cd=cd, a_is_dense=a_is_dense, b_row_major=b_row_major, cd_col_major=cd_col_major, ws=ws)
+
+
+@_on_device_of("A")
+def _linear(A, meta, Bt, *, bias, act, residual, row_scale, col_scale, pre, out, cd, a_is_dense, b_row_major,
+            cd_col_major, ws):
     where = "sp24_linear"
     ab = _FROM_TORCH.get(A.dtype)
     _refuse(ab is None or ab == "i32", ERR_DTYPE, where)

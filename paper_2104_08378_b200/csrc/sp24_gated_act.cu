@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(team_threads(V), 1) gated_act_rows_kernel(cons
     const int K = row < p.rows ? F : 0, s = row < p.rows ? shift(row) : 0;
     fetch(row + step, next);
     Pairs<T> y[V];
-    float top = 0.f, unused = 0.f, inv = 0.f;
+    float top = 0.f, unused[1] = {}, inv = 0.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       gated_vector<T>(p.act, x.g[v], x.u[v], gated, y[v]);
@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(1024, 1) gated_act_kernel(const GatedParams p)
     };
     float inv = 0.f;
     if (is_code<OUT>) {
-      float top = 0.f, unused = 0.f;
+      float top = 0.f, unused[1] = {};
 #pragma unroll 2
       for (int i = threadIdx.x; i < vectors; i += blockDim.x) {
         Pairs<T> f;

@@ -303,9 +303,328 @@ PyObject* apply_mask(PyObject*, PyObject* const* v, Py_ssize_t n) {
   }
 }
 
+// ---- the operators around the products: as the Python forms check and call them -----------------------------------------
+// A matrix with contiguous rows on the current device, of the sizes and type given (-1: any); false: not an ordinary one.
+struct Matrix {
+  const at::Tensor* t = nullptr;
+  void* p = nullptr;
+  int64_t ld = 0;
+  bool init(PyObject* o, int64_t rows, int64_t cols, int type) {
+    t = plain(o, 2);
+    if (t == nullptr || t->dim() != 2 || t->get_device() != c10::cuda::current_device()) return false;
+    if ((rows >= 0 && (t->size(0) != rows || t->size(1) != cols)) || (type >= 0 && t->scalar_type() != kScalar[type])) return false;
+    if (t->size(1) > 1 && t->stride(1) != 1) return false;
+    ld = t->size(0) > 1 ? t->stride(0) : (t->size(1) > 1 ? t->size(1) : 1);
+    p = t->data_ptr();
+    return true;
+  }
+};
+// The same for a contiguous vector, or None; *type (if asked for): which of the two types it has.
+bool vector(PyObject* o, int64_t n, int type_a, int type_b, const void** p, int* type = nullptr) {
+  *p = nullptr;
+  if (o == Py_None) return true;
+  const at::Tensor* t = plain(o, 1);
+  if (t == nullptr || t->dim() != 1 || t->size(0) != n || (n > 1 && t->stride(0) != 1) || t->get_device() != c10::cuda::current_device()) return false;
+  const int code = type_code(t->scalar_type());
+  if (code != type_a && code != type_b) return false;
+  if (type) *type = code;
+  *p = t->data_ptr();
+  return true;
+}
+bool float_type(int code) { return code == SP24_F16 || code == SP24_BF16 || code == SP24_F32; }
+// 8-bit type of a name, `otherwise` for None, -1: no such type
+int quant_code(PyObject* name, int otherwise) {
+  if (name == Py_None) return otherwise;
+  const int code = type_code(name);
+  return code == SP24_I8 || code == SP24_E4M3 || code == SP24_E5M2 ? code : -1;
+}
+int act_code(PyObject* name) {
+  static const char* const names[5] = {nullptr, "relu", "gelu", "silu", "gelu_tanh"};
+  if (name == Py_None) return SP24_ACT_NONE;
+  if (!PyUnicode_CheckExact(name)) return -1;
+  for (int i = 1; i < 5; ++i)
+    if (PyUnicode_CompareWithASCIIString(name, names[i]) == 0) return i;
+  return -1;
+}
+// A given result (its checks passed), or the tensor made for it
+struct Result {
+  PyObject* given;
+  at::Tensor made;
+  PyObject* object() {
+    if (given != Py_None) {
+      Py_INCREF(given);
+      return given;
+    }
+    return made.defined() ? THPVariable_Wrap(std::move(made)) : Py_NewRef(Py_None);
+  }
+};
+// (What makes and calls without the interpreter's lock: a Python error is none of its possible outcomes.)
+template <typename Call>
+int unlocked(Call call) {
+  pybind11::gil_scoped_release go;
+  return (int)call();
+}
+
+// rms_norm(address, x, weight, eps, residual, quant, with_rstd, h_out, out) -> (y, h, scale, rstd)
+PyObject* rms_norm(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 9 || at::impl::torch_function_mode_enabled()) return none();
+  try {
+    Matrix x, r, h, y;
+    double eps;
+    if (!x.init(v[1], -1, -1, -1) || !number(v[3], &eps) || (v[6] != Py_True && v[6] != Py_False)) return none();
+    const int t = type_code(x.t->scalar_type()), out = quant_code(v[5], t);
+    const int64_t rows = x.t->size(0), K = x.t->size(1);
+    const void* weight;
+    int weight_type = SP24_F32;
+    if (!float_type(t) || out < 0 || !vector(v[2], K, t, SP24_F32, &weight, &weight_type)) return none();
+    if (v[4] != Py_None ? !r.init(v[4], rows, K, t) : v[7] != Py_None) return none();
+    if ((v[7] != Py_None && !h.init(v[7], rows, K, t)) || (v[8] != Py_None && !y.init(v[8], rows, K, out))) return none();
+    const auto fn = function<decltype(&sp24_rms_norm)>(v[0]);
+    const cudaStream_t stream = Stream().handle;
+    const int64_t packed = rows > 1 && K > 1 ? K : (K > 1 ? K : 1);
+    Result ry{v[8], {}}, rh{v[7], {}};
+    at::Tensor scale, rstd;
+    const int status = unlocked([&] {
+      const auto options = x.t->options();
+      if (v[4] != Py_None && v[7] == Py_None) {
+        rh.made = at::empty({rows, K}, options);
+        h.p = rh.made.data_ptr();
+        h.ld = packed;
+      }
+      if (v[8] == Py_None) {
+        ry.made = at::empty({rows, K}, options.dtype(kScalar[out]));
+        y.p = ry.made.data_ptr();
+        y.ld = packed;
+      }
+      if (out != t) scale = at::empty({rows}, options.dtype(at::kFloat));
+      if (v[6] == Py_True) rstd = at::empty({rows}, options.dtype(at::kFloat));
+      return fn((sp24_dtype)t, rows, K, x.p, x.ld, r.p, r.ld, weight, (sp24_dtype)weight_type, (float)eps, h.p, h.ld, (sp24_dtype)out, y.p, y.ld,
+                scale.defined() ? (float*)scale.data_ptr() : nullptr, rstd.defined() ? (float*)rstd.data_ptr() : nullptr, stream);
+    });
+    if (status != SP24_OK) return PyLong_FromLong(status);
+    Result rs{Py_None, std::move(scale)}, rr{Py_None, std::move(rstd)};
+    return Py_BuildValue("(NNNN)", ry.object(), rh.object(), rs.object(), rr.object());
+  } catch (...) {
+    return none();
+  }
+}
+
+// rms_norm_backward(address, address of the workspace's size, dy, h, weight, rstd, dh, out) -> (dx, dweight)
+PyObject* rms_norm_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 8 || v[5] == Py_None || at::impl::torch_function_mode_enabled()) return none();
+  try {
+    Matrix dy, h, dh, dx;
+    if (!dy.init(v[2], -1, -1, -1)) return none();
+    const int t = type_code(dy.t->scalar_type());
+    const int64_t rows = dy.t->size(0), K = dy.t->size(1);
+    const void *weight, *rstd;
+    int weight_type = SP24_F32;
+    if (!float_type(t) || !h.init(v[3], rows, K, t) || !vector(v[4], K, t, SP24_F32, &weight, &weight_type) ||
+        !vector(v[5], rows, SP24_F32, SP24_F32, &rstd))
+      return none();
+    if ((v[6] != Py_None && !dh.init(v[6], rows, K, t)) || (v[7] != Py_None && !dx.init(v[7], rows, K, t))) return none();
+    const auto fn = function<decltype(&sp24_rms_norm_backward)>(v[0]);
+    const auto size = function<decltype(&sp24_rms_norm_backward_workspace_bytes)>(v[1]);
+    const cudaStream_t stream = Stream().handle;
+    Result rdx{v[7], {}}, rdw{Py_None, {}};
+    const int status = unlocked([&] {
+      const auto options = dy.t->options();
+      if (v[7] == Py_None) {
+        rdx.made = at::empty({rows, K}, options);
+        dx.p = rdx.made.data_ptr();
+        dx.ld = K > 1 ? K : 1;
+      }
+      at::Tensor ws;
+      size_t bytes = 0;
+      if (v[4] != Py_None) {
+        rdw.made = at::empty({K}, options.dtype(at::kFloat));
+        bytes = size(rows, K);
+        ws = at::empty({(int64_t)bytes}, options.dtype(at::kByte));
+      }
+      return fn((sp24_dtype)t, rows, K, dy.p, dy.ld, h.p, h.ld, weight, (sp24_dtype)weight_type, (const float*)rstd, dh.p, dh.ld, dx.p, dx.ld,
+                rdw.made.defined() ? (float*)rdw.made.data_ptr() : nullptr, ws.defined() ? ws.data_ptr() : nullptr, bytes, stream);
+    });
+    if (status != SP24_OK) return PyLong_FromLong(status);
+    return Py_BuildValue("(NN)", rdx.object(), rdw.object());
+  } catch (...) {
+    return none();
+  }
+}
+
+// gated_act(address, g, u, act, quant, out) -> (y, scale)
+PyObject* gated_act(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 6 || at::impl::torch_function_mode_enabled()) return none();
+  try {
+    Matrix g, u, y;
+    if (!g.init(v[1], -1, -1, -1)) return none();
+    const int t = type_code(g.t->scalar_type()), act = act_code(v[3]), out = quant_code(v[4], t);
+    const int64_t rows = g.t->size(0), F = g.t->size(1);
+    if (!float_type(t) || act < 0 || out < 0 || (v[2] != Py_None && !u.init(v[2], rows, F, t)) || (v[5] != Py_None && !y.init(v[5], rows, F, out)))
+      return none();
+    const auto fn = function<decltype(&sp24_gated_act)>(v[0]);
+    const cudaStream_t stream = Stream().handle;
+    Result ry{v[5], {}}, rs{Py_None, {}};
+    const int status = unlocked([&] {
+      const auto options = g.t->options();
+      if (v[5] == Py_None) {
+        ry.made = at::empty({rows, F}, options.dtype(kScalar[out]));
+        y.p = ry.made.data_ptr();
+        y.ld = F > 1 ? F : 1;
+      }
+      if (out != t) rs.made = at::empty({rows}, options.dtype(at::kFloat));
+      return fn((sp24_dtype)t, (sp24_act)act, rows, F, g.p, g.ld, u.p, u.ld, (sp24_dtype)out, y.p, y.ld,
+                rs.made.defined() ? (float*)rs.made.data_ptr() : nullptr, stream);
+    });
+    if (status != SP24_OK) return PyLong_FromLong(status);
+    return Py_BuildValue("(NN)", ry.object(), rs.object());
+  } catch (...) {
+    return none();
+  }
+}
+
+// gated_act_backward(address, dy, g, u, act, dg, du) -> (dg, du)
+PyObject* gated_act_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 7 || at::impl::torch_function_mode_enabled()) return none();
+  try {
+    Matrix dy, g, u, dg, du;
+    if (!dy.init(v[1], -1, -1, -1)) return none();
+    const int t = type_code(dy.t->scalar_type()), act = act_code(v[4]);
+    const int64_t rows = dy.t->size(0), F = dy.t->size(1);
+    if (!float_type(t) || act < 0 || !g.init(v[2], rows, F, t) || (v[3] != Py_None ? !u.init(v[3], rows, F, t) : v[6] != Py_None)) return none();
+    if ((v[5] != Py_None && !dg.init(v[5], rows, F, t)) || (v[6] != Py_None && !du.init(v[6], rows, F, t))) return none();
+    const auto fn = function<decltype(&sp24_gated_act_backward)>(v[0]);
+    const cudaStream_t stream = Stream().handle;
+    Result rdg{v[5], {}}, rdu{v[6], {}};
+    const int status = unlocked([&] {
+      auto make = [&](Result& r, Matrix& m) {
+        r.made = at::empty({rows, F}, dy.t->options());
+        m.p = r.made.data_ptr();
+        m.ld = F > 1 ? F : 1;
+      };
+      if (v[5] == Py_None) make(rdg, dg);
+      if (v[3] != Py_None && v[6] == Py_None) make(rdu, du);
+      return fn((sp24_dtype)t, (sp24_act)act, rows, F, dy.p, dy.ld, g.p, g.ld, u.p, u.ld, dg.p, dg.ld, du.p, du.ld, stream);
+    });
+    if (status != SP24_OK) return PyLong_FromLong(status);
+    return Py_BuildValue("(NN)", rdg.object(), rdu.object());
+  } catch (...) {
+    return none();
+  }
+}
+
+// act_backward(address, address of the workspace's size, dy, pre, act, cd_col_major, transposed, bias, out) -> (dz, dzt, dbias)
+PyObject* act_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 9 || at::impl::torch_function_mode_enabled()) return none();
+  try {
+    for (int i = 5; i < 8; ++i)
+      if (v[i] != Py_True && v[i] != Py_False) return none();
+    Matrix dy, z, dz;
+    const int act = act_code(v[4]);
+    if (act < 0 || !dy.init(v[2], -1, -1, -1)) return none();
+    const int t = type_code(dy.t->scalar_type());
+    const int64_t rows = dy.t->size(0), cols = dy.t->size(1);
+    if (!float_type(t)) return none();
+    if (act != SP24_ACT_NONE && (!z.init(v[3], rows, cols, t) || (v[8] != Py_None && !dz.init(v[8], rows, cols, t)))) return none();
+    const int over_rows = v[5] == Py_True;
+    const auto fn = function<decltype(&sp24_act_backward)>(v[0]);
+    const auto size = function<decltype(&sp24_act_backward_workspace_bytes)>(v[1]);
+    const cudaStream_t stream = Stream().handle;
+    Result rdz{act == SP24_ACT_NONE ? v[2] : v[8], {}}, rdzt{Py_None, {}}, rdb{Py_None, {}};
+    const int status = unlocked([&] {
+      const auto options = dy.t->options();
+      if (act != SP24_ACT_NONE && v[8] == Py_None) {
+        rdz.made = at::empty({rows, cols}, options);
+        dz.p = rdz.made.data_ptr();
+        dz.ld = cols > 1 ? cols : 1;
+      }
+      if (v[6] == Py_True) rdzt.made = at::empty({cols, rows}, options);
+      at::Tensor ws;
+      size_t bytes = 0;
+      if (v[7] == Py_True) {
+        rdb.made = at::empty({over_rows ? cols : rows}, options.dtype(at::kFloat));
+        bytes = size(rows, cols, over_rows);
+        ws = at::empty({(int64_t)bytes}, options.dtype(at::kByte));
+      }
+      return fn((sp24_dtype)t, (sp24_act)act, rows, cols, dy.p, dy.ld, z.p, z.ld, dz.p, dz.ld, rdzt.made.defined() ? rdzt.made.data_ptr() : nullptr,
+                rows > 1 ? rows : 1, rdb.made.defined() ? (float*)rdb.made.data_ptr() : nullptr, over_rows, ws.defined() ? ws.data_ptr() : nullptr, bytes, stream);
+    });
+    if (status != SP24_OK) return PyLong_FromLong(status);
+    return Py_BuildValue("(NNN)", rdz.object(), rdzt.object(), rdb.object());
+  } catch (...) {
+    return none();
+  }
+}
+
+// linear(address, workspaces, address of sp24_meta_bytes, A, meta, Bt, bias, act, residual, row_scale, col_scale, pre, out, cd, a_is_dense, b_row_major,
+// cd_col_major, ws) -> D or (D, pre)
+PyObject* linear(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 18) return none();
+  try {
+    Product p;
+    Matrix a, b, r, z, d;
+    if (!a.init(v[3], -1, -1, -1)) return none();
+    const int ab = type_code(a.t->scalar_type()), act = act_code(v[7]);
+    PyObject* bf16 = nullptr;  // (Product takes INT32 results of int8 operands where none is named)
+    if (v[13] == Py_None && ab == SP24_I8 && (bf16 = PyUnicode_FromString("bf16")) == nullptr) return none();
+    const bool ok = ab >= 0 && ab != SP24_I32 && act >= 0 && p.init(v[3], v[4], -1, bf16 ? bf16 : v[13], v[14], v[15], v[16]);
+    Py_XDECREF(bf16);
+    if (!ok || !b.init(v[5], -1, -1, ab)) return none();
+    p.d.lda = a.ld;
+    p.d.ldb = b.ld;
+    const bool b_rows = p.d.order_b == SP24_ROW_MAJOR;
+    if (b.t->size(b_rows ? 0 : 1) != p.d.K) return none();
+    p.d.N = b.t->size(b_rows ? 1 : 0);
+    const auto bytes = function<decltype(&sp24_meta_bytes)>(v[2]);
+    const void* meta = nullptr;
+    if (!p.d.a_is_dense) {
+      const at::Tensor* m = plain(v[4], 1);
+      if (m == nullptr || m->dim() != 1 || m->scalar_type() != at::kByte || (m->size(0) > 1 && m->stride(0) != 1) ||
+          m->get_device() != c10::cuda::current_device() || (size_t)m->size(0) != bytes((sp24_dtype)ab, p.d.M, p.d.K, SP24_META_TCGEN05))
+        return none();
+      meta = m->data_ptr();
+    }
+    const int64_t rows = p.cols ? p.d.N : p.d.M, cols = p.cols ? p.d.M : p.d.N;
+    const int cd = (int)p.d.cd_type;
+    sp24_linear_epilogue e = {};
+    e.act = (sp24_act)act;
+    if (!vector(v[6], p.d.M, SP24_F32, SP24_F32, (const void**)&e.bias) || !vector(v[9], p.d.M, SP24_F32, SP24_F32, (const void**)&e.row_scale) ||
+        !vector(v[10], p.d.N, SP24_F32, SP24_F32, (const void**)&e.col_scale))
+      return none();
+    if (v[8] != Py_None && !r.init(v[8], rows, cols, cd)) return none();
+    const bool make_pre = v[11] == Py_True, no_pre = v[11] == Py_False || v[11] == Py_None;
+    if (!make_pre && !no_pre && !z.init(v[11], rows, cols, cd)) return none();
+    if (v[12] != Py_None && !d.init(v[12], rows, cols, cd)) return none();
+    p.stream = Stream().handle;
+    if (!workspace(v[1], v[17], *a.t, p.stream, &p.ws, &p.ws_bytes)) return none();
+    const auto fn = function<decltype(&sp24_linear)>(v[0]);
+    Result rd{v[12], {}}, rz{make_pre || no_pre ? Py_None : v[11], {}};
+    const int status = unlocked([&] {
+      auto make = [&](Result& to, Matrix& m) {
+        to.made = at::empty({rows, cols}, a.t->options().dtype(kScalar[cd]));
+        m.p = to.made.data_ptr();
+        m.ld = cols > 1 ? cols : 1;
+      };
+      if (v[12] == Py_None) make(rd, d);
+      if (make_pre) make(rz, z);
+      p.d.ldd = d.ld;
+      p.d.ldc = r.p || v[8] != Py_None ? r.ld : d.ld;
+      e.residual = r.p;
+      e.pre = z.p;
+      e.ld_pre = z.ld;
+      return fn(&p.d, &e, a.p, meta, b.p, d.p, p.ws, p.ws_bytes, p.stream);
+    });
+    if (status != SP24_OK) return PyLong_FromLong(status);
+    if (no_pre) return rd.object();
+    return Py_BuildValue("(NN)", rd.object(), rz.object());
+  } catch (...) {
+    return none();
+  }
+}
+
 #define SP24_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SP24_METHOD(gemm), SP24_METHOD(gemm_i8_dequant), SP24_METHOD(conv3x3_nhwc), SP24_METHOD(compress),
-                         SP24_METHOD(apply_mask), {nullptr, nullptr, 0, nullptr}};
+                         SP24_METHOD(apply_mask), SP24_METHOD(rms_norm), SP24_METHOD(rms_norm_backward), SP24_METHOD(gated_act),
+                         SP24_METHOD(gated_act_backward), SP24_METHOD(act_backward), SP24_METHOD(linear), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

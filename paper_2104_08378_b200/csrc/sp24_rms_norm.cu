@@ -64,15 +64,16 @@ __global__ void __launch_bounds__(team_threads(V), 1) rms_norm_rows_kernel(const
     const int K = row < p.rows ? (int)p.K : 0, s = row < p.rows ? shift(row) : 0;
     if (!WHOLE) fetch_weights(s);
     uint4 h[V];
-    float2 sum2 = both(0.f);
-    float top = 0.f;
+    float sum[V], top = 0.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
+      float2 sum2 = both(0.f);
       h[v] = RESIDUAL ? add_packed<T>(x[v], b[v]) : x[v];
       Pairs<T> f;
       unpack<T>(h[v], f);
 #pragma unroll
       for (int n = 0; n < N / 2; ++n) sum2 = fma2(f[n], f[n], sum2);
+      sum[v] = sum2.x + sum2.y;
       if (is_code<OUT>) {
         weighted(v, f);
 #pragma unroll
@@ -88,9 +89,8 @@ __global__ void __launch_bounds__(team_threads(V), 1) rms_norm_rows_kernel(const
         for (int v = 0; v < V; ++v) store_vector<WHOLE>(ph, tx + v * team, K, s, h[v]);
       }
     }
-    float sum = sum2.x + sum2.y;
     sums.reduce<true, is_code<OUT>>(sum, top, turn);
-    const float rstd = rsqrtf(sum / (float)p.K + p.eps);
+    const float rstd = rsqrtf(sum[0] / (float)p.K + p.eps);
     if (tx == 0 && K && p.rstd) p.rstd[row] = rstd;
     float factor = rstd;
     if (is_code<OUT>) {
@@ -159,9 +159,9 @@ __global__ void __launch_bounds__(1024, 1) rms_norm_kernel(const NormParams p) {
         for (int n = 0; n < P; ++n) top = max_abs(top, f[n].x, f[n].y);
       }
     }
-    float sum = sum2.x + sum2.y;
-    sums.reduce(sum, top, turn);
-    const float rstd = rsqrtf(sum / (float)p.K + p.eps);
+    float sum[1] = {sum2.x + sum2.y};
+    sums.reduce<true, is_code<OUT>>(sum, top, turn);
+    const float rstd = rsqrtf(sum[0] / (float)p.K + p.eps);
     if (threadIdx.x == 0 && p.rstd) p.rstd[row] = rstd;
     float factor = rstd;
     if (is_code<OUT>) {
@@ -255,9 +255,10 @@ __global__ void __launch_bounds__(AHEAD ? kAheadThreads : team_threads(V), 1) rm
     const bool live = row < p.rows;
     if (AHEAD) fetch_row(row + step, next);
     const float r = x.rstd;
-    float2 sum2 = both(0.f);
+    float sum[V], unused = 0.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
+      float2 sum2 = both(0.f);
       Pairs<T> g, f;
       unpack<T>(x.dy[v], g);
       unpack<T>(x.h[v], f);
@@ -269,10 +270,10 @@ __global__ void __launch_bounds__(AHEAD ? kAheadThreads : team_threads(V), 1) rm
       weighted(v, g);
 #pragma unroll
       for (int n = 0; n < P; ++n) sum2 = fma2(g[n], f[n], sum2);
+      sum[v] = sum2.x + sum2.y;
     }
-    float sum = sum2.x + sum2.y, unused = 0.f;
     sums.reduce<true, false>(sum, unused, turn);
-    const float along = -sum * over_k * r * r;
+    const float along = -sum[0] * over_k * r * r;
     T* dx = static_cast<T*>(p.dx) + row * p.lddx;
     uint4 out[V];
 #pragma unroll
@@ -368,9 +369,9 @@ __global__ void __launch_bounds__(1024, 1) rms_norm_grad_kernel(const NormGradPa
         sum2 = fma2(mul2(g[n], make_float2(weight(k), weight(k + 1))), f[n], sum2);
       }
     }
-    float sum = sum2.x + sum2.y, unused = 0.f;
+    float sum[1] = {sum2.x + sum2.y}, unused = 0.f;
     sums.reduce<true, false>(sum, unused, turn);
-    const float along = -sum / (float)p.K * rstd * rstd;
+    const float along = -sum[0] / (float)p.K * rstd * rstd;
     for (int i = threadIdx.x; i < vectors; i += blockDim.x) {
       Pairs<T> g, f, d = {};
       load(i, g, f);

@@ -112,37 +112,64 @@ __device__ __forceinline__ float finite_or_nan(float top) { return top < __int_a
 // maximum (of values >= 0).  All threads of a block's warps call it together.  Two buffers in turn, so that one barrier is enough: whoever
 // writes a buffer again has passed the barrier of the one between, which the readers reach behind their reads.
 constexpr int kMostTeams = 15;  // of several warps: each has a hardware barrier of its own
+// The sum is over groups of 32 neighbouring vectors (a warp's v-th ones) and then over the groups, each by halves, however many vectors a thread
+// has, so that a row's bits do not depend on how many other rows there are.  (V = 4: 64 groups, in pairs first.)
 struct RowSums {
-  float sum[2][32], top[2][32];
-  template <bool SUM = true, bool TOP = true>
-  __device__ __forceinline__ void reduce(float& s, float& t, int& turn) {
-    auto over = [&](int lanes) {
-      for (int i = lanes >> 1; i > 0; i >>= 1) {
-        if (SUM) s += __shfl_xor_sync(~0u, s, i);
-        if (TOP) t = max_abs(t, __shfl_xor_sync(~0u, t, i), 0.f);
-      }
-    };
-    auto over_warp = [&] {
+  float groups[2][64], top[2][32];
+  // s: of each of the thread's vectors; the row's sum is in s[0] afterwards
+  template <bool SUM, bool TOP, int V>
+  __device__ __forceinline__ void reduce(float (&s)[V], float& t, int& turn) {
+    if (blockDim.x < 32) {
       if (SUM) {
 #pragma unroll
-        for (int i = 16; i > 0; i >>= 1) s += __shfl_xor_sync(~0u, s, i);
+        for (int v = V / 2; v > 0; v /= 2)
+#pragma unroll
+          for (int i = 0; i < v; ++i) s[i] += s[i + v];
       }
-      if (TOP) asm volatile("redux.sync.max.abs.NaN.f32 %0, %0, 0xffffffff;" : "+f"(t));
+      for (int i = blockDim.x >> 1; i > 0; i >>= 1) {
+        if (SUM) s[0] += __shfl_xor_sync(~0u, s[0], i);
+        if (TOP) t = max_abs(t, __shfl_xor_sync(~0u, t, i), 0.f);
+      }
+      return;
+    }
+    auto sum_over_warp = [&](float& x) {
+#pragma unroll
+      for (int i = 16; i > 0; i >>= 1) x += __shfl_xor_sync(~0u, x, i);
     };
-    if (blockDim.x < 32) return over(blockDim.x);
-    over_warp();
+    auto top_over_warp = [&] { asm volatile("redux.sync.max.abs.NaN.f32 %0, %0, 0xffffffff;" : "+f"(t)); };
+    if (SUM) {
+      if (V == 4) {
+        s[0] += s[2];
+        s[1] += s[3];
+      }
+#pragma unroll
+      for (int v = 0; v < (V < 2 ? V : 2); ++v) sum_over_warp(s[v]);
+    }
+    if (TOP) top_over_warp();
     const int warps = blockDim.x >> 5;
-    if (warps == 1) return;
-    const int lane = threadIdx.x & 31, first = threadIdx.y * warps;
+    if (warps == 1) {
+      if (SUM && V > 1) s[0] += s[1];
+      return;
+    }
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = threadIdx.y * warps;
+    // (twice as many groups as warps with two vectors: at most 32 of a team, of all teams those of 24 warps of 48)
     if (lane == 0) {
-      if (SUM) sum[turn][first + (threadIdx.x >> 5)] = s;
-      if (TOP) top[turn][first + (threadIdx.x >> 5)] = t;
+      if (SUM) {
+#pragma unroll
+        for (int v = 0; v < (V < 2 ? V : 2); ++v) groups[turn][(V < 2 ? 1 : 2) * first + v * warps + warp] = s[v];
+      }
+      if (TOP) top[turn][first + warp] = t;
     }
     asm volatile("bar.sync %0, %1;" ::"r"(threadIdx.y + 1), "r"(blockDim.x) : "memory");
-    if (SUM) s = lane < warps ? sum[turn][first + lane] : 0.f;
+    if (SUM) {
+      constexpr int G = V < 2 ? 1 : 2;
+      s[0] = lane < G * warps ? groups[turn][G * first + lane] : 0.f;
+      if (G * warps > 32) s[0] += lane + 32 < G * warps ? groups[turn][G * first + lane + 32] : 0.f;
+    }
     if (TOP) t = lane < warps ? top[turn][first + lane] : 0.f;
     turn ^= 1;
-    over_warp();
+    if (SUM) sum_over_warp(s[0]);
+    if (TOP) top_over_warp();
   }
 };
 

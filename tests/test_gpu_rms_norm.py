@@ -178,3 +178,18 @@ def test_offsets_past_32_bits(sp):
     w = rand((64,), "bf16", 27)
     n, _ = rms_norm64(x, w, 1e-6)
     close(sp.rms_norm(x, w)[0], n, "bf16", ARITHMETIC * n.abs())
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("K", [8, 64, 128, 264, 512, 1024, 1096, 4096, 8192, 12288, 16384, 20000])
+def test_a_row_does_not_depend_on_the_others(sp, t, K):
+    """The same bits for a row by itself, among a few and among many (other numbers of teams, vectors to a thread and blocks)."""
+    x, r, w = rand((1200, K), t, 28), rand((1200, K), t, 29), rand((K,), t, 30)
+    y, _, _, rstd = sp.rms_norm(x, w, residual=r, with_rstd=True)
+    q, _, scale, _ = sp.rms_norm(x, w, quant="i8")
+    dx, _ = sp.rms_norm_backward(r, x, w, rstd, dh=y)
+    for rows in (slice(0, 1), slice(7, 8), slice(100, 260), slice(600, 1199)):
+        a = sp.rms_norm(x[rows], w, residual=r[rows], with_rstd=True)
+        b = sp.rms_norm(x[rows], w, quant="i8")
+        assert torch.equal(a[0], y[rows]) and torch.equal(a[3], rstd[rows]) and torch.equal(b[0], q[rows]) and torch.equal(b[2], scale[rows])
+        assert torch.equal(sp.rms_norm_backward(r[rows], x[rows], w, rstd[rows], dh=y[rows])[0], dx[rows])
