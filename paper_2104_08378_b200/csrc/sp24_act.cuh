@@ -7,65 +7,100 @@ namespace sp24 {
 
 inline bool is_act(int act) { return act >= SP24_ACT_NONE && act <= SP24_ACT_GELU_TANH; }
 
+// ---- pairs: two FP32 operations of one instruction, each rounded by itself --------------------------------------------------
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  asm("{ .reg .b64 x, y; mov.b64 x, {%0, %1}; mov.b64 y, {%2, %3}; mul.rn.f32x2 x, x, y; mov.b64 {%0, %1}, x; }" : "+f"(a.x), "+f"(a.y) : "f"(b.x), "f"(b.y));
+  return a;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  asm("{ .reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mov.b64 z, {%0, %1}; fma.rn.f32x2 z, x, y, z; mov.b64 {%0, %1}, z; }"
+      : "+f"(c.x), "+f"(c.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return c;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// ---- activations, two values at a time ----------------------------------------------------------------------------------------------
+// 2^v and 1 / v of the special-function units, without the instructions that keep results below 2^-126 (which become 0: next to the 1 they are added to, or as a
+// factor of a value below 2^7, they do not count).  They set the pace: two of them to an activation, of which a multiprocessor does sixteen a
+// cycle.
+__device__ __forceinline__ float exp2_fast(float v) {
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(v));
+  return v;
+}
+__device__ __forceinline__ float reciprocal_fast(float v) {
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(v));
+  return v;
+}
+constexpr float kLog2e = 1.4426950408889634f;
+
 // Phi(z) = (1 + erf(z / sqrt 2)) / 2 by Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26 (absolute error of
 // erf at most 1.5e-7; half of that here): erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2), t = 1 / (1 + p x), for x >= 0.  `density`:
-// exp(-z^2 / 2) / sqrt(2 pi), which the slope needs as well.  One exponential and one reciprocal.
-__device__ __forceinline__ float normal_cdf(float z, float* density) {
-  const float t = __fdividef(1.f, fmaf(fabsf(z), 0.3275911f * 0.70710678f, 1.f));
-  const float e = __expf(-0.5f * z * z);
-  float poly = fmaf(t, 1.061405429f, -1.453152027f);
-  poly = fmaf(t, poly, 1.421413741f);
-  poly = fmaf(t, poly, -0.284496736f);
-  poly = fmaf(t, poly, 0.254829592f);
-  const float tail = 0.5f * t * poly * e;  // Phi(-|z|)
-  *density = 0.39894228f * e;
-  return z < 0.f ? tail : 1.f - tail;
+// exp(-z^2 / 2), which the slope needs as well.
+__device__ __forceinline__ float2 normal_cdf(float2 z, float2* density) {
+  constexpr float p = 0.3275911f * 0.70710678f;
+  const float2 t = make_float2(reciprocal_fast(fmaf(fabsf(z.x), p, 1.f)), reciprocal_fast(fmaf(fabsf(z.y), p, 1.f)));
+  const float2 square = mul2(mul2(z, both(-0.5f * kLog2e)), z);
+  *density = make_float2(exp2_fast(square.x), exp2_fast(square.y));
+  float2 poly = fma2(t, both(0.5f * 1.061405429f), both(0.5f * -1.453152027f));
+  poly = fma2(t, poly, both(0.5f * 1.421413741f));
+  poly = fma2(t, poly, both(0.5f * -0.284496736f));
+  poly = fma2(t, poly, both(0.5f * 0.254829592f));
+  const float2 tail = mul2(mul2(t, poly), *density);  // Phi(-|z|)
+  return make_float2(z.x < 0.f ? tail.x : 1.f - tail.x, z.y < 0.f ? tail.y : 1.f - tail.y);
 }
 
-// 1 / (1 + exp(-v)).  (exp(-v) = inf gives 0; __fdividef gives 0 for divisors above 2^126 as well.)
-__device__ __forceinline__ float logistic(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
+// 1 / (1 + exp(-v)) of v = z * factor / log2(e).  (exp(-v) = inf gives 0.)
+__device__ __forceinline__ float2 logistic_of(float2 v_log2e) {
+  const float2 e = make_float2(exp2_fast(-v_log2e.x), exp2_fast(-v_log2e.y));
+  return make_float2(reciprocal_fast(1.f + e.x), reciprocal_fast(1.f + e.y));
+}
 
-// gelu with tanh: (1 + tanh(u)) / 2 = logistic(2 u), u = sqrt(2 / pi) (z + 0.044715 z^3).  (z^2 is limited where the logistic has
+// gelu with tanh: (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u)), u = sqrt(2 / pi) (z + 0.044715 z^3).  (z^2 is limited where the logistic has
 // long been 0 or 1, so that 0 times it is 0.)
-__device__ __forceinline__ float limited_square(float z) { return fminf(z * z, 1e9f); }
-__device__ __forceinline__ float tanh_argument(float z) { return z * fmaf(1.5957691f * 0.044715f, limited_square(z), 1.5957691f); }
+__device__ __forceinline__ float2 limited_square(float2 z) {
+  const float2 s = mul2(z, z);
+  return make_float2(fminf(s.x, 1e9f), fminf(s.y, 1e9f));
+}
+__device__ __forceinline__ float2 tanh_logistic(float2 z) {
+  constexpr float c = 1.5957691216f * kLog2e;  // 2 sqrt(2 / pi), for 2^v
+  return logistic_of(mul2(z, fma2(both(c * 0.044715f), limited_square(z), both(c))));
+}
 
 template <int ACT>
-__device__ __forceinline__ float act_value(float z) {
-  if (ACT == SP24_ACT_RELU) return z < 0.f ? 0.f : z;  // (NaN stays)
+__device__ __forceinline__ float2 act_value(float2 z) {
+  if (ACT == SP24_ACT_RELU) return make_float2(z.x < 0.f ? 0.f : z.x, z.y < 0.f ? 0.f : z.y);  // (NaN stays)
   if (ACT == SP24_ACT_GELU) {
-    float density;
-    return z * normal_cdf(z, &density);
+    float2 density;
+    return mul2(z, normal_cdf(z, &density));
   }
-  if (ACT == SP24_ACT_SILU) return z * logistic(z);
-  if (ACT == SP24_ACT_GELU_TANH) return z * logistic(tanh_argument(z));
+  if (ACT == SP24_ACT_SILU) return mul2(z, logistic_of(mul2(z, both(kLog2e))));
+  if (ACT == SP24_ACT_GELU_TANH) return mul2(z, tanh_logistic(z));
   return z;
 }
 
 // act(z), and act'(z) in *slope
 template <int ACT>
-__device__ __forceinline__ float act_and_slope(float z, float* slope) {
+__device__ __forceinline__ float2 act_and_slope(float2 z, float2* slope) {
   if (ACT == SP24_ACT_RELU) {
-    *slope = z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
-    return z < 0.f ? 0.f : z;
+    slope->x = z.x > 0.f ? 1.f : (z.x <= 0.f ? 0.f : z.x);
+    slope->y = z.y > 0.f ? 1.f : (z.y <= 0.f ? 0.f : z.y);
+    return act_value<ACT>(z);
   }
   if (ACT == SP24_ACT_GELU) {
-    float density;
-    const float cdf = normal_cdf(z, &density);
-    *slope = fmaf(z, density, cdf);
-    return z * cdf;
+    float2 density;
+    const float2 cdf = normal_cdf(z, &density);
+    *slope = fma2(mul2(z, density), both(0.39894228f), cdf);
+    return mul2(z, cdf);
   }
-  if (ACT == SP24_ACT_SILU) {
-    const float p = logistic(z);
-    *slope = p * fmaf(z, 1.f - p, 1.f);
-    return z * p;
+  if (ACT == SP24_ACT_SILU || ACT == SP24_ACT_GELU_TANH) {  // z p(v): p + p (1 - p) z v'
+    const float2 p = ACT == SP24_ACT_SILU ? logistic_of(mul2(z, both(kLog2e))) : tanh_logistic(z);
+    const float2 q = mul2(mul2(p, make_float2(1.f - p.x, 1.f - p.y)), z);
+    *slope = ACT == SP24_ACT_SILU ? make_float2(q.x + p.x, q.y + p.y)
+                                  : fma2(q, fma2(both(1.5957691216f * 0.134145f), limited_square(z), both(1.5957691216f)), p);
+    return mul2(z, p);
   }
-  if (ACT == SP24_ACT_GELU_TANH) {
-    const float p = logistic(tanh_argument(z));
-    *slope = fmaf(p * (1.f - p) * z, fmaf(1.5957691f * 0.134145f, limited_square(z), 1.5957691f), p);
-    return z * p;
-  }
-  *slope = 1.f;
+  *slope = both(1.f);
   return z;
 }
 

@@ -18,32 +18,34 @@ struct ActGradParams {
   int32_t over_rows;
 };
 
-// 16-bit types, all rows (of dzt too) whole vectors at 16-byte boundaries.  A block to a tile of 64 x 64, transposed on its way out of
+// 16-bit types, all rows (of dzt too) whole vectors at 16-byte boundaries.  A block to a tile of 128 x 128 (rows of 256 bytes both ways), transposed on its way out of
 // shared memory by ldmatrix.trans: the eight rows of matrix i are 8 j + 2 i + b (j = 0..3, b = 0, 1), which leaves lane 4 c + j with eight
 // consecutive rows of column c, so that a warp stores eight segments of 64 bytes.  Unit u (16 bytes) of row m lies at
 // u ^ (2 (m >> 3 & 3) + (m & 1)): the eight rows of a matrix are in different banks.
+constexpr int kWide = 128, kUnits = kWide / 8, kWideThreads = 512;
 template <typename T, int ACT>
-__global__ void __launch_bounds__(256) act_grad_tile_kernel(const ActGradParams p) {
-  __shared__ uint4 tile[kTile * kTile / 8];
-  __shared__ float over[8][kTile];  // sums over the rows of each warp
-  const int64_t col_tiles = (p.cols + kTile - 1) / kTile;
-  const int64_t row0 = (int64_t)(blockIdx.x / col_tiles) * kTile, col0 = (int64_t)(blockIdx.x % col_tiles) * kTile;
-  const int u = threadIdx.x % 8, m0 = threadIdx.x / 8, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+__global__ void __launch_bounds__(kWideThreads) act_grad_tile_kernel(const ActGradParams p) {
+  constexpr int kPasses = kWide * kUnits / kWideThreads, kRows = kWide / kPasses;
+  __shared__ uint4 tile[kWide * kUnits];
+  __shared__ float over[kWideThreads / 32][kWide];  // sums over the rows of each warp
+  const int64_t col_tiles = (p.cols + kWide - 1) / kWide;
+  const int64_t row0 = (int64_t)(blockIdx.x / col_tiles) * kWide, col0 = (int64_t)(blockIdx.x % col_tiles) * kWide;
+  const int u = threadIdx.x % kUnits, m0 = threadIdx.x / kUnits, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int64_t c = col0 + 8 * u;
   wait_for_stream();
-  uint4 dy[2] = {}, z[2] = {};
+  uint4 dy[kPasses] = {}, z[kPasses] = {};
 #pragma unroll
-  for (int v = 0; v < 2; ++v)
-    if (const int64_t r = row0 + m0 + 32 * v; r < p.rows && c < p.cols) dy[v] = ld_stream(static_cast<const T*>(p.dy) + r * p.lddy + c);
+  for (int v = 0; v < kPasses; ++v)
+    if (const int64_t r = row0 + m0 + kRows * v; r < p.rows && c < p.cols) dy[v] = ld_stream(static_cast<const T*>(p.dy) + r * p.lddy + c);
   if (ACT != SP24_ACT_NONE) {
 #pragma unroll
-    for (int v = 0; v < 2; ++v)
-      if (const int64_t r = row0 + m0 + 32 * v; r < p.rows && c < p.cols) z[v] = ld_stream(static_cast<const T*>(p.z) + r * p.ldz + c);
+    for (int v = 0; v < kPasses; ++v)
+      if (const int64_t r = row0 + m0 + kRows * v; r < p.rows && c < p.cols) z[v] = ld_stream(static_cast<const T*>(p.z) + r * p.ldz + c);
   }
   Pairs<T> sums = {};
 #pragma unroll
-  for (int v = 0; v < 2; ++v) {
-    const int m = m0 + 32 * v;
+  for (int v = 0; v < kPasses; ++v) {
+    const int m = m0 + kRows * v;
     const int64_t r = row0 + m;
     Pairs<T> d, f;
     unpack<T>(dy[v], d);
@@ -52,55 +54,55 @@ __global__ void __launch_bounds__(256) act_grad_tile_kernel(const ActGradParams 
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
         float2 slope;
-        act_and_slope<ACT>(f[n].x, &slope.x);
-        act_and_slope<ACT>(f[n].y, &slope.y);
+        act_and_slope<ACT>(f[n], &slope);
         d[n] = mul2(d[n], slope);
       }
     }
     const uint4 packed = pack<T>(d);
     if (p.dz && r < p.rows && c < p.cols) *reinterpret_cast<uint4*>(static_cast<T*>(p.dz) + r * p.lddz + c) = packed;
-    tile[m * 8 + (u ^ (2 * (m >> 3 & 3) + (m & 1)))] = packed;
+    tile[m * kUnits + (u ^ (2 * (m >> 3 & 3) + (m & 1)))] = packed;
     if (p.partial && p.over_rows) {
 #pragma unroll
       for (int n = 0; n < 4; ++n) sums[n] = make_float2(sums[n].x + d[n].x, sums[n].y + d[n].y);
     } else if (p.partial) {
       float s = ((d[0].x + d[0].y) + (d[1].x + d[1].y)) + ((d[2].x + d[2].y) + (d[3].x + d[3].y));
 #pragma unroll
-      for (int i = 1; i < 8; i *= 2) s += __shfl_xor_sync(~0u, s, i);
-      if (u == 0 && r < p.rows) p.partial[col0 / kTile * p.rows + r] = s;
+      for (int i = 1; i < kUnits; i *= 2) s += __shfl_xor_sync(~0u, s, i);
+      if (u == 0 && r < p.rows) p.partial[col0 / kWide * p.rows + r] = s;
     }
   }
   if (p.partial && p.over_rows) {
 #pragma unroll
-    for (int i = 8; i < 32; i *= 2)
+    for (int i = kUnits; i < 32; i *= 2)
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
         sums[n].x += __shfl_xor_sync(~0u, sums[n].x, i);
         sums[n].y += __shfl_xor_sync(~0u, sums[n].y, i);
       }
-    if (lane < 8) {
+    if (lane < kUnits) {
 #pragma unroll
       for (int n = 0; n < 4; ++n) *reinterpret_cast<float2*>(&over[warp][8 * u + 2 * n]) = sums[n];
     }
   }
   __syncthreads();
   if (p.dzt) {
+    static_assert(kWideThreads / 32 == kUnits, "a warp to a unit: eight columns");
     const int i = lane >> 3, j = (lane & 7) >> 1, b = lane & 1;  // this lane's row of matrix i for ldmatrix
+    const int64_t col = col0 + 8 * warp + (lane >> 2);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int m32 = 32 * k, unit = warp;  // rows m32..m32 + 31, columns 8 unit..8 unit + 7
-      const int m = m32 + 8 * j + 2 * i + b;
+    for (int k = 0; k < kWide / 32; ++k) {
+      const int m = 32 * k + 8 * j + 2 * i + b;
       uint32_t x[4];
-      ptx::ldmatrix_x4_trans(ptx::smem_u32(&tile[m * 8 + (unit ^ (2 * (m >> 3 & 3) + (m & 1)))]), x[0], x[1], x[2], x[3]);
-      const int64_t col = col0 + 8 * unit + (lane >> 2), r = row0 + m32 + 8 * (lane & 3);
+      ptx::ldmatrix_x4_trans(ptx::smem_u32(&tile[m * kUnits + (warp ^ (2 * (m >> 3 & 3) + (m & 1)))]), x[0], x[1], x[2], x[3]);
+      const int64_t r = row0 + 32 * k + 8 * (lane & 3);
       if (col < p.cols && r < p.rows) *reinterpret_cast<uint4*>(static_cast<T*>(p.dzt) + col * p.lddzt + r) = make_uint4(x[0], x[1], x[2], x[3]);
     }
   }
-  if (p.partial && p.over_rows && threadIdx.x < kTile) {
+  if (p.partial && p.over_rows && threadIdx.x < kWide) {
     float s = over[0][threadIdx.x];
 #pragma unroll
-    for (int w = 1; w < 8; ++w) s += over[w][threadIdx.x];
-    if (col0 + threadIdx.x < p.cols) p.partial[row0 / kTile * p.cols + col0 + threadIdx.x] = s;
+    for (int w = 1; w < kWideThreads / 32; ++w) s += over[w][threadIdx.x];
+    if (col0 + threadIdx.x < p.cols) p.partial[row0 / kWide * p.cols + col0 + threadIdx.x] = s;
   }
 }
 
@@ -118,9 +120,9 @@ __global__ void __launch_bounds__(256) act_grad_kernel(const ActGradParams p) {
     if (r < p.rows && c < p.cols) {
       d = to_float(static_cast<const T*>(p.dy)[r * p.lddy + c]);
       if (ACT != SP24_ACT_NONE) {
-        float slope;
-        act_and_slope<ACT>(to_float(static_cast<const T*>(p.z)[r * p.ldz + c]), &slope);
-        d *= slope;
+        float2 slope;
+        act_and_slope<ACT>(both(to_float(static_cast<const T*>(p.z)[r * p.ldz + c])), &slope);
+        d *= slope.x;
       }
       if (p.dz) static_cast<T*>(p.dz)[r * p.lddz + c] = round_to<T>(d);
     }
@@ -176,20 +178,21 @@ extern "C" sp24_status sp24_act_backward(sp24_dtype t, sp24_act act, int64_t row
   SP24_RETURN_IF(dbias && (!workspace || !aligned16(workspace) || workspace_bytes < sp24_act_backward_workspace_bytes(rows, cols, sum_over_rows)),
                  SP24_ERR_WORKSPACE);
   if (!dz && !dzt && !dbias) return SP24_OK;
-  const int64_t row_tiles = (rows + kTile - 1) / kTile, col_tiles = (cols + kTile - 1) / kTile;
+  const bool whole = t != SP24_F32 && cols % 8 == 0 && (!dzt || rows % 8 == 0) && whole_rows(dy, rows, lddy, 2, 16) &&
+                     (!reads_z || whole_rows(z, rows, ldz, 2, 16)) && whole_rows(dz, rows, lddz, 2, 16) && whole_rows(dzt, cols, lddzt, 2, 16);
+  const int64_t edge = whole ? kWide : kTile;  // (the workspace has room for the sums of the smaller tiles)
+  const int64_t row_tiles = (rows + edge - 1) / edge, col_tiles = (cols + edge - 1) / edge;
   SP24_RETURN_IF(row_tiles * col_tiles > 0x7fffffff, SP24_ERR_SHAPE);
   sp24_status st = check_arch();
   if (st != SP24_OK) return st;
   const ActGradParams p = {rows, cols, dy, z, dz, dzt, dbias ? static_cast<float*>(workspace) : nullptr, lddy, ldz, lddz, lddzt, sum_over_rows != 0};
-  const bool whole = t != SP24_F32 && cols % 8 == 0 && (!dzt || rows % 8 == 0) && whole_rows(dy, rows, lddy, 2, 16) &&
-                     (!reads_z || whole_rows(z, rows, ldz, 2, 16)) && (!dz || whole_rows(dz, rows, lddz, 2, 16)) &&
-                     (!dzt || whole_rows(dzt, cols, lddzt, 2, 16));
+  const dim3 grid((unsigned)(row_tiles * col_tiles));
   st = with_float_type(t, [&](auto type) {
     using T = typename decltype(type)::type;
     return with_act(act, [&](auto a) {
       if constexpr (sizeof(T) == 2)
-        if (whole) return launch_overlapped(act_grad_tile_kernel<T, decltype(a)::value>, dim3((unsigned)(row_tiles * col_tiles)), dim3(256), 0, s, 1, p);
-      return launch_overlapped(act_grad_kernel<T, decltype(a)::value>, dim3((unsigned)(row_tiles * col_tiles)), dim3(256), 0, s, 1, p);
+        if (whole) return launch_overlapped(act_grad_tile_kernel<T, decltype(a)::value>, grid, dim3(kWideThreads), 0, s, 1, p);
+      return launch_overlapped(act_grad_kernel<T, decltype(a)::value>, grid, dim3(256), 0, s, 1, p);
     });
   });
   if (st != SP24_OK || !dbias) return st;

@@ -21,7 +21,7 @@ __device__ __forceinline__ void gated_vector(int act, const uint4& g, const uint
   unpack<T>(g, y);
   device_with_act(act, [&](auto a) {
 #pragma unroll
-    for (int n = 0; n < P; ++n) y[n] = make_float2(act_value<decltype(a)::value>(y[n].x), act_value<decltype(a)::value>(y[n].y));
+    for (int n = 0; n < P; ++n) y[n] = act_value<decltype(a)::value>(y[n]);
   });
   if (gated) {
     Pairs<T> f;
@@ -183,10 +183,8 @@ __global__ void __launch_bounds__(kThreads) gated_act_grad_kernel(const GatedGra
 #pragma unroll
         for (int n = 0; n < P; ++n) {
           float2 slope;
-          du[n].x = act_and_slope<decltype(a)::value>(f[n].x, &slope.x);
-          du[n].y = act_and_slope<decltype(a)::value>(f[n].y, &slope.y);
+          du[n] = mul2(act_and_slope<decltype(a)::value>(f[n], &slope), d[n]);
           dg[n] = mul2(gated ? mul2(d[n], w[n]) : d[n], slope);
-          du[n] = mul2(du[n], d[n]);
         }
       });
       store_vector<WHOLE>(static_cast<T*>(p.dg) + row * p.lddg, i, F, s, pack<T>(dg));

@@ -222,7 +222,7 @@ static void choose_tile(const sp24_gemm_desc* d, bool has_c, bool conv, int& cta
     }
     // one m-block: the width that needs the fewest rounds of tiles, operand bytes per k as the tie-break
     // (without metadata columns two 256-column accumulators fit, so 256 x 256 keeps its epilogue overlapped)
-    const int widths[3] = {224, has_240 ? 240 : 0, k_major_b && d->ab_type != SP24_F32 ? 256 : 0};
+    const int widths[3] = {224, has_240 ? 240 : 0, d->ab_type != SP24_F32 ? 256 : 0};
     double best = 0.0;
     for (const int bn : widths) {
       if (bn == 0) continue;

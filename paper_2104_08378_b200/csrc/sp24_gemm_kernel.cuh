@@ -318,21 +318,37 @@ __device__ __forceinline__ void compute_row(const uint32_t (&r)[COLUMNS], const 
 }
 
 // Epilogue of sp24_linear, one thread's row of a box: z = row_scale * col_scale * acc + bias in place of the accumulators, then the
-// activation, the residual and the rounding, all in FP32.  col_scale: that of column `lane` of the box; the columns are the same for all lanes of
-// the warp, their scales go round by shuffles.
+// activation, the residual and the rounding, all in FP32, by pairs.  col_scales: the box's columns' scales in shared memory (the same for all lanes:
+// eight wide reads instead of a shuffle for each column), if it has any.
 template <int KIND, int COLUMNS>
-__device__ __forceinline__ void scale_row(uint32_t (&r)[COLUMNS], float scale, float col_scale, float bias) {
+__device__ __forceinline__ void scale_row(uint32_t (&r)[COLUMNS], float scale, bool scaled, uint32_t col_scales, float bias) {
+  auto pair = [&](int e, float2 f) {
+    const float2 a = KIND == 1 ? make_float2(__int2float_rn((int)r[e]), __int2float_rn((int)r[e + 1])) : make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1]));
+    const float2 z = fma2(a, f, both(bias));
+    r[e] = __float_as_uint(z.x);
+    r[e + 1] = __float_as_uint(z.y);
+  };
+  if (one_byte_operands(KIND) && scaled) {
 #pragma unroll
-  for (int e = 0; e < COLUMNS; ++e) {
-    const float a = KIND == 1 ? __int2float_rn((int)r[e]) : __uint_as_float(r[e]);
-    const float f = one_byte_operands(KIND) ? scale * __shfl_sync(~0u, col_scale, e) : scale;
-    r[e] = __float_as_uint(fmaf(a, f, bias));
+    for (int e = 0; e < COLUMNS; e += 4) {
+      uint32_t c[4];
+      ptx::ld_shared_v4(col_scales + 4 * e, c[0], c[1], c[2], c[3]);
+      pair(e, mul2(make_float2(__uint_as_float(c[0]), __uint_as_float(c[1])), both(scale)));
+      pair(e + 2, mul2(make_float2(__uint_as_float(c[2]), __uint_as_float(c[3])), both(scale)));
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < COLUMNS; e += 2) pair(e, both(scale));
   }
 }
 template <int ACT, int COLUMNS>
 __device__ __forceinline__ void activate_row(uint32_t (&r)[COLUMNS]) {
 #pragma unroll
-  for (int e = 0; e < COLUMNS; ++e) r[e] = __float_as_uint(act_value<ACT>(__uint_as_float(r[e])));
+  for (int e = 0; e < COLUMNS; e += 2) {
+    const float2 y = act_value<ACT>(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])));
+    r[e] = __float_as_uint(y.x);
+    r[e + 1] = __float_as_uint(y.y);
+  }
 }
 template <int COLUMNS>
 __device__ __forceinline__ void activate_row(uint32_t (&r)[COLUMNS], int act) {
@@ -437,6 +453,10 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
   constexpr int kRowsPerStore = 32 / kUnits;
   const int q = warp & 3, turn = (warp - kFirstEpiWarp) >> 2;  // lane quarter, and first box of this warp there
   uint8_t* stage = epi + (warp - kFirstEpiWarp) * 2048;
+  // LINEAR with scales of the columns: two buffers of a box's, behind all warps' stages
+  const bool scaled = LINEAR && one_byte_operands(KIND) && p.col_scale;
+  const uint32_t col_scales = ptx::smem_u32(epi) + WARPS * 2048 + (warp - kFirstEpiWarp) * 256;
+  uint32_t col_buffer = 0;
   const uint8_t* Cb = static_cast<const uint8_t*>(p.C);
   uint8_t* Db = static_cast<uint8_t*>(p.D);
   const size_t ldc_b = (size_t)p.ldc * CS, ldd_b = (size_t)p.ldd * CS;
@@ -586,7 +606,7 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
     uint32_t r[kCols], creg[P][W];
     float scale = 1.f, bias = 0.f, col_scale = 1.f;
     auto load_col_scale = [&](int col0) {  // lane e: that of column e of the box
-      if (LINEAR && one_byte_operands(KIND) && p.col_scale) col_scale = p.col_scale[min(col0 + lane, N - 1)];
+      if (scaled) col_scale = p.col_scale[min(col0 + lane, N - 1)];
     };
     auto load_scale = [&](int row0) {
       if (LINEAR) {
@@ -628,7 +648,12 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
       if (KIND == 0 && p.acc_f16) widen_f16_accumulators(r);
       bool again = false;
       if constexpr (LINEAR) {
-        scale_row<KIND>(r, scale, col_scale, bias);
+        if (scaled) {  // (the other buffer may still be read)
+          col_buffer ^= 128;
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(col_scales + col_buffer + 4 * lane), "f"(col_scale) : "memory");
+          __syncwarp();
+        }
+        scale_row<KIND>(r, scale, scaled, col_scales + col_buffer, bias);
         if (p.pre) {
           pack_row<CS>(r, p.cd_type, o);
           store_to(static_cast<uint8_t*>(p.pre), (size_t)p.ld_pre * CS, false, o, row0, col0);
@@ -1249,7 +1274,7 @@ sp24_status launch(const TileShape& tile, const sp24_gemm_desc* d, const GemmPar
   const bool staged = !LINEAR && C::staged_epilogue(cs, p.cd_col_major);
   int tile_m = kBlockM * CTAS * MBLK;
   const int warps = LINEAR ? kEpiWarps : epilogue_warps<KIND, SPARSE, BLOCK_N, CTAS, MBLK, B_MN>(d, tile_n);
-  p.epi_bytes = warps * (staged ? 4096 : 2048);
+  p.epi_bytes = warps * (staged ? 4096 : 2048) + (LINEAR && one_byte_operands(KIND) ? warps * 256 : 0);
   const int es = KIND == 0 ? 2 : (one_byte_operands(KIND) ? 1 : 4);
   const uint32_t atom_elems = kAtomBytes / es;
   const uint64_t a_cols = SPARSE ? d->K / 2 : d->K;
@@ -1391,6 +1416,8 @@ sp24_status launch_shape(TileShape t, bool sparse, bool b_mn, const sp24_gemm_de
     SP24_SHAPE(2, 240, 1, false)  // 2-byte outputs only
   }
   if constexpr (!tf32)  // dense variant only
+    if (is(2, 256, 1) && !sparse && b_mn) return launch<KIND, false, 256, 2, 1, true, LINEAR>(t, d, p, A, meta, B, s);
+  if constexpr (!tf32)
     if (is(2, 256, 2) && !sparse && !b_mn) return launch<KIND, false, 256, 2, 2, false, LINEAR>(t, d, p, A, meta, B, s);
   if (t.ctas == 1 && t.block_n == 128 && (t.mblk == 2 || t.mblk == kTallBlocks) && sparse && !b_mn)
     return launch<KIND, true, 128, 1, kTallBlocks, false, LINEAR>(t, d, p, A, meta, B, s);

@@ -7,7 +7,7 @@
 
 #include <type_traits>
 
-#include "sp24_common.cuh"
+#include "sp24_act.cuh"
 
 namespace sp24 {
 
@@ -172,19 +172,6 @@ struct RowSums {
     if (TOP) top_over_warp();
   }
 };
-
-// ---- pairs: two FP32 operations of one instruction, each rounded by itself --------------------------------------------------
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-  asm("{ .reg .b64 x, y; mov.b64 x, {%0, %1}; mov.b64 y, {%2, %3}; mul.rn.f32x2 x, x, y; mov.b64 {%0, %1}, x; }" : "+f"(a.x), "+f"(a.y) : "f"(b.x), "f"(b.y));
-  return a;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  asm("{ .reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mov.b64 z, {%0, %1}; fma.rn.f32x2 z, x, y, z; mov.b64 {%0, %1}, z; }"
-      : "+f"(c.x), "+f"(c.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return c;
-}
-__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
 // ---- rows in registers --------------------------------------------------------------------------------------------
 // A thread has V vectors of a row, number threadIdx.x + v * blockDim.x: 16 bytes of the type T that the operator works on, N elements, N / 2
