@@ -18,13 +18,14 @@ struct ActGradParams {
   int32_t over_rows;
 };
 
-// 16-bit types, all rows (of dzt too) whole vectors at 16-byte boundaries.  A block to a tile of 128 x 128 (rows of 256 bytes both ways), transposed on its way out of
+// 16-bit types, all rows (of dzt too) whole vectors at 16-byte boundaries.  A block to a tile of 128 x 128 (rows of 256 bytes both ways; of 64 x 64 where those
+// would leave SMs idle: 128 x 4096 5.4 -> 3.6 us), transposed on its way out of
 // shared memory by ldmatrix.trans: the eight rows of matrix i are 8 j + 2 i + b (j = 0..3, b = 0, 1), which leaves lane 4 c + j with eight
 // consecutive rows of column c, so that a warp stores eight segments of 64 bytes.  Unit u (16 bytes) of row m lies at
 // u ^ (2 (m >> 3 & 3) + (m & 1)): the eight rows of a matrix are in different banks.
-constexpr int kWide = 128, kUnits = kWide / 8, kWideThreads = 512;
-template <typename T, int ACT>
-__global__ void __launch_bounds__(kWideThreads) act_grad_tile_kernel(const ActGradParams p) {
+template <typename T, int ACT, int kWide>
+__global__ void __launch_bounds__(4 * kWide) act_grad_tile_kernel(const ActGradParams p) {
+  constexpr int kUnits = kWide / 8, kWideThreads = 4 * kWide;
   constexpr int kPasses = kWide * kUnits / kWideThreads, kRows = kWide / kPasses;
   __shared__ uint4 tile[kWide * kUnits];
   __shared__ float over[kWideThreads / 32][kWide];  // sums over the rows of each warp
@@ -180,7 +181,8 @@ extern "C" sp24_status sp24_act_backward(sp24_dtype t, sp24_act act, int64_t row
   if (!dz && !dzt && !dbias) return SP24_OK;
   const bool whole = t != SP24_F32 && cols % 8 == 0 && (!dzt || rows % 8 == 0) && whole_rows(dy, rows, lddy, 2, 16) &&
                      (!reads_z || whole_rows(z, rows, ldz, 2, 16)) && whole_rows(dz, rows, lddz, 2, 16) && whole_rows(dzt, cols, lddzt, 2, 16);
-  const int64_t edge = whole ? kWide : kTile;  // (the workspace has room for the sums of the smaller tiles)
+  const bool wide = whole && (rows + 127) / 128 * ((cols + 127) / 128) >= 2 * sm_count();
+  const int64_t edge = wide ? 2 * kTile : kTile;  // (the workspace has room for the sums of the smaller tiles)
   const int64_t row_tiles = (rows + edge - 1) / edge, col_tiles = (cols + edge - 1) / edge;
   SP24_RETURN_IF(row_tiles * col_tiles > 0x7fffffff, SP24_ERR_SHAPE);
   sp24_status st = check_arch();
@@ -191,7 +193,9 @@ extern "C" sp24_status sp24_act_backward(sp24_dtype t, sp24_act act, int64_t row
     using T = typename decltype(type)::type;
     return with_act(act, [&](auto a) {
       if constexpr (sizeof(T) == 2)
-        if (whole) return launch_overlapped(act_grad_tile_kernel<T, decltype(a)::value>, grid, dim3(kWideThreads), 0, s, 1, p);
+        if (whole)
+          return launch_overlapped(wide ? act_grad_tile_kernel<T, decltype(a)::value, 2 * kTile> : act_grad_tile_kernel<T, decltype(a)::value, kTile>, grid,
+                                   dim3((unsigned)(4 * edge)), 0, s, 1, p);
       return launch_overlapped(act_grad_kernel<T, decltype(a)::value>, grid, dim3(256), 0, s, 1, p);
     });
   });

@@ -341,17 +341,17 @@ inline bool whole_rows(const void* base, int64_t rows, int64_t ld, size_t es, si
 }
 
 // Teams, blocks and vectors to a thread for rows that a team holds in registers: a block to an SM, as many teams to a block as its threads
-// and the SM's rows allow.  Each thread has two vectors on their way where there are rows enough, one where most SMs have a row or two;
-// four in the longest rows.  (Registers: 1024 threads with one vector, 768 with two, 512 with four.)
+// and the SM's rows allow.  Each thread has two vectors on their way where there are rows enough, one where an SM has few; four in the
+// longest rows.  (Registers: 1024 threads with one vector, 768 with two, 512 with four.)
 constexpr int team_threads(int v) { return v == 1 ? 1024 : v == 2 ? 768 : 512; }
 constexpr int64_t kMostTeamVectors = 4 * team_threads(4);
 struct TeamLaunch {
   dim3 grid, block;
   int v;
-  // with_two: threads of a block with two vectors each, where they suffice
-  TeamLaunch(int64_t rows, int64_t vectors, int with_two = team_threads(2)) {
+  // with_two: threads of a block with two vectors each, where they suffice; from_rows: rows of an SM from which on they have two
+  TeamLaunch(int64_t rows, int64_t vectors, int from_rows, int with_two = team_threads(2)) {
     const int64_t sms = sm_count();
-    v = vectors > 2 * team_threads(2) ? 4 : vectors > team_threads(1) || rows > 2 * sms ? 2 : 1;
+    v = vectors > 2 * team_threads(2) ? 4 : vectors > team_threads(1) || rows > from_rows * sms ? 2 : 1;
     const int64_t most = v == 2 && vectors <= 2 * with_two ? with_two : team_threads(v);
     const int64_t lanes = (vectors + v - 1) / v;
     int64_t team = (lanes + 31) / 32 * 32;
