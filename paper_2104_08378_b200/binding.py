@@ -130,7 +130,8 @@ if hasattr(torch._C, "_cuda_getCurrentRawStream"):
 else:                          # a CPU-only build of torch has no CUDA tensors: every call is for the functions below
     class _native:
         gemm = gemm_i8_dequant = conv3x3_nhwc = compress = apply_mask = staticmethod(lambda *args: None)
-        rms_norm = rms_norm_backward = gated_act = gated_act_backward = act_backward = linear = staticmethod(lambda *args: None)
+        rms_norm = rms_norm_backward = gated_act = gated_act_backward = act_backward = linear = linear_backward = staticmethod(
+            lambda *args: None)
 
 # Addresses for the native form of the short calls, which does what the functions below do if all arguments are of the
 # ordinary kind, and returns None if not (then they do it themselves) or the status of a call that was refused.
@@ -744,7 +745,6 @@ def _linear(A, meta, Bt, *, bias, act, residual, row_scale, col_scale, pre, out,
     return out if z is None else (out, z)
 
 
-@_on_device_of("dy")
 def linear_backward(dy: torch.Tensor, pre: torch.Tensor | None, Bt: torch.Tensor, W: torch.Tensor, *, act: str | None = None,
                     meta: torch.Tensor | None = None, b_row_major: bool = False, cd_col_major: bool = False,
                     ws: torch.Tensor | None = None):
@@ -752,6 +752,15 @@ def linear_backward(dy: torch.Tensor, pre: torch.Tensor | None, Bt: torch.Tensor
     weights W [M, K] themselves: (dBt, dW, dbias).  dy and pre are [N, M] with cd_col_major, else [M, N]; Bt [N, K], or [K, N]
     with b_row_major; dBt has Bt's form.  With meta the entries of dW that the 2:4 pattern leaves out are zeros.  The
     residual's gradient is dy.  sp24_act_backward, then two dense products (and sp24_apply_mask)."""
+    done = _native.linear_backward(_ACT_BACKWARD, _ACT_BYTES, _GEMM, _META_BYTES, _APPLY_MASK, _workspaces, dy, pre, Bt, W, act,
+                                   meta, b_row_major, cd_col_major, ws)
+    if done is not None:
+        return done if type(done) is not int else _check(done, "sp24_linear_backward")
+    return _linear_backward(dy, pre, Bt, W, act=act, meta=meta, b_row_major=b_row_major, cd_col_major=cd_col_major, ws=ws)
+
+
+@_on_device_of("dy")
+def _linear_backward(dy, pre, Bt, W, *, act, meta, b_row_major, cd_col_major, ws):
     where = "sp24_linear_backward"
     _float_code(dy, where)
     _matrix(dy, where)

@@ -103,7 +103,9 @@ __global__ void __launch_bounds__(AHEAD ? team_threads(V) : 1024, 1) gated_act_r
   }
 }
 
-// Longer rows: a block to a row; for 8-bit results a pass before it for the row's maximum, behind which the caches have the row.
+// Longer rows: a block to a row, each thread with its first kKept vectors' results in registers (rows of up to 4096 vectors) and the others computed twice for
+// 8-bit results, the second time from the caches.
+constexpr int kKept = 4;
 template <typename T, typename OUT>
 __global__ void __launch_bounds__(1024, 1) gated_act_kernel(const GatedParams p) {
   constexpr int P = kVector<T> / 2;
@@ -120,24 +122,28 @@ __global__ void __launch_bounds__(1024, 1) gated_act_kernel(const GatedParams p)
       const uint4 a = load_vector<false>(g, i, K, shift);
       gated_vector<T>(p.act, a, u ? load_vector<false>(u, i, K, shift) : a, u != nullptr, f);
     };
-    float inv = 0.f;
+    Pairs<T> kept[kKept];
+    float top = 0.f, unused[1] = {}, inv = 0.f;
+    auto count = [&](const Pairs<T>& f) {
+#pragma unroll
+      for (int n = 0; n < P; ++n) top = max_abs(top, f[n].x, f[n].y);
+    };
+#pragma unroll
+    for (int v = 0; v < kKept; ++v) {
+      value(threadIdx.x + v * 1024, kept[v]);
+      if (is_code<OUT>) count(kept[v]);
+    }
     if (is_code<OUT>) {
-      float top = 0.f, unused[1] = {};
-#pragma unroll 2
-      for (int i = threadIdx.x; i < vectors; i += blockDim.x) {
+      for (int i = threadIdx.x + kKept * 1024; i < vectors; i += 1024) {
         Pairs<T> f;
         value(i, f);
-#pragma unroll
-        for (int n = 0; n < P; ++n) top = max_abs(top, f[n].x, f[n].y);
+        count(f);
       }
       sums.reduce<false, true>(unused, top, turn);
       const float scale = row_scale<OUT>(finite_or_nan(top), 1.f, &inv);
       if (threadIdx.x == 0) p.scale[row] = scale;
     }
-#pragma unroll 2
-    for (int i = threadIdx.x; i < vectors; i += blockDim.x) {
-      Pairs<T> f;
-      value(i, f);
+    auto store = [&](int i, Pairs<T>& f) {
       if constexpr (is_code<OUT>) {
 #pragma unroll
         for (int n = 0; n < P; ++n) f[n] = mul2(f[n], both(inv));
@@ -145,6 +151,13 @@ __global__ void __launch_bounds__(1024, 1) gated_act_kernel(const GatedParams p)
       } else {
         store_vector<false>(y, i, K, shift, pack<T>(f));
       }
+    };
+#pragma unroll
+    for (int v = 0; v < kKept; ++v) store(threadIdx.x + v * 1024, kept[v]);
+    for (int i = threadIdx.x + kKept * 1024; i < vectors; i += 1024) {
+      Pairs<T> f;
+      value(i, f);
+      store(i, f);
     }
   }
 }

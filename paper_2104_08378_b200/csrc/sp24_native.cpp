@@ -621,10 +621,88 @@ PyObject* linear(PyObject*, PyObject* const* v, Py_ssize_t n) {
   }
 }
 
+// linear_backward(addresses of sp24_act_backward, of its workspace's size, of sp24_gemm, of sp24_meta_bytes, of sp24_apply_mask, workspaces, dy, pre, Bt, W, act,
+// meta, b_row_major, cd_col_major, ws) -> (dBt, dW, dbias)
+PyObject* linear_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 15 || at::impl::torch_function_mode_enabled()) return none();
+  try {
+    for (int i = 12; i < 14; ++i)
+      if (v[i] != Py_True && v[i] != Py_False) return none();
+    Matrix dy, z, b, w;
+    const int act = act_code(v[10]);
+    if (act < 0 || !dy.init(v[6], -1, -1, -1)) return none();
+    const int t = type_code(dy.t->scalar_type());
+    if (!float_type(t) || !w.init(v[9], -1, -1, t) || !b.init(v[8], -1, -1, t)) return none();
+    const bool b_rows = v[12] == Py_True, cols_out = v[13] == Py_True;
+    const int64_t M = w.t->size(0), K = w.t->size(1), N = b.t->size(b_rows ? 1 : 0);
+    const int64_t rows = dy.t->size(0), cols = dy.t->size(1);
+    if (b.t->size(b_rows ? 0 : 1) != K || rows != (cols_out ? N : M) || cols != (cols_out ? M : N) || M % 16 || N % 16 || K % 16 || M == 0 || N == 0 || K == 0)
+      return none();
+    if (act != SP24_ACT_NONE && !z.init(v[7], rows, cols, t)) return none();
+    const void* meta = nullptr;
+    if (v[11] != Py_None) {
+      const at::Tensor* m = plain(v[11], 1);
+      if (t == SP24_F32 || m == nullptr || m->dim() != 1 || m->scalar_type() != at::kByte || (m->size(0) > 1 && m->stride(0) != 1) ||
+          m->get_device() != c10::cuda::current_device() ||
+          (size_t)m->size(0) != function<decltype(&sp24_meta_bytes)>(v[3])((sp24_dtype)t, M, K, SP24_META_TCGEN05))
+        return none();
+      meta = m->data_ptr();
+    }
+    const cudaStream_t stream = Stream().handle;
+    void* ws;
+    size_t ws_bytes;
+    if (!workspace(v[5], v[14], *dy.t, stream, &ws, &ws_bytes)) return none();
+    const auto act_fn = function<decltype(&sp24_act_backward)>(v[0]);
+    const auto act_bytes = function<decltype(&sp24_act_backward_workspace_bytes)>(v[1]);
+    const auto gemm_fn = function<decltype(&sp24_gemm)>(v[2]);
+    const auto mask_fn = function<decltype(&sp24_apply_mask)>(v[4]);
+    Result rx{Py_None, {}}, rw{Py_None, {}}, rb{Py_None, {}};
+    const int status = unlocked([&]() -> int {
+      const auto options = dy.t->options();
+      at::Tensor dz, dzt = at::empty({cols, rows}, options);
+      void* pdz = dy.p;
+      int64_t lddz = dy.ld;
+      if (act != SP24_ACT_NONE) {
+        dz = at::empty({rows, cols}, options);
+        pdz = dz.data_ptr();
+        lddz = cols;
+      }
+      rb.made = at::empty({M}, options.dtype(at::kFloat));
+      const size_t bytes = act_bytes(rows, cols, cols_out);
+      const at::Tensor sums = at::empty({(int64_t)bytes}, options.dtype(at::kByte));
+      int st = act_fn((sp24_dtype)t, (sp24_act)act, rows, cols, dy.p, dy.ld, z.p, z.ld, act != SP24_ACT_NONE ? pdz : nullptr, lddz, dzt.data_ptr(), rows,
+                      (float*)rb.made.data_ptr(), cols_out, sums.data_ptr(), bytes, stream);
+      if (st != SP24_OK) return st;
+      rx.made = at::empty({b.t->size(0), b.t->size(1)}, options);
+      rw.made = at::empty({M, K}, options);
+      const float one = 1.f, zero = 0.f;
+      // D = A B of dense A (rows_ x inner), B by rows if `by_rows`
+      auto product = [&](const void* A, int64_t lda, int64_t m, int64_t n_, int64_t inner, const void* B, int64_t ldb, bool by_rows, void* D, bool cols_) {
+        const sp24_order order = cols_ ? SP24_COL_MAJOR : SP24_ROW_MAJOR;
+        const int64_t ldd = cols_ ? m : n_;
+        const sp24_gemm_desc d = {(sp24_dtype)t, (sp24_dtype)t, m, n_, inner, lda, ldb, ldd, ldd, by_rows ? SP24_ROW_MAJOR : SP24_COL_MAJOR, order, order, 1};
+        return (int)gemm_fn(&d, &one, A, nullptr, B, &zero, nullptr, D, ws, ws_bytes, stream);
+      };
+      const void *tokens = cols_out ? pdz : dzt.data_ptr(), *features = cols_out ? dzt.data_ptr() : pdz;  // N x M, M x N
+      const int64_t ld_tokens = cols_out ? lddz : rows, ld_features = cols_out ? rows : lddz;
+      st = product(tokens, ld_tokens, N, K, M, w.p, w.ld, true, rx.made.data_ptr(), b_rows);
+      if (st != SP24_OK) return st;
+      st = product(features, ld_features, M, K, N, b.p, b.ld, !b_rows, rw.made.data_ptr(), false);
+      if (st != SP24_OK || meta == nullptr) return st;
+      return (int)mask_fn((sp24_dtype)t, M, K, rw.made.data_ptr(), K, meta, SP24_META_TCGEN05, rw.made.data_ptr(), K, stream);
+    });
+    if (status != SP24_OK) return PyLong_FromLong(status);
+    return Py_BuildValue("(NNN)", rx.object(), rw.object(), rb.object());
+  } catch (...) {
+    return none();
+  }
+}
+
 #define SP24_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SP24_METHOD(gemm), SP24_METHOD(gemm_i8_dequant), SP24_METHOD(conv3x3_nhwc), SP24_METHOD(compress),
                          SP24_METHOD(apply_mask), SP24_METHOD(rms_norm), SP24_METHOD(rms_norm_backward), SP24_METHOD(gated_act),
-                         SP24_METHOD(gated_act_backward), SP24_METHOD(act_backward), SP24_METHOD(linear), {nullptr, nullptr, 0, nullptr}};
+                         SP24_METHOD(gated_act_backward), SP24_METHOD(act_backward), SP24_METHOD(linear),
+                         SP24_METHOD(linear_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

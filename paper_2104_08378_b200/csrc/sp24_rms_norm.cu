@@ -119,7 +119,9 @@ __global__ void __launch_bounds__(team_threads(V), 1) rms_norm_rows_kernel(const
   }
 }
 
-// Longer rows: a block to a row, two passes over it (the second from the caches).
+// Longer rows: a block to a row, each thread with its first kKept vectors of h in registers (rows of up to 4096 vectors) and the others read twice, the second time
+// from the caches.
+constexpr int kKept = 4;
 template <typename T, typename OUT>
 __global__ void __launch_bounds__(1024, 1) rms_norm_kernel(const NormParams p) {
   constexpr int P = kVector<T> / 2;
@@ -138,19 +140,28 @@ __global__ void __launch_bounds__(1024, 1) rms_norm_kernel(const NormParams p) {
       return r ? add_packed<T>(a, load_vector<false>(r, i, K, shift)) : a;
     };
     auto weighted = [&](int i, Pairs<T>& f) {
+      if (!p.weight) return;
+      Pairs<T> w;
+      if (p.weight_f32 && sizeof(T) == 2) {
 #pragma unroll
-      for (int n = 0; n < P; ++n) {
-        const int k = i * kVector<T> - shift + 2 * n;
-        if (p.weight && k >= 0 && k < K) f[n].x *= load_weight<T>(p.weight, p.weight_f32, k);
-        if (p.weight && k + 1 >= 0 && k + 1 < K) f[n].y *= load_weight<T>(p.weight, p.weight_f32, k + 1);
+        for (int q = 0; q < 2; ++q) {
+          Pairs<float> half;
+          unpack<float>(load_vector<false>(static_cast<const float*>(p.weight), 2 * i + q, K, shift), half);
+          w[q * (P / 2)] = half[0];
+          w[q * (P / 2) + P / 2 - 1] = half[1];
+        }
+      } else {
+        unpack<T>(load_vector<false>(static_cast<const T*>(p.weight), i, K, shift), w);
       }
+#pragma unroll
+      for (int n = 0; n < P; ++n) f[n] = mul2(f[n], w[n]);
     };
+    uint4 kept[kKept];
     float2 sum2 = both(0.f);
     float top = 0.f;
-#pragma unroll 2
-    for (int i = threadIdx.x; i < vectors; i += blockDim.x) {
+    auto count = [&](int i, const uint4& v) {
       Pairs<T> f;
-      unpack<T>(value(i), f);
+      unpack<T>(v, f);
 #pragma unroll
       for (int n = 0; n < P; ++n) sum2 = fma2(f[n], f[n], sum2);
       if (is_code<OUT>) {
@@ -158,7 +169,12 @@ __global__ void __launch_bounds__(1024, 1) rms_norm_kernel(const NormParams p) {
 #pragma unroll
         for (int n = 0; n < P; ++n) top = max_abs(top, f[n].x, f[n].y);
       }
-    }
+    };
+#pragma unroll
+    for (int v = 0; v < kKept; ++v) kept[v] = value(threadIdx.x + v * 1024);
+#pragma unroll
+    for (int v = 0; v < kKept; ++v) count(threadIdx.x + v * 1024, kept[v]);
+    for (int i = threadIdx.x + kKept * 1024; i < vectors; i += 1024) count(i, value(i));
     float sum[1] = {sum2.x + sum2.y};
     sums.reduce<true, is_code<OUT>>(sum, top, turn);
     const float rstd = rsqrtf(sum[0] / (float)p.K + p.eps);
@@ -168,9 +184,7 @@ __global__ void __launch_bounds__(1024, 1) rms_norm_kernel(const NormParams p) {
       const float scale = row_scale<OUT>(top, rstd, &factor);
       if (threadIdx.x == 0) p.scale[row] = scale;
     }
-#pragma unroll 2
-    for (int i = threadIdx.x; i < vectors; i += blockDim.x) {
-      const uint4 v = value(i);
+    auto store = [&](int i, const uint4& v) {
       Pairs<T> f;
       unpack<T>(v, f);
       if (is_code<OUT>) weighted(i, f);
@@ -180,7 +194,10 @@ __global__ void __launch_bounds__(1024, 1) rms_norm_kernel(const NormParams p) {
       if (h) store_vector<false>(h, i, K, shift, v);
       if constexpr (is_code<OUT>) store_codes<false, OUT>(y, i, K, shift, f);
       else store_vector<false>(y, i, K, shift, pack<T>(f));
-    }
+    };
+#pragma unroll
+    for (int v = 0; v < kKept; ++v) store(threadIdx.x + v * 1024, kept[v]);
+    for (int i = threadIdx.x + kKept * 1024; i < vectors; i += 1024) store(i, value(i));
   }
 }
 
@@ -338,15 +355,21 @@ __global__ void __launch_bounds__(AHEAD ? kAheadThreads : team_threads(V), 1) rm
   }
 }
 
-// Longer rows: a block to a row, two passes over it, the block's part of dweight in the workspace.
+// Longer rows: a block to a row, two passes over it (the second from the caches).  The block's part of dweight: of each thread's first kKept vectors in
+// registers (rows of up to 4096 vectors), of the others in the workspace.
 template <typename T>
 __global__ void __launch_bounds__(1024, 1) rms_norm_grad_kernel(const NormGradParams p) {
-  constexpr int P = kVector<T> / 2;
+  constexpr int N = kVector<T>, P = N / 2;
   __shared__ RowSums sums;
   int turn = 0;
-  const int K = (int)p.K, vectors = (K + kVector<T> - 1) / kVector<T>;
+  const int K = (int)p.K, vectors = (K + N - 1) / N;
   wait_for_stream();
   float* part = p.partial ? p.partial + blockIdx.x * p.K : nullptr;
+  Pairs<T> acc[kKept];
+#pragma unroll
+  for (int v = 0; v < kKept; ++v)
+#pragma unroll
+    for (int n = 0; n < P; ++n) acc[v][n] = both(0.f);
   bool first = true;
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, first = false) {
     const T* dy = static_cast<const T*>(p.dy) + row * p.lddy;
@@ -354,38 +377,70 @@ __global__ void __launch_bounds__(1024, 1) rms_norm_grad_kernel(const NormGradPa
     const T* dh = p.dh ? static_cast<const T*>(p.dh) + row * p.lddh : nullptr;
     T* dx = static_cast<T*>(p.dx) + row * p.lddx;
     const float rstd = p.rstd[row];
-    auto weight = [&](int k) { return p.weight && k < K ? load_weight<T>(p.weight, p.weight_f32, k) : 1.f; };
     auto load = [&](int i, Pairs<T>& g, Pairs<T>& f) {
       unpack<T>(load_vector<false>(dy, i, K, 0), g);
       unpack<T>(load_vector<false>(h, i, K, 0), f);
     };
-    float2 sum2 = both(0.f);
-    for (int i = threadIdx.x; i < vectors; i += blockDim.x) {
-      Pairs<T> g, f;
-      load(i, g, f);
+    auto weighted = [&](int i, Pairs<T>& f) {
+      if (!p.weight) return;
 #pragma unroll
       for (int n = 0; n < P; ++n) {
-        const int k = i * kVector<T> + 2 * n;
-        sum2 = fma2(mul2(g[n], make_float2(weight(k), weight(k + 1))), f[n], sum2);
+        const int k = i * N + 2 * n;
+        f[n] = mul2(f[n], make_float2(k < K ? load_weight<T>(p.weight, p.weight_f32, k) : 0.f, k + 1 < K ? load_weight<T>(p.weight, p.weight_f32, k + 1) : 0.f));
       }
+    };
+    float2 sum2 = both(0.f);
+#pragma unroll 4
+    for (int i = threadIdx.x; i < vectors; i += 1024) {
+      Pairs<T> g, f;
+      load(i, g, f);
+      weighted(i, g);
+#pragma unroll
+      for (int n = 0; n < P; ++n) sum2 = fma2(g[n], f[n], sum2);
     }
     float sum[1] = {sum2.x + sum2.y}, unused = 0.f;
     sums.reduce<true, false>(sum, unused, turn);
     const float along = -sum[0] / (float)p.K * rstd * rstd;
-    for (int i = threadIdx.x; i < vectors; i += blockDim.x) {
-      Pairs<T> g, f, d = {};
-      load(i, g, f);
+    auto finish = [&](int i, Pairs<T>& g, const Pairs<T>& f) {
+      Pairs<T> d = {};
       if (dh) unpack<T>(load_vector<false>(dh, i, K, 0), d);
+      weighted(i, g);
 #pragma unroll
-      for (int n = 0; n < P; ++n) {
-        const int k = i * kVector<T> + 2 * n;
-        if (part && k < K) part[k] = fmaf(g[n].x * f[n].x, rstd, first ? 0.f : part[k]);
-        if (part && k + 1 < K) part[k + 1] = fmaf(g[n].y * f[n].y, rstd, first ? 0.f : part[k + 1]);
-        g[n] = fma2(fma2(f[n], both(along), mul2(g[n], make_float2(weight(k), weight(k + 1)))), both(rstd), d[n]);
-      }
+      for (int n = 0; n < P; ++n) g[n] = fma2(fma2(f[n], both(along), g[n]), both(rstd), d[n]);
       store_vector<false>(dx, i, K, 0, pack<T>(g));
+    };
+#pragma unroll
+    for (int v = 0; v < kKept; ++v) {
+      const int i = threadIdx.x + v * 1024;
+      Pairs<T> g, f;
+      load(i, g, f);
+#pragma unroll
+      for (int n = 0; n < P; ++n) acc[v][n] = fma2(mul2(g[n], f[n]), both(rstd), acc[v][n]);
+      finish(i, g, f);
+    }
+    for (int i = threadIdx.x + kKept * 1024; i < vectors; i += 1024) {
+      Pairs<T> g, f;
+      load(i, g, f);
+      if (part) {
+#pragma unroll
+        for (int n = 0; n < P; ++n) {
+          const int k = i * N + 2 * n;
+          if (k < K) part[k] = fmaf(g[n].x * f[n].x, rstd, first ? 0.f : part[k]);
+          if (k + 1 < K) part[k + 1] = fmaf(g[n].y * f[n].y, rstd, first ? 0.f : part[k + 1]);
+        }
+      }
+      finish(i, g, f);
     }
   }
+  if (!part) return;
+#pragma unroll
+  for (int v = 0; v < kKept; ++v)
+#pragma unroll
+    for (int n = 0; n < P; ++n) {
+      const int k = (threadIdx.x + v * 1024) * N + 2 * n;
+      if (k < K) part[k] = acc[v][n].x;
+      if (k + 1 < K) part[k + 1] = acc[v][n].y;
+    }
 }
 
 // out[k] = the sum of `parts` rows, in their order within each of eight shares and then the shares in theirs.
@@ -514,6 +569,7 @@ extern "C" sp24_status sp24_rms_norm_backward(sp24_dtype t, int64_t rows, int64_
       };
       return weight && weight_type == SP24_F32 ? launch(TypeOf<float>{}) : launch(TypeOf<T>{});
     }
+    if (blocks > sm_count()) blocks = sm_count();
     return launch_overlapped(rms_norm_grad_kernel<T>, dim3((unsigned)blocks), dim3(1024), 0, s, 1, p);
   });
   if (st != SP24_OK || !dweight) return st;

@@ -49,6 +49,10 @@ def calls(sp):
     yield lambda: sp.linear(vals, meta, X, bias=bias, act="gelu", residual=res, pre=True, cd_col_major=True)
     yield lambda: sp.linear(vals, meta, X, cd="f32")
     yield lambda: sp.linear(v8, m8, X8, row_scale=rs, col_scale=cs)
+    W = sp.decompress(vals, meta)
+    dz, Xt = rand((48, 64), "bf16", 15), rand((128, 48), "bf16", 16)
+    yield lambda: sp.linear_backward(dz, res, X, W, act="gelu", meta=meta, cd_col_major=True)
+    yield lambda: sp.linear_backward(dz.T.contiguous(), None, Xt, W, b_row_major=True)
     yield lambda: sp.linear(i8, None, X8, a_is_dense=True, cd="f16", pre=torch.empty((64, 32), dtype=torch.float16, device="cuda"))
 
 
@@ -121,7 +125,7 @@ def test_refusals(sp, monkeypatch, silent):
 
 
 @pytest.mark.parametrize("offset,pad", [(0, 0), (1, 1), (3, 5), (8, 8)])
-@pytest.mark.parametrize("K", [1, 7, 64, 250, 1531, 4096, 17000])
+@pytest.mark.parametrize("K", [1, 7, 64, 250, 1531, 4096, 17000, 33001])
 def test_outputs_stay_inside_their_rows(sp, offset, pad, K):
     """Results into the middle of wider matrices, at every alignment: what surrounds them keeps its bytes."""
     rows = 5
