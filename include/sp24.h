@@ -392,7 +392,8 @@ sp24_status sp24_prune_2d(sp24_dtype t, int64_t M, int64_t K, const void* x, int
  *   weight: K values of weight_type (t or SP24_F32), or NULL for ones.
  *   scale: rows floats for 8-bit results, else ignored.  rstd: rows floats that receive 1 / sqrt(mean(h^2) + eps), or NULL.
  *   h and y may each be the same buffer, with the same leading dimension, as x or residual (y: if out_type == t), but not
- *   each other.  Else outputs overlap neither inputs nor each other. */
+ *   each other.  Else outputs overlap neither inputs nor each other.
+ *   mean(h^2) is held in FP32: rows with values above about 10^19 overflow it and give zeros (scale 0). */
 sp24_status sp24_rms_norm(sp24_dtype t, int64_t rows, int64_t K, const void* x, int64_t ldx, const void* residual,
                           int64_t ldr, const void* weight, sp24_dtype weight_type, float eps, void* h, int64_t ldh,
                           sp24_dtype out_type, void* y, int64_t ldy, float* scale, float* rstd, void* stream);
@@ -403,7 +404,7 @@ sp24_status sp24_rms_norm(sp24_dtype t, int64_t rows, int64_t K, const void* x, 
  * both x and the residual.  Everything in FP32, dx rounded once to t.  dweight: K floats, or NULL if it is not wanted.
  *   dx may be the same buffer as dy, h or dh (same leading dimension).
  *   workspace: sp24_rms_norm_backward_workspace_bytes(rows, K) bytes (0 for NULL dweight), 16-byte aligned, contents of no
- *   matter before or after.  The rows' sums are added in an order that rows and K fix: the same call gives the same bits. */
+ *   matter before or after.  The rows' sums are added in an order that rows, K and the device fix: the same call gives the same bits. */
 size_t sp24_rms_norm_backward_workspace_bytes(int64_t rows, int64_t K);
 sp24_status sp24_rms_norm_backward(sp24_dtype t, int64_t rows, int64_t K, const void* dy, int64_t lddy, const void* h,
                                    int64_t ldh, const void* weight, sp24_dtype weight_type, const float* rstd,

@@ -774,6 +774,8 @@ def _linear_backward(dy, pre, Bt, W, *, act, meta, b_row_major, cd_col_major, ws
     _refuse(meta is not None and dy.dtype == torch.float32, ERR_DTYPE, where)   # (apply_mask knows the 2:4 pattern only)
     if meta is not None:
         _vector(meta, meta_bytes(_FROM_TORCH[W.dtype], M, K), where, dy, (torch.uint8,))
+    if N == 0:
+        return Bt.new_empty(Bt.shape), torch.zeros_like(W), dy.new_zeros(M, dtype=torch.float32)
     dz, dzt, dbias = act_backward(dy, pre, act=act, cd_col_major=cd_col_major)
     tokens, features = (dz, dzt) if cd_col_major else (dzt, dz)          # [N, M], [M, N]
     dBt = gemm(tokens, None, W, a_is_dense=True, b_row_major=True, cd_col_major=b_row_major, ws=ws)

@@ -256,7 +256,7 @@ extern "C" sp24_status sp24_gated_act_backward(sp24_dtype t, sp24_act act, int64
                                                const void* g, int64_t ldg, const void* u, int64_t ldu, void* dg, int64_t lddg, void* du,
                                                int64_t lddu, void* stream) {
   SP24_RETURN_IF(!is_float_type(t), SP24_ERR_DTYPE);
-  SP24_RETURN_IF(!is_act(act) || (!u && du), SP24_ERR_UNSUPPORTED);
+  SP24_RETURN_IF(!is_act(act) || (!u && du) || (du && du == dg), SP24_ERR_UNSUPPORTED);
   SP24_RETURN_IF(rows < 0 || F < 1 || F > kMostColumns, SP24_ERR_SHAPE);
   if (rows == 0) return SP24_OK;
   SP24_RETURN_IF(!dy || !g || !dg || (u && !du), SP24_ERR_NULL);

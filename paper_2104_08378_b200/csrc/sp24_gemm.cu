@@ -606,6 +606,7 @@ extern "C" sp24_status sp24_linear(const sp24_gemm_desc* d, const sp24_linear_ep
   SP24_RETURN_IF(d == nullptr || e == nullptr, SP24_ERR_NULL);
   SP24_RETURN_IF((int)e->act < SP24_ACT_NONE || (int)e->act > SP24_ACT_GELU_TANH, SP24_ERR_UNSUPPORTED);
   SP24_RETURN_IF(e->col_scale && elem_bytes(d->ab_type) != 1, SP24_ERR_UNSUPPORTED);
+  SP24_RETURN_IF(e->pre && (e->pre == D || e->pre == e->residual), SP24_ERR_UNSUPPORTED);
   return run_gemm(d, nullptr, A, meta, B, nullptr, e->residual, D, workspace, workspace_bytes, stream, nullptr, nullptr, false, e);
 }
 

@@ -480,7 +480,7 @@ extern "C" sp24_status sp24_rms_norm(sp24_dtype t, int64_t rows, int64_t K, cons
   SP24_RETURN_IF(!is_float_type(t) || (out_type != t && !is_code_type(out_type)), SP24_ERR_DTYPE);
   SP24_RETURN_IF(weight && weight_type != t && weight_type != SP24_F32, SP24_ERR_DTYPE);
   SP24_RETURN_IF(rows < 0 || K < 1 || K > kMostColumns, SP24_ERR_SHAPE);
-  SP24_RETURN_IF(!(eps >= 0.f) || (h && !residual), SP24_ERR_UNSUPPORTED);
+  SP24_RETURN_IF(!(eps >= 0.f) || (h && !residual) || (h && h == y), SP24_ERR_UNSUPPORTED);
   if (rows == 0) return SP24_OK;
   SP24_RETURN_IF(!x || !y || (is_code_type(out_type) && !scale), SP24_ERR_NULL);
   SP24_RETURN_IF(!row_fits(rows, K, ldx) || (residual && !row_fits(rows, K, ldr)) || (h && !row_fits(rows, K, ldh)) || !row_fits(rows, K, ldy), SP24_ERR_STRIDE);

@@ -1,6 +1,9 @@
 """The linear layer's product with scales, bias, activation and residual, and its gradients, against plain implementations in 64
 bits; and the operators of a feed-forward layer one after the other."""
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -147,6 +150,33 @@ def test_values_that_are_not_finite(sp):
 def test_nothing_to_do(sp):
     _, A, meta, X = layer(sp, 64, 32, 64, "bf16", False, False, 12)
     assert sp.linear(A, meta, X[:0], act="silu", cd_col_major=True).shape == (0, 64)
+    W, none = sp.decompress(A, meta), X[:0]
+    dX, dW, db = sp.linear_backward(none.new_empty(0, 64), none.new_empty(0, 64), none, W, act="silu", cd_col_major=True)
+    assert dX.shape == (0, 64) and dW.shape == W.shape and not dW.any() and db.shape == (64,) and not db.any()
+
+
+def test_the_first_calls_may_be_captured():
+    """A process whose first calls of the operators on rows are made inside a capture (the products load their kernels before: their
+    first call outside)."""
+    code = (
+        "import torch\n"
+        "from paper_2104_08378_b200 import binding as sp\n"
+        "x = torch.randn(64, 1024, device='cuda').bfloat16(); w = torch.randn(1024, device='cuda').bfloat16()\n"
+        "g = torch.cuda.CUDAGraph()\n"
+        "with torch.cuda.graph(g):\n"
+        "    y, h, s, r = sp.rms_norm(x, w, residual=x, quant='e4m3', with_rstd=True)\n"
+        "    a, t = sp.gated_act(x[:, :512], x[:, 512:], quant='i8')\n"
+        "    d = sp.rms_norm_backward(x, h, w, r)\n"
+        "    e = sp.gated_act_backward(x, x, x)\n"
+        "    f = sp.act_backward(x, x, act='gelu')\n"
+        "g.replay(); torch.cuda.synchronize()\n"
+        "want = sp.rms_norm(x, w, residual=x, quant='e4m3'); assert torch.equal(want[0].view(torch.uint8), y.view(torch.uint8))\n"
+        "assert torch.equal(sp.gated_act_backward(x, x, x)[0], e[0]) and torch.equal(sp.rms_norm_backward(x, h, w, r)[1], d[1])\n"
+        "assert torch.equal(sp.act_backward(x, x, act='gelu')[1], f[1])\n"
+        "print('same')\n")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0 and done.stdout.split()[-1:] == ["same"], done
 
 
 @pytest.mark.parametrize("t", ["bf16", "f16", "f32"])

@@ -193,3 +193,21 @@ def test_a_row_does_not_depend_on_the_others(sp, t, K):
         b = sp.rms_norm(x[rows], w, quant="i8")
         assert torch.equal(a[0], y[rows]) and torch.equal(a[3], rstd[rows]) and torch.equal(b[0], q[rows]) and torch.equal(b[2], scale[rows])
         assert torch.equal(sp.rms_norm_backward(r[rows], x[rows], w, rstd[rows], dh=y[rows])[0], dx[rows])
+
+
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+def test_small_and_large_values(sp, t):
+    """The sum with the residual is rounded once, subnormal values and overflows to infinity included; norms of rows of subnormals, and of rows whose
+    squares leave FP32."""
+    x, r = rand((4, 264), t, 31), rand((4, 264), t, 32)
+    tiny = 2.0 ** -20 if t == "f16" else 2.0 ** -130
+    x[0], r[0] = x[0] * tiny, r[0] * tiny
+    x[1, :8], r[1, :8] = (60000.0, 60000.0) if t == "f16" else (3e38, 3e38)
+    y, h, _, rstd = sp.rms_norm(x, residual=r, eps=0.0 if t == "f16" else 1e-30, with_rstd=True)
+    assert torch.equal(h, (x.double() + r.double()).to(DTYPE[t])) and torch.isinf(h[1, :8]).all()
+    n, _ = rms_norm64(h[[0, 2, 3]], None, 0.0 if t == "f16" else 1e-30)
+    close(y[[0, 2, 3]], n, t, ARITHMETIC * n.abs() + (0 if t == "f16" else 1e-20))
+    if t == "bf16":
+        big = torch.full((1, 264), 1e30, dtype=torch.bfloat16, device="cuda")
+        y, _, scale, _ = sp.rms_norm(big, quant="i8")
+        assert float(scale) == 0 and not sp.rms_norm(big)[0].any()

@@ -10,7 +10,7 @@ ONE = ctypes.c_void_p(4096)
 F = ctypes.c_float
 
 
-def norm(t=sp.BF16, rows=4, K=64, x=ONE, ldx=64, r=ONE, ldr=64, w=ONE, wt=sp.BF16, eps=1e-6, h=ONE, ldh=64, out=sp.BF16, y=ONE,
+def norm(t=sp.BF16, rows=4, K=64, x=ONE, ldx=64, r=ONE, ldr=64, w=ONE, wt=sp.BF16, eps=1e-6, h=ctypes.c_void_p(8192), ldh=64, out=sp.BF16, y=ONE,
          ldy=64, scale=ONE, rstd=ONE):
     return sp.lib.sp24_rms_norm(t, rows, K, x, ldx, r, ldr, w, wt, F(eps), h, ldh, out, y, ldy, scale, rstd, None)
 
@@ -18,7 +18,7 @@ def norm(t=sp.BF16, rows=4, K=64, x=ONE, ldx=64, r=ONE, ldr=64, w=ONE, wt=sp.BF1
 @pytest.mark.parametrize("status,args", [
     (2, {"t": sp.I8}), (2, {"t": sp.I32}), (2, {"out": sp.F16}), (2, {"out": sp.I32}), (2, {"wt": sp.F16}), (2, {"t": 99}),
     (3, {"rows": -1}), (3, {"K": 0}), (3, {"K": 2 ** 30 + 1}),
-    (6, {"eps": -1.0}), (6, {"eps": float("nan")}), (6, {"r": None}),
+    (6, {"eps": -1.0}), (6, {"h": ONE}), (6, {"eps": float("nan")}), (6, {"r": None}),
     (1, {"x": None}), (1, {"y": None}), (1, {"out": sp.I8, "scale": None}),
     (4, {"ldx": 63}), (4, {"ldr": 63}), (4, {"ldh": 0}), (4, {"ldy": -64}),
     (5, {"x": ctypes.c_void_p(4097)}), (5, {"w": ctypes.c_void_p(4098), "wt": sp.F32}), (5, {"rstd": ctypes.c_void_p(4098)}),
@@ -69,7 +69,7 @@ def gated(t=sp.BF16, act=3, rows=4, F=64, g=ONE, ldg=64, u=ONE, ldu=64, out=sp.B
     return sp.lib.sp24_gated_act(t, act, rows, F, g, ldg, u, ldu, out, y, ldy, scale, None)
 
 
-def gated_backward(t=sp.BF16, act=3, rows=4, F=64, dy=ONE, lddy=64, g=ONE, ldg=64, u=ONE, ldu=64, dg=ONE, lddg=64, du=ONE, lddu=64):
+def gated_backward(t=sp.BF16, act=3, rows=4, F=64, dy=ONE, lddy=64, g=ONE, ldg=64, u=ONE, ldu=64, dg=ONE, lddg=64, du=ctypes.c_void_p(8192), lddu=64):
     return sp.lib.sp24_gated_act_backward(t, act, rows, F, dy, lddy, g, ldg, u, ldu, dg, lddg, du, lddu, None)
 
 
@@ -87,7 +87,7 @@ def test_gated(status, args):
 
 
 @pytest.mark.parametrize("status,args", [
-    (2, {"t": sp.I32}), (6, {"act": 9}), (6, {"u": None}), (3, {"F": 0}), (1, {"dy": None}), (1, {"g": None}), (1, {"dg": None}),
+    (2, {"t": sp.I32}), (6, {"act": 9}), (6, {"u": None}), (6, {"du": ONE}), (3, {"F": 0}), (1, {"dy": None}), (1, {"g": None}), (1, {"dg": None}),
     (1, {"du": None}), (4, {"lddy": 1}), (4, {"ldg": 1}), (4, {"ldu": 1}), (4, {"lddg": 1}), (4, {"lddu": 1}),
     (5, {"dg": ctypes.c_void_p(4097)}), (0, {"rows": 0})])
 def test_gated_backward(status, args):
@@ -104,7 +104,7 @@ def test_act_backward(status, args):
 
 
 def linear(ab=sp.BF16, cd=sp.BF16, M=64, N=32, K=64, lda=32, ldb=64, ldc=32, ldd=32, order=0, dense=0, act=1, row_scale=ONE, col_scale=None, bias=ONE,
-           residual=ONE, pre=ONE, ld_pre=32, A=ONE, meta=ONE, B=ONE, D=ONE, ws=ONE, ws_bytes=256):
+           residual=ONE, pre=ctypes.c_void_p(8192), ld_pre=32, A=ONE, meta=ONE, B=ONE, D=ctypes.c_void_p(12288), ws=ONE, ws_bytes=256):
     d = sp.GemmDesc(ab, cd, M, N, K, lda, ldb, ldc, ldd, sp.COL_MAJOR, 0, order, dense)
     e = sp.LinearEpilogue(row_scale, col_scale, bias, act, residual, pre, ld_pre)
     return sp.lib.sp24_linear(ctypes.byref(d), ctypes.byref(e), A, meta, B, D, ws, ws_bytes, None)
@@ -112,7 +112,7 @@ def linear(ab=sp.BF16, cd=sp.BF16, M=64, N=32, K=64, lda=32, ldb=64, ldc=32, ldd
 
 @pytest.mark.parametrize("status,args", [
     (2, {"ab": sp.I32}), (2, {"cd": sp.F16}), (2, {"ab": sp.I8, "cd": sp.I32}), (2, {"ab": sp.I8, "cd": sp.I8}), (2, {"ab": sp.E4M3, "cd": sp.I32}),
-    (6, {"ab": sp.F32, "cd": sp.F16}), (6, {"act": 7}), (6, {"act": -1}), (6, {"col_scale": ONE}), (6, {"order": 1, "ldd": 64}), (6, {"order": 3}),
+    (6, {"ab": sp.F32, "cd": sp.F16}), (6, {"act": 7}), (6, {"pre": ONE}), (6, {"pre": ctypes.c_void_p(12288)}), (6, {"act": -1}), (6, {"col_scale": ONE}), (6, {"order": 1, "ldd": 64}), (6, {"order": 3}),
     (3, {"M": 40}), (3, {"N": 24}), (3, {"K": 72}), (3, {"ab": sp.I8, "M": 48}), (3, {"M": -16}),
     (1, {"A": None}), (1, {"meta": None}), (1, {"B": None}), (1, {"D": None}), (7, {"ws": None}), (7, {"ws_bytes": 255}),
     (4, {"lda": 24}), (4, {"ldb": 56}), (4, {"ldc": 24}), (4, {"ldd": 36}), (4, {"ld_pre": 24}), (4, {"ld_pre": 36}),
