@@ -35,8 +35,9 @@ __device__ __forceinline__ void gated_vector(int act, const uint4& g, const uint
 // AHEAD: the team's next row is on its way from before this one's activations to the end of it, in registers of its own (two sets in
 // turn): the exponentials and reciprocals take half as long as the memory does.  Else it sets out behind them, and more teams, each at another
 // place of its row, hide that.
+constexpr int many_threads(int v) { return v == 2 ? 1024 : 768; }
 template <typename T, typename OUT, int V, bool AHEAD, bool WHOLE>
-__global__ void __launch_bounds__(AHEAD ? team_threads(V) : 1024, 1) gated_act_rows_kernel(const GatedParams p) {
+__global__ void __launch_bounds__(AHEAD ? team_threads(V) : many_threads(V), 1) gated_act_rows_kernel(const GatedParams p) {
   constexpr int N = kVector<T>, P = N / 2;
   __shared__ RowSums sums;
   int turn = 0;
@@ -238,15 +239,23 @@ extern "C" sp24_status sp24_gated_act(sp24_dtype t, sp24_act act, int64_t rows, 
     return with_out_type<T>(out_type, [&](auto out) {
       using OUT = typename decltype(out)::type;
       if (vectors > kMostTeamVectors) return launch_overlapped(gated_act_kernel<T, OUT>, dim3((unsigned)(rows < 65535 ? rows : 65535)), dim3(1024), 0, s, 1, p);
-      // Two vectors to a thread: 768 threads with the next row ahead, or 1024 without, if that puts half as many threads again to work (team sizes
-      // differ): silu bf16 8192 x 8192 -> e4m3 69.1, 57.5 us, x 5120 39.1, 37.9; not x 6144 43.6, 47.5, x 4096 29.7, 29.3.
+      // Where a row's team leaves threads out (768 of them with two vectors and the next row ahead), more teams without it: two vectors and 1024 threads,
+      // if that puts half as many threads again to work (silu bf16 8192 x 8192 -> e4m3 69.1, 57.5 us, x 5120 39.1, 37.9; not x 6144 43.6, 47.5,
+      // x 4096 29.7, 29.3); for 8-bit results of rows of one team, which all wait for the maximum, two teams with four vectors if there are many
+      // rows (8192 x 12288 89.7, 85.5, x 9216 77.5, 74.3; not 1024 x 12288 13.5, 15.0, nor -> bf16 92.5, 95.4).
       const int64_t team = ((vectors + 1) / 2 + 31) / 32 * 32;
       const bool many = vectors <= 1024 && 2 * (1024 / team) >= 3 * (team_threads(2) / team);
-      const TeamLaunch at(rows, vectors, 2, many ? 1024 : team_threads(2));
-      const auto kernel = at.v == 2 && many
-                              ? (whole ? gated_act_rows_kernel<T, OUT, 2, false, true> : gated_act_rows_kernel<T, OUT, 2, false, false>)
-                              : with_flags([](auto four, auto two, auto whole) { return gated_act_rows_kernel<T, OUT, four.value ? 4 : two.value ? 2 : 1, true, whole.value>; },
-                                           at.v == 4, at.v >= 2, whole);
+      const bool two_teams = is_code_type(out_type) && vectors > 1024 && vectors <= 2 * many_threads(4) && rows >= 32 * (int64_t)sm_count();
+      TeamLaunch at(rows, vectors, 2, many ? many_threads(2) : team_threads(2));
+      if (two_teams) {
+        const unsigned of_four = (unsigned)((vectors + 3) / 4 + 31) / 32 * 32;
+        at.block = dim3(of_four, many_threads(4) / of_four);
+        at.grid = dim3((unsigned)sm_count());
+      }
+      const auto kernel = two_teams               ? (whole ? gated_act_rows_kernel<T, OUT, 4, false, true> : gated_act_rows_kernel<T, OUT, 4, false, false>)
+                          : at.v == 2 && many ? (whole ? gated_act_rows_kernel<T, OUT, 2, false, true> : gated_act_rows_kernel<T, OUT, 2, false, false>)
+                                                  : with_flags([](auto four, auto two, auto whole) { return gated_act_rows_kernel<T, OUT, four.value ? 4 : two.value ? 2 : 1, true, whole.value>; },
+                                                               at.v == 4, at.v >= 2, whole);
       return launch_overlapped(kernel, at.grid, at.block, 0, s, 1, p);
     });
   });

@@ -169,3 +169,15 @@ def test_captured(sp):
     graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("t,F", [("bf16", 12288), ("bf16", 9001), ("f16", 8192), ("f32", 4096), ("f32", 5000), ("bf16", 5120), ("bf16", 20000)])
+def test_a_row_does_not_depend_on_the_others(sp, t, F):
+    """Enough rows for every arrangement of teams: the same bits as a few by themselves."""
+    rows = 4800
+    g, u = rand((rows, F), t, 18), rand((rows, F), t, 19)
+    for quant in (None, "i8"):
+        y, scale = sp.gated_act(g, u, act="gelu", quant=quant)
+        for some in (slice(0, 1), slice(3201, 3209), slice(4400, 4800)):
+            y2, scale2 = sp.gated_act(g[some], u[some], act="gelu", quant=quant)
+            assert torch.equal(y2, y[some]) and (quant is None or torch.equal(scale2, scale[some]))
