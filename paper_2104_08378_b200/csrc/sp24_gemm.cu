@@ -221,7 +221,8 @@ static void choose_tile(const sp24_gemm_desc* d, bool has_c, bool conv, int& cta
       return;
     }
     // one m-block: the width that needs the fewest rounds of tiles, operand bytes per k as the tie-break
-    // (without metadata columns two 256-column accumulators fit, so 256 x 256 keeps its epilogue overlapped)
+    // (without metadata columns two 256-column accumulators fit, so 256 x 256 keeps its epilogue overlapped; with N contiguous
+    // it loads the two 128-byte chunks of B to a CTA that 224 columns need as well: bf16 4096 x 2048 x 8192 114 -> 96 us)
     const int widths[3] = {224, has_240 ? 240 : 0, d->ab_type != SP24_F32 ? 256 : 0};
     double best = 0.0;
     for (const int bn : widths) {

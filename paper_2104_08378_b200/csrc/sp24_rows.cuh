@@ -93,17 +93,6 @@ __device__ __forceinline__ float row_scale(float top, float factor, float* inv) 
   return scale;
 }
 
-template <typename OUT>
-__device__ __forceinline__ OUT to_code(float v) {
-  if constexpr (std::is_same_v<OUT, int8_t>) {
-    return (int8_t)max(min(__float2int_rn(v), 127), -127);  // (NaN: 0)
-  } else {
-    OUT o;
-    o.__x = __nv_cvt_float_to_fp8(v, __NV_SATFINITE, std::is_same_v<OUT, __nv_fp8_e4m3> ? __NV_E4M3 : __NV_E5M2);
-    return o;
-  }
-}
-
 // an infinite maximum counts as NaN (where no factor of the row turns it into one)
 __device__ __forceinline__ float finite_or_nan(float top) { return top < __int_as_float(0x7f800000) ? top : __int_as_float(0x7fffffff); }
 

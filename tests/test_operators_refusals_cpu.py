@@ -127,3 +127,21 @@ def test_linear_without_a_problem():
     x, w, m = torch.zeros(32, 64, dtype=torch.bfloat16), torch.zeros(64, 32, dtype=torch.bfloat16), torch.zeros(4096, dtype=torch.uint8)
     refused(6, sp.linear, w, m, x)
     refused(6, sp.linear_backward, x, x, x, w)
+
+
+def test_calls_are_made_with_the_tensors_device_current(monkeypatch):
+    """By position or by name, and not where it is current already; a stand-in for a tensor on a second device."""
+    import contextlib
+    import types
+    made = []
+
+    @contextlib.contextmanager
+    def device(d):
+        made.append(d)
+        yield
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "device", device)
+    call = sp._on_device_of("x")(lambda x, y=1: (x.device, y))
+    there, here = (types.SimpleNamespace(is_cuda=True, device=f"cuda:{i}", get_device=lambda i=i: i) for i in (1, 0))
+    assert call(there, y=2) == ("cuda:1", 2) and call(x=there) == ("cuda:1", 1) and made == ["cuda:1", "cuda:1"]
+    assert call(here) == ("cuda:0", 1) and len(made) == 2
