@@ -659,19 +659,16 @@ PyObject* linear_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
     Result rx{Py_None, {}}, rw{Py_None, {}}, rb{Py_None, {}};
     const int status = unlocked([&]() -> int {
       const auto options = dy.t->options();
-      at::Tensor dz, dzt = at::empty({cols, rows}, options);
-      void* pdz = dy.p;
-      int64_t lddz = dy.ld;
-      if (act != SP24_ACT_NONE) {
-        dz = at::empty({rows, cols}, options);
-        pdz = dz.data_ptr();
-        lddz = cols;
-      }
+      // dz (where there is an activation), its transpose and the partial sums of the bias's gradient, in one allocation
+      const size_t bytes = act_bytes(rows, cols, cols_out), matrix = ((size_t)rows * cols * dy.t->element_size() + 255) / 256 * 256;
+      const at::Tensor scratch = at::empty({(int64_t)(matrix * (act != SP24_ACT_NONE ? 2 : 1) + bytes)}, options.dtype(at::kByte));
+      char* const pdzt = (char*)scratch.data_ptr();
+      void* const sums = pdzt + matrix * (act != SP24_ACT_NONE ? 2 : 1);
+      void* const pdz = act != SP24_ACT_NONE ? pdzt + matrix : dy.p;
+      const int64_t lddz = act != SP24_ACT_NONE ? cols : dy.ld;
       rb.made = at::empty({M}, options.dtype(at::kFloat));
-      const size_t bytes = act_bytes(rows, cols, cols_out);
-      const at::Tensor sums = at::empty({(int64_t)bytes}, options.dtype(at::kByte));
-      int st = act_fn((sp24_dtype)t, (sp24_act)act, rows, cols, dy.p, dy.ld, z.p, z.ld, act != SP24_ACT_NONE ? pdz : nullptr, lddz, dzt.data_ptr(), rows,
-                      (float*)rb.made.data_ptr(), cols_out, sums.data_ptr(), bytes, stream);
+      int st = act_fn((sp24_dtype)t, (sp24_act)act, rows, cols, dy.p, dy.ld, z.p, z.ld, act != SP24_ACT_NONE ? pdz : nullptr, lddz, pdzt, rows,
+                      (float*)rb.made.data_ptr(), cols_out, sums, bytes, stream);
       if (st != SP24_OK) return st;
       rx.made = at::empty({b.t->size(0), b.t->size(1)}, options);
       rw.made = at::empty({M, K}, options);
@@ -683,7 +680,7 @@ PyObject* linear_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
         const sp24_gemm_desc d = {(sp24_dtype)t, (sp24_dtype)t, m, n_, inner, lda, ldb, ldd, ldd, by_rows ? SP24_ROW_MAJOR : SP24_COL_MAJOR, order, order, 1};
         return (int)gemm_fn(&d, &one, A, nullptr, B, &zero, nullptr, D, ws, ws_bytes, stream);
       };
-      const void *tokens = cols_out ? pdz : dzt.data_ptr(), *features = cols_out ? dzt.data_ptr() : pdz;  // N x M, M x N
+      const void *tokens = cols_out ? pdz : pdzt, *features = cols_out ? pdzt : pdz;  // N x M, M x N
       const int64_t ld_tokens = cols_out ? lddz : rows, ld_features = cols_out ? rows : lddz;
       st = product(tokens, ld_tokens, N, K, M, w.p, w.ld, true, rx.made.data_ptr(), b_rows);
       if (st != SP24_OK) return st;

@@ -224,8 +224,8 @@ __device__ __forceinline__ uint4 add_packed(const uint4& a, const uint4& b) {
 }
 
 // ---- rows that start between 16-byte boundaries ----------------------------------------------------------------------------------
-// Bytes `o` (below 4 * WORDS) and on of the 8 * WORDS bytes {lo, hi}.
-template <int WORDS>
+// Bytes `o` (below 4 * WORDS; a multiple of BYTES) and on of the 8 * WORDS bytes {lo, hi}.
+template <int BYTES, int WORDS>
 __device__ __forceinline__ void from_byte(const uint32_t (&lo)[WORDS], const uint32_t (&hi)[WORDS], int o, uint32_t (&out)[WORDS]) {
   uint32_t w[2 * WORDS];
 #pragma unroll
@@ -240,7 +240,7 @@ __device__ __forceinline__ void from_byte(const uint32_t (&lo)[WORDS], const uin
     for (int i = 0; i + by < 2 * WORDS; ++i) w[i] = shift ? w[i + by] : w[i];
   }
 #pragma unroll
-  for (int i = 0; i < WORDS; ++i) out[i] = __funnelshift_r(w[i], w[i + 1], 8 * (o & 3));
+  for (int i = 0; i < WORDS; ++i) out[i] = BYTES % 4 == 0 ? w[i] : __funnelshift_r(w[i], w[i + 1], 8 * (o & 3));
 }
 
 // Where the vectors of a row lie: number i holds the elements from i * N - shift on, so that the words of a row whose first element lies
@@ -268,7 +268,7 @@ __device__ __forceinline__ uint4 load_vector(const T* row, int i, int K, int shi
   if (o) {
     a = word(i + 1);
     const uint32_t lo[4] = {w[0], w[1], w[2], w[3]}, hi[4] = {a.x, a.y, a.z, a.w};
-    from_byte(lo, hi, o, w);
+    from_byte<(int)sizeof(T)>(lo, hi, o, w);
   }
   if (first < 0 || first + N > K) {
     T* e = reinterpret_cast<T*>(w);
