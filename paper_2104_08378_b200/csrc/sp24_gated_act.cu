@@ -182,22 +182,23 @@ __global__ void __launch_bounds__(kThreads) gated_act_grad_kernel(const GatedGra
     const int64_t row = base + threadIdx.y;
     if (row >= p.rows) break;
     const int s = WHOLE ? 0 : shift_of<T, kVector<T>>(static_cast<const T*>(p.dg) + row * p.lddg);
-    uint4 dy[V], g[V], u[V] = {};
+    const T *pdy = static_cast<const T*>(p.dy) + row * p.lddy, *pg = static_cast<const T*>(p.g) + row * p.ldg, *pu = static_cast<const T*>(p.u) + row * p.ldu;
+    Words<WHOLE> dy[V], g[V], u[V] = {};
 #pragma unroll
-    for (int v = 0; v < V; ++v) dy[v] = load_vector<WHOLE>(static_cast<const T*>(p.dy) + row * p.lddy, i0 + v * (int)blockDim.x, F, s);
+    for (int v = 0; v < V; ++v) load_words<WHOLE>(dy[v], pdy, i0 + v * (int)blockDim.x, F, s);
 #pragma unroll
-    for (int v = 0; v < V; ++v) g[v] = load_vector<WHOLE>(static_cast<const T*>(p.g) + row * p.ldg, i0 + v * (int)blockDim.x, F, s);
+    for (int v = 0; v < V; ++v) load_words<WHOLE>(g[v], pg, i0 + v * (int)blockDim.x, F, s);
     if (gated) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) u[v] = load_vector<WHOLE>(static_cast<const T*>(p.u) + row * p.ldu, i0 + v * (int)blockDim.x, F, s);
+      for (int v = 0; v < V; ++v) load_words<WHOLE>(u[v], pu, i0 + v * (int)blockDim.x, F, s);
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int i = i0 + v * (int)blockDim.x;
       Pairs<T> d, f, w, dg, du;
-      unpack<T>(dy[v], d);
-      unpack<T>(g[v], f);
-      unpack<T>(u[v], w);
+      unpack<T>(vector_of<WHOLE>(dy[v], pdy, i, F, s), d);
+      unpack<T>(vector_of<WHOLE>(g[v], pg, i, F, s), f);
+      unpack<T>(vector_of<WHOLE>(u[v], pu, i, F, s), w);
       device_with_act(p.act, [&](auto a) {
 #pragma unroll
         for (int n = 0; n < P; ++n) {

@@ -250,14 +250,67 @@ __device__ __forceinline__ int shift_of(const E* row) {
   return (int)(reinterpret_cast<uintptr_t>(row) / sizeof(E) % N);
 }
 
-// Vector i of a row of K elements, zeros where the row has none.  If the vectors do not lie at boundaries, out of the two words that one lies in.  A word is
-// read if one of the row's elements is in it: the bytes beside them are in the same 16, and not used.
+// The words that vector i of a row of K elements lies in: one if the vectors lie at boundaries, else two, of which the vector is made where it is used, so that
+// nothing waits for them before.  A word is read if one of the row's elements is in it: the bytes beside them are in the same 16, and not used.
+template <bool WHOLE>
+struct Words {
+  uint4 lo, hi;
+};
+template <>
+struct Words<true> {
+  uint4 lo;
+};
+template <typename T>
+__device__ __forceinline__ int behind_words(const T* row, int shift) {  // bytes that the vectors lie behind the words
+  return (int)(reinterpret_cast<uintptr_t>(row - shift) & 15);
+}
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void load_words(Words<WHOLE>& to, const T* row, int i, int K, int shift) {
+  constexpr int N = kVector<T>;
+  if constexpr (WHOLE) {
+    to.lo = i * N < K ? __ldcs(reinterpret_cast<const uint4*>(row) + i) : make_uint4(0, 0, 0, 0);
+  } else {
+    const int o = behind_words(row, shift);
+    const uint4* words = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(row - shift) - o);
+    auto word = [&](int j) {
+      const int e = j * N - shift - o / (int)sizeof(T);  // the word's first element
+      return e < K && e + N > 0 ? words[j] : make_uint4(0, 0, 0, 0);
+    };
+    to.lo = word(i);
+    if (o) to.hi = word(i + 1);
+  }
+}
+// The vector, zeros where the row has no elements.
+template <bool WHOLE, typename T>
+__device__ __forceinline__ uint4 vector_of(const Words<WHOLE>& from, const T* row, int i, int K, int shift) {
+  if constexpr (WHOLE) {
+    return from.lo;
+  } else {
+    constexpr int N = kVector<T>;
+    const int first = i * N - shift, o = behind_words(row, shift);
+    uint32_t w[4] = {from.lo.x, from.lo.y, from.lo.z, from.lo.w};
+    if (o) {
+      const uint32_t lo[4] = {w[0], w[1], w[2], w[3]}, hi[4] = {from.hi.x, from.hi.y, from.hi.z, from.hi.w};
+      from_byte<(int)sizeof(T)>(lo, hi, o, w);
+    }
+    if (first < 0 || first + N > K) {
+      T* e = reinterpret_cast<T*>(w);
+      const T zero = {};
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+        if ((unsigned)(first + n) >= (unsigned)K) e[n] = zero;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+// Both at once, where registers count: the operators that hold rows (words apart: spills; norm bf16 8192 x 12287 -> e4m3 252, 296 us, silu f16
+// 4099 x 5461 43, 51).  gated_act_backward, which holds none, has its loads apart: f16 4099 x 5461 75, 67 us.
 template <bool WHOLE, typename T>
 __device__ __forceinline__ uint4 load_vector(const T* row, int i, int K, int shift) {
   constexpr int N = kVector<T>;
   if (WHOLE) return i * N < K ? __ldcs(reinterpret_cast<const uint4*>(row) + i) : make_uint4(0, 0, 0, 0);
   const int first = i * N - shift;  // its first element's number
-  const int o = (int)(reinterpret_cast<uintptr_t>(row - shift) & 15), behind = o / (int)sizeof(T);  // the vectors lie so far behind the words
+  const int o = behind_words(row, shift), behind = o / (int)sizeof(T);
   const uint4* words = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(row - shift) - o);
   auto word = [&](int j) {
     const int e = j * N - shift - behind;  // the word's first element
