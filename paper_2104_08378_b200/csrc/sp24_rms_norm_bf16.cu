@@ -1,0 +1,7 @@
+// The root-mean-square norm and its gradient on BF16 rows.
+#include "sp24_rms_norm_kernel.cuh"
+
+namespace sp24 {
+template sp24_status launch_rms_norm<__nv_bfloat16>(sp24_dtype, const NormParams&, bool, cudaStream_t);
+template sp24_status launch_rms_norm_grad<__nv_bfloat16>(const NormGradParams&, bool, int64_t&, cudaStream_t);
+}  // namespace sp24
