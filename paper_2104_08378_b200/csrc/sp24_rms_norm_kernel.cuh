@@ -8,7 +8,10 @@ namespace {
 
 // Rows of up to kMostTeamVectors vectors: a team of threads to a row, which holds it in registers, and the weight for all its rows.  One pass: the
 // team's next row (without a residual the next two, in as many registers) is on its way while this one is reduced, multiplied and
-// stored.
+// stored.  n = h rstd w with rstd from the row's sum of squares; 8-bit rows need no second reduction, since max |n| = rstd max |h w|.
+// Bound by HBM: bf16 8192 x 12288 with residual -> e4m3 111 us = 6.35 TB/s, -> bf16 125 us = 6.45 TB/s (a copy: 6.5); a block to a row and two passes
+// took 427.  Short calls are a launch: bf16 32 x 4096 2.1 us.  (One block of up to 1024 threads to an SM and the next row in registers instead of more blocks:
+// what is on its way does not depend on where the teams stand.)
 template <typename T, typename OUT, typename W, int V, bool RESIDUAL, bool WHOLE>
 __global__ void __launch_bounds__(team_threads(V), 1) rms_norm_rows_kernel(const NormParams p) {
   constexpr int N = kVector<T>, kWords = sizeof(W) / sizeof(T);  // 16-byte words of a vector's weights
@@ -196,6 +199,8 @@ __global__ void __launch_bounds__(1024, 1) rms_norm_kernel(const NormParams p) {
 // Rows of up to kMostTeamVectors vectors: a team of threads to a row, with the weight and the team's part of dweight in registers for all
 // its rows.  AHEAD: the team's next row is on its way from before this one's work to the end of it, in registers of its own (two sets in
 // turn).  At the end the block adds its teams' parts up, in an order that their number fixes.
+// dx = rstd (v - h rstd^2 mean(v h)) + dh with v = dy w: one reduction to a row.  Bound by HBM: bf16 8192 x 8192 with dh 89 us = 6.0 TB/s (single set of
+// registers 123, two passes 498); 512 threads of 123 registers are enough because 49 KB are on their way all the time.  512 x 4096 8.7 us, two launches.
 constexpr int kAheadThreads = 512;
 template <typename T, typename W, int V, bool AHEAD, bool WHOLE>
 __global__ void __launch_bounds__(AHEAD ? kAheadThreads : team_threads(V), 1) rms_norm_grad_rows_kernel(const NormGradParams p) {
