@@ -181,3 +181,20 @@ def test_a_row_does_not_depend_on_the_others(sp, t, F):
         for some in (slice(0, 1), slice(3201, 3209), slice(4400, 4800)):
             y2, scale2 = sp.gated_act(g[some], u[some], act="gelu", quant=quant)
             assert torch.equal(y2, y[some]) and (quant is None or torch.equal(scale2, scale[some]))
+
+
+def test_offsets_past_32_bits(sp):
+    """Rows 2^31 + 8 elements apart, of operands and results."""
+    ld = 2 ** 31 + 8
+    room = [torch.empty(ld + 64, dtype=torch.bfloat16, device="cuda").as_strided((2, 64), (ld, 1)) for _ in range(3)]
+    g, u, y = room
+    g.copy_(rand((2, 64), "bf16", 20))
+    u.copy_(rand((2, 64), "bf16", 21))
+    a, slope = act64(g.double(), "silu")
+    sp.gated_act(g, u, out=y)
+    close(y, a * u.double(), "bf16", VALUE * (g.double() * u.double()).abs())
+    dg, du = sp.gated_act_backward(y, g, u)
+    close(dg, y.double() * u.double() * slope, "bf16", SLOPE * (y.double() * u.double()).abs())
+    dz, dzt, db = sp.act_backward(u, g, act="silu", cd_col_major=True, out=y)
+    close(dz, u.double() * slope, "bf16", SLOPE * u.double().abs())
+    assert torch.equal(dzt, dz.T)
