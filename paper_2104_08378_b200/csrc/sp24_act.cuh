@@ -34,18 +34,22 @@ __device__ __forceinline__ float reciprocal_fast(float v) {
 }
 constexpr float kLog2e = 1.4426950408889634f;
 
-// Phi(z) = (1 + erf(z / sqrt 2)) / 2 by Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26 (absolute error of
-// erf at most 1.5e-7; half of that here): erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2), t = 1 / (1 + p x), for x >= 0.  `density`:
-// exp(-z^2 / 2), which the slope needs as well.
+// Phi of the normal distribution: Phi(-|z|) = exp(-z^2 / 2) t (q1 + q2 t + ... + q8 t^7) with t = 1 / (1 + 0.304 |z|), which a positive z subtracts from 1.
+// The polynomial is a fit of exp(z^2 / 2) Phi(-|z|) by Remez's exchange with the smallest relative error, 8.4e-8, for |z| <= 13.5 (beyond,
+// exp(-z^2 / 2) is 0).  So the tail keeps its leading bits, which a fit with an absolute error does not: at most 2^-19 + 1.25 z^2 2^-24 of the value are lost
+// (t and its powers, the exponential, and z^2 / 2 log2(e) rounded three times).  `density`: exp(-z^2 / 2), which the slope needs as well.
 __device__ __forceinline__ float2 normal_cdf(float2 z, float2* density) {
-  constexpr float p = 0.3275911f * 0.70710678f;
+  constexpr float p = 0.304f;
   const float2 t = make_float2(reciprocal_fast(fmaf(fabsf(z.x), p, 1.f)), reciprocal_fast(fmaf(fabsf(z.y), p, 1.f)));
   const float2 square = mul2(mul2(z, both(-0.5f * kLog2e)), z);
   *density = make_float2(exp2_fast(square.x), exp2_fast(square.y));
-  float2 poly = fma2(t, both(0.5f * 1.061405429f), both(0.5f * -1.453152027f));
-  poly = fma2(t, poly, both(0.5f * 1.421413741f));
-  poly = fma2(t, poly, both(0.5f * -0.284496736f));
-  poly = fma2(t, poly, both(0.5f * 0.254829592f));
+  float2 poly = fma2(t, both(3.6857929563e-02f), both(-1.5529669541e-01f));
+  poly = fma2(t, poly, both(1.9218532803e-01f));
+  poly = fma2(t, poly, both(-4.3127016641e-02f));
+  poly = fma2(t, poly, both(1.2355224943e-01f));
+  poly = fma2(t, poly, both(1.0242285091e-01f));
+  poly = fma2(t, poly, both(1.2217071321e-01f));
+  poly = fma2(t, poly, both(1.2123468153e-01f));
   const float2 tail = mul2(mul2(t, poly), *density);  // Phi(-|z|)
   return make_float2(z.x < 0.f ? tail.x : 1.f - tail.x, z.y < 0.f ? tail.y : 1.f - tail.y);
 }

@@ -24,7 +24,7 @@ struct ActGradParams {
 // consecutive rows of column c, so that a warp stores eight segments of 64 bytes.  Unit u (16 bytes) of row m lies at
 // u ^ (2 (m >> 3 & 3) + (m & 1)): the eight rows of a matrix are in different banks.
 // dz = dy act'(z) is needed in both orders, and reading dy and z once for both is what the tile is for.  Bound by HBM and, with GELU, the arithmetic of the slope:
-// bf16 4096 x 8192 with the bias 51 us = 5.2 TB/s (ReLU 46; by elements 125, tiles of 64 x 64 62); three blocks to an SM instead of two spill (75).
+// bf16 4096 x 8192 with the bias 52 us = 5.1 TB/s (ReLU 46; by elements 125, tiles of 64 x 64 62); three blocks to an SM instead of two spill (75).
 template <typename T, int ACT, int kWide>
 __global__ void __launch_bounds__(4 * kWide) act_grad_tile_kernel(const ActGradParams p) {
   constexpr int kUnits = kWide / 8, kWideThreads = 4 * kWide;

@@ -36,7 +36,7 @@ __device__ __forceinline__ void gated_vector(int act, const uint4& g, const uint
 // turn): the exponentials and reciprocals take half as long as the memory does.  Else it sets out behind them, and more teams, each at another
 // place of its row, hide that.
 // Bound by the special-function units (52 % busy: an exponential and a reciprocal for each value), the ALU (46 %) and HBM, which the barrier of 8-bit rows keeps from
-// overlapping wholly: silu bf16 8192 x 12288 -> e4m3 85 us = 5.9 TB/s, -> bf16 92 us = 6.5 TB/s, gelu -> int8 97 us; two passes took 455.
+// overlapping wholly: silu bf16 8192 x 12288 -> e4m3 85 us = 5.9 TB/s, -> bf16 92 us = 6.5 TB/s, gelu -> int8 104 us; two passes took 455.
 constexpr int many_threads(int v) { return v == 2 ? 1024 : 768; }
 template <typename T, typename OUT, int V, bool AHEAD, bool WHOLE>
 __global__ void __launch_bounds__(AHEAD ? team_threads(V) : many_threads(V), 1) gated_act_rows_kernel(const GatedParams p) {
@@ -174,7 +174,7 @@ struct GatedGradParams {
 };
 
 // Element by element: two vectors to a thread, all their loads before the first use.  Bound by HBM: bf16 4096 x 8192 51 us = 6.6 TB/s with any activation
-// (an element to a thread 214); rows that lie otherwise than the results' take two words and a shift for each vector: f16 4099 x 5461 55 us, 4.0 TB/s.
+// (an element to a thread 214); rows that lie otherwise than the results' take two words and a shift for each vector: f16 4099 x 5461 with GELU 57 us, 3.9 TB/s.
 template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(kThreads) gated_act_grad_kernel(const GatedGradParams p) {
   constexpr int P = kVector<T> / 2, V = 2;
