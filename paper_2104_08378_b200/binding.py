@@ -659,7 +659,7 @@ def act_backward(dy: torch.Tensor, pre: torch.Tensor | None, *, act: str | None,
                  transposed: bool = True, bias: bool = True, out: torch.Tensor | None = None):
     """sp24_act_backward: (dz, dz transposed or None, dbias or None) from the gradient of act(pre).  cd_col_major as in the
     product that made pre: True: dy and pre are [N, M], else [M, N]; dbias [M] sums over the N tokens.  Without an activation
-    dz is dy itself and pre is not read.  out may be dy or pre."""
+    dz is dy itself (with `out`: a copy of it there) and pre is not read.  out may be dy or pre."""
     done = _native.act_backward(_ACT_BACKWARD, _ACT_BYTES, dy, pre, act, cd_col_major, transposed, bias, out)
     if done is not None:
         return done if type(done) is not int else _check(done, "sp24_act_backward")
@@ -672,7 +672,7 @@ def _act_backward(dy, pre, *, act, cd_col_major, transposed, bias, out):
     t, code = _float_code(dy, where), _act_code(act, where)
     lddy = ldz = _matrix(dy, where)
     rows, cols = dy.shape
-    dz = None
+    dz = out
     if code:
         _refuse(pre is None, 1, where)
         ldz = _matrix(pre, where, dy, dy.shape, dy.dtype)

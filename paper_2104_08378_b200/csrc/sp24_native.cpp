@@ -524,12 +524,12 @@ PyObject* act_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
     const int t = type_code(dy.t->scalar_type());
     const int64_t rows = dy.t->size(0), cols = dy.t->size(1);
     if (!float_type(t)) return none();
-    if (act != SP24_ACT_NONE && (!z.init(v[3], rows, cols, t) || (v[8] != Py_None && !dz.init(v[8], rows, cols, t)))) return none();
+    if ((act != SP24_ACT_NONE && !z.init(v[3], rows, cols, t)) || (v[8] != Py_None && !dz.init(v[8], rows, cols, t))) return none();
     const int over_rows = v[5] == Py_True;
     const auto fn = function<decltype(&sp24_act_backward)>(v[0]);
     const auto size = function<decltype(&sp24_act_backward_workspace_bytes)>(v[1]);
     const cudaStream_t stream = Stream().handle;
-    Result rdz{act == SP24_ACT_NONE ? v[2] : v[8], {}}, rdzt{Py_None, {}}, rdb{Py_None, {}};
+    Result rdz{act == SP24_ACT_NONE && v[8] == Py_None ? v[2] : v[8], {}}, rdzt{Py_None, {}}, rdb{Py_None, {}};
     const int status = unlocked([&] {
       const auto options = dy.t->options();
       if (act != SP24_ACT_NONE && v[8] == Py_None) {
