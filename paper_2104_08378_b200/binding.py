@@ -750,7 +750,7 @@ def linear_backward(dy: torch.Tensor, pre: torch.Tensor | None, Bt: torch.Tensor
                     ws: torch.Tensor | None = None):
     """Gradients of linear (16-bit operands, or float32 in the TF32 mode without meta) from dy, its `pre` (None without an activation) and Bt, and the pruned
     weights W [M, K] themselves: (dBt, dW, dbias).  dy and pre are [N, M] with cd_col_major, else [M, N]; Bt [N, K], or [K, N]
-    with b_row_major; dBt has Bt's form.  With meta the entries of dW that the 2:4 pattern leaves out are zeros.  The
+    with b_row_major; dBt has Bt's form.  dy and pre may have any leading dimension and alignment, Bt and W those of gemm's operands.  With meta the entries of dW that the 2:4 pattern leaves out are zeros.  The
     residual's gradient is dy.  sp24_act_backward, then two dense products (and sp24_apply_mask)."""
     done = _native.linear_backward(_ACT_BACKWARD, _ACT_BYTES, _GEMM, _META_BYTES, _APPLY_MASK, _workspaces, dy, pre, Bt, W, act,
                                    meta, b_row_major, cd_col_major, ws)
@@ -776,7 +776,9 @@ def _linear_backward(dy, pre, Bt, W, *, act, meta, b_row_major, cd_col_major, ws
         _vector(meta, meta_bytes(_FROM_TORCH[W.dtype], M, K), where, dy, (torch.uint8,))
     if N == 0:
         return Bt.new_empty(Bt.shape), torch.zeros_like(W), dy.new_zeros(M, dtype=torch.float32)
-    dz, dzt, dbias = act_backward(dy, pre, act=act, cd_col_major=cd_col_major)
+    # (without an activation dz is dy itself, where a product can take it)
+    out = dy.new_empty(dy.shape) if act is None and (dy.data_ptr() % 16 or dy.stride(0) * dy.element_size() % 16) else None
+    dz, dzt, dbias = act_backward(dy, pre, act=act, cd_col_major=cd_col_major, out=out)
     tokens, features = (dz, dzt) if cd_col_major else (dzt, dz)          # [N, M], [M, N]
     dBt = gemm(tokens, None, W, a_is_dense=True, b_row_major=True, cd_col_major=b_row_major, ws=ws)
     dW = gemm(features, None, Bt, a_is_dense=True, b_row_major=not b_row_major, ws=ws)

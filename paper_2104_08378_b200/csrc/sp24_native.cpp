@@ -659,15 +659,16 @@ PyObject* linear_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
     Result rx{Py_None, {}}, rw{Py_None, {}}, rb{Py_None, {}};
     const int status = unlocked([&]() -> int {
       const auto options = dy.t->options();
-      // dz (where there is an activation), its transpose and the partial sums of the bias's gradient, in one allocation
+      // dz (without an activation dy itself, where a product can take it), its transpose and the partial sums of the bias's gradient, in one allocation
+      const bool makes_dz = act != SP24_ACT_NONE || (uintptr_t)dy.p % 16 != 0 || dy.ld * dy.t->element_size() % 16 != 0;
       const size_t bytes = act_bytes(rows, cols, cols_out), matrix = ((size_t)rows * cols * dy.t->element_size() + 255) / 256 * 256;
-      const at::Tensor scratch = at::empty({(int64_t)(matrix * (act != SP24_ACT_NONE ? 2 : 1) + bytes)}, options.dtype(at::kByte));
+      const at::Tensor scratch = at::empty({(int64_t)(matrix * (makes_dz ? 2 : 1) + bytes)}, options.dtype(at::kByte));
       char* const pdzt = (char*)scratch.data_ptr();
-      void* const sums = pdzt + matrix * (act != SP24_ACT_NONE ? 2 : 1);
-      void* const pdz = act != SP24_ACT_NONE ? pdzt + matrix : dy.p;
-      const int64_t lddz = act != SP24_ACT_NONE ? cols : dy.ld;
+      void* const sums = pdzt + matrix * (makes_dz ? 2 : 1);
+      void* const pdz = makes_dz ? pdzt + matrix : dy.p;
+      const int64_t lddz = makes_dz ? cols : dy.ld;
       rb.made = at::empty({M}, options.dtype(at::kFloat));
-      int st = act_fn((sp24_dtype)t, (sp24_act)act, rows, cols, dy.p, dy.ld, z.p, z.ld, act != SP24_ACT_NONE ? pdz : nullptr, lddz, pdzt, rows,
+      int st = act_fn((sp24_dtype)t, (sp24_act)act, rows, cols, dy.p, dy.ld, z.p, z.ld, makes_dz ? pdz : nullptr, lddz, pdzt, rows,
                       (float*)rb.made.data_ptr(), cols_out, sums, bytes, stream);
       if (st != SP24_OK) return st;
       rx.made = at::empty({b.t->size(0), b.t->size(1)}, options);

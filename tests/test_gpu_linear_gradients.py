@@ -42,3 +42,22 @@ def test_a_result_is_written_without_an_activation(either, t):
         for wrong in (torch.empty((rows, cols + 1), dtype=dy.dtype, device="cuda"), torch.empty((rows, cols), dtype=torch.float64, device="cuda")):
             with pytest.raises(either.Sp24Error):
                 either.act_backward(dy, None, act=None, out=wrong)
+
+
+@pytest.mark.parametrize("t", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("act", [None, "silu"])
+@pytest.mark.parametrize("cols", [True, False])
+def test_the_results_gradient_may_lie_anywhere(either, t, act, cols):
+    """The same gradients from dy in rows between 16-byte boundaries, and behind one, as from a packed dy."""
+    M, N, K = 96, 48, 64
+    W, X, dy = rand((M, K), t, 2), rand((N, K), t, 3), rand((N, M) if cols else (M, N), t, 4)
+    pre = rand(dy.shape, t, 5)
+    want = either.linear_backward(dy, pre, X, W, act=act, cd_col_major=cols)
+    for pad, offset in ((3, 0), (16, 1), (0, 1)):
+        room = torch.empty(dy.shape[0] * (dy.shape[1] + pad) + offset, dtype=dy.dtype, device="cuda")[offset:]
+        there = room.as_strided(dy.shape, (dy.shape[1] + pad, 1))
+        there.copy_(dy)
+        got = either.linear_backward(there, pre, X, W, act=act, cd_col_major=cols)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and torch.equal(there, dy)
+        # (its sums go through tiles in another order: chains of fewer than 64 additions)
+        close(got[2], want[2].double(), "f32", 2.0 ** -17 * dy.double().abs().sum(0 if cols else 1))
