@@ -152,8 +152,8 @@ __global__ void __launch_bounds__(1024, 1) rms_norm_kernel(const NormParams p) {
       for (int n = 0; n < P; ++n) f[n] = mul2(f[n], w[n]);
     };
     uint4 kept[kKept];
+    float sum[2], top = 0.f;  // of the first vector, and of the others: of rows of 64 groups of vectors the same order as the teams'
     float2 sum2 = both(0.f);
-    float top = 0.f;
     auto count = [&](int i, const uint4& v) {
       Pairs<T> f;
       unpack<T>(v, f);
@@ -167,10 +167,13 @@ __global__ void __launch_bounds__(1024, 1) rms_norm_kernel(const NormParams p) {
     };
 #pragma unroll
     for (int v = 0; v < kKept; ++v) kept[v] = value(threadIdx.x + v * 1024);
+    count(threadIdx.x, kept[0]);
+    sum[0] = sum2.x + sum2.y;
+    sum2 = both(0.f);
 #pragma unroll
-    for (int v = 0; v < kKept; ++v) count(threadIdx.x + v * 1024, kept[v]);
+    for (int v = 1; v < kKept; ++v) count(threadIdx.x + v * 1024, kept[v]);
     for (int i = threadIdx.x + kKept * 1024; i < vectors; i += 1024) count(i, value(i));
-    float sum[1] = {sum2.x + sum2.y};
+    sum[1] = sum2.x + sum2.y;
     sums.reduce<true, is_code<OUT>>(sum, top, turn);
     const float rstd = rsqrtf(sum[0] / (float)p.K + p.eps);
     if (threadIdx.x == 0 && p.rstd) p.rstd[row] = rstd;

@@ -101,8 +101,9 @@ __device__ __forceinline__ float finite_or_nan(float top) { return top < __int_a
 // maximum (of values >= 0).  All threads of a block's warps call it together.  Two buffers in turn, so that one barrier is enough: whoever
 // writes a buffer again has passed the barrier of the one between, which the readers reach behind their reads.
 constexpr int kMostTeams = 15;  // of several warps: each has a hardware barrier of its own
-// The sum is over groups of 32 neighbouring vectors (a warp's v-th ones) and then over the groups, each by halves, however many vectors a thread
-// has, so that a row's bits do not depend on how many other rows there are.  (V = 4: 64 groups, in pairs first.)
+// The sum is over groups of 32 neighbouring vectors (a warp's v-th ones) and then over the groups, group g first with g + 32 and then by halves, however many
+// vectors a thread has, so that a row's bits do not depend on how many other rows there are nor on how they lie.  (Four sums of a warp take six shuffles: each
+// of the first two sends away half of what a lane holds.)
 struct RowSums {
   float groups[2][64], top[2][32];
   // s: of each of the thread's vectors; the row's sum is in s[0] afterwards
@@ -126,32 +127,33 @@ struct RowSums {
       for (int i = 16; i > 0; i >>= 1) x += __shfl_xor_sync(~0u, x, i);
     };
     auto top_over_warp = [&] { asm volatile("redux.sync.max.abs.NaN.f32 %0, %0, 0xffffffff;" : "+f"(t)); };
-    if (SUM) {
-      if (V == 4) {
-        s[0] += s[2];
-        s[1] += s[3];
-      }
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, first = threadIdx.y * warps;
+    constexpr int G = V;  // groups of a warp: at most 64 of all teams (32 warps with one or two, 16 with four)
+    if constexpr (SUM && V == 4) {  // (teams of many warps); of lanes 8 v on: the v-th group's sum
+      const bool hi = lane & 16, odd = lane & 8;
+      const float a = (hi ? s[2] : s[0]) + __shfl_xor_sync(~0u, hi ? s[0] : s[2], 16), b = (hi ? s[3] : s[1]) + __shfl_xor_sync(~0u, hi ? s[1] : s[3], 16);
+      s[0] = (odd ? b : a) + __shfl_xor_sync(~0u, odd ? a : b, 8);
 #pragma unroll
-      for (int v = 0; v < (V < 2 ? V : 2); ++v) sum_over_warp(s[v]);
+      for (int i = 4; i > 0; i >>= 1) s[0] += __shfl_xor_sync(~0u, s[0], i);
+      if ((lane & 7) == 0) groups[turn][G * first + (lane >> 3) * warps + warp] = s[0];
+    } else if constexpr (SUM) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) sum_over_warp(s[v]);
     }
     if (TOP) top_over_warp();
-    const int warps = blockDim.x >> 5;
-    if (warps == 1) {
-      if (SUM && V > 1) s[0] += s[1];
+    if (V != 4 && warps == 1) {
+      if (SUM && V == 2) s[0] += s[V - 1];
       return;
     }
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = threadIdx.y * warps;
-    // (twice as many groups as warps with two vectors: at most 32 of a team, of all teams those of 24 warps of 48)
     if (lane == 0) {
-      if (SUM) {
+      if (SUM && V != 4) {
 #pragma unroll
-        for (int v = 0; v < (V < 2 ? V : 2); ++v) groups[turn][(V < 2 ? 1 : 2) * first + v * warps + warp] = s[v];
+        for (int v = 0; v < V; ++v) groups[turn][G * first + v * warps + warp] = s[v];
       }
       if (TOP) top[turn][first + warp] = t;
     }
     asm volatile("bar.sync %0, %1;" ::"r"(threadIdx.y + 1), "r"(blockDim.x) : "memory");
     if (SUM) {
-      constexpr int G = V < 2 ? 1 : 2;
       s[0] = lane < G * warps ? groups[turn][G * first + lane] : 0.f;
       if (G * warps > 32) s[0] += lane + 32 < G * warps ? groups[turn][G * first + lane + 32] : 0.f;
     }
