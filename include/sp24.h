@@ -406,7 +406,7 @@ sp24_status sp24_rms_norm(sp24_dtype t, int64_t rows, int64_t K, const void* x, 
  * both x and the residual.  Everything in FP32, dx rounded once to t.  dweight: K floats, or NULL if it is not wanted.
  *   dx may be the same buffer as dy, h or dh (same leading dimension).
  *   workspace: sp24_rms_norm_backward_workspace_bytes(rows, K) bytes (0 for NULL dweight), 16-byte aligned, contents of no
- *   matter before or after.  The rows' sums are added in an order that rows, K and the device fix: the same call gives the same bits. */
+ *   matter before or after (a row of K floats for each of the current device's SMs at most).  The rows' sums are added in an order that rows, K and the device fix: the same call gives the same bits. */
 size_t sp24_rms_norm_backward_workspace_bytes(int64_t rows, int64_t K);
 sp24_status sp24_rms_norm_backward(sp24_dtype t, int64_t rows, int64_t K, const void* dy, int64_t lddy, const void* h,
                                    int64_t ldh, const void* weight, sp24_dtype weight_type, const float* rstd,

@@ -21,9 +21,11 @@ __global__ void __launch_bounds__(256) column_sums_kernel(const float* partial, 
   }
 }
 
-// Blocks of the gradient's kernel: each keeps a row of dweight's sums in the workspace.
-constexpr int64_t kMostPartials = 592;
-int64_t grad_blocks(int64_t rows) { return rows < kMostPartials ? rows : kMostPartials; }
+// Blocks of the gradient's kernel at most, one to an SM: each keeps a row of dweight's sums in the workspace.  (Where no device tells its SMs, room for the largest.)
+int64_t most_grad_blocks(int64_t rows) {
+  const int64_t sms = sm_count() > 1 ? sm_count() : 592;
+  return rows < sms ? rows : sms;
+}
 
 }  // namespace
 
@@ -59,7 +61,7 @@ extern "C" sp24_status sp24_rms_norm(sp24_dtype t, int64_t rows, int64_t K, cons
 
 extern "C" size_t sp24_rms_norm_backward_workspace_bytes(int64_t rows, int64_t K) {
   if (rows <= 0 || K < 1 || K > kMostColumns) return 0;
-  return (size_t)grad_blocks(rows) * (size_t)K * sizeof(float);
+  return (size_t)most_grad_blocks(rows) * (size_t)K * sizeof(float);
 }
 
 extern "C" sp24_status sp24_rms_norm_backward(sp24_dtype t, int64_t rows, int64_t K, const void* dy, int64_t lddy, const void* h,
@@ -85,7 +87,7 @@ extern "C" sp24_status sp24_rms_norm_backward(sp24_dtype t, int64_t rows, int64_
                  SP24_ERR_WORKSPACE);
   sp24_status st = check_arch();
   if (st != SP24_OK) return st;
-  int64_t blocks = grad_blocks(rows);
+  int64_t blocks = 0;
   const NormGradParams p = {rows, K, dy, h, weight, dh, rstd, dx, dweight ? static_cast<float*>(workspace) : nullptr, lddy, ldh, lddh, lddx, weight_type == SP24_F32};
   const bool whole = K * es % 16 == 0 && whole_rows(dy, rows, lddy, es, 16) && whole_rows(h, rows, ldh, es, 16) && whole_rows(dh, rows, lddh, es, 16) &&
                      whole_rows(dx, rows, lddx, es, 16) && aligned16(weight);

@@ -29,7 +29,7 @@ struct NormGradParams {
 // WHOLE rows (and weight): see load_vector.
 template <typename T>
 sp24_status launch_rms_norm(sp24_dtype out_type, const NormParams& p, bool whole, cudaStream_t s);
-// blocks: at most so many rows of partial sums; set to those that there will be.
+// blocks: set to the number of blocks and of rows of partial sums, at most one to an SM.
 template <typename T>
 sp24_status launch_rms_norm_grad(const NormGradParams& p, bool whole, int64_t& blocks, cudaStream_t s);
 

@@ -462,8 +462,7 @@ template <typename T>
 sp24_status launch_rms_norm_grad(const NormGradParams& p, bool whole, int64_t& blocks, cudaStream_t s) {
   const int64_t vectors = row_vectors(p.K, sizeof(T), true);
   if (vectors <= kMostTeamVectors) {
-    TeamLaunch at(p.rows, vectors, 2, kAheadThreads);  // (bf16 512 x 4096 with one vector and two: 9.4, 8.7 us)
-    if (at.grid.x > blocks) at.grid.x = (unsigned)blocks;
+    const TeamLaunch at(p.rows, vectors, 2, kAheadThreads);  // (bf16 512 x 4096 with one vector and two: 9.4, 8.7 us)
     blocks = at.grid.x;
     const int slots = at.block.x < 32 ? (int)(at.block.x * at.block.y / 32) : (int)at.block.y;
     const size_t smem = p.partial ? (size_t)slots * vectors * kVector<T> * sizeof(float) : 0;  // (at most 64 KB: V vectors for each thread)
@@ -478,7 +477,7 @@ sp24_status launch_rms_norm_grad(const NormGradParams& p, bool whole, int64_t& b
     };
     return p.weight && p.weight_f32 ? launch(TypeOf<float>{}) : launch(TypeOf<T>{});
   }
-  if (blocks > sm_count()) blocks = sm_count();
+  blocks = p.rows < sm_count() ? p.rows : sm_count();
   return launch_overlapped(rms_norm_grad_kernel<T>, dim3((unsigned)blocks), dim3(1024), 0, s, 1, p);
 }
 
