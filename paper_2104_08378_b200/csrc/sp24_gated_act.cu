@@ -249,17 +249,17 @@ extern "C" sp24_status sp24_gated_act(sp24_dtype t, sp24_act act, int64_t rows, 
       // rows (8192 x 12288 89.7, 85.5, x 9216 77.5, 74.3; not 1024 x 12288 13.5, 15.0, nor -> bf16 92.5, 95.4).
       const int64_t team = ((vectors + 1) / 2 + 31) / 32 * 32;
       const bool many = vectors <= 1024 && 2 * (1024 / team) >= 3 * (team_threads(2) / team);
-      const bool two_teams = is_code_type(out_type) && vectors > 1024 && vectors <= 2 * many_threads(4) && rows >= 32 * (int64_t)sm_count();
-      TeamLaunch at(rows, vectors, 2, many ? many_threads(2) : team_threads(2));
-      if (two_teams) {
-        const unsigned of_four = (unsigned)((vectors + 3) / 4 + 31) / 32 * 32;
-        at.block = dim3(of_four, many_threads(4) / of_four);
-        at.grid = dim3((unsigned)sm_count());
-      }
-      const auto kernel = two_teams               ? (whole ? gated_act_rows_kernel<T, OUT, 4, false, true> : gated_act_rows_kernel<T, OUT, 4, false, false>)
-                          : at.v == 2 && many ? (whole ? gated_act_rows_kernel<T, OUT, 2, false, true> : gated_act_rows_kernel<T, OUT, 2, false, false>)
-                                                  : with_flags([](auto four, auto two, auto whole) { return gated_act_rows_kernel<T, OUT, four.value ? 4 : two.value ? 2 : 1, true, whole.value>; },
-                                                               at.v == 4, at.v >= 2, whole);
+      if constexpr (is_code<OUT>)
+        if (vectors > 1024 && vectors <= 2 * many_threads(4) && rows >= 32 * (int64_t)sm_count()) {
+          const unsigned of_four = (unsigned)((vectors + 3) / 4 + 31) / 32 * 32;
+          return launch_overlapped(whole ? gated_act_rows_kernel<T, OUT, 4, false, true> : gated_act_rows_kernel<T, OUT, 4, false, false>,
+                                   dim3((unsigned)sm_count()), dim3(of_four, many_threads(4) / of_four), 0, s, 1, p);
+        }
+      const TeamLaunch at(rows, vectors, 2, many ? many_threads(2) : team_threads(2));
+      const auto kernel = at.v == 2 && many
+                              ? (whole ? gated_act_rows_kernel<T, OUT, 2, false, true> : gated_act_rows_kernel<T, OUT, 2, false, false>)
+                              : with_flags([](auto four, auto two, auto whole) { return gated_act_rows_kernel<T, OUT, four.value ? 4 : two.value ? 2 : 1, true, whole.value>; },
+                                           at.v == 4, at.v >= 2, whole);
       return launch_overlapped(kernel, at.grid, at.block, 0, s, 1, p);
     });
   });
