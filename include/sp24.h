@@ -386,8 +386,9 @@ sp24_status sp24_prune_2d(sp24_dtype t, int64_t M, int64_t K, const void* x, int
  *   scale[i] = max |n[i, .]| / L with L = 127, 448, 57344, y = n / scale[i] rounded to the nearest code (ties to even).
  *   A row of zeros, or of |h weight| all below 2^-110, has scale 0 and codes 0.  A row with a NaN or an infinity in h has scale NaN and
  *   codes 0 (SP24_I8) or NaN.
+ *   The codes are computed as h weight (L / max |h weight|): a value next to a tie may go the other way than n divided by the rounded scale.
  * The codes and scales are what the products with 8-bit operands take (the scales as sp24_linear's col_scale).  A row's results
- *   depend on its values and on where it lies modulo 16 bytes (the order of its sum), not on the other rows or their number.
+ *   depend on its values and on where it and its result lie modulo 16 bytes (the order of its sum), not on the other rows or their number.
  *   t: SP24_F16, SP24_BF16 or SP24_F32.  rows >= 0, 1 <= K <= 2^30; any leading dimensions >= K, any alignment that the
  *   types have; fastest where rows start at 16-byte boundaries.
  *   residual: rows x K of type t, or NULL.  h: where x + residual goes, or NULL; without residual it has to be NULL.

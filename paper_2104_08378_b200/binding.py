@@ -468,7 +468,8 @@ def prune_2d(x: torch.Tensor, out: torch.Tensor | None = None, dtype: str | None
 
 # ---- the operators around the products -----------------------------------------------------------------------------------
 # Their tensors may be on another device than the current one (all on the same): the call is then made with that one current,
-# on its current stream.  What torch knows about the tensors is checked here, the rest by the library.
+# on its current stream.  What torch knows about the tensors is checked here, the rest by the library.  Their results carry no
+# gradient for autograd (nor do those of the products above): the gradients are calls of their own.
 ERR_DTYPE, ERR_SHAPE, ERR_STRIDE, ERR_UNSUPPORTED = 2, 3, 4, 6
 _QUANT = ("i8", "e4m3", "e5m2")
 ACT = {None: 0, "relu": 1, "gelu": 2, "silu": 3, "gelu_tanh": 4}
@@ -698,7 +699,8 @@ def linear(A: torch.Tensor, meta: torch.Tensor | None, Bt: torch.Tensor, *, bias
     """sp24_linear: D = act(row_scale[i] * col_scale[j] * (A B)[i, j] + bias[i]) + residual[i, j].  A, meta, Bt, cd,
     a_is_dense, b_row_major, cd_col_major as for gemm (cd defaults to A's type, bf16 for 8-bit operands); bias and row_scale
     [M], col_scale [N] float32 (col_scale: 8-bit operands); residual in D's type and shape, and may be `out`.  Returns D, or
-    with pre=True (or a tensor for it) (D, what act was applied to)."""
+    with pre=True (or a tensor for it) (D, what act was applied to).  M, N and K are multiples of 16, with 8-bit operands of
+    32, as for gemm: other numbers of tokens are padded by the caller."""
     done = _native.linear(_LINEAR, _workspaces, _META_BYTES, A, meta, Bt, bias, act, residual, row_scale, col_scale, pre,
                           out, cd, a_is_dense, b_row_major, cd_col_major, ws)
     if done is not None:
@@ -751,7 +753,8 @@ def linear_backward(dy: torch.Tensor, pre: torch.Tensor | None, Bt: torch.Tensor
     """Gradients of linear (16-bit operands, or float32 in the TF32 mode without meta) from dy, its `pre` (None without an activation) and Bt, and the pruned
     weights W [M, K] themselves: (dBt, dW, dbias).  dy and pre are [N, M] with cd_col_major, else [M, N]; Bt [N, K], or [K, N]
     with b_row_major; dBt has Bt's form.  dy and pre may have any leading dimension and alignment, Bt and W those of gemm's operands.  With meta the entries of dW that the 2:4 pattern leaves out are zeros.  The
-    residual's gradient is dy.  sp24_act_backward, then two dense products (and sp24_apply_mask)."""
+    residual's gradient is dy.  sp24_act_backward, then two dense products (and sp24_apply_mask).  dz = dy act'(pre) is an operand of
+    both products, so it is rounded to dy's type before them (float32: the tensor cores read it as TF32); dbias is not."""
     done = _native.linear_backward(_ACT_BACKWARD, _ACT_BYTES, _GEMM, _META_BYTES, _APPLY_MASK, _workspaces, dy, pre, Bt, W, act,
                                    meta, b_row_major, cd_col_major, ws)
     if done is not None:

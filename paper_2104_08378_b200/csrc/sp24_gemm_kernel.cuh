@@ -319,9 +319,9 @@ __device__ __forceinline__ void compute_row(const uint32_t (&r)[COLUMNS], const 
 
 // Epilogue of sp24_linear, one thread's row of a box: z = row_scale * col_scale * acc + bias in place of the accumulators, then the
 // activation, the residual and the rounding, all in FP32, by pairs.  col_scales: the box's columns' scales in shared memory (the same for all lanes:
-// eight wide reads instead of a shuffle for each column), if it has any.  What it costs next to the plain product, us, device: bf16 16384 x 4096 x 4096 226 -> 226
-// with a bias, 227 with SiLU, 231 with GELU, 244 with a residual (266 as C of sp24_gemm); int8 16384 x 512 x 4096 -> bf16 21.4 (sp24_gemm_i8_dequant) -> 23.1 with
-// scales of rows and columns; int8 4096 x 32 x 4096 4.7 -> 5.0, 5.6 with bias, scales and residual.
+// eight wide reads instead of a shuffle for each column), if it has any.  What it costs next to the plain product, us, device, in turn: bf16 16384 x 4096 x 4096 227 -> 228
+// with a bias and with SiLU, 231 with GELU, 242 with a residual (241 as C of sp24_gemm); int8 16384 x 512 x 4096 -> bf16 17.8 (sp24_gemm_i8_dequant, twelve epilogue
+// warps) -> 19.2 with scales of rows and columns; int8 4096 x 32 x 4096 4.5 -> 4.7, 5.2 with bias, scales and residual.
 template <int KIND, int COLUMNS>
 __device__ __forceinline__ void scale_row(uint32_t (&r)[COLUMNS], float scale, bool scaled, uint32_t col_scales, float bias) {
   auto pair = [&](int e, float2 f) {
