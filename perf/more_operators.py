@@ -300,10 +300,10 @@ def _run_own(s):
     y = sp.expert_linear(s["down"]["vals"], s["down"]["meta"], a, order.offsets)
     out = sp.expert_combine(y, order, weights, residual=s["x"])
     dy, dweights = sp.expert_combine_backward(s["dout"], y, order, weights)
-    da, d_down, _ = sp.expert_linear_backward(dy, None, a, s["down"]["W"], order.offsets, meta=s["down"]["meta"])
+    da, d_down, _ = sp.expert_linear_backward(dy, None, a, s["down"]["W"], order.offsets, meta=s["down"]["meta"], bias=False)
     dgu = torch.empty_like(gu)
     sp.gated_act_backward(da, gu[:, :F], gu[:, F:], act=act, dg=dgu[:, :F], du=dgu[:, F:])
-    dxs, d_up, _ = sp.expert_linear_backward(dgu, None, xs, s["up"]["W"], order.offsets, meta=s["up"]["meta"])
+    dxs, d_up, _ = sp.expert_linear_backward(dgu, None, xs, s["up"]["W"], order.offsets, meta=s["up"]["meta"], bias=False)
     dx = sp.expert_combine(dxs, order, residual=s["dout"])
     return out, dx, d_up, d_down, sp.route_backward(dweights, s["logits"], experts)
 
