@@ -441,6 +441,113 @@ sp24_status sp24_act_backward(sp24_dtype t, sp24_act act, int64_t rows, int64_t 
                               const void* z, int64_t ldz, void* dz, int64_t lddz, void* dzt, int64_t lddzt, float* dbias,
                               int sum_over_rows, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- experts ------------------------------------------------------------------------------------------------------------
+ * (No counterpart in the paper: a feed-forward layer of E experts with 2:4-sparse weights, of which each token uses k.)  The
+ * calls in the order of a layer: sp24_route chooses the experts of each token, sp24_expert_order gives every chosen slot (token,
+ * number) a row so that the rows of an expert lie together, sp24_expert_gather brings the tokens' rows there, sp24_expert_linear
+ * multiplies each expert's rows with its own weights, and sp24_expert_combine adds a token's rows up.  How many rows an expert
+ * has is known on the device only; nothing is read back.
+ *
+ * Routing.  l = logits[t, .] as FP32; scores s = softmax(l) or 1 / (1 + exp(-l)).
+ *   Choice: experts by l (bias == NULL) or by s + bias, the largest first, the lower index first among equal ones.  With
+ *   groups > 1 (a divisor of E; group g is experts g E / groups and on) only experts of the top_groups best groups: by the
+ *   largest of those values (SP24_GROUP_MAX) or by the sum of the two largest s + bias (SP24_GROUP_TOP2).  The values are
+ *   compared as real numbers: computed in FP32, and in FP64 where two are too close to tell.
+ *   weights[t, i] = scale * s of the i-th chosen, with renorm != 0 divided by the sum of the chosen s (their sum is then scale).
+ *   A logit of -infinity or NaN, and a bias of -infinity or NaN, is never chosen; where that leaves fewer than k, the rest has
+ *   experts -1 and weights 0 (a token without any: a padded batch).  A NaN among the logits, and with softmax +infinity, makes
+ *   the token's other weights NaN.
+ *   t: SP24_F16, SP24_BF16 or SP24_F32.  T >= 0 tokens, 1 <= E <= 1024, ld >= E, any alignment that the types have.
+ *   1 <= k <= min(32, top_groups * E / groups), groups <= 32.  bias: E floats.  weights: T x k floats, experts: T x k int32. */
+typedef enum { SP24_SCORE_SOFTMAX = 0, SP24_SCORE_SIGMOID = 1 } sp24_score;
+typedef enum { SP24_GROUP_MAX = 0, SP24_GROUP_TOP2 = 1 } sp24_group_score;
+sp24_status sp24_route(sp24_dtype t, int64_t T, int64_t E, const void* logits, int64_t ld, sp24_score score, const float* bias, int groups,
+                       int top_groups, sp24_group_score group_score, int k, int renorm, float scale, float* weights, int32_t* experts, void* stream);
+
+/* Gradient of sp24_route's weights with respect to the logits, the choice being fixed: from dweights (T x k floats), the logits and
+ * the experts chosen.  g = scale * dweights of the chosen, u = s / sum of the chosen s:
+ *   renorm: dl = u (g - sum u g) of the chosen experts (sigmoid: times 1 - s), 0 of the others;
+ *   else softmax: dl = s (g - sum of the chosen s g), g = 0 of the others; sigmoid: dl = g s (1 - s) of the chosen, 0 of the others.
+ * In FP32, rounded once to t.  A slot whose expert is negative or not below E counts for nothing; an expert that stands in two slots of a token
+ * gets both slots' gradients.  dlogits may be the logits themselves (same leading dimension). */
+sp24_status sp24_route_backward(sp24_dtype t, int64_t T, int64_t E, const float* dweights, const void* logits, int64_t ld, const int32_t* experts,
+                                int k, sp24_score score, int renorm, float scale, void* dlogits, int64_t ldd, void* stream);
+
+/* Order of `slots` = T k slots by their experts, stable: the slots of expert e get the rows offsets[e] and on, in their own order.
+ *   offsets: E + 1 int32; every one a multiple of `align`, the last where all rows end.
+ *   position: slots int32, the row of each slot, -1 if its expert is negative or not below E.
+ *   source: sp24_expert_rows(slots, E, align) int32, the slot of each row, -1 for rows that have none: between the experts where
+ *           align > 1, and behind the last.
+ *   1 <= E <= 1024, 1 <= align <= 256, 0 <= slots, sp24_expert_rows(...) < 2^31.  align = 1 is for inference; the gradient of the products'
+ *   weights wants 16. */
+int64_t sp24_expert_rows(int64_t slots, int64_t E, int64_t align);  /* slots + (align - 1) min(E, slots), up to a multiple of align */
+sp24_status sp24_expert_order(int64_t slots, int64_t E, int64_t align, const int32_t* experts, int32_t* offsets, int32_t* position,
+                              int32_t* source, void* stream);
+
+/* Rows in the experts' order: out[position[t, i], .] = x[t, .] for i < k; rows whose source is negative become zeros.  With scale (T floats), also
+ * out_scale[position[t, i]] = scale[t], 0 for those.  Any type of 1, 2 or 4 bytes; T x K of them, out rows x K.  Positions that are negative or not
+ * below `rows` are left out.  Fastest where rows start at 16-byte boundaries.  out overlaps no input. */
+sp24_status sp24_expert_gather(sp24_dtype t, int64_t T, int64_t K, const void* x, int64_t ldx, const float* scale, int k, const int32_t* position,
+                               int64_t rows, const int32_t* source, void* out, int64_t ldo, float* out_scale, void* stream);
+
+/* The tokens' sums: out[t, .] = sum over i < k of weights[t, i] y[position[t, i], .] (weights == NULL: ones) + residual[t, .], in FP32 in this order,
+ * rounded once to t (SP24_F16, SP24_BF16 or SP24_F32).  Slots without a row count for nothing, whatever their weight.  With NULL weights it is the gradient of
+ * sp24_expert_gather.  out may be the residual (same leading dimension). */
+sp24_status sp24_expert_combine(sp24_dtype t, int64_t T, int64_t K, int64_t rows, const void* y, int64_t ldy, int k, const int32_t* position,
+                                const float* weights, const void* residual, int64_t ldr, void* out, int64_t ldo, void* stream);
+
+/* Its gradients: dy[position[t, i], .] = weights[t, i] dout[t, .], rounded once; dweights[t, i] = sum over . of dout[t, .] y[position[t, i], .] in FP32 (0 of
+ * slots without a row); rows of dy whose source is negative become zeros.  dy may be y (same leading dimension). */
+sp24_status sp24_expert_combine_backward(sp24_dtype t, int64_t T, int64_t K, int64_t rows, const void* dout, int64_t lddo, const void* y, int64_t ldy, int k,
+                                         const int32_t* position, const int32_t* source, const float* weights, void* dy, int64_t lddy, float* dweights,
+                                         void* stream);
+
+/* sp24_linear of every expert's rows with its own weights, in one launch.  For rows r from offsets[e] to offsets[e + 1]:
+ *   z[r, i] = row_scale[e, i] * col_scale[r] * sum_k A_e[i, k] X[r, k] + bias[e, i],   D[r, i] = act(z[r, i]) + residual[r, i],
+ * with the arithmetic of sp24_linear.  Rows before offsets[0] and from offsets[E] on are neither used nor written.
+ *   A: the experts' values one after the other: E M rows of K / 2 (dense: K) values, leading dimension lda.
+ *   meta: E times sp24_meta_bytes(ab_type, M, K, SP24_META_TCGEN05) bytes, each expert's as sp24_compress gives it (not for dense A).
+ *   X: rows x K (leading dimension ldx), D, residual, pre: rows x M of cd_type (ldd, ld_residual, ld_pre), 16-byte aligned with leading
+ *      dimensions of whole 16 bytes.  residual may be D.
+ *   row_scale, bias: E x M floats; col_scale: rows floats; each may be NULL (col_scale: 8-bit operand types only).
+ *   offsets: device, E + 1 int32, 0 <= offsets[0] <= ... <= offsets[E] <= rows (values outside count as the nearest that are not).
+ *   ab_type: SP24_F16, SP24_BF16, SP24_I8, SP24_E4M3 or SP24_E5M2, cd_type as for sp24_linear.  M and K are multiples of 16, with 8-bit operands of
+ *   32; rows is any number.  1 <= E <= 1024, E M < 2^31.
+ *   workspace: as for sp24_gemm (sp24_gemm_status tells of an expired wait). */
+typedef struct {
+  sp24_dtype ab_type, cd_type;
+  int64_t E, M, K, rows;
+  int64_t lda, ldx, ldd, ld_residual, ld_pre;
+  int a_is_dense;
+} sp24_expert_desc;
+typedef struct {
+  const float* row_scale;
+  const float* col_scale;
+  const float* bias;
+  sp24_act act;
+  const void* residual;
+  void* pre;
+} sp24_expert_epilogue;
+sp24_status sp24_expert_linear(const sp24_expert_desc* d, const sp24_expert_epilogue* e, const void* A, const void* meta, const void* X,
+                               const int32_t* offsets, void* D, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The products of its gradient, for F16 or BF16 operands: dX[r, .] = sum_i dz[r, i] W_e[i, .] and dW_e[i, .] = sum over the expert's rows of dz[r, i] X[r, .], each
+ * rounded once to ab_type, with dense W (E M rows of K values, leading dimension d->lda).
+ *   sp24_expert_linear_dx: dz: rows x M (leading dimension d->ldd), dX: rows x K (ldx); only rows of experts are written.
+ *   sp24_expert_linear_dw: dzt: dz transposed, M x rows (leading dimension lddzt), X: rows x K (ldx), dW: E M x K (lda).  An expert without rows gets zeros.
+ *      Every offset is a multiple of 16 (sp24_expert_order with align = 16): the weights' gradients of an expert that is not so placed are NaN.
+ *   d->cd_type is ab_type; d->ld_residual, d->ld_pre and d->a_is_dense are not used.  Sizes, alignment and workspace as above.
+ * sp24_expert_bias_grad: dbias[e, i] = sum over the expert's rows of dy[r, i] act'(z[r, i]) in FP32, in an order that the offsets fix (z may be NULL for
+ *   SP24_ACT_NONE).  t: SP24_F16, SP24_BF16 or SP24_F32; any leading dimensions and alignment.  workspace: sp24_expert_bias_grad_workspace_bytes(...) bytes,
+ *   16-byte aligned, contents of no matter. */
+sp24_status sp24_expert_linear_dx(const sp24_expert_desc* d, const void* dz, const void* W, const int32_t* offsets, void* dX, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+sp24_status sp24_expert_linear_dw(const sp24_expert_desc* d, const void* dzt, int64_t lddzt, const void* X, const int32_t* offsets, void* dW, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+size_t sp24_expert_bias_grad_workspace_bytes(int64_t E, int64_t M, int64_t rows);
+sp24_status sp24_expert_bias_grad(sp24_dtype t, sp24_act act, int64_t E, int64_t M, int64_t rows, const void* dy, int64_t lddy, const void* z, int64_t ldz,
+                                  const int32_t* offsets, float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
 /* End-to-end convenience for callers whose data lives in HOST memory (pinned for speed):
  * copies dense A (M x K, row-major, packed), B (N rows of K, packed) and, if beta != 0, C
  * (M x N packed) to the device buffers the caller provides, runs sp24_compress (TCGEN05

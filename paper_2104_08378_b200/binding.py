@@ -14,6 +14,7 @@ import ctypes
 import functools
 import os
 from ctypes import byref
+from typing import NamedTuple
 
 import torch
 
@@ -37,7 +38,9 @@ EXPORTS = [
     "sp24_gemm_static_ws_status", "sp24_set_tile_override", "sp24_test_set_fault_hooks", "sp24_gemm_f16acc",
     "sp24_gemm_plan", "sp24_rms_norm", "sp24_rms_norm_backward_workspace_bytes", "sp24_rms_norm_backward",
     "sp24_gated_act", "sp24_gated_act_backward", "sp24_act_backward_workspace_bytes", "sp24_act_backward",
-    "sp24_linear",
+    "sp24_linear", "sp24_route", "sp24_route_backward", "sp24_expert_rows", "sp24_expert_order", "sp24_expert_gather",
+    "sp24_expert_combine", "sp24_expert_combine_backward", "sp24_expert_linear", "sp24_expert_linear_dx", "sp24_expert_linear_dw",
+    "sp24_expert_bias_grad_workspace_bytes", "sp24_expert_bias_grad",
 ]
 
 
@@ -59,6 +62,16 @@ class GemmDesc(ctypes.Structure):
 class LinearEpilogue(ctypes.Structure):
     _fields_ = [("row_scale", ctypes.c_void_p), ("col_scale", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("act", ctypes.c_int),
                 ("residual", ctypes.c_void_p), ("pre", ctypes.c_void_p), ("ld_pre", ctypes.c_int64)]
+
+
+class ExpertDesc(ctypes.Structure):
+    _fields_ = [("ab_type", ctypes.c_int), ("cd_type", ctypes.c_int)] + [
+        (name, ctypes.c_int64) for name in ("E", "M", "K", "rows", "lda", "ldx", "ldd", "ld_residual", "ld_pre")] + [("a_is_dense", ctypes.c_int)]
+
+
+class ExpertEpilogue(ctypes.Structure):
+    _fields_ = [("row_scale", ctypes.c_void_p), ("col_scale", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("act", ctypes.c_int),
+                ("residual", ctypes.c_void_p), ("pre", ctypes.c_void_p)]
 
 
 def _load() -> ctypes.CDLL:
@@ -115,6 +128,24 @@ def _load() -> ctypes.CDLL:
     lib.sp24_act_backward_workspace_bytes.restype = sz
     lib.sp24_act_backward.argtypes = [ci, ci, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, ci, vp, sz, vp]
     lib.sp24_linear.argtypes = [ctypes.POINTER(GemmDesc), ctypes.POINTER(LinearEpilogue), vp, vp, vp, vp, vp, sz, vp]
+    cf = ctypes.c_float
+    lib.sp24_route.argtypes = [ci, i64, i64, vp, i64, ci, vp, ci, ci, ci, ci, ci, cf, vp, vp, vp]
+    lib.sp24_route_backward.argtypes = [ci, i64, i64, vp, vp, i64, vp, ci, ci, ci, cf, vp, i64, vp]
+    lib.sp24_expert_rows.argtypes = [i64, i64, i64]
+    lib.sp24_expert_rows.restype = i64
+    lib.sp24_expert_order.argtypes = [i64, i64, i64, vp, vp, vp, vp, vp]
+    lib.sp24_expert_gather.argtypes = [ci, i64, i64, vp, i64, vp, ci, vp, i64, vp, vp, i64, vp, vp]
+    lib.sp24_expert_combine.argtypes = [ci, i64, i64, i64, vp, i64, ci, vp, vp, vp, i64, vp, i64, vp]
+    lib.sp24_expert_combine_backward.argtypes = [ci, i64, i64, i64, vp, i64, vp, i64, ci, vp, vp, vp, vp, i64, vp, vp]
+    lib.sp24_expert_linear.argtypes = [ctypes.POINTER(ExpertDesc), ctypes.POINTER(ExpertEpilogue), vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.sp24_expert_linear_dx.argtypes = [ctypes.POINTER(ExpertDesc), vp, vp, vp, vp, vp, sz, vp]
+    lib.sp24_expert_linear_dw.argtypes = [ctypes.POINTER(ExpertDesc), vp, i64, vp, vp, vp, vp, sz, vp]
+    lib.sp24_expert_bias_grad_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.sp24_expert_bias_grad_workspace_bytes.restype = sz
+    lib.sp24_expert_bias_grad.argtypes = [ci, ci, i64, i64, i64, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+    for name in ("sp24_route", "sp24_route_backward", "sp24_expert_order", "sp24_expert_gather", "sp24_expert_combine", "sp24_expert_combine_backward",
+                 "sp24_expert_linear", "sp24_expert_linear_dx", "sp24_expert_linear_dw", "sp24_expert_bias_grad"):
+        getattr(lib, name).restype = ci
     for name in ("sp24_linear", "sp24_rms_norm", "sp24_rms_norm_backward", "sp24_gated_act", "sp24_gated_act_backward", "sp24_act_backward"):
         getattr(lib, name).restype = ci
     for name in ("sp24_prune", "sp24_compress", "sp24_decompress", "sp24_gemm", "sp24_gemm_status",
@@ -788,3 +819,274 @@ def _linear_backward(dy, pre, Bt, W, *, act, meta, b_row_major, cd_col_major, ws
     if meta is not None:
         apply_mask(dW, meta, out=dW)
     return dBt, dW, dbias
+
+
+# ---- experts -------------------------------------------------------------------------------------------------------------------
+SCORE = {"softmax": 0, "sigmoid": 1}
+GROUP_SCORE = {"max": 0, "top2": 1}
+
+
+class ExpertOrder(NamedTuple):
+    """Where the slots (token, number) of a routing lie in the experts' order: the first row of each expert and the end [E + 1], the row of
+    each slot [T, k] and the slot, T * k of them, of each row [rows]; -1 where there is none.  All int32."""
+    offsets: torch.Tensor
+    position: torch.Tensor
+    source: torch.Tensor
+
+
+def route(logits: torch.Tensor, k: int, *, score: str = "softmax", bias: torch.Tensor | None = None, groups: int = 1, top_groups: int | None = None,
+          group_score: str = "max", renorm: bool = True, scale: float = 1.0):
+    """sp24_route: (weights [T, k] float32, experts [T, k] int32) from the logits [T, E] (f16, bf16 or f32), the best expert first.  score: "softmax" or
+    "sigmoid"; bias [E] float32 is added to the scores for the choice only; groups of E / groups experts, of which the top_groups (default: all) best by
+    group_score ("max", or "top2": the sum of the two largest) stay; renorm: the weights of a token add up to scale.  Logits of -inf are never chosen;
+    a slot that is left over has expert -1 and weight 0."""
+    return _route(logits, k, score, bias, groups, groups if top_groups is None else top_groups, group_score, renorm, scale)
+
+
+@_on_device_of("logits")
+def _route(logits, k, score, bias, groups, top_groups, group_score, renorm, scale):
+    where = "sp24_route"
+    t = _float_code(logits, where)
+    ld = _matrix(logits, where)
+    T, E = logits.shape
+    _refuse(score not in SCORE or group_score not in GROUP_SCORE, ERR_UNSUPPORTED, where)
+    _vector(bias, E, where, logits)
+    _refuse(not 1 <= k <= max(1, E), ERR_SHAPE, where)
+    weights = logits.new_empty((T, k), dtype=torch.float32)
+    experts = logits.new_empty((T, k), dtype=torch.int32)
+    _check(lib.sp24_route(t, T, E, _ptr(logits), ld, SCORE[score], _ptr(bias), groups, top_groups, GROUP_SCORE[group_score], k, 1 if renorm else 0, scale,
+                          _ptr(weights), _ptr(experts), _stream()), where)
+    return weights, experts
+
+
+def _slots(t: torch.Tensor, where: str, like: torch.Tensor, dtype, shape=None):
+    """A contiguous [T, k] of the type, on the device of `like`."""
+    _refuse(t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)), ERR_SHAPE, where)
+    _refuse(not t.is_cuda or t.device != like.device, ERR_UNSUPPORTED, where)
+    _refuse(t.dtype != dtype, ERR_DTYPE, where)
+    _refuse(not t.is_contiguous(), ERR_STRIDE, where)
+
+
+@_on_device_of("dweights")
+def route_backward(dweights: torch.Tensor, logits: torch.Tensor, experts: torch.Tensor, *, score: str = "softmax", renorm: bool = True, scale: float = 1.0,
+                   out: torch.Tensor | None = None) -> torch.Tensor:
+    """sp24_route_backward: the gradient of the logits [T, E] from that of route's weights [T, k], for the experts that it chose; score, renorm and scale as
+    there.  out may be the logits."""
+    where = "sp24_route_backward"
+    t = _float_code(logits, where)
+    ld = _matrix(logits, where)
+    T, E = logits.shape
+    _refuse(score not in SCORE, ERR_UNSUPPORTED, where)
+    _slots(experts, where, logits, torch.int32, (T, experts.shape[-1]))
+    _slots(dweights, where, logits, torch.float32, experts.shape)
+    dlogits = logits.new_empty((T, E)) if out is None else out
+    ldd = _matrix(dlogits, where, logits, logits.shape, logits.dtype)
+    _check(lib.sp24_route_backward(t, T, E, _ptr(dweights), _ptr(logits), ld, _ptr(experts), experts.shape[1], SCORE[score], 1 if renorm else 0, scale,
+                                   _ptr(dlogits), ldd, _stream()), where)
+    return dlogits
+
+
+@_on_device_of("experts")
+def expert_order(experts: torch.Tensor, E: int, *, align: int = 1) -> ExpertOrder:
+    """sp24_expert_order: where each slot of experts [T, k] (int32; negative or not below E: none) lies when the rows of an expert lie together, in their own
+    order.  Every expert's rows begin at a multiple of align: 1 for inference, 16 where expert_linear_backward is to follow."""
+    where = "sp24_expert_order"
+    _slots(experts, where, experts, torch.int32)
+    n = experts.numel()
+    _refuse(not 1 <= E <= 1024 or not 1 <= align <= 256 or n >= 2 ** 31, ERR_SHAPE, where)
+    order = ExpertOrder(experts.new_empty(E + 1), torch.empty_like(experts), experts.new_empty(lib.sp24_expert_rows(n, E, align)))
+    _check(lib.sp24_expert_order(n, E, align, _ptr(experts), _ptr(order.offsets), _ptr(order.position), _ptr(order.source), _stream()), where)
+    return order
+
+
+def _check_order(order: ExpertOrder, T: int, where: str, like: torch.Tensor):
+    _slots(order.position, where, like, torch.int32, (T, order.position.shape[-1]))
+    _vector(order.source, order.source.shape[0], where, like, (torch.int32,))
+
+
+@_on_device_of("x")
+def expert_gather(x: torch.Tensor, order: ExpertOrder, *, scale: torch.Tensor | None = None, out: torch.Tensor | None = None):
+    """sp24_expert_gather: (rows of x [T, K] in the order of the experts [rows, K], their scales [rows] or None without scale [T]); rows that no slot has are
+    zeros.  x of any type with 1, 2 or 4 bytes, as rms_norm gives it with its scale."""
+    where = "sp24_expert_gather"
+    code = _FROM_TORCH.get(x.dtype)
+    _refuse(code is None, ERR_DTYPE, where)
+    ldx = _matrix(x, where)
+    T, K = x.shape
+    _check_order(order, T, where, x)
+    rows = order.source.shape[0]
+    _vector(scale, T, where, x)
+    y = x.new_empty((rows, K)) if out is None else out
+    ldy = _matrix(y, where, x, (rows, K), x.dtype)
+    scales = None if scale is None else x.new_empty(rows, dtype=torch.float32)
+    _check(lib.sp24_expert_gather(DTYPE_CODE[code], T, K, _ptr(x), ldx, _ptr(scale), order.position.shape[1], _ptr(order.position), rows, _ptr(order.source),
+                                  _ptr(y), ldy, _ptr(scales), _stream()), where)
+    return y, scales
+
+
+@_on_device_of("y")
+def expert_combine(y: torch.Tensor, order: ExpertOrder, weights: torch.Tensor | None = None, *, residual: torch.Tensor | None = None,
+                   out: torch.Tensor | None = None) -> torch.Tensor:
+    """sp24_expert_combine: the sums [T, K] of each token's rows of y [rows, K] with route's weights [T, k] (None: ones, the gradient of expert_gather),
+    plus the residual [T, K].  out may be the residual."""
+    where = "sp24_expert_combine"
+    t = _float_code(y, where)
+    ldy = _matrix(y, where)
+    rows, K = y.shape
+    T, k = order.position.shape
+    _check_order(order, T, where, y)
+    _refuse(order.source.shape[0] != rows, ERR_SHAPE, where)
+    if weights is not None:
+        _slots(weights, where, y, torch.float32, (T, k))
+    o = y.new_empty((T, K)) if out is None else out
+    ldo = ldr = _matrix(o, where, y, (T, K), y.dtype)
+    if residual is not None:
+        ldr = _matrix(residual, where, y, (T, K), y.dtype)
+    _check(lib.sp24_expert_combine(t, T, K, rows, _ptr(y), ldy, k, _ptr(order.position), _ptr(weights), _ptr(residual), ldr, _ptr(o), ldo, _stream()), where)
+    return o
+
+
+@_on_device_of("dout")
+def expert_combine_backward(dout: torch.Tensor, y: torch.Tensor, order: ExpertOrder, weights: torch.Tensor, *, out: torch.Tensor | None = None):
+    """sp24_expert_combine_backward: (dy [rows, K], dweights [T, k]) of expert_combine from the gradient of its result; the residual's is dout itself.  Rows of dy
+    that no slot has are zeros.  out may be y."""
+    where = "sp24_expert_combine_backward"
+    t = _float_code(dout, where)
+    lddo = _matrix(dout, where)
+    T, K = dout.shape
+    _check_order(order, T, where, dout)
+    rows = order.source.shape[0]
+    ldy = _matrix(y, where, dout, (rows, K), dout.dtype)
+    _slots(weights, where, dout, torch.float32, order.position.shape)
+    dy = dout.new_empty((rows, K)) if out is None else out
+    lddy = _matrix(dy, where, dout, (rows, K), dout.dtype)
+    dweights = torch.empty_like(weights)
+    _check(lib.sp24_expert_combine_backward(t, T, K, rows, _ptr(dout), lddo, _ptr(y), ldy, order.position.shape[1], _ptr(order.position), _ptr(order.source),
+                                            _ptr(weights), _ptr(dy), lddy, _ptr(dweights), _stream()), where)
+    return dy, dweights
+
+
+def _stack(t: torch.Tensor, where: str, like: torch.Tensor | None = None, shape=None, dtype=None) -> int:
+    """The leading dimension of [E, M, columns]: E matrices with contiguous rows, one after the other."""
+    _refuse(t.dim() != 3 or (shape is not None and tuple(t.shape) != tuple(shape)), ERR_SHAPE, where)
+    _refuse(not t.is_cuda or (like is not None and t.device != like.device), ERR_UNSUPPORTED, where)
+    _refuse(dtype is not None and t.dtype != dtype, ERR_DTYPE, where)
+    E, M, n = t.shape
+    ld = t.stride(1) if M > 1 else (t.stride(0) if E > 1 else max(1, n))
+    _refuse((n > 1 and t.stride(2) != 1) or (E > 1 and M > 0 and t.stride(0) != M * ld), ERR_STRIDE, where)
+    return ld
+
+
+@_on_device_of("W")
+def expert_compress(W: torch.Tensor):
+    """sp24_compress of every expert's weights W [E, M, K]: (vals [E, M, K/2], meta [E, bytes]) as expert_linear takes them."""
+    where = "sp24_compress"
+    dt = _FROM_TORCH.get(W.dtype)
+    _refuse(dt is None or dt in ("i32", "f32"), ERR_DTYPE, where)
+    ld = _stack(W, where)
+    E, M, K = W.shape
+    vals, meta = W.new_empty((E, M, K // 2)), W.new_empty((E, meta_bytes(dt, M, K)), dtype=torch.uint8)
+    # (the metadata of an expert is whole blocks of 128 rows)
+    for first, n in ([(0, E * M)] if M % 128 == 0 else [(e, M) for e in range(E)]):
+        _check(lib.sp24_compress(DTYPE_CODE[dt], n, K, _ptr(W[first] if E else W), ld, _ptr(vals[first] if E else vals), K // 2,
+                                 _ptr(meta[first] if E else meta), META_TCGEN05, None, _stream()), where)
+    return vals, meta
+
+
+@_on_device_of("A")
+def expert_linear(A: torch.Tensor, meta: torch.Tensor | None, X: torch.Tensor, offsets: torch.Tensor, *, bias: torch.Tensor | None = None,
+                  act: str | None = None, residual: torch.Tensor | None = None, row_scale: torch.Tensor | None = None,
+                  col_scale: torch.Tensor | None = None, pre: bool | torch.Tensor = False, out: torch.Tensor | None = None, cd: str | None = None,
+                  a_is_dense: bool = False, ws: torch.Tensor | None = None):
+    """sp24_expert_linear: for the rows r of expert e, offsets[e] <= r < offsets[e + 1],
+    D[r, i] = act(row_scale[e, i] * col_scale[r] * (A_e X[r])[i] + bias[e, i]) + residual[r, i].  A: vals [E, M, K/2] and meta [E, bytes] of expert_compress (or
+    dense [E, M, K] with a_is_dense), X [rows, K], offsets [E + 1] int32 of expert_order, bias and row_scale [E, M], col_scale [rows] (8-bit operands),
+    residual [rows, M] in D's type (it may be `out`).  Returns D [rows, M] of type cd (A's own, bf16 for 8-bit operands), or with pre=True (or a tensor
+    for it) (D, what act was applied to).  Rows that belong to no expert are left as they are.  M and K are multiples of 16, with 8-bit operands of 32."""
+    where = "sp24_expert_linear"
+    ab = _FROM_TORCH.get(A.dtype)
+    _refuse(ab not in ("f16", "bf16") + _QUANT, ERR_DTYPE, where)
+    lda, ldx = _stack(A, where), _matrix(X, where, A, None, A.dtype)
+    E, M, K = A.shape[0], A.shape[1], A.shape[2] * (1 if a_is_dense else 2)
+    rows = X.shape[0]
+    _refuse(X.shape[1] != K, ERR_SHAPE, where)
+    _vector(offsets, E + 1, where, A, (torch.int32,))
+    if not a_is_dense:
+        _refuse(meta is None, 1, where)
+        _refuse(meta.dim() != 2, ERR_SHAPE, where)
+        _slots(meta, where, A, torch.uint8, (E, meta_bytes(ab, M, K)))
+    cd = cd or ("bf16" if ab in _QUANT else ab)
+    _refuse(cd not in TORCH_DTYPE, ERR_DTYPE, where)
+    shape, dtype = (rows, M), TORCH_DTYPE[cd]
+    D = A.new_empty(shape, dtype=dtype) if out is None else out
+    ldd = _matrix(D, where, A, shape, dtype)
+    ld_residual = ld_pre = ldd
+    if residual is not None:
+        ld_residual = _matrix(residual, where, A, shape, dtype)
+    for v in (bias, row_scale):
+        if v is not None:
+            _slots(v, where, A, torch.float32, (E, M))
+    _vector(col_scale, rows, where, A)
+    z = None
+    if pre is not False and pre is not None:
+        z = torch.empty_like(D) if pre is True else pre
+        ld_pre = _matrix(z, where, A, shape, dtype)
+    stream = _stream()
+    ws = ws if ws is not None else workspace(A.device, stream)
+    desc = ExpertDesc(DTYPE_CODE[ab], DTYPE_CODE[cd], E, M, K, rows, lda, ldx, ldd, ld_residual, ld_pre, 1 if a_is_dense else 0)
+    epilogue = ExpertEpilogue(_ptr(row_scale), _ptr(col_scale), _ptr(bias), _act_code(act, where), _ptr(residual), _ptr(z))
+    _check(lib.sp24_expert_linear(byref(desc), byref(epilogue), _ptr(A), _ptr(meta), _ptr(X), _ptr(offsets), _ptr(D), _ptr(ws), ws.numel(), stream), where)
+    return D if z is None else (D, z)
+
+
+@_on_device_of("dy")
+def expert_linear_backward(dy: torch.Tensor, pre: torch.Tensor | None, X: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, *, act: str | None = None,
+                           meta: torch.Tensor | None = None, bias: bool = True, ws: torch.Tensor | None = None):
+    """Gradients of expert_linear (16-bit operands) from dy [rows, M], its `pre` (None without an activation), X [rows, K] and the pruned weights W [E, M, K]
+    themselves: (dX [rows, K], dW [E, M, K], dbias [E, M] float32, or None with bias=False).  Every offset is a multiple of 16 (expert_order with align=16): the
+    dW of an expert that is not so placed is NaN.  With meta [E, bytes] the entries of dW that the 2:4 pattern leaves out are zeros.  Rows of dX that belong to
+    no expert are left as they are; an expert without rows has dW and dbias of zeros.  The residual's gradient is dy.  dz = dy act'(pre) is rounded to dy's type
+    before the two products, dbias is not."""
+    where = "sp24_expert_linear_backward"
+    code = _FROM_TORCH.get(dy.dtype)
+    _refuse(code not in ("f16", "bf16"), ERR_DTYPE, where)
+    lddy = _matrix(dy, where)
+    ldw = _stack(W, where, dy, None, dy.dtype)
+    E, M, K = W.shape
+    rows = dy.shape[0]
+    _refuse(dy.shape[1] != M, ERR_SHAPE, where)
+    ldx = _matrix(X, where, dy, (rows, K), dy.dtype)
+    _vector(offsets, E + 1, where, dy, (torch.int32,))
+    a = _act_code(act, where)
+    _refuse(M % 16 or K % 16, ERR_SHAPE, where)
+    _refuse(bool(a) and pre is None, 1, where)
+    ldz = _matrix(pre, where, dy, dy.shape, dy.dtype) if a else lddy
+    if meta is not None:
+        _slots(meta, where, dy, torch.uint8, (E, meta_bytes(code, M, K)))
+    t, stream = DTYPE_CODE[code], _stream()
+    ws = ws if ws is not None else workspace(dy.device, stream)
+    # dz in both orders: the products contract over different axes (without an activation dz is dy itself, where a product can take it)
+    dz, lddz = dy, lddy
+    if a or dy.data_ptr() % 16 or lddy * dy.element_size() % 16:
+        dz, lddz = dy.new_empty((rows, M)), M
+    lddzt = (rows + 7) // 8 * 8
+    dzt = dy.new_empty((M, lddzt))
+    if rows:
+        _check(lib.sp24_act_backward(t, a, rows, M, _ptr(dy), lddy, _ptr(pre) if a else None, ldz, None if dz is dy else _ptr(dz), lddz, _ptr(dzt), lddzt,
+                                     None, 1, None, 0, stream), where)
+    dX, dW = dy.new_empty((rows, K)), dy.new_empty((E, M, K))
+    desc = ExpertDesc(t, t, E, M, K, rows, ldw, K, lddz, 0, 0, 1)
+    _check(lib.sp24_expert_linear_dx(byref(desc), _ptr(dz), _ptr(W), _ptr(offsets), _ptr(dX), _ptr(ws), ws.numel(), stream), where)
+    desc = ExpertDesc(t, t, E, M, K, rows, K, ldx, lddz, 0, 0, 1)
+    _check(lib.sp24_expert_linear_dw(byref(desc), _ptr(dzt), max(8, lddzt), _ptr(X), _ptr(offsets), _ptr(dW), _ptr(ws), ws.numel(), stream), where)
+    if meta is not None:
+        for first, n in ([(0, E * M)] if M % 128 == 0 else [(e, M) for e in range(E)]):
+            _check(lib.sp24_apply_mask(t, n, K, _ptr(dW[first]), K, _ptr(meta[first]), META_TCGEN05, _ptr(dW[first]), K, stream), where)
+    dbias = None
+    if bias:
+        dbias = dy.new_empty((E, M), dtype=torch.float32)
+        size = lib.sp24_expert_bias_grad_workspace_bytes(E, M, rows)
+        scratch = dy.new_empty(size, dtype=torch.uint8)
+        _check(lib.sp24_expert_bias_grad(t, a, E, M, rows, _ptr(dy), lddy, _ptr(pre) if a else None, ldz, _ptr(offsets), _ptr(dbias), _ptr(scratch), size, stream),
+               where)
+    return dX, dW, dbias

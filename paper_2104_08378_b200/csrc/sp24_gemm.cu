@@ -144,6 +144,17 @@ Settings& settings() {
 }
 
 }  // namespace
+
+// Test hooks for the failure path (set through sp24_test_set_fault_hooks only): a shorter limit, and a
+// pipeline that stalls by leaving out one k-block.  Nothing faults or hangs: the waits expire and the
+// kernel returns.
+void set_wait_limit(GemmParams& p) {
+  Settings& cfg = settings();
+  p.wait_limit = kWaitTimeoutCycles;
+  const long long v = cfg.test_wait_cycles.load(std::memory_order_relaxed);
+  if (v >= 1000000) p.wait_limit = v;
+  p.test_skip_stage = cfg.test_skip_stage.load(std::memory_order_relaxed);
+}
 }  // namespace sp24
 
 using namespace sp24;
@@ -541,16 +552,8 @@ static sp24_status run_gemm(const sp24_gemm_desc* d, const void* alpha, const vo
   p.a_fmt = (d->ab_type == SP24_BF16 || d->ab_type == SP24_E5M2) ? 1 : 0;
   p.cd_type = (int)d->cd_type;
   p.has_c = has_c ? 1 : 0;
-  p.wait_limit = kWaitTimeoutCycles;
-  // Test hooks for the failure path (set through sp24_test_set_fault_hooks only): a shorter limit, and a
-  // pipeline that stalls by leaving out one k-block.  Nothing faults or hangs: the waits expire and the
-  // kernel returns.
+  set_wait_limit(p);
   Settings& cfg = settings();
-  {
-    const long long v = cfg.test_wait_cycles.load(std::memory_order_relaxed);
-    if (v >= 1000000) p.wait_limit = v;
-    p.test_skip_stage = cfg.test_skip_stage.load(std::memory_order_relaxed);
-  }
   p.cd_col_major = d->order_d == SP24_COL_MAJOR ? 1 : 0;
   const bool sparse = !d->a_is_dense;
   const bool i8 = d->ab_type == SP24_I8, tf32 = d->ab_type == SP24_F32, f8 = is_fp8(d->ab_type);

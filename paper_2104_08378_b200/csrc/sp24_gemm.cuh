@@ -82,6 +82,10 @@ struct GemmParams {
   const float* col_scale;
   void* pre;
   int64_t ld_pre;
+  // the products of many experts in one launch (see the kernel's GROUP): E + 1 first rows, of `rows` rows; bytes of the tables made of them; metadata
+  // blocks of 128 rows of an expert
+  const int32_t* offsets;
+  int32_t experts, rows, table_bytes, meta_blocks;
 };
 
 constexpr int kSwizzle128Atom32 = 1280;
@@ -127,5 +131,15 @@ sp24_status launch_gemm(TileShape tile, bool sparse, bool b_mn, const sp24_gemm_
 template <int KIND>
 sp24_status launch_linear(TileShape tile, bool sparse, bool b_mn, const sp24_gemm_desc* d, const GemmParams& p, const void* A,
                           const void* meta, const void* B, cudaStream_t s);
+
+// ---- in sp24_expert_{f16,i8,f8}.cu ---------------------------------------------------------------------
+// One launch of the kernel over the problems of all experts (group: see the kernel's Group).  d: M, N and K of an expert's problem, of which the one that
+// differs from expert to expert is p.rows, the rows there are; sizes and leading dimensions as for launch_gemm.
+template <int KIND>
+sp24_status launch_experts(int group, TileShape tile, bool sparse, const sp24_gemm_desc* d, const GemmParams& p, const void* A, const void* meta, const void* B,
+                           cudaStream_t s);
+
+// The status record's limit of a wait and test hook (sp24_test_set_fault_hooks) into p.
+void set_wait_limit(GemmParams& p);
 
 }  // namespace sp24

@@ -189,6 +189,90 @@ __device__ __forceinline__ void tile_coords(int t, const GemmParams& p, int& mt,
   if (band & 1) nt = p.n_tiles - 1 - nt;
 }
 
+// GROUP: the products of many experts in one launch (sp24_expert_linear and its gradients), each a problem of its own over the same
+// tensor maps.  The experts' rows are a range of one dimension, known on the device only: of the columns (B and D hold the rows of tokens), of the rows
+// (A and D), or of K (A and B; D is an expert's own).
+enum Group { kOneProblem = 0, kColumnsByExpert = 1, kRowsByExpert = 2, kKByExpert = 3 };
+
+// In shared memory: where each expert's rows begin (E + 1 entries, in range and in order whatever the offsets are), and its first tile (E + 1, the last: how
+// many there are).
+struct Experts {
+  int *row, *tile;
+};
+
+// One tile: its problem's sizes, the tile's place in it, and where the expert's rows begin.
+struct Tile {
+  int mt, nt, M, N, k, expert, at;
+};
+
+template <int GROUP, int TILE_M>
+__device__ __forceinline__ void lay_out_experts(const GemmParams& p, const Experts& x) {
+  const int E = p.experts;
+  for (int e = threadIdx.x; e <= E; e += blockDim.x) x.row[e] = min(max(p.offsets[e], 0), p.rows);
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    const int lane = threadIdx.x;
+    int tiles = 0, end = 0;  // of the experts before
+    for (int e0 = 0; e0 <= E; e0 += 32) {
+      const int e = e0 + lane;
+      int last = e <= E ? x.row[e] : 0;  // (a row before that of an expert in front counts as that one)
+#pragma unroll
+      for (int i = 1; i < 32; i <<= 1) last = max(last, __shfl_up_sync(~0u, last, i));
+      last = max(last, end);
+      if (e <= E) x.row[e] = last;
+      __syncwarp();
+      const int next = e + 1 <= E ? max(x.row[e + 1], last) : last;  // (lane 31: the next chunk's first, as it came)
+      const int n = next - last;
+      int mine = 0;
+      if (e < E) {
+        if (GROUP == kColumnsByExpert) mine = p.m_tiles * ((n + p.tile_n - 1) / p.tile_n);
+        else if (GROUP == kRowsByExpert) mine = p.n_tiles * ((n + TILE_M - 1) / TILE_M);
+        else mine = p.m_tiles * p.n_tiles;
+      }
+      int sum = mine;
+#pragma unroll
+      for (int i = 1; i < 32; i <<= 1) {
+        const int left = __shfl_up_sync(~0u, sum, i);
+        if (lane >= i) sum += left;
+      }
+      if (e <= E) x.tile[e] = tiles + sum - mine;
+      tiles += __shfl_sync(~0u, sum, 31);
+      end = __shfl_sync(~0u, last, 31);
+      __syncwarp();
+    }
+  }
+  __syncthreads();
+}
+
+template <int GROUP>
+__device__ __forceinline__ Tile find_tile(int t, const GemmParams& p, const Experts& x) {
+  Tile g = {0, 0, (int)p.M, (int)p.N, 0, 0, 0};
+  if constexpr (GROUP == kOneProblem) {
+    tile_coords(t, p, g.mt, g.nt);
+  } else {
+    int lo = 0, hi = p.experts - 1;  // the last expert whose first tile is not behind t
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (x.tile[mid] <= t) lo = mid;
+      else hi = mid - 1;
+    }
+    const int r = t - x.tile[lo], n = x.row[lo + 1] - x.row[lo], q = p.by_band(r);  // (by the tiles of the dimension that all experts share)
+    g.expert = lo;
+    g.at = x.row[lo];
+    if constexpr (GROUP == kRowsByExpert) {
+      g.mt = q;
+      g.nt = r - q * p.n_tiles;
+      g.M = n;
+    } else {
+      g.nt = q;
+      g.mt = r - q * p.m_tiles;
+      if constexpr (GROUP == kColumnsByExpert) g.N = n;
+      else g.k = n;
+    }
+  }
+  return g;
+}
+
 template <int KIND>
 __device__ __forceinline__ uint32_t make_idesc(bool sparse, bool b_mn_major, int a_fmt, int m, int n, bool acc_f16) {
   uint32_t d = 0;
@@ -443,10 +527,10 @@ __device__ __forceinline__ void convert_row_staged(const uint32_t (&r)[32], uint
 // half as wide, meet in pairs).
 // C is loaded in the order of the stores (whole 64-byte row segments as well) into registers, four boxes ahead, the
 // first four of a tile before its accumulators are complete, and goes to the rows' owners through the buffer.
-template <int KIND, int CS, bool COLS, bool HAS_C, int BLOCK_N, int CTAS, int MBLK, int ACC_STAGES, int WARPS, bool SPLIT, bool LINEAR>
+template <int KIND, int CS, bool COLS, bool HAS_C, int BLOCK_N, int CTAS, int MBLK, int ACC_STAGES, int WARPS, bool SPLIT, bool LINEAR, int GROUP>
 __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh, uint8_t* epi, uint32_t tmem_base,
                                               int cta_rank, int cluster_id, int num_clusters, int num_tiles, int warp,
-                                              int lane, uint32_t parts, int split_rank) {
+                                              int lane, uint32_t parts, int split_rank, const Experts& experts) {
   constexpr int kCols = CS == 4 ? 16 : 32;  // columns of a box
   constexpr int W = kCols * CS / 4;         // 32-bit words of one box row
   constexpr int P = LINEAR ? 2 : 4;         // boxes whose C values are held in registers (as many copies of the code of a box)
@@ -460,8 +544,10 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
   const bool scaled = LINEAR && one_byte_operands(KIND) && p.col_scale;
   const uint8_t* Cb = static_cast<const uint8_t*>(p.C);
   uint8_t* Db = static_cast<uint8_t*>(p.D);
+  uint8_t* Zb = static_cast<uint8_t*>(p.pre);
+  const float *row_scales = p.row_scale, *biases = p.bias, *col_scales = p.col_scale;
   const size_t ldc_b = (size_t)p.ldc * CS, ldd_b = (size_t)p.ldd * CS;
-  const int M = (int)p.M, N = (int)p.N;
+  int M = (int)p.M, N = (int)p.N;
   constexpr bool has_c = HAS_C;
   // this lane's row of the buffer, its unit 0 under the swizzle (xor the unit into bits 4..5) ...
   const uint32_t own_row = ptx::smem_u32(stage) + (uint32_t)(lane * 64 + ((((lane >> 1) ^ (lane >> 3)) & 3) << 4));
@@ -487,8 +573,28 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
   int acc = 0;
   uint32_t acc_phase = 0;
   for (int t = cluster_id; t < num_tiles && !sh->abort; t += num_clusters) {
-    int mt, nt;
-    tile_coords(t, p, mt, nt);
+    const Tile g = find_tile<GROUP>(t, p, experts);
+    const int mt = g.mt, nt = g.nt;
+    bool no_sums = false;  // (no k: the accumulators hold nothing)
+    uint32_t instead = 0;
+    if constexpr (GROUP != kOneProblem) {  // everything of this expert
+      M = g.M;
+      N = g.N;
+      const int64_t lines = GROUP == kKByExpert ? (int64_t)g.expert * M : g.at;
+      Db = static_cast<uint8_t*>(p.D) + lines * ldd_b;
+      if (GROUP == kColumnsByExpert) {
+        Cb = static_cast<const uint8_t*>(p.C) + lines * ldc_b;
+        Zb = static_cast<uint8_t*>(p.pre) + lines * p.ld_pre * CS;
+        row_scales = p.row_scale + (int64_t)g.expert * M;
+        biases = p.bias + (int64_t)g.expert * M;
+        col_scales = p.col_scale + g.at;
+      }
+      if (GROUP == kKByExpert) {
+        const bool placed = ((g.at | g.k) & 15) == 0;
+        no_sums = g.k == 0 || !placed;
+        instead = placed ? 0u : 0x7fffffffu;
+      }
+    }
     const int tile_col = nt * p.tile_n, col_end = min(N, tile_col + p.tile_n);  // columns of this tile stop here
     // the boxes of this lane quarter: `nsub` in a row, `blocks` rows of them (m-blocks); the warps take them in turn
     const int row_q = (is_tall<CTAS, MBLK> ? mt * p.mblk * kBlockM : first_row<CTAS, MBLK>(mt, cta_rank, M)) + q * 32;
@@ -607,13 +713,13 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
     uint32_t r[kCols], creg[P][W];
     float scale = 1.f, bias = 0.f, col_scale = 1.f;
     auto load_col_scale = [&](int col0) {  // lane e: that of column e of the box
-      if (scaled) col_scale = p.col_scale[min(col0 + lane, N - 1)];
+      if (scaled) col_scale = col_scales[min(col0 + lane, N - 1)];
     };
     auto load_scale = [&](int row0) {
       if (LINEAR) {
         const int row = min(row0 + lane, M - 1);
-        if (p.row_scale) scale = p.row_scale[row];
-        if (p.bias) bias = p.bias[row];
+        if (p.row_scale) scale = row_scales[row];
+        if (p.bias) bias = biases[row];
       } else if (KIND == 1 && p.dequant) {
         const int row = min(row0 + lane, M - 1);
         scale = p.row_scale[row];
@@ -646,7 +752,11 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
           }
         }
       }
-      if (KIND == 0 && p.acc_f16) widen_f16_accumulators(r);
+      if (GROUP == kOneProblem && KIND == 0 && p.acc_f16) widen_f16_accumulators(r);
+      if (GROUP == kKByExpert && no_sums) {
+#pragma unroll
+        for (int e = 0; e < kCols; ++e) r[e] = instead;
+      }
       bool again = false;
       if constexpr (LINEAR) {
         if (scaled) {
@@ -658,7 +768,7 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
         scale_row<KIND>(r, scale, scaled, ptx::smem_u32(stage), bias);
         if (__builtin_expect(p.pre != nullptr, 0)) {
           pack_row<CS>(r, p.cd_type, o);
-          store_to(static_cast<uint8_t*>(p.pre), (size_t)p.ld_pre * CS, again, o, row0, col0);
+          store_to(Zb, (size_t)p.ld_pre * CS, again, o, row0, col0);
           again = true;
         }
         if (__builtin_expect(p.act != SP24_ACT_NONE, 0)) activate_row(r, p.act);
@@ -735,7 +845,7 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
 // and without C apart (the registers of four boxes of it): f16 256 x 256 x 512 3.29 -> 3.19, BERT FFN 12.48 -> 12.26, bf16
 // 8480 x 896 x 384 7.83 -> 7.46, with C 9920 x 544 x 1216 16.1 -> 15.6, f16 1184 x 736 x 1008 5.92 -> 5.82; none slower.
 template <int KIND, bool SPARSE, int BLOCK_N, int CTAS, int MBLK, bool B_MN, int CS, bool COLS, bool HAS_C, bool SPLIT = false, int WARPS = kEpiWarps,
-          bool LINEAR = false>
+          bool LINEAR = false, int GROUP = kOneProblem>
 __global__ void __launch_bounds__(32 * (kFirstEpiWarp + WARPS), 1)
 gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
             const __grid_constant__ CUtensorMap map_e, const __grid_constant__ CUtensorMap map_c,
@@ -745,14 +855,15 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   // Operand atoms need 1024-byte alignment for the 128-byte swizzle.
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   constexpr bool kTall = is_tall<CTAS, MBLK>;
-  constexpr bool kStaged = !LINEAR && C::staged_epilogue(CS, COLS);
+  constexpr bool kStaged = !LINEAR && GROUP == kOneProblem && C::staged_epilogue(CS, COLS);
   static_assert(!kTall || (SPARSE && !B_MN && C::kABoxes == 1 && C::kBBoxes == 2), "tall tiles: sparse A, K-major B");
   // tall tiles: [slots of A and metadata | slots of B | epilogue staging]
   const int tile_n = p.tile_n, b_bytes = C::b_bytes(tile_n), b_slot_bytes = kTall ? b_bytes : 0;
   const int kps = C::kPairsOfKBlocks ? p.kps : 1;  // k-blocks of a stage
   const int slot_bytes = kTall ? C::kABlockBytes + C::kEBlockBytes : kps * (C::kABytes + b_bytes + C::kEAlloc);
   uint8_t* b_ring = smem + p.stages * slot_bytes;
-  uint8_t* epi = b_ring + (kTall ? p.b_stages * b_slot_bytes : SPLIT ? p.part_bytes : 0);
+  uint8_t* epi = b_ring + (kTall ? p.b_stages * b_slot_bytes : SPLIT ? p.part_bytes : GROUP != kOneProblem ? p.table_bytes : 0);
+  const Experts experts = {reinterpret_cast<int*>(b_ring), reinterpret_cast<int*>(b_ring) + p.experts + 1};
   Shared* sh = reinterpret_cast<Shared*>(epi + p.epi_bytes);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -764,8 +875,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   const int num_clusters = SPLIT ? gridDim.x >> split_log : gridDim.x / CTAS;
   // this CTA's k-blocks
   const int kb_begin = SPLIT ? (p.k_blocks * split_rank) >> split_log : 0;
-  const int kb_end = SPLIT ? (p.k_blocks * (split_rank + 1)) >> split_log : p.k_blocks;
-  const int num_tiles = p.m_tiles * p.n_tiles;
+  const int last_kb = SPLIT ? (p.k_blocks * (split_rank + 1)) >> split_log : p.k_blocks;
+  int num_tiles = p.m_tiles * p.n_tiles;
   // (test hook: the CTA whose k-block is left out waits longer, so that the others' waits for its sums are the first to expire)
   auto wait_limit = [&] { return SPLIT && p.test_skip_stage == 2 + split_rank ? 4 * p.wait_limit : p.wait_limit; };
 
@@ -809,6 +920,21 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   const uint32_t tmem_base = sh->tmem_base;
   let_next_start();
   wait_for_stream();
+  static_assert(GROUP == kOneProblem || (!kTall && !SPLIT && MBLK == 1), "experts: tiles of one m-block");
+  if constexpr (GROUP != kOneProblem) {
+    lay_out_experts<GROUP, kBlockM * CTAS>(p, experts);
+    num_tiles = experts.tile[p.experts];
+  }
+
+  // columns of a tile that are multiplied: those there are, up to the instruction's next multiple
+  auto columns = [&](const Tile& g) -> int {
+    if constexpr (GROUP == kColumnsByExpert) {
+      constexpr int step = one_byte_operands(KIND) ? 32 : 16;
+      return min(tile_n, (g.N - g.nt * tile_n + step - 1) / step * step);
+    } else {
+      return min(tile_n, (int)(p.N - (int64_t)g.nt * tile_n));
+    }
+  };
 
   // tall tiles: m-blocks of tile row mt that have rows (the rest are neither loaded nor multiplied) ...
   auto tall_live = [&](int mt) -> int { return min(p.mblk, ((int)p.M - mt * p.mblk * kBlockM + kBlockM - 1) / kBlockM); };
@@ -929,12 +1055,21 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       const uint32_t ring = ptx::smem_u32(smem);
       const uint32_t full0 = CTAS == 2 ? ptx::map_to_cta(ptx::smem_u32(&sh->full[0]), 0) : ptx::smem_u32(&sh->full[0]);
       for (int t = cluster_id; t < num_tiles && !sh->abort; t += num_clusters) {
-        int mt, nt;
-        tile_coords(t, p, mt, nt);
+        const Tile g = find_tile<GROUP>(t, p, experts);
+        const int mt = g.mt, nt = g.nt;
         // the last n-tile may be narrower: the pair then splits only the columns that exist
-        const int n_eff = min(tile_n, (int)(p.N - (int64_t)nt * tile_n));
-        const int col0 = nt * tile_n + (int)cta_rank * (n_eff / CTAS);  // first B row (N index)
-        const int row0 = first_row<CTAS, MBLK>(mt, (int)cta_rank, (int)p.M);
+        const int n_eff = columns(g);
+        int col0 = nt * tile_n + (int)cta_rank * (n_eff / CTAS);  // first B row (N index)
+        int row0 = first_row<CTAS, MBLK>(mt, (int)cta_rank, g.M);
+        int meta_block = row0 / kBlockM;
+        if constexpr (GROUP == kColumnsByExpert) {
+          meta_block += g.expert * p.meta_blocks;
+          row0 += g.expert * g.M;
+          col0 += g.at;
+        }
+        if constexpr (GROUP == kRowsByExpert) row0 += g.at;
+        const int k0 = GROUP == kKByExpert ? g.at & ~15 : 0;  // (a copy starts at a 16-byte boundary, wherever the expert does)
+        const int kb_end = GROUP == kKByExpert ? (g.k + C::kKPerStage - 1) / C::kKPerStage : last_kb;
         const uint32_t tx_bytes = (uint32_t)((C::kABytes + C::kEBytes + b_bytes) * CTAS);
         // implicit convolution: (image, row, column) of this CTA's first output pixel
         int conv_n = 0, conv_p = 0, conv_q = 0, conv_c0 = 0, conv_r = 0, conv_s = 0;
@@ -955,7 +1090,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
               const uint32_t sa = ring + stage * slot_bytes, sb = sa + 2 * C::kABytes, se = sb + 2 * b_bytes;
               const uint32_t full = full0 + 8 * stage;
               if (cta_rank == 0) ptx::mbar_expect_tx(&sh->full[stage], 2 * tx_bytes);
-              ptx::tma_load_3d<CTAS>(se, &map_e, full, 0, 16 * kb * C::kEBlocks, row0 / kBlockM);
+              ptx::tma_load_3d<CTAS>(se, &map_e, full, 0, 16 * kb * C::kEBlocks, meta_block);
               ptx::tma_load_3d<CTAS>(sa, &map_a, full, 0, row0, kb);
               ptx::tma_load_3d<CTAS>(sb, &map_b, full, 0, col0, kb * C::kBBoxes);
             }
@@ -976,14 +1111,19 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
           const uint32_t full = full0 + 8 * stage;
           if (cta_rank == 0) ptx::mbar_expect_tx(&sh->full[stage], tx_bytes);
           // both m-blocks' rows and metadata blocks are neighbours: one box each
-          if (SPARSE) ptx::tma_load_3d<CTAS>(se, &map_e, full, 0, 16 * kb * C::kEBlocks, row0 / kBlockM);
+          if (SPARSE) ptx::tma_load_3d<CTAS>(se, &map_e, full, 0, 16 * kb * C::kEBlocks, meta_block);
 #pragma unroll
           for (int i = 0; i < C::kABoxes; ++i)
-            ptx::tma_load_2d<CTAS>(sa + i * MBLK * kBlockM * kAtomBytes, &map_a, full, (kb * C::kABoxes + i) * box_elems, row0);
+            ptx::tma_load_2d<CTAS>(sa + i * MBLK * kBlockM * kAtomBytes, &map_a, full, k0 + (kb * C::kABoxes + i) * box_elems, row0);
           if (B_MN) {
             // B stored N-contiguous: boxes of 128 bytes along N x all k-rows of the stage
-            for (int c = 0; c < C::b_chunks(tile_n); ++c)
-              ptx::tma_load_2d<CTAS>(sb + c * C::kBChunkBytes, &map_b, full, col0 + c * C::kBChunkElems, kb * C::kKPerStage);
+            for (int c = 0; c < C::b_chunks(tile_n); ++c) {
+              // (the weights of the experts are a third dimension: what is behind one expert's last row is zeros, not the next one's)
+              if constexpr (GROUP == kRowsByExpert)
+                ptx::tma_load_3d<CTAS>(sb + c * C::kBChunkBytes, &map_b, full, col0 + c * C::kBChunkElems, kb * C::kKPerStage, g.expert);
+              else
+                ptx::tma_load_2d<CTAS>(sb + c * C::kBChunkBytes, &map_b, full, col0 + c * C::kBChunkElems, k0 + kb * C::kKPerStage);
+            }
           } else if (p.conv) {
             // k = (r * 3 + s) * C + c: a stage holds channels of one filter tap; rows = output pixels
 #pragma unroll
@@ -1019,11 +1159,12 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       int stage = 0, acc = 0;
       uint32_t phase = 0, acc_phase = 0, e_buf = 0;
       for (int t = cluster_id; t < num_tiles && !sh->abort; t += num_clusters) {
-        int mt, nt;
-        tile_coords(t, p, mt, nt);
+        const Tile g = find_tile<GROUP>(t, p, experts);
+        const int mt = g.mt;
         // instruction N = the columns this tile really has (a multiple of 16, of 32 for int8)
-        const int n_eff = min(tile_n, (int)(p.N - (int64_t)nt * tile_n));
-        const int live = live_blocks<CTAS, MBLK>(mt, (int)p.M);  // m-blocks with rows (others are not multiplied)
+        const int n_eff = columns(g);
+        const int live = live_blocks<CTAS, MBLK>(mt, g.M);  // m-blocks with rows (others are not multiplied)
+        const int kb_end = GROUP == kKByExpert ? (g.k + C::kKPerStage - 1) / C::kKPerStage : last_kb;
         const uint32_t idesc = make_idesc<KIND>(SPARSE, B_MN, p.a_fmt, kBlockM * CTAS, n_eff, KIND == 0 && p.acc_f16);
         // the MMAs of a k-block: A, B and metadata at sa, sb, se
         auto multiply = [&](int kb, uint32_t sa, uint32_t sb, uint32_t se) {
@@ -1049,6 +1190,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             const uint64_t da0 = ptx::smem_desc(sa + j * C::kABlockBytes, ptx::kLayoutSw128, 1024);
 #pragma unroll
             for (int k = 0; k < C::kMmasPerStage; ++k) {
+              // (of an expert's last k-block only its own rows: what is behind them belongs to another)
+              if (GROUP == kKByExpert && kb * C::kKPerStage + k * (C::kKPerStage / C::kMmasPerStage) >= g.k) break;
               const uint32_t accumulate = (kb > 0 || k > 0) ? 1u : 0u;
               if (SPARSE) {
                 // 32 bytes of compressed A and 64 bytes of B per instruction
@@ -1111,8 +1254,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     if constexpr (!kStaged) {
       // loads and stores by the epilogue warps themselves
       if (SPLIT) ptx::cluster_wait();  // (the set-up's: the other CTAs' barriers are there)
-      epilogue_direct<KIND, CS, COLS, HAS_C, BLOCK_N, CTAS, MBLK, C::kAccStages, WARPS, SPLIT, LINEAR>(p, sh, epi, tmem_base, (int)cta_rank, cluster_id,
-                                                                          num_clusters, num_tiles, warp, lane, ptx::smem_u32(b_ring), split_rank);
+      epilogue_direct<KIND, CS, COLS, HAS_C, BLOCK_N, CTAS, MBLK, C::kAccStages, WARPS, SPLIT, LINEAR, GROUP>(p, sh, epi, tmem_base, (int)cta_rank, cluster_id,
+                                                                          num_clusters, num_tiles, warp, lane, ptx::smem_u32(b_ring), split_rank, experts);
       // (all that this warp sends is on its way: the cluster may leave when every warp has come so far)
       if (SPLIT) {
         __syncwarp();
