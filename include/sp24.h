@@ -537,16 +537,19 @@ sp24_status sp24_expert_linear(const sp24_expert_desc* d, const sp24_expert_epil
  *   sp24_expert_linear_dw: dzt: dz transposed, M x rows (leading dimension lddzt), X: rows x K (ldx), dW: E M x K (lda).  An expert without rows gets zeros.
  *      Every offset is a multiple of 16 (sp24_expert_order with align = 16): the weights' gradients of an expert that is not so placed are NaN.
  *   d->cd_type is ab_type; d->ld_residual, d->ld_pre and d->a_is_dense are not used.  Sizes, alignment and workspace as above.
- * sp24_expert_bias_grad: dbias[e, i] = sum over the expert's rows of dy[r, i] act'(z[r, i]) in FP32, in an order that the offsets fix (z may be NULL for
- *   SP24_ACT_NONE).  t: SP24_F16, SP24_BF16 or SP24_F32; any leading dimensions and alignment.  workspace: sp24_expert_bias_grad_workspace_bytes(...) bytes,
- *   16-byte aligned, contents of no matter. */
+ * sp24_expert_act_backward: what they and the bias's gradient are made of, dz[r, i] = dy[r, i] act'(z[r, i]) rounded to t, for all rows (dz: rows x M or NULL; dzt: M x
+ *   rows or NULL, fastest with lddzt the rows up to a multiple of 8 or more, of which the elements behind the last row may be written), and dbias[e, i] (E x M
+ *   floats or NULL) = the sum of the expert's dz before their rounding, in an order that the offsets fix.  z may be NULL for SP24_ACT_NONE.  t: SP24_F16, SP24_BF16 or
+ *   SP24_F32; any leading dimensions and alignment.  workspace (for dbias): sp24_expert_act_backward_workspace_bytes(...) bytes, 16-byte aligned, contents of no
+ *   matter. */
+size_t sp24_expert_act_backward_workspace_bytes(int64_t E, int64_t M, int64_t rows);
+sp24_status sp24_expert_act_backward(sp24_dtype t, sp24_act act, int64_t E, int64_t M, int64_t rows, const void* dy, int64_t lddy, const void* z, int64_t ldz,
+                                     const int32_t* offsets, void* dz, int64_t lddz, void* dzt, int64_t lddzt, float* dbias, void* workspace,
+                                     size_t workspace_bytes, void* stream);
 sp24_status sp24_expert_linear_dx(const sp24_expert_desc* d, const void* dz, const void* W, const int32_t* offsets, void* dX, void* workspace,
                                   size_t workspace_bytes, void* stream);
 sp24_status sp24_expert_linear_dw(const sp24_expert_desc* d, const void* dzt, int64_t lddzt, const void* X, const int32_t* offsets, void* dW, void* workspace,
                                   size_t workspace_bytes, void* stream);
-size_t sp24_expert_bias_grad_workspace_bytes(int64_t E, int64_t M, int64_t rows);
-sp24_status sp24_expert_bias_grad(sp24_dtype t, sp24_act act, int64_t E, int64_t M, int64_t rows, const void* dy, int64_t lddy, const void* z, int64_t ldz,
-                                  const int32_t* offsets, float* dbias, void* workspace, size_t workspace_bytes, void* stream);
 
 /* End-to-end convenience for callers whose data lives in HOST memory (pinned for speed):
  * copies dense A (M x K, row-major, packed), B (N rows of K, packed) and, if beta != 0, C

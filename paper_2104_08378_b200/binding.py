@@ -40,7 +40,7 @@ EXPORTS = [
     "sp24_gated_act", "sp24_gated_act_backward", "sp24_act_backward_workspace_bytes", "sp24_act_backward",
     "sp24_linear", "sp24_route", "sp24_route_backward", "sp24_expert_rows", "sp24_expert_order", "sp24_expert_gather",
     "sp24_expert_combine", "sp24_expert_combine_backward", "sp24_expert_linear", "sp24_expert_linear_dx", "sp24_expert_linear_dw",
-    "sp24_expert_bias_grad_workspace_bytes", "sp24_expert_bias_grad",
+    "sp24_expert_act_backward_workspace_bytes", "sp24_expert_act_backward",
 ]
 
 
@@ -140,11 +140,11 @@ def _load() -> ctypes.CDLL:
     lib.sp24_expert_linear.argtypes = [ctypes.POINTER(ExpertDesc), ctypes.POINTER(ExpertEpilogue), vp, vp, vp, vp, vp, vp, sz, vp]
     lib.sp24_expert_linear_dx.argtypes = [ctypes.POINTER(ExpertDesc), vp, vp, vp, vp, vp, sz, vp]
     lib.sp24_expert_linear_dw.argtypes = [ctypes.POINTER(ExpertDesc), vp, i64, vp, vp, vp, vp, sz, vp]
-    lib.sp24_expert_bias_grad_workspace_bytes.argtypes = [i64, i64, i64]
-    lib.sp24_expert_bias_grad_workspace_bytes.restype = sz
-    lib.sp24_expert_bias_grad.argtypes = [ci, ci, i64, i64, i64, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+    lib.sp24_expert_act_backward_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.sp24_expert_act_backward_workspace_bytes.restype = sz
+    lib.sp24_expert_act_backward.argtypes = [ci, ci, i64, i64, i64, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, sz, vp]
     for name in ("sp24_route", "sp24_route_backward", "sp24_expert_order", "sp24_expert_gather", "sp24_expert_combine", "sp24_expert_combine_backward",
-                 "sp24_expert_linear", "sp24_expert_linear_dx", "sp24_expert_linear_dw", "sp24_expert_bias_grad"):
+                 "sp24_expert_linear", "sp24_expert_linear_dx", "sp24_expert_linear_dw", "sp24_expert_act_backward"):
         getattr(lib, name).restype = ci
     for name in ("sp24_linear", "sp24_rms_norm", "sp24_rms_norm_backward", "sp24_gated_act", "sp24_gated_act_backward", "sp24_act_backward"):
         getattr(lib, name).restype = ci
@@ -1071,9 +1071,14 @@ def expert_linear_backward(dy: torch.Tensor, pre: torch.Tensor | None, X: torch.
         dz, lddz = dy.new_empty((rows, M)), M
     lddzt = (rows + 7) // 8 * 8
     dzt = dy.new_empty((M, lddzt))
-    if rows:
-        _check(lib.sp24_act_backward(t, a, rows, M, _ptr(dy), lddy, _ptr(pre) if a else None, ldz, None if dz is dy else _ptr(dz), lddz, _ptr(dzt), lddzt,
-                                     None, 1, None, 0, stream), where)
+    dbias = scratch = None
+    size = 0
+    if bias:
+        dbias = dy.new_empty((E, M), dtype=torch.float32)
+        size = lib.sp24_expert_act_backward_workspace_bytes(E, M, rows)
+        scratch = dy.new_empty(size, dtype=torch.uint8)
+    _check(lib.sp24_expert_act_backward(t, a, E, M, rows, _ptr(dy), lddy, _ptr(pre) if a else None, ldz, _ptr(offsets), None if dz is dy else _ptr(dz), lddz,
+                                        _ptr(dzt), lddzt, _ptr(dbias), _ptr(scratch), size, stream), where)
     dX, dW = dy.new_empty((rows, K)), dy.new_empty((E, M, K))
     desc = ExpertDesc(t, t, E, M, K, rows, ldw, K, lddz, 0, 0, 1)
     _check(lib.sp24_expert_linear_dx(byref(desc), _ptr(dz), _ptr(W), _ptr(offsets), _ptr(dX), _ptr(ws), ws.numel(), stream), where)
@@ -1082,11 +1087,4 @@ def expert_linear_backward(dy: torch.Tensor, pre: torch.Tensor | None, X: torch.
     if meta is not None:
         for first, n in ([(0, E * M)] if M % 128 == 0 else [(e, M) for e in range(E)]):
             _check(lib.sp24_apply_mask(t, n, K, _ptr(dW[first]), K, _ptr(meta[first]), META_TCGEN05, _ptr(dW[first]), K, stream), where)
-    dbias = None
-    if bias:
-        dbias = dy.new_empty((E, M), dtype=torch.float32)
-        size = lib.sp24_expert_bias_grad_workspace_bytes(E, M, rows)
-        scratch = dy.new_empty(size, dtype=torch.uint8)
-        _check(lib.sp24_expert_bias_grad(t, a, E, M, rows, _ptr(dy), lddy, _ptr(pre) if a else None, ldz, _ptr(offsets), _ptr(dbias), _ptr(scratch), size, stream),
-               where)
     return dX, dW, dbias

@@ -16,7 +16,25 @@ struct ActGradParams {
   float* partial;  // sums over the rows of a tile (over_rows: [row tiles][cols]) or over its columns ([column tiles][rows]); or null
   int64_t lddy, ldz, lddz, lddzt;
   int32_t over_rows;
+  const int32_t* offsets;  // EXPERTS: see sp24_expert_act_backward
+  int32_t experts;
 };
+
+// Rows [lo, hi) of expert e, as the products take them.
+__device__ __forceinline__ void rows_of_expert(const ActGradParams& p, int e, int64_t& lo, int64_t& hi) {
+  lo = min(max((int64_t)p.offsets[e], (int64_t)0), p.rows);
+  hi = max(lo, min((int64_t)p.offsets[e + 1], p.rows));
+}
+// The first expert whose rows end behind row r, E if there is none (offsets in order).
+__device__ __forceinline__ int expert_of_row(const ActGradParams& p, int64_t r) {
+  int lo = 0, hi = p.experts;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (p.offsets[mid + 1] > r) hi = mid;
+    else lo = mid + 1;
+  }
+  return lo;
+}
 
 // 16-bit types, all rows (of dzt too) whole vectors at 16-byte boundaries.  A block to a tile of 128 x 128 (rows of 256 bytes both ways; of 64 x 64 where those
 // would leave SMs idle: 128 x 4096 5.4 -> 3.6 us), transposed on its way out of
@@ -25,7 +43,9 @@ struct ActGradParams {
 // u ^ (2 (m >> 3 & 3) + (m & 1)): the eight rows of a matrix are in different banks.
 // dz = dy act'(z) is needed in both orders, and reading dy and z once for both is what the tile is for.  Bound by HBM and, with GELU, the arithmetic of the slope:
 // bf16 4096 x 8192 with the bias 52 us = 5.1 TB/s (ReLU 46; by elements 125, tiles of 64 x 64 62); three blocks to an SM instead of two spill (75).
-template <typename T, int ACT, int kWide>
+// EXPERTS: the bias's gradient of each expert's rows.  Tile i of the rows has a partial sum of its own for every expert that it meets, in row i + (expert) of
+// `partial`, which no other tile and expert share.
+template <typename T, int ACT, int kWide, bool EXPERTS = false>
 __global__ void __launch_bounds__(4 * kWide) act_grad_tile_kernel(const ActGradParams p) {
   constexpr int kUnits = kWide / 8, kWideThreads = 4 * kWide;
   constexpr int kPasses = kWide * kUnits / kWideThreads, kRows = kWide / kPasses;
@@ -74,7 +94,7 @@ __global__ void __launch_bounds__(4 * kWide) act_grad_tile_kernel(const ActGradP
       if (u == 0 && r < p.rows) p.partial[col0 / kWide * p.rows + r] = s;
     }
   }
-  if (p.partial && p.over_rows) {
+  auto sum_over_warp = [&] {
 #pragma unroll
     for (int i = kUnits; i < 32; i *= 2)
 #pragma unroll
@@ -86,7 +106,15 @@ __global__ void __launch_bounds__(4 * kWide) act_grad_tile_kernel(const ActGradP
 #pragma unroll
       for (int n = 0; n < 4; ++n) *reinterpret_cast<float2*>(&over[warp][8 * u + 2 * n]) = sums[n];
     }
-  }
+  };
+  auto sum_over_warps = [&](int64_t at) {  // to row `at` of the partial sums
+    if (threadIdx.x >= kWide) return;
+    float s = over[0][threadIdx.x];
+#pragma unroll
+    for (int w = 1; w < kWideThreads / 32; ++w) s += over[w][threadIdx.x];
+    if (col0 + threadIdx.x < p.cols) p.partial[at * p.cols + col0 + threadIdx.x] = s;
+  };
+  if (p.partial && p.over_rows) sum_over_warp();
   __syncthreads();
   if (p.dzt) {
     static_assert(kWideThreads / 32 == kUnits, "a warp to a unit: eight columns");
@@ -101,11 +129,44 @@ __global__ void __launch_bounds__(4 * kWide) act_grad_tile_kernel(const ActGradP
       if (col < p.cols && r < p.rows) *reinterpret_cast<uint4*>(static_cast<T*>(p.dzt) + col * p.lddzt + r) = make_uint4(x[0], x[1], x[2], x[3]);
     }
   }
-  if (p.partial && p.over_rows && threadIdx.x < kWide) {
-    float s = over[0][threadIdx.x];
+  if (!EXPERTS) {
+    if (p.partial && p.over_rows) sum_over_warps(row0 / kWide);
+  } else if (p.partial) {
+    // The sums above are of all rows of the tile, as they are wanted where they all belong to one expert.  Elsewhere they are made again, expert by expert.
+    const int64_t end = min(p.rows, row0 + kWide);
+    int64_t lo = 0, hi = 0;
+    for (int e = expert_of_row(p, row0); e < p.experts; ++e) {
+      rows_of_expert(p, e, lo, hi);
+      if (lo >= end) break;
+      if (hi <= lo) continue;
+      if (lo <= row0 && hi >= end) {
+        sum_over_warps(row0 / kWide + e);
+        break;
+      }
 #pragma unroll
-    for (int w = 1; w < kWideThreads / 32; ++w) s += over[w][threadIdx.x];
-    if (col0 + threadIdx.x < p.cols) p.partial[row0 / kWide * p.cols + col0 + threadIdx.x] = s;
+      for (int n = 0; n < 4; ++n) sums[n] = make_float2(0.f, 0.f);
+      for (int v = 0; v < kPasses; ++v) {
+        const int64_t r = row0 + m0 + kRows * v;
+        if (r < lo || r >= hi || r >= end || c >= p.cols) continue;
+        Pairs<T> d, f;
+        unpack<T>(*reinterpret_cast<const uint4*>(static_cast<const T*>(p.dy) + r * p.lddy + c), d);
+        if (ACT != SP24_ACT_NONE) {
+          unpack<T>(*reinterpret_cast<const uint4*>(static_cast<const T*>(p.z) + r * p.ldz + c), f);
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            float2 slope;
+            act_and_slope<ACT>(f[n], &slope);
+            d[n] = mul2(d[n], slope);
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < 4; ++n) sums[n] = make_float2(sums[n].x + d[n].x, sums[n].y + d[n].y);
+      }
+      __syncthreads();  // (the sums in shared memory have been read)
+      sum_over_warp();
+      __syncthreads();
+      sum_over_warps(row0 / kWide + e);
+    }
   }
 }
 
@@ -144,6 +205,52 @@ __global__ void __launch_bounds__(256) act_grad_kernel(const ActGradParams p) {
     if (p.over_rows && at < p.cols) p.partial[row0 / kTile * p.cols + at] = sum;
     if (!p.over_rows && at < p.rows) p.partial[col0 / kTile * p.rows + at] = sum;
   }
+}
+
+// The partial sums of the experts' rows for any type, size and alignment: tiles of kTile rows as above.
+template <typename T, int ACT>
+__global__ void __launch_bounds__(256) expert_sums_kernel(const ActGradParams p) {
+  __shared__ float over[4][kTile];
+  wait_for_stream();
+  const int x = threadIdx.x % kTile, y = threadIdx.x / kTile;
+  const int64_t row0 = (int64_t)blockIdx.y * kTile, end = min(p.rows, row0 + kTile), c = (int64_t)blockIdx.x * kTile + x;
+  for (int e = expert_of_row(p, row0); e < p.experts; ++e) {
+    int64_t lo, hi;
+    rows_of_expert(p, e, lo, hi);
+    if (lo >= end) break;
+    if (hi <= lo) continue;
+    float sum = 0.f;
+    if (c < p.cols)
+      for (int64_t r = max(lo, row0) + y; r < min(hi, end); r += 4) {
+        float d = to_float(static_cast<const T*>(p.dy)[r * p.lddy + c]);
+        if (ACT != SP24_ACT_NONE) {
+          float2 slope;
+          act_and_slope<ACT>(both(to_float(static_cast<const T*>(p.z)[r * p.ldz + c])), &slope);
+          d *= slope.x;
+        }
+        sum += d;
+      }
+    over[y][x] = sum;
+    __syncthreads();
+    if (y == 0 && c < p.cols) p.partial[((int64_t)blockIdx.y + e) * p.cols + c] = (over[0][x] + over[1][x]) + (over[2][x] + over[3][x]);
+    __syncthreads();
+  }
+}
+
+// An expert's partial sums added up, tile after tile: four tiles side by side, so that a long chain of loads is a quarter as long.
+__global__ void __launch_bounds__(256) expert_bias_kernel(const ActGradParams p, int edge, float* dbias) {
+  __shared__ float over[4][kTile];
+  wait_for_stream();
+  const int x = threadIdx.x % kTile, y = threadIdx.x / kTile, e = blockIdx.y;
+  const int64_t c = (int64_t)blockIdx.x * kTile + x;
+  int64_t lo, hi;
+  rows_of_expert(p, e, lo, hi);
+  float sum = 0.f;
+  if (hi > lo && c < p.cols)
+    for (int64_t i = lo / edge + y; i <= (hi - 1) / edge; i += 4) sum += p.partial[(i + e) * p.cols + c];
+  over[y][x] = sum;
+  __syncthreads();
+  if (y == 0 && c < p.cols) dbias[(int64_t)e * p.cols + c] = (over[0][x] + over[1][x]) + (over[2][x] + over[3][x]);
 }
 
 }  // namespace
@@ -203,4 +310,56 @@ extern "C" sp24_status sp24_act_backward(sp24_dtype t, sp24_act act, int64_t row
   });
   if (st != SP24_OK || !dbias) return st;
   return column_sums(static_cast<const float*>(workspace), sum_over_rows ? row_tiles : col_tiles, sums, dbias, s);
+}
+
+extern "C" size_t sp24_expert_act_backward_workspace_bytes(int64_t E, int64_t M, int64_t rows) {
+  if (E < 1 || E > 1024 || M < 1 || M > kMostColumns || rows < 0 || rows > kMostColumns) return 0;
+  return (size_t)((rows + kTile - 1) / kTile + E) * (size_t)M * sizeof(float);
+}
+
+extern "C" sp24_status sp24_expert_act_backward(sp24_dtype t, sp24_act act, int64_t E, int64_t M, int64_t rows, const void* dy, int64_t lddy,
+                                                const void* z, int64_t ldz, const int32_t* offsets, void* dz, int64_t lddz, void* dzt, int64_t lddzt,
+                                                float* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+  SP24_RETURN_IF(!is_float_type(t), SP24_ERR_DTYPE);
+  SP24_RETURN_IF(!is_act(act), SP24_ERR_UNSUPPORTED);
+  SP24_RETURN_IF(E < 1 || E > 1024 || M < 1 || M > kMostColumns || rows < 0 || rows > kMostColumns, SP24_ERR_SHAPE);
+  const bool reads_z = act != SP24_ACT_NONE;
+  SP24_RETURN_IF((rows > 0 && (!dy || (reads_z && !z))) || (dbias && !offsets), SP24_ERR_NULL);
+  SP24_RETURN_IF(!row_fits(rows, M, lddy) || (reads_z && !row_fits(rows, M, ldz)) || (dz && !row_fits(rows, M, lddz)) || (dzt && !row_fits(M, rows, lddzt)),
+                 SP24_ERR_STRIDE);
+  const size_t es = elem_bytes(t);
+  SP24_RETURN_IF(!aligned(dy, es) || (reads_z && !aligned(z, es)) || !aligned(dz, es) || !aligned(dzt, es) || !aligned(dbias, 4) || !aligned(offsets, 4), SP24_ERR_ALIGN);
+  SP24_RETURN_IF(dbias && (!workspace || !aligned16(workspace) || workspace_bytes < sp24_expert_act_backward_workspace_bytes(E, M, rows)), SP24_ERR_WORKSPACE);
+  if (!dbias && (rows == 0 || (!dz && !dzt))) return SP24_OK;
+  // (rows of dzt are written up to a whole vector, which their leading dimension has room for)
+  const bool whole = t != SP24_F32 && M % 8 == 0 && whole_rows(dy, rows, lddy, 2, 16) && (!reads_z || whole_rows(z, rows, ldz, 2, 16)) &&
+                     whole_rows(dz, rows, lddz, 2, 16) && (!dzt || (whole_rows(dzt, M, lddzt, 2, 16) && lddzt >= (rows + 7) / 8 * 8));
+  const bool wide = whole && (rows + 127) / 128 * ((M + 127) / 128) >= 2 * sm_count();
+  const int64_t edge = wide ? 2 * kTile : kTile, row_tiles = (rows + edge - 1) / edge, col_tiles = (M + edge - 1) / edge;
+  SP24_RETURN_IF(row_tiles * col_tiles > 0x7fffffff || (dbias && !whole && row_tiles > 65535), SP24_ERR_SHAPE);
+  sp24_status st = check_arch();
+  SP24_RETURN_IF(st != SP24_OK, st);
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  ActGradParams p = {rows, M, dy, z, dz, dzt, dbias ? static_cast<float*>(workspace) : nullptr, lddy, ldz, lddz, lddzt, 1, offsets, (int)E};
+  if (rows > 0) {
+    const dim3 grid((unsigned)(row_tiles * col_tiles));
+    st = with_float_type(t, [&](auto type) {
+      using T = typename decltype(type)::type;
+      return with_act(act, [&](auto a) {
+        constexpr int kAct = decltype(a)::value;
+        if constexpr (sizeof(T) == 2)
+          if (whole)
+            return launch_overlapped(wide ? act_grad_tile_kernel<T, kAct, 2 * kTile, true> : act_grad_tile_kernel<T, kAct, kTile, true>, grid, dim3((unsigned)(4 * edge)),
+                                     0, s, 1, p);
+        ActGradParams q = p;
+        q.partial = nullptr;
+        sp24_status done = SP24_OK;
+        if (dz || dzt) done = launch_overlapped(act_grad_kernel<T, kAct>, grid, dim3(256), 0, s, 1, q);
+        if (done != SP24_OK || !dbias) return done;
+        return launch_overlapped(expert_sums_kernel<T, kAct>, dim3((unsigned)col_tiles, (unsigned)row_tiles), dim3(256), 0, s, 1, p);
+      });
+    });
+    SP24_RETURN_IF(st != SP24_OK || !dbias, st);
+  }
+  return launch_overlapped(expert_bias_kernel, dim3((unsigned)((M + kTile - 1) / kTile), (unsigned)E), dim3(256), 0, s, 1, p, (int)edge, dbias);
 }

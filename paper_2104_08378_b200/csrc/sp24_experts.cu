@@ -18,6 +18,7 @@ struct OrderParams {
   int32_t *offsets, *position, *source;
 };
 
+constexpr int kBatch = 8;
 __global__ void __launch_bounds__(1024) order_kernel(const OrderParams p) {
   extern __shared__ int32_t counts[];  // [warps][E], then [E] of the block, [E] of the experts' first rows
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
@@ -36,11 +37,14 @@ __global__ void __launch_bounds__(1024) order_kernel(const OrderParams p) {
     const int e = i < end ? p.experts[i] : -1;
     return e >= 0 && e < p.E ? e : -1;
   };
-  for (int64_t i = begin; i < end; i += 32) {
-    const int e = expert_of(i + lane);
-    const uint32_t same = __match_any_sync(~0u, e);
-    if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
-    __syncwarp();
+  // kBatch groups at a time: their loads are all on the way before the first is used
+  for (int64_t i = begin; i < end; i += 32 * kBatch) {
+    int e[kBatch];
+#pragma unroll
+    for (int n = 0; n < kBatch; ++n) e[n] = expert_of(i + 32 * n + lane);
+#pragma unroll
+    for (int n = 0; n < kBatch; ++n)
+      if (e[n] >= 0) atomicAdd(&mine[e[n]], 1);  // (a sum of ones: any order)
   }
   __syncthreads();
   // counts of the warps before, in the place of the warp's; the block's
@@ -92,17 +96,26 @@ __global__ void __launch_bounds__(1024) order_kernel(const OrderParams p) {
   int32_t all = lane < warps ? of_warps[lane] : 0;
   all = __reduce_add_sync(~0u, all);
   for (int64_t r = all + (int64_t)rank * blockDim.x + threadIdx.x; r < p.rows; r += (int64_t)blocks * blockDim.x) p.source[r] = -1;
-  for (int64_t i = begin; i < end; i += 32) {
-    const int x = expert_of(i + lane);
-    const uint32_t same = __match_any_sync(~0u, x);
-    int32_t row = -1;
-    if (x >= 0) row = first[x] + mine[x] + __popc(same & ((1u << lane) - 1));
-    __syncwarp();
-    if (x >= 0 && lane == __ffs(same) - 1) mine[x] += __popc(same);
-    __syncwarp();
-    if (i + lane < end) {
-      p.position[i + lane] = row;
-      if (row >= 0) p.source[row] = (int32_t)(i + lane);
+  for (int64_t i = begin; i < end; i += 32 * kBatch) {
+    int x[kBatch];
+    uint32_t same[kBatch];
+#pragma unroll
+    for (int n = 0; n < kBatch; ++n) x[n] = expert_of(i + 32 * n + lane);
+#pragma unroll
+    for (int n = 0; n < kBatch; ++n) same[n] = __match_any_sync(~0u, x[n]);
+#pragma unroll
+    for (int n = 0; n < kBatch; ++n) {
+      if (i + 32 * n >= end) break;
+      int32_t row = -1;
+      if (x[n] >= 0) row = first[x[n]] + mine[x[n]] + __popc(same[n] & ((1u << lane) - 1));
+      __syncwarp();
+      if (x[n] >= 0 && lane == __ffs(same[n]) - 1) mine[x[n]] += __popc(same[n]);
+      __syncwarp();
+      const int64_t at = i + 32 * n + lane;
+      if (at < end) {
+        p.position[at] = row;
+        if (row >= 0) p.source[row] = (int32_t)at;
+      }
     }
   }
   // no block leaves while another may still read its counts
@@ -214,6 +227,7 @@ struct Values {
 
 template <typename T, typename W>
 __global__ void __launch_bounds__(256) combine_kernel(const RowsParams p) {
+  constexpr int U = sizeof(W) == 16 ? 2 : 4;
   __shared__ int32_t place[kMostChosen];
   __shared__ float weight[kMostChosen];
   wait_for_stream();
@@ -225,135 +239,96 @@ __global__ void __launch_bounds__(256) combine_kernel(const RowsParams p) {
       weight[threadIdx.x] = p.weights ? p.weights[t * p.k + threadIdx.x] : 1.f;
     }
     __syncthreads();
-    for (int64_t c = threadIdx.x; c < p.K; c += blockDim.x) {
-      Values<T, W> sum, x;
+    // U columns of vectors at a time, their loads on the way together
+    for (int64_t c0 = threadIdx.x; c0 < p.K; c0 += U * blockDim.x) {
+      Values<T, W> sum[U], x[U];
 #pragma unroll
-      for (int n = 0; n < sum.N; ++n) sum.v[n] = 0.f;
-      for (int i = 0; i < p.k; ++i) {
-        if (place[i] < 0) continue;
-        x.load(reinterpret_cast<const W*>(p.y + (int64_t)place[i] * p.ld_y) + c);
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int n = 0; n < sum.N; ++n) sum.v[n] = fmaf(weight[i], x.v[n], sum.v[n]);
-      }
-      if (p.residual) {
-        x.load(reinterpret_cast<const W*>(p.residual + t * p.ld_res) + c);
+        for (int n = 0; n < sum[u].N; ++n) sum[u].v[n] = 0.f;
+      auto add = [&](const uint8_t* row, float w) {
 #pragma unroll
-        for (int n = 0; n < sum.N; ++n) sum.v[n] += x.v[n];
-      }
-      sum.store(reinterpret_cast<W*>(p.out + t * p.ld_out) + c);
+        for (int u = 0; u < U; ++u)
+          if (c0 + u * blockDim.x < p.K) x[u].load(reinterpret_cast<const W*>(row) + c0 + u * blockDim.x);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int n = 0; n < sum[u].N; ++n) sum[u].v[n] = fmaf(w, x[u].v[n], sum[u].v[n]);
+      };
+#pragma unroll 4
+      for (int i = 0; i < p.k; ++i)
+        if (place[i] >= 0) add(p.y + (int64_t)place[i] * p.ld_y, weight[i]);
+      if (p.residual) add(p.residual + t * p.ld_res, 1.f);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (c0 + u * blockDim.x < p.K) sum[u].store(reinterpret_cast<W*>(p.out + t * p.ld_out) + c0 + u * blockDim.x);
     }
   }
 }
 
-// in: dout, y, out: dy, sums: dweights
-template <typename T, typename W>
+// in: dout, y, out: dy, sums: dweights.  The token's gradient stays in registers (V vectors of each thread; longer rows in several passes) while its k rows go by; the
+// k sums meet in shared memory once.
+template <typename T, typename W, int V>
 __global__ void __launch_bounds__(256) combine_backward_kernel(const RowsParams p) {
-  __shared__ float parts[2][8];
+  __shared__ float parts[2][kMostChosen][8];
   wait_for_stream();
   if (blockIdx.x >= p.token_blocks) {
     clear_rows<W>(p, p.ld_out, p.out, nullptr);
     return;
   }
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int64_t step = (int64_t)V * blockDim.x;
   int turn = 0;
-  for (int64_t t = blockIdx.x; t < p.T; t += p.token_blocks) {
+  for (int64_t t = blockIdx.x; t < p.T; t += p.token_blocks, turn ^= 1) {  // (a buffer is written again behind the other one's barrier)
     const W* d_row = reinterpret_cast<const W*>(p.in + t * p.ld_in);
-    for (int i = 0; i < p.k; ++i) {
-      int32_t r = p.position[t * p.k + i];
-      if (r >= p.rows) r = -1;
-      float dot = 0.f;
-      if (r >= 0) {
-        const float w = p.weights[t * p.k + i];
-        const W* y_row = reinterpret_cast<const W*>(p.y + (int64_t)r * p.ld_y);
-        W* out = reinterpret_cast<W*>(p.out + (int64_t)r * p.ld_out);
-        for (int64_t c = threadIdx.x; c < p.K; c += blockDim.x) {
-          Values<T, W> d, y;
-          d.load(d_row + c);
-          y.load(y_row + c);
+    const int32_t place = lane < p.k ? p.position[t * p.k + lane] : -1;
+    const float weight = lane < p.k ? p.weights[t * p.k + lane] : 0.f;
+    for (int64_t c0 = 0; c0 < p.K; c0 += step) {
+      Values<T, W> d[V];
 #pragma unroll
-          for (int n = 0; n < d.N; ++n) {
-            dot = fmaf(d.v[n], y.v[n], dot);
-            d.v[n] *= w;
+      for (int v = 0; v < V; ++v) {
+        const int64_t c = c0 + v * blockDim.x + threadIdx.x;
+        if (c < p.K) d[v].load(d_row + c);
+      }
+#pragma unroll 2
+      for (int i = 0; i < p.k; ++i) {
+        const int32_t r = __shfl_sync(~0u, place, i);
+        const float w = __shfl_sync(~0u, weight, i);
+        float dot = 0.f;
+        if (r >= 0 && r < p.rows) {
+          const W* y_row = reinterpret_cast<const W*>(p.y + (int64_t)r * p.ld_y);
+          W* out = reinterpret_cast<W*>(p.out + (int64_t)r * p.ld_out);
+          Values<T, W> y[V];
+#pragma unroll
+          for (int v = 0; v < V; ++v) {
+            const int64_t c = c0 + v * blockDim.x + threadIdx.x;
+            if (c < p.K) y[v].load(y_row + c);
           }
-          d.store(out + c);
-        }
-      }
 #pragma unroll
-      for (int s = 16; s > 0; s >>= 1) dot += __shfl_xor_sync(~0u, dot, s);
-      if (lane == 0) parts[turn][warp] = dot;
-      __syncthreads();
-      if (threadIdx.x == 0) {
-        float sum = parts[turn][0];
-        for (int w = 1; w < warps; ++w) sum += parts[turn][w];
-        p.sums[t * p.k + i] = sum;
+          for (int v = 0; v < V; ++v) {
+            const int64_t c = c0 + v * blockDim.x + threadIdx.x;
+            if (c < p.K) {
+#pragma unroll
+              for (int n = 0; n < y[v].N; ++n) {
+                dot = fmaf(d[v].v[n], y[v].v[n], dot);
+                y[v].v[n] = w * d[v].v[n];
+              }
+              y[v].store(out + c);
+            }
+          }
+        }
+#pragma unroll
+        for (int s = 16; s > 0; s >>= 1) dot += __shfl_xor_sync(~0u, dot, s);
+        if (lane == 0) parts[turn][i][warp] = c0 ? parts[turn][i][warp] + dot : dot;
       }
-      turn ^= 1;  // (a buffer is written again behind the other one's barrier)
+    }
+    __syncthreads();
+    if (threadIdx.x < p.k) {
+      float sum = parts[turn][threadIdx.x][0];
+      for (int w = 1; w < warps; ++w) sum += parts[turn][threadIdx.x][w];
+      p.sums[t * p.k + threadIdx.x] = sum;
     }
   }
-}
-
-// ---- the bias's gradient ------------------------------------------------------------------------------------------
-// Sums over an expert's rows in parts of kBiasRows, then over the parts; an expert's parts begin where those of the experts before end at the latest.
-constexpr int kBiasRows = 256, kBiasColumns = 64;
-struct BiasParams {
-  int64_t rows, M, lddy, ldz;
-  int E;
-  const void *dy, *z;
-  const int32_t* offsets;
-  float *partial, *dbias;
-};
-// rows [lo, hi) of expert e, as the products take them
-__device__ __forceinline__ void rows_of_expert(const int32_t* offsets, int64_t rows, int e, int64_t& lo, int64_t& hi) {
-  lo = min(max((int64_t)offsets[e], (int64_t)0), rows);
-  hi = max(lo, min((int64_t)offsets[e + 1], rows));
-}
-
-// Block (column tile, part): the part's expert and rows by a search over the offsets.  Parts of expert e are number offsets[e] / kBiasRows + e and on.
-template <typename T, int ACT>
-__global__ void __launch_bounds__(256) bias_parts_kernel(const BiasParams p) {
-  __shared__ float over[4][kBiasColumns];
-  wait_for_stream();
-  int e = 0, high = p.E - 1;  // the last expert whose first part is not behind this one
-  while (e < high) {
-    const int mid = (e + high + 1) / 2;
-    int64_t lo, hi;
-    rows_of_expert(p.offsets, p.rows, mid, lo, hi);
-    if (lo / kBiasRows + mid <= blockIdx.y) e = mid;
-    else high = mid - 1;
-  }
-  int64_t lo, hi;
-  rows_of_expert(p.offsets, p.rows, e, lo, hi);
-  const int64_t begin = lo + ((int64_t)blockIdx.y - (lo / kBiasRows + e)) * kBiasRows, end = min(hi, begin + kBiasRows);
-  const int x = threadIdx.x % kBiasColumns, y = threadIdx.x / kBiasColumns;
-  const int64_t c = (int64_t)blockIdx.x * kBiasColumns + x;
-  float sum = 0.f;
-  if (c < p.M && begin >= lo) {
-    for (int64_t r = begin + y; r < end; r += 4) {
-      float d = to_float(static_cast<const T*>(p.dy)[r * p.lddy + c]);
-      if (ACT != SP24_ACT_NONE) {
-        float2 slope;
-        act_and_slope<ACT>(both(to_float(static_cast<const T*>(p.z)[r * p.ldz + c])), &slope);
-        d *= slope.x;
-      }
-      sum += d;
-    }
-  }
-  over[y][x] = sum;
-  __syncthreads();
-  if (y == 0 && c < p.M) p.partial[(int64_t)blockIdx.y * p.M + c] = (over[0][x] + over[1][x]) + (over[2][x] + over[3][x]);
-}
-
-__global__ void __launch_bounds__(256) bias_sums_kernel(const BiasParams p) {
-  wait_for_stream();
-  const int64_t c = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  const int e = blockIdx.y;
-  if (c >= p.M) return;
-  int64_t lo, hi;
-  rows_of_expert(p.offsets, p.rows, e, lo, hi);
-  const int64_t first = lo / kBiasRows + e, parts = (hi - lo + kBiasRows - 1) / kBiasRows;
-  float sum = 0.f;
-  for (int64_t i = 0; i < parts; ++i) sum += p.partial[(first + i) * p.M + c];
-  p.dbias[(int64_t)e * p.M + c] = sum;
 }
 
 bool code_or_float(sp24_dtype t) { return is_float_type(t) || is_code_type(t) || t == SP24_I32; }
@@ -507,45 +482,14 @@ extern "C" sp24_status sp24_expert_combine_backward(sp24_dtype t, int64_t T, int
       p.K = K * es / (int64_t)sizeof(W);
       const unsigned threads = row_threads(p.K);
       p.token_blocks = (int)token_blocks(T);
-      return launch_overlapped(combine_backward_kernel<Type, W>, dim3(p.token_blocks + clearing_blocks(rows, threads)), dim3(threads), 0,
-                               static_cast<cudaStream_t>(stream), 1, p);
+      const dim3 grid(p.token_blocks + clearing_blocks(rows, threads));
+      const cudaStream_t s = static_cast<cudaStream_t>(stream);
+      if (p.K <= threads) return launch_overlapped(combine_backward_kernel<Type, W, 1>, grid, dim3(threads), 0, s, 1, p);
+      if (p.K <= 2 * threads || sizeof(W) == 16) return launch_overlapped(combine_backward_kernel<Type, W, 2>, grid, dim3(threads), 0, s, 1, p);
+      return launch_overlapped(combine_backward_kernel<Type, W, 8>, grid, dim3(threads), 0, s, 1, p);
     };
     if (whole) return run(uint4{});
     if constexpr (sizeof(Type) == 4) return run(uint32_t{});
     else return run(uint16_t{});
   });
-}
-
-extern "C" size_t sp24_expert_bias_grad_workspace_bytes(int64_t E, int64_t M, int64_t rows) {
-  if (E < 1 || M < 1 || rows < 0) return 0;
-  return (size_t)((rows / kBiasRows + E + 1) * M) * 4;
-}
-
-extern "C" sp24_status sp24_expert_bias_grad(sp24_dtype t, sp24_act act, int64_t E, int64_t M, int64_t rows, const void* dy, int64_t lddy,
-                                             const void* z, int64_t ldz, const int32_t* offsets, float* dbias, void* workspace,
-                                             size_t workspace_bytes, void* stream) {
-  SP24_RETURN_IF(!is_float_type(t), SP24_ERR_DTYPE);
-  SP24_RETURN_IF(!is_act(act), SP24_ERR_UNSUPPORTED);
-  SP24_RETURN_IF(E < 1 || E > kMostExperts || M < 1 || M > kMostColumns || rows < 0 || rows > int64_t(1) << 23, SP24_ERR_SHAPE);
-  SP24_RETURN_IF(offsets == nullptr || dbias == nullptr || (rows > 0 && (dy == nullptr || (act != SP24_ACT_NONE && z == nullptr))), SP24_ERR_NULL);
-  SP24_RETURN_IF(!row_fits(rows, M, lddy) || (act != SP24_ACT_NONE && !row_fits(rows, M, ldz)), SP24_ERR_STRIDE);
-  SP24_RETURN_IF(!aligned(dy, elem_bytes(t)) || !aligned(z, elem_bytes(t)) || !aligned(offsets, 4) || !aligned(dbias, 4), SP24_ERR_ALIGN);
-  SP24_RETURN_IF(workspace == nullptr || !aligned16(workspace) || workspace_bytes < sp24_expert_bias_grad_workspace_bytes(E, M, rows), SP24_ERR_WORKSPACE);
-  const sp24_status arch = check_arch();
-  SP24_RETURN_IF(arch != SP24_OK, arch);
-  BiasParams p = {rows, M, lddy, ldz, (int)E, dy, z, offsets, static_cast<float*>(workspace), dbias};
-  const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const dim3 parts((unsigned)((M + kBiasColumns - 1) / kBiasColumns), (unsigned)(rows / kBiasRows + E + 1));
-  const sp24_status st = with_float_type(t, [&](auto type) {
-    using Type = typename decltype(type)::type;
-    switch (act) {
-      case SP24_ACT_RELU: return launch_overlapped(bias_parts_kernel<Type, SP24_ACT_RELU>, parts, dim3(256), 0, s, 1, p);
-      case SP24_ACT_GELU: return launch_overlapped(bias_parts_kernel<Type, SP24_ACT_GELU>, parts, dim3(256), 0, s, 1, p);
-      case SP24_ACT_SILU: return launch_overlapped(bias_parts_kernel<Type, SP24_ACT_SILU>, parts, dim3(256), 0, s, 1, p);
-      case SP24_ACT_GELU_TANH: return launch_overlapped(bias_parts_kernel<Type, SP24_ACT_GELU_TANH>, parts, dim3(256), 0, s, 1, p);
-      default: return launch_overlapped(bias_parts_kernel<Type, SP24_ACT_NONE>, parts, dim3(256), 0, s, 1, p);
-    }
-  });
-  SP24_RETURN_IF(st != SP24_OK, st);
-  return launch_overlapped(bias_sums_kernel, dim3((unsigned)((M + 255) / 256), (unsigned)E), dim3(256), 0, s, 1, p);
 }

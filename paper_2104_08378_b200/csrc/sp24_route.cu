@@ -13,7 +13,7 @@ struct RouteParams {
   int64_t T, ld;
   int E, k, groups, group_experts, top_groups;
   int sigmoid, top2, renorm;
-  float scale, score_error;
+  float scale;
   const void* logits;
   const float* bias;
   float* weights;
@@ -32,9 +32,7 @@ template <typename T>
 __device__ __forceinline__ float logit(const void* row, int64_t e) { return to_float(static_cast<const T*>(row)[e]); }
 
 // One warp has a token; lane i has experts i, i + 32, ... (V of them, fewer than 32 V experts).
-// The choice is k rounds of the largest key, the lowest index first.  FP64 where FP32 does not tell: a score is off by at most 2^-22 of
-// it (sigmoid: the exponential's two units in the last place, a sum, a division) or 2^-18 (softmax: the difference to the largest
-// logit, up to 88 where the score is not 0, is rounded before the exponential), s + b by half a step more.
+// The choice is k rounds of the largest key, the lowest index first.  Where FP32 does not tell two values apart, FP64 does.
 template <int V>
 struct Choice {
   uint32_t key[V];
@@ -140,12 +138,68 @@ __device__ __noinline__ void choose64(const RouteParams& p, const void* row, flo
   __syncwarp();
 }
 
+// Lane i's candidate among the m best by FP32 (m <= 32; none of the others can be among them): its place by s + b in FP64, the lower index first.
 template <typename T, int V>
+__device__ __noinline__ int order64(const RouteParams& p, const void* row, float top_logit, int lane, int m, int expert) {
+  double sum = 1.0, c = -INFINITY;
+  if (!p.sigmoid) {
+    sum = 0.0;
+    for (int v = 0; v < V; ++v) {
+      const int e = v * 32 + lane;
+      const float l = e < p.E ? logit<T>(row, e) : -INFINITY;
+      if (l > -INFINITY) sum += exp((double)l - (double)top_logit);
+    }
+    sum = warp_sum(sum);
+  }
+  if (lane < m) {
+    const double l = (double)logit<T>(row, expert);
+    c = (p.sigmoid ? 1.0 / (1.0 + exp(-l)) : exp(l - (double)top_logit) / sum) + (double)p.bias[expert];
+  }
+  int place = 0;
+  for (int i = 0; i < m; ++i) {
+    const double other = __shfl_sync(~0u, c, i);
+    const int e = __shfl_sync(~0u, expert, i);
+    place += other > c || (other == c && e < expert);
+  }
+  // the i-th place's expert to lane i
+  int mine = -1;
+  for (int i = 0; i < m; ++i) {
+    const uint32_t at = __ballot_sync(~0u, lane < m && place == i);
+    const int e = __shfl_sync(~0u, expert, __ffs(at) - 1);
+    if (lane == i) mine = e;
+  }
+  return mine;
+}
+
+// What bounds it: instructions, about 500 a token of 256 experts with groups and a bias (the scores a tenth of it, eight rounds of choosing half), so nothing is done
+// per expert that can be done once: the bias and the groups of a lane's experts stay in registers over its tokens, scores for the choice come from the
+// special-function units (the weights are computed again, exactly, for the chosen), the best of a group is found in shared memory by 32 / groups lanes
+// each.  BIAS, GROUPS: kernels without either carry none of it.
+template <typename T, int V, bool BIAS, bool GROUPS>
 __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RouteParams p) {
   __shared__ int32_t chosen_of[kRouteWarps][kMostChosen];
+  extern __shared__ float values_of[];  // GROUPS: E for each warp
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int32_t* chosen = chosen_of[warp];
+  float* values = values_of + warp * p.E;
   wait_for_stream();
+  const bool two = GROUPS && p.top2, scores = BIAS || two, total = !p.sigmoid && !p.renorm;
+  float bias[V], bias_size = 0.f;
+  uint32_t group_bit[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int e = v * 32 + lane;
+    if (BIAS) {
+      bias[v] = e < p.E ? p.bias[e] : -INFINITY;
+      bias_size = fmaxf(bias_size, fabsf(bias[v]) < INFINITY ? fabsf(bias[v]) : 0.f);
+    }
+    if (GROUPS) group_bit[v] = 1u << ((e < p.E ? e / p.group_experts : 0) & 31);
+  }
+  if (BIAS) asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(bias_size));
+  // lanes to a group: a power of two
+  int parts = 1;
+  if (GROUPS)
+    while (2 * parts * p.groups <= 32) parts *= 2;
   for (int64_t t = (int64_t)blockIdx.x * kRouteWarps + warp; t < p.T; t += (int64_t)gridDim.x * kRouteWarps) {
     const void* row = static_cast<const T*>(p.logits) + t * p.ld;
     float l[V];
@@ -155,105 +209,134 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RoutePara
     for (int v = 0; v < V; ++v) {
       const int e = v * 32 + lane;
       l[v] = e < p.E ? logit<T>(row, e) : -INFINITY;
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
       nan |= l[v] != l[v];
       top = fmaxf(top, l[v]);
     }
     asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(top));
     nan = __any_sync(~0u, nan) || (!p.sigmoid && top == INFINITY);
-    const bool scores = p.bias || (p.groups > 1 && p.top2), total = !p.sigmoid && !p.renorm;
-    float sum = 1.f;
     Choice<V> choice;
-    float by_group[V];  // SP24_GROUP_TOP2: s + bias
-    float scored[V];
-    if (scores || total) {
-      float part = 0.f;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        scored[v] = p.sigmoid ? 1.f / (1.f + expf(-l[v])) : (l[v] > -INFINITY ? expf(l[v] - top) : 0.f);
-        part += scored[v];
-      }
-      if (!p.sigmoid) sum = warp_sum(part);
-    }
-    const float inv = 1.f / sum;
+    float inv = 1.f, error = 0.f;  // of two scores' difference
     bool sure = true;
+    if (total) {
+      float sum = 0.f;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int e = v * 32 + lane;
-      float c = l[v];
-      if (scores) {
-        const float s = scored[v] * inv + (p.bias && e < p.E ? p.bias[e] : 0.f);
-        by_group[v] = l[v] > -INFINITY && s > -INFINITY ? s : -INFINITY;
-        if (p.bias) c = by_group[v];
-      }
-      choice.key[v] = c > -INFINITY ? order_key(c) : 0u;
+      for (int v = 0; v < V; ++v) sum += l[v] > -INFINITY ? expf(l[v] - top) : 0.f;
+      inv = 1.f / warp_sum(sum);
     }
-    if (p.groups > 1) {
-      float mine = -INFINITY, error = 0.f;  // of group `lane`: its value, and how far it may be off
-      for (int g = 0; g < p.groups; ++g) {
-        const int first = g * p.group_experts, last = first + p.group_experts;
-        uint32_t one = 0, two = 0;
+    if (scores) {
+      // For the choice: off by less than 1.5 2^-22 (sigmoid: half a step of the sum, a step of the reciprocal, a quarter of the exponential's two) or
+      // 2^-20 of the largest (softmax: the exponential's argument, up to d below the largest's, rounded twice, (d + 8) exp(-d) 2^-23 at most, and the sum).
+      float c[V];
+      if (p.sigmoid) {
+        error = 2.f * 1.5f * 0x1p-22f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) c[v] = reciprocal_fast(1.f + exp2_fast(-kLog2e * l[v]));
+      } else {
+        float sum = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          const int e = v * 32 + lane;
-          const uint32_t x = e >= first && e < last ? (p.top2 ? (by_group[v] > -INFINITY ? order_key(by_group[v]) : 0u) : choice.key[v]) : 0u;
-          two = max(two, min(one, x));
-          one = max(one, x);
+          c[v] = l[v] > -INFINITY ? exp2_fast(kLog2e * (l[v] - top)) : 0.f;
+          sum += c[v];
         }
-        const uint32_t best = __reduce_max_sync(~0u, one);
-        float value = best > kDeadKey ? key_value(best) : -INFINITY;
-        if (p.top2 && best > kDeadKey) {
-          const uint32_t holders = __ballot_sync(~0u, one == best);
-          if (lane == __ffs(holders) - 1) one = two;
-          const uint32_t second = __reduce_max_sync(~0u, one);
-          if (second > kDeadKey) value += key_value(second);
-        }
-        if (lane == g) mine = value;
+        const float part = 1.f / warp_sum(sum);
+        error = 2.f * 0x1p-20f * part;  // (the largest score)
+#pragma unroll
+        for (int v = 0; v < V; ++v) c[v] *= part;
       }
-      if (scores) error = 2.f * p.score_error + 0x1p-21f * fabsf(mine);  // (of two scores, each at most 1)
-      bool open = lane < p.groups, kept = false;
-      float worst = INFINITY, slack = 0.f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        if (BIAS) c[v] += bias[v];
+        if (!(l[v] > -INFINITY) || !(c[v] > -INFINITY)) c[v] = -INFINITY;
+        if (two && v * 32 + lane < p.E) values[v * 32 + lane] = c[v];
+        if (!BIAS) c[v] = l[v];
+        choice.key[v] = c[v] > -INFINITY ? order_key(c[v]) : 0u;
+        if (GROUPS && !two && v * 32 + lane < p.E) values[v * 32 + lane] = c[v];
+      }
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        choice.key[v] = l[v] > -INFINITY ? order_key(l[v]) : 0u;
+        if (GROUPS && v * 32 + lane < p.E) values[v * 32 + lane] = l[v] > -INFINITY ? l[v] : -INFINITY;
+      }
+    }
+    if constexpr (GROUPS) {
+      __syncwarp();
+      const int g = lane / parts;
+      float one = -INFINITY, second = -INFINITY;
+      if (g < p.groups)
+        for (int i = lane & (parts - 1); i < p.group_experts; i += parts) {
+          const float x = values[g * p.group_experts + i];
+          second = fmaxf(second, fminf(one, x));
+          one = fmaxf(one, x);
+        }
+      for (int i = parts >> 1; i > 0; i >>= 1) {
+        const float a = __shfl_xor_sync(~0u, one, i), b = __shfl_xor_sync(~0u, second, i);
+        second = fmaxf(fminf(one, a), fmaxf(second, b));
+        one = fmaxf(one, a);
+      }
+      __syncwarp();
+      const float value = two && second > -INFINITY ? one + second : one;
+      // rounds of the best group, the first of equal ones; the lanes of a group go together
+      bool open = g < p.groups && value > -INFINITY;
+      const uint32_t key = open ? order_key(value) : 0u;
+      uint32_t kept = 0, worst = 0;
       for (int i = 0; i < p.top_groups; ++i) {
-        const uint32_t m = __reduce_max_sync(~0u, open && mine > -INFINITY ? order_key(mine) : 0u);
+        const uint32_t m = __reduce_max_sync(~0u, open ? key : 0u);
         if (m <= kDeadKey) break;
-        const int at = __ffs(__ballot_sync(~0u, open && mine > -INFINITY && order_key(mine) == m)) - 1;
-        if (lane == at) { open = false; kept = true; }
-        worst = key_value(m);
-        slack = __shfl_sync(~0u, error, at);
+        const int at = (__ffs(__ballot_sync(~0u, open && key == m)) - 1) / parts;
+        if (g == at) open = false;
+        kept |= 1u << at;
+        worst = m;
       }
-      if (scores && __any_sync(~0u, open && mine > -INFINITY && mine + error + slack >= worst)) sure = false;
-      const uint32_t groups = __ballot_sync(~0u, kept);
+      if (scores) {
+        const uint32_t next = __reduce_max_sync(~0u, open ? key : 0u);
+        if (next > kDeadKey) {  // (sums of two: twice the error, and roundings of values)
+          const float a = key_value(worst), b = key_value(next);
+          if (a - b <= 2.f * error + 0x1p-21f * (fabsf(a) + fabsf(b) + bias_size)) sure = false;
+        }
+      }
 #pragma unroll
       for (int v = 0; v < V; ++v)
-        if (!(groups >> ((v * 32 + lane) / p.group_experts & 31) & 1)) choice.key[v] = 0;
+        if (!(kept & group_bit[v])) choice.key[v] = 0;
     }
-    // k rounds, and with a bias one more: the best that is left has to be as clearly behind as the others behind one another
-    float last = INFINITY, last_l = 0.f, last_b = 0.f, last_s = 0.f;
-    const int rounds = p.bias && p.k < p.E ? p.k + 1 : p.k;
     int mine = -1;  // lane i: the i-th chosen
     if (sure) {
-      for (int i = 0; i < rounds; ++i) {
+      // With a bias, values too close to tell: go on until one is clearly behind (what is behind that cannot be among the k), then by FP64
+      bool close_ones = false;
+      float last = INFINITY;
+      int last_expert = -1, m = 0;
+      for (;; ++m) {
         uint32_t key;
         int e;
+        if (!BIAS && m == p.k) break;
         if (!choice.best(lane, key, e)) break;
-        if (p.bias) {
-          const float v = key_value(key), li = logit<T>(row, e), b = p.bias[e], s = fabsf(v - b);
-          const float error = p.score_error * (s + last_s) + 0x1p-22f * (fabsf(v) + fabsf(b) + fabsf(last_b));
-          if (i && last - v <= error && !(li == last_l && b == last_b)) sure = false;
-          last = v;
-          last_l = li;
-          last_b = b;
-          last_s = s;
+        if (BIAS) {
+          const float value = key_value(key);
+          const bool near = m > 0 && last - value <= error + 0x1p-22f * (fabsf(value) + bias_size);
+          if (m >= p.k && !near) break;
+          if (m == 32) {  // (no end in sight)
+            sure = false;
+            break;
+          }
+          // (the same logit under the same bias: a tie, whatever the arithmetic)
+          close_ones |= near && !(logit<T>(row, e) == logit<T>(row, last_expert) && p.bias[e] == p.bias[last_expert]);
+          last = value;
+          last_expert = e;
         }
-        if (i == p.k) break;
-        if (lane == i) mine = e;
+        if (lane == m) mine = e;
         choice.take(lane, e);
       }
+      if (BIAS && sure && close_ones) mine = order64<T, V>(p, row, top, lane, m, mine);
     }
     if (!sure) {
       choose64<T, V>(p, row, top, lane, chosen);
       mine = lane < p.k ? chosen[lane] : -1;
       __syncwarp();
     }
+    if (lane >= p.k) mine = -1;
     // weights: lane i's
     float w = 0.f;
     const float lm = mine >= 0 ? logit<T>(row, mine) : -INFINITY;
@@ -330,12 +413,20 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_backward_kernel(const 
       along = warp_sum(s * g);
       d = g;
     }
-    for (int i = lane; i < p.E; i += 32) dl[i] = 0.f;
-    __syncwarp();
-    for (int i = 0; i < p.k; ++i) {  // (the same expert twice: one after the other)
-      if (lane == i && e >= 0) dl[e] += d;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      if (v * 32 + lane < p.E) dl[v * 32 + lane] = 0.f;
+    const uint32_t same = __match_any_sync(~0u, e);
+    if (__any_sync(~0u, e >= 0 && (same & (same - 1)))) {  // an expert twice: one after the other
+      for (int i = 0; i < p.k; ++i) {
+        if (lane == i && e >= 0) dl[e] += d;
+        __syncwarp();
+      }
+    } else {
       __syncwarp();
+      if (e >= 0) dl[e] = d;
     }
+    __syncwarp();
     T* out = static_cast<T*>(p.dlogits) + t * p.ldd;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -353,11 +444,13 @@ sp24_status with_experts(int64_t E, F&& f) {
   if (E <= 64) return f(std::integral_constant<int, 2>{});
   if (E <= 128) return f(std::integral_constant<int, 4>{});
   if (E <= 256) return f(std::integral_constant<int, 8>{});
+  if (E <= 512) return f(std::integral_constant<int, 16>{});
   return f(std::integral_constant<int, 32>{});
 }
 
-unsigned route_blocks(int64_t T) {
-  const int64_t blocks = (T + kRouteWarps - 1) / kRouteWarps, most = (int64_t)sm_count() * 64;
+// blocks of a warp to a token, at most `per_sm` to an SM
+unsigned route_blocks(int64_t T, int per_sm) {
+  const int64_t blocks = (T + kRouteWarps - 1) / kRouteWarps, most = (int64_t)sm_count() * per_sm;
   return (unsigned)(blocks < most ? blocks : most);
 }
 
@@ -385,12 +478,15 @@ extern "C" sp24_status sp24_route(sp24_dtype t, int64_t T, int64_t E, const void
   p.T = T; p.ld = ld; p.E = (int)E; p.k = k;
   p.groups = groups; p.group_experts = (int)(E / groups); p.top_groups = top_groups;
   p.sigmoid = score == SP24_SCORE_SIGMOID; p.top2 = group_score == SP24_GROUP_TOP2 && p.group_experts > 1 ? 1 : 0;
-  p.renorm = renorm != 0; p.scale = scale; p.score_error = p.sigmoid ? 0x1p-22f : 0x1p-18f;
+  p.renorm = renorm != 0; p.scale = scale;
   p.logits = logits; p.bias = bias; p.weights = weights; p.experts = experts;
   return with_float_type(t, [&](auto type) {
     using Type = typename decltype(type)::type;
     return with_experts(E, [&](auto v) {
-      return launch_overlapped(route_kernel<Type, decltype(v)::value>, dim3(route_blocks(T)), dim3(32 * kRouteWarps), 0, static_cast<cudaStream_t>(stream), 1, p);
+      return with_flags([&](auto with_bias, auto with_groups) {
+        return launch_overlapped(route_kernel<Type, decltype(v)::value, decltype(with_bias)::value, decltype(with_groups)::value>, dim3(route_blocks(T, 4)),
+                                 dim3(32 * kRouteWarps), decltype(with_groups)::value ? (size_t)(kRouteWarps * E * 4) : 0, static_cast<cudaStream_t>(stream), 1, p);
+      }, bias != nullptr, groups > 1);
     });
   });
 }
@@ -415,7 +511,7 @@ extern "C" sp24_status sp24_route_backward(sp24_dtype t, int64_t T, int64_t E, c
   return with_float_type(t, [&](auto type) {
     using Type = typename decltype(type)::type;
     return with_experts(E, [&](auto v) {
-      return launch_overlapped(route_backward_kernel<Type, decltype(v)::value>, dim3(route_blocks(T)), dim3(32 * kRouteWarps),
+      return launch_overlapped(route_backward_kernel<Type, decltype(v)::value>, dim3(route_blocks(T, 8)), dim3(32 * kRouteWarps),
                                (size_t)(kRouteWarps * E * 4), static_cast<cudaStream_t>(stream), 1, p);
     });
   });

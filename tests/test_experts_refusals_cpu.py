@@ -130,15 +130,17 @@ def test_gradients_own_strides():
     assert gradient("dx", rows=0, a=None) == 0
 
 
-def bias(t=sp.BF16, act=3, E=4, M=64, rows=48, dy=ONE, lddy=64, z=ONE, ldz=64, offsets=ONE, out=ONE, ws=ONE, ws_bytes=1 << 20):
-    return sp.lib.sp24_expert_bias_grad(t, act, E, M, rows, dy, lddy, z, ldz, offsets, out, ws, ws_bytes, None)
+def act_backward(t=sp.BF16, act=3, E=4, M=64, rows=48, dy=ONE, lddy=64, z=ONE, ldz=64, offsets=ONE, dz=ONE, lddz=64, dzt=ONE, lddzt=48, out=ONE, ws=ONE,
+                 ws_bytes=1 << 20):
+    return sp.lib.sp24_expert_act_backward(t, act, E, M, rows, dy, lddy, z, ldz, offsets, dz, lddz, dzt, lddzt, out, ws, ws_bytes, None)
 
 
 @pytest.mark.parametrize("status,args", [
-    (2, {"t": sp.I8}), (6, {"act": 9}), (3, {"E": 0}), (3, {"M": 0}), (3, {"rows": -1}), (1, {"dy": None}), (1, {"z": None}), (1, {"offsets": None}), (1, {"out": None}),
-    (4, {"lddy": 63}), (4, {"ldz": 63}), (5, {"dy": ODD}), (5, {"out": ODD}), (7, {"ws": None}), (7, {"ws_bytes": 64}), (7, {"ws": ctypes.c_void_p(4104)})])
-def test_bias(status, args):
-    assert bias(**args) == status
+    (2, {"t": sp.I8}), (6, {"act": 9}), (3, {"E": 0}), (3, {"E": 1025}), (3, {"M": 0}), (3, {"rows": -1}), (1, {"dy": None}), (1, {"z": None}), (1, {"offsets": None}),
+    (4, {"lddy": 63}), (4, {"ldz": 63}), (4, {"lddz": 63}), (4, {"lddzt": 47}), (5, {"dy": ODD}), (5, {"out": ODD}), (5, {"dzt": ODD}), (7, {"ws": None}),
+    (7, {"ws_bytes": 64}), (7, {"ws": ctypes.c_void_p(4104)}), (0, {"out": None, "dz": None, "dzt": None})])
+def test_act_backward(status, args):
+    assert act_backward(**args) == status
 
 
 def test_nothing_to_describe():
