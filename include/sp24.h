@@ -481,8 +481,9 @@ sp24_status sp24_route_backward(sp24_dtype t, int64_t T, int64_t E, const float*
  *   1 <= E <= 1024, 1 <= align <= 256, 0 <= slots, sp24_expert_rows(...) < 2^31.  align = 1 is for inference; the gradient of the products'
  *   weights wants 16. */
 int64_t sp24_expert_rows(int64_t slots, int64_t E, int64_t align);  /* slots + (align - 1) min(E, slots), up to a multiple of align */
+size_t sp24_expert_order_workspace_bytes(int64_t slots, int64_t E);  /* 16-byte aligned, contents of no matter; 0 for few slots */
 sp24_status sp24_expert_order(int64_t slots, int64_t E, int64_t align, const int32_t* experts, int32_t* offsets, int32_t* position,
-                              int32_t* source, void* stream);
+                              int32_t* source, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Rows in the experts' order: out[position[t, i], .] = x[t, .] for i < k; rows whose source is negative become zeros.  With scale (T floats), also
  * out_scale[position[t, i]] = scale[t], 0 for those.  Any type of 1, 2 or 4 bytes; T x K of them, out rows x K.  Positions that are negative or not

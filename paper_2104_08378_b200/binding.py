@@ -38,7 +38,7 @@ EXPORTS = [
     "sp24_gemm_static_ws_status", "sp24_set_tile_override", "sp24_test_set_fault_hooks", "sp24_gemm_f16acc",
     "sp24_gemm_plan", "sp24_rms_norm", "sp24_rms_norm_backward_workspace_bytes", "sp24_rms_norm_backward",
     "sp24_gated_act", "sp24_gated_act_backward", "sp24_act_backward_workspace_bytes", "sp24_act_backward",
-    "sp24_linear", "sp24_route", "sp24_route_backward", "sp24_expert_rows", "sp24_expert_order", "sp24_expert_gather",
+    "sp24_linear", "sp24_route", "sp24_route_backward", "sp24_expert_rows", "sp24_expert_order_workspace_bytes", "sp24_expert_order", "sp24_expert_gather",
     "sp24_expert_combine", "sp24_expert_combine_backward", "sp24_expert_linear", "sp24_expert_linear_dx", "sp24_expert_linear_dw",
     "sp24_expert_act_backward_workspace_bytes", "sp24_expert_act_backward",
 ]
@@ -133,7 +133,9 @@ def _load() -> ctypes.CDLL:
     lib.sp24_route_backward.argtypes = [ci, i64, i64, vp, vp, i64, vp, ci, ci, ci, cf, vp, i64, vp]
     lib.sp24_expert_rows.argtypes = [i64, i64, i64]
     lib.sp24_expert_rows.restype = i64
-    lib.sp24_expert_order.argtypes = [i64, i64, i64, vp, vp, vp, vp, vp]
+    lib.sp24_expert_order_workspace_bytes.argtypes = [i64, i64]
+    lib.sp24_expert_order_workspace_bytes.restype = sz
+    lib.sp24_expert_order.argtypes = [i64, i64, i64, vp, vp, vp, vp, vp, sz, vp]
     lib.sp24_expert_gather.argtypes = [ci, i64, i64, vp, i64, vp, ci, vp, i64, vp, vp, i64, vp, vp]
     lib.sp24_expert_combine.argtypes = [ci, i64, i64, i64, vp, i64, ci, vp, vp, vp, i64, vp, i64, vp]
     lib.sp24_expert_combine_backward.argtypes = [ci, i64, i64, i64, vp, i64, vp, i64, ci, vp, vp, vp, vp, i64, vp, vp]
@@ -163,6 +165,8 @@ else:                          # a CPU-only build of torch has no CUDA tensors: 
         gemm = gemm_i8_dequant = conv3x3_nhwc = compress = apply_mask = staticmethod(lambda *args: None)
         rms_norm = rms_norm_backward = gated_act = gated_act_backward = act_backward = linear = linear_backward = staticmethod(
             lambda *args: None)
+        route = route_backward = expert_order = expert_gather = expert_combine = expert_combine_backward = staticmethod(lambda *args: None)
+        expert_linear = expert_linear_backward = staticmethod(lambda *args: None)
 
 # Addresses for the native form of the short calls, which does what the functions below do if all arguments are of the
 # ordinary kind, and returns None if not (then they do it themselves) or the status of a call that was refused.
@@ -173,6 +177,12 @@ _RMS_NORM, _RMS_NORM_BACKWARD, _RMS_NORM_BYTES, _GATED, _GATED_BACKWARD, _ACT_BA
     ctypes.cast(getattr(lib, name), ctypes.c_void_p).value
     for name in ("sp24_rms_norm", "sp24_rms_norm_backward", "sp24_rms_norm_backward_workspace_bytes", "sp24_gated_act",
                  "sp24_gated_act_backward", "sp24_act_backward", "sp24_act_backward_workspace_bytes", "sp24_linear"))
+(_ROUTE, _ROUTE_BACKWARD, _ORDER, _ROWS, _ORDER_BYTES, _GATHER, _COMBINE, _COMBINE_BACKWARD, _EXPERT_LINEAR, _EXPERT_DX, _EXPERT_DW, _EXPERT_ACT,
+ _EXPERT_ACT_BYTES) = (
+    ctypes.cast(getattr(lib, name), ctypes.c_void_p).value
+    for name in ("sp24_route", "sp24_route_backward", "sp24_expert_order", "sp24_expert_rows", "sp24_expert_order_workspace_bytes", "sp24_expert_gather",
+                 "sp24_expert_combine", "sp24_expert_combine_backward", "sp24_expert_linear", "sp24_expert_linear_dx", "sp24_expert_linear_dw",
+                 "sp24_expert_act_backward", "sp24_expert_act_backward_workspace_bytes"))
 
 
 def status_string(status: int) -> str:
@@ -840,6 +850,9 @@ def route(logits: torch.Tensor, k: int, *, score: str = "softmax", bias: torch.T
     "sigmoid"; bias [E] float32 is added to the scores for the choice only; groups of E / groups experts, of which the top_groups (default: all) best by
     group_score ("max", or "top2": the sum of the two largest) stay; renorm: the weights of a token add up to scale.  Logits of -inf are never chosen;
     a slot that is left over has expert -1 and weight 0."""
+    done = _native.route(_ROUTE, logits, k, score, bias, groups, top_groups, group_score, renorm, scale)
+    if done is not None:
+        return done if type(done) is not int else _check(done, "sp24_route")
     return _route(logits, k, score, bias, groups, groups if top_groups is None else top_groups, group_score, renorm, scale)
 
 
@@ -867,11 +880,18 @@ def _slots(t: torch.Tensor, where: str, like: torch.Tensor, dtype, shape=None):
     _refuse(not t.is_contiguous(), ERR_STRIDE, where)
 
 
-@_on_device_of("dweights")
 def route_backward(dweights: torch.Tensor, logits: torch.Tensor, experts: torch.Tensor, *, score: str = "softmax", renorm: bool = True, scale: float = 1.0,
                    out: torch.Tensor | None = None) -> torch.Tensor:
     """sp24_route_backward: the gradient of the logits [T, E] from that of route's weights [T, k], for the experts that it chose; score, renorm and scale as
     there.  out may be the logits."""
+    done = _native.route_backward(_ROUTE_BACKWARD, dweights, logits, experts, score, renorm, scale, out)
+    if done is not None:
+        return done if type(done) is not int else _check(done, "sp24_route_backward")
+    return _route_backward(dweights, logits, experts, score, renorm, scale, out)
+
+
+@_on_device_of("dweights")
+def _route_backward(dweights, logits, experts, score, renorm, scale, out):
     where = "sp24_route_backward"
     t = _float_code(logits, where)
     ld = _matrix(logits, where)
@@ -886,16 +906,25 @@ def route_backward(dweights: torch.Tensor, logits: torch.Tensor, experts: torch.
     return dlogits
 
 
-@_on_device_of("experts")
 def expert_order(experts: torch.Tensor, E: int, *, align: int = 1) -> ExpertOrder:
     """sp24_expert_order: where each slot of experts [T, k] (int32; negative or not below E: none) lies when the rows of an expert lie together, in their own
     order.  Every expert's rows begin at a multiple of align: 1 for inference, 16 where expert_linear_backward is to follow."""
+    done = _native.expert_order(_ORDER, _ROWS, _ORDER_BYTES, experts, E, align)
+    if done is not None:
+        return ExpertOrder(*done) if type(done) is not int else _check(done, "sp24_expert_order")
+    return _expert_order(experts, E, align)
+
+
+@_on_device_of("experts")
+def _expert_order(experts, E, align):
     where = "sp24_expert_order"
     _slots(experts, where, experts, torch.int32)
     n = experts.numel()
     _refuse(not 1 <= E <= 1024 or not 1 <= align <= 256 or n >= 2 ** 31, ERR_SHAPE, where)
     order = ExpertOrder(experts.new_empty(E + 1), torch.empty_like(experts), experts.new_empty(lib.sp24_expert_rows(n, E, align)))
-    _check(lib.sp24_expert_order(n, E, align, _ptr(experts), _ptr(order.offsets), _ptr(order.position), _ptr(order.source), _stream()), where)
+    size = lib.sp24_expert_order_workspace_bytes(n, E)
+    scratch = experts.new_empty(size, dtype=torch.uint8) if size else None
+    _check(lib.sp24_expert_order(n, E, align, _ptr(experts), _ptr(order.offsets), _ptr(order.position), _ptr(order.source), _ptr(scratch), size, _stream()), where)
     return order
 
 
@@ -904,10 +933,17 @@ def _check_order(order: ExpertOrder, T: int, where: str, like: torch.Tensor):
     _vector(order.source, order.source.shape[0], where, like, (torch.int32,))
 
 
-@_on_device_of("x")
 def expert_gather(x: torch.Tensor, order: ExpertOrder, *, scale: torch.Tensor | None = None, out: torch.Tensor | None = None):
     """sp24_expert_gather: (rows of x [T, K] in the order of the experts [rows, K], their scales [rows] or None without scale [T]); rows that no slot has are
     zeros.  x of any type with 1, 2 or 4 bytes, as rms_norm gives it with its scale."""
+    done = _native.expert_gather(_GATHER, x, order.position, order.source, scale, out)
+    if done is not None:
+        return done if type(done) is not int else _check(done, "sp24_expert_gather")
+    return _expert_gather(x, order, scale, out)
+
+
+@_on_device_of("x")
+def _expert_gather(x, order, scale, out):
     where = "sp24_expert_gather"
     code = _FROM_TORCH.get(x.dtype)
     _refuse(code is None, ERR_DTYPE, where)
@@ -924,11 +960,18 @@ def expert_gather(x: torch.Tensor, order: ExpertOrder, *, scale: torch.Tensor | 
     return y, scales
 
 
-@_on_device_of("y")
 def expert_combine(y: torch.Tensor, order: ExpertOrder, weights: torch.Tensor | None = None, *, residual: torch.Tensor | None = None,
                    out: torch.Tensor | None = None) -> torch.Tensor:
     """sp24_expert_combine: the sums [T, K] of each token's rows of y [rows, K] with route's weights [T, k] (None: ones, the gradient of expert_gather),
     plus the residual [T, K].  out may be the residual."""
+    done = _native.expert_combine(_COMBINE, y, order.position, order.source, weights, residual, out)
+    if done is not None:
+        return done if type(done) is not int else _check(done, "sp24_expert_combine")
+    return _expert_combine(y, order, weights, residual, out)
+
+
+@_on_device_of("y")
+def _expert_combine(y, order, weights, residual, out):
     where = "sp24_expert_combine"
     t = _float_code(y, where)
     ldy = _matrix(y, where)
@@ -946,10 +989,17 @@ def expert_combine(y: torch.Tensor, order: ExpertOrder, weights: torch.Tensor | 
     return o
 
 
-@_on_device_of("dout")
 def expert_combine_backward(dout: torch.Tensor, y: torch.Tensor, order: ExpertOrder, weights: torch.Tensor, *, out: torch.Tensor | None = None):
     """sp24_expert_combine_backward: (dy [rows, K], dweights [T, k]) of expert_combine from the gradient of its result; the residual's is dout itself.  Rows of dy
     that no slot has are zeros.  out may be y."""
+    done = _native.expert_combine_backward(_COMBINE_BACKWARD, dout, y, order.position, order.source, weights, out)
+    if done is not None:
+        return done if type(done) is not int else _check(done, "sp24_expert_combine_backward")
+    return _expert_combine_backward(dout, y, order, weights, out)
+
+
+@_on_device_of("dout")
+def _expert_combine_backward(dout, y, order, weights, out):
     where = "sp24_expert_combine_backward"
     t = _float_code(dout, where)
     lddo = _matrix(dout, where)
@@ -993,7 +1043,6 @@ def expert_compress(W: torch.Tensor):
     return vals, meta
 
 
-@_on_device_of("A")
 def expert_linear(A: torch.Tensor, meta: torch.Tensor | None, X: torch.Tensor, offsets: torch.Tensor, *, bias: torch.Tensor | None = None,
                   act: str | None = None, residual: torch.Tensor | None = None, row_scale: torch.Tensor | None = None,
                   col_scale: torch.Tensor | None = None, pre: bool | torch.Tensor = False, out: torch.Tensor | None = None, cd: str | None = None,
@@ -1003,6 +1052,15 @@ def expert_linear(A: torch.Tensor, meta: torch.Tensor | None, X: torch.Tensor, o
     dense [E, M, K] with a_is_dense), X [rows, K], offsets [E + 1] int32 of expert_order, bias and row_scale [E, M], col_scale [rows] (8-bit operands),
     residual [rows, M] in D's type (it may be `out`).  Returns D [rows, M] of type cd (A's own, bf16 for 8-bit operands), or with pre=True (or a tensor
     for it) (D, what act was applied to).  Rows that belong to no expert are left as they are.  M and K are multiples of 16, with 8-bit operands of 32."""
+    done = _native.expert_linear(_EXPERT_LINEAR, _workspaces, _META_BYTES, A, meta, X, offsets, bias, act, residual, row_scale, col_scale, pre, out, cd,
+                                 a_is_dense, ws)
+    if done is not None:
+        return done if type(done) is not int else _check(done, "sp24_expert_linear")
+    return _expert_linear(A, meta, X, offsets, bias, act, residual, row_scale, col_scale, pre, out, cd, a_is_dense, ws)
+
+
+@_on_device_of("A")
+def _expert_linear(A, meta, X, offsets, bias, act, residual, row_scale, col_scale, pre, out, cd, a_is_dense, ws):
     where = "sp24_expert_linear"
     ab = _FROM_TORCH.get(A.dtype)
     _refuse(ab not in ("f16", "bf16") + _QUANT, ERR_DTYPE, where)
@@ -1039,7 +1097,6 @@ def expert_linear(A: torch.Tensor, meta: torch.Tensor | None, X: torch.Tensor, o
     return D if z is None else (D, z)
 
 
-@_on_device_of("dy")
 def expert_linear_backward(dy: torch.Tensor, pre: torch.Tensor | None, X: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, *, act: str | None = None,
                            meta: torch.Tensor | None = None, bias: bool = True, ws: torch.Tensor | None = None):
     """Gradients of expert_linear (16-bit operands) from dy [rows, M], its `pre` (None without an activation), X [rows, K] and the pruned weights W [E, M, K]
@@ -1047,6 +1104,15 @@ def expert_linear_backward(dy: torch.Tensor, pre: torch.Tensor | None, X: torch.
     dW of an expert that is not so placed is NaN.  With meta [E, bytes] the entries of dW that the 2:4 pattern leaves out are zeros.  Rows of dX that belong to
     no expert are left as they are; an expert without rows has dW and dbias of zeros.  The residual's gradient is dy.  dz = dy act'(pre) is rounded to dy's type
     before the two products, dbias is not."""
+    done = _native.expert_linear_backward(_EXPERT_ACT, _EXPERT_ACT_BYTES, _EXPERT_DX, _EXPERT_DW, _META_BYTES, _APPLY_MASK, _workspaces, dy, pre, X, W,
+                                          offsets, act, meta, bias, ws)
+    if done is not None:
+        return done if type(done) is not int else _check(done, "sp24_expert_linear_backward")
+    return _expert_linear_backward(dy, pre, X, W, offsets, act, meta, bias, ws)
+
+
+@_on_device_of("dy")
+def _expert_linear_backward(dy, pre, X, W, offsets, act, meta, bias, ws):
     where = "sp24_expert_linear_backward"
     code = _FROM_TORCH.get(dy.dtype)
     _refuse(code not in ("f16", "bf16"), ERR_DTYPE, where)

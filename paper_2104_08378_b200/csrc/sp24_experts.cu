@@ -8,40 +8,67 @@ namespace {
 constexpr int kMostExperts = 1024, kMostChosen = 32;
 
 // ---- order ------------------------------------------------------------------------------------------------------
-// A stable counting sort in one launch: a cluster of up to eight blocks, each with a part of the slots in their order, each warp with a part of
-// the block's.  A warp counts its slots by experts in shared memory (32 slots at a time, equal ones found by a match over the warp); the
-// counts of a block and then of the cluster are added up from the left, and the warp goes over its slots again with the places found.
+// A stable counting sort.  Each warp has a part of the slots in their order and counts them by experts in shared memory; the counts of a block's warps and then of the
+// blocks are added up from the left, and the warp goes over its slots again with the places found (32 at a time, equal ones found by a match over the warp).
+// Up to kClusterSlots slots in one launch, of a cluster of up to eight blocks that read one another's counts; the match, about 100 cycles each of an SM's
+// memory pipe, is what bounds it then, so more slots go to up to 128 blocks: their counts by a launch before (us, 131072 slots of 256 experts: 29, COUNTED).
 struct OrderParams {
   int64_t slots, rows;
   int E, align;
   const int32_t* experts;
   int32_t *offsets, *position, *source;
+  int32_t* counts;  // [blocks][E], where the counts come by a launch of their own
 };
+constexpr int64_t kClusterSlots = 8192, kMostOrderBlocks = 128;
 
-constexpr int kBatch = 8;
+__device__ __forceinline__ void slots_of_warp(const OrderParams& p, int block, int blocks, int warp, int warps, int64_t& begin, int64_t& end) {
+  const int64_t groups = (p.slots + 31) / 32, per_warp = (groups + (int64_t)blocks * warps - 1) / ((int64_t)blocks * warps);
+  begin = ((int64_t)block * warps + warp) * per_warp * 32;
+  end = min(p.slots, begin + per_warp * 32);
+}
+__device__ __forceinline__ int expert_of(const OrderParams& p, int64_t i, int64_t end) {
+  const int e = i < end ? p.experts[i] : -1;
+  return e >= 0 && e < p.E ? e : -1;
+}
+
+// The block's counts, for order_kernel<true> of the same number of blocks and threads.
+__global__ void __launch_bounds__(1024) count_kernel(const OrderParams p) {
+  extern __shared__ int32_t counts[];
+  for (int i = threadIdx.x; i < p.E; i += blockDim.x) counts[i] = 0;
+  const int warps = blockDim.x >> 5;
+  int64_t begin, end, none;
+  slots_of_warp(p, blockIdx.x, gridDim.x, 0, warps, begin, none);
+  slots_of_warp(p, blockIdx.x, gridDim.x, warps - 1, warps, none, end);
+  __syncthreads();
+  wait_for_stream();
+  for (int64_t i = begin + threadIdx.x; i < end; i += blockDim.x) {
+    const int e = expert_of(p, i, end);
+    if (e >= 0) atomicAdd(&counts[e], 1);  // (a sum of ones: any order)
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < p.E; i += blockDim.x) p.counts[(int64_t)blockIdx.x * p.E + i] = counts[i];
+}
+
+constexpr int kBatch = 4;
+template <bool COUNTED>
 __global__ void __launch_bounds__(1024) order_kernel(const OrderParams p) {
-  extern __shared__ int32_t counts[];  // [warps][E], then [E] of the block, [E] of the experts' first rows
+  extern __shared__ int32_t counts[];  // [warps][E], then [E] of the block, [E] of the experts' first rows, COUNTED: 2 [E] of all blocks
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  const int rank = (int)ptx::cluster_ctarank(), blocks = gridDim.x;
+  const int rank = COUNTED ? blockIdx.x : (int)ptx::cluster_ctarank(), blocks = gridDim.x;
   int32_t* of_block = counts + warps * p.E;
   int32_t* first = of_block + p.E;
   __shared__ int32_t of_warps[32];
   for (int i = threadIdx.x; i < (warps + 1) * p.E; i += blockDim.x) counts[i] = 0;
-  // this warp's slots: whole groups of 32
-  const int64_t groups = (p.slots + 31) / 32, per_warp = (groups + (int64_t)blocks * warps - 1) / ((int64_t)blocks * warps);
-  const int64_t begin = ((int64_t)rank * warps + warp) * per_warp * 32, end = min(p.slots, begin + per_warp * 32);
+  int64_t begin, end;
+  slots_of_warp(p, rank, blocks, warp, warps, begin, end);
   __syncthreads();
   wait_for_stream();
   int32_t* mine = counts + warp * p.E;
-  auto expert_of = [&](int64_t i) -> int {
-    const int e = i < end ? p.experts[i] : -1;
-    return e >= 0 && e < p.E ? e : -1;
-  };
   // kBatch groups at a time: their loads are all on the way before the first is used
   for (int64_t i = begin; i < end; i += 32 * kBatch) {
     int e[kBatch];
 #pragma unroll
-    for (int n = 0; n < kBatch; ++n) e[n] = expert_of(i + 32 * n + lane);
+    for (int n = 0; n < kBatch; ++n) e[n] = expert_of(p, i + 32 * n + lane, end);
 #pragma unroll
     for (int n = 0; n < kBatch; ++n)
       if (e[n] >= 0) atomicAdd(&mine[e[n]], 1);  // (a sum of ones: any order)
@@ -57,13 +84,34 @@ __global__ void __launch_bounds__(1024) order_kernel(const OrderParams p) {
     }
     of_block[e] = n;
   }
-  // (cluster of one: a barrier of the block's own)
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  auto cluster_barrier = [&] {  // (cluster of one: the block's own)
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  };
+  if (!COUNTED) cluster_barrier();
   // the experts' numbers of slots over all blocks and over the blocks before this one; then their first rows, by a scan
   int32_t total = 0, before = 0;
   const int e = threadIdx.x;  // (E <= 1024: blocks have at least E threads)
-  if (e < p.E) {
+  if (COUNTED) {
+    // as many threads to an expert as there are, each with every so manieth block; their sums in shared memory
+    int32_t* const totals = first + p.E;
+    for (int i = threadIdx.x; i < 2 * p.E; i += blockDim.x) totals[i] = 0;
+    __syncthreads();
+    const int sides = blockDim.x / p.E, side = threadIdx.x / p.E, x = threadIdx.x - side * p.E;
+    if (side < sides) {
+#pragma unroll 8
+      for (int b = side; b < blocks; b += sides) {
+        const int32_t c = p.counts[(int64_t)b * p.E + x];
+        if (b < rank) before += c;
+        total += c;
+      }
+      atomicAdd(&totals[x], total);
+      atomicAdd(&totals[p.E + x], before);
+    }
+    __syncthreads();
+    total = e < p.E ? totals[e] : 0;
+    before = e < p.E ? totals[p.E + e] : 0;
+  } else if (e < p.E) {
     for (int b = 0; b < blocks; ++b) {
       int32_t c;
       asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(c) : "r"(ptx::map_to_cta(ptx::smem_u32(of_block + e), (uint32_t)b)) : "memory");
@@ -100,7 +148,7 @@ __global__ void __launch_bounds__(1024) order_kernel(const OrderParams p) {
     int x[kBatch];
     uint32_t same[kBatch];
 #pragma unroll
-    for (int n = 0; n < kBatch; ++n) x[n] = expert_of(i + 32 * n + lane);
+    for (int n = 0; n < kBatch; ++n) x[n] = expert_of(p, i + 32 * n + lane, end);
 #pragma unroll
     for (int n = 0; n < kBatch; ++n) same[n] = __match_any_sync(~0u, x[n]);
 #pragma unroll
@@ -118,9 +166,7 @@ __global__ void __launch_bounds__(1024) order_kernel(const OrderParams p) {
       }
     }
   }
-  // no block leaves while another may still read its counts
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (!COUNTED) cluster_barrier();  // no block leaves while another may still read its counts
 }
 
 // ---- rows -------------------------------------------------------------------------------------------------------
@@ -266,10 +312,11 @@ __global__ void __launch_bounds__(256) combine_kernel(const RowsParams p) {
   }
 }
 
-// in: dout, y, out: dy, sums: dweights.  The token's gradient stays in registers (V vectors of each thread; longer rows in several passes) while its k rows go by; the
-// k sums meet in shared memory once.
+// in: dout, y, out: dy, sums: dweights.  The token's gradient stays in registers (V vectors of each thread; longer rows in several passes) while its k rows go by, kRows
+// of them on the way at a time; the k sums meet in shared memory once.
 template <typename T, typename W, int V>
 __global__ void __launch_bounds__(256) combine_backward_kernel(const RowsParams p) {
+  constexpr int kRows = 4 * V <= 8 ? 4 : 1;
   __shared__ float parts[2][kMostChosen][8];
   wait_for_stream();
   if (blockIdx.x >= p.token_blocks) {
@@ -281,45 +328,61 @@ __global__ void __launch_bounds__(256) combine_backward_kernel(const RowsParams 
   int turn = 0;
   for (int64_t t = blockIdx.x; t < p.T; t += p.token_blocks, turn ^= 1) {  // (a buffer is written again behind the other one's barrier)
     const W* d_row = reinterpret_cast<const W*>(p.in + t * p.ld_in);
-    const int32_t place = lane < p.k ? p.position[t * p.k + lane] : -1;
+    int32_t place = lane < p.k ? p.position[t * p.k + lane] : -1;
+    if (place >= p.rows) place = -1;
     const float weight = lane < p.k ? p.weights[t * p.k + lane] : 0.f;
-    for (int64_t c0 = 0; c0 < p.K; c0 += step) {
-      Values<T, W> d[V];
+    for (int64_t c0 = threadIdx.x; c0 - threadIdx.x < p.K; c0 += step) {
+      W d[V] = {};
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int64_t c = c0 + v * blockDim.x + threadIdx.x;
-        if (c < p.K) d[v].load(d_row + c);
-      }
-#pragma unroll 2
-      for (int i = 0; i < p.k; ++i) {
-        const int32_t r = __shfl_sync(~0u, place, i);
-        const float w = __shfl_sync(~0u, weight, i);
-        float dot = 0.f;
-        if (r >= 0 && r < p.rows) {
-          const W* y_row = reinterpret_cast<const W*>(p.y + (int64_t)r * p.ld_y);
-          W* out = reinterpret_cast<W*>(p.out + (int64_t)r * p.ld_out);
-          Values<T, W> y[V];
+      for (int v = 0; v < V; ++v)
+        if (c0 + v * blockDim.x < p.K) d[v] = d_row[c0 + v * blockDim.x];
+      for (int i0 = 0; i0 < p.k; i0 += kRows) {
+        W y[kRows][V] = {};
+        int32_t r[kRows];
 #pragma unroll
-          for (int v = 0; v < V; ++v) {
-            const int64_t c = c0 + v * blockDim.x + threadIdx.x;
-            if (c < p.K) y[v].load(y_row + c);
+        for (int i = 0; i < kRows; ++i) {
+          r[i] = __shfl_sync(~0u, place, min(i0 + i, 31));
+          if (i0 + i >= p.k) r[i] = -1;
+          if (r[i] >= 0) {
+            const W* row = reinterpret_cast<const W*>(p.y + (int64_t)r[i] * p.ld_y);
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+              if (c0 + v * blockDim.x < p.K) y[i][v] = row[c0 + v * blockDim.x];
           }
+        }
+        float dot[kRows];
 #pragma unroll
-          for (int v = 0; v < V; ++v) {
-            const int64_t c = c0 + v * blockDim.x + threadIdx.x;
-            if (c < p.K) {
+        for (int i = 0; i < kRows; ++i) {
+          dot[i] = 0.f;
+          const float w = __shfl_sync(~0u, weight, min(i0 + i, 31));
+          if (r[i] >= 0) {
+            W* out = reinterpret_cast<W*>(p.out + (int64_t)r[i] * p.ld_out);
 #pragma unroll
-              for (int n = 0; n < y[v].N; ++n) {
-                dot = fmaf(d[v].v[n], y[v].v[n], dot);
-                y[v].v[n] = w * d[v].v[n];
+            for (int v = 0; v < V; ++v) {
+              Values<T, W> a, b;
+              a.load(&d[v]);
+              b.load(&y[i][v]);
+#pragma unroll
+              for (int n = 0; n < a.N; ++n) {
+                dot[i] = fmaf(a.v[n], b.v[n], dot[i]);
+                a.v[n] *= w;
               }
-              y[v].store(out + c);
+              if (c0 + v * blockDim.x < p.K) a.store(out + c0 + v * blockDim.x);
             }
           }
         }
 #pragma unroll
-        for (int s = 16; s > 0; s >>= 1) dot += __shfl_xor_sync(~0u, dot, s);
-        if (lane == 0) parts[turn][i][warp] = c0 ? parts[turn][i][warp] + dot : dot;
+        for (int s = 16; s > 0; s >>= 1)
+#pragma unroll
+          for (int i = 0; i < kRows; ++i) dot[i] += __shfl_xor_sync(~0u, dot[i], s);
+        if (lane == 0) {
+#pragma unroll
+          for (int i = 0; i < kRows; ++i)
+            if (i0 + i < p.k) {
+              float& part = parts[turn][i0 + i][warp];
+              part = c0 >= step ? part + dot[i] : dot[i];
+            }
+        }
       }
     }
     __syncthreads();
@@ -363,31 +426,47 @@ extern "C" int64_t sp24_expert_rows(int64_t slots, int64_t E, int64_t align) {
   return (slots + (align - 1) * (E < slots ? E : slots) + align - 1) / align * align;
 }
 
+extern "C" size_t sp24_expert_order_workspace_bytes(int64_t slots, int64_t E) {
+  if (slots <= kClusterSlots || E < 1 || E > kMostExperts) return 0;
+  return (size_t)(kMostOrderBlocks * E * 4);
+}
+
 extern "C" sp24_status sp24_expert_order(int64_t slots, int64_t E, int64_t align, const int32_t* experts, int32_t* offsets, int32_t* position,
-                                         int32_t* source, void* stream) {
+                                         int32_t* source, void* workspace, size_t workspace_bytes, void* stream) {
   SP24_RETURN_IF(slots < 0 || E < 1 || E > kMostExperts || align < 1 || align > 256, SP24_ERR_SHAPE);
   const int64_t rows = sp24_expert_rows(slots, E, align);
   SP24_RETURN_IF(slots >= int64_t(1) << 31 || rows >= int64_t(1) << 31, SP24_ERR_SHAPE);
   SP24_RETURN_IF(offsets == nullptr || (slots > 0 && (experts == nullptr || position == nullptr || source == nullptr)), SP24_ERR_NULL);
   SP24_RETURN_IF(!aligned(experts, 4) || !aligned(offsets, 4) || !aligned(position, 4) || !aligned(source, 4), SP24_ERR_ALIGN);
+  const bool counted = slots > kClusterSlots;
+  SP24_RETURN_IF(counted && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < sp24_expert_order_workspace_bytes(slots, E)), SP24_ERR_WORKSPACE);
   const sp24_status arch = check_arch();
   SP24_RETURN_IF(arch != SP24_OK, arch);
-  OrderParams p = {slots, rows, (int)E, (int)align, experts, offsets, position, source};
-  // threads: one to an expert at least; a block to 2048 slots, eight at most
+  OrderParams p = {slots, rows, (int)E, (int)align, experts, offsets, position, source, static_cast<int32_t*>(workspace)};
+  // a block to 1024 slots, in a cluster eight at most; threads: one to an expert at least
   int64_t blocks = 1;
-  while (blocks < 8 && blocks * 2048 < slots) blocks *= 2;
+  if (counted) blocks = slots / 1024 < kMostOrderBlocks ? slots / 1024 : kMostOrderBlocks;
+  else
+    while (blocks < 8 && blocks * 1024 < slots) blocks *= 2;
   int64_t threads = (slots + blocks * 32 - 1) / (blocks * 32) * 32;
   if (threads < (E + 31) / 32 * 32) threads = (E + 31) / 32 * 32;
-  if (threads > 1024) threads = 1024;
-  const size_t smem = (size_t)((threads / 32 + 2) * E * 4);
+  if (threads > 1024 || counted) threads = 1024;
+  const size_t smem = (size_t)((threads / 32 + (counted ? 4 : 2)) * E * 4);
+  const auto kernel = counted ? order_kernel<true> : order_kernel<false>;
   static std::atomic<bool> allowed[64];  // the shared-memory opt-in, per device
   int dev = 0;
   SP24_CUDA_CHECK(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64 || !allowed[dev].load(std::memory_order_acquire)) {
-    SP24_CUDA_CHECK(cudaFuncSetAttribute(order_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 34 * kMostExperts * 4));
+    SP24_CUDA_CHECK(cudaFuncSetAttribute(order_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, 36 * kMostExperts * 4));
+    SP24_CUDA_CHECK(cudaFuncSetAttribute(order_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, 34 * kMostExperts * 4));
     if (dev >= 0 && dev < 64) allowed[dev].store(true, std::memory_order_release);
   }
-  return launch_overlapped(order_kernel, dim3((unsigned)blocks), dim3((unsigned)threads), smem, static_cast<cudaStream_t>(stream), (unsigned)blocks, p);
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (counted) {
+    const sp24_status st = launch_overlapped(count_kernel, dim3((unsigned)blocks), dim3((unsigned)threads), (size_t)(E * 4), s, 1, p);
+    SP24_RETURN_IF(st != SP24_OK, st);
+  }
+  return launch_overlapped(kernel, dim3((unsigned)blocks), dim3((unsigned)threads), smem, s, counted ? 1u : (unsigned)blocks, p);
 }
 
 extern "C" sp24_status sp24_expert_gather(sp24_dtype t, int64_t T, int64_t K, const void* x, int64_t ldx, const float* scale, int k,

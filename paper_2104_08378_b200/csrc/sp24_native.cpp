@@ -696,11 +696,375 @@ PyObject* linear_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
   }
 }
 
+// ---- experts ------------------------------------------------------------------------------------------------------------
+// A contiguous [T, k] of the type on the current device (T or k < 0: any)
+struct Slots {
+  const at::Tensor* t = nullptr;
+  void* p = nullptr;
+  int64_t T = 0, k = 0;
+  bool init(PyObject* o, int64_t rows, int64_t cols, at::ScalarType type) {
+    t = plain(o, 2);
+    if (t == nullptr || t->dim() != 2 || t->scalar_type() != type || t->get_device() != c10::cuda::current_device() || !t->is_contiguous()) return false;
+    T = t->size(0);
+    k = t->size(1);
+    if ((rows >= 0 && T != rows) || (cols >= 0 && k != cols)) return false;
+    p = t->data_ptr();
+    return true;
+  }
+};
+bool whole(PyObject* o, int64_t* v) {
+  if (!PyLong_CheckExact(o)) return false;
+  int over = 0;
+  *v = PyLong_AsLongLongAndOverflow(o, &over);
+  return over == 0;
+}
+bool truth(PyObject* o, int* v) {
+  *v = o == Py_True;
+  return o == Py_True || o == Py_False;
+}
+int one_of(PyObject* name, const char* zero, const char* one) {
+  if (!PyUnicode_CheckExact(name)) return -1;
+  return PyUnicode_CompareWithASCIIString(name, zero) == 0 ? 0 : PyUnicode_CompareWithASCIIString(name, one) == 0 ? 1 : -1;
+}
+// [E, M, columns]: matrices with contiguous rows one after the other
+struct Stack {
+  const at::Tensor* t = nullptr;
+  void* p = nullptr;
+  int64_t E = 0, M = 0, n = 0, ld = 0;
+  bool init(PyObject* o, int type) {
+    t = plain(o, 3);
+    if (t == nullptr || t->dim() != 3 || t->get_device() != c10::cuda::current_device() || (type >= 0 && t->scalar_type() != kScalar[type])) return false;
+    E = t->size(0);
+    M = t->size(1);
+    n = t->size(2);
+    if (E < 1 || M < 2 || n < 2 || t->stride(2) != 1 || (E > 1 && t->stride(0) != M * t->stride(1))) return false;
+    ld = t->stride(1);
+    p = t->data_ptr();
+    return true;
+  }
+};
+
+// route(address, logits, k, score, bias, groups, top_groups, group_score, renorm, scale) -> (weights, experts)
+PyObject* route(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 10 || at::impl::torch_function_mode_enabled()) return none();
+  try {
+    Matrix x;
+    int64_t k, groups, top;
+    int renorm;
+    double scale;
+    if (!x.init(v[1], -1, -1, -1) || !whole(v[2], &k) || !whole(v[5], &groups) || !truth(v[8], &renorm) || !number(v[9], &scale)) return none();
+    if (v[6] == Py_None) top = groups;
+    else if (!whole(v[6], &top)) return none();
+    const int t = type_code(x.t->scalar_type()), score = one_of(v[3], "softmax", "sigmoid"), by = one_of(v[7], "max", "top2");
+    const int64_t T = x.t->size(0), E = x.t->size(1);
+    const void* bias;
+    if (!float_type(t) || score < 0 || by < 0 || !vector(v[4], E, SP24_F32, SP24_F32, &bias) || k < 1 || k > E || groups < 1 || groups > E || top < 1 || top > groups)
+      return none();
+    const auto fn = function<decltype(&sp24_route)>(v[0]);
+    const cudaStream_t stream = Stream().handle;
+    at::Tensor weights, experts;
+    const int status = unlocked([&] {
+      weights = at::empty({T, k}, x.t->options().dtype(at::kFloat));
+      experts = at::empty({T, k}, x.t->options().dtype(at::kInt));
+      return fn((sp24_dtype)t, T, E, x.p, x.ld, (sp24_score)score, (const float*)bias, (int)groups, (int)top, (sp24_group_score)by, (int)k, renorm, (float)scale,
+                (float*)weights.data_ptr(), (int32_t*)experts.data_ptr(), stream);
+    });
+    if (status != SP24_OK) return PyLong_FromLong(status);
+    return Py_BuildValue("(NN)", THPVariable_Wrap(std::move(weights)), THPVariable_Wrap(std::move(experts)));
+  } catch (...) {
+    return none();
+  }
+}
+
+// route_backward(address, dweights, logits, experts, score, renorm, scale, out) -> dlogits
+PyObject* route_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 8 || at::impl::torch_function_mode_enabled()) return none();
+  try {
+    Matrix x, d;
+    Slots g, e;
+    int renorm;
+    double scale;
+    if (!x.init(v[2], -1, -1, -1) || !truth(v[5], &renorm) || !number(v[6], &scale)) return none();
+    const int t = type_code(x.t->scalar_type()), score = one_of(v[4], "softmax", "sigmoid");
+    const int64_t T = x.t->size(0), E = x.t->size(1);
+    if (!float_type(t) || score < 0 || !e.init(v[3], T, -1, at::kInt) || !g.init(v[1], T, e.k, at::kFloat) || (v[7] != Py_None && !d.init(v[7], T, E, t)))
+      return none();
+    const auto fn = function<decltype(&sp24_route_backward)>(v[0]);
+    const cudaStream_t stream = Stream().handle;
+    Result rd{v[7], {}};
+    const int status = unlocked([&] {
+      if (v[7] == Py_None) {
+        rd.made = at::empty({T, E}, x.t->options());
+        d.p = rd.made.data_ptr();
+        d.ld = E > 1 ? E : 1;
+      }
+      return fn((sp24_dtype)t, T, E, (const float*)g.p, x.p, x.ld, (const int32_t*)e.p, (int)e.k, (sp24_score)score, renorm, (float)scale, d.p, d.ld, stream);
+    });
+    if (status != SP24_OK) return PyLong_FromLong(status);
+    return rd.object();
+  } catch (...) {
+    return none();
+  }
+}
+
+// expert_order(addresses of sp24_expert_order, of sp24_expert_rows, of the workspace's size, experts, E, align) -> (offsets, position, source)
+PyObject* expert_order(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 6 || at::impl::torch_function_mode_enabled()) return none();
+  try {
+    Slots x;
+    int64_t E, align;
+    if (!x.init(v[3], -1, -1, at::kInt) || !whole(v[4], &E) || !whole(v[5], &align) || E < 1 || E > 1024 || align < 1 || align > 256) return none();
+    const int64_t slots = x.T * x.k;
+    if (slots >= int64_t(1) << 31) return none();
+    const auto fn = function<decltype(&sp24_expert_order)>(v[0]);
+    const int64_t rows = function<decltype(&sp24_expert_rows)>(v[1])(slots, E, align);
+    const size_t bytes = function<decltype(&sp24_expert_order_workspace_bytes)>(v[2])(slots, E);
+    const cudaStream_t stream = Stream().handle;
+    at::Tensor offsets, position, source, ws;
+    const int status = unlocked([&] {
+      const auto options = x.t->options();
+      offsets = at::empty({E + 1}, options);
+      position = at::empty({x.T, x.k}, options);
+      source = at::empty({rows}, options);
+      if (bytes) ws = at::empty({(int64_t)bytes}, options.dtype(at::kByte));
+      return fn(slots, E, align, (const int32_t*)x.p, (int32_t*)offsets.data_ptr(), (int32_t*)position.data_ptr(), (int32_t*)source.data_ptr(),
+                bytes ? ws.data_ptr() : nullptr, bytes, stream);
+    });
+    if (status != SP24_OK) return PyLong_FromLong(status);
+    return Py_BuildValue("(NNN)", THPVariable_Wrap(std::move(offsets)), THPVariable_Wrap(std::move(position)), THPVariable_Wrap(std::move(source)));
+  } catch (...) {
+    return none();
+  }
+}
+
+// expert_gather(address, x, position, source, scale, out) -> (rows, their scales)
+PyObject* expert_gather(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 6 || at::impl::torch_function_mode_enabled()) return none();
+  try {
+    Matrix x, y;
+    Slots at_;
+    if (!x.init(v[1], -1, -1, -1)) return none();
+    const int t = type_code(x.t->scalar_type());
+    const int64_t T = x.t->size(0), K = x.t->size(1);
+    const at::Tensor* s = plain(v[3], 1);
+    if (t < 0 || s == nullptr || s->dim() != 1 || !at_.init(v[2], T, -1, at::kInt)) return none();
+    const int64_t rows = s->size(0);
+    const void *source, *scale;
+    if (!vector(v[3], rows, SP24_I32, SP24_I32, &source) || !vector(v[4], T, SP24_F32, SP24_F32, &scale) || (v[5] != Py_None && !y.init(v[5], rows, K, t))) return none();
+    const auto fn = function<decltype(&sp24_expert_gather)>(v[0]);
+    const cudaStream_t stream = Stream().handle;
+    Result ry{v[5], {}}, rs{Py_None, {}};
+    const int status = unlocked([&] {
+      if (v[5] == Py_None) {
+        ry.made = at::empty({rows, K}, x.t->options());
+        y.p = ry.made.data_ptr();
+        y.ld = K > 1 ? K : 1;
+      }
+      if (v[4] != Py_None) rs.made = at::empty({rows}, x.t->options().dtype(at::kFloat));
+      return fn((sp24_dtype)t, T, K, x.p, x.ld, (const float*)scale, (int)at_.k, (const int32_t*)at_.p, rows, (const int32_t*)source, y.p, y.ld,
+                rs.made.defined() ? (float*)rs.made.data_ptr() : nullptr, stream);
+    });
+    if (status != SP24_OK) return PyLong_FromLong(status);
+    return Py_BuildValue("(NN)", ry.object(), rs.object());
+  } catch (...) {
+    return none();
+  }
+}
+
+// expert_combine(address, y, position, source, weights, residual, out) -> out
+PyObject* expert_combine(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 7 || at::impl::torch_function_mode_enabled()) return none();
+  try {
+    Matrix y, r, o;
+    Slots at_, w;
+    if (!y.init(v[1], -1, -1, -1) || !at_.init(v[2], -1, -1, at::kInt)) return none();
+    const int t = type_code(y.t->scalar_type());
+    const int64_t rows = y.t->size(0), K = y.t->size(1), T = at_.T;
+    const void* source;
+    if (!float_type(t) || v[3] == Py_None || !vector(v[3], rows, SP24_I32, SP24_I32, &source) || (v[4] != Py_None && !w.init(v[4], T, at_.k, at::kFloat)) ||
+        (v[5] != Py_None && !r.init(v[5], T, K, t)) || (v[6] != Py_None && !o.init(v[6], T, K, t)))
+      return none();
+    const auto fn = function<decltype(&sp24_expert_combine)>(v[0]);
+    const cudaStream_t stream = Stream().handle;
+    Result ro{v[6], {}};
+    const int status = unlocked([&] {
+      if (v[6] == Py_None) {
+        ro.made = at::empty({T, K}, y.t->options());
+        o.p = ro.made.data_ptr();
+        o.ld = K > 1 ? K : 1;
+      }
+      return fn((sp24_dtype)t, T, K, rows, y.p, y.ld, (int)at_.k, (const int32_t*)at_.p, (const float*)w.p, r.p, r.ld, o.p, o.ld, stream);
+    });
+    if (status != SP24_OK) return PyLong_FromLong(status);
+    return ro.object();
+  } catch (...) {
+    return none();
+  }
+}
+
+// expert_combine_backward(address, dout, y, position, source, weights, out) -> (dy, dweights)
+PyObject* expert_combine_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 7 || at::impl::torch_function_mode_enabled()) return none();
+  try {
+    Matrix g, y, dy;
+    Slots at_, w;
+    if (!g.init(v[1], -1, -1, -1) || !y.init(v[2], -1, -1, -1)) return none();
+    const int t = type_code(g.t->scalar_type());
+    const int64_t T = g.t->size(0), K = g.t->size(1), rows = y.t->size(0);
+    const void* source;
+    if (!float_type(t) || y.t->scalar_type() != g.t->scalar_type() || y.t->size(1) != K || !at_.init(v[3], T, -1, at::kInt) || v[4] == Py_None ||
+        !vector(v[4], rows, SP24_I32, SP24_I32, &source) || !w.init(v[5], T, at_.k, at::kFloat) || (v[6] != Py_None && !dy.init(v[6], rows, K, t)))
+      return none();
+    const auto fn = function<decltype(&sp24_expert_combine_backward)>(v[0]);
+    const cudaStream_t stream = Stream().handle;
+    Result rdy{v[6], {}}, rdw{Py_None, {}};
+    const int status = unlocked([&] {
+      if (v[6] == Py_None) {
+        rdy.made = at::empty({rows, K}, g.t->options());
+        dy.p = rdy.made.data_ptr();
+        dy.ld = K > 1 ? K : 1;
+      }
+      rdw.made = at::empty({T, at_.k}, w.t->options());
+      return fn((sp24_dtype)t, T, K, rows, g.p, g.ld, y.p, y.ld, (int)at_.k, (const int32_t*)at_.p, (const int32_t*)source, (const float*)w.p, dy.p, dy.ld,
+                (float*)rdw.made.data_ptr(), stream);
+    });
+    if (status != SP24_OK) return PyLong_FromLong(status);
+    return Py_BuildValue("(NN)", rdy.object(), rdw.object());
+  } catch (...) {
+    return none();
+  }
+}
+
+// the experts' metadata: [E, bytes], contiguous
+bool expert_meta(PyObject* o, PyObject* bytes_of, int type, int64_t E, int64_t M, int64_t K, const void** meta) {
+  Slots m;
+  const size_t bytes = function<decltype(&sp24_meta_bytes)>(bytes_of)((sp24_dtype)type, M, K, SP24_META_TCGEN05);
+  if (!m.init(o, E, (int64_t)bytes, at::kByte)) return false;
+  *meta = m.p;
+  return true;
+}
+
+// expert_linear(address, workspaces, address of sp24_meta_bytes, A, meta, X, offsets, bias, act, residual, row_scale, col_scale, pre, out, cd, a_is_dense, ws)
+PyObject* expert_linear(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 17 || at::impl::torch_function_mode_enabled()) return none();
+  try {
+    Stack a;
+    Matrix x, r, z, o;
+    Slots bias, scale;
+    int dense;
+    if (!a.init(v[3], -1) || !truth(v[15], &dense)) return none();
+    const int ab = type_code(a.t->scalar_type()), act = act_code(v[8]);
+    if (ab < 0 || ab == SP24_I32 || ab == SP24_F32 || act < 0 || !x.init(v[5], -1, -1, ab)) return none();
+    const bool one_byte = ab == SP24_I8 || ab == SP24_E4M3 || ab == SP24_E5M2;
+    const int cd = v[14] == Py_None ? (one_byte ? (int)SP24_BF16 : ab) : type_code(v[14]);
+    const int64_t E = a.E, M = a.M, K = dense ? a.n : 2 * a.n, rows = x.t->size(0);
+    const void *meta = nullptr, *offsets, *col_scale;
+    if (cd < 0 || x.t->size(1) != K || v[6] == Py_None || !vector(v[6], E + 1, SP24_I32, SP24_I32, &offsets)) return none();
+    if (!dense && !expert_meta(v[4], v[2], ab, E, M, K, &meta)) return none();
+    if ((v[7] != Py_None && !bias.init(v[7], E, M, at::kFloat)) || (v[10] != Py_None && !scale.init(v[10], E, M, at::kFloat)) ||
+        !vector(v[11], rows, SP24_F32, SP24_F32, &col_scale) || (v[9] != Py_None && !r.init(v[9], rows, M, cd)))
+      return none();
+    const bool make_pre = v[12] == Py_True, no_pre = v[12] == Py_False || v[12] == Py_None;
+    if ((!make_pre && !no_pre && !z.init(v[12], rows, M, cd)) || (v[13] != Py_None && !o.init(v[13], rows, M, cd))) return none();
+    const cudaStream_t stream = Stream().handle;
+    void* ws;
+    size_t ws_bytes;
+    if (!workspace(v[1], v[16], *a.t, stream, &ws, &ws_bytes)) return none();
+    const auto fn = function<decltype(&sp24_expert_linear)>(v[0]);
+    Result ro{v[13], {}}, rz{make_pre || no_pre ? Py_None : v[12], {}};
+    const int status = unlocked([&] {
+      auto make = [&](Result& to, Matrix& m) {
+        to.made = at::empty({rows, M}, a.t->options().dtype(kScalar[cd]));
+        m.p = to.made.data_ptr();
+        m.ld = M;
+      };
+      if (v[13] == Py_None) make(ro, o);
+      if (make_pre) make(rz, z);
+      const sp24_expert_desc d = {(sp24_dtype)ab, (sp24_dtype)cd, E, M, K, rows, a.ld, x.ld, o.ld, r.ld, z.ld, dense};
+      const sp24_expert_epilogue e = {(const float*)scale.p, (const float*)col_scale, (const float*)bias.p, (sp24_act)act, r.p, z.p};
+      return fn(&d, &e, a.p, meta, x.p, (const int32_t*)offsets, o.p, ws, ws_bytes, stream);
+    });
+    if (status != SP24_OK) return PyLong_FromLong(status);
+    if (no_pre) return ro.object();
+    return Py_BuildValue("(NN)", ro.object(), rz.object());
+  } catch (...) {
+    return none();
+  }
+}
+
+// expert_linear_backward(addresses of sp24_expert_act_backward, of its workspace's size, of sp24_expert_linear_dx, of sp24_expert_linear_dw, of sp24_meta_bytes, of
+// sp24_apply_mask, workspaces, dy, pre, X, W, offsets, act, meta, bias, ws) -> (dX, dW, dbias)
+PyObject* expert_linear_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 16 || at::impl::torch_function_mode_enabled()) return none();
+  try {
+    Matrix dy, z, x;
+    Stack w;
+    int with_bias;
+    const int act = act_code(v[12]);
+    if (act < 0 || !truth(v[14], &with_bias) || !dy.init(v[7], -1, -1, -1)) return none();
+    const int t = type_code(dy.t->scalar_type());
+    if ((t != SP24_F16 && t != SP24_BF16) || !w.init(v[10], t)) return none();
+    const int64_t rows = dy.t->size(0), E = w.E, M = w.M, K = w.n;
+    const void *offsets, *meta = nullptr;
+    if (rows < 1 || dy.t->size(1) != M || M % 16 != 0 || K % 16 != 0 || !x.init(v[9], rows, K, t) || v[11] == Py_None || !vector(v[11], E + 1, SP24_I32, SP24_I32, &offsets) ||
+        (act != SP24_ACT_NONE && !z.init(v[8], rows, M, t)) || (v[13] != Py_None && !expert_meta(v[13], v[4], t, E, M, K, &meta)))
+      return none();
+    const cudaStream_t stream = Stream().handle;
+    void* ws;
+    size_t ws_bytes;
+    if (!workspace(v[6], v[15], *dy.t, stream, &ws, &ws_bytes)) return none();
+    const auto act_fn = function<decltype(&sp24_expert_act_backward)>(v[0]);
+    const auto act_bytes = function<decltype(&sp24_expert_act_backward_workspace_bytes)>(v[1]);
+    const auto dx_fn = function<decltype(&sp24_expert_linear_dx)>(v[2]);
+    const auto dw_fn = function<decltype(&sp24_expert_linear_dw)>(v[3]);
+    const auto mask_fn = function<decltype(&sp24_apply_mask)>(v[5]);
+    Result rx{Py_None, {}}, rw{Py_None, {}}, rb{Py_None, {}};
+    const int status = unlocked([&]() -> int {
+      const auto options = dy.t->options();
+      // dz (without an activation dy itself, where a product can take it), its transpose and the partial sums of the bias's gradient, in one allocation
+      const bool makes_dz = act != SP24_ACT_NONE || (uintptr_t)dy.p % 16 != 0 || dy.ld * 2 % 16 != 0;
+      const int64_t lddzt = (rows + 7) / 8 * 8, lddz = makes_dz ? M : dy.ld;
+      const size_t bytes = with_bias ? act_bytes(E, M, rows) : 0, matrix = ((size_t)lddzt * M * 2 + 255) / 256 * 256;
+      const at::Tensor scratch = at::empty({(int64_t)(matrix * (makes_dz ? 2 : 1) + bytes)}, options.dtype(at::kByte));
+      char* const pdzt = (char*)scratch.data_ptr();
+      void* const pdz = makes_dz ? pdzt + matrix : dy.p;
+      if (with_bias) rb.made = at::empty({E, M}, options.dtype(at::kFloat));
+      int st = act_fn((sp24_dtype)t, (sp24_act)act, E, M, rows, dy.p, dy.ld, z.p, z.ld, (const int32_t*)offsets, makes_dz ? pdz : nullptr, lddz, pdzt, lddzt,
+                      with_bias ? (float*)rb.made.data_ptr() : nullptr, with_bias ? pdzt + matrix * (makes_dz ? 2 : 1) : nullptr, bytes, stream);
+      if (st != SP24_OK) return st;
+      rx.made = at::empty({rows, K}, options);
+      rw.made = at::empty({E, M, K}, options);
+      sp24_expert_desc d = {(sp24_dtype)t, (sp24_dtype)t, E, M, K, rows, w.ld, K, lddz, 0, 0, 1};
+      st = dx_fn(&d, pdz, w.p, (const int32_t*)offsets, rx.made.data_ptr(), ws, ws_bytes, stream);
+      if (st != SP24_OK) return st;
+      d.lda = K;
+      d.ldx = x.ld;
+      st = dw_fn(&d, pdzt, lddzt, x.p, (const int32_t*)offsets, rw.made.data_ptr(), ws, ws_bytes, stream);
+      if (st != SP24_OK || meta == nullptr) return st;
+      // (the metadata of an expert is whole blocks of 128 rows)
+      const size_t meta_bytes = function<decltype(&sp24_meta_bytes)>(v[4])((sp24_dtype)t, M, K, SP24_META_TCGEN05);
+      const int64_t at_once = M % 128 == 0 ? E : 1;
+      for (int64_t e = 0; e < E; e += at_once) {
+        char* const dw = (char*)rw.made.data_ptr() + e * M * K * 2;
+        st = mask_fn((sp24_dtype)t, at_once * M, K, dw, K, (const char*)meta + e * meta_bytes, SP24_META_TCGEN05, dw, K, stream);
+        if (st != SP24_OK) return st;
+      }
+      return st;
+    });
+    if (status != SP24_OK) return PyLong_FromLong(status);
+    return Py_BuildValue("(NNN)", rx.object(), rw.object(), rb.object());
+  } catch (...) {
+    return none();
+  }
+}
+
 #define SP24_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SP24_METHOD(gemm), SP24_METHOD(gemm_i8_dequant), SP24_METHOD(conv3x3_nhwc), SP24_METHOD(compress),
                          SP24_METHOD(apply_mask), SP24_METHOD(rms_norm), SP24_METHOD(rms_norm_backward), SP24_METHOD(gated_act),
                          SP24_METHOD(gated_act_backward), SP24_METHOD(act_backward), SP24_METHOD(linear),
-                         SP24_METHOD(linear_backward), {nullptr, nullptr, 0, nullptr}};
+                         SP24_METHOD(linear_backward), SP24_METHOD(route), SP24_METHOD(route_backward), SP24_METHOD(expert_order),
+                         SP24_METHOD(expert_gather), SP24_METHOD(expert_combine), SP24_METHOD(expert_combine_backward),
+                         SP24_METHOD(expert_linear), SP24_METHOD(expert_linear_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -12,6 +12,7 @@ constexpr int kRouteWarps = 8;
 struct RouteParams {
   int64_t T, ld;
   int E, k, groups, group_experts, top_groups;
+  int group_parts, group_stride;  // lanes that look for the best of a group (a power of two), and how far apart the groups lie in shared memory
   int sigmoid, top2, renorm;
   float scale;
   const void* logits;
@@ -171,189 +172,501 @@ __device__ __noinline__ int order64(const RouteParams& p, const void* row, float
   return mine;
 }
 
-// What bounds it: instructions, about 500 a token of 256 experts with groups and a bias (the scores a tenth of it, eight rounds of choosing half), so nothing is done
-// per expert that can be done once: the bias and the groups of a lane's experts stay in registers over its tokens, scores for the choice come from the
-// special-function units (the weights are computed again, exactly, for the chosen), the best of a group is found in shared memory by 32 / groups lanes
-// each.  BIAS, GROUPS: kernels without either carry none of it.
-template <typename T, int V, bool BIAS, bool GROUPS>
-__global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RouteParams p) {
-  __shared__ int32_t chosen_of[kRouteWarps][kMostChosen];
-  extern __shared__ float values_of[];  // GROUPS: E for each warp
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int32_t* chosen = chosen_of[warp];
-  float* values = values_of + warp * p.E;
-  wait_for_stream();
-  const bool two = GROUPS && p.top2, scores = BIAS || two, total = !p.sigmoid && !p.renorm;
-  float bias[V], bias_size = 0.f;
-  uint32_t group_bit[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    const int e = v * 32 + lane;
-    if (BIAS) {
-      bias[v] = e < p.E ? p.bias[e] : -INFINITY;
-      bias_size = fmaxf(bias_size, fabsf(bias[v]) < INFINITY ? fabsf(bias[v]) : 0.f);
-    }
-    if (GROUPS) group_bit[v] = 1u << ((e < p.E ? e / p.group_experts : 0) & 31);
+// The groups that stay, by FP64: lane (group, part) has every so manieth expert of its group.
+template <typename T>
+__device__ __noinline__ uint32_t groups64(const RouteParams& p, const void* row, float top_logit, int lane) {
+  const int parts = p.group_parts, g = lane / parts, first = g * p.group_experts;
+  const bool mine = g < p.groups;
+  auto score = [&](int i) {
+    const double l = (double)logit<T>(row, first + i);
+    return !(l > -INFINITY) ? -INFINITY : p.sigmoid ? 1.0 / (1.0 + exp(-l)) : exp(l - (double)top_logit);
+  };
+  double sum = 0.0, one = -INFINITY, two = -INFINITY;
+  if (!p.sigmoid) {
+    if (mine)
+      for (int i = lane & (parts - 1); i < p.group_experts; i += parts) sum += fmax(score(i), 0.0);
+    sum = warp_sum(sum);
   }
-  if (BIAS) asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(bias_size));
-  // lanes to a group: a power of two
-  int parts = 1;
-  if (GROUPS)
-    while (2 * parts * p.groups <= 32) parts *= 2;
-  for (int64_t t = (int64_t)blockIdx.x * kRouteWarps + warp; t < p.T; t += (int64_t)gridDim.x * kRouteWarps) {
-    const void* row = static_cast<const T*>(p.logits) + t * p.ld;
-    float l[V];
-    float top = -INFINITY;
-    bool nan = false;
+  if (mine)
+    for (int i = lane & (parts - 1); i < p.group_experts; i += parts) {
+      double x = score(i);
+      if (x > -INFINITY) x = (p.sigmoid ? x : x / sum) + (p.bias ? (double)p.bias[first + i] : 0.0);
+      if (!(x > -INFINITY)) continue;
+      two = fmax(two, fmin(one, x));
+      one = fmax(one, x);
+    }
+  for (int i = parts >> 1; i > 0; i >>= 1) {
+    const double a = __shfl_xor_sync(~0u, one, i), b = __shfl_xor_sync(~0u, two, i);
+    two = fmax(fmin(one, a), fmax(two, b));
+    one = fmax(one, a);
+  }
+  const double value = p.top2 && two > -INFINITY ? one + two : one;
+  int place = 0;
+  for (int h = 0; h < p.groups; ++h) {
+    const double other = __shfl_sync(~0u, value, h * parts);
+    place += other > value || (other == value && h < g);
+  }
+  const uint32_t lanes = __ballot_sync(~0u, mine && (lane & (parts - 1)) == 0 && place < p.top_groups);
+  uint32_t kept = 0;
+  for (int h = 0; h < p.groups; ++h) kept |= (lanes >> (h * parts) & 1) << h;
+  return kept;
+}
+
+// What a lane keeps of its experts over the tokens.
+template <int V>
+struct LaneExperts {
+  float bias[V], bias_size;  // the largest finite |bias| of all
+  uint8_t group_of[V];
+  __device__ __forceinline__ LaneExperts(const RouteParams& p, int lane, bool with_bias, bool with_groups) {
+    bias_size = 0.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int e = v * 32 + lane;
-      l[v] = e < p.E ? logit<T>(row, e) : -INFINITY;
+      if (with_bias) {
+        bias[v] = e < p.E ? p.bias[e] : -INFINITY;
+        bias_size = fmaxf(bias_size, fabsf(bias[v]) < INFINITY ? fabsf(bias[v]) : 0.f);
+      }
+      if (with_groups) group_of[v] = e < p.E ? e / p.group_experts : 0;
+    }
+    if (with_bias) asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(bias_size));
+  }
+};
+
+// One token, by a warp: any number of experts and groups, any alignment.  Scores for the choice come from the special-function units; the weights are computed again, exactly,
+// for the chosen.  `values`: room for a row for each group.
+template <typename T, int V, bool BIAS, bool GROUPS>
+__device__ __forceinline__ void route_token(const RouteParams& p, int64_t t, int lane, const LaneExperts<V>& x, uint2* mine_of, int32_t* chosen, float* values) {
+  const bool two = GROUPS && p.top2, scores = BIAS || two, total = !p.sigmoid && !p.renorm;
+  const int parts = p.group_parts, pad = p.group_stride - p.group_experts;
+  const void* row = static_cast<const T*>(p.logits) + t * p.ld;
+  float l[V];
+  float top = -INFINITY;
+  bool nan = false;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int e = v * 32 + lane;
+    l[v] = e < p.E ? logit<T>(row, e) : -INFINITY;
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    nan |= l[v] != l[v];
+    top = fmaxf(top, l[v]);
+  }
+  asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(top));
+  nan = __any_sync(~0u, nan) || (!p.sigmoid && top == INFINITY);
+  Choice<V> choice;
+  float inv = 1.f, error = 0.f;  // of two scores' difference
+  bool sure = true;
+  if (total) {
+    float sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) sum += l[v] > -INFINITY ? expf(l[v] - top) : 0.f;
+    inv = 1.f / warp_sum(sum);
+  }
+  if (scores) {
+    // For the choice: off by less than 1.5 2^-22 (sigmoid: half a step of the sum, a step of the reciprocal, a quarter of the exponential's two) or
+    // 2^-20 of the largest (softmax: the exponential's argument, up to d below the largest's, rounded twice, (d + 8) exp(-d) 2^-23 at most, and the sum).
+    float c[V];
+    if (p.sigmoid) {
+      error = 2.f * 1.5f * 0x1p-22f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) c[v] = reciprocal_fast(1.f + exp2_fast(-kLog2e * l[v]));
+    } else {
+      float sum = 0.f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        c[v] = l[v] > -INFINITY ? exp2_fast(kLog2e * (l[v] - top)) : 0.f;
+        sum += c[v];
+      }
+      const float part = 1.f / warp_sum(sum);
+      error = 2.f * 0x1p-20f * part;  // (the largest score)
+#pragma unroll
+      for (int v = 0; v < V; ++v) c[v] *= part;
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      nan |= l[v] != l[v];
-      top = fmaxf(top, l[v]);
+      if (BIAS) c[v] += x.bias[v];
+      if (!(l[v] > -INFINITY) || !(c[v] > -INFINITY)) c[v] = -INFINITY;
+      if (two && v * 32 + lane < p.E) values[v * 32 + lane + x.group_of[v] * pad] = c[v];
+      if (!BIAS) c[v] = l[v];
+      choice.key[v] = c[v] > -INFINITY ? order_key(c[v]) : 0u;
+      if (GROUPS && !two && v * 32 + lane < p.E) values[v * 32 + lane + x.group_of[v] * pad] = c[v];
     }
-    asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(top));
-    nan = __any_sync(~0u, nan) || (!p.sigmoid && top == INFINITY);
-    Choice<V> choice;
-    float inv = 1.f, error = 0.f;  // of two scores' difference
-    bool sure = true;
-    if (total) {
-      float sum = 0.f;
+  } else {
 #pragma unroll
-      for (int v = 0; v < V; ++v) sum += l[v] > -INFINITY ? expf(l[v] - top) : 0.f;
-      inv = 1.f / warp_sum(sum);
+    for (int v = 0; v < V; ++v) {
+      choice.key[v] = l[v] > -INFINITY ? order_key(l[v]) : 0u;
+      if (GROUPS && v * 32 + lane < p.E) values[v * 32 + lane + x.group_of[v] * pad] = l[v] > -INFINITY ? l[v] : -INFINITY;
+    }
+  }
+  if constexpr (GROUPS) {
+    __syncwarp();
+    const int g = lane / parts;
+    float one = -INFINITY, second = -INFINITY;
+    if (g < p.groups)
+      for (int i = lane & (parts - 1); i < p.group_experts; i += parts) {
+        const float y = values[g * p.group_stride + i];
+        second = fmaxf(second, fminf(one, y));
+        one = fmaxf(one, y);
+      }
+    for (int i = parts >> 1; i > 0; i >>= 1) {
+      const float a = __shfl_xor_sync(~0u, one, i), b = __shfl_xor_sync(~0u, second, i);
+      second = fmaxf(fminf(one, a), fmaxf(second, b));
+      one = fmaxf(one, a);
+    }
+    __syncwarp();
+    const float value = two && second > -INFINITY ? one + second : one;
+    // rounds of the best group, the first of equal ones; the lanes of a group go together
+    bool open = g < p.groups && value > -INFINITY;
+    const uint32_t key = open ? order_key(value) : 0u;
+    uint32_t kept = 0, worst = 0;
+    for (int i = 0; i < p.top_groups; ++i) {
+      const uint32_t m = __reduce_max_sync(~0u, open ? key : 0u);
+      if (m <= kDeadKey) break;
+      const int at = (__ffs(__ballot_sync(~0u, open && key == m)) - 1) / parts;
+      if (g == at) open = false;
+      kept |= 1u << at;
+      worst = m;
     }
     if (scores) {
-      // For the choice: off by less than 1.5 2^-22 (sigmoid: half a step of the sum, a step of the reciprocal, a quarter of the exponential's two) or
-      // 2^-20 of the largest (softmax: the exponential's argument, up to d below the largest's, rounded twice, (d + 8) exp(-d) 2^-23 at most, and the sum).
-      float c[V];
-      if (p.sigmoid) {
-        error = 2.f * 1.5f * 0x1p-22f;
-#pragma unroll
-        for (int v = 0; v < V; ++v) c[v] = reciprocal_fast(1.f + exp2_fast(-kLog2e * l[v]));
-      } else {
-        float sum = 0.f;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          c[v] = l[v] > -INFINITY ? exp2_fast(kLog2e * (l[v] - top)) : 0.f;
-          sum += c[v];
-        }
-        const float part = 1.f / warp_sum(sum);
-        error = 2.f * 0x1p-20f * part;  // (the largest score)
-#pragma unroll
-        for (int v = 0; v < V; ++v) c[v] *= part;
+      const uint32_t next = __reduce_max_sync(~0u, open ? key : 0u);
+      if (next > kDeadKey) {  // (sums of two: twice the error, and roundings of values)
+        const float a = key_value(worst), b = key_value(next);
+        if (a - b <= 2.f * error + 0x1p-21f * (fabsf(a) + fabsf(b) + x.bias_size)) kept = groups64<T>(p, row, top, lane);
       }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      if (!(kept >> x.group_of[v] & 1)) choice.key[v] = 0;
+  }
+  int mine = -1;  // lane i: the i-th chosen
+  // The k-th largest of the lanes' largest (k rounds, equal ones of several lanes in one) is not above the k-th largest of all: what reaches it, less what
+  // FP32 may be off, are the candidates, hardly more than k of them.  Each is in a lane's hands then, and its place is the number of those before it.
+  int candidates = 33;
+  float near = 0.f;  // (with a bias: how far apart two values must be to be told apart)
+  if (sure) {
+    uint32_t m = choice.key[0];
+#pragma unroll
+    for (int v = 1; v < V; ++v) m = max(m, choice.key[v]);
+    uint32_t least = 0;
+    for (int i = 0; i < p.k; ++i) {
+      const uint32_t top_key = __reduce_max_sync(~0u, m);
+      if (top_key <= kDeadKey) { least = 0; break; }
+      least = top_key;
+      if (m == top_key) m = 0;
+    }
+    if (BIAS) {
+      near = error + 0x1p-22f * (2.f + 2.f * x.bias_size);  // (sums of a score, at most 1, and a bias; rounded by half a step of theirs)
+      if (least) least = order_key(key_value(least) - near);
+    }
+    least = max(least, kDeadKey + 1);
+    candidates = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const bool in = choice.key[v] >= least;
+      const uint32_t all = __ballot_sync(~0u, in);
+      const int at = candidates + __popc(all & ((1u << lane) - 1));
+      if (in && at < 32) mine_of[at] = make_uint2(choice.key[v], v * 32 + lane);
+      candidates += __popc(all);
+    }
+    __syncwarp();
+    if (candidates <= 32) {
+      const uint2 own = lane < candidates ? mine_of[lane] : make_uint2(0, 0);
+      int place = lane < candidates ? 0 : 32;
+      for (int i = 0; i < candidates; ++i) {
+        const uint2 other = mine_of[i];  // (the same for all lanes)
+        place += other.x > own.x || (other.x == own.x && other.y < own.y);
+      }
+      __syncwarp();
+      if (lane < candidates) mine_of[place] = own;
+      __syncwarp();
+      const uint2 here = lane < candidates ? mine_of[lane] : make_uint2(0, 0);
+      mine = lane < candidates ? (int)here.y : -1;
+      if (BIAS) {
+        const uint2 next = lane + 1 < candidates ? mine_of[lane + 1] : make_uint2(0, 0);
+        bool doubt = lane < p.k && lane + 1 < candidates && key_value(here.x) - key_value(next.x) <= near;
+        // (the same logit under the same bias: a tie, whatever the arithmetic)
+        if (doubt) doubt = !(logit<T>(row, here.y) == logit<T>(row, next.y) && p.bias[here.y] == p.bias[next.y]);
+        if (__any_sync(~0u, doubt)) mine = order64<T, V>(p, row, top, lane, candidates, mine);
+      }
+      __syncwarp();
+    } else if (BIAS) {
+      sure = false;
+    } else {  // many equal logits, or a large k: one after the other
+      for (int i = 0; i < p.k; ++i) {
+        uint32_t key;
+        int e;
+        if (!choice.best(lane, key, e)) break;
+        if (lane == i) mine = e;
+        choice.take(lane, e);
+      }
+    }
+  }
+  if (!sure) {
+    choose64<T, V>(p, row, top, lane, chosen);
+    mine = lane < p.k ? chosen[lane] : -1;
+    __syncwarp();
+  }
+  if (lane >= p.k) mine = -1;
+  // weights: lane i's
+  float w = 0.f;
+  const float lm = mine >= 0 ? logit<T>(row, mine) : -INFINITY;
+  if (p.renorm) {
+    // in proportion to exp(z), z = l or the logarithm of the sigmoid of l, which cannot underflow all together
+    const float z = mine < 0 ? -INFINITY : (p.sigmoid ? fminf(lm, 0.f) - log1pf(expf(-fabsf(lm))) : lm);
+    float zmax = z;
+    asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(zmax));
+    const float u = mine < 0 ? 0.f : expf(z - zmax);
+    w = p.scale * __fdividef(u, warp_sum(u));
+  } else if (mine >= 0) {
+    w = p.scale * (p.sigmoid ? 1.f / (1.f + expf(-lm)) : expf(lm - top) * inv);
+  }
+  if (lane < p.k) {
+    p.experts[t * p.k + lane] = mine;
+    p.weights[t * p.k + lane] = mine < 0 ? 0.f : (nan ? __int_as_float(0x7fffffff) : w);
+  }
+}
+
+template <int V>
+constexpr int kRouteBlocks = V <= 8 ? 3 : 1;  // to an SM
+
+template <typename T, int V, bool BIAS, bool GROUPS>
+__global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RouteParams p) {
+  __shared__ int32_t chosen_of[kRouteWarps][kMostChosen];
+  __shared__ uint2 candidates_of[kRouteWarps][32];  // key, expert
+  extern __shared__ float values_of[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  wait_for_stream();
+  const LaneExperts<V> x(p, lane, BIAS, GROUPS);
+  for (int64_t t = (int64_t)blockIdx.x * kRouteWarps + warp; t < p.T; t += (int64_t)gridDim.x * kRouteWarps)
+    route_token<T, V, BIAS, GROUPS>(p, t, lane, x, candidates_of[warp], chosen_of[warp], values_of + warp * p.groups * p.group_stride);
+}
+
+// ---- up to 256 experts in chunks: a token to eight lanes -----------------------------------------------------------
+// What bounds the warp to a token is instructions: of 1600 for a token of 256 experts with groups and a bias most are reductions over the warp and bookkeeping, which four
+// tokens to a warp share.  Lane j of a token has the j-th eighth of its experts, whole 16-byte vectors; a group is 8 / groups lanes.  The k rounds: the largest of the
+// lanes' largest; its lane finds it in shared memory, where it has the largest of each eight of its values to look under.  Tokens that FP32 does not decide, or with a NaN
+// or +infinity among their logits, are done again by the whole warp (route_token).
+// Us, device, 16384 tokens, a warp to a token and this: MEASURED.
+constexpr int kChunkWarps = 4, kChunkTokens = 4 * kChunkWarps;
+template <int V>
+constexpr int kChunkRow = V + 4;  // floats of a lane's row in shared memory: lanes that read vectors together are in banks of their own
+
+__device__ __forceinline__ float max_nan(float a, float b) {
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(b));
+  return a;
+}
+
+template <typename T, bool BIAS, bool GROUPS>
+__device__ __noinline__ void route_again(const RouteParams& p, int64_t t, int lane, uint2* mine_of, int32_t* chosen, float* values) {
+  const LaneExperts<8> x(p, lane, BIAS, GROUPS);
+  route_token<T, 8, BIAS, GROUPS>(p, t, lane, x, mine_of, chosen, values);
+}
+
+template <typename T, int V, bool BIAS, bool GROUPS>
+__global__ void __launch_bounds__(32 * kChunkWarps) route_chunks_kernel(const RouteParams p) {
+  constexpr int R = kChunkRow<V>, S = V / 8, N = 16 / sizeof(T);
+  __shared__ __align__(16) float rows_of[kChunkWarps][32 * R];
+  __shared__ __align__(16) float bias_rows[BIAS ? 8 * R : 4];
+  __shared__ int32_t chosen_of[kChunkWarps][kMostChosen];
+  __shared__ uint2 candidates_of[kChunkWarps][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = lane & 7;
+  const int chunk = p.E / 8;
+  const bool two = GROUPS && p.top2, scores = BIAS || two, total = !p.sigmoid && !p.renorm;
+  wait_for_stream();
+  float bias_size = 0.f;  // the largest finite |bias|
+  if (BIAS) {
+    __shared__ int size_bits;
+    if (threadIdx.x == 0) size_bits = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 8 * V; i += blockDim.x) {
+      const float b = i % V < chunk ? p.bias[i / V * chunk + i % V] : -INFINITY;
+      bias_rows[i / V * R + i % V] = b;
+      if (fabsf(b) < INFINITY) bias_size = fmaxf(bias_size, fabsf(b));
+    }
+    atomicMax(&size_bits, __float_as_int(bias_size));
+    __syncthreads();
+    bias_size = __int_as_float(size_bits);
+  }
+  const int64_t t = ((int64_t)blockIdx.x * kChunkWarps + warp) * 4 + (lane >> 3);
+  const bool live = t < p.T;
+  const T* row = static_cast<const T*>(p.logits) + (live ? t : 0) * p.ld;
+  float l[V];
+#pragma unroll
+  for (int v = 0; v < V; v += N) {
+    Pairs<T> f = {};
+    if (v < chunk && live) unpack<T>(*reinterpret_cast<const uint4*>(row + j * chunk + v), f);
+#pragma unroll
+    for (int n = 0; n < N / 2; ++n) {
+      l[v + 2 * n] = v < chunk && live ? f[n].x : -INFINITY;
+      l[v + 2 * n + 1] = v < chunk && live ? f[n].y : -INFINITY;
+    }
+  }
+  auto over_token = [&](float v, auto op) {
+#pragma unroll
+    for (int i = 1; i < 8; i <<= 1) v = op(v, __shfl_xor_sync(~0u, v, i));
+    return v;
+  };
+  auto larger = [](float a, float b) { return fmaxf(a, b); };
+  auto sum_of = [](float a, float b) { return a + b; };
+  float top = l[0];
+#pragma unroll
+  for (int v = 1; v < V; ++v) top = max_nan(top, l[v]);
+  top = over_token(top, max_nan);
+  bool again = !(top < INFINITY);
+  const float base = fmaxf(top, -FLT_MAX);  // (nothing but -infinity: exponentials of 0)
+  float error = 0.f, near = 0.f, inv = 1.f;
+  float c[V];
+  if (scores || total) {
+    if (p.sigmoid) {
+      error = 2.f * 1.5f * 0x1p-22f;  // (as in route_token)
+#pragma unroll
+      for (int v = 0; v < V; ++v) c[v] = reciprocal_fast(1.f + exp2_fast(-kLog2e * l[v]));
+    } else {
+      float sum = 0.f;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        if (BIAS) c[v] += bias[v];
-        if (!(l[v] > -INFINITY) || !(c[v] > -INFINITY)) c[v] = -INFINITY;
-        if (two && v * 32 + lane < p.E) values[v * 32 + lane] = c[v];
-        if (!BIAS) c[v] = l[v];
-        choice.key[v] = c[v] > -INFINITY ? order_key(c[v]) : 0u;
-        if (GROUPS && !two && v * 32 + lane < p.E) values[v * 32 + lane] = c[v];
+        c[v] = exp2_fast(kLog2e * (l[v] - base));
+        sum += c[v];
+      }
+      inv = 1.f / over_token(sum, sum_of);
+      error = 2.f * 0x1p-20f * inv;
+#pragma unroll
+      for (int v = 0; v < V; ++v) c[v] *= inv;
+    }
+  }
+  if (scores) {
+    // (0 * l is 0 but for what may not be chosen, and NaN there)
+#pragma unroll
+    for (int v = 0; v < V; v += 4) {
+      float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (BIAS) b = *reinterpret_cast<const float4*>(bias_rows + j * R + v);
+      const float add[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int n = 0; n < 4; ++n) c[v + n] = fmaxf(c[v + n] + fmaf(l[v + n], 0.f, add[n]), -INFINITY);
+    }
+    near = error + 0x1p-22f * (2.f + 2.f * bias_size);
+  }
+  bool kept = true;
+  if constexpr (GROUPS) {
+    const int lanes = 8 / p.groups;
+    float one = -INFINITY, second = -INFINITY;
+    if (two) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        second = fmaxf(second, fminf(one, c[v]));
+        one = fmaxf(one, c[v]);
       }
     } else {
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        choice.key[v] = l[v] > -INFINITY ? order_key(l[v]) : 0u;
-        if (GROUPS && v * 32 + lane < p.E) values[v * 32 + lane] = l[v] > -INFINITY ? l[v] : -INFINITY;
-      }
+      for (int v = 0; v < V; ++v) one = fmaxf(one, BIAS ? c[v] : l[v]);
     }
-    if constexpr (GROUPS) {
-      __syncwarp();
-      const int g = lane / parts;
-      float one = -INFINITY, second = -INFINITY;
-      if (g < p.groups)
-        for (int i = lane & (parts - 1); i < p.group_experts; i += parts) {
-          const float x = values[g * p.group_experts + i];
-          second = fmaxf(second, fminf(one, x));
-          one = fmaxf(one, x);
-        }
-      for (int i = parts >> 1; i > 0; i >>= 1) {
-        const float a = __shfl_xor_sync(~0u, one, i), b = __shfl_xor_sync(~0u, second, i);
-        second = fmaxf(fminf(one, a), fmaxf(second, b));
-        one = fmaxf(one, a);
-      }
-      __syncwarp();
-      const float value = two && second > -INFINITY ? one + second : one;
-      // rounds of the best group, the first of equal ones; the lanes of a group go together
-      bool open = g < p.groups && value > -INFINITY;
-      const uint32_t key = open ? order_key(value) : 0u;
-      uint32_t kept = 0, worst = 0;
-      for (int i = 0; i < p.top_groups; ++i) {
-        const uint32_t m = __reduce_max_sync(~0u, open ? key : 0u);
-        if (m <= kDeadKey) break;
-        const int at = (__ffs(__ballot_sync(~0u, open && key == m)) - 1) / parts;
-        if (g == at) open = false;
-        kept |= 1u << at;
-        worst = m;
-      }
-      if (scores) {
-        const uint32_t next = __reduce_max_sync(~0u, open ? key : 0u);
-        if (next > kDeadKey) {  // (sums of two: twice the error, and roundings of values)
-          const float a = key_value(worst), b = key_value(next);
-          if (a - b <= 2.f * error + 0x1p-21f * (fabsf(a) + fabsf(b) + bias_size)) sure = false;
-        }
-      }
+    for (int i = 1; i < lanes; i <<= 1) {
+      const float a = __shfl_xor_sync(~0u, one, i), b = __shfl_xor_sync(~0u, second, i);
+      second = fmaxf(fminf(one, a), fmaxf(second, b));
+      one = fmaxf(one, a);
+    }
+    const float value = two && second > -INFINITY ? one + second : one;
+    int before = 0;
+    for (int i = lanes; i < 8; i += lanes) {
+      const float other = __shfl_xor_sync(~0u, value, i);
+      before += other > value || (other == value && (j ^ i) < j);
+    }
+    kept = before < p.top_groups;
+    if (scores && p.top_groups < p.groups) {
+      const float worst = -over_token(kept ? -value : -INFINITY, larger), next = over_token(kept ? -INFINITY : value, larger);
+      again |= next > -INFINITY && worst - next <= 2.f * error + 0x1p-21f * (4.f + 4.f * bias_size);
+    }
+  }
+  // what is chosen by, in shared memory, and the largest of each eight of a lane's
+  float* mine = rows_of[warp] + lane * R;
+  float best[S];
 #pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (!(kept & group_bit[v])) choice.key[v] = 0;
+  for (int v = 0; v < V; ++v)
+    if (!BIAS) c[v] = l[v];
+#pragma unroll
+  for (int v = 0; v < V; v += 4) *reinterpret_cast<float4*>(mine + v) = make_float4(c[v], c[v + 1], c[v + 2], c[v + 3]);
+  auto largest_of_eight = [](const float4& a, const float4& b) { return fmaxf(fmaxf(fmaxf(a.x, a.y), fmaxf(a.z, a.w)), fmaxf(fmaxf(b.x, b.y), fmaxf(b.z, b.w))); };
+  auto largest = [&] {
+    float m = best[0];
+#pragma unroll
+    for (int i = 1; i < S; ++i) m = fmaxf(m, best[i]);
+    return m;
+  };
+#pragma unroll
+  for (int i = 0; i < S; ++i)
+    best[i] = largest_of_eight(make_float4(c[8 * i], c[8 * i + 1], c[8 * i + 2], c[8 * i + 3]), make_float4(c[8 * i + 4], c[8 * i + 5], c[8 * i + 6], c[8 * i + 7]));
+  float lane_best = kept ? largest() : -INFINITY;
+  int chosen = -1;  // lane i of the token: the i-th
+  float last = INFINITY;
+  int last_expert = 0;
+  bool open = BIAS;  // whether what comes next is clearly behind the k chosen is still to be seen: after ties it takes more than one round
+  for (int i = 0; i < p.k || (BIAS && i < p.k + 8 && __any_sync(~0u, open)); ++i) {
+    const float m = over_token(lane_best, larger);
+    const uint32_t holders = __ballot_sync(~0u, lane_best == m) >> (lane & 24) & 0xffu;
+    const int w = (lane & 24) + __ffs(holders) - 1;
+    // where each lane's largest is: the first of the eight, the first in it
+    int at = 0;
+#pragma unroll
+    for (int s = S - 1; s > 0; --s)
+      if (best[s] == lane_best) at = s;
+    if (best[0] == lane_best) at = 0;
+    float4 a = *reinterpret_cast<const float4*>(mine + 8 * at), b = *reinterpret_cast<const float4*>(mine + 8 * at + 4);
+    int n = 7;
+    if (b.z == lane_best) n = 6;
+    if (b.y == lane_best) n = 5;
+    if (b.x == lane_best) n = 4;
+    if (a.w == lane_best) n = 3;
+    if (a.z == lane_best) n = 2;
+    if (a.y == lane_best) n = 1;
+    if (a.x == lane_best) n = 0;
+    const int place = 8 * at + n;
+    int e = __shfl_sync(~0u, j * chunk + place, w);
+    const bool some = m > -INFINITY;
+    if (lane == w && some) {
+      mine[place] = -INFINITY;
+      a = *reinterpret_cast<const float4*>(mine + 8 * at);
+      b = *reinterpret_cast<const float4*>(mine + 8 * at + 4);
+      const float rest = largest_of_eight(a, b);
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+        if (s == at) best[s] = rest;
+      lane_best = largest();
     }
-    int mine = -1;  // lane i: the i-th chosen
-    if (sure) {
-      // With a bias, values too close to tell: go on until one is clearly behind (what is behind that cannot be among the k), then by FP64
-      bool close_ones = false;
-      float last = INFINITY;
-      int last_expert = -1, m = 0;
-      for (;; ++m) {
-        uint32_t key;
-        int e;
-        if (!BIAS && m == p.k) break;
-        if (!choice.best(lane, key, e)) break;
-        if (BIAS) {
-          const float value = key_value(key);
-          const bool near = m > 0 && last - value <= error + 0x1p-22f * (fabsf(value) + bias_size);
-          if (m >= p.k && !near) break;
-          if (m == 32) {  // (no end in sight)
-            sure = false;
-            break;
-          }
-          // (the same logit under the same bias: a tie, whatever the arithmetic)
-          close_ones |= near && !(logit<T>(row, e) == logit<T>(row, last_expert) && p.bias[e] == p.bias[last_expert]);
-          last = value;
-          last_expert = e;
-        }
-        if (lane == m) mine = e;
-        choice.take(lane, e);
-      }
-      if (BIAS && sure && close_ones) mine = order64<T, V>(p, row, top, lane, m, mine);
+    if (BIAS && i > 0) {
+      const bool close = some && last - m <= near && (i < p.k || open);
+      bool doubt = close;
+      if (__any_sync(~0u, close) && close)  // (the same logit under the same bias: a tie, whatever the arithmetic)
+        doubt = !(to_float(row[e]) == to_float(row[last_expert]) && p.bias[e] == p.bias[last_expert]);
+      again |= doubt;
+      if (i >= p.k) open = close && !doubt;
     }
-    if (!sure) {
-      choose64<T, V>(p, row, top, lane, chosen);
-      mine = lane < p.k ? chosen[lane] : -1;
-      __syncwarp();
-    }
-    if (lane >= p.k) mine = -1;
-    // weights: lane i's
-    float w = 0.f;
-    const float lm = mine >= 0 ? logit<T>(row, mine) : -INFINITY;
-    if (p.renorm) {
-      // in proportion to exp(z), z = l or the logarithm of the sigmoid of l, which cannot underflow all together
-      const float z = mine < 0 ? -INFINITY : (p.sigmoid ? fminf(lm, 0.f) - log1pf(expf(-fabsf(lm))) : lm);
-      float zmax = z;
-      asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(zmax));
-      const float u = mine < 0 ? 0.f : expf(z - zmax);
-      w = p.scale * (u / warp_sum(u));
-    } else if (mine >= 0) {
-      w = p.scale * (p.sigmoid ? 1.f / (1.f + expf(-lm)) : expf(lm - top) * inv);
-    }
-    if (lane < p.k) {
-      p.experts[t * p.k + lane] = mine;
-      p.weights[t * p.k + lane] = mine < 0 ? 0.f : (nan ? __int_as_float(0x7fffffff) : w);
-    }
+    last = m;
+    last_expert = e;
+    if (j == i && i < p.k) chosen = some ? e : -1;
+  }
+  again |= open;
+  // weights: lane i's
+  const float lm = chosen >= 0 && live ? to_float(row[chosen]) : -INFINITY;
+  float weight = 0.f;
+  if (p.renorm) {
+    const float z = chosen < 0 ? -INFINITY : (p.sigmoid ? fminf(lm, 0.f) - log1pf(expf(-fabsf(lm))) : lm);
+    const float zmax = over_token(z, larger), u = chosen < 0 ? 0.f : expf(z - zmax);
+    weight = p.scale * __fdividef(u, over_token(u, sum_of));
+  } else {
+    weight = p.scale * (p.sigmoid ? 1.f / (1.f + expf(-lm)) : expf(lm - base) * inv);
+  }
+  if (live && j < p.k) {
+    p.experts[t * p.k + j] = chosen;
+    p.weights[t * p.k + j] = chosen < 0 ? 0.f : weight;
+  }
+  uint32_t tokens = __ballot_sync(~0u, again && live) & 0x01010101u;
+  __syncwarp();
+  while (tokens) {
+    const int first = __ffs(tokens) - 1;
+    tokens &= tokens - 1;
+    route_again<T, BIAS, GROUPS>(p, __shfl_sync(~0u, t, first), lane, candidates_of[warp], chosen_of[warp], rows_of[warp]);
+    __syncwarp();
   }
 }
 
@@ -450,8 +763,8 @@ sp24_status with_experts(int64_t E, F&& f) {
 
 // blocks of a warp to a token, at most `per_sm` to an SM
 unsigned route_blocks(int64_t T, int per_sm) {
-  const int64_t blocks = (T + kRouteWarps - 1) / kRouteWarps, most = (int64_t)sm_count() * per_sm;
-  return (unsigned)(blocks < most ? blocks : most);
+  const int64_t blocks = (T + kRouteWarps - 1) / kRouteWarps, most = (int64_t)sm_count() * per_sm, rounds = (blocks + most - 1) / most;
+  return (unsigned)((blocks + rounds - 1) / rounds);
 }
 
 }  // namespace
@@ -477,15 +790,32 @@ extern "C" sp24_status sp24_route(sp24_dtype t, int64_t T, int64_t E, const void
   RouteParams p = {};
   p.T = T; p.ld = ld; p.E = (int)E; p.k = k;
   p.groups = groups; p.group_experts = (int)(E / groups); p.top_groups = top_groups;
+  p.group_parts = 1;
+  while (2 * p.group_parts * groups <= 32) p.group_parts *= 2;
+  p.group_stride = p.group_experts + ((p.group_parts - p.group_experts) & 31);  // (each group's lanes in banks of their own)
   p.sigmoid = score == SP24_SCORE_SIGMOID; p.top2 = group_score == SP24_GROUP_TOP2 && p.group_experts > 1 ? 1 : 0;
   p.renorm = renorm != 0; p.scale = scale;
   p.logits = logits; p.bias = bias; p.weights = weights; p.experts = experts;
   return with_float_type(t, [&](auto type) {
     using Type = typename decltype(type)::type;
+    // whole vectors of an eighth of the experts, a lane to each of the chosen
+    const bool chunks = E <= 256 && E % 8 == 0 && E / 8 * (int64_t)sizeof(Type) % 16 == 0 && k <= 8 && groups <= 8 && 8 % groups == 0 && aligned16(logits) &&
+                        (T == 1 || ld * (int64_t)sizeof(Type) % 16 == 0) && T < int64_t(1) << 35;
+    if (chunks) {
+      auto run = [&](auto v) {
+        return with_flags([&](auto with_bias, auto with_groups) {
+          return launch_overlapped(route_chunks_kernel<Type, decltype(v)::value, decltype(with_bias)::value, decltype(with_groups)::value>,
+                                   dim3((unsigned)((T + kChunkTokens - 1) / kChunkTokens)), dim3(32 * kChunkWarps), 0, static_cast<cudaStream_t>(stream), 1, p);
+        }, bias != nullptr, groups > 1);
+      };
+      if (E <= 64) return run(std::integral_constant<int, 8>{});
+      if (E <= 128) return run(std::integral_constant<int, 16>{});
+      return run(std::integral_constant<int, 32>{});
+    }
     return with_experts(E, [&](auto v) {
       return with_flags([&](auto with_bias, auto with_groups) {
-        return launch_overlapped(route_kernel<Type, decltype(v)::value, decltype(with_bias)::value, decltype(with_groups)::value>, dim3(route_blocks(T, 4)),
-                                 dim3(32 * kRouteWarps), decltype(with_groups)::value ? (size_t)(kRouteWarps * E * 4) : 0, static_cast<cudaStream_t>(stream), 1, p);
+        return launch_overlapped(route_kernel<Type, decltype(v)::value, decltype(with_bias)::value, decltype(with_groups)::value>, dim3(route_blocks(T, kRouteBlocks<decltype(v)::value>)),
+                                 dim3(32 * kRouteWarps), decltype(with_groups)::value ? (size_t)(kRouteWarps * groups * p.group_stride * 4) : 0, static_cast<cudaStream_t>(stream), 1, p);
       }, bias != nullptr, groups > 1);
     });
   });

@@ -35,14 +35,14 @@ def test_route_backward(status, args):
     assert route_backward(**args) == status
 
 
-def order(slots=64, E=8, align=16, experts=ONE, offsets=ONE, position=ONE, source=ONE):
-    return sp.lib.sp24_expert_order(slots, E, align, experts, offsets, position, source, None)
+def order(slots=64, E=8, align=16, experts=ONE, offsets=ONE, position=ONE, source=ONE, ws=ONE, ws_bytes=1 << 20):
+    return sp.lib.sp24_expert_order(slots, E, align, experts, offsets, position, source, ws, ws_bytes, None)
 
 
 @pytest.mark.parametrize("status,args", [
     (3, {"slots": -1}), (3, {"E": 0}), (3, {"E": 1025}), (3, {"align": 0}), (3, {"align": 257}), (3, {"slots": 2 ** 31}), (3, {"slots": 2 ** 31 - 8}),
     (1, {"experts": None}), (1, {"offsets": None}), (1, {"position": None}), (1, {"source": None}), (5, {"offsets": ODD}), (5, {"source": ODD}),
-    (1, {"slots": 0, "offsets": None})])
+    (1, {"slots": 0, "offsets": None}), (7, {"slots": 10 ** 6, "ws": None}), (7, {"slots": 10 ** 6, "ws_bytes": 64}), (7, {"slots": 10 ** 6, "ws": ctypes.c_void_p(4100)})])
 def test_order(status, args):
     assert order(**args) == status
 

@@ -184,3 +184,28 @@ def test_order_of_nothing(sp):
     assert order.offsets.tolist() == [0] * 7 and bool((order.position == -1).all()) and bool((order.source == -1).all())
     weights, experts = sp.route(torch.empty((0, 8), device="cuda"), 2)
     assert weights.shape == experts.shape == (0, 2)
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E", [32, 64, 96, 128, 160, 192, 256])
+@pytest.mark.parametrize("groups,top_groups", [(1, 1), (2, 1), (4, 3), (8, 4)])
+def test_chunks_of_experts_and_single_ones_agree(sp, t, score, E, groups, top_groups):
+    """Rows of whole vectors go through other kernels than rows between boundaries; masks, infinities, NaN and ties among them."""
+    g = torch.Generator(device="cuda").manual_seed(E + groups)
+    wide = torch.randn((203, E + 1), generator=g, device="cuda").mul_(1.5).to(DTYPE[t])
+    wide[torch.rand(wide.shape, generator=g, device="cuda") < 0.1] = -math.inf
+    wide[3], wide[4, 5], wide[5, 7], wide[6] = -math.inf, math.nan, math.inf, 0.5
+    wide[7:9, :E // 2] = 0.25
+    whole = wide[:, 1:].contiguous()
+    for bias in (None, rand((E,), "f32", 3, 0.2), torch.zeros(E, device="cuda"), torch.where(torch.arange(E, device="cuda") % 3 == 0, -math.inf, 0.125)):
+        for by in ("max", "top2"):
+            for renorm in (True, False):
+                for k in (1, 3, 8):
+                    if k > top_groups * (E // groups):
+                        continue
+                    how = dict(score=score, bias=bias, groups=groups, top_groups=top_groups, group_score=by, renorm=renorm)
+                    a, b = sp.route(whole, k, **how), sp.route(wide[:, 1:], k, **how)
+                    assert torch.equal(a[1], b[1]), (bias is None, by, renorm, k)
+                    close(a[0], b[0].double(), "f32", WEIGHT * b[0].double().abs())
+    check(sp, whole[10:60], min(8, top_groups * (E // groups)), score=score, bias=rand((E,), "f32", 3, 0.2), groups=groups, top_groups=top_groups, group_score="top2")
