@@ -7,7 +7,7 @@ namespace sp24 {
 namespace {
 
 // The kernel is that of sp24_linear; only where a tile lies is looked up (a search in shared memory, in a table that every CTA makes of the
-// offsets at its start) and the last dimension of the tensor maps is that of all experts.  Tiles of one m-block; the columns of a tile as its caller chose.
+// offsets at its start) and the last dimension of the tensor maps is that of all experts.  Tiles of one m-block; the columns of a tile are its caller's choice.
 template <int KIND, bool SPARSE, int BLOCK_N, int CTAS, int GROUP>
 sp24_status launch_group(const TileShape& tile, const sp24_gemm_desc* d, const GemmParams& base, const void* A, const void* meta, const void* B, cudaStream_t stream) {
   constexpr bool kBMn = GROUP != kColumnsByExpert, kLinear = GROUP == kColumnsByExpert;
@@ -97,6 +97,7 @@ template <int KIND>
 sp24_status launch_group_shape(int group, TileShape t, bool sparse, const sp24_gemm_desc* d, const GemmParams& p, const void* A, const void* meta, const void* B,
                                cudaStream_t s) {
   const bool one = t.ctas == 1 && t.block_n == 128, pair = t.ctas == 2 && t.block_n == 224, wide = t.ctas == 2 && t.block_n == 256;
+  if (t.mblk != 1) return SP24_ERR_UNSUPPORTED;
   if (group == kColumnsByExpert) {
     if (one) return sparse ? launch_group<KIND, true, 128, 1, kColumnsByExpert>(t, d, p, A, meta, B, s) : launch_group<KIND, false, 128, 1, kColumnsByExpert>(t, d, p, A, meta, B, s);
     if (pair && sparse) return launch_group<KIND, true, 224, 2, kColumnsByExpert>(t, d, p, A, meta, B, s);

@@ -41,10 +41,52 @@ sp24_status run(int group, TileShape tile, bool sparse, const sp24_gemm_desc* d,
   return launch_experts<0>(group, tile, sparse, d, p, A, meta, B, s);
 }
 
+// Tests and benchmarks: the shape that sp24_set_tile_override names, of any number of columns (whole 32) that a built one has.
+void tile_override(TileShape* t, bool dense) {
+  int ctas, columns, mblk;
+  forced_tile(&ctas, &columns, &mblk);
+  if (ctas) *t = {ctas, ctas == 1 ? 128 : dense ? 256 : 224, mblk, columns, 0};
+}
+
 // Rows of an expert with rows, in the mean: what the tiles are chosen by.
 int64_t mean_rows(const sp24_expert_desc* d) {
   const int64_t met = d->E < d->rows ? d->E : d->rows;
   return met ? (d->rows + met - 1) / met : 0;
+}
+
+// The tile with the smallest estimated time, if every expert with rows has the mean number of them.  Two parts, us: the weights' way from HBM (with a little more where
+// an expert's rows take several tiles), and the tiles x time of one over the CTAs or pairs (k-blocks of 256 bytes of K, a fixed part and one per column each, then the
+// epilogue by columns, longer where other matrices are read or written); the sum of their cubes is compared, which is near the longer one.  Tiles of an expert: half a
+// tile more than the rows ask for; where one would do for the mean, from 0.4 of its columns on there are experts with twice the mean or more.
+// Fitted to bf16 and int8 products of 6 shapes (E, M, K from 8, 512, 512 to 64, 4096, 4096), 1 to 1024 rows an expert in the mean, even and uneven, at every width: 3.3 % off
+// the best in the mean over the 312, 37 % at worst (32 x 512 x 4096, 48 rows, uneven).  Tiles of two m-blocks, which long products of one problem take, were slower
+// nearly everywhere (bf16 16 experts 8192 x 4096, 16384 rows: 568 us, 518 and less with one).
+TileShape choose_expert_tile(const sp24_expert_desc* d, bool has_c, bool has_pre) {
+  const int64_t mean = mean_rows(d), met = d->E < d->rows ? d->E : d->rows;
+  const int cs = elem_bytes(d->cd_type), es = elem_bytes(d->ab_type);
+  const double k_blocks = (double)((d->K * es + 255) / 256) * (d->a_is_dense ? 2.0 : 1.0);
+  const double store = (cs == 4 ? (has_c ? 2.0 : 1.0) : (has_c ? 1.4 : 0.6)) + (has_pre ? (cs == 4 ? 1.0 : 0.6) : 0.0);
+  const double weights = (double)met * d->M * d->K * (d->a_is_dense ? es : 0.5 * es + 0.125) / 6.6e6;
+  TileShape best = {1, 128, 1, 32, 0};
+  double least = 0.0;
+  auto consider = [&](int ctas, int block_n, int tile_n, double tile) {
+    const int64_t rows = 128 * ctas, slots = sm_count() / ctas > 0 ? sm_count() / ctas : 1;
+    const double full = (double)mean / tile_n;
+    const double of_expert = full >= 1.0 ? full + 0.5 : full > 0.4 ? 1.0 + 0.5 * (full - 0.4) / 0.6 : 1.0;
+    const double rounds = (double)((d->M + rows - 1) / rows) * (double)met * of_expert / (double)slots;
+    const double time = tile * (rounds < 1.0 ? 1.0 : rounds + 0.6), way = weights * (1.0 + 0.07 * (of_expert - 1.0));
+    const double cost = time * time * time + way * way * way;
+    if (least == 0.0 || cost < least) {
+      least = cost;
+      best = {ctas, block_n, 1, tile_n, 0};
+    }
+  };
+  for (int n = 32; n <= 128; n += 32) consider(1, 128, n, k_blocks * (0.2 + 0.00095 * n) + 0.1 + store * 0.01 * n);
+  if (d->M <= 128) return best;
+  if (d->a_is_dense) consider(2, 256, 256, k_blocks * (0.165 + 0.00085 * 256) + 0.1 + store * 2.56);
+  else
+    for (int n = 64; n <= 224; n += 32) consider(2, 224, n, k_blocks * (0.165 + 0.00085 * n) + 0.1 + store * 0.01 * n);
+  return best;
 }
 
 }  // namespace
@@ -92,14 +134,9 @@ extern "C" sp24_status sp24_expert_linear(const sp24_expert_desc* d, const sp24_
   p.beta = p.has_c ? 1.f : 0.f;
   const sp24_gemm_desc g = {d->ab_type, d->cd_type, d->M, d->rows, d->K, d->lda, d->ldx, d->ld_residual, d->ldd, SP24_COL_MAJOR, SP24_COL_MAJOR, SP24_COL_MAJOR,
                             d->a_is_dense};
-  const int64_t mean = mean_rows(d);
-  TileShape tile = {1, 128, 1, 32, 0};
-  if (mean > 128 && d->M > 128) {
-    tile.ctas = 2;
-    tile.block_n = tile.tile_n = d->a_is_dense ? 256 : 224;
-  } else {
-    while (tile.tile_n < 128 && tile.tile_n < mean) tile.tile_n += 32;
-  }
+  TileShape tile = choose_expert_tile(d, e->residual != nullptr, e->pre != nullptr);
+  tile_override(&tile, d->a_is_dense != 0);
+  SP24_RETURN_IF(tile.tile_n > tile.block_n || tile.tile_n % 32, SP24_ERR_UNSUPPORTED);
   return run(kColumnsByExpert, tile, !d->a_is_dense, &g, p, A, meta, X, stream);
 }
 

@@ -155,6 +155,13 @@ void set_wait_limit(GemmParams& p) {
   if (v >= 1000000) p.wait_limit = v;
   p.test_skip_stage = cfg.test_skip_stage.load(std::memory_order_relaxed);
 }
+
+void forced_tile(int* ctas, int* block_n, int* mblk) {
+  Settings& cfg = settings();
+  *ctas = cfg.ctas.load(std::memory_order_relaxed);
+  *block_n = cfg.block_n.load(std::memory_order_relaxed);
+  *mblk = cfg.mblk.load(std::memory_order_relaxed);
+}
 }  // namespace sp24
 
 using namespace sp24;

@@ -141,5 +141,7 @@ sp24_status launch_experts(int group, TileShape tile, bool sparse, const sp24_ge
 
 // The status record's limit of a wait and test hook (sp24_test_set_fault_hooks) into p.
 void set_wait_limit(GemmParams& p);
+// The tile shape of sp24_set_tile_override; *ctas = 0: none.
+void forced_tile(int* ctas, int* block_n, int* mblk);
 
 }  // namespace sp24

@@ -104,6 +104,23 @@ def test_sizes(sp, ab, cd, dense, counts, M, K):
     check(sp, counts, M, K, ab, cd, "silu", 3, dense=dense, pad=16, pre=False)
 
 
+@pytest.mark.parametrize("tile", ["1x32x1", "1x64x1", "1x96x1", "1x128x1", "2x64x1", "2x96x1", "2x128x1", "2x160x1", "2x192x1", "2x224x1"])
+@pytest.mark.parametrize("ab,cd", [("bf16", "f32"), ("f16", "f16"), ("i8", "bf16"), ("e4m3", "f16")])
+def test_every_width(sp, force_tile, tile, ab, cd):
+    """Whatever tile a problem is given: experts that end inside one, at its edge, and with a row more."""
+    n = int(tile.split("x")[1])
+    force_tile(tile)
+    check(sp, [n - 1, n, 1, 0, n + 1, 2 * n + 17], 288, 544, ab, cd, "gelu", 1)
+    check(sp, [3, 2 * n], 160, 96, ab, cd, None, 2, bias=False, residual=False, pre=False)
+
+
+@pytest.mark.parametrize("ab", ["bf16", "i8"])
+def test_every_dense_width(sp, force_tile, ab):
+    for tile in ("1x64x1", "1x128x1", "2x128x1", "2x256x1"):
+        force_tile(tile)
+        check(sp, [255, 0, 256, 1, 257], 288, 416, ab, "bf16", "silu", 1, dense=True)
+
+
 def test_the_residual_may_be_the_result(sp):
     W, A, meta = weights(sp, 3, 64, 128, "bf16", False, 1)
     X, r = rand((50, 128), "bf16", 2), rand((50, 64), "bf16", 3)
