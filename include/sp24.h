@@ -536,6 +536,7 @@ sp24_status sp24_expert_linear(const sp24_expert_desc* d, const sp24_expert_epil
  * rounded once to ab_type, with dense W (E M rows of K values, leading dimension d->lda).
  *   sp24_expert_linear_dx: dz: rows x M (leading dimension d->ldd), dX: rows x K (ldx); only rows of experts are written.
  *   sp24_expert_linear_dw: dzt: dz transposed, M x rows (leading dimension lddzt), X: rows x K (ldx), dW: E M x K (lda).  An expert without rows gets zeros.
+ *      meta (or NULL): the weights' metadata, as for sp24_expert_linear; the entries of dW that it does not name as kept are zeros.
  *      Every offset is a multiple of 16 (sp24_expert_order with align = 16): the weights' gradients of an expert that is not so placed are NaN.
  *   d->cd_type is ab_type; d->ld_residual, d->ld_pre and d->a_is_dense are not used.  Sizes, alignment and workspace as above.
  * sp24_expert_act_backward: what they and the bias's gradient are made of, dz[r, i] = dy[r, i] act'(z[r, i]) rounded to t, for all rows (dz: rows x M or NULL; dzt: M x
@@ -549,8 +550,8 @@ sp24_status sp24_expert_act_backward(sp24_dtype t, sp24_act act, int64_t E, int6
                                      size_t workspace_bytes, void* stream);
 sp24_status sp24_expert_linear_dx(const sp24_expert_desc* d, const void* dz, const void* W, const int32_t* offsets, void* dX, void* workspace,
                                   size_t workspace_bytes, void* stream);
-sp24_status sp24_expert_linear_dw(const sp24_expert_desc* d, const void* dzt, int64_t lddzt, const void* X, const int32_t* offsets, void* dW, void* workspace,
-                                  size_t workspace_bytes, void* stream);
+sp24_status sp24_expert_linear_dw(const sp24_expert_desc* d, const void* dzt, int64_t lddzt, const void* X, const int32_t* offsets, const void* meta, void* dW,
+                                  void* workspace, size_t workspace_bytes, void* stream);
 
 /* End-to-end convenience for callers whose data lives in HOST memory (pinned for speed):
  * copies dense A (M x K, row-major, packed), B (N rows of K, packed) and, if beta != 0, C

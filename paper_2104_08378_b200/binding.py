@@ -141,7 +141,7 @@ def _load() -> ctypes.CDLL:
     lib.sp24_expert_combine_backward.argtypes = [ci, i64, i64, i64, vp, i64, vp, i64, ci, vp, vp, vp, vp, i64, vp, vp]
     lib.sp24_expert_linear.argtypes = [ctypes.POINTER(ExpertDesc), ctypes.POINTER(ExpertEpilogue), vp, vp, vp, vp, vp, vp, sz, vp]
     lib.sp24_expert_linear_dx.argtypes = [ctypes.POINTER(ExpertDesc), vp, vp, vp, vp, vp, sz, vp]
-    lib.sp24_expert_linear_dw.argtypes = [ctypes.POINTER(ExpertDesc), vp, i64, vp, vp, vp, vp, sz, vp]
+    lib.sp24_expert_linear_dw.argtypes = [ctypes.POINTER(ExpertDesc), vp, i64, vp, vp, vp, vp, vp, sz, vp]
     lib.sp24_expert_act_backward_workspace_bytes.argtypes = [i64, i64, i64]
     lib.sp24_expert_act_backward_workspace_bytes.restype = sz
     lib.sp24_expert_act_backward.argtypes = [ci, ci, i64, i64, i64, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, sz, vp]
@@ -1104,7 +1104,7 @@ def expert_linear_backward(dy: torch.Tensor, pre: torch.Tensor | None, X: torch.
     dW of an expert that is not so placed is NaN.  With meta [E, bytes] the entries of dW that the 2:4 pattern leaves out are zeros.  Rows of dX that belong to
     no expert are left as they are; an expert without rows has dW and dbias of zeros.  The residual's gradient is dy.  dz = dy act'(pre) is rounded to dy's type
     before the two products, dbias is not."""
-    done = _native.expert_linear_backward(_EXPERT_ACT, _EXPERT_ACT_BYTES, _EXPERT_DX, _EXPERT_DW, _META_BYTES, _APPLY_MASK, _workspaces, dy, pre, X, W,
+    done = _native.expert_linear_backward(_EXPERT_ACT, _EXPERT_ACT_BYTES, _EXPERT_DX, _EXPERT_DW, _META_BYTES, _workspaces, dy, pre, X, W,
                                           offsets, act, meta, bias, ws)
     if done is not None:
         return done if type(done) is not int else _check(done, "sp24_expert_linear_backward")
@@ -1149,8 +1149,5 @@ def _expert_linear_backward(dy, pre, X, W, offsets, act, meta, bias, ws):
     desc = ExpertDesc(t, t, E, M, K, rows, ldw, K, lddz, 0, 0, 1)
     _check(lib.sp24_expert_linear_dx(byref(desc), _ptr(dz), _ptr(W), _ptr(offsets), _ptr(dX), _ptr(ws), ws.numel(), stream), where)
     desc = ExpertDesc(t, t, E, M, K, rows, K, ldx, lddz, 0, 0, 1)
-    _check(lib.sp24_expert_linear_dw(byref(desc), _ptr(dzt), max(8, lddzt), _ptr(X), _ptr(offsets), _ptr(dW), _ptr(ws), ws.numel(), stream), where)
-    if meta is not None:
-        for first, n in ([(0, E * M)] if M % 128 == 0 else [(e, M) for e in range(E)]):
-            _check(lib.sp24_apply_mask(t, n, K, _ptr(dW[first]), K, _ptr(meta[first]), META_TCGEN05, _ptr(dW[first]), K, stream), where)
+    _check(lib.sp24_expert_linear_dw(byref(desc), _ptr(dzt), max(8, lddzt), _ptr(X), _ptr(offsets), _ptr(meta), _ptr(dW), _ptr(ws), ws.numel(), stream), where)
     return dX, dW, dbias

@@ -57,6 +57,9 @@ __global__ void __launch_bounds__(4 * kWide) act_grad_tile_kernel(const ActGradP
   const int64_t c = col0 + 8 * u;
   wait_for_stream();
   uint4 dy[kPasses] = {}, z[kPasses] = {};
+  // EXPERTS: the first expert whose rows end behind row0, by as many threads as there are experts while the tile is on its way
+  int first_expert = 0, end_of_mine = 0;
+  if (EXPERTS && p.partial && threadIdx.x < p.experts) end_of_mine = p.offsets[threadIdx.x + 1];
 #pragma unroll
   for (int v = 0; v < kPasses; ++v)
     if (const int64_t r = row0 + m0 + kRows * v; r < p.rows && c < p.cols) dy[v] = ld_stream(static_cast<const T*>(p.dy) + r * p.lddy + c);
@@ -64,6 +67,11 @@ __global__ void __launch_bounds__(4 * kWide) act_grad_tile_kernel(const ActGradP
 #pragma unroll
     for (int v = 0; v < kPasses; ++v)
       if (const int64_t r = row0 + m0 + kRows * v; r < p.rows && c < p.cols) z[v] = ld_stream(static_cast<const T*>(p.z) + r * p.ldz + c);
+  }
+  if (EXPERTS && p.partial) {
+    first_expert = __syncthreads_count(threadIdx.x < p.experts && end_of_mine <= row0);
+    for (int e = kWideThreads; e < p.experts; e += kWideThreads)
+      first_expert += __syncthreads_count(e + threadIdx.x < p.experts && p.offsets[e + threadIdx.x + 1] <= row0);
   }
   Pairs<T> sums = {};
 #pragma unroll
@@ -135,7 +143,7 @@ __global__ void __launch_bounds__(4 * kWide) act_grad_tile_kernel(const ActGradP
     // The sums above are of all rows of the tile, as they are wanted where they all belong to one expert.  Elsewhere they are made again, expert by expert.
     const int64_t end = min(p.rows, row0 + kWide);
     int64_t lo = 0, hi = 0;
-    for (int e = expert_of_row(p, row0); e < p.experts; ++e) {
+    for (int e = first_expert; e < p.experts; ++e) {
       rows_of_expert(p, e, lo, hi);
       if (lo >= end) break;
       if (hi <= lo) continue;

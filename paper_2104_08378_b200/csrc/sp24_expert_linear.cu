@@ -168,14 +168,15 @@ extern "C" sp24_status sp24_expert_linear_dx(const sp24_expert_desc* d, const vo
   return run(kRowsByExpert, tile, false, &g, p, dz, nullptr, W, stream);
 }
 
-extern "C" sp24_status sp24_expert_linear_dw(const sp24_expert_desc* d, const void* dzt, int64_t lddzt, const void* X, const int32_t* offsets, void* dW,
-                                             void* workspace, size_t workspace_bytes, void* stream) {
+extern "C" sp24_status sp24_expert_linear_dw(const sp24_expert_desc* d, const void* dzt, int64_t lddzt, const void* X, const int32_t* offsets, const void* meta,
+                                             void* dW, void* workspace, size_t workspace_bytes, void* stream) {
   SP24_RETURN_IF(d == nullptr, SP24_ERR_NULL);
   SP24_RETURN_IF((d->ab_type != SP24_F16 && d->ab_type != SP24_BF16) || d->cd_type != d->ab_type, SP24_ERR_DTYPE);
   sp24_status st = check_sizes(d);
   SP24_RETURN_IF(st != SP24_OK, st);
   st = check_gradient(d, dzt, lddzt, d->rows, X, d->ldx, offsets, dW, d->lda, workspace, workspace_bytes);
   SP24_RETURN_IF(st != SP24_OK, st);
+  SP24_RETURN_IF(reinterpret_cast<uintptr_t>(meta) & 1, SP24_ERR_ALIGN);
   if (d->rows == 0) {  // no expert has any
     SP24_CUDA_CHECK(cudaMemset2DAsync(dW, (size_t)d->lda * 2, 0, (size_t)d->K * 2, (size_t)(d->E * d->M), static_cast<cudaStream_t>(stream)));
     return SP24_OK;
@@ -184,5 +185,7 @@ extern "C" sp24_status sp24_expert_linear_dw(const sp24_expert_desc* d, const vo
   const sp24_gemm_desc g = {d->ab_type, d->cd_type, d->M, d->K, d->rows, lddzt, d->ldx, 0, d->lda, SP24_ROW_MAJOR, SP24_ROW_MAJOR, SP24_ROW_MAJOR, 1};
   TileShape tile = {1, 128, 1, 128, 0};
   if (d->M > 128 && d->K > 128) tile = {2, 256, 1, 256, 0};
+  p.keep = static_cast<const uint8_t*>(meta);
+  p.keep_kb = (int)(2 * ((d->K + 255) / 256));
   return run(kKByExpert, tile, false, &g, p, dzt, nullptr, X, stream);
 }

@@ -171,13 +171,13 @@ __global__ void __launch_bounds__(1024) order_kernel(const OrderParams p) {
 
 // ---- rows -------------------------------------------------------------------------------------------------------
 // A block has a token (or several one after the other), its threads the vectors of the row, at most kAhead of them in registers at a time; the
-// blocks behind those look for rows without a slot and clear them.  A vector is 16 bytes, or one element of the type where rows are not made of
+// blocks before those look for rows without a slot and clear them.  A vector is 16 bytes, or one element of the type where rows are not made of
 // whole ones at 16-byte boundaries.
 struct RowsParams {
   int64_t T, K, rows;        // K in vectors
   int64_t ld_in, ld_out, ld_y, ld_res;  // bytes
   int k;
-  int token_blocks;
+  int clear_blocks, token_blocks;
   const int32_t *position, *source;
   const uint8_t *in, *y, *residual;
   uint8_t* out;
@@ -191,26 +191,21 @@ __device__ __forceinline__ W zero_vector() {
   else return W(0);
 }
 
+// The first p.clear_blocks blocks.  A warp looks at 32 rows at a time, as far apart as there are warps: rows without a slot come in long runs, behind the last expert.
 template <typename W>
 __device__ void clear_rows(const RowsParams& p, int64_t ld, uint8_t* out, float* scale) {
-  const int64_t blocks = gridDim.x - p.token_blocks;
-  for (int64_t r0 = (int64_t)(blockIdx.x - p.token_blocks) * blockDim.x; r0 < p.rows; r0 += blocks * blockDim.x) {
-    const int64_t r = r0 + threadIdx.x;
+  const int lane = threadIdx.x & 31;
+  const int64_t warps = (int64_t)p.clear_blocks * (blockDim.x >> 5), warp = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  for (int64_t r0 = warp; r0 < p.rows; r0 += 32 * warps) {
+    const int64_t r = r0 + lane * warps;
     const bool empty = r < p.rows && p.source[r] < 0;
     if (empty && scale) scale[r] = 0.f;
-    __shared__ int32_t list[1024];
-    __shared__ int count;
-    if (threadIdx.x == 0) count = 0;
-    __syncthreads();
-    if (empty) list[atomicAdd(&count, 1)] = threadIdx.x;  // (in any order: they all become zeros)
-    __syncthreads();
-    const int n = count;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    for (int i = warp; i < n; i += warps) {
-      W* row = reinterpret_cast<W*>(out + (r0 + list[i]) * ld);
+    uint32_t left = __ballot_sync(~0u, empty);
+    while (left) {
+      W* row = reinterpret_cast<W*>(out + (r0 + (__ffs(left) - 1) * warps) * ld);
+      left &= left - 1;
       for (int64_t c = lane; c < p.K; c += 32) row[c] = zero_vector<W>();
     }
-    __syncthreads();
   }
 }
 
@@ -219,11 +214,11 @@ template <typename W>
 __global__ void __launch_bounds__(256) gather_kernel(const RowsParams p) {
   __shared__ int32_t place[kMostChosen];
   wait_for_stream();
-  if (blockIdx.x >= p.token_blocks) {
+  if (blockIdx.x < p.clear_blocks) {
     clear_rows<W>(p, p.ld_out, p.out, p.sums);
     return;
   }
-  for (int64_t t = blockIdx.x; t < p.T; t += p.token_blocks) {
+  for (int64_t t = blockIdx.x - p.clear_blocks; t < p.T; t += p.token_blocks) {
     __syncthreads();
     if (threadIdx.x < p.k) {
       int32_t r = p.position[t * p.k + threadIdx.x];
@@ -319,14 +314,14 @@ __global__ void __launch_bounds__(256) combine_backward_kernel(const RowsParams 
   constexpr int kRows = 4 * V <= 8 ? 4 : 1;
   __shared__ float parts[2][kMostChosen][8];
   wait_for_stream();
-  if (blockIdx.x >= p.token_blocks) {
+  if (blockIdx.x < p.clear_blocks) {
     clear_rows<W>(p, p.ld_out, p.out, nullptr);
     return;
   }
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   const int64_t step = (int64_t)V * blockDim.x;
   int turn = 0;
-  for (int64_t t = blockIdx.x; t < p.T; t += p.token_blocks, turn ^= 1) {  // (a buffer is written again behind the other one's barrier)
+  for (int64_t t = blockIdx.x - p.clear_blocks; t < p.T; t += p.token_blocks, turn ^= 1) {  // (a buffer is written again behind the other one's barrier)
     const W* d_row = reinterpret_cast<const W*>(p.in + t * p.ld_in);
     int32_t place = lane < p.k ? p.position[t * p.k + lane] : -1;
     if (place >= p.rows) place = -1;
@@ -410,9 +405,9 @@ unsigned token_blocks(int64_t T) {
   const int64_t most = (int64_t)sm_count() * 32;
   return (unsigned)(T < most ? T : most);
 }
-// blocks that look for rows to clear
+// blocks that look for rows to clear: a warp to four rows, at most two blocks to an SM
 unsigned clearing_blocks(int64_t rows, unsigned threads) {
-  const int64_t n = (rows + threads - 1) / threads, most = sm_count();
+  const int64_t warps = threads / 32, n = (rows + 4 * warps - 1) / (4 * warps), most = 2 * (int64_t)sm_count();
   return (unsigned)(n < most ? n : most);
 }
 
@@ -493,7 +488,8 @@ extern "C" sp24_status sp24_expert_gather(sp24_dtype t, int64_t T, int64_t K, co
     p.K = K * es / (int64_t)sizeof(W);
     const unsigned threads = row_threads(p.K);
     p.token_blocks = (int)token_blocks(T);
-    return launch_overlapped(gather_kernel<W>, dim3(p.token_blocks + clearing_blocks(rows, threads)), dim3(threads), 0, static_cast<cudaStream_t>(stream), 1, p);
+    p.clear_blocks = (int)clearing_blocks(rows, threads);
+    return launch_overlapped(gather_kernel<W>, dim3(p.token_blocks + p.clear_blocks), dim3(threads), 0, static_cast<cudaStream_t>(stream), 1, p);
   };
   if (whole_vectors(es, K, {x, out}, {ldx, ldo})) return run(uint4{});
   if (es == 4) return run(uint32_t{});
@@ -561,7 +557,8 @@ extern "C" sp24_status sp24_expert_combine_backward(sp24_dtype t, int64_t T, int
       p.K = K * es / (int64_t)sizeof(W);
       const unsigned threads = row_threads(p.K);
       p.token_blocks = (int)token_blocks(T);
-      const dim3 grid(p.token_blocks + clearing_blocks(rows, threads));
+      p.clear_blocks = (int)clearing_blocks(rows, threads);
+      const dim3 grid(p.token_blocks + p.clear_blocks);
       const cudaStream_t s = static_cast<cudaStream_t>(stream);
       if (p.K <= threads) return launch_overlapped(combine_backward_kernel<Type, W, 1>, grid, dim3(threads), 0, s, 1, p);
       if (p.K <= 2 * threads || sizeof(W) == 16) return launch_overlapped(combine_backward_kernel<Type, W, 2>, grid, dim3(threads), 0, s, 1, p);

@@ -86,6 +86,9 @@ struct GemmParams {
   // blocks of 128 rows of an expert
   const int32_t* offsets;
   int32_t experts, rows, table_bytes, meta_blocks;
+  // the weights' gradient: metadata of the weights (TCGEN05, 16-bit types), whose left out entries become zeros, or null, and its 128-column blocks
+  const uint8_t* keep;
+  int32_t keep_kb;
 };
 
 constexpr int kSwizzle128Atom32 = 1280;

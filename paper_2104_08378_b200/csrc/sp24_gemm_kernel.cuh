@@ -715,6 +715,18 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
     auto load_col_scale = [&](int col0) {  // lane e: that of column e of the box
       if (scaled) col_scale = col_scales[min(col0 + lane, N - 1)];
     };
+    // kKByExpert: which of the box's columns this lane's row of the weights keeps: the metadata of its 32 columns (two times four groups; see meta_offset)
+    uint32_t keep = 0;
+    auto load_keep = [&](int row0, int col0) {
+      if constexpr (GROUP == kKByExpert) {
+        if (p.keep) {
+          const int row = row0 + lane;
+          const uint8_t* at = p.keep + ((int64_t)(g.expert * p.meta_blocks + (row >> 7)) * p.keep_kb + (col0 >> 7)) * 2048 + 16 * (row & 7) + 2 * (row >> 3 & 1) +
+                              256 * (row >> 4 & 7) + 4 * (col0 >> 5 & 3);
+          if (row < M) keep = *reinterpret_cast<const uint16_t*>(at) | (uint32_t)*reinterpret_cast<const uint16_t*>(at + 128) << 16;
+        }
+      }
+    };
     auto load_scale = [&](int row0) {
       if (LINEAR) {
         const int row = min(row0 + lane, M - 1);
@@ -737,6 +749,7 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
       step(j, sc, WARPS / 4);
       const bool more = j < blocks;
       uint32_t o[W];
+      const uint32_t kept = keep;
       if (has_c) share_c(c);
       ptx::tmem_ld_wait(r);
       if (!more) hand_back();
@@ -756,6 +769,15 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
       if (GROUP == kKByExpert && no_sums) {
 #pragma unroll
         for (int e = 0; e < kCols; ++e) r[e] = instead;
+      }
+      if (GROUP == kKByExpert && p.keep) {
+#pragma unroll
+        for (int e = 0; e < kCols; e += 4) {
+          const uint32_t nibble = kept >> e & 15u, columns = 1u << (nibble & 3u) | 1u << (nibble >> 2);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!(columns >> i & 1u)) r[e + i] = 0;
+        }
       }
       bool again = false;
       if constexpr (LINEAR) {
@@ -781,6 +803,7 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
         ptx::tmem_ld_32x32b(t_acc + j * BLOCK_N + sc * kCols, r);
         if (j != j0) load_scale(row_q + j * kBlockM);
         load_col_scale(tile_col + sc * kCols);
+        load_keep(row_q + j * kBlockM, tile_col + sc * kCols);
       }
       if (has_c) fetch_c(c);
       store(o, row0, col0, again);
@@ -790,6 +813,7 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
     if (any) {
       load_scale(row_q + j * kBlockM);
       load_col_scale(tile_col + sc * kCols);
+      load_keep(row_q + j * kBlockM, tile_col + sc * kCols);
     }
     if (has_c && mine) {
 #pragma unroll

@@ -992,32 +992,31 @@ PyObject* expert_linear(PyObject*, PyObject* const* v, Py_ssize_t n) {
   }
 }
 
-// expert_linear_backward(addresses of sp24_expert_act_backward, of its workspace's size, of sp24_expert_linear_dx, of sp24_expert_linear_dw, of sp24_meta_bytes, of
-// sp24_apply_mask, workspaces, dy, pre, X, W, offsets, act, meta, bias, ws) -> (dX, dW, dbias)
+// expert_linear_backward(addresses of sp24_expert_act_backward, of its workspace's size, of sp24_expert_linear_dx, of sp24_expert_linear_dw, of sp24_meta_bytes,
+// workspaces, dy, pre, X, W, offsets, act, meta, bias, ws) -> (dX, dW, dbias)
 PyObject* expert_linear_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
-  if (n != 16 || at::impl::torch_function_mode_enabled()) return none();
+  if (n != 15 || at::impl::torch_function_mode_enabled()) return none();
   try {
     Matrix dy, z, x;
     Stack w;
     int with_bias;
-    const int act = act_code(v[12]);
-    if (act < 0 || !truth(v[14], &with_bias) || !dy.init(v[7], -1, -1, -1)) return none();
+    const int act = act_code(v[11]);
+    if (act < 0 || !truth(v[13], &with_bias) || !dy.init(v[6], -1, -1, -1)) return none();
     const int t = type_code(dy.t->scalar_type());
-    if ((t != SP24_F16 && t != SP24_BF16) || !w.init(v[10], t)) return none();
+    if ((t != SP24_F16 && t != SP24_BF16) || !w.init(v[9], t)) return none();
     const int64_t rows = dy.t->size(0), E = w.E, M = w.M, K = w.n;
     const void *offsets, *meta = nullptr;
-    if (rows < 1 || dy.t->size(1) != M || M % 16 != 0 || K % 16 != 0 || !x.init(v[9], rows, K, t) || v[11] == Py_None || !vector(v[11], E + 1, SP24_I32, SP24_I32, &offsets) ||
-        (act != SP24_ACT_NONE && !z.init(v[8], rows, M, t)) || (v[13] != Py_None && !expert_meta(v[13], v[4], t, E, M, K, &meta)))
+    if (rows < 1 || dy.t->size(1) != M || M % 16 != 0 || K % 16 != 0 || !x.init(v[8], rows, K, t) || v[10] == Py_None || !vector(v[10], E + 1, SP24_I32, SP24_I32, &offsets) ||
+        (act != SP24_ACT_NONE && !z.init(v[7], rows, M, t)) || (v[12] != Py_None && !expert_meta(v[12], v[4], t, E, M, K, &meta)))
       return none();
     const cudaStream_t stream = Stream().handle;
     void* ws;
     size_t ws_bytes;
-    if (!workspace(v[6], v[15], *dy.t, stream, &ws, &ws_bytes)) return none();
+    if (!workspace(v[5], v[14], *dy.t, stream, &ws, &ws_bytes)) return none();
     const auto act_fn = function<decltype(&sp24_expert_act_backward)>(v[0]);
     const auto act_bytes = function<decltype(&sp24_expert_act_backward_workspace_bytes)>(v[1]);
     const auto dx_fn = function<decltype(&sp24_expert_linear_dx)>(v[2]);
     const auto dw_fn = function<decltype(&sp24_expert_linear_dw)>(v[3]);
-    const auto mask_fn = function<decltype(&sp24_apply_mask)>(v[5]);
     Result rx{Py_None, {}}, rw{Py_None, {}}, rb{Py_None, {}};
     const int status = unlocked([&]() -> int {
       const auto options = dy.t->options();
@@ -1039,17 +1038,7 @@ PyObject* expert_linear_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
       if (st != SP24_OK) return st;
       d.lda = K;
       d.ldx = x.ld;
-      st = dw_fn(&d, pdzt, lddzt, x.p, (const int32_t*)offsets, rw.made.data_ptr(), ws, ws_bytes, stream);
-      if (st != SP24_OK || meta == nullptr) return st;
-      // (the metadata of an expert is whole blocks of 128 rows)
-      const size_t meta_bytes = function<decltype(&sp24_meta_bytes)>(v[4])((sp24_dtype)t, M, K, SP24_META_TCGEN05);
-      const int64_t at_once = M % 128 == 0 ? E : 1;
-      for (int64_t e = 0; e < E; e += at_once) {
-        char* const dw = (char*)rw.made.data_ptr() + e * M * K * 2;
-        st = mask_fn((sp24_dtype)t, at_once * M, K, dw, K, (const char*)meta + e * meta_bytes, SP24_META_TCGEN05, dw, K, stream);
-        if (st != SP24_OK) return st;
-      }
-      return st;
+      return dw_fn(&d, pdzt, lddzt, x.p, (const int32_t*)offsets, meta, rw.made.data_ptr(), ws, ws_bytes, stream);
     });
     if (status != SP24_OK) return PyLong_FromLong(status);
     return Py_BuildValue("(NNN)", rx.object(), rw.object(), rb.object());

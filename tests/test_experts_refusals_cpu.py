@@ -113,7 +113,7 @@ def gradient(which, ab=sp.F16, cd=sp.F16, E=4, M=64, K=64, rows=48, lda=64, ldx=
     d = ctypes.byref(sp.ExpertDesc(ab, cd, E, M, K, rows, lda, ldx, ldd, 0, 0, 1))
     if which == "dx":
         return sp.lib.sp24_expert_linear_dx(d, a, b, offsets, out, ws, ws_bytes, None)
-    return sp.lib.sp24_expert_linear_dw(d, a, lddzt, b, offsets, out, ws, ws_bytes, None)
+    return sp.lib.sp24_expert_linear_dw(d, a, lddzt, b, offsets, None, out, ws, ws_bytes, None)
 
 
 @pytest.mark.parametrize("which", ["dx", "dw"])
@@ -145,7 +145,7 @@ def test_act_backward(status, args):
 
 def test_nothing_to_describe():
     assert sp.lib.sp24_expert_linear(None, None, None, None, None, None, None, None, 0, None) == 1
-    assert sp.lib.sp24_expert_linear_dx(None, None, None, None, None, None, 0, None) == sp.lib.sp24_expert_linear_dw(None, None, 8, None, None, None, None, 0, None) == 1
+    assert sp.lib.sp24_expert_linear_dx(None, None, None, None, None, None, 0, None) == sp.lib.sp24_expert_linear_dw(None, None, 8, None, None, None, None, None, 0, None) == 1
 
 
 def refused(status, fn, *args, **kwargs):
