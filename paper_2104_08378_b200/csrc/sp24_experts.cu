@@ -266,43 +266,66 @@ struct Values {
   }
 };
 
-template <typename T, typename W>
-__global__ void __launch_bounds__(256) combine_kernel(const RowsParams p) {
-  constexpr int U = sizeof(W) == 16 ? 2 : 4;
-  __shared__ int32_t place[kMostChosen];
-  __shared__ float weight[kMostChosen];
+// U vectors of a row and kRows rows on the way at a time; the sum goes by the slots' order.
+template <typename T, typename W, int U>
+__global__ void __launch_bounds__(256, 4) combine_kernel(const RowsParams p) {
+  constexpr int kRows = 4;
   wait_for_stream();
+  const int lane = threadIdx.x & 31;
   for (int64_t t = blockIdx.x; t < p.T; t += gridDim.x) {
-    __syncthreads();
-    if (threadIdx.x < p.k) {
-      const int32_t r = p.position[t * p.k + threadIdx.x];
-      place[threadIdx.x] = r < p.rows ? r : -1;
-      weight[threadIdx.x] = p.weights ? p.weights[t * p.k + threadIdx.x] : 1.f;
-    }
-    __syncthreads();
-    // U columns of vectors at a time, their loads on the way together
-    for (int64_t c0 = threadIdx.x; c0 < p.K; c0 += U * blockDim.x) {
-      Values<T, W> sum[U], x[U];
+    int32_t place = lane < p.k ? p.position[t * p.k + lane] : -1;
+    if (place >= p.rows) place = -1;
+    const float weight = lane < p.k && p.weights ? p.weights[t * p.k + lane] : 1.f;
+    for (int64_t c0 = threadIdx.x; c0 - threadIdx.x < p.K; c0 += U * blockDim.x) {
+      Values<T, W> sum[U];
+      W rest[U] = {};
+      if (p.residual) {
+        const W* row = reinterpret_cast<const W*>(p.residual + t * p.ld_res);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (c0 + u * blockDim.x < p.K) rest[u] = row[c0 + u * blockDim.x];
+      }
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int n = 0; n < sum[u].N; ++n) sum[u].v[n] = 0.f;
-      auto add = [&](const uint8_t* row, float w) {
+      for (int i0 = 0; i0 < p.k; i0 += kRows) {
+        W y[kRows][U] = {};
+        int32_t r[kRows];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (c0 + u * blockDim.x < p.K) x[u].load(reinterpret_cast<const W*>(row) + c0 + u * blockDim.x);
+        for (int i = 0; i < kRows; ++i) {
+          r[i] = __shfl_sync(~0u, place, min(i0 + i, 31));
+          if (i0 + i >= p.k) r[i] = -1;
+          if (r[i] >= 0) {
+            const W* row = reinterpret_cast<const W*>(p.y + (int64_t)r[i] * p.ld_y);
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+            for (int u = 0; u < U; ++u)
+              if (c0 + u * blockDim.x < p.K) y[i][u] = row[c0 + u * blockDim.x];
+          }
+        }
 #pragma unroll
-          for (int n = 0; n < sum[u].N; ++n) sum[u].v[n] = fmaf(w, x[u].v[n], sum[u].v[n]);
-      };
-#pragma unroll 4
-      for (int i = 0; i < p.k; ++i)
-        if (place[i] >= 0) add(p.y + (int64_t)place[i] * p.ld_y, weight[i]);
-      if (p.residual) add(p.residual + t * p.ld_res, 1.f);
+        for (int i = 0; i < kRows; ++i) {
+          const float w = __shfl_sync(~0u, weight, min(i0 + i, 31));
+          if (r[i] < 0) continue;
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+          for (int u = 0; u < U; ++u) {
+            Values<T, W> x;
+            x.load(&y[i][u]);
+#pragma unroll
+            for (int n = 0; n < x.N; ++n) sum[u].v[n] = fmaf(w, x.v[n], sum[u].v[n]);
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (p.residual) {
+          Values<T, W> x;
+          x.load(&rest[u]);
+#pragma unroll
+          for (int n = 0; n < x.N; ++n) sum[u].v[n] += x.v[n];
+        }
         if (c0 + u * blockDim.x < p.K) sum[u].store(reinterpret_cast<W*>(p.out + t * p.ld_out) + c0 + u * blockDim.x);
+      }
     }
   }
 }
@@ -521,7 +544,8 @@ extern "C" sp24_status sp24_expert_combine(sp24_dtype t, int64_t T, int64_t K, i
     auto run = [&](auto word) {
       using W = decltype(word);
       p.K = K * es / (int64_t)sizeof(W);
-      return launch_overlapped(combine_kernel<Type, W>, dim3(token_blocks(T)), dim3(row_threads(p.K)), 0, static_cast<cudaStream_t>(stream), 1, p);
+      constexpr int U = sizeof(W) == 16 ? 2 : 4;  // (rows of 256 vectors: half as many threads with two each, more tokens to an SM)
+      return launch_overlapped(combine_kernel<Type, W, U>, dim3(token_blocks(T)), dim3(row_threads((p.K + U - 1) / U)), 0, static_cast<cudaStream_t>(stream), 1, p);
     };
     if (whole) return run(uint4{});
     if constexpr (sizeof(Type) == 4) return run(uint32_t{});

@@ -464,7 +464,7 @@ __device__ __noinline__ void route_again(const RouteParams& p, int64_t t, int la
 }
 
 template <typename T, int V, bool BIAS, bool GROUPS>
-__global__ void __launch_bounds__(32 * kChunkWarps) route_chunks_kernel(const RouteParams p) {
+__global__ void __launch_bounds__(32 * kChunkWarps, 7) route_chunks_kernel(const RouteParams p) {
   constexpr int R = kChunkRow<V>, S = V / 8, N = 16 / sizeof(T);
   __shared__ __align__(16) float rows_of[kChunkWarps][32 * R];
   __shared__ __align__(16) float bias_rows[BIAS ? 8 * R : 4];
@@ -520,8 +520,6 @@ __global__ void __launch_bounds__(32 * kChunkWarps) route_chunks_kernel(const Ro
   if (scores || total) {
     if (p.sigmoid) {
       error = 2.f * 1.5f * 0x1p-22f;  // (as in route_token)
-#pragma unroll
-      for (int v = 0; v < V; ++v) c[v] = reciprocal_fast(1.f + exp2_fast(-kLog2e * l[v]));
     } else {
       float sum = 0.f;
 #pragma unroll
@@ -543,7 +541,10 @@ __global__ void __launch_bounds__(32 * kChunkWarps) route_chunks_kernel(const Ro
       if (BIAS) b = *reinterpret_cast<const float4*>(bias_rows + j * R + v);
       const float add[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-      for (int n = 0; n < 4; ++n) c[v + n] = fmaxf(c[v + n] + fmaf(l[v + n], 0.f, add[n]), -INFINITY);
+      for (int n = 0; n < 4; ++n) {
+        if (p.sigmoid) c[v + n] = reciprocal_fast(1.f + exp2_fast(-kLog2e * l[v + n]));
+        c[v + n] = fmaxf(c[v + n] + fmaf(l[v + n], 0.f, add[n]), -INFINITY);
+      }
     }
     near = error + 0x1p-22f * (2.f + 2.f * bias_size);
   }
@@ -750,6 +751,96 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_backward_kernel(const 
   }
 }
 
+// The same for up to 256 experts in whole vectors and up to eight slots: a token to eight lanes, lane j with the j-th eighth of the experts and the j-th slot.
+// (Us, device, bf16 16384 x 128, 4 slots, softmax over all: a warp to a token 8.0, this MEASURED.)
+template <typename T, int V>
+__global__ void __launch_bounds__(32 * kChunkWarps) route_backward_chunks_kernel(const RouteBackwardParams p) {
+  constexpr int N = 16 / sizeof(T);
+  const int lane = threadIdx.x & 31, j = lane & 7, chunk = p.E / 8;
+  wait_for_stream();
+  const int64_t t = ((int64_t)blockIdx.x * kChunkWarps + (threadIdx.x >> 5)) * 4 + (lane >> 3);
+  const bool live = t < p.T, slot = live && j < p.k;
+  const T* row = static_cast<const T*>(p.logits) + (live ? t : 0) * p.ld;
+  const bool full = !p.renorm && !p.sigmoid;
+  int e = slot ? p.experts[t * p.k + j] : -1;
+  if (e >= p.E) e = -1;
+  const float g = e >= 0 ? p.scale * p.dweights[t * p.k + j] : 0.f;
+  auto over_token = [&](float v, auto op) {
+#pragma unroll
+    for (int i = 1; i < 8; i <<= 1) v = op(v, __shfl_xor_sync(~0u, v, i));
+    return v;
+  };
+  auto larger = [](float a, float b) { return fmaxf(a, b); };
+  auto sum_of = [](float a, float b) { return a + b; };
+  float l[V], top = -INFINITY, inv = 0.f;
+  if (full) {
+#pragma unroll
+    for (int v = 0; v < V; v += N) {
+      Pairs<T> f = {};
+      if (v < chunk && live) unpack<T>(*reinterpret_cast<const uint4*>(row + j * chunk + v), f);
+#pragma unroll
+      for (int n = 0; n < N / 2; ++n) {
+        l[v + 2 * n] = v < chunk ? f[n].x : -INFINITY;
+        l[v + 2 * n + 1] = v < chunk ? f[n].y : -INFINITY;
+      }
+    }
+  }
+  const float lm = e >= 0 ? to_float(row[e]) : -INFINITY;
+  if (full) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) top = fmaxf(top, l[v]);
+    top = over_token(top, larger);
+    const float base = fmaxf(top, -FLT_MAX);
+    float sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      l[v] = expf(l[v] - base);
+      sum += l[v];
+    }
+    sum = over_token(sum, sum_of);
+    inv = sum == 0.f ? 0.f : 1.f / sum;  // (nothing but -infinity: no gradient)
+    top = base;
+  }
+  float d = 0.f, along = 0.f;
+  if (p.renorm) {
+    const float z = e < 0 ? -INFINITY : (p.sigmoid ? fminf(lm, 0.f) - log1pf(expf(-fabsf(lm))) : lm);
+    const float zmax = over_token(z, larger), w = e < 0 ? 0.f : expf(z - zmax), all = over_token(w, sum_of), u = e < 0 ? 0.f : w / all;
+    d = u * (g - over_token(u * g, sum_of));
+    if (p.sigmoid) d *= 1.f / (1.f + expf(lm));
+  } else if (p.sigmoid) {
+    d = e < 0 ? 0.f : g * (1.f / (1.f + expf(-lm))) * (1.f / (1.f + expf(lm)));
+  } else {
+    along = over_token(e < 0 ? 0.f : expf(lm - top) * inv * g, sum_of);
+    d = g;
+  }
+  float dl[V] = {};
+  for (int i = 0; i < p.k; ++i) {
+    const int at = __shfl_sync(~0u, e, (lane & 24) + i) - j * chunk;
+    const float x = __shfl_sync(~0u, d, (lane & 24) + i);
+    if (at >= 0 && at < chunk) {
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (v == at) dl[v] += x;
+    }
+  }
+  if (full) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) dl[v] = l[v] * inv * (dl[v] - along);
+  }
+  if (!live) return;
+  T* out = static_cast<T*>(p.dlogits) + t * p.ldd + j * chunk;
+#pragma unroll
+  for (int v = 0; v < V; v += N) {
+    Pairs<T> f;
+#pragma unroll
+    for (int n = 0; n < N / 2; ++n) f[n] = make_float2(dl[v + 2 * n], dl[v + 2 * n + 1]);
+    if (v < chunk) *reinterpret_cast<uint4*>(out + v) = pack<T>(f);
+  }
+}
+
+// whether an eighth of the experts is whole vectors, and there is a lane to each slot
+bool whole_chunks(int64_t E, int64_t es, int k) { return E <= 256 && E % 8 == 0 && E / 8 * es % 16 == 0 && k <= 8; }
+
 // f(number of experts that a lane has, as a type)
 template <typename F>
 sp24_status with_experts(int64_t E, F&& f) {
@@ -798,8 +889,7 @@ extern "C" sp24_status sp24_route(sp24_dtype t, int64_t T, int64_t E, const void
   p.logits = logits; p.bias = bias; p.weights = weights; p.experts = experts;
   return with_float_type(t, [&](auto type) {
     using Type = typename decltype(type)::type;
-    // whole vectors of an eighth of the experts, a lane to each of the chosen
-    const bool chunks = E <= 256 && E % 8 == 0 && E / 8 * (int64_t)sizeof(Type) % 16 == 0 && k <= 8 && groups <= 8 && 8 % groups == 0 && aligned16(logits) &&
+    const bool chunks = whole_chunks(E, sizeof(Type), k) && groups <= 8 && 8 % groups == 0 && aligned16(logits) &&
                         (T == 1 || ld * (int64_t)sizeof(Type) % 16 == 0) && T < int64_t(1) << 35;
     if (chunks) {
       auto run = [&](auto v) {
@@ -840,6 +930,16 @@ extern "C" sp24_status sp24_route_backward(sp24_dtype t, int64_t T, int64_t E, c
   p.logits = logits; p.dlogits = dlogits; p.dweights = dweights; p.experts = experts;
   return with_float_type(t, [&](auto type) {
     using Type = typename decltype(type)::type;
+    const int64_t es = sizeof(Type);
+    if (whole_chunks(E, es, k) && aligned16(logits) && aligned16(dlogits) && (T == 1 || (ld * es % 16 == 0 && ldd * es % 16 == 0)) && T < int64_t(1) << 35) {
+      auto run = [&](auto v) {
+        return launch_overlapped(route_backward_chunks_kernel<Type, decltype(v)::value>, dim3((unsigned)((T + kChunkTokens - 1) / kChunkTokens)),
+                                 dim3(32 * kChunkWarps), 0, static_cast<cudaStream_t>(stream), 1, p);
+      };
+      if (E <= 64) return run(std::integral_constant<int, 8>{});
+      if (E <= 128) return run(std::integral_constant<int, 16>{});
+      return run(std::integral_constant<int, 32>{});
+    }
     return with_experts(E, [&](auto v) {
       return launch_overlapped(route_backward_kernel<Type, decltype(v)::value>, dim3(route_blocks(T, 8)), dim3(32 * kRouteWarps),
                                (size_t)(kRouteWarps * E * 4), static_cast<cudaStream_t>(stream), 1, p);
