@@ -463,8 +463,39 @@ __device__ __noinline__ void route_again(const RouteParams& p, int64_t t, int la
   route_token<T, 8, BIAS, GROUPS>(p, t, lane, x, mine_of, chosen, values);
 }
 
+// s + b of one expert in FP64 (sigmoid)
+template <typename T>
+__device__ __noinline__ double exact_sigmoid(const RouteParams& p, const T* row, int e) {
+  return 1.0 / (1.0 + exp(-(double)to_float(row[e]))) + (p.bias ? (double)p.bias[e] : 0.0);
+}
+
+// Whether the lane's group stays, by FP64: the sum of the two largest of the group's `n` candidates in this lane (places in the lane's chunk) and its other lanes'.
+template <typename T>
+__device__ __noinline__ bool exact_group(const RouteParams& p, const T* row, int lane, const float* places, int n) {
+  const int j = lane & 7, chunk = p.E / 8, lanes = 8 / p.groups;
+  double one = -INFINITY, two = -INFINITY;
+  const int most = __reduce_max_sync(~0u, n);
+  for (int i = 0; i < most; ++i) {
+    const double x = i < n ? exact_sigmoid(p, row, j * chunk + __float_as_int(places[i])) : -INFINITY;
+    two = fmax(two, fmin(one, x));
+    one = fmax(one, x);
+  }
+  for (int i = 1; i < lanes; i <<= 1) {
+    const double a = __shfl_xor_sync(~0u, one, i), b = __shfl_xor_sync(~0u, two, i);
+    two = fmax(fmin(one, a), fmax(two, b));
+    one = fmax(one, a);
+  }
+  const double value = two > -INFINITY ? one + two : one;
+  int before = 0;
+  for (int i = lanes; i < 8; i += lanes) {
+    const double other = __shfl_xor_sync(~0u, value, i);
+    before += other > value || (other == value && (j ^ i) < j);
+  }
+  return before < p.top_groups;
+}
+
 template <typename T, int V, bool BIAS, bool GROUPS>
-__global__ void __launch_bounds__(32 * kChunkWarps, 7) route_chunks_kernel(const RouteParams p) {
+__global__ void __launch_bounds__(32 * kChunkWarps) route_chunks_kernel(const RouteParams p) {
   constexpr int R = kChunkRow<V>, S = V / 8, N = 16 / sizeof(T);
   __shared__ __align__(16) float rows_of[kChunkWarps][32 * R];
   __shared__ __align__(16) float bias_rows[BIAS ? 8 * R : 4];
@@ -576,7 +607,18 @@ __global__ void __launch_bounds__(32 * kChunkWarps, 7) route_chunks_kernel(const
     kept = before < p.top_groups;
     if (scores && p.top_groups < p.groups) {
       const float worst = -over_token(kept ? -value : -INFINITY, larger), next = over_token(kept ? -INFINITY : value, larger);
-      again |= next > -INFINITY && worst - next <= 2.f * error + 0x1p-21f * (4.f + 4.f * bias_size);
+      const bool doubt = next > -INFINITY && worst - next <= 2.f * error + 0x1p-21f * (4.f + 4.f * bias_size);
+      if (!(two && p.sigmoid)) {
+        again |= doubt;
+      } else if (__any_sync(~0u, doubt && !again)) {
+        // once more in FP64, with what is not clearly behind the second of the group
+        int n = 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          if (doubt && c[v] > -INFINITY && !(c[v] < second - near)) rows_of[warp][lane * R + n++] = __int_as_float(v);
+        const bool exact = exact_group(p, row, lane, rows_of[warp] + lane * R, n);
+        if (doubt) kept = exact;
+      }
     }
   }
   // what is chosen by, in shared memory, and the largest of each eight of a lane's
@@ -601,7 +643,7 @@ __global__ void __launch_bounds__(32 * kChunkWarps, 7) route_chunks_kernel(const
   int chosen = -1;  // lane i of the token: the i-th
   float last = INFINITY;
   int last_expert = 0;
-  bool open = BIAS;  // whether what comes next is clearly behind the k chosen is still to be seen: after ties it takes more than one round
+  bool followed = false, open = BIAS;  // whether what comes next is clearly behind the k chosen is still to be seen: after ties it takes more than one round
   for (int i = 0; i < p.k || (BIAS && i < p.k + 8 && __any_sync(~0u, open)); ++i) {
     const float m = over_token(lane_best, larger);
     const uint32_t holders = __ballot_sync(~0u, lane_best == m) >> (lane & 24) & 0xffu;
@@ -622,8 +664,9 @@ __global__ void __launch_bounds__(32 * kChunkWarps, 7) route_chunks_kernel(const
     if (a.y == lane_best) n = 1;
     if (a.x == lane_best) n = 0;
     const int place = 8 * at + n;
-    int e = __shfl_sync(~0u, j * chunk + place, w);
+    const int e = __shfl_sync(~0u, j * chunk + place, w);
     const bool some = m > -INFINITY;
+    int put = e;
     if (lane == w && some) {
       mine[place] = -INFINITY;
       a = *reinterpret_cast<const float4*>(mine + 8 * at);
@@ -636,15 +679,28 @@ __global__ void __launch_bounds__(32 * kChunkWarps, 7) route_chunks_kernel(const
     }
     if (BIAS && i > 0) {
       const bool close = some && last - m <= near && (i < p.k || open);
-      bool doubt = close;
-      if (__any_sync(~0u, close) && close)  // (the same logit under the same bias: a tie, whatever the arithmetic)
-        doubt = !(to_float(row[e]) == to_float(row[last_expert]) && p.bias[e] == p.bias[last_expert]);
-      again |= doubt;
-      if (i >= p.k) open = close && !doubt;
+      bool doubt = false;
+      if (__any_sync(~0u, close)) {
+        // (the same logit under the same bias: a tie, whatever the arithmetic)
+        doubt = close && !(to_float(row[e]) == to_float(row[last_expert]) && p.bias[e] == p.bias[last_expert]);
+        if (p.sigmoid && __any_sync(~0u, doubt)) {  // the two in FP64, by the token's even and odd lanes
+          const double mine = exact_sigmoid(p, row, j & 1 ? e : last_expert), other = __shfl_xor_sync(~0u, mine, 1);
+          const double a = j & 1 ? other : mine, b = j & 1 ? mine : other;
+          if (doubt && !followed && (b > a || (b == a && e < last_expert))) {
+            if (j == i - 1) chosen = e;
+            put = last_expert;
+          }
+          again |= doubt && followed;  // (the one before followed as closely: it is not between these two alone)
+        } else {
+          again |= doubt;
+        }
+      }
+      followed = close;
+      if (i >= p.k) open = close;
     }
     last = m;
-    last_expert = e;
-    if (j == i && i < p.k) chosen = some ? e : -1;
+    last_expert = put;
+    if (j == i && i < p.k) chosen = some ? put : -1;
   }
   again |= open;
   // weights: lane i's

@@ -69,6 +69,24 @@ def test_close_scores_are_told_apart_in_64_bits(sp):
         check(sp, logits, 6, score=score, bias=torch.full((40,), -8.0, device="cuda"), groups=4, top_groups=2, group_score="top2")
 
 
+@pytest.mark.parametrize("E", [64, 128, 256, 40])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_pairs_and_triples_of_close_scores(sp, score, E):
+    """Steps of 0.05 with one, two or three logits each, some equal and some a unit in the last place apart, in any places of the row."""
+    g = torch.Generator(device="cuda").manual_seed(E)
+    T = 400
+    level = (torch.arange(E, device="cuda") // 2).float() * 0.05
+    level[2::7] = level[1::7][:len(level[2::7])]
+    units = torch.randint(0, 3, (T, E), generator=g, device="cuda", dtype=torch.int32)
+    logits = ((level + 0.0173).expand(T, E).contiguous().view(torch.int32) + units).view(torch.float32)
+    logits = torch.gather(logits, 1, torch.rand((T, E), generator=g, device="cuda").argsort(1))
+    for bias in (0.5, -3.0):
+        b = torch.full((E,), bias, device="cuda")
+        check(sp, logits, 8, score=score, bias=b)
+        check(sp, logits, 3, score=score, bias=b, groups=4, top_groups=2, group_score="top2")
+        check(sp, logits, 3, score=score, groups=4, top_groups=3, group_score="top2")
+
+
 def test_masked_experts_and_tokens(sp):
     for t in ("bf16", "f32"):
         logits = rand((40, 48), t, 5, 1.5)
