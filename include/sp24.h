@@ -455,8 +455,8 @@ sp24_status sp24_act_backward(sp24_dtype t, sp24_act act, int64_t rows, int64_t 
  *   compared as real numbers: computed in FP32, and in FP64 where two are too close to tell.
  *   weights[t, i] = scale * s of the i-th chosen, with renorm != 0 divided by the sum of the chosen s (their sum is then scale).
  *   A logit of -infinity or NaN, and a bias of -infinity or NaN, is never chosen; where that leaves fewer than k, the rest has
- *   experts -1 and weights 0 (a token without any: a padded batch).  A NaN among the logits, and with softmax +infinity, makes
- *   the token's other weights NaN.
+ *   experts -1 and weights 0 (a token without any: a padded batch).  A NaN among the logits makes the weights of what the token
+ *   chooses NaN; so does +infinity with softmax, where under a bias or SP24_GROUP_TOP2 nothing is chosen.
  *   t: SP24_F16, SP24_BF16 or SP24_F32.  T >= 0 tokens, 1 <= E <= 1024, ld >= E, any alignment that the types have.
  *   1 <= k <= min(32, top_groups * E / groups), groups <= 32.  bias: E floats.  weights: T x k floats, experts: T x k int32. */
 typedef enum { SP24_SCORE_SOFTMAX = 0, SP24_SCORE_SIGMOID = 1 } sp24_score;

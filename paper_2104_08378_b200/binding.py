@@ -897,7 +897,8 @@ def _route_backward(dweights, logits, experts, score, renorm, scale, out):
     ld = _matrix(logits, where)
     T, E = logits.shape
     _refuse(score not in SCORE, ERR_UNSUPPORTED, where)
-    _slots(experts, where, logits, torch.int32, (T, experts.shape[-1]))
+    _slots(experts, where, logits, torch.int32)
+    _refuse(experts.shape[0] != T, ERR_SHAPE, where)
     _slots(dweights, where, logits, torch.float32, experts.shape)
     dlogits = logits.new_empty((T, E)) if out is None else out
     ldd = _matrix(dlogits, where, logits, logits.shape, logits.dtype)
@@ -929,7 +930,8 @@ def _expert_order(experts, E, align):
 
 
 def _check_order(order: ExpertOrder, T: int, where: str, like: torch.Tensor):
-    _slots(order.position, where, like, torch.int32, (T, order.position.shape[-1]))
+    _slots(order.position, where, like, torch.int32)
+    _refuse(order.position.shape[0] != T or order.source.dim() != 1, ERR_SHAPE, where)
     _vector(order.source, order.source.shape[0], where, like, (torch.int32,))
 
 
@@ -976,6 +978,7 @@ def _expert_combine(y, order, weights, residual, out):
     t = _float_code(y, where)
     ldy = _matrix(y, where)
     rows, K = y.shape
+    _slots(order.position, where, y, torch.int32)
     T, k = order.position.shape
     _check_order(order, T, where, y)
     _refuse(order.source.shape[0] != rows, ERR_SHAPE, where)

@@ -221,7 +221,8 @@ __global__ void __launch_bounds__(256) expert_sums_kernel(const ActGradParams p)
   __shared__ float over[4][kTile];
   wait_for_stream();
   const int x = threadIdx.x % kTile, y = threadIdx.x / kTile;
-  const int64_t row0 = (int64_t)blockIdx.y * kTile, end = min(p.rows, row0 + kTile), c = (int64_t)blockIdx.x * kTile + x;
+  const int64_t col_tiles = (p.cols + kTile - 1) / kTile, tile = blockIdx.x / col_tiles;
+  const int64_t row0 = tile * kTile, end = min(p.rows, row0 + kTile), c = blockIdx.x % col_tiles * kTile + x;
   for (int e = expert_of_row(p, row0); e < p.experts; ++e) {
     int64_t lo, hi;
     rows_of_expert(p, e, lo, hi);
@@ -240,7 +241,7 @@ __global__ void __launch_bounds__(256) expert_sums_kernel(const ActGradParams p)
       }
     over[y][x] = sum;
     __syncthreads();
-    if (y == 0 && c < p.cols) p.partial[((int64_t)blockIdx.y + e) * p.cols + c] = (over[0][x] + over[1][x]) + (over[2][x] + over[3][x]);
+    if (y == 0 && c < p.cols) p.partial[(tile + e) * p.cols + c] = (over[0][x] + over[1][x]) + (over[2][x] + over[3][x]);
     __syncthreads();
   }
 }
@@ -344,7 +345,7 @@ extern "C" sp24_status sp24_expert_act_backward(sp24_dtype t, sp24_act act, int6
                      whole_rows(dz, rows, lddz, 2, 16) && (!dzt || (whole_rows(dzt, M, lddzt, 2, 16) && lddzt >= (rows + 7) / 8 * 8));
   const bool wide = whole && (rows + 127) / 128 * ((M + 127) / 128) >= 2 * sm_count();
   const int64_t edge = wide ? 2 * kTile : kTile, row_tiles = (rows + edge - 1) / edge, col_tiles = (M + edge - 1) / edge;
-  SP24_RETURN_IF(row_tiles * col_tiles > 0x7fffffff || (dbias && !whole && row_tiles > 65535), SP24_ERR_SHAPE);
+  SP24_RETURN_IF(row_tiles * col_tiles > 0x7fffffff, SP24_ERR_SHAPE);
   sp24_status st = check_arch();
   SP24_RETURN_IF(st != SP24_OK, st);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -364,7 +365,7 @@ extern "C" sp24_status sp24_expert_act_backward(sp24_dtype t, sp24_act act, int6
         sp24_status done = SP24_OK;
         if (dz || dzt) done = launch_overlapped(act_grad_kernel<T, kAct>, grid, dim3(256), 0, s, 1, q);
         if (done != SP24_OK || !dbias) return done;
-        return launch_overlapped(expert_sums_kernel<T, kAct>, dim3((unsigned)col_tiles, (unsigned)row_tiles), dim3(256), 0, s, 1, p);
+        return launch_overlapped(expert_sums_kernel<T, kAct>, grid, dim3(256), 0, s, 1, p);
       });
     });
     SP24_RETURN_IF(st != SP24_OK || !dbias, st);
