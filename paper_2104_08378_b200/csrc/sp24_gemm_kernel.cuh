@@ -716,7 +716,12 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
       if (scaled) col_scale = col_scales[min(col0 + lane, N - 1)];
     };
     // kKByExpert: which of the box's columns this lane's row of the weights keeps: the metadata of its 32 columns (two times four groups; see meta_offset)
-    uint32_t keep = 0;
+    // (lane i of 0..15 and i + 16: the byte-permute selectors that copy the two of a group's columns that nibble i names, 4 = a byte of zeros)
+    uint32_t keep = 0, selectors = 0;
+    if (GROUP == kKByExpert) {
+      const uint32_t columns = 1u << (lane & 3) | 1u << (lane >> 2 & 3);
+      selectors = (columns & 1u ? 0x10u : 0x44u) | (columns & 2u ? 0x3200u : 0x4400u) | (columns & 4u ? 0x100000u : 0x440000u) | (columns & 8u ? 0x32000000u : 0x44000000u);
+    }
     auto load_keep = [&](int row0, int col0) {
       if constexpr (GROUP == kKByExpert) {
         if (p.keep) {
@@ -770,15 +775,6 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
 #pragma unroll
         for (int e = 0; e < kCols; ++e) r[e] = instead;
       }
-      if (GROUP == kKByExpert && p.keep) {
-#pragma unroll
-        for (int e = 0; e < kCols; e += 4) {
-          const uint32_t nibble = kept >> e & 15u, columns = 1u << (nibble & 3u) | 1u << (nibble >> 2);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (!(columns >> i & 1u)) r[e + i] = 0;
-        }
-      }
       bool again = false;
       if constexpr (LINEAR) {
         if (scaled) {
@@ -798,6 +794,16 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
         pack_row<CS>(r, p.cd_type, o);
       } else {
         compute_row<KIND, CS, kCols>(r, c, has_c, p, scale, bias, o);
+      }
+      if constexpr (GROUP == kKByExpert) {
+        if (p.keep) {  // a nibble's selectors for its group's two words, from the lane of its number (five instructions a group; by bits 14: 54 -> 74 us where K is short)
+#pragma unroll
+          for (int e = 0; e < kCols / 4; ++e) {
+            const uint32_t s = __shfl_sync(~0u, selectors, (int)(kept >> (4 * e)));
+            o[2 * e] = __byte_perm(o[2 * e], 0, s);
+            o[2 * e + 1] = __byte_perm(o[2 * e + 1], 0, s >> 16);
+          }
+        }
       }
       if (more) {
         ptx::tmem_ld_32x32b(t_acc + j * BLOCK_N + sc * kCols, r);
