@@ -171,30 +171,28 @@ __global__ void __launch_bounds__(1024) order_kernel(const OrderParams p) {
 }
 
 // ---- rows -------------------------------------------------------------------------------------------------------
-// A block has a token (or several one after the other), its threads the vectors of the row, at most kAhead of them in registers at a time; the
-// blocks before those look for rows without a slot and clear them.  A vector is 16 bytes, or one element of the type where rows are not made of
-// whole ones at 16-byte boundaries.
+// A block has a token, or several one after the other, its threads the row's vectors of 16 bytes; blocks before those look for rows without a slot and clear them.
+// WHOLE: rows are whole vectors at 16-byte boundaries.  Else the vectors lie at the boundaries of the row that is written, and what is read is made of the two
+// words that it lies in (load_words).  Bound by HBM: us, device, and of the floor at the copy's rate, e4m3 8192 x 4096 to 8 rows each 51 (91 %); bf16 8192 x 4096, 4
+// rows each: gathering 56 (91 %), sums 53 (97 %), the sums' gradient 101 (91 %);
+// bf16 8192 x 4095, where every row lies otherwise: 62, 88, 152 (by elements 117, 97, 175).
 struct RowsParams {
-  int64_t T, K, rows;        // K in vectors
-  int64_t ld_in, ld_out, ld_y, ld_res;  // bytes
+  int64_t T, K, rows;
+  int64_t ld_in, ld_out, ld_y, ld_res;  // elements
   int k;
   int clear_blocks, token_blocks;
   const int32_t *position, *source;
-  const uint8_t *in, *y, *residual;
-  uint8_t* out;
+  const void *in, *y, *residual;
+  void* out;
   const float* weights;  // gather: scales
-  float* sums;           // gather: the rows' scales
+  float* sums;           // gather: the rows' scales; the sums' gradient: that of the weights
 };
 
-template <typename W>
-__device__ __forceinline__ W zero_vector() {
-  if constexpr (sizeof(W) == 16) return make_uint4(0, 0, 0, 0);
-  else return W(0);
-}
-
 // The first p.clear_blocks blocks.  A warp looks at 32 rows at a time, as far apart as there are warps: rows without a slot come in long runs, behind the last expert.
-template <typename W>
-__device__ void clear_rows(const RowsParams& p, int64_t ld, uint8_t* out, float* scale) {
+// (With a block to 256 rows in a row, 1216 rows of 4096 bf16 values, 960 of them empty, took 27 us; 5.5.)
+template <bool WHOLE, typename E>
+__device__ void clear_rows(const RowsParams& p, float* scale) {
+  constexpr int N = kVector<E>;
   const int lane = threadIdx.x & 31;
   const int64_t warps = (int64_t)p.clear_blocks * (blockDim.x >> 5), warp = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
   for (int64_t r0 = warp; r0 < p.rows; r0 += 32 * warps) {
@@ -203,22 +201,25 @@ __device__ void clear_rows(const RowsParams& p, int64_t ld, uint8_t* out, float*
     if (empty && scale) scale[r] = 0.f;
     uint32_t left = __ballot_sync(~0u, empty);
     while (left) {
-      W* row = reinterpret_cast<W*>(out + (r0 + (__ffs(left) - 1) * warps) * ld);
+      E* row = static_cast<E*>(p.out) + (r0 + (__ffs(left) - 1) * warps) * p.ld_out;
       left &= left - 1;
-      for (int64_t c = lane; c < p.K; c += 32) row[c] = zero_vector<W>();
+      const int shift = WHOLE ? 0 : shift_of<E, N>(row);
+      for (int c = lane; c * N - shift < p.K; c += 32) store_vector<WHOLE>(row, c, (int)p.K, shift, make_uint4(0, 0, 0, 0));
     }
   }
 }
 
-// A token's row is read once and written to its k places.
-template <typename W>
+// A token's row is read once (again from the L1 where rows lie between boundaries) and written to its k places.
+template <typename E, bool WHOLE>
 __global__ void __launch_bounds__(256) gather_kernel(const RowsParams p) {
+  constexpr int N = kVector<E>;
   __shared__ int32_t place[kMostChosen];
   wait_for_stream();
   if (blockIdx.x < p.clear_blocks) {
-    clear_rows<W>(p, p.ld_out, p.out, p.sums);
+    clear_rows<WHOLE, E>(p, p.sums);
     return;
   }
+  const int K = (int)p.K;
   for (int64_t t = blockIdx.x - p.clear_blocks; t < p.T; t += p.token_blocks) {
     __syncthreads();
     if (threadIdx.x < p.k) {
@@ -228,145 +229,150 @@ __global__ void __launch_bounds__(256) gather_kernel(const RowsParams p) {
       if (p.sums && r >= 0) p.sums[r] = p.weights[t];
     }
     __syncthreads();
-    const W* row = reinterpret_cast<const W*>(p.in + t * p.ld_in);
-    for (int64_t c = threadIdx.x; c < p.K; c += blockDim.x) {
-      const W v = row[c];
-      for (int i = 0; i < p.k; ++i)
-        if (place[i] >= 0) reinterpret_cast<W*>(p.out + (int64_t)place[i] * p.ld_out)[c] = v;
+    const E* row = static_cast<const E*>(p.in) + t * p.ld_in;
+    if constexpr (WHOLE) {
+      for (int c = threadIdx.x; c * N < K; c += blockDim.x) {
+        const uint4 v = reinterpret_cast<const uint4*>(row)[c];
+        for (int i = 0; i < p.k; ++i)
+          if (place[i] >= 0) store_vector<true>(static_cast<E*>(p.out) + place[i] * p.ld_out, c, K, 0, v);
+      }
+    } else {
+      // (place after place: four of them together took 81 us where this takes 62, bf16 8192 x 4095, 4 rows each)
+      for (int i = 0; i < p.k; ++i) {
+        if (place[i] < 0) continue;
+        E* out = static_cast<E*>(p.out) + place[i] * p.ld_out;
+        const int shift = shift_of<E, N>(out);
+#pragma unroll 2
+        for (int c = threadIdx.x; c * N - shift < K; c += blockDim.x) store_vector<false>(out, c, K, shift, load_vector<false>(row, c, K, shift));
+      }
     }
   }
 }
 
-// Values of a vector as FP32 and back
-template <typename T, typename W>
-struct Values {
-  static constexpr int N = sizeof(W) / sizeof(T);
-  float v[N];
-  __device__ __forceinline__ void load(const W* at) {
-    if constexpr (sizeof(W) == 16) {
-      Pairs<T> f;
-      unpack<T>(*reinterpret_cast<const uint4*>(at), f);
-#pragma unroll
-      for (int i = 0; i < N / 2; ++i) {
-        v[2 * i] = f[i].x;
-        v[2 * i + 1] = f[i].y;
-      }
-    } else {
-      v[0] = to_float(*reinterpret_cast<const T*>(at));
-    }
+// What a vector of a row is made of, and the vector: of FP32 rows between boundaries its four elements (us, 2048 x 4095, 4 rows each: two words and selects 48, 31), else load_words.
+template <bool WHOLE, typename T>
+using Parts = std::conditional_t<!WHOLE && sizeof(T) == 4, uint4, Words<WHOLE>>;
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void load_parts(Parts<WHOLE, T>& to, const T* row, int i, int K, int shift) {
+  if constexpr (!WHOLE && sizeof(T) == 4) {
+    const int e = 4 * i - shift;
+    const uint32_t* at = reinterpret_cast<const uint32_t*>(row) + e;
+    to.x = (unsigned)e < (unsigned)K ? at[0] : 0u;
+    to.y = (unsigned)(e + 1) < (unsigned)K ? at[1] : 0u;
+    to.z = (unsigned)(e + 2) < (unsigned)K ? at[2] : 0u;
+    to.w = (unsigned)(e + 3) < (unsigned)K ? at[3] : 0u;
+  } else {
+    load_words<WHOLE>(to, row, i, K, shift);
   }
-  __device__ __forceinline__ void store(W* at) const {
-    if constexpr (sizeof(W) == 16) {
-      Pairs<T> f;
-#pragma unroll
-      for (int i = 0; i < N / 2; ++i) f[i] = make_float2(v[2 * i], v[2 * i + 1]);
-      *reinterpret_cast<uint4*>(at) = pack<T>(f);
-    } else {
-      *reinterpret_cast<T*>(at) = round_to<T>(v[0]);
-    }
-  }
-};
+}
+template <bool WHOLE, typename T>
+__device__ __forceinline__ uint4 from_parts(const Parts<WHOLE, T>& from, const T* row, int i, int K, int shift) {
+  if constexpr (!WHOLE && sizeof(T) == 4) return from;
+  else return vector_of<WHOLE>(from, row, i, K, shift);
+}
 
-// U vectors of a row and kRows rows on the way at a time; the sum goes by the slots' order.
-template <typename T, typename W, int U>
+// U vectors of a row and four rows on the way at a time; the sum goes by the slots' order.
+template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(256, 4) combine_kernel(const RowsParams p) {
-  constexpr int kRows = 4;
+  constexpr int kRows = 4, U = WHOLE ? 2 : 1, N = kVector<T>;
   wait_for_stream();
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, K = (int)p.K;
   for (int64_t t = blockIdx.x; t < p.T; t += gridDim.x) {
     int32_t place = lane < p.k ? p.position[t * p.k + lane] : -1;
     if (place >= p.rows) place = -1;
     const float weight = lane < p.k && p.weights ? p.weights[t * p.k + lane] : 1.f;
-    for (int64_t c0 = threadIdx.x; c0 - threadIdx.x < p.K; c0 += U * blockDim.x) {
-      Values<T, W> sum[U];
-      W rest[U] = {};
-      if (p.residual) {
-        const W* row = reinterpret_cast<const W*>(p.residual + t * p.ld_res);
+    T* out = static_cast<T*>(p.out) + t * p.ld_out;
+    const int shift = WHOLE ? 0 : shift_of<T, N>(out);
+    const T* residual = p.residual ? static_cast<const T*>(p.residual) + t * p.ld_res : nullptr;
+    for (int c0 = 0; c0 * N - shift < K; c0 += U * blockDim.x) {
+      const int c = c0 + threadIdx.x;
+      Parts<WHOLE, T> rest[U] = {};
+      if (residual) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (c0 + u * blockDim.x < p.K) rest[u] = row[c0 + u * blockDim.x];
+        for (int u = 0; u < U; ++u) load_parts<WHOLE, T>(rest[u], residual, c + u * blockDim.x, K, shift);
       }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int n = 0; n < sum[u].N; ++n) sum[u].v[n] = 0.f;
+      Pairs<T> sum[U] = {};
       for (int i0 = 0; i0 < p.k; i0 += kRows) {
-        W y[kRows][U] = {};
-        int32_t r[kRows];
+        Parts<WHOLE, T> y[kRows][U] = {};
+        const T* row[kRows];
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-          r[i] = __shfl_sync(~0u, place, min(i0 + i, 31));
-          if (i0 + i >= p.k) r[i] = -1;
-          if (r[i] >= 0) {
-            const W* row = reinterpret_cast<const W*>(p.y + (int64_t)r[i] * p.ld_y);
+          const int32_t r = __shfl_sync(~0u, place, min(i0 + i, 31));
+          row[i] = i0 + i < p.k && r >= 0 ? static_cast<const T*>(p.y) + r * p.ld_y : nullptr;
+          if (row[i]) {
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-              if (c0 + u * blockDim.x < p.K) y[i][u] = row[c0 + u * blockDim.x];
+            for (int u = 0; u < U; ++u) load_parts<WHOLE, T>(y[i][u], row[i], c + u * blockDim.x, K, shift);
           }
         }
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
           const float w = __shfl_sync(~0u, weight, min(i0 + i, 31));
-          if (r[i] < 0) continue;
+          if (!row[i]) continue;
 #pragma unroll
           for (int u = 0; u < U; ++u) {
-            Values<T, W> x;
-            x.load(&y[i][u]);
+            Pairs<T> x;
+            unpack<T>(from_parts<WHOLE, T>(y[i][u], row[i], c + u * blockDim.x, K, shift), x);
 #pragma unroll
-            for (int n = 0; n < x.N; ++n) sum[u].v[n] = fmaf(w, x.v[n], sum[u].v[n]);
+            for (int n = 0; n < N / 2; ++n) sum[u][n] = fma2(both(w), x[n], sum[u][n]);
           }
         }
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (p.residual) {
-          Values<T, W> x;
-          x.load(&rest[u]);
+        if (residual) {
+          Pairs<T> x;
+          unpack<T>(from_parts<WHOLE, T>(rest[u], residual, c + u * blockDim.x, K, shift), x);
 #pragma unroll
-          for (int n = 0; n < x.N; ++n) sum[u].v[n] += x.v[n];
+          for (int n = 0; n < N / 2; ++n) sum[u][n] = make_float2(sum[u][n].x + x[n].x, sum[u][n].y + x[n].y);
         }
-        if (c0 + u * blockDim.x < p.K) sum[u].store(reinterpret_cast<W*>(p.out + t * p.ld_out) + c0 + u * blockDim.x);
+        store_vector<WHOLE>(out, c + u * blockDim.x, K, shift, pack<T>(sum[u]));
       }
     }
   }
 }
 
-// in: dout, y, out: dy, sums: dweights.  The token's gradient stays in registers (V vectors of each thread; longer rows in several passes) while its k rows go by, kRows
-// of them on the way at a time; the k sums meet in shared memory once.
-template <typename T, typename W, int V>
+// in: dout, y, out: dy, sums: dweights.  V vectors of a row and kRows of its k rows on the way at a time; WHOLE: the token's gradient stays in registers while they go by (else the
+// vectors of each row lie otherwise).  The k sums meet in shared memory once.
+template <typename T, bool WHOLE, int V>
 __global__ void __launch_bounds__(256) combine_backward_kernel(const RowsParams p) {
-  constexpr int kRows = 4 * V <= 8 ? 4 : 1;
+  constexpr int kRows = WHOLE ? 4 : 2, N = kVector<T>;
+  static_assert(WHOLE || V == 1, "vectors at the boundaries of each row");
   __shared__ float parts[2][kMostChosen][8];
   wait_for_stream();
   if (blockIdx.x < p.clear_blocks) {
-    clear_rows<W>(p, p.ld_out, p.out, nullptr);
+    clear_rows<WHOLE, T>(p, nullptr);
     return;
   }
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  const int64_t step = (int64_t)V * blockDim.x;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, K = (int)p.K, step = V * blockDim.x;
   int turn = 0;
   for (int64_t t = blockIdx.x - p.clear_blocks; t < p.T; t += p.token_blocks, turn ^= 1) {  // (a buffer is written again behind the other one's barrier)
-    const W* d_row = reinterpret_cast<const W*>(p.in + t * p.ld_in);
+    const T* d_row = static_cast<const T*>(p.in) + t * p.ld_in;
     int32_t place = lane < p.k ? p.position[t * p.k + lane] : -1;
     if (place >= p.rows) place = -1;
     const float weight = lane < p.k ? p.weights[t * p.k + lane] : 0.f;
-    for (int64_t c0 = threadIdx.x; c0 - threadIdx.x < p.K; c0 += step) {
-      W d[V] = {};
+    for (int c0 = 0; c0 * N - (WHOLE ? 0 : N - 1) < K; c0 += step) {
+      const int c = c0 + threadIdx.x;
+      Parts<WHOLE, T> d[WHOLE ? V : kRows] = {};
+      if (WHOLE) {
 #pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (c0 + v * blockDim.x < p.K) d[v] = d_row[c0 + v * blockDim.x];
+        for (int v = 0; v < V; ++v) load_parts<WHOLE, T>(d[v], d_row, c + v * blockDim.x, K, 0);
+      }
       for (int i0 = 0; i0 < p.k; i0 += kRows) {
-        W y[kRows][V] = {};
+        Parts<WHOLE, T> y[kRows][V] = {};
         int32_t r[kRows];
+        int shift[kRows];
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
           r[i] = __shfl_sync(~0u, place, min(i0 + i, 31));
           if (i0 + i >= p.k) r[i] = -1;
+          shift[i] = 0;
           if (r[i] >= 0) {
-            const W* row = reinterpret_cast<const W*>(p.y + (int64_t)r[i] * p.ld_y);
+            if (!WHOLE) {
+              shift[i] = shift_of<T, N>(static_cast<T*>(p.out) + r[i] * p.ld_out);
+              load_parts<WHOLE, T>(d[i], d_row, c, K, shift[i]);
+            }
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-              if (c0 + v * blockDim.x < p.K) y[i][v] = row[c0 + v * blockDim.x];
+            for (int v = 0; v < V; ++v) load_parts<WHOLE, T>(y[i][v], static_cast<const T*>(p.y) + r[i] * p.ld_y, c + v * blockDim.x, K, shift[i]);
           }
         }
         float dot[kRows];
@@ -375,18 +381,20 @@ __global__ void __launch_bounds__(256) combine_backward_kernel(const RowsParams 
           dot[i] = 0.f;
           const float w = __shfl_sync(~0u, weight, min(i0 + i, 31));
           if (r[i] >= 0) {
-            W* out = reinterpret_cast<W*>(p.out + (int64_t)r[i] * p.ld_out);
+            const T* y_row = static_cast<const T*>(p.y) + r[i] * p.ld_y;
+            T* out = static_cast<T*>(p.out) + r[i] * p.ld_out;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-              Values<T, W> a, b;
-              a.load(&d[v]);
-              b.load(&y[i][v]);
+              Pairs<T> a, b;
+              unpack<T>(from_parts<WHOLE, T>(d[WHOLE ? v : i], d_row, c + v * blockDim.x, K, shift[i]), a);
+              unpack<T>(from_parts<WHOLE, T>(y[i][v], y_row, c + v * blockDim.x, K, shift[i]), b);
 #pragma unroll
-              for (int n = 0; n < a.N; ++n) {
-                dot[i] = fmaf(a.v[n], b.v[n], dot[i]);
-                a.v[n] *= w;
+              for (int n = 0; n < N / 2; ++n) {
+                dot[i] = fmaf(a[n].x, b[n].x, dot[i]);
+                dot[i] = fmaf(a[n].y, b[n].y, dot[i]);
+                a[n] = mul2(a[n], both(w));
               }
-              if (c0 + v * blockDim.x < p.K) a.store(out + c0 + v * blockDim.x);
+              store_vector<WHOLE>(out, c + v * blockDim.x, K, shift[i], pack<T>(a));
             }
           }
         }
@@ -399,7 +407,7 @@ __global__ void __launch_bounds__(256) combine_backward_kernel(const RowsParams 
           for (int i = 0; i < kRows; ++i)
             if (i0 + i < p.k) {
               float& part = parts[turn][i0 + i][warp];
-              part = c0 >= step ? part + dot[i] : dot[i];
+              part = c0 ? part + dot[i] : dot[i];
             }
         }
       }
@@ -423,8 +431,11 @@ bool whole_vectors(int es, int64_t K, std::initializer_list<const void*> at, std
   return ok;
 }
 
-// threads to a row of n vectors: whole warps, at most 256
-unsigned row_threads(int64_t n) { return (unsigned)(n >= 256 ? 256 : (n + 31) / 32 * 32); }
+// threads to a row of n vectors: whole warps, at most 256, as many rounds of them as 256 would take
+unsigned row_threads(int64_t n) {
+  const int64_t rounds = (n + 255) / 256;
+  return (unsigned)(((n + rounds - 1) / rounds + 31) / 32 * 32);
+}
 unsigned token_blocks(int64_t T) {
   const int64_t most = (int64_t)sm_count() * 32;
   return (unsigned)(T < most ? T : most);
@@ -506,18 +517,18 @@ extern "C" sp24_status sp24_expert_gather(sp24_dtype t, int64_t T, int64_t K, co
   SP24_RETURN_IF(arch != SP24_OK, arch);
   RowsParams p = {};
   p.T = T; p.K = K; p.rows = rows; p.k = k;
-  p.ld_in = ldx * es; p.ld_out = ldo * es;
-  p.in = static_cast<const uint8_t*>(x); p.out = static_cast<uint8_t*>(out);
+  p.ld_in = ldx; p.ld_out = ldo;
+  p.in = x; p.out = out;
   p.position = position; p.source = source; p.weights = scale; p.sums = out_scale;
-  auto run = [&](auto word) {
-    using W = decltype(word);
-    p.K = K * es / (int64_t)sizeof(W);
-    const unsigned threads = row_threads(p.K);
-    p.token_blocks = (int)token_blocks(T);
-    p.clear_blocks = (int)clearing_blocks(rows, threads);
-    return launch_overlapped(gather_kernel<W>, dim3(p.token_blocks + p.clear_blocks), dim3(threads), 0, static_cast<cudaStream_t>(stream), 1, p);
+  const bool whole = whole_vectors(es, K, {x, out}, {ldx, ldo});
+  const unsigned threads = row_threads(row_vectors(K, es, whole));
+  p.token_blocks = (int)token_blocks(T);
+  p.clear_blocks = (int)clearing_blocks(rows, threads);
+  auto run = [&](auto element) {
+    using E = decltype(element);
+    return launch_overlapped(whole ? gather_kernel<E, true> : gather_kernel<E, false>, dim3(p.token_blocks + p.clear_blocks), dim3(threads), 0,
+                             static_cast<cudaStream_t>(stream), 1, p);
   };
-  if (whole_vectors(es, K, {x, out}, {ldx, ldo})) return run(uint4{});
   if (es == 4) return run(uint32_t{});
   if (es == 2) return run(uint16_t{});
   return run(uint8_t{});
@@ -537,22 +548,16 @@ extern "C" sp24_status sp24_expert_combine(sp24_dtype t, int64_t T, int64_t K, i
   const sp24_status arch = check_arch();
   SP24_RETURN_IF(arch != SP24_OK, arch);
   RowsParams p = {};
-  p.T = T; p.rows = rows; p.k = k;
-  p.ld_y = ldy * es; p.ld_out = ldo * es; p.ld_res = ldr * es;
-  p.y = static_cast<const uint8_t*>(y); p.residual = static_cast<const uint8_t*>(residual); p.out = static_cast<uint8_t*>(out);
+  p.T = T; p.K = K; p.rows = rows; p.k = k;
+  p.ld_y = ldy; p.ld_out = ldo; p.ld_res = ldr;
+  p.y = y; p.residual = residual; p.out = out;
   p.position = position; p.weights = weights;
   const bool whole = whole_vectors(es, K, {y, out, residual}, {ldy, ldo, residual ? ldr : 0});
   return with_float_type(t, [&](auto type) {
     using Type = typename decltype(type)::type;
-    auto run = [&](auto word) {
-      using W = decltype(word);
-      p.K = K * es / (int64_t)sizeof(W);
-      constexpr int U = sizeof(W) == 16 ? 2 : 4;  // (rows of 256 vectors: half as many threads with two each, more tokens to an SM)
-      return launch_overlapped(combine_kernel<Type, W, U>, dim3(token_blocks(T)), dim3(row_threads((p.K + U - 1) / U)), 0, static_cast<cudaStream_t>(stream), 1, p);
-    };
-    if (whole) return run(uint4{});
-    if constexpr (sizeof(Type) == 4) return run(uint32_t{});
-    else return run(uint16_t{});
+    const int64_t n = row_vectors(K, es, whole);  // (whole vectors: half as many threads with two each, more tokens to an SM)
+    return launch_overlapped(whole ? combine_kernel<Type, true> : combine_kernel<Type, false>, dim3(token_blocks(T)), dim3(row_threads(whole ? (n + 1) / 2 : n)), 0,
+                             static_cast<cudaStream_t>(stream), 1, p);
   });
 }
 
@@ -572,27 +577,18 @@ extern "C" sp24_status sp24_expert_combine_backward(sp24_dtype t, int64_t T, int
   const sp24_status arch = check_arch();
   SP24_RETURN_IF(arch != SP24_OK, arch);
   RowsParams p = {};
-  p.T = T; p.rows = rows; p.k = k;
-  p.ld_in = lddo * es; p.ld_y = ldy * es; p.ld_out = lddy * es;
-  p.in = static_cast<const uint8_t*>(dout); p.y = static_cast<const uint8_t*>(y); p.out = static_cast<uint8_t*>(dy);
+  p.T = T; p.K = K; p.rows = rows; p.k = k;
+  p.ld_in = lddo; p.ld_y = ldy; p.ld_out = lddy;
+  p.in = dout; p.y = y; p.out = dy;
   p.position = position; p.source = source; p.weights = weights; p.sums = dweights;
   const bool whole = whole_vectors(es, K, {dout, y, dy}, {lddo, ldy, lddy});
   return with_float_type(t, [&](auto type) {
     using Type = typename decltype(type)::type;
-    auto run = [&](auto word) {
-      using W = decltype(word);
-      p.K = K * es / (int64_t)sizeof(W);
-      const unsigned threads = row_threads(p.K);
-      p.token_blocks = (int)token_blocks(T);
-      p.clear_blocks = (int)clearing_blocks(rows, threads);
-      const dim3 grid(p.token_blocks + p.clear_blocks);
-      const cudaStream_t s = static_cast<cudaStream_t>(stream);
-      if (p.K <= threads) return launch_overlapped(combine_backward_kernel<Type, W, 1>, grid, dim3(threads), 0, s, 1, p);
-      if (p.K <= 2 * threads || sizeof(W) == 16) return launch_overlapped(combine_backward_kernel<Type, W, 2>, grid, dim3(threads), 0, s, 1, p);
-      return launch_overlapped(combine_backward_kernel<Type, W, 8>, grid, dim3(threads), 0, s, 1, p);
-    };
-    if (whole) return run(uint4{});
-    if constexpr (sizeof(Type) == 4) return run(uint32_t{});
-    else return run(uint16_t{});
+    const int64_t n = row_vectors(K, es, whole);
+    const unsigned threads = row_threads(n);
+    p.token_blocks = (int)token_blocks(T);
+    p.clear_blocks = (int)clearing_blocks(rows, threads);
+    const auto kernel = !whole ? combine_backward_kernel<Type, false, 1> : n <= threads ? combine_backward_kernel<Type, true, 1> : combine_backward_kernel<Type, true, 2>;
+    return launch_overlapped(kernel, dim3(p.token_blocks + p.clear_blocks), dim3(threads), 0, static_cast<cudaStream_t>(stream), 1, p);
   });
 }
