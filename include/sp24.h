@@ -325,6 +325,7 @@ sp24_status sp24_gemm_static_ws_status(void* stream);
  * following sp24_gemm / sp24_gemm_i8_dequant / sp24_conv3x3_nhwc call in this process.
  *   ctas: 1 or 2 CTAs per tile; block_n: columns per tile; mblk: 128-row blocks per CTA (1 to 3);
  *   the shape must be one of the built ones, else those calls return SP24_ERR_UNSUPPORTED.
+ *   (sp24_expert_linear: ctas 1 and up to 128 columns, or 2 and up to 224, dense 256, whole 32; mblk 1.)
  *   ctas == 0 restores the automatic choice.  band: m-tiles per band of the tile sweep, 0 = default.
  * The environment variables SP24_TILE=<ctas>x<block_n>x<mblk>, SP24_BAND=<band> and SP24_LOG=1
  * (print the problem and the chosen tile shape of every call to stderr) give the initial values;
