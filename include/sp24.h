@@ -325,7 +325,7 @@ sp24_status sp24_gemm_static_ws_status(void* stream);
  * following sp24_gemm / sp24_gemm_i8_dequant / sp24_conv3x3_nhwc call in this process.
  *   ctas: 1 or 2 CTAs per tile; block_n: columns per tile; mblk: 128-row blocks per CTA (1 to 3);
  *   the shape must be one of the built ones, else those calls return SP24_ERR_UNSUPPORTED.
- *   (sp24_expert_linear: ctas 1 and up to 128 columns, or 2 and up to 224, dense 256, whole 32; mblk 1.)
+ *   (sp24_expert_linear and sp24_expert_linear_dx: ctas 1 and up to 128 columns, or 2 and up to 224, dense 256, whole 32; mblk 1.)
  *   ctas == 0 restores the automatic choice.  band: m-tiles per band of the tile sweep, 0 = default.
  * The environment variables SP24_TILE=<ctas>x<block_n>x<mblk>, SP24_BAND=<band> and SP24_LOG=1
  * (print the problem and the chosen tile shape of every call to stderr) give the initial values;
@@ -535,23 +535,21 @@ sp24_status sp24_expert_linear(const sp24_expert_desc* d, const sp24_expert_epil
 
 /* The products of its gradient, for F16 or BF16 operands: dX[r, .] = sum_i dz[r, i] W_e[i, .] and dW_e[i, .] = sum over the expert's rows of dz[r, i] X[r, .], each
  * rounded once to ab_type, with dense W (E M rows of K values, leading dimension d->lda).
- *   sp24_expert_linear_dx: dz: rows x M (leading dimension d->ldd), dX: rows x K (ldx); only rows of experts are written.
- *   sp24_expert_linear_dw: dzt: dz transposed, M x rows (leading dimension lddzt), X: rows x K (ldx), dW: E M x K (lda).  An expert without rows gets zeros.
+ *   dz: rows x M (leading dimension d->ldd), X, dX: rows x K (ldx; only rows of experts are written), dW: E M x K (lda; an expert without rows gets zeros).
+ *   sp24_expert_linear_dw: every offset is a multiple of 16 (sp24_expert_order with align = 16): the weights' gradients of an expert that is not so placed are NaN.
  *      meta (or NULL): the weights' metadata, as for sp24_expert_linear; the entries of dW that it does not name as kept are zeros.
- *      Every offset is a multiple of 16 (sp24_expert_order with align = 16): the weights' gradients of an expert that is not so placed are NaN.
  *   d->cd_type is ab_type; d->ld_residual, d->ld_pre and d->a_is_dense are not used.  Sizes, alignment and workspace as above.
- * sp24_expert_act_backward: what they and the bias's gradient are made of, dz[r, i] = dy[r, i] act'(z[r, i]) rounded to t, for all rows (dz: rows x M or NULL; dzt: M x
- *   rows or NULL, fastest with lddzt the rows up to a multiple of 8 or more, of which the elements behind the last row may be written), and dbias[e, i] (E x M
- *   floats or NULL) = the sum of the expert's dz before their rounding, in an order that the offsets fix.  z may be NULL for SP24_ACT_NONE.  t: SP24_F16, SP24_BF16 or
- *   SP24_F32; any leading dimensions and alignment.  workspace (for dbias): sp24_expert_act_backward_workspace_bytes(...) bytes, 16-byte aligned, contents of no
- *   matter. */
+ * sp24_expert_act_backward: what they and the bias's gradient are made of, dz[r, i] = dy[r, i] act'(z[r, i]) rounded to t, for all rows (rows x M, or NULL), and dbias[e, i]
+ *   (E x M floats or NULL) = the sum of the expert's dz before their rounding, in an order that the offsets fix.  z may be NULL for SP24_ACT_NONE.  t: SP24_F16, SP24_BF16 or
+ *   SP24_F32; any leading dimensions and alignment; dz may be dy or z (same leading dimension) where dbias is NULL.  workspace (for dbias):
+ *   sp24_expert_act_backward_workspace_bytes(...) bytes, 16-byte aligned, contents of no matter. */
 size_t sp24_expert_act_backward_workspace_bytes(int64_t E, int64_t M, int64_t rows);
 sp24_status sp24_expert_act_backward(sp24_dtype t, sp24_act act, int64_t E, int64_t M, int64_t rows, const void* dy, int64_t lddy, const void* z, int64_t ldz,
-                                     const int32_t* offsets, void* dz, int64_t lddz, void* dzt, int64_t lddzt, float* dbias, void* workspace,
-                                     size_t workspace_bytes, void* stream);
+                                     const int32_t* offsets, void* dz, int64_t lddz, float* dbias, void* workspace, size_t workspace_bytes,
+                                     void* stream);
 sp24_status sp24_expert_linear_dx(const sp24_expert_desc* d, const void* dz, const void* W, const int32_t* offsets, void* dX, void* workspace,
                                   size_t workspace_bytes, void* stream);
-sp24_status sp24_expert_linear_dw(const sp24_expert_desc* d, const void* dzt, int64_t lddzt, const void* X, const int32_t* offsets, const void* meta, void* dW,
+sp24_status sp24_expert_linear_dw(const sp24_expert_desc* d, const void* dz, const void* X, const int32_t* offsets, const void* meta, void* dW,
                                   void* workspace, size_t workspace_bytes, void* stream);
 
 /* End-to-end convenience for callers whose data lives in HOST memory (pinned for speed):

@@ -141,10 +141,10 @@ def _load() -> ctypes.CDLL:
     lib.sp24_expert_combine_backward.argtypes = [ci, i64, i64, i64, vp, i64, vp, i64, ci, vp, vp, vp, vp, i64, vp, vp]
     lib.sp24_expert_linear.argtypes = [ctypes.POINTER(ExpertDesc), ctypes.POINTER(ExpertEpilogue), vp, vp, vp, vp, vp, vp, sz, vp]
     lib.sp24_expert_linear_dx.argtypes = [ctypes.POINTER(ExpertDesc), vp, vp, vp, vp, vp, sz, vp]
-    lib.sp24_expert_linear_dw.argtypes = [ctypes.POINTER(ExpertDesc), vp, i64, vp, vp, vp, vp, vp, sz, vp]
+    lib.sp24_expert_linear_dw.argtypes = [ctypes.POINTER(ExpertDesc), vp, vp, vp, vp, vp, vp, sz, vp]
     lib.sp24_expert_act_backward_workspace_bytes.argtypes = [i64, i64, i64]
     lib.sp24_expert_act_backward_workspace_bytes.restype = sz
-    lib.sp24_expert_act_backward.argtypes = [ci, ci, i64, i64, i64, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, sz, vp]
+    lib.sp24_expert_act_backward.argtypes = [ci, ci, i64, i64, i64, vp, i64, vp, i64, vp, vp, i64, vp, vp, sz, vp]
     for name in ("sp24_route", "sp24_route_backward", "sp24_expert_order", "sp24_expert_gather", "sp24_expert_combine", "sp24_expert_combine_backward",
                  "sp24_expert_linear", "sp24_expert_linear_dx", "sp24_expert_linear_dw", "sp24_expert_act_backward"):
         getattr(lib, name).restype = ci
@@ -1134,12 +1134,10 @@ def _expert_linear_backward(dy, pre, X, W, offsets, act, meta, bias, ws):
         _slots(meta, where, dy, torch.uint8, (E, meta_bytes(code, M, K)))
     t, stream = DTYPE_CODE[code], _stream()
     ws = ws if ws is not None else workspace(dy.device, stream)
-    # dz in both orders: the products contract over different axes (without an activation dz is dy itself, where a product can take it)
+    # (without an activation dz is dy itself, where a product can take it)
     dz, lddz = dy, lddy
     if a or dy.data_ptr() % 16 or lddy * dy.element_size() % 16:
         dz, lddz = dy.new_empty((rows, M)), M
-    lddzt = (rows + 7) // 8 * 8
-    dzt = dy.new_empty((M, lddzt))
     dbias = scratch = None
     size = 0
     if bias:
@@ -1147,10 +1145,10 @@ def _expert_linear_backward(dy, pre, X, W, offsets, act, meta, bias, ws):
         size = lib.sp24_expert_act_backward_workspace_bytes(E, M, rows)
         scratch = dy.new_empty(size, dtype=torch.uint8)
     _check(lib.sp24_expert_act_backward(t, a, E, M, rows, _ptr(dy), lddy, _ptr(pre) if a else None, ldz, _ptr(offsets), None if dz is dy else _ptr(dz), lddz,
-                                        _ptr(dzt), lddzt, _ptr(dbias), _ptr(scratch), size, stream), where)
+                                        _ptr(dbias), _ptr(scratch), size, stream), where)
     dX, dW = dy.new_empty((rows, K)), dy.new_empty((E, M, K))
     desc = ExpertDesc(t, t, E, M, K, rows, ldw, K, lddz, 0, 0, 1)
     _check(lib.sp24_expert_linear_dx(byref(desc), _ptr(dz), _ptr(W), _ptr(offsets), _ptr(dX), _ptr(ws), ws.numel(), stream), where)
     desc = ExpertDesc(t, t, E, M, K, rows, K, ldx, lddz, 0, 0, 1)
-    _check(lib.sp24_expert_linear_dw(byref(desc), _ptr(dzt), max(8, lddzt), _ptr(X), _ptr(offsets), _ptr(meta), _ptr(dW), _ptr(ws), ws.numel(), stream), where)
+    _check(lib.sp24_expert_linear_dw(byref(desc), _ptr(dz), _ptr(X), _ptr(offsets), _ptr(meta), _ptr(dW), _ptr(ws), ws.numel(), stream), where)
     return dX, dW, dbias

@@ -43,13 +43,13 @@ __device__ __forceinline__ int expert_of_row(const ActGradParams& p, int64_t r) 
 // u ^ (2 (m >> 3 & 3) + (m & 1)): the eight rows of a matrix are in different banks.
 // dz = dy act'(z) is needed in both orders, and reading dy and z once for both is what the tile is for.  Bound by HBM and, with GELU, the arithmetic of the slope:
 // bf16 4096 x 8192 with the bias 52 us = 5.1 TB/s (ReLU 46; by elements 125, tiles of 64 x 64 62); three blocks to an SM instead of two spill (75).
-// EXPERTS: the bias's gradient of each expert's rows.  Tile i of the rows has a partial sum of its own for every expert that it meets, in row i + (expert) of
+// EXPERTS: dz in its own order only, and the bias's gradient of each expert's rows.  Tile i of the rows has a partial sum of its own for every expert that it meets, in row i + (expert) of
 // `partial`, which no other tile and expert share.
 template <typename T, int ACT, int kWide, bool EXPERTS = false>
 __global__ void __launch_bounds__(4 * kWide) act_grad_tile_kernel(const ActGradParams p) {
   constexpr int kUnits = kWide / 8, kWideThreads = 4 * kWide;
   constexpr int kPasses = kWide * kUnits / kWideThreads, kRows = kWide / kPasses;
-  __shared__ uint4 tile[kWide * kUnits];
+  __shared__ uint4 tile[EXPERTS ? 1 : kWide * kUnits];
   __shared__ float over[kWideThreads / 32][kWide];  // sums over the rows of each warp
   const int64_t col_tiles = (p.cols + kWide - 1) / kWide;
   const int64_t row0 = (int64_t)(blockIdx.x / col_tiles) * kWide, col0 = (int64_t)(blockIdx.x % col_tiles) * kWide;
@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(4 * kWide) act_grad_tile_kernel(const ActGradP
     }
     const uint4 packed = pack<T>(d);
     if (p.dz && r < p.rows && c < p.cols) *reinterpret_cast<uint4*>(static_cast<T*>(p.dz) + r * p.lddz + c) = packed;
-    tile[m * kUnits + (u ^ (2 * (m >> 3 & 3) + (m & 1)))] = packed;
+    if (!EXPERTS) tile[m * kUnits + (u ^ (2 * (m >> 3 & 3) + (m & 1)))] = packed;
     if (p.partial && p.over_rows) {
 #pragma unroll
       for (int n = 0; n < 4; ++n) sums[n] = make_float2(sums[n].x + d[n].x, sums[n].y + d[n].y);
@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(4 * kWide) act_grad_tile_kernel(const ActGradP
   };
   if (p.partial && p.over_rows) sum_over_warp();
   __syncthreads();
-  if (p.dzt) {
+  if (!EXPERTS && p.dzt) {
     static_assert(kWideThreads / 32 == kUnits, "a warp to a unit: eight columns");
     const int i = lane >> 3, j = (lane & 7) >> 1, b = lane & 1;  // this lane's row of matrix i for ldmatrix
     const int64_t col = col0 + 8 * warp + (lane >> 2);
@@ -327,29 +327,27 @@ extern "C" size_t sp24_expert_act_backward_workspace_bytes(int64_t E, int64_t M,
 }
 
 extern "C" sp24_status sp24_expert_act_backward(sp24_dtype t, sp24_act act, int64_t E, int64_t M, int64_t rows, const void* dy, int64_t lddy,
-                                                const void* z, int64_t ldz, const int32_t* offsets, void* dz, int64_t lddz, void* dzt, int64_t lddzt,
-                                                float* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+                                                const void* z, int64_t ldz, const int32_t* offsets, void* dz, int64_t lddz, float* dbias, void* workspace,
+                                                size_t workspace_bytes, void* stream) {
   SP24_RETURN_IF(!is_float_type(t), SP24_ERR_DTYPE);
   SP24_RETURN_IF(!is_act(act), SP24_ERR_UNSUPPORTED);
   SP24_RETURN_IF(E < 1 || E > 1024 || M < 1 || M > kMostColumns || rows < 0 || rows > kMostColumns, SP24_ERR_SHAPE);
   const bool reads_z = act != SP24_ACT_NONE;
   SP24_RETURN_IF((rows > 0 && (!dy || (reads_z && !z))) || (dbias && !offsets), SP24_ERR_NULL);
-  SP24_RETURN_IF(!row_fits(rows, M, lddy) || (reads_z && !row_fits(rows, M, ldz)) || (dz && !row_fits(rows, M, lddz)) || (dzt && !row_fits(M, rows, lddzt)),
-                 SP24_ERR_STRIDE);
+  SP24_RETURN_IF(!row_fits(rows, M, lddy) || (reads_z && !row_fits(rows, M, ldz)) || (dz && !row_fits(rows, M, lddz)), SP24_ERR_STRIDE);
   const size_t es = elem_bytes(t);
-  SP24_RETURN_IF(!aligned(dy, es) || (reads_z && !aligned(z, es)) || !aligned(dz, es) || !aligned(dzt, es) || !aligned(dbias, 4) || !aligned(offsets, 4), SP24_ERR_ALIGN);
+  SP24_RETURN_IF(!aligned(dy, es) || (reads_z && !aligned(z, es)) || !aligned(dz, es) || !aligned(dbias, 4) || !aligned(offsets, 4), SP24_ERR_ALIGN);
   SP24_RETURN_IF(dbias && (!workspace || !aligned16(workspace) || workspace_bytes < sp24_expert_act_backward_workspace_bytes(E, M, rows)), SP24_ERR_WORKSPACE);
-  if (!dbias && (rows == 0 || (!dz && !dzt))) return SP24_OK;
-  // (rows of dzt are written up to a whole vector, which their leading dimension has room for)
+  if (!dbias && (rows == 0 || !dz)) return SP24_OK;
   const bool whole = t != SP24_F32 && M % 8 == 0 && whole_rows(dy, rows, lddy, 2, 16) && (!reads_z || whole_rows(z, rows, ldz, 2, 16)) &&
-                     whole_rows(dz, rows, lddz, 2, 16) && (!dzt || (whole_rows(dzt, M, lddzt, 2, 16) && lddzt >= (rows + 7) / 8 * 8));
+                     whole_rows(dz, rows, lddz, 2, 16);
   const bool wide = whole && (rows + 127) / 128 * ((M + 127) / 128) >= 2 * sm_count();
   const int64_t edge = wide ? 2 * kTile : kTile, row_tiles = (rows + edge - 1) / edge, col_tiles = (M + edge - 1) / edge;
   SP24_RETURN_IF(row_tiles * col_tiles > 0x7fffffff, SP24_ERR_SHAPE);
   sp24_status st = check_arch();
   SP24_RETURN_IF(st != SP24_OK, st);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  ActGradParams p = {rows, M, dy, z, dz, dzt, dbias ? static_cast<float*>(workspace) : nullptr, lddy, ldz, lddz, lddzt, 1, offsets, (int)E};
+  ActGradParams p = {rows, M, dy, z, dz, nullptr, dbias ? static_cast<float*>(workspace) : nullptr, lddy, ldz, lddz, 0, 1, offsets, (int)E};
   if (rows > 0) {
     const dim3 grid((unsigned)(row_tiles * col_tiles));
     st = with_float_type(t, [&](auto type) {
@@ -363,7 +361,7 @@ extern "C" sp24_status sp24_expert_act_backward(sp24_dtype t, sp24_act act, int6
         ActGradParams q = p;
         q.partial = nullptr;
         sp24_status done = SP24_OK;
-        if (dz || dzt) done = launch_overlapped(act_grad_kernel<T, kAct>, grid, dim3(256), 0, s, 1, q);
+        if (dz) done = launch_overlapped(act_grad_kernel<T, kAct>, grid, dim3(256), 0, s, 1, q);
         if (done != SP24_OK || !dbias) return done;
         return launch_overlapped(expert_sums_kernel<T, kAct>, grid, dim3(256), 0, s, 1, p);
       });

@@ -10,7 +10,7 @@ namespace {
 // offsets at its start) and the last dimension of the tensor maps is that of all experts.  Tiles of one m-block; the columns of a tile are its caller's choice.
 template <int KIND, bool SPARSE, int BLOCK_N, int CTAS, int GROUP>
 sp24_status launch_group(const TileShape& tile, const sp24_gemm_desc* d, const GemmParams& base, const void* A, const void* meta, const void* B, cudaStream_t stream) {
-  constexpr bool kBMn = GROUP != kColumnsByExpert, kLinear = GROUP == kColumnsByExpert;
+  constexpr bool kBMn = GROUP == kKByExpert, kLinear = GROUP == kColumnsByExpert;
   using C = Cfg<KIND, SPARSE, BLOCK_N, CTAS, 1, kBMn>;
   GemmParams p = base;
   const int tile_n = p.tile_n = tile.tile_n;
@@ -25,21 +25,23 @@ sp24_status launch_group(const TileShape& tile, const sp24_gemm_desc* d, const G
   p.m_tiles = (int)((d->M + tile_m - 1) / tile_m);
   p.n_tiles = (int)((d->N + tile_n - 1) / tile_n);
   p.k_blocks = (int)((d->K + C::kKPerStage - 1) / C::kKPerStage);
-  p.by_band = FastDiv::by((uint32_t)(GROUP == kRowsByExpert ? p.n_tiles : p.m_tiles));
+  p.by_band = FastDiv::by((uint32_t)p.m_tiles);
   p.meta_kb = (int)(2 * ((d->K + 255) / 256));
   p.meta_blocks = (int)((d->M + kBlockM - 1) / kBlockM);
   // tiles there can be at most: every expert with rows has one that is not full
   const int64_t met = p.experts < p.rows ? p.experts : p.rows;
   int64_t tiles;
-  if (GROUP == kColumnsByExpert) tiles = p.m_tiles * (p.rows / tile_n + met);
-  else if (GROUP == kRowsByExpert) tiles = p.n_tiles * (p.rows / tile_m + met);
+  if (columns_by_expert(GROUP)) tiles = p.m_tiles * (p.rows / tile_n + met);
   else tiles = (int64_t)p.m_tiles * p.n_tiles * p.experts;
   SP24_RETURN_IF(tiles >= int64_t(1) << 31, SP24_ERR_SHAPE);
   const uint32_t b_box_rows = (uint32_t)C::b_rows(tile_n);
   CUtensorMap map_a, map_b, map_e;
   sp24_status st;
-  if (GROUP == kColumnsByExpert) {
-    if (p.kps == 2)
+  if (columns_by_expert(GROUP)) {
+    if (GROUP == kColumnsTransposed)
+      st = make_map(&map_a, MapShape{A, {(uint64_t)d->M, (uint64_t)d->K, E}, {(uint64_t)d->lda * es, (uint64_t)(d->K * d->lda) * es},
+                                     {atom_elems, (uint32_t)C::kKPerStage, 1}, es, 128});
+    else if (p.kps == 2)
       st = make_map(&map_a, MapShape{A, {atom_elems, E * d->M, a_cols / atom_elems}, {(uint64_t)d->lda * es, kAtomBytes}, {atom_elems, kBlockM, 2}, es, 128});
     else
       st = make_map(&map_a, A, es, E * d->M, a_cols, d->lda * es, atom_elems, kBlockM, 128);
@@ -51,13 +53,8 @@ sp24_status launch_group(const TileShape& tile, const sp24_gemm_desc* d, const G
     } else {
       st = make_map(&map_b, B, es, rows, d->K, d->ldb * es, atom_elems, b_box_rows, 128);
     }
-  } else if (GROUP == kRowsByExpert) {
-    st = make_map(&map_a, A, es, rows, a_cols, d->lda * es, atom_elems, kBlockM, 128);
-    if (st != SP24_OK) return st;
-    st = make_map(&map_b, MapShape{B, {(uint64_t)d->N, (uint64_t)d->K, E}, {(uint64_t)d->ldb * es, (uint64_t)(d->K * d->ldb) * es},
-                                   {(uint32_t)C::kBChunkElems, (uint32_t)C::kKPerStage, 1}, es, 128});
   } else {
-    st = make_map(&map_a, A, es, d->M, rows, d->lda * es, atom_elems, kBlockM, 128);
+    st = make_map(&map_a, A, es, rows, d->M, d->lda * es, atom_elems, C::kKPerStage, 128);
     if (st != SP24_OK) return st;
     st = make_map(&map_b, B, es, rows, d->N, d->ldb * es, C::kBChunkElems, C::kKPerStage, 128);
   }
@@ -71,7 +68,7 @@ sp24_status launch_group(const TileShape& tile, const sp24_gemm_desc* d, const G
   }
   using Kernel = void (*)(CUtensorMap, CUtensorMap, CUtensorMap, CUtensorMap, CUtensorMap, GemmParams);
   Kernel forms[4] = {};  // [with C][bytes]
-#define SP24_FORM(CS_, C_) forms[2 * C_ + (CS_ >> 2)] = gemm_kernel<KIND, SPARSE, BLOCK_N, CTAS, 1, kBMn, CS_, kLinear, C_, false, kEpiWarps, kLinear, GROUP>;
+#define SP24_FORM(CS_, C_) forms[2 * C_ + (CS_ >> 2)] = gemm_kernel<KIND, SPARSE, BLOCK_N, CTAS, 1, kBMn, CS_, columns_by_expert(GROUP), C_, false, kEpiWarps, kLinear, GROUP>;
   SP24_FORM(2, false)
   if constexpr (kLinear) { SP24_FORM(2, true) SP24_FORM(4, false) SP24_FORM(4, true) }
 #undef SP24_FORM
@@ -104,9 +101,9 @@ sp24_status launch_group_shape(int group, TileShape t, bool sparse, const sp24_g
     if (wide && !sparse) return launch_group<KIND, false, 256, 2, kColumnsByExpert>(t, d, p, A, meta, B, s);
   }
   if constexpr (KIND == 0) {
-    if (group == kRowsByExpert && !sparse) {
-      if (one) return launch_group<KIND, false, 128, 1, kRowsByExpert>(t, d, p, A, meta, B, s);
-      if (wide) return launch_group<KIND, false, 256, 2, kRowsByExpert>(t, d, p, A, meta, B, s);
+    if (group == kColumnsTransposed && !sparse) {
+      if (one) return launch_group<KIND, false, 128, 1, kColumnsTransposed>(t, d, p, A, meta, B, s);
+      if (wide) return launch_group<KIND, false, 256, 2, kColumnsTransposed>(t, d, p, A, meta, B, s);
     }
     if (group == kKByExpert && !sparse) {
       if (one) return launch_group<KIND, false, 128, 1, kKByExpert>(t, d, p, A, meta, B, s);

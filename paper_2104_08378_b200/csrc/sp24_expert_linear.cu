@@ -6,7 +6,7 @@ namespace sp24 {
 namespace {
 
 constexpr int64_t kMostExperts = 1024, kMostRows = int64_t(1) << 30;
-enum { kColumnsByExpert = 1, kRowsByExpert = 2, kKByExpert = 3 };  // as the kernel has them
+enum { kColumnsByExpert = 1, kColumnsTransposed = 2, kKByExpert = 3 };  // as the kernel has them
 
 bool whole16(int64_t ld, int bytes) { return ld * bytes % 16 == 0; }
 
@@ -161,20 +161,23 @@ extern "C" sp24_status sp24_expert_linear_dx(const sp24_expert_desc* d, const vo
   st = check_gradient(d, dz, d->ldd, d->M, W, d->lda, offsets, dX, d->ldx, workspace, workspace_bytes);
   SP24_RETURN_IF(st != SP24_OK, st);
   GemmParams p = params(d, offsets, dX, workspace);
-  // rows of tokens times K: dz is the operand with rows, W_e the one with columns
-  const sp24_gemm_desc g = {d->ab_type, d->cd_type, d->rows, d->K, d->M, d->ldd, d->lda, 0, d->ldx, SP24_ROW_MAJOR, SP24_ROW_MAJOR, SP24_ROW_MAJOR, 1};
+  p.cd_col_major = 1;
+  // W_e, transposed, times rows of dz: the tokens are columns as in the product itself, so that an expert's last tile is as wide as its rows ask for
+  const sp24_gemm_desc g = {d->ab_type, d->cd_type, d->K, d->rows, d->M, d->lda, d->ldd, 0, d->ldx, SP24_COL_MAJOR, SP24_COL_MAJOR, SP24_COL_MAJOR, 1};
   TileShape tile = {1, 128, 1, 128, 0};
   if (mean_rows(d) > 128 && d->K > 128) tile = {2, 256, 1, 256, 0};
-  return run(kRowsByExpert, tile, false, &g, p, dz, nullptr, W, stream);
+  tile_override(&tile, true);
+  SP24_RETURN_IF(tile.tile_n > tile.block_n || tile.tile_n % 32, SP24_ERR_UNSUPPORTED);
+  return run(kColumnsTransposed, tile, false, &g, p, W, nullptr, dz, stream);
 }
 
-extern "C" sp24_status sp24_expert_linear_dw(const sp24_expert_desc* d, const void* dzt, int64_t lddzt, const void* X, const int32_t* offsets, const void* meta,
-                                             void* dW, void* workspace, size_t workspace_bytes, void* stream) {
+extern "C" sp24_status sp24_expert_linear_dw(const sp24_expert_desc* d, const void* dz, const void* X, const int32_t* offsets, const void* meta, void* dW,
+                                             void* workspace, size_t workspace_bytes, void* stream) {
   SP24_RETURN_IF(d == nullptr, SP24_ERR_NULL);
   SP24_RETURN_IF((d->ab_type != SP24_F16 && d->ab_type != SP24_BF16) || d->cd_type != d->ab_type, SP24_ERR_DTYPE);
   sp24_status st = check_sizes(d);
   SP24_RETURN_IF(st != SP24_OK, st);
-  st = check_gradient(d, dzt, lddzt, d->rows, X, d->ldx, offsets, dW, d->lda, workspace, workspace_bytes);
+  st = check_gradient(d, dz, d->ldd, d->M, X, d->ldx, offsets, dW, d->lda, workspace, workspace_bytes);
   SP24_RETURN_IF(st != SP24_OK, st);
   SP24_RETURN_IF(reinterpret_cast<uintptr_t>(meta) & 1, SP24_ERR_ALIGN);
   if (d->rows == 0) {  // no expert has any
@@ -182,10 +185,10 @@ extern "C" sp24_status sp24_expert_linear_dw(const sp24_expert_desc* d, const vo
     return SP24_OK;
   }
   GemmParams p = params(d, offsets, dW, workspace);
-  const sp24_gemm_desc g = {d->ab_type, d->cd_type, d->M, d->K, d->rows, lddzt, d->ldx, 0, d->lda, SP24_ROW_MAJOR, SP24_ROW_MAJOR, SP24_ROW_MAJOR, 1};
+  const sp24_gemm_desc g = {d->ab_type, d->cd_type, d->M, d->K, d->rows, d->ldd, d->ldx, 0, d->lda, SP24_ROW_MAJOR, SP24_ROW_MAJOR, SP24_ROW_MAJOR, 1};
   TileShape tile = {1, 128, 1, 128, 0};
   if (d->M > 128 && d->K > 128) tile = {2, 256, 1, 256, 0};
   p.keep = static_cast<const uint8_t*>(meta);
   p.keep_kb = (int)(2 * ((d->K + 255) / 256));
-  return run(kKByExpert, tile, false, &g, p, dzt, nullptr, X, stream);
+  return run(kKByExpert, tile, false, &g, p, dz, nullptr, X, stream);
 }

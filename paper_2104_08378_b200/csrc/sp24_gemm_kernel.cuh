@@ -190,9 +190,13 @@ __device__ __forceinline__ void tile_coords(int t, const GemmParams& p, int& mt,
 }
 
 // GROUP: the products of many experts in one launch (sp24_expert_linear and its gradients), each a problem of its own over the same
-// tensor maps.  The experts' rows are a range of one dimension, known on the device only: of the columns (B and D hold the rows of tokens), of the rows
-// (A and D), or of K (A and B; D is an expert's own).
-enum Group { kOneProblem = 0, kColumnsByExpert = 1, kRowsByExpert = 2, kKByExpert = 3 };
+// tensor maps.  The experts' rows are a range of one dimension, known on the device only: of the columns (B and D hold the rows of tokens), or of K (A and B; D is an
+// expert's own).
+enum Group { kOneProblem = 0, kColumnsByExpert = 1, kColumnsTransposed = 2, kKByExpert = 3 };
+__host__ __device__ constexpr bool columns_by_expert(int group) { return group == kColumnsByExpert || group == kColumnsTransposed; }
+// A with M contiguous (MN-major operand, 16-bit types): the weights of an expert, M x K as they are stored, times rows of M values (kColumnsTransposed), and rows of M
+// values whose products with others are summed over the rows (kKByExpert).  In shared memory as B with N contiguous: chunks of 64 rows of A, a k-row of 128 bytes each.
+__host__ __device__ constexpr bool a_transposed(int group) { return group == kColumnsTransposed || group == kKByExpert; }
 
 // In shared memory: where each expert's rows begin (E + 1 entries, in range and in order whatever the offsets are), and its first tile (E + 1, the last: how
 // many there are).
@@ -205,7 +209,7 @@ struct Tile {
   int mt, nt, M, N, k, expert, at;
 };
 
-template <int GROUP, int TILE_M>
+template <int GROUP>
 __device__ __forceinline__ void lay_out_experts(const GemmParams& p, const Experts& x) {
   const int E = p.experts;
   for (int e = threadIdx.x; e <= E; e += blockDim.x) x.row[e] = min(max(p.offsets[e], 0), p.rows);
@@ -225,8 +229,7 @@ __device__ __forceinline__ void lay_out_experts(const GemmParams& p, const Exper
       const int n = next - last;
       int mine = 0;
       if (e < E) {
-        if (GROUP == kColumnsByExpert) mine = p.m_tiles * ((n + p.tile_n - 1) / p.tile_n);
-        else if (GROUP == kRowsByExpert) mine = p.n_tiles * ((n + TILE_M - 1) / TILE_M);
+        if (columns_by_expert(GROUP)) mine = p.m_tiles * ((n + p.tile_n - 1) / p.tile_n);
         else mine = p.m_tiles * p.n_tiles;
       }
       int sum = mine;
@@ -256,25 +259,19 @@ __device__ __forceinline__ Tile find_tile(int t, const GemmParams& p, const Expe
       if (x.tile[mid] <= t) lo = mid;
       else hi = mid - 1;
     }
-    const int r = t - x.tile[lo], n = x.row[lo + 1] - x.row[lo], q = p.by_band(r);  // (by the tiles of the dimension that all experts share)
+    const int r = t - x.tile[lo], n = x.row[lo + 1] - x.row[lo], q = p.by_band(r);  // (by the tiles of a column of them)
     g.expert = lo;
     g.at = x.row[lo];
-    if constexpr (GROUP == kRowsByExpert) {
-      g.mt = q;
-      g.nt = r - q * p.n_tiles;
-      g.M = n;
-    } else {
-      g.nt = q;
-      g.mt = r - q * p.m_tiles;
-      if constexpr (GROUP == kColumnsByExpert) g.N = n;
-      else g.k = n;
-    }
+    g.nt = q;
+    g.mt = r - q * p.m_tiles;
+    if constexpr (columns_by_expert(GROUP)) g.N = n;
+    else g.k = n;
   }
   return g;
 }
 
 template <int KIND>
-__device__ __forceinline__ uint32_t make_idesc(bool sparse, bool b_mn_major, int a_fmt, int m, int n, bool acc_f16) {
+__device__ __forceinline__ uint32_t make_idesc(bool sparse, bool b_mn_major, int a_fmt, int m, int n, bool acc_f16, bool a_mn_major = false) {
   uint32_t d = 0;
   d |= (sparse ? 1u : 0u) << 2;
   d |= (KIND == 1 ? 2u : (acc_f16 ? 0u : 1u)) << 4;  // accumulator: int32 / fp32 / fp16
@@ -282,7 +279,8 @@ __device__ __forceinline__ uint32_t make_idesc(bool sparse, bool b_mn_major, int
   uint32_t fmt = (KIND == 0 || KIND == 3) ? (uint32_t)a_fmt : (KIND == 1 ? 1u : 2u);
   d |= fmt << 7;
   d |= fmt << 10;
-  d |= (b_mn_major ? 1u : 0u) << 16;               // A is always K-major
+  d |= (a_mn_major ? 1u : 0u) << 15;               // (of experts' gradients only)
+  d |= (b_mn_major ? 1u : 0u) << 16;
   d |= (uint32_t)(n >> 3) << 17;
   d |= (uint32_t)(m >> 4) << 24;
   return d;                                        // no negate, no saturate
@@ -951,14 +949,15 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   let_next_start();
   wait_for_stream();
   static_assert(GROUP == kOneProblem || (!kTall && !SPLIT && MBLK == 1), "experts: tiles of one m-block");
+  static_assert(!a_transposed(GROUP) || (KIND == 0 && !SPARSE && C::kABytes == kBlockM / C::kAtomElems * C::kBChunkBytes), "A with M contiguous: dense, 16-bit");
   if constexpr (GROUP != kOneProblem) {
-    lay_out_experts<GROUP, kBlockM * CTAS>(p, experts);
+    lay_out_experts<GROUP>(p, experts);
     num_tiles = experts.tile[p.experts];
   }
 
   // columns of a tile that are multiplied: those there are, up to the instruction's next multiple
   auto columns = [&](const Tile& g) -> int {
-    if constexpr (GROUP == kColumnsByExpert) {
+    if constexpr (columns_by_expert(GROUP)) {
       constexpr int step = one_byte_operands(KIND) ? 32 : 16;
       return min(tile_n, (g.N - g.nt * tile_n + step - 1) / step * step);
     } else {
@@ -1092,13 +1091,13 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         int col0 = nt * tile_n + (int)cta_rank * (n_eff / CTAS);  // first B row (N index)
         int row0 = first_row<CTAS, MBLK>(mt, (int)cta_rank, g.M);
         int meta_block = row0 / kBlockM;
+        if constexpr (GROUP == kColumnsTransposed) col0 += g.at;
         if constexpr (GROUP == kColumnsByExpert) {
           meta_block += g.expert * p.meta_blocks;
           row0 += g.expert * g.M;
           col0 += g.at;
         }
-        if constexpr (GROUP == kRowsByExpert) row0 += g.at;
-        const int k0 = GROUP == kKByExpert ? g.at & ~15 : 0;  // (a copy starts at a 16-byte boundary, wherever the expert does)
+        const int k0 = GROUP == kKByExpert ? g.at : 0;
         const int kb_end = GROUP == kKByExpert ? (g.k + C::kKPerStage - 1) / C::kKPerStage : last_kb;
         const uint32_t tx_bytes = (uint32_t)((C::kABytes + C::kEBytes + b_bytes) * CTAS);
         // implicit convolution: (image, row, column) of this CTA's first output pixel
@@ -1142,18 +1141,24 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
           if (cta_rank == 0) ptx::mbar_expect_tx(&sh->full[stage], tx_bytes);
           // both m-blocks' rows and metadata blocks are neighbours: one box each
           if (SPARSE) ptx::tma_load_3d<CTAS>(se, &map_e, full, 0, 16 * kb * C::kEBlocks, meta_block);
+          if constexpr (a_transposed(GROUP)) {
 #pragma unroll
-          for (int i = 0; i < C::kABoxes; ++i)
-            ptx::tma_load_2d<CTAS>(sa + i * MBLK * kBlockM * kAtomBytes, &map_a, full, k0 + (kb * C::kABoxes + i) * box_elems, row0);
+            for (int c = 0; c < kBlockM / C::kAtomElems; ++c) {
+              // (the weights of the experts are a third dimension: what is behind one expert's last row is zeros, not the next one's)
+              if constexpr (GROUP == kColumnsTransposed)
+                ptx::tma_load_3d<CTAS>(sa + c * C::kBChunkBytes, &map_a, full, row0 + c * C::kAtomElems, kb * C::kKPerStage, g.expert);
+              else
+                ptx::tma_load_2d<CTAS>(sa + c * C::kBChunkBytes, &map_a, full, row0 + c * C::kAtomElems, k0 + kb * C::kKPerStage);
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < C::kABoxes; ++i)
+              ptx::tma_load_2d<CTAS>(sa + i * MBLK * kBlockM * kAtomBytes, &map_a, full, (kb * C::kABoxes + i) * box_elems, row0);
+          }
           if (B_MN) {
             // B stored N-contiguous: boxes of 128 bytes along N x all k-rows of the stage
-            for (int c = 0; c < C::b_chunks(tile_n); ++c) {
-              // (the weights of the experts are a third dimension: what is behind one expert's last row is zeros, not the next one's)
-              if constexpr (GROUP == kRowsByExpert)
-                ptx::tma_load_3d<CTAS>(sb + c * C::kBChunkBytes, &map_b, full, col0 + c * C::kBChunkElems, kb * C::kKPerStage, g.expert);
-              else
-                ptx::tma_load_2d<CTAS>(sb + c * C::kBChunkBytes, &map_b, full, col0 + c * C::kBChunkElems, k0 + kb * C::kKPerStage);
-            }
+            for (int c = 0; c < C::b_chunks(tile_n); ++c)
+              ptx::tma_load_2d<CTAS>(sb + c * C::kBChunkBytes, &map_b, full, col0 + c * C::kBChunkElems, k0 + kb * C::kKPerStage);
           } else if (p.conv) {
             // k = (r * 3 + s) * C + c: a stage holds channels of one filter tap; rows = output pixels
 #pragma unroll
@@ -1195,7 +1200,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         const int n_eff = columns(g);
         const int live = live_blocks<CTAS, MBLK>(mt, g.M);  // m-blocks with rows (others are not multiplied)
         const int kb_end = GROUP == kKByExpert ? (g.k + C::kKPerStage - 1) / C::kKPerStage : last_kb;
-        const uint32_t idesc = make_idesc<KIND>(SPARSE, B_MN, p.a_fmt, kBlockM * CTAS, n_eff, KIND == 0 && p.acc_f16);
+        const uint32_t idesc = make_idesc<KIND>(SPARSE, B_MN, p.a_fmt, kBlockM * CTAS, n_eff, KIND == 0 && p.acc_f16, a_transposed(GROUP));
         // the MMAs of a k-block: A, B and metadata at sa, sb, se
         auto multiply = [&](int kb, uint32_t sa, uint32_t sb, uint32_t se) {
           // metadata columns alternate between two small tensor-memory buffers from k-block to k-block
@@ -1217,7 +1222,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             if (j >= live) break;
             const uint32_t d_tmem = tmem_base + (acc * MBLK + j) * BLOCK_N;
             const uint32_t e_tmem = e_base + j * 8;
-            const uint64_t da0 = ptx::smem_desc(sa + j * C::kABlockBytes, ptx::kLayoutSw128, 1024);
+            const uint64_t da0 = a_transposed(GROUP) ? ptx::smem_desc(sa, ptx::kLayoutSw128, 1024, C::kBChunkBytes) : ptx::smem_desc(sa + j * C::kABlockBytes, ptx::kLayoutSw128, 1024);
 #pragma unroll
             for (int k = 0; k < C::kMmasPerStage; ++k) {
               // (of an expert's last k-block only its own rows: what is behind them belongs to another)
@@ -1234,7 +1239,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                   ptx::mma_sparse<KIND, CTAS>(d_tmem, da, db, e_tmem + 2 * k, idesc, accumulate);
                 }
               } else {
-                const uint64_t da = ptx::desc_at(da0, (k >> 2) * kBlockM * kAtomBytes + (k & 3) * 32);
+                const uint64_t da = ptx::desc_at(da0, a_transposed(GROUP) ? k * C::kBKStepBytes : (k >> 2) * kBlockM * kAtomBytes + (k & 3) * 32);
                 const uint64_t db = ptx::desc_at(db0, B_MN ? k * C::kBKStepBytes : (k >> 2) * b_atom + (k & 3) * 32);
                 ptx::mma_dense<KIND, CTAS>(d_tmem, da, db, idesc, accumulate);
               }

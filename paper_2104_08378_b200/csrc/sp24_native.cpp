@@ -1020,16 +1020,20 @@ PyObject* expert_linear_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
     Result rx{Py_None, {}}, rw{Py_None, {}}, rb{Py_None, {}};
     const int status = unlocked([&]() -> int {
       const auto options = dy.t->options();
-      // dz (without an activation dy itself, where a product can take it), its transpose and the partial sums of the bias's gradient, in one allocation
+      // dz (without an activation dy itself, where a product can take it) and the partial sums of the bias's gradient, in one allocation
       const bool makes_dz = act != SP24_ACT_NONE || (uintptr_t)dy.p % 16 != 0 || dy.ld * 2 % 16 != 0;
-      const int64_t lddzt = (rows + 7) / 8 * 8, lddz = makes_dz ? M : dy.ld;
-      const size_t bytes = with_bias ? act_bytes(E, M, rows) : 0, matrix = ((size_t)lddzt * M * 2 + 255) / 256 * 256;
-      const at::Tensor scratch = at::empty({(int64_t)(matrix * (makes_dz ? 2 : 1) + bytes)}, options.dtype(at::kByte));
-      char* const pdzt = (char*)scratch.data_ptr();
-      void* const pdz = makes_dz ? pdzt + matrix : dy.p;
+      const int64_t lddz = makes_dz ? M : dy.ld;
+      const size_t bytes = with_bias ? act_bytes(E, M, rows) : 0, matrix = makes_dz ? ((size_t)rows * M * 2 + 255) / 256 * 256 : 0;
+      at::Tensor scratch;
+      char* room = nullptr;
+      if (matrix + bytes) {
+        scratch = at::empty({(int64_t)(matrix + bytes)}, options.dtype(at::kByte));
+        room = (char*)scratch.data_ptr();
+      }
+      void* const pdz = makes_dz ? room : dy.p;
       if (with_bias) rb.made = at::empty({E, M}, options.dtype(at::kFloat));
-      int st = act_fn((sp24_dtype)t, (sp24_act)act, E, M, rows, dy.p, dy.ld, z.p, z.ld, (const int32_t*)offsets, makes_dz ? pdz : nullptr, lddz, pdzt, lddzt,
-                      with_bias ? (float*)rb.made.data_ptr() : nullptr, with_bias ? pdzt + matrix * (makes_dz ? 2 : 1) : nullptr, bytes, stream);
+      int st = act_fn((sp24_dtype)t, (sp24_act)act, E, M, rows, dy.p, dy.ld, z.p, z.ld, (const int32_t*)offsets, makes_dz ? pdz : nullptr, lddz,
+                      with_bias ? (float*)rb.made.data_ptr() : nullptr, with_bias ? room + matrix : nullptr, bytes, stream);
       if (st != SP24_OK) return st;
       rx.made = at::empty({rows, K}, options);
       rw.made = at::empty({E, M, K}, options);
@@ -1038,7 +1042,7 @@ PyObject* expert_linear_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
       if (st != SP24_OK) return st;
       d.lda = K;
       d.ldx = x.ld;
-      return dw_fn(&d, pdzt, lddzt, x.p, (const int32_t*)offsets, meta, rw.made.data_ptr(), ws, ws_bytes, stream);
+      return dw_fn(&d, pdz, x.p, (const int32_t*)offsets, meta, rw.made.data_ptr(), ws, ws_bytes, stream);
     });
     if (status != SP24_OK) return PyLong_FromLong(status);
     return Py_BuildValue("(NNN)", rx.object(), rw.object(), rb.object());

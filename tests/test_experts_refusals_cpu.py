@@ -109,11 +109,11 @@ def test_linear(status, args):
     assert linear(**args) == status
 
 
-def gradient(which, ab=sp.F16, cd=sp.F16, E=4, M=64, K=64, rows=48, lda=64, ldx=64, ldd=64, lddzt=48, a=ONE, b=ONE, offsets=ONE, out=ONE, ws=ONE, ws_bytes=256):
+def gradient(which, ab=sp.F16, cd=sp.F16, E=4, M=64, K=64, rows=48, lda=64, ldx=64, ldd=64, a=ONE, b=ONE, offsets=ONE, out=ONE, ws=ONE, ws_bytes=256):
     d = ctypes.byref(sp.ExpertDesc(ab, cd, E, M, K, rows, lda, ldx, ldd, 0, 0, 1))
     if which == "dx":
         return sp.lib.sp24_expert_linear_dx(d, a, b, offsets, out, ws, ws_bytes, None)
-    return sp.lib.sp24_expert_linear_dw(d, a, lddzt, b, offsets, None, out, ws, ws_bytes, None)
+    return sp.lib.sp24_expert_linear_dw(d, a, b, offsets, None, out, ws, ws_bytes, None)
 
 
 @pytest.mark.parametrize("which", ["dx", "dw"])
@@ -126,26 +126,25 @@ def test_gradients(which, status, args):
 
 
 def test_gradients_own_strides():
-    assert gradient("dx", ldd=56) == gradient("dx", ldd=68) == gradient("dw", lddzt=40) == gradient("dw", lddzt=52) == 4
+    assert gradient("dx", ldd=56) == gradient("dx", ldd=68) == gradient("dw", ldd=56) == gradient("dw", ldd=68) == 4
     assert gradient("dx", rows=0, a=None) == 0
 
 
-def act_backward(t=sp.BF16, act=3, E=4, M=64, rows=48, dy=ONE, lddy=64, z=ONE, ldz=64, offsets=ONE, dz=ONE, lddz=64, dzt=ONE, lddzt=48, out=ONE, ws=ONE,
-                 ws_bytes=1 << 20):
-    return sp.lib.sp24_expert_act_backward(t, act, E, M, rows, dy, lddy, z, ldz, offsets, dz, lddz, dzt, lddzt, out, ws, ws_bytes, None)
+def act_backward(t=sp.BF16, act=3, E=4, M=64, rows=48, dy=ONE, lddy=64, z=ONE, ldz=64, offsets=ONE, dz=ONE, lddz=64, out=ONE, ws=ONE, ws_bytes=1 << 20):
+    return sp.lib.sp24_expert_act_backward(t, act, E, M, rows, dy, lddy, z, ldz, offsets, dz, lddz, out, ws, ws_bytes, None)
 
 
 @pytest.mark.parametrize("status,args", [
     (2, {"t": sp.I8}), (6, {"act": 9}), (3, {"E": 0}), (3, {"E": 1025}), (3, {"M": 0}), (3, {"rows": -1}), (1, {"dy": None}), (1, {"z": None}), (1, {"offsets": None}),
-    (4, {"lddy": 63}), (4, {"ldz": 63}), (4, {"lddz": 63}), (4, {"lddzt": 47}), (5, {"dy": ODD}), (5, {"out": ODD}), (5, {"dzt": ODD}), (7, {"ws": None}),
-    (7, {"ws_bytes": 64}), (7, {"ws": ctypes.c_void_p(4104)}), (0, {"out": None, "dz": None, "dzt": None})])
+    (4, {"lddy": 63}), (4, {"ldz": 63}), (4, {"lddz": 63}), (5, {"dy": ODD}), (5, {"out": ODD}), (5, {"dz": ODD}), (7, {"ws": None}),
+    (7, {"ws_bytes": 64}), (7, {"ws": ctypes.c_void_p(4104)}), (0, {"out": None, "dz": None})])
 def test_act_backward(status, args):
     assert act_backward(**args) == status
 
 
 def test_nothing_to_describe():
     assert sp.lib.sp24_expert_linear(None, None, None, None, None, None, None, None, 0, None) == 1
-    assert sp.lib.sp24_expert_linear_dx(None, None, None, None, None, None, 0, None) == sp.lib.sp24_expert_linear_dw(None, None, 8, None, None, None, None, None, 0, None) == 1
+    assert sp.lib.sp24_expert_linear_dx(None, None, None, None, None, None, 0, None) == sp.lib.sp24_expert_linear_dw(None, None, None, None, None, None, None, 0, None) == 1
 
 
 def refused(status, fn, *args, **kwargs):
