@@ -64,9 +64,9 @@ int64_t mean_rows(const sp24_expert_desc* d) {
 TileShape choose_expert_tile(const sp24_expert_desc* d, bool has_c, bool has_pre) {
   const int64_t mean = mean_rows(d), met = d->E < d->rows ? d->E : d->rows;
   const int cs = elem_bytes(d->cd_type), es = elem_bytes(d->ab_type);
-  const double k_blocks = (double)((d->K * es + 255) / 256) * (d->a_is_dense ? 2.0 : 1.0);
+  const double k_blocks = (double)((d->K * es + 255) / 256);
   const double store = (cs == 4 ? (has_c ? 2.0 : 1.0) : (has_c ? 1.4 : 0.6)) + (has_pre ? (cs == 4 ? 1.0 : 0.6) : 0.0);
-  const double weights = (double)met * d->M * d->K * (d->a_is_dense ? es : 0.5 * es + 0.125) / 6.6e6;
+  const double weights = (double)met * d->M * d->K * (0.5 * es + 0.125) / 6.6e6;
   TileShape best = {1, 128, 1, 32, 0};
   double least = 0.0;
   auto consider = [&](int ctas, int block_n, int tile_n, double tile) {
@@ -83,9 +83,32 @@ TileShape choose_expert_tile(const sp24_expert_desc* d, bool has_c, bool has_pre
   };
   for (int n = 32; n <= 128; n += 32) consider(1, 128, n, k_blocks * (0.2 + 0.00095 * n) + 0.1 + store * 0.01 * n);
   if (d->M <= 128) return best;
-  if (d->a_is_dense) consider(2, 256, 256, k_blocks * (0.165 + 0.00085 * 256) + 0.1 + store * 2.56);
-  else
-    for (int n = 64; n <= 224; n += 32) consider(2, 224, n, k_blocks * (0.165 + 0.00085 * n) + 0.1 + store * 0.01 * n);
+  for (int n = 64; n <= 224; n += 32) consider(2, 224, n, k_blocks * (0.165 + 0.00085 * n) + 0.1 + store * 0.01 * n);
+  return best;
+}
+
+// The same for dense weights (D and dX): M features of the result, K of the contraction.  Pairs of CTAs whatever the rows, if there are features for them; what a column
+// of a tile costs next to its 256 rows was set so that up to 160 columns, with which the ring has four stages (three from 192 on), are taken where there are a few rounds of
+// tiles and 256 where there are many.  Us, device, bf16 dX, widths 96, 128, 160, 256 and today's: 8 experts 2816 x 2048, 128 rows each 24, 25, 18, 20; 528: 60, 50, 54, 62;
+// 1024: 93, 86, 73, 90; 50 of 2336 x 1760, 16 rows 55, 56, 56, 58, 1024 479, 420, 422, 391.
+TileShape choose_dense_tile(const sp24_expert_desc* d, int64_t M, int64_t K) {
+  const int64_t mean = mean_rows(d), met = d->E < d->rows ? d->E : d->rows;
+  const int es = elem_bytes(d->ab_type), ctas = M > 128 ? 2 : 1, most = ctas == 2 ? 256 : 128;
+  const double k_blocks = (double)((K * es + 255) / 256), weights = (double)met * M * K * es / 6.6e6;
+  const int64_t rows = 128 * ctas, slots = sm_count() / ctas > 0 ? sm_count() / ctas : 1;
+  TileShape best = {ctas, most, 1, most, 0};
+  double least = 0.0;
+  for (int n = 64; n <= most; n += 32) {
+    const double full = (double)mean / n;
+    const double of_expert = full >= 1.0 ? full + 0.5 : full > 0.4 ? 1.0 + 0.25 * (full - 0.4) / 0.6 : 1.0;
+    const double rounds = (double)((M + rows - 1) / rows) * (double)met * of_expert / (double)slots;
+    const double time = (k_blocks * 0.0028 * (30 + n) + 0.5) * (rounds < 1.0 ? 1.0 : rounds + 0.3), way = weights * (1.0 + 0.07 * (of_expert - 1.0));
+    const double cost = time * time * time + way * way * way;
+    if (least == 0.0 || cost < least) {
+      least = cost;
+      best.tile_n = n;
+    }
+  }
   return best;
 }
 
@@ -134,7 +157,7 @@ extern "C" sp24_status sp24_expert_linear(const sp24_expert_desc* d, const sp24_
   p.beta = p.has_c ? 1.f : 0.f;
   const sp24_gemm_desc g = {d->ab_type, d->cd_type, d->M, d->rows, d->K, d->lda, d->ldx, d->ld_residual, d->ldd, SP24_COL_MAJOR, SP24_COL_MAJOR, SP24_COL_MAJOR,
                             d->a_is_dense};
-  TileShape tile = choose_expert_tile(d, e->residual != nullptr, e->pre != nullptr);
+  TileShape tile = d->a_is_dense ? choose_dense_tile(d, d->M, d->K) : choose_expert_tile(d, e->residual != nullptr, e->pre != nullptr);
   tile_override(&tile, d->a_is_dense != 0);
   SP24_RETURN_IF(tile.tile_n > tile.block_n || tile.tile_n % 32, SP24_ERR_UNSUPPORTED);
   return run(kColumnsByExpert, tile, !d->a_is_dense, &g, p, A, meta, X, stream);
@@ -164,8 +187,7 @@ extern "C" sp24_status sp24_expert_linear_dx(const sp24_expert_desc* d, const vo
   p.cd_col_major = 1;
   // W_e, transposed, times rows of dz: the tokens are columns as in the product itself, so that an expert's last tile is as wide as its rows ask for
   const sp24_gemm_desc g = {d->ab_type, d->cd_type, d->K, d->rows, d->M, d->lda, d->ldd, 0, d->ldx, SP24_COL_MAJOR, SP24_COL_MAJOR, SP24_COL_MAJOR, 1};
-  TileShape tile = {1, 128, 1, 128, 0};
-  if (mean_rows(d) > 128 && d->K > 128) tile = {2, 256, 1, 256, 0};
+  TileShape tile = choose_dense_tile(d, d->K, d->M);
   tile_override(&tile, true);
   SP24_RETURN_IF(tile.tile_n > tile.block_n || tile.tile_n % 32, SP24_ERR_UNSUPPORTED);
   return run(kColumnsTransposed, tile, false, &g, p, W, nullptr, dz, stream);

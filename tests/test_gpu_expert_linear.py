@@ -116,9 +116,15 @@ def test_every_width(sp, force_tile, tile, ab, cd):
 
 @pytest.mark.parametrize("ab", ["bf16", "i8"])
 def test_every_dense_width(sp, force_tile, ab):
-    for tile in ("1x64x1", "1x128x1", "2x128x1", "2x256x1"):
+    for tile in ("1x64x1", "1x128x1", "2x64x1", "2x128x1", "2x160x1", "2x224x1", "2x256x1"):
         force_tile(tile)
         check(sp, [255, 0, 256, 1, 257], 288, 416, ab, "bf16", "silu", 1, dense=True)
+
+
+@pytest.mark.parametrize("tile", ["1x32x1", "1x128x1", "2x64x1", "2x96x1", "2x160x1", "2x192x1", "2x256x1"])
+def test_every_width_of_the_gradient(sp, force_tile, tile):
+    force_tile(tile)
+    check_gradients(sp, [64, 0, 96, 16, 272], 160, 304, "bf16", "silu", 1)
 
 
 def test_the_residual_may_be_the_result(sp):
