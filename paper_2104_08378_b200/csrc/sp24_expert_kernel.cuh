@@ -17,7 +17,9 @@ sp24_status launch_group(const TileShape& tile, const sp24_gemm_desc* d, const G
   const int cs = elem_bytes(d->cd_type), es = elem_bytes(d->ab_type);
   const uint32_t atom_elems = kAtomBytes / es;
   const uint64_t E = (uint64_t)p.experts, rows = (uint64_t)p.rows, a_cols = (uint64_t)(SPARSE ? d->K / 2 : d->K);
-  p.epi_bytes = kEpiWarps * 2048;
+  // twelve epilogue warps for the weights' gradients, whose k-blocks are the few of an expert's rows (us, bf16 8 experts 2816 x 2048, 4224 rows, with the pattern: eight 62, 56)
+  constexpr int kWarps = GROUP == kKByExpert ? 12 : kEpiWarps;
+  p.epi_bytes = kWarps * 2048;
   p.table_bytes = (8 * (p.experts + 1) + 1023) / 1024 * 1024;
   p.kps = C::k_blocks_of_a_stage(tile_n, p.epi_bytes + p.table_bytes, (int64_t)a_cols, false);
   p.stages = C::ring_stages(C::stage_bytes(tile_n) * p.kps, p.epi_bytes + p.table_bytes);
@@ -68,7 +70,7 @@ sp24_status launch_group(const TileShape& tile, const sp24_gemm_desc* d, const G
   }
   using Kernel = void (*)(CUtensorMap, CUtensorMap, CUtensorMap, CUtensorMap, CUtensorMap, GemmParams);
   Kernel forms[4] = {};  // [with C][bytes]
-#define SP24_FORM(CS_, C_) forms[2 * C_ + (CS_ >> 2)] = gemm_kernel<KIND, SPARSE, BLOCK_N, CTAS, 1, kBMn, CS_, columns_by_expert(GROUP), C_, false, kEpiWarps, kLinear, GROUP>;
+#define SP24_FORM(CS_, C_) forms[2 * C_ + (CS_ >> 2)] = gemm_kernel<KIND, SPARSE, BLOCK_N, CTAS, 1, kBMn, CS_, columns_by_expert(GROUP), C_, false, kWarps, kLinear, GROUP>;
   SP24_FORM(2, false)
   if constexpr (kLinear) { SP24_FORM(2, true) SP24_FORM(4, false) SP24_FORM(4, true) }
 #undef SP24_FORM
@@ -87,7 +89,7 @@ sp24_status launch_group(const TileShape& tile, const sp24_gemm_desc* d, const G
   }
   int64_t clusters = sm_count() / CTAS;
   if (clusters > tiles) clusters = tiles;
-  return launch_overlapped(kernel, dim3((unsigned)(clusters * CTAS)), dim3(kNumThreads), C::kSmemBytes, stream, CTAS, map_a, map_b, map_e, map_a, map_a, p);
+  return launch_overlapped(kernel, dim3((unsigned)(clusters * CTAS)), dim3(32 * (kFirstEpiWarp + kWarps)), C::kSmemBytes, stream, CTAS, map_a, map_b, map_e, map_a, map_a, p);
 }
 
 template <int KIND>
