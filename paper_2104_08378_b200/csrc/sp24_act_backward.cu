@@ -16,25 +16,9 @@ struct ActGradParams {
   float* partial;  // sums over the rows of a tile (over_rows: [row tiles][cols]) or over its columns ([column tiles][rows]); or null
   int64_t lddy, ldz, lddz, lddzt;
   int32_t over_rows;
-  const int32_t* offsets;  // EXPERTS: see sp24_expert_act_backward
+  const int32_t* offsets;  // see sp24_expert_act_backward
   int32_t experts;
 };
-
-// Rows [lo, hi) of expert e, as the products take them.
-__device__ __forceinline__ void rows_of_expert(const ActGradParams& p, int e, int64_t& lo, int64_t& hi) {
-  lo = min(max((int64_t)p.offsets[e], (int64_t)0), p.rows);
-  hi = max(lo, min((int64_t)p.offsets[e + 1], p.rows));
-}
-// The first expert whose rows end behind row r, E if there is none (offsets in order).
-__device__ __forceinline__ int expert_of_row(const ActGradParams& p, int64_t r) {
-  int lo = 0, hi = p.experts;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (p.offsets[mid + 1] > r) hi = mid;
-    else lo = mid + 1;
-  }
-  return lo;
-}
 
 // 16-bit types, all rows (of dzt too) whole vectors at 16-byte boundaries.  A block to a tile of 128 x 128 (rows of 256 bytes both ways; of 64 x 64 where those
 // would leave SMs idle: 128 x 4096 5.4 -> 3.6 us), transposed on its way out of
@@ -43,13 +27,11 @@ __device__ __forceinline__ int expert_of_row(const ActGradParams& p, int64_t r) 
 // u ^ (2 (m >> 3 & 3) + (m & 1)): the eight rows of a matrix are in different banks.
 // dz = dy act'(z) is needed in both orders, and reading dy and z once for both is what the tile is for.  Bound by HBM and, with GELU, the arithmetic of the slope:
 // bf16 4096 x 8192 with the bias 52 us = 5.1 TB/s (ReLU 46; by elements 125, tiles of 64 x 64 62); three blocks to an SM instead of two spill (75).
-// EXPERTS: dz in its own order only, and the bias's gradient of each expert's rows.  Tile i of the rows has a partial sum of its own for every expert that it meets, in row i + (expert) of
-// `partial`, which no other tile and expert share.
-template <typename T, int ACT, int kWide, bool EXPERTS = false>
+template <typename T, int ACT, int kWide>
 __global__ void __launch_bounds__(4 * kWide) act_grad_tile_kernel(const ActGradParams p) {
   constexpr int kUnits = kWide / 8, kWideThreads = 4 * kWide;
   constexpr int kPasses = kWide * kUnits / kWideThreads, kRows = kWide / kPasses;
-  __shared__ uint4 tile[EXPERTS ? 1 : kWide * kUnits];
+  __shared__ uint4 tile[kWide * kUnits];
   __shared__ float over[kWideThreads / 32][kWide];  // sums over the rows of each warp
   const int64_t col_tiles = (p.cols + kWide - 1) / kWide;
   const int64_t row0 = (int64_t)(blockIdx.x / col_tiles) * kWide, col0 = (int64_t)(blockIdx.x % col_tiles) * kWide;
@@ -57,9 +39,6 @@ __global__ void __launch_bounds__(4 * kWide) act_grad_tile_kernel(const ActGradP
   const int64_t c = col0 + 8 * u;
   wait_for_stream();
   uint4 dy[kPasses] = {}, z[kPasses] = {};
-  // EXPERTS: the first expert whose rows end behind row0, by as many threads as there are experts while the tile is on its way
-  int first_expert = 0, end_of_mine = 0;
-  if (EXPERTS && p.partial && threadIdx.x < p.experts) end_of_mine = p.offsets[threadIdx.x + 1];
 #pragma unroll
   for (int v = 0; v < kPasses; ++v)
     if (const int64_t r = row0 + m0 + kRows * v; r < p.rows && c < p.cols) dy[v] = ld_stream(static_cast<const T*>(p.dy) + r * p.lddy + c);
@@ -67,11 +46,6 @@ __global__ void __launch_bounds__(4 * kWide) act_grad_tile_kernel(const ActGradP
 #pragma unroll
     for (int v = 0; v < kPasses; ++v)
       if (const int64_t r = row0 + m0 + kRows * v; r < p.rows && c < p.cols) z[v] = ld_stream(static_cast<const T*>(p.z) + r * p.ldz + c);
-  }
-  if (EXPERTS && p.partial) {
-    first_expert = __syncthreads_count(threadIdx.x < p.experts && end_of_mine <= row0);
-    for (int e = kWideThreads; e < p.experts; e += kWideThreads)
-      first_expert += __syncthreads_count(e + threadIdx.x < p.experts && p.offsets[e + threadIdx.x + 1] <= row0);
   }
   Pairs<T> sums = {};
 #pragma unroll
@@ -91,7 +65,7 @@ __global__ void __launch_bounds__(4 * kWide) act_grad_tile_kernel(const ActGradP
     }
     const uint4 packed = pack<T>(d);
     if (p.dz && r < p.rows && c < p.cols) *reinterpret_cast<uint4*>(static_cast<T*>(p.dz) + r * p.lddz + c) = packed;
-    if (!EXPERTS) tile[m * kUnits + (u ^ (2 * (m >> 3 & 3) + (m & 1)))] = packed;
+    tile[m * kUnits + (u ^ (2 * (m >> 3 & 3) + (m & 1)))] = packed;
     if (p.partial && p.over_rows) {
 #pragma unroll
       for (int n = 0; n < 4; ++n) sums[n] = make_float2(sums[n].x + d[n].x, sums[n].y + d[n].y);
@@ -102,7 +76,7 @@ __global__ void __launch_bounds__(4 * kWide) act_grad_tile_kernel(const ActGradP
       if (u == 0 && r < p.rows) p.partial[col0 / kWide * p.rows + r] = s;
     }
   }
-  auto sum_over_warp = [&] {
+  if (p.partial && p.over_rows) {
 #pragma unroll
     for (int i = kUnits; i < 32; i *= 2)
 #pragma unroll
@@ -114,17 +88,9 @@ __global__ void __launch_bounds__(4 * kWide) act_grad_tile_kernel(const ActGradP
 #pragma unroll
       for (int n = 0; n < 4; ++n) *reinterpret_cast<float2*>(&over[warp][8 * u + 2 * n]) = sums[n];
     }
-  };
-  auto sum_over_warps = [&](int64_t at) {  // to row `at` of the partial sums
-    if (threadIdx.x >= kWide) return;
-    float s = over[0][threadIdx.x];
-#pragma unroll
-    for (int w = 1; w < kWideThreads / 32; ++w) s += over[w][threadIdx.x];
-    if (col0 + threadIdx.x < p.cols) p.partial[at * p.cols + col0 + threadIdx.x] = s;
-  };
-  if (p.partial && p.over_rows) sum_over_warp();
+  }
   __syncthreads();
-  if (!EXPERTS && p.dzt) {
+  if (p.dzt) {
     static_assert(kWideThreads / 32 == kUnits, "a warp to a unit: eight columns");
     const int i = lane >> 3, j = (lane & 7) >> 1, b = lane & 1;  // this lane's row of matrix i for ldmatrix
     const int64_t col = col0 + 8 * warp + (lane >> 2);
@@ -137,44 +103,11 @@ __global__ void __launch_bounds__(4 * kWide) act_grad_tile_kernel(const ActGradP
       if (col < p.cols && r < p.rows) *reinterpret_cast<uint4*>(static_cast<T*>(p.dzt) + col * p.lddzt + r) = make_uint4(x[0], x[1], x[2], x[3]);
     }
   }
-  if (!EXPERTS) {
-    if (p.partial && p.over_rows) sum_over_warps(row0 / kWide);
-  } else if (p.partial) {
-    // The sums above are of all rows of the tile, as they are wanted where they all belong to one expert.  Elsewhere they are made again, expert by expert.
-    const int64_t end = min(p.rows, row0 + kWide);
-    int64_t lo = 0, hi = 0;
-    for (int e = first_expert; e < p.experts; ++e) {
-      rows_of_expert(p, e, lo, hi);
-      if (lo >= end) break;
-      if (hi <= lo) continue;
-      if (lo <= row0 && hi >= end) {
-        sum_over_warps(row0 / kWide + e);
-        break;
-      }
+  if (p.partial && p.over_rows && threadIdx.x < kWide) {
+    float s = over[0][threadIdx.x];
 #pragma unroll
-      for (int n = 0; n < 4; ++n) sums[n] = make_float2(0.f, 0.f);
-      for (int v = 0; v < kPasses; ++v) {
-        const int64_t r = row0 + m0 + kRows * v;
-        if (r < lo || r >= hi || r >= end || c >= p.cols) continue;
-        Pairs<T> d, f;
-        unpack<T>(*reinterpret_cast<const uint4*>(static_cast<const T*>(p.dy) + r * p.lddy + c), d);
-        if (ACT != SP24_ACT_NONE) {
-          unpack<T>(*reinterpret_cast<const uint4*>(static_cast<const T*>(p.z) + r * p.ldz + c), f);
-#pragma unroll
-          for (int n = 0; n < 4; ++n) {
-            float2 slope;
-            act_and_slope<ACT>(f[n], &slope);
-            d[n] = mul2(d[n], slope);
-          }
-        }
-#pragma unroll
-        for (int n = 0; n < 4; ++n) sums[n] = make_float2(sums[n].x + d[n].x, sums[n].y + d[n].y);
-      }
-      __syncthreads();  // (the sums in shared memory have been read)
-      sum_over_warp();
-      __syncthreads();
-      sum_over_warps(row0 / kWide + e);
-    }
+    for (int w = 1; w < kWideThreads / 32; ++w) s += over[w][threadIdx.x];
+    if (col0 + threadIdx.x < p.cols) p.partial[row0 / kWide * p.cols + col0 + threadIdx.x] = s;
   }
 }
 
@@ -215,6 +148,88 @@ __global__ void __launch_bounds__(256) act_grad_kernel(const ActGradParams p) {
   }
 }
 
+// ---- experts ----------------------------------------------------------------------------------------------------------
+// Rows [lo, hi) of expert e, as the products take them.
+__device__ __forceinline__ void rows_of_expert(const ActGradParams& p, int e, int64_t& lo, int64_t& hi) {
+  lo = min(max((int64_t)p.offsets[e], (int64_t)0), p.rows);
+  hi = max(lo, min((int64_t)p.offsets[e + 1], p.rows));
+}
+// The first expert whose rows end behind row r, E if there is none (offsets in order).
+__device__ __forceinline__ int expert_of_row(const ActGradParams& p, int64_t r) {
+  int lo = 0, hi = p.experts;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (p.offsets[mid + 1] > r) hi = mid;
+    else lo = mid + 1;
+  }
+  return lo;
+}
+
+// dz, and the bias's gradient of each expert's rows: tile i of kTile rows has a partial sum of its own for every expert that it meets, in row i + (expert) of
+// `partial`, which no other tile and expert share.  16-bit types, rows of whole vectors at 16-byte boundaries.  The tile's values go through shared memory in FP32, where a
+// column's sum may end at any row.  Bound by HBM and the arithmetic of the slope: us, device, bf16 8192 x 4096 in 8 experts, GELU 46, SiLU 44, without the sums 35 (floor 31);
+// 2048 x 4096 in 64 18.5 (with sums over the lanes of a tile of 128 x 128, and once more from dy and z for each expert of a tile that several share, 50, 45, 37 and 32).
+template <typename T, int ACT>
+__global__ void __launch_bounds__(256) expert_act_grad_kernel(const ActGradParams p) {
+  constexpr int kUnits = kTile / 8, kPasses = kTile * kUnits / 256, kRows = kTile / kPasses;
+  __shared__ __align__(16) float tile[kTile][kTile + 4];
+  __shared__ float over[4][kTile];
+  const int64_t col_tiles = (p.cols + kTile - 1) / kTile;
+  const int64_t row0 = (int64_t)(blockIdx.x / col_tiles) * kTile, col0 = (int64_t)(blockIdx.x % col_tiles) * kTile;
+  const int u = threadIdx.x % kUnits, m0 = threadIdx.x / kUnits;
+  const int64_t c = col0 + 8 * u;
+  wait_for_stream();
+  uint4 dy[kPasses] = {}, z[kPasses] = {};
+#pragma unroll
+  for (int v = 0; v < kPasses; ++v)
+    if (const int64_t r = row0 + m0 + kRows * v; r < p.rows && c < p.cols) dy[v] = ld_stream(static_cast<const T*>(p.dy) + r * p.lddy + c);
+  if (ACT != SP24_ACT_NONE) {
+#pragma unroll
+    for (int v = 0; v < kPasses; ++v)
+      if (const int64_t r = row0 + m0 + kRows * v; r < p.rows && c < p.cols) z[v] = ld_stream(static_cast<const T*>(p.z) + r * p.ldz + c);
+  }
+#pragma unroll
+  for (int v = 0; v < kPasses; ++v) {
+    const int m = m0 + kRows * v;
+    const int64_t r = row0 + m;
+    Pairs<T> d, f;
+    unpack<T>(dy[v], d);
+    unpack<T>(z[v], f);
+    if (ACT != SP24_ACT_NONE) {
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        float2 slope;
+        act_and_slope<ACT>(f[n], &slope);
+        d[n] = mul2(d[n], slope);
+      }
+    }
+    if (p.dz && r < p.rows && c < p.cols) *reinterpret_cast<uint4*>(static_cast<T*>(p.dz) + r * p.lddz + c) = pack<T>(d);
+    if (p.partial) {
+      *reinterpret_cast<float4*>(&tile[m][8 * u]) = make_float4(d[0].x, d[0].y, d[1].x, d[1].y);
+      *reinterpret_cast<float4*>(&tile[m][8 * u + 4]) = make_float4(d[2].x, d[2].y, d[3].x, d[3].y);
+    }
+  }
+  if (!p.partial) return;
+  int e = 0;  // the first expert whose rows end behind row0
+  for (int i = 0; i < p.experts; i += 256) e += __syncthreads_count(i + threadIdx.x < p.experts && p.offsets[i + threadIdx.x + 1] <= row0);
+  const int64_t end = min(p.rows, row0 + kTile);
+  const int x = threadIdx.x % kTile, y = threadIdx.x / kTile;
+  for (; e < p.experts; ++e) {
+    int64_t lo, hi;
+    rows_of_expert(p, e, lo, hi);
+    if (lo >= end) break;
+    if (hi <= lo) continue;
+    const int first = max((int)(max(lo, row0) - row0), y * (kTile / 4)), last = min((int)(min(hi, end) - row0), (y + 1) * (kTile / 4));
+    float sum = 0.f;
+#pragma unroll 8
+    for (int m = first; m < last; ++m) sum += tile[m][x];
+    over[y][x] = sum;
+    __syncthreads();
+    if (y == 0 && col0 + x < p.cols) p.partial[(row0 / kTile + e) * p.cols + col0 + x] = (over[0][x] + over[1][x]) + (over[2][x] + over[3][x]);
+    __syncthreads();
+  }
+}
+
 // The partial sums of the experts' rows for any type, size and alignment: tiles of kTile rows as above.
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256) expert_sums_kernel(const ActGradParams p) {
@@ -247,7 +262,7 @@ __global__ void __launch_bounds__(256) expert_sums_kernel(const ActGradParams p)
 }
 
 // An expert's partial sums added up, tile after tile: four tiles side by side, so that a long chain of loads is a quarter as long.
-__global__ void __launch_bounds__(256) expert_bias_kernel(const ActGradParams p, int edge, float* dbias) {
+__global__ void __launch_bounds__(256) expert_bias_kernel(const ActGradParams p, float* dbias) {
   __shared__ float over[4][kTile];
   wait_for_stream();
   const int x = threadIdx.x % kTile, y = threadIdx.x / kTile, e = blockIdx.y;
@@ -256,7 +271,7 @@ __global__ void __launch_bounds__(256) expert_bias_kernel(const ActGradParams p,
   rows_of_expert(p, e, lo, hi);
   float sum = 0.f;
   if (hi > lo && c < p.cols)
-    for (int64_t i = lo / edge + y; i <= (hi - 1) / edge; i += 4) sum += p.partial[(i + e) * p.cols + c];
+    for (int64_t i = lo / kTile + y; i <= (hi - 1) / kTile; i += 4) sum += p.partial[(i + e) * p.cols + c];
   over[y][x] = sum;
   __syncthreads();
   if (y == 0 && c < p.cols) dbias[(int64_t)e * p.cols + c] = (over[0][x] + over[1][x]) + (over[2][x] + over[3][x]);
@@ -341,8 +356,7 @@ extern "C" sp24_status sp24_expert_act_backward(sp24_dtype t, sp24_act act, int6
   if (!dbias && (rows == 0 || !dz)) return SP24_OK;
   const bool whole = t != SP24_F32 && M % 8 == 0 && whole_rows(dy, rows, lddy, 2, 16) && (!reads_z || whole_rows(z, rows, ldz, 2, 16)) &&
                      whole_rows(dz, rows, lddz, 2, 16);
-  const bool wide = whole && (rows + 127) / 128 * ((M + 127) / 128) >= 2 * sm_count();
-  const int64_t edge = wide ? 2 * kTile : kTile, row_tiles = (rows + edge - 1) / edge, col_tiles = (M + edge - 1) / edge;
+  const int64_t row_tiles = (rows + kTile - 1) / kTile, col_tiles = (M + kTile - 1) / kTile;
   SP24_RETURN_IF(row_tiles * col_tiles > 0x7fffffff, SP24_ERR_SHAPE);
   sp24_status st = check_arch();
   SP24_RETURN_IF(st != SP24_OK, st);
@@ -355,9 +369,7 @@ extern "C" sp24_status sp24_expert_act_backward(sp24_dtype t, sp24_act act, int6
       return with_act(act, [&](auto a) {
         constexpr int kAct = decltype(a)::value;
         if constexpr (sizeof(T) == 2)
-          if (whole)
-            return launch_overlapped(wide ? act_grad_tile_kernel<T, kAct, 2 * kTile, true> : act_grad_tile_kernel<T, kAct, kTile, true>, grid, dim3((unsigned)(4 * edge)),
-                                     0, s, 1, p);
+          if (whole) return launch_overlapped(expert_act_grad_kernel<T, kAct>, grid, dim3(256), 0, s, 1, p);
         ActGradParams q = p;
         q.partial = nullptr;
         sp24_status done = SP24_OK;
@@ -368,5 +380,5 @@ extern "C" sp24_status sp24_expert_act_backward(sp24_dtype t, sp24_act act, int6
     });
     SP24_RETURN_IF(st != SP24_OK || !dbias, st);
   }
-  return launch_overlapped(expert_bias_kernel, dim3((unsigned)((M + kTile - 1) / kTile), (unsigned)E), dim3(256), 0, s, 1, p, (int)edge, dbias);
+  return launch_overlapped(expert_bias_kernel, dim3((unsigned)((M + kTile - 1) / kTile), (unsigned)E), dim3(256), 0, s, 1, p, dbias);
 }
