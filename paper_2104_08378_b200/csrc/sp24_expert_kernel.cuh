@@ -36,6 +36,7 @@ sp24_status launch_group(const TileShape& tile, const sp24_gemm_desc* d, const G
   if (columns_by_expert(GROUP)) tiles = p.m_tiles * (p.rows / tile_n + met);
   else tiles = (int64_t)p.m_tiles * p.n_tiles * p.experts;
   SP24_RETURN_IF(tiles >= int64_t(1) << 31, SP24_ERR_SHAPE);
+  if (GROUP == kKByExpert) p.by_expert = FastDiv::by((uint32_t)(p.m_tiles * p.n_tiles));
   const uint32_t b_box_rows = (uint32_t)C::b_rows(tile_n);
   CUtensorMap map_a, map_b, map_e;
   sp24_status st;

@@ -89,6 +89,7 @@ struct GemmParams {
   // the weights' gradient: metadata of the weights (TCGEN05, 16-bit types), whose left out entries become zeros, or null, and its 128-column blocks
   const uint8_t* keep;
   int32_t keep_kb;
+  FastDiv by_expert;  // tiles of an expert's weights' gradient
 };
 
 constexpr int kSwizzle128Atom32 = 1280;

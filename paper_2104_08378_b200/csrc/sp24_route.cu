@@ -631,15 +631,15 @@ __global__ void __launch_bounds__(32 * kChunkWarps) route_chunks_kernel(const Ro
 #pragma unroll
   for (int v = 0; v < V; v += 4) *reinterpret_cast<float4*>(mine + v) = make_float4(c[v], c[v + 1], c[v + 2], c[v + 3]);
   auto largest_of_eight = [](const float4& a, const float4& b) { return fmaxf(fmaxf(fmaxf(a.x, a.y), fmaxf(a.z, a.w)), fmaxf(fmaxf(b.x, b.y), fmaxf(b.z, b.w))); };
+#pragma unroll
+  for (int i = 0; i < S; ++i)
+    best[i] = largest_of_eight(make_float4(c[8 * i], c[8 * i + 1], c[8 * i + 2], c[8 * i + 3]), make_float4(c[8 * i + 4], c[8 * i + 5], c[8 * i + 6], c[8 * i + 7]));
   auto largest = [&] {
     float m = best[0];
 #pragma unroll
     for (int i = 1; i < S; ++i) m = fmaxf(m, best[i]);
     return m;
   };
-#pragma unroll
-  for (int i = 0; i < S; ++i)
-    best[i] = largest_of_eight(make_float4(c[8 * i], c[8 * i + 1], c[8 * i + 2], c[8 * i + 3]), make_float4(c[8 * i + 4], c[8 * i + 5], c[8 * i + 6], c[8 * i + 7]));
   float lane_best = kept ? largest() : -INFINITY;
   int chosen = -1;  // lane i of the token: the i-th
   float last = INFINITY;
