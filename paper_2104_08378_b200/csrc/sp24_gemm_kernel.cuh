@@ -581,10 +581,12 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
     const uint32_t columns = 1u << (lane & 3) | 1u << (lane >> 2 & 3);
     selectors = (columns & 1u ? 0x10u : 0x44u) | (columns & 2u ? 0x3200u : 0x4400u) | (columns & 4u ? 0x100000u : 0x440000u) | (columns & 8u ? 0x32000000u : 0x44000000u);
   }
-  auto load_keep = [&](int t) {
+  Tile ahead = {};
+  auto look_ahead = [&](int t) {
     if constexpr (GROUP == kKByExpert) {
-      if (p.keep && t < num_tiles) {
-        const Tile g = find_tile<GROUP>(t, p, experts);
+      if (t >= num_tiles) return;
+      const Tile g = ahead = find_tile<GROUP>(t, p, experts);
+      if (p.keep) {
         const int row = first_row<CTAS, MBLK>(g.mt, cta_rank, g.M) + q * 32 + lane;
         const uint8_t* at = p.keep + (int64_t)(g.expert * p.meta_blocks + (row >> 7)) * p.keep_kb * 2048 + 16 * (row & 7) + 2 * (row >> 3 & 1) + 256 * (row >> 4 & 7);
 #pragma unroll
@@ -599,11 +601,11 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
       }
     }
   };
-  load_keep(cluster_id);
+  look_ahead(cluster_id);
   int acc = 0;
   uint32_t acc_phase = 0;
   for (int t = cluster_id; t < num_tiles && !sh->abort; t += num_clusters) {
-    const Tile g = find_tile<GROUP>(t, p, experts);
+    const Tile g = GROUP == kKByExpert ? ahead : find_tile<GROUP>(t, p, experts);
     const int mt = g.mt, nt = g.nt;
     bool no_sums = false;  // (no k: the accumulators hold nothing)
     uint32_t instead = 0;
@@ -837,7 +839,7 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
     if constexpr (GROUP == kKByExpert) {
 #pragma unroll
       for (int i = 0; i < kTileBoxes; ++i) keep[i] = low[i] | high[i] << 16;  // (joined here: a use of them before would wait for HBM)
-      load_keep(t + num_clusters);
+      look_ahead(t + num_clusters);
     }
     if (any) {
       load_scale(row_q + j * kBlockM);
