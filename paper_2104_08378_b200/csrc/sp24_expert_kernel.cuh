@@ -17,7 +17,8 @@ sp24_status launch_group(const TileShape& tile, const sp24_gemm_desc* d, const G
   const int cs = elem_bytes(d->cd_type), es = elem_bytes(d->ab_type);
   const uint32_t atom_elems = kAtomBytes / es;
   const uint64_t E = (uint64_t)p.experts, rows = (uint64_t)p.rows, a_cols = (uint64_t)(SPARSE ? d->K / 2 : d->K);
-  // twelve epilogue warps for the weights' gradients, whose k-blocks are the few of an expert's rows (us, bf16 8 experts 2816 x 2048, 4224 rows, with the pattern: eight 62, 56)
+  // twelve epilogue warps for the weights' gradients, whose k-blocks are the few of an expert's rows (us, bf16, with the pattern, eight, twelve and sixteen: 50 experts
+  // 2336 x 1760, 656 rows 119, 104, 142; 8 of 2048 x 1408, 4224 rows 30, 26, 26)
   constexpr int kWarps = GROUP == kKByExpert ? 12 : kEpiWarps;
   p.epi_bytes = kWarps * 2048;
   p.table_bytes = (8 * (p.experts + 1) + 1023) / 1024 * 1024;
