@@ -383,10 +383,11 @@ __device__ __forceinline__ void route_token(const RouteParams& p, int64_t t, int
       const uint2 here = lane < candidates ? mine_of[lane] : make_uint2(0, 0);
       mine = lane < candidates ? (int)here.y : -1;
       if (BIAS) {
-        const uint2 next = lane + 1 < candidates ? mine_of[lane + 1] : make_uint2(0, 0);
-        bool doubt = lane < p.k && lane + 1 < candidates && key_value(here.x) - key_value(next.x) <= near;
+        // A chosen one against the one before, all that are left against the last chosen: there may be equals of it before one that it is too close to.
+        const uint2 before = lane > 0 && lane < candidates ? mine_of[min(lane, p.k) - 1] : make_uint2(0, 0);
+        bool doubt = lane > 0 && lane < candidates && key_value(before.x) - key_value(here.x) <= near;
         // (the same logit under the same bias: a tie, whatever the arithmetic)
-        if (doubt) doubt = !(logit<T>(row, here.y) == logit<T>(row, next.y) && p.bias[here.y] == p.bias[next.y]);
+        if (doubt) doubt = !(logit<T>(row, here.y) == logit<T>(row, before.y) && p.bias[here.y] == p.bias[before.y]);
         if (__any_sync(~0u, doubt)) mine = order64<T, V>(p, row, top, lane, candidates, mine);
       }
       __syncwarp();
