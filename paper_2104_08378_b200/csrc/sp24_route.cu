@@ -941,7 +941,11 @@ extern "C" sp24_status sp24_route(sp24_dtype t, int64_t T, int64_t E, const void
   p.groups = groups; p.group_experts = (int)(E / groups); p.top_groups = top_groups;
   p.group_parts = 1;
   while (2 * p.group_parts * groups <= 32) p.group_parts *= 2;
-  p.group_stride = p.group_experts + ((p.group_parts - p.group_experts) & 31);  // (each group's lanes in banks of their own)
+  // Each group's lanes in banks of their own, but for the few shapes (E above 780, groups of 34 to 44, 67 or 68) whose rows would ask for more than
+  // the shared memory that a kernel has without an opt-in.
+  p.group_stride = p.group_experts + ((p.group_parts - p.group_experts) & 31);
+  constexpr size_t kStatic = kRouteWarps * (kMostChosen * sizeof(int32_t) + 32 * sizeof(uint2));  // (route_kernel's arrays)
+  if (kRouteWarps * groups * p.group_stride * sizeof(float) + kStatic > 48 * 1024) p.group_stride = p.group_experts;
   p.sigmoid = score == SP24_SCORE_SIGMOID; p.top2 = group_score == SP24_GROUP_TOP2 && p.group_experts > 1 ? 1 : 0;
   p.renorm = renorm != 0; p.scale = scale;
   p.logits = logits; p.bias = bias; p.weights = weights; p.experts = experts;
