@@ -593,7 +593,7 @@ __device__ __forceinline__ void epilogue_direct(const GemmParams& p, Shared* sh,
         for (int i = 0; i < kTileBoxes; ++i) {
           const int sc = turn + i * (WARPS / 4), col = g.nt * p.tile_n + sc * kCols;
           if (row < g.M && sc * kCols < p.tile_n && col < g.N) {
-            const uint8_t* of_box = at + (col >> 7) * 2048 + 4 * (col >> 5 & 3);
+            const uint8_t* of_box = at + (int64_t)(col >> 7) * 2048 + 4 * (col >> 5 & 3);
             low[i] = *reinterpret_cast<const uint16_t*>(of_box);
             high[i] = *reinterpret_cast<const uint16_t*>(of_box + 128);
           }
