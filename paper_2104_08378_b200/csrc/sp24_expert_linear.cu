@@ -41,12 +41,13 @@ sp24_status run(int group, TileShape tile, bool sparse, const sp24_gemm_desc* d,
   return launch_experts<0>(group, tile, sparse, d, p, A, meta, B, s);
 }
 
-// Tests and benchmarks: the shape that sp24_set_tile_override names, of any number of columns (whole 32) that a built one has.
-void tile_override(TileShape* t, bool dense) {
+// Tests and benchmarks: the shape that sp24_set_tile_override names, of any number of columns (whole 32) that a built one has; ctas 0: none is named.
+TileShape forced_shape(bool dense) {
   int ctas, columns, mblk;
   forced_tile(&ctas, &columns, &mblk);
-  if (ctas) *t = {ctas, ctas == 1 ? 128 : dense ? 256 : 224, mblk, columns, 0};
+  return {ctas, ctas == 1 ? 128 : dense ? 256 : 224, mblk, columns, 0};
 }
+bool is_built(const TileShape& t) { return (t.ctas == 1 || t.ctas == 2) && t.mblk == 1 && t.tile_n >= 32 && t.tile_n <= t.block_n && t.tile_n % 32 == 0; }
 
 // Rows of an expert with rows, in the mean: what the tiles are chosen by.
 int64_t mean_rows(const sp24_expert_desc* d) {
@@ -141,6 +142,8 @@ extern "C" sp24_status sp24_expert_linear(const sp24_expert_desc* d, const sp24_
                             reinterpret_cast<uintptr_t>(offsets);
   SP24_RETURN_IF(!aligned16(A) || !aligned16(X) || !aligned16(D) || !aligned16(e->residual) || !aligned16(e->pre) || (!d->a_is_dense && !aligned16(meta)) ||
                      (vectors & 3), SP24_ERR_ALIGN);
+  const TileShape forced = forced_shape(d->a_is_dense != 0);
+  SP24_RETURN_IF(forced.ctas && !is_built(forced), SP24_ERR_UNSUPPORTED);
   const sp24_status arch = check_arch();
   SP24_RETURN_IF(arch != SP24_OK, arch);
   GemmParams p = params(d, offsets, D, workspace);
@@ -157,9 +160,7 @@ extern "C" sp24_status sp24_expert_linear(const sp24_expert_desc* d, const sp24_
   p.beta = p.has_c ? 1.f : 0.f;
   const sp24_gemm_desc g = {d->ab_type, d->cd_type, d->M, d->rows, d->K, d->lda, d->ldx, d->ld_residual, d->ldd, SP24_COL_MAJOR, SP24_COL_MAJOR, SP24_COL_MAJOR,
                             d->a_is_dense};
-  TileShape tile = d->a_is_dense ? choose_dense_tile(d, d->M, d->K) : choose_expert_tile(d, e->residual != nullptr, e->pre != nullptr);
-  tile_override(&tile, d->a_is_dense != 0);
-  SP24_RETURN_IF(tile.tile_n > tile.block_n || tile.tile_n % 32, SP24_ERR_UNSUPPORTED);
+  const TileShape tile = forced.ctas ? forced : d->a_is_dense ? choose_dense_tile(d, d->M, d->K) : choose_expert_tile(d, e->residual != nullptr, e->pre != nullptr);
   return run(kColumnsByExpert, tile, !d->a_is_dense, &g, p, A, meta, X, stream);
 }
 
@@ -171,7 +172,7 @@ static sp24_status check_gradient(const sp24_expert_desc* d, const void* in, int
   SP24_RETURN_IF(ld_in < least_in || ld_other < d->K || ld_out < d->K, SP24_ERR_STRIDE);
   SP24_RETURN_IF(!whole16(ld_in, 2) || !whole16(ld_other, 2) || !whole16(ld_out, 2), SP24_ERR_STRIDE);
   SP24_RETURN_IF(!aligned16(in) || !aligned16(other) || !aligned16(out) || (reinterpret_cast<uintptr_t>(offsets) & 3), SP24_ERR_ALIGN);
-  return check_arch();
+  return SP24_OK;
 }
 
 extern "C" sp24_status sp24_expert_linear_dx(const sp24_expert_desc* d, const void* dz, const void* W, const int32_t* offsets, void* dX, void* workspace,
@@ -183,14 +184,15 @@ extern "C" sp24_status sp24_expert_linear_dx(const sp24_expert_desc* d, const vo
   if (d->rows == 0) return SP24_OK;
   st = check_gradient(d, dz, d->ldd, d->M, W, d->lda, offsets, dX, d->ldx, workspace, workspace_bytes);
   SP24_RETURN_IF(st != SP24_OK, st);
+  const TileShape forced = forced_shape(true);
+  SP24_RETURN_IF(forced.ctas && !is_built(forced), SP24_ERR_UNSUPPORTED);
+  st = check_arch();
+  SP24_RETURN_IF(st != SP24_OK, st);
   GemmParams p = params(d, offsets, dX, workspace);
   p.cd_col_major = 1;
   // W_e, transposed, times rows of dz: the tokens are columns as in the product itself, so that an expert's last tile is as wide as its rows ask for
   const sp24_gemm_desc g = {d->ab_type, d->cd_type, d->K, d->rows, d->M, d->lda, d->ldd, 0, d->ldx, SP24_COL_MAJOR, SP24_COL_MAJOR, SP24_COL_MAJOR, 1};
-  TileShape tile = choose_dense_tile(d, d->K, d->M);
-  tile_override(&tile, true);
-  SP24_RETURN_IF(tile.tile_n > tile.block_n || tile.tile_n % 32, SP24_ERR_UNSUPPORTED);
-  return run(kColumnsTransposed, tile, false, &g, p, W, nullptr, dz, stream);
+  return run(kColumnsTransposed, forced.ctas ? forced : choose_dense_tile(d, d->K, d->M), false, &g, p, W, nullptr, dz, stream);
 }
 
 extern "C" sp24_status sp24_expert_linear_dw(const sp24_expert_desc* d, const void* dz, const void* X, const int32_t* offsets, const void* meta, void* dW,
@@ -202,6 +204,8 @@ extern "C" sp24_status sp24_expert_linear_dw(const sp24_expert_desc* d, const vo
   st = check_gradient(d, dz, d->ldd, d->M, X, d->ldx, offsets, dW, d->lda, workspace, workspace_bytes);
   SP24_RETURN_IF(st != SP24_OK, st);
   SP24_RETURN_IF(reinterpret_cast<uintptr_t>(meta) & 1, SP24_ERR_ALIGN);
+  st = check_arch();
+  SP24_RETURN_IF(st != SP24_OK, st);
   if (d->rows == 0) {  // no expert has any
     SP24_CUDA_CHECK(cudaMemset2DAsync(dW, (size_t)d->lda * 2, 0, (size_t)d->K * 2, (size_t)(d->E * d->M), static_cast<cudaStream_t>(stream)));
     return SP24_OK;
