@@ -488,18 +488,19 @@ sp24_status sp24_expert_order(int64_t slots, int64_t E, int64_t align, const int
 
 /* Rows in the experts' order: out[position[t, i], .] = x[t, .] for i < k; rows whose source is negative become zeros.  With scale (T floats), also
  * out_scale[position[t, i]] = scale[t], 0 for those.  Any type of 1, 2 or 4 bytes; T x K of them, out rows x K.  Positions that are negative or not
- * below `rows` are left out.  Fastest where rows start at 16-byte boundaries.  out overlaps no input. */
+ * below `rows` are left out.  Fastest where rows start at 16-byte boundaries.  out and x may not overlap (SP24_ERR_UNSUPPORTED). */
 sp24_status sp24_expert_gather(sp24_dtype t, int64_t T, int64_t K, const void* x, int64_t ldx, const float* scale, int k, const int32_t* position,
                                int64_t rows, const int32_t* source, void* out, int64_t ldo, float* out_scale, void* stream);
 
 /* The tokens' sums: out[t, .] = sum over i < k of weights[t, i] y[position[t, i], .] (weights == NULL: ones) + residual[t, .], in FP32 in this order,
  * rounded once to t (SP24_F16, SP24_BF16 or SP24_F32).  Slots without a row count for nothing, whatever their weight.  With NULL weights it is the gradient of
- * sp24_expert_gather.  out may be the residual (same leading dimension). */
+ * sp24_expert_gather.  out may be the residual (same leading dimension), else it may overlap neither that nor y (SP24_ERR_UNSUPPORTED). */
 sp24_status sp24_expert_combine(sp24_dtype t, int64_t T, int64_t K, int64_t rows, const void* y, int64_t ldy, int k, const int32_t* position,
                                 const float* weights, const void* residual, int64_t ldr, void* out, int64_t ldo, void* stream);
 
 /* Its gradients: dy[position[t, i], .] = weights[t, i] dout[t, .], rounded once; dweights[t, i] = sum over . of dout[t, .] y[position[t, i], .] in FP32 (0 of
- * slots without a row); rows of dy whose source is negative become zeros.  dy may be y (same leading dimension). */
+ * slots without a row); rows of dy whose source is negative become zeros.  dy may be y (same leading dimension), else it may overlap neither that nor dout
+ * (SP24_ERR_UNSUPPORTED). */
 sp24_status sp24_expert_combine_backward(sp24_dtype t, int64_t T, int64_t K, int64_t rows, const void* dout, int64_t lddo, const void* y, int64_t ldy, int k,
                                          const int32_t* position, const int32_t* source, const float* weights, void* dy, int64_t lddy, float* dweights,
                                          void* stream);

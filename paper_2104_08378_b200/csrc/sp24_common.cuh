@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <utility>
 
 #include "sp24.h"
 
@@ -28,6 +29,33 @@ inline bool is_fp8(sp24_dtype t) { return t == SP24_E4M3 || t == SP24_E5M2; }
 inline bool is_ab_type(sp24_dtype t) { return t == SP24_F16 || t == SP24_BF16 || t == SP24_I8 || is_fp8(t); }
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// Rows in memory: `bytes` each (no more than `ld` if there are several), `ld` bytes apart.
+struct RowsAt {
+  const void* at;
+  int64_t rows, bytes, ld;
+};
+// Whether two of them share a byte.  Exact: halves of one wide matrix side by side do not.
+inline bool overlap(RowsAt a, RowsAt b) {
+  if (a.at == nullptr || b.at == nullptr || a.rows <= 0 || b.rows <= 0) return false;
+  if (reinterpret_cast<uintptr_t>(a.at) > reinterpret_cast<uintptr_t>(b.at)) std::swap(a, b);
+  const int64_t from = (int64_t)(reinterpret_cast<uintptr_t>(b.at) - reinterpret_cast<uintptr_t>(a.at));  // of b's first byte behind a's
+  if (from >= (a.rows - 1) * a.ld + a.bytes) return false;
+  if (a.ld == b.ld && a.rows > 1) {  // b starts in a row of a, or between two, where it may reach into the next
+    const int64_t in_row = from % a.ld;
+    return in_row < a.bytes || a.ld - in_row < b.bytes;
+  }
+  // row after row of the one with fewer: does the last row of the other that starts before its end reach into it
+  const bool b_fewer = b.rows < a.rows;
+  const RowsAt &few = b_fewer ? b : a, &many = b_fewer ? a : b;
+  for (int64_t i = 0; i < few.rows; ++i) {
+    const int64_t start = i * few.ld + (b_fewer ? from : -from), end = start + few.bytes;  // behind the other's first byte
+    if (end <= 0) continue;
+    const int64_t j = many.rows > 1 ? (end - 1) / many.ld : 0;
+    if ((j < many.rows ? j : many.rows - 1) * many.ld + many.bytes > start) return true;
+  }
+  return false;
+}
 
 // The current device must be a compute-capability 10.x part; the answer is cached per device.
 sp24_status check_arch();

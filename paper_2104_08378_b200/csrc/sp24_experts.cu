@@ -513,6 +513,8 @@ extern "C" sp24_status sp24_expert_gather(sp24_dtype t, int64_t T, int64_t K, co
   const int es = elem_bytes(t);
   SP24_RETURN_IF(!aligned(x, es) || !aligned(out, es) || !aligned(scale, 4) || !aligned(out_scale, 4) || !aligned(position, 4) || !aligned(source, 4),
                  SP24_ERR_ALIGN);
+  const RowsAt result = {out, rows, K * es, ldo * es};
+  SP24_RETURN_IF(overlap(result, {x, T, K * es, ldx * es}), SP24_ERR_UNSUPPORTED);
   const sp24_status arch = check_arch();
   SP24_RETURN_IF(arch != SP24_OK, arch);
   RowsParams p = {};
@@ -545,6 +547,8 @@ extern "C" sp24_status sp24_expert_combine(sp24_dtype t, int64_t T, int64_t K, i
   SP24_RETURN_IF(out == residual && T > 1 && ldo != ldr, SP24_ERR_STRIDE);
   const int es = elem_bytes(t);
   SP24_RETURN_IF(!aligned(y, es) || !aligned(out, es) || !aligned(residual, es) || !aligned(weights, 4) || !aligned(position, 4), SP24_ERR_ALIGN);
+  const RowsAt result = {out, T, K * es, ldo * es};
+  SP24_RETURN_IF(overlap(result, {y, rows, K * es, ldy * es}) || (residual != out && overlap(result, {residual, T, K * es, ldr * es})), SP24_ERR_UNSUPPORTED);
   const sp24_status arch = check_arch();
   SP24_RETURN_IF(arch != SP24_OK, arch);
   RowsParams p = {};
@@ -574,6 +578,8 @@ extern "C" sp24_status sp24_expert_combine_backward(sp24_dtype t, int64_t T, int
   const int es = elem_bytes(t);
   SP24_RETURN_IF(!aligned(dout, es) || !aligned(y, es) || !aligned(dy, es) || !aligned(weights, 4) || !aligned(dweights, 4) || !aligned(position, 4) ||
                      !aligned(source, 4), SP24_ERR_ALIGN);
+  const RowsAt result = {dy, rows, K * es, lddy * es};
+  SP24_RETURN_IF(overlap(result, {dout, T, K * es, lddo * es}) || (y != dy && overlap(result, {y, rows, K * es, ldy * es})), SP24_ERR_UNSUPPORTED);
   const sp24_status arch = check_arch();
   SP24_RETURN_IF(arch != SP24_OK, arch);
   RowsParams p = {};

@@ -1,0 +1,51 @@
+"""Results that lie over inputs which are read in another order: refused, before any device work, by the experts' operators."""
+import ctypes
+
+import pytest
+
+from paper_2104_08378_b200 import binding as sp
+
+BASE = 1 << 20
+UNSUPPORTED = 6
+
+
+def at(offset):
+    return ctypes.c_void_p(BASE + offset)
+
+
+FAR = at(1 << 18)
+
+
+def gather(x, out, T=4, K=64, rows=8, ldx=64, ldo=64):
+    return sp.lib.sp24_expert_gather(sp.BF16, T, K, x, ldx, None, 2, FAR, rows, FAR, out, ldo, None, None)
+
+
+# (offsets in bytes; rows of 128 bytes)
+@pytest.mark.parametrize("args", [
+    {"x": at(0), "out": at(0)}, {"x": at(128), "out": at(0)}, {"x": at(0), "out": at(3 * 128 + 64)}, {"x": at(7 * 128), "out": at(0)}, {"x": at(2), "out": at(0)},
+    {"x": at(0), "out": at(0), "T": 1, "rows": 1}, {"x": at(64), "out": at(0), "ldx": 128, "ldo": 128}, {"x": at(0), "out": at(1200), "ldx": 640},
+    {"x": at(254), "out": at(0), "ldo": 128}])
+def test_gather(args):
+    assert gather(**args) == UNSUPPORTED
+
+
+def combine(y, out, residual=None, T=4, rows=8, ldr=64):
+    return sp.lib.sp24_expert_combine(sp.BF16, T, 64, rows, y, 64, 2, FAR, FAR, residual, ldr, out, 64, None)
+
+
+@pytest.mark.parametrize("args", [
+    {"y": at(0), "out": at(0)}, {"y": at(0), "out": at(0), "residual": at(0)}, {"y": at(0), "out": at(7 * 128)}, {"y": at(512), "out": at(128)},
+    {"y": at(1 << 16), "out": at(0), "residual": at(128)}, {"y": at(1 << 16), "out": at(256), "residual": at(0)}, {"y": at(0), "out": at(0), "T": 1, "rows": 1}])
+def test_combine(args):
+    assert combine(**args) == UNSUPPORTED
+
+
+def combine_backward(dout, y, dy, rows=8):
+    return sp.lib.sp24_expert_combine_backward(sp.BF16, 4, 64, rows, dout, 64, y, 64, 2, FAR, FAR, FAR, dy, 64, FAR, None)
+
+
+@pytest.mark.parametrize("args", [
+    {"dout": at(0), "y": at(1 << 16), "dy": at(0)}, {"dout": at(1024 - 128), "y": at(1 << 16), "dy": at(0)}, {"dout": at(1 << 16), "y": at(0), "dy": at(128)},
+    {"dout": at(1 << 16), "y": at(128), "dy": at(0)}, {"dout": at(0), "y": at(0), "dy": at(0)}])
+def test_combine_backward(args):
+    assert combine_backward(**args) == UNSUPPORTED

@@ -1,0 +1,55 @@
+"""Results beside their inputs in one matrix, which share no byte with them, and those that are refused by both forms of the binding."""
+import pytest
+import torch
+
+from experts_util import choice
+from operators_util import rand
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def sp():
+    from paper_2104_08378_b200 import binding
+    return binding
+
+
+def refused(sp, fn, *args, **kwargs):
+    with pytest.raises(sp.Sp24Error) as e:
+        fn(*args, **kwargs)
+    assert e.value.status == sp.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("T,K", [(1, 64), (40, 64), (40, 75)])
+def test_rows_side_by_side(sp, T, K):
+    order = sp.expert_order(choice(T, 5, 1, 1), 5)
+    wide = rand((T, 2 * K), "bf16", 2)
+    x, out = wide[:, :K], wide[:, K:]
+    want = sp.expert_gather(x.clone(), order)[0]
+    assert torch.equal(sp.expert_gather(x, order, out=out)[0], want)
+    weights = rand((T, 1), "f32", 3)
+    want = sp.expert_combine(out.clone(), order, weights)
+    sp.expert_combine(out, order, weights, out=x)
+    assert torch.equal(x, want)
+    y = rand((T, K), "bf16", 4)
+    want = sp.expert_combine_backward(x.clone(), y, order, weights)
+    got = sp.expert_combine_backward(x, y, order, weights, out=out)
+    assert torch.equal(out, want[0])
+    # A sum's order goes by where the rows lie: chains of at most K / 2 + 16 additions on both sides, of half a step of FP32 (2^-24) each.
+    products = x.double() * y.double()[order.position[:, 0].long()]
+    assert bool(((got[1] - want[1]).double().abs()[:, 0] <= 2 * (K / 2 + 16) * 2.0 ** -24 * products.abs().sum(1)).all())
+
+
+def test_rows_over_their_inputs(sp):
+    order = sp.expert_order(choice(40, 5, 1, 1), 5)
+    x, y, weights = rand((41, 64), "bf16", 2), rand((40, 64), "bf16", 3), rand((40, 1), "f32", 4)
+    for name in ("gather", "combine", "combine_backward"):
+        for out in (x[:40], x[1:]):
+            if name == "gather":
+                refused(sp, sp.expert_gather, x[:40], order, out=out)
+            elif name == "combine":
+                refused(sp, sp.expert_combine, x[:40], order, weights, out=out)
+                if out.data_ptr() != x.data_ptr():
+                    refused(sp, sp.expert_combine, y, order, weights, residual=x[:40], out=out)
+            else:
+                refused(sp, sp.expert_combine_backward, x[:40], y, order, weights, out=out)
