@@ -542,7 +542,7 @@ sp24_status sp24_expert_linear(const sp24_expert_desc* d, const sp24_expert_epil
  *   d->cd_type is ab_type; d->ld_residual, d->ld_pre and d->a_is_dense are not used.  Sizes, alignment and workspace as above.
  * sp24_expert_act_backward: what they and the bias's gradient are made of, dz[r, i] = dy[r, i] act'(z[r, i]) rounded to t, for all rows (rows x M, or NULL), and dbias[e, i]
  *   (E x M floats or NULL) = the sum of the expert's dz before their rounding, in an order that the offsets fix.  z may be NULL for SP24_ACT_NONE.  t: SP24_F16, SP24_BF16 or
- *   SP24_F32; any leading dimensions and alignment; dz overlaps neither input.  workspace (for dbias):
+ *   SP24_F32; any leading dimensions and alignment; dz may overlap neither input (SP24_ERR_UNSUPPORTED: the sums read both again).  workspace (for dbias):
  *   sp24_expert_act_backward_workspace_bytes(...) bytes, 16-byte aligned, contents of no matter. */
 size_t sp24_expert_act_backward_workspace_bytes(int64_t E, int64_t M, int64_t rows);
 sp24_status sp24_expert_act_backward(sp24_dtype t, sp24_act act, int64_t E, int64_t M, int64_t rows, const void* dy, int64_t lddy, const void* z, int64_t ldz,

@@ -354,6 +354,9 @@ extern "C" sp24_status sp24_expert_act_backward(sp24_dtype t, sp24_act act, int6
   SP24_RETURN_IF(!aligned(dy, es) || (reads_z && !aligned(z, es)) || !aligned(dz, es) || !aligned(dbias, 4) || !aligned(offsets, 4), SP24_ERR_ALIGN);
   SP24_RETURN_IF(dbias && (!workspace || !aligned16(workspace) || workspace_bytes < sp24_expert_act_backward_workspace_bytes(E, M, rows)), SP24_ERR_WORKSPACE);
   if (!dbias && (rows == 0 || !dz)) return SP24_OK;
+  const int64_t width = M * (int64_t)es;
+  const RowsAt result = {dz, rows, width, lddz * (int64_t)es};
+  SP24_RETURN_IF(overlap(result, {dy, rows, width, lddy * (int64_t)es}) || (reads_z && overlap(result, {z, rows, width, ldz * (int64_t)es})), SP24_ERR_UNSUPPORTED);
   const bool whole = t != SP24_F32 && M % 8 == 0 && whole_rows(dy, rows, lddy, 2, 16) && (!reads_z || whole_rows(z, rows, ldz, 2, 16)) &&
                      whole_rows(dz, rows, lddz, 2, 16);
   const int64_t row_tiles = (rows + kTile - 1) / kTile, col_tiles = (M + kTile - 1) / kTile;

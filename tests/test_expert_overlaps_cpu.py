@@ -49,3 +49,15 @@ def combine_backward(dout, y, dy, rows=8):
     {"dout": at(1 << 16), "y": at(128), "dy": at(0)}, {"dout": at(0), "y": at(0), "dy": at(0)}])
 def test_combine_backward(args):
     assert combine_backward(**args) == UNSUPPORTED
+
+
+def act_backward(dy, z, dz, t=sp.BF16, act=3, M=64, lddz=64):
+    return sp.lib.sp24_expert_act_backward(t, act, 4, M, 48, dy, 64, z, 64, FAR, dz, lddz, FAR, FAR, 1 << 20, None)
+
+
+@pytest.mark.parametrize("args", [
+    {"dy": at(0), "z": at(1 << 16), "dz": at(0)}, {"dy": at(1 << 16), "z": at(0), "dz": at(0)}, {"dy": at(0), "z": at(1 << 16), "dz": at(47 * 128)},
+    {"dy": at(0), "z": None, "dz": at(0), "act": 0}, {"dy": at(256), "z": at(1 << 16), "dz": at(0), "t": sp.F32}, {"dy": at(0), "z": at(1 << 16), "dz": at(64), "M": 33},
+    {"dy": at(0), "z": at(1 << 16), "dz": at(160), "lddz": 640}])
+def test_act_backward(args):
+    assert act_backward(**args) == UNSUPPORTED
