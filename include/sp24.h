@@ -511,7 +511,8 @@ sp24_status sp24_expert_combine_backward(sp24_dtype t, int64_t T, int64_t K, int
  *   A: the experts' values one after the other: E M rows of K / 2 (dense: K) values, leading dimension lda.
  *   meta: E times sp24_meta_bytes(ab_type, M, K, SP24_META_TCGEN05) bytes, each expert's as sp24_compress gives it (not for dense A).
  *   X: rows x K (leading dimension ldx), D, residual, pre: rows x M of cd_type (ldd, ld_residual, ld_pre), 16-byte aligned with leading
- *      dimensions of whole 16 bytes.  residual may be D.
+ *      dimensions of whole 16 bytes.  residual may be D (same leading dimension); else D and pre may overlap neither each other nor A, X or the
+ *      residual (SP24_ERR_UNSUPPORTED).
  *   row_scale, bias: E x M floats; col_scale: rows floats; each may be NULL (col_scale: 8-bit operand types only).
  *   offsets: device, E + 1 int32, 0 <= offsets[0] <= ... <= offsets[E] <= rows (values outside count as the nearest that are not).
  *   ab_type: SP24_F16, SP24_BF16, SP24_I8, SP24_E4M3 or SP24_E5M2, cd_type as for sp24_linear.  M and K are multiples of 16, with 8-bit operands of
@@ -539,7 +540,8 @@ sp24_status sp24_expert_linear(const sp24_expert_desc* d, const sp24_expert_epil
  *   dz: rows x M (leading dimension d->ldd), X, dX: rows x K (ldx; only rows of experts are written), dW: E M x K (lda; an expert without rows gets zeros).
  *   sp24_expert_linear_dw: every offset is a multiple of 16 (sp24_expert_order with align = 16): the weights' gradients of an expert that is not so placed are NaN.
  *      meta (or NULL): the weights' metadata, as for sp24_expert_linear; the entries of dW that it does not name as kept are zeros.
- *   d->cd_type is ab_type; d->ld_residual, d->ld_pre and d->a_is_dense are not used.  Sizes, alignment and workspace as above.
+ *   d->cd_type is ab_type; d->ld_residual, d->ld_pre and d->a_is_dense are not used.  dX and dW may overlap no operand (SP24_ERR_UNSUPPORTED).  Sizes, alignment and
+ *   workspace as above.
  * sp24_expert_act_backward: what they and the bias's gradient are made of, dz[r, i] = dy[r, i] act'(z[r, i]) rounded to t, for all rows (rows x M, or NULL), and dbias[e, i]
  *   (E x M floats or NULL) = the sum of the expert's dz before their rounding, in an order that the offsets fix.  z may be NULL for SP24_ACT_NONE.  t: SP24_F16, SP24_BF16 or
  *   SP24_F32; any leading dimensions and alignment; dz may overlap neither input (SP24_ERR_UNSUPPORTED: the sums read both again).  workspace (for dbias):

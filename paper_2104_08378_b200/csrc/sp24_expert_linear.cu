@@ -142,6 +142,12 @@ extern "C" sp24_status sp24_expert_linear(const sp24_expert_desc* d, const sp24_
                             reinterpret_cast<uintptr_t>(offsets);
   SP24_RETURN_IF(!aligned16(A) || !aligned16(X) || !aligned16(D) || !aligned16(e->residual) || !aligned16(e->pre) || (!d->a_is_dense && !aligned16(meta)) ||
                      (vectors & 3), SP24_ERR_ALIGN);
+  SP24_RETURN_IF(e->residual == D && d->rows > 1 && d->ld_residual != d->ldd, SP24_ERR_STRIDE);
+  const RowsAt result = {D, d->rows, d->M * cs, d->ldd * cs}, pre = {e->pre, d->rows, d->M * cs, d->ld_pre * cs},
+               residual = {e->residual, d->rows, d->M * cs, d->ld_residual * cs}, x = {X, d->rows, d->K * es, d->ldx * es},
+               a = {A, d->E * d->M, (d->a_is_dense ? d->K : d->K / 2) * es, d->lda * es};
+  SP24_RETURN_IF(overlap(result, x) || overlap(result, a) || overlap(result, pre) || (e->residual != D && overlap(result, residual)) || overlap(pre, x) ||
+                     overlap(pre, a) || overlap(pre, residual), SP24_ERR_UNSUPPORTED);
   const TileShape forced = forced_shape(d->a_is_dense != 0);
   SP24_RETURN_IF(forced.ctas && !is_built(forced), SP24_ERR_UNSUPPORTED);
   const sp24_status arch = check_arch();
@@ -164,14 +170,16 @@ extern "C" sp24_status sp24_expert_linear(const sp24_expert_desc* d, const sp24_
   return run(kColumnsByExpert, tile, !d->a_is_dense, &g, p, A, meta, X, stream);
 }
 
-// What the two products of the gradient ask of their arguments: a matrix each of M, K and again K or M columns
-static sp24_status check_gradient(const sp24_expert_desc* d, const void* in, int64_t ld_in, int64_t least_in, const void* other, int64_t ld_other, const int32_t* offsets,
-                                  void* out, int64_t ld_out, const void* workspace, size_t workspace_bytes) {
-  SP24_RETURN_IF(offsets == nullptr || out == nullptr || (d->rows > 0 && (in == nullptr || other == nullptr)), SP24_ERR_NULL);
+// What the two products of the gradient ask of their arguments: dz, `other` of so many rows of K columns, and `out` alike
+static sp24_status check_gradient(const sp24_expert_desc* d, const void* dz, const void* other, int64_t other_rows, int64_t ld_other, const int32_t* offsets, void* out,
+                                  int64_t out_rows, int64_t ld_out, const void* workspace, size_t workspace_bytes) {
+  SP24_RETURN_IF(offsets == nullptr || out == nullptr || (d->rows > 0 && (dz == nullptr || other == nullptr)), SP24_ERR_NULL);
   SP24_RETURN_IF(workspace == nullptr || workspace_bytes < 256 || !aligned16(workspace), SP24_ERR_WORKSPACE);
-  SP24_RETURN_IF(ld_in < least_in || ld_other < d->K || ld_out < d->K, SP24_ERR_STRIDE);
-  SP24_RETURN_IF(!whole16(ld_in, 2) || !whole16(ld_other, 2) || !whole16(ld_out, 2), SP24_ERR_STRIDE);
-  SP24_RETURN_IF(!aligned16(in) || !aligned16(other) || !aligned16(out) || (reinterpret_cast<uintptr_t>(offsets) & 3), SP24_ERR_ALIGN);
+  SP24_RETURN_IF(d->ldd < d->M || ld_other < d->K || ld_out < d->K, SP24_ERR_STRIDE);
+  SP24_RETURN_IF(!whole16(d->ldd, 2) || !whole16(ld_other, 2) || !whole16(ld_out, 2), SP24_ERR_STRIDE);
+  SP24_RETURN_IF(!aligned16(dz) || !aligned16(other) || !aligned16(out) || (reinterpret_cast<uintptr_t>(offsets) & 3), SP24_ERR_ALIGN);
+  const RowsAt result = {out, out_rows, d->K * 2, ld_out * 2};
+  SP24_RETURN_IF(overlap(result, {dz, d->rows, d->M * 2, d->ldd * 2}) || overlap(result, {other, other_rows, d->K * 2, ld_other * 2}), SP24_ERR_UNSUPPORTED);
   return SP24_OK;
 }
 
@@ -182,7 +190,7 @@ extern "C" sp24_status sp24_expert_linear_dx(const sp24_expert_desc* d, const vo
   sp24_status st = check_sizes(d);
   SP24_RETURN_IF(st != SP24_OK, st);
   if (d->rows == 0) return SP24_OK;
-  st = check_gradient(d, dz, d->ldd, d->M, W, d->lda, offsets, dX, d->ldx, workspace, workspace_bytes);
+  st = check_gradient(d, dz, W, d->E * d->M, d->lda, offsets, dX, d->rows, d->ldx, workspace, workspace_bytes);
   SP24_RETURN_IF(st != SP24_OK, st);
   const TileShape forced = forced_shape(true);
   SP24_RETURN_IF(forced.ctas && !is_built(forced), SP24_ERR_UNSUPPORTED);
@@ -201,7 +209,7 @@ extern "C" sp24_status sp24_expert_linear_dw(const sp24_expert_desc* d, const vo
   SP24_RETURN_IF((d->ab_type != SP24_F16 && d->ab_type != SP24_BF16) || d->cd_type != d->ab_type, SP24_ERR_DTYPE);
   sp24_status st = check_sizes(d);
   SP24_RETURN_IF(st != SP24_OK, st);
-  st = check_gradient(d, dz, d->ldd, d->M, X, d->ldx, offsets, dW, d->lda, workspace, workspace_bytes);
+  st = check_gradient(d, dz, X, d->rows, d->ldx, offsets, dW, d->E * d->M, d->lda, workspace, workspace_bytes);
   SP24_RETURN_IF(st != SP24_OK, st);
   SP24_RETURN_IF(reinterpret_cast<uintptr_t>(meta) & 1, SP24_ERR_ALIGN);
   st = check_arch();

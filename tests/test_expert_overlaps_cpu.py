@@ -61,3 +61,38 @@ def act_backward(dy, z, dz, t=sp.BF16, act=3, M=64, lddz=64):
     {"dy": at(0), "z": at(1 << 16), "dz": at(160), "lddz": 640}])
 def test_act_backward(args):
     assert act_backward(**args) == UNSUPPORTED
+
+
+# 4 experts, M = K = 64 in 16 bits: the weights' values are 16 KB (dense 32 KB), 33 rows of X, D, residual and pre a little more than 4 KB each
+W_AT, X_AT, D_AT, R_AT, Z_AT = 0, 1 << 16, 2 << 16, 3 << 16, 5 << 16
+
+
+def linear(A=W_AT, X=X_AT, D=D_AT, residual=None, pre=None, ldr=64, dense=0):
+    d = sp.ExpertDesc(sp.BF16, sp.BF16, 4, 64, 64, 33, 64 if dense else 32, 64, 64, ldr, 64, dense)
+    e = sp.ExpertEpilogue(None, None, None, 0, None if residual is None else at(residual), None if pre is None else at(pre))
+    return sp.lib.sp24_expert_linear(ctypes.byref(d), ctypes.byref(e), at(A), FAR, at(X), FAR, at(D), at(7 << 16), 256, None)
+
+
+@pytest.mark.parametrize("args", [
+    {"D": X_AT}, {"D": X_AT + 32 * 128}, {"D": X_AT - 32 * 128}, {"D": W_AT}, {"D": W_AT + 16384 - 64}, {"D": W_AT + 32768 - 64, "dense": 1}, {"pre": X_AT}, {"pre": W_AT},
+    {"pre": D_AT}, {"pre": D_AT + 128}, {"residual": R_AT, "pre": R_AT}, {"residual": R_AT, "pre": R_AT + 128}, {"residual": D_AT + 128}, {"residual": D_AT - 256}])
+def test_linear(args):
+    assert linear(**args) == UNSUPPORTED
+
+
+def test_the_residual_that_is_the_result_has_its_rows():
+    assert linear(residual=D_AT, ldr=72) == 4
+
+
+def gradient(which, dz=X_AT, other=W_AT, out=D_AT):
+    d = ctypes.byref(sp.ExpertDesc(sp.BF16, sp.BF16, 4, 64, 64, 48, 64, 64, 64, 0, 0, 1))
+    if which == "dx":
+        return sp.lib.sp24_expert_linear_dx(d, at(dz), at(other), FAR, at(out), at(7 << 16), 256, None)
+    return sp.lib.sp24_expert_linear_dw(d, at(dz), at(other), FAR, None, at(out), at(7 << 16), 256, None)
+
+
+@pytest.mark.parametrize("which,args", [
+    ("dx", {"out": X_AT}), ("dx", {"out": X_AT + 47 * 128}), ("dx", {"out": W_AT}), ("dx", {"out": 255 * 128}), ("dw", {"out": X_AT}), ("dw", {"out": X_AT - 255 * 128}),
+    ("dw", {"out": W_AT + 47 * 128}), ("dw", {"out": W_AT})])
+def test_gradients(which, args):
+    assert gradient(which, **args) == UNSUPPORTED

@@ -53,3 +53,18 @@ def test_rows_over_their_inputs(sp):
                     refused(sp, sp.expert_combine, y, order, weights, residual=x[:40], out=out)
             else:
                 refused(sp, sp.expert_combine_backward, x[:40], y, order, weights, out=out)
+
+
+def test_products_beside_and_over_their_operands(sp):
+    """D and pre beside X in one matrix; over it, and a residual a row further on, refused."""
+    E, M, K, rows = 3, 64, 64, 50
+    A, meta = sp.expert_compress(rand((E, M, K), "bf16", 1))
+    wide, offsets = rand((rows + 1, 4 * K), "bf16", 2), torch.tensor([0, 20, 20, 50], dtype=torch.int32, device="cuda")
+    X, D, Z, R = (wide[:rows, i * K:(i + 1) * K] for i in range(4))
+    want = sp.expert_linear(A, meta, X.clone(), offsets, act="silu", residual=R.clone(), pre=True)
+    got = sp.expert_linear(A, meta, X, offsets, act="silu", residual=R, pre=Z, out=D)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and got[0] is D
+    refused(sp, sp.expert_linear, A, meta, X, offsets, out=X)
+    refused(sp, sp.expert_linear, A, meta, X, offsets, pre=X)
+    refused(sp, sp.expert_linear, A, meta, X, offsets, residual=wide[1:, :K], out=wide[:rows, :K])
+    refused(sp, sp.expert_linear, A, meta, X, offsets, residual=wide[1:, K:2 * K], out=D)
