@@ -470,7 +470,7 @@ sp24_status sp24_route(sp24_dtype t, int64_t T, int64_t E, const void* logits, i
  *   renorm: dl = u (g - sum u g) of the chosen experts (sigmoid: times 1 - s), 0 of the others;
  *   else softmax: dl = s (g - sum of the chosen s g), g = 0 of the others; sigmoid: dl = g s (1 - s) of the chosen, 0 of the others.
  * In FP32, rounded once to t.  A slot whose expert is negative or not below E counts for nothing; an expert that stands in two slots of a token
- * gets both slots' gradients.  dlogits may be the logits themselves (same leading dimension). */
+ * gets both slots' gradients.  dlogits may be the logits themselves (same leading dimension), else may not overlap them (SP24_ERR_UNSUPPORTED). */
 sp24_status sp24_route_backward(sp24_dtype t, int64_t T, int64_t E, const float* dweights, const void* logits, int64_t ld, const int32_t* experts,
                                 int k, sp24_score score, int renorm, float scale, void* dlogits, int64_t ldd, void* stream);
 

@@ -984,6 +984,8 @@ extern "C" sp24_status sp24_route_backward(sp24_dtype t, int64_t T, int64_t E, c
   SP24_RETURN_IF(!row_fits(T, E, ld) || !row_fits(T, E, ldd), SP24_ERR_STRIDE);
   SP24_RETURN_IF(dlogits == logits && T > 1 && ld != ldd, SP24_ERR_STRIDE);
   SP24_RETURN_IF(!aligned(logits, elem_bytes(t)) || !aligned(dlogits, elem_bytes(t)) || !aligned(dweights, 4) || !aligned(experts, 4), SP24_ERR_ALIGN);
+  const int64_t width = E * elem_bytes(t);
+  SP24_RETURN_IF(logits != dlogits && overlap({dlogits, T, width, ldd * elem_bytes(t)}, {logits, T, width, ld * elem_bytes(t)}), SP24_ERR_UNSUPPORTED);
   const sp24_status arch = check_arch();
   SP24_RETURN_IF(arch != SP24_OK, arch);
   RouteBackwardParams p = {};

@@ -96,3 +96,8 @@ def gradient(which, dz=X_AT, other=W_AT, out=D_AT):
     ("dw", {"out": W_AT + 47 * 128}), ("dw", {"out": W_AT})])
 def test_gradients(which, args):
     assert gradient(which, **args) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("logits,out,T,ld", [(0, 256, 4, 64), (3 * 256, 0, 4, 64), (0, 4, 4, 64), (0, 4, 1, 64), (0, 252, 4, 128), (508, 0, 4, 128)])
+def test_route_backward(logits, out, T, ld):
+    assert sp.lib.sp24_route_backward(sp.F32, T, 64, FAR, at(logits), ld, FAR, 8, 0, 1, ctypes.c_float(1.0), at(out), ld, None) == UNSUPPORTED

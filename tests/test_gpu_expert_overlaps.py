@@ -68,3 +68,13 @@ def test_products_beside_and_over_their_operands(sp):
     refused(sp, sp.expert_linear, A, meta, X, offsets, pre=X)
     refused(sp, sp.expert_linear, A, meta, X, offsets, residual=wide[1:, :K], out=wide[:rows, :K])
     refused(sp, sp.expert_linear, A, meta, X, offsets, residual=wide[1:, K:2 * K], out=D)
+
+
+@pytest.mark.parametrize("E", [64, 65])
+def test_logits_and_their_gradient_side_by_side(sp, E):
+    wide = rand((41, 2 * E), "f32", 1)
+    logits, out = wide[:40, :E], wide[:40, E:]
+    g, experts = rand((40, 3), "f32", 2), choice(40, E, 3, 3)
+    want = sp.route_backward(g, logits.clone(), experts)
+    assert sp.route_backward(g, logits, experts, out=out) is out and torch.equal(out, want)
+    refused(sp, sp.route_backward, g, logits, experts, out=wide[1:, :E])
