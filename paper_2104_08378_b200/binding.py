@@ -864,7 +864,7 @@ def _route(logits, k, score, bias, groups, top_groups, group_score, renorm, scal
     T, E = logits.shape
     _refuse(score not in SCORE or group_score not in GROUP_SCORE, ERR_UNSUPPORTED, where)
     _vector(bias, E, where, logits)
-    _refuse(not 1 <= k <= max(1, E), ERR_SHAPE, where)
+    _refuse(not 1 <= k <= max(1, E) or not 1 <= groups <= max(1, E) or not 1 <= top_groups <= groups, ERR_SHAPE, where)
     weights = logits.new_empty((T, k), dtype=torch.float32)
     experts = logits.new_empty((T, k), dtype=torch.int32)
     _check(lib.sp24_route(t, T, E, _ptr(logits), ld, SCORE[score], _ptr(bias), groups, top_groups, GROUP_SCORE[group_score], k, 1 if renorm else 0, scale,

@@ -27,3 +27,11 @@ def test_wide_groups(sp, E, groups, group_score):
         assert torch.equal(experts, want)
         # (as in test_gpu_route.py: the exponential of a difference, the logarithm of the sigmoid, a sum and a division)
         assert bool(((weights.double() - want_weights).abs() <= 2.0 ** -17 * want_weights).all())
+
+
+@pytest.mark.parametrize("how", [{"groups": 2 ** 32 + 1}, {"groups": 2 ** 32 + 4, "top_groups": 2}, {"groups": 4, "top_groups": 2 ** 32 + 2}, {"groups": -1}, {"groups": 4, "top_groups": 0},
+                                 {"groups": 2 ** 70}])
+def test_numbers_of_groups_that_do_not_fit_an_int(sp, how):
+    with pytest.raises(sp.Sp24Error) as e:
+        sp.route(rand((4, 64), "f32", 1), 2, **how)
+    assert e.value.status == sp.ERR_SHAPE
