@@ -337,7 +337,7 @@ extern "C" sp24_status sp24_act_backward(sp24_dtype t, sp24_act act, int64_t row
 }
 
 extern "C" size_t sp24_expert_act_backward_workspace_bytes(int64_t E, int64_t M, int64_t rows) {
-  if (E < 1 || E > 1024 || M < 1 || M > kMostColumns || rows < 0 || rows > kMostColumns) return 0;
+  if (E < 1 || E > kMostExperts || M < 1 || M > kMostColumns || rows < 0 || rows > kMostColumns) return 0;
   return (size_t)((rows + kTile - 1) / kTile + E) * (size_t)M * sizeof(float);
 }
 
@@ -346,7 +346,7 @@ extern "C" sp24_status sp24_expert_act_backward(sp24_dtype t, sp24_act act, int6
                                                 size_t workspace_bytes, void* stream) {
   SP24_RETURN_IF(!is_float_type(t), SP24_ERR_DTYPE);
   SP24_RETURN_IF(!is_act(act), SP24_ERR_UNSUPPORTED);
-  SP24_RETURN_IF(E < 1 || E > 1024 || M < 1 || M > kMostColumns || rows < 0 || rows > kMostColumns, SP24_ERR_SHAPE);
+  SP24_RETURN_IF(E < 1 || E > kMostExperts || M < 1 || M > kMostColumns || rows < 0 || rows > kMostColumns, SP24_ERR_SHAPE);
   const bool reads_z = act != SP24_ACT_NONE;
   SP24_RETURN_IF((rows > 0 && (!dy || (reads_z && !z))) || (dbias && !offsets), SP24_ERR_NULL);
   SP24_RETURN_IF(!row_fits(rows, M, lddy) || (reads_z && !row_fits(rows, M, ldz)) || (dz && !row_fits(rows, M, lddz)), SP24_ERR_STRIDE);

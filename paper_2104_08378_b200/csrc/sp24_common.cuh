@@ -57,6 +57,8 @@ inline bool overlap(RowsAt a, RowsAt b) {
   return false;
 }
 
+constexpr int kMostExperts = 1024, kMostChosen = 32;  // experts of a layer, and of one token
+
 // The current device must be a compute-capability 10.x part; the answer is cached per device.
 sp24_status check_arch();
 

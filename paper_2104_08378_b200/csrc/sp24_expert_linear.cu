@@ -5,8 +5,7 @@
 namespace sp24 {
 namespace {
 
-constexpr int64_t kMostExperts = 1024, kMostRows = int64_t(1) << 30;
-enum { kColumnsByExpert = 1, kColumnsTransposed = 2, kKByExpert = 3 };  // as the kernel has them
+constexpr int64_t kMostRows = int64_t(1) << 30;
 
 bool whole16(int64_t ld, int bytes) { return ld * bytes % 16 == 0; }
 

@@ -5,8 +5,6 @@
 namespace sp24 {
 namespace {
 
-constexpr int kMostExperts = 1024, kMostChosen = 32;
-
 // ---- order ------------------------------------------------------------------------------------------------------
 // A stable counting sort.  Each warp has a part of the slots in their order and counts them by experts in shared memory; the counts of a block's warps and then of the
 // blocks are added up from the left, and the warp goes over its slots again with the places found (32 at a time, equal ones found by a match over the warp).

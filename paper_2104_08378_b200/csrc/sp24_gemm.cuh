@@ -136,6 +136,10 @@ template <int KIND>
 sp24_status launch_linear(TileShape tile, bool sparse, bool b_mn, const sp24_gemm_desc* d, const GemmParams& p, const void* A,
                           const void* meta, const void* B, cudaStream_t s);
 
+// The products of many experts in one launch (sp24_expert_linear and its gradients), each a problem of its own over the same tensor maps.  The experts' rows are a
+// range of one dimension, known on the device only.
+enum Group { kOneProblem = 0, kColumnsByExpert = 1, kColumnsTransposed = 2, kKByExpert = 3 };
+
 // ---- in sp24_expert_{f16,i8,f8}.cu ---------------------------------------------------------------------
 // One launch of the kernel over the problems of all experts (group: see the kernel's Group).  d: M, N and K of an expert's problem, of which the one that
 // differs from expert to expert is p.rows, the rows there are; sizes and leading dimensions as for launch_gemm.

@@ -189,10 +189,7 @@ __device__ __forceinline__ void tile_coords(int t, const GemmParams& p, int& mt,
   if (band & 1) nt = p.n_tiles - 1 - nt;
 }
 
-// GROUP: the products of many experts in one launch (sp24_expert_linear and its gradients), each a problem of its own over the same
-// tensor maps.  The experts' rows are a range of one dimension, known on the device only: of the columns (B and D hold the rows of tokens), or of K (A and B; D is an
-// expert's own).
-enum Group { kOneProblem = 0, kColumnsByExpert = 1, kColumnsTransposed = 2, kKByExpert = 3 };
+// GROUP, see Group: the experts' rows are a range of the columns (B and D hold the rows of tokens), or of K (A and B; D is an expert's own).
 __host__ __device__ constexpr bool columns_by_expert(int group) { return group == kColumnsByExpert || group == kColumnsTransposed; }
 // A with M contiguous (MN-major operand, 16-bit types): the weights of an expert, M x K as they are stored, times rows of M values (kColumnsTransposed), and rows of M
 // values whose products with others are summed over the rows (kKByExpert).  In shared memory as B with N contiguous: chunks of 64 rows of A, a k-row of 128 bytes each.

@@ -6,7 +6,7 @@
 namespace sp24 {
 namespace {
 
-constexpr int kMostExperts = 1024, kMostChosen = 32, kMostGroups = 32;
+constexpr int kMostGroups = 32;
 constexpr int kRouteWarps = 8;
 
 struct RouteParams {
@@ -74,24 +74,23 @@ __device__ __forceinline__ double warp_max(double v) {
   return v;
 }
 
-// The whole choice in FP64, for the tokens of which FP32 cannot tell it: rare, so kept out of the way.
+// The whole choice under a bias in FP64, for the tokens of which FP32 cannot tell it: rare, so kept out of the way.
 template <typename T, int V>
 __device__ __noinline__ void choose64(const RouteParams& p, const void* row, float top_logit, int lane, int32_t* chosen) {
-  double c[V], by[V];
+  double c[V];
   double sum = 0.0;
   for (int v = 0; v < V; ++v) {
     const int e = v * 32 + lane;
     const float l = e < p.E ? logit<T>(row, e) : -INFINITY;
-    by[v] = p.sigmoid ? 1.0 / (1.0 + exp(-(double)l)) : exp((double)l - (double)top_logit);
-    c[v] = l > -INFINITY ? (double)l : -INFINITY;  // (NaN too)
-    if (l > -INFINITY) sum += by[v];
+    c[v] = !(l > -INFINITY) ? -INFINITY : p.sigmoid ? 1.0 / (1.0 + exp(-(double)l)) : exp((double)l - (double)top_logit);  // (NaN too)
+    if (l > -INFINITY) sum += c[v];
   }
   sum = p.sigmoid ? 1.0 : warp_sum(sum);
   for (int v = 0; v < V; ++v) {
     const int e = v * 32 + lane;
-    const double b = p.bias && e < p.E ? (double)p.bias[e] : 0.0;
-    by[v] = c[v] > -INFINITY && by[v] / sum + b > -INFINITY ? by[v] / sum + b : -INFINITY;
-    if (p.bias) c[v] = by[v];
+    if (!(c[v] > -INFINITY)) continue;
+    c[v] = c[v] / sum + (double)p.bias[e];
+    if (!(c[v] > -INFINITY)) c[v] = -INFINITY;
   }
   if (p.groups > 1) {
     double mine = -INFINITY;  // of group `lane`
@@ -99,10 +98,9 @@ __device__ __noinline__ void choose64(const RouteParams& p, const void* row, flo
       double one = -INFINITY, two = -INFINITY;
       for (int v = 0; v < V; ++v) {
         const int e = v * 32 + lane;
-        const double x = p.top2 ? by[v] : c[v];
         if (e / p.group_experts == g && e < p.E) {
-          two = fmax(two, fmin(one, x));
-          one = fmax(one, x);
+          two = fmax(two, fmin(one, c[v]));
+          one = fmax(one, c[v]);
         }
       }
 #pragma unroll
@@ -256,7 +254,6 @@ __device__ __forceinline__ void route_token(const RouteParams& p, int64_t t, int
   nan = __any_sync(~0u, nan) || (!p.sigmoid && top == INFINITY);
   Choice<V> choice;
   float inv = 1.f, error = 0.f;  // of two scores' difference
-  bool sure = true;
   if (total) {
     float sum = 0.f;
 #pragma unroll
@@ -342,71 +339,65 @@ __device__ __forceinline__ void route_token(const RouteParams& p, int64_t t, int
   int mine = -1;  // lane i: the i-th chosen
   // The k-th largest of the lanes' largest (k rounds, equal ones of several lanes in one) is not above the k-th largest of all: what reaches it, less what
   // FP32 may be off, are the candidates, hardly more than k of them.  Each is in a lane's hands then, and its place is the number of those before it.
-  int candidates = 33;
+  int candidates = 0;
   float near = 0.f;  // (with a bias: how far apart two values must be to be told apart)
-  if (sure) {
-    uint32_t m = choice.key[0];
+  uint32_t m = choice.key[0];
 #pragma unroll
-    for (int v = 1; v < V; ++v) m = max(m, choice.key[v]);
-    uint32_t least = 0;
-    for (int i = 0; i < p.k; ++i) {
-      const uint32_t top_key = __reduce_max_sync(~0u, m);
-      if (top_key <= kDeadKey) { least = 0; break; }
-      least = top_key;
-      if (m == top_key) m = 0;
-    }
-    if (BIAS) {
-      near = error + 0x1p-22f * (2.f + 2.f * x.bias_size);  // (sums of a score, at most 1, and a bias; rounded by half a step of theirs)
-      if (least) least = order_key(key_value(least) - near);
-    }
-    least = max(least, kDeadKey + 1);
-    candidates = 0;
+  for (int v = 1; v < V; ++v) m = max(m, choice.key[v]);
+  uint32_t least = 0;
+  for (int i = 0; i < p.k; ++i) {
+    const uint32_t top_key = __reduce_max_sync(~0u, m);
+    if (top_key <= kDeadKey) { least = 0; break; }
+    least = top_key;
+    if (m == top_key) m = 0;
+  }
+  if (BIAS) {
+    near = error + 0x1p-22f * (2.f + 2.f * x.bias_size);  // (sums of a score, at most 1, and a bias; rounded by half a step of theirs)
+    if (least) least = order_key(key_value(least) - near);
+  }
+  least = max(least, kDeadKey + 1);
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const bool in = choice.key[v] >= least;
-      const uint32_t all = __ballot_sync(~0u, in);
-      const int at = candidates + __popc(all & ((1u << lane) - 1));
-      if (in && at < 32) mine_of[at] = make_uint2(choice.key[v], v * 32 + lane);
-      candidates += __popc(all);
+  for (int v = 0; v < V; ++v) {
+    const bool in = choice.key[v] >= least;
+    const uint32_t all = __ballot_sync(~0u, in);
+    const int at = candidates + __popc(all & ((1u << lane) - 1));
+    if (in && at < 32) mine_of[at] = make_uint2(choice.key[v], v * 32 + lane);
+    candidates += __popc(all);
+  }
+  __syncwarp();
+  if (candidates <= 32) {
+    const uint2 own = lane < candidates ? mine_of[lane] : make_uint2(0, 0);
+    int place = lane < candidates ? 0 : 32;
+    for (int i = 0; i < candidates; ++i) {
+      const uint2 other = mine_of[i];  // (the same for all lanes)
+      place += other.x > own.x || (other.x == own.x && other.y < own.y);
     }
     __syncwarp();
-    if (candidates <= 32) {
-      const uint2 own = lane < candidates ? mine_of[lane] : make_uint2(0, 0);
-      int place = lane < candidates ? 0 : 32;
-      for (int i = 0; i < candidates; ++i) {
-        const uint2 other = mine_of[i];  // (the same for all lanes)
-        place += other.x > own.x || (other.x == own.x && other.y < own.y);
-      }
-      __syncwarp();
-      if (lane < candidates) mine_of[place] = own;
-      __syncwarp();
-      const uint2 here = lane < candidates ? mine_of[lane] : make_uint2(0, 0);
-      mine = lane < candidates ? (int)here.y : -1;
-      if (BIAS) {
-        // A chosen one against the one before, all that are left against the last chosen: there may be equals of it before one that it is too close to.
-        const uint2 before = lane > 0 && lane < candidates ? mine_of[min(lane, p.k) - 1] : make_uint2(0, 0);
-        bool doubt = lane > 0 && lane < candidates && key_value(before.x) - key_value(here.x) <= near;
-        // (the same logit under the same bias: a tie, whatever the arithmetic)
-        if (doubt) doubt = !(logit<T>(row, here.y) == logit<T>(row, before.y) && p.bias[here.y] == p.bias[before.y]);
-        if (__any_sync(~0u, doubt)) mine = order64<T, V>(p, row, top, lane, candidates, mine);
-      }
-      __syncwarp();
-    } else if (BIAS) {
-      sure = false;
-    } else {  // many equal logits, or a large k: one after the other
-      for (int i = 0; i < p.k; ++i) {
-        uint32_t key;
-        int e;
-        if (!choice.best(lane, key, e)) break;
-        if (lane == i) mine = e;
-        choice.take(lane, e);
-      }
+    if (lane < candidates) mine_of[place] = own;
+    __syncwarp();
+    const uint2 here = lane < candidates ? mine_of[lane] : make_uint2(0, 0);
+    mine = lane < candidates ? (int)here.y : -1;
+    if (BIAS) {
+      // A chosen one against the one before, all that are left against the last chosen: there may be equals of it before one that it is too close to.
+      const uint2 before = lane > 0 && lane < candidates ? mine_of[min(lane, p.k) - 1] : make_uint2(0, 0);
+      bool doubt = lane > 0 && lane < candidates && key_value(before.x) - key_value(here.x) <= near;
+      // (the same logit under the same bias: a tie, whatever the arithmetic)
+      if (doubt) doubt = !(logit<T>(row, here.y) == logit<T>(row, before.y) && p.bias[here.y] == p.bias[before.y]);
+      if (__any_sync(~0u, doubt)) mine = order64<T, V>(p, row, top, lane, candidates, mine);
     }
-  }
-  if (!sure) {
+    __syncwarp();
+  } else if constexpr (BIAS) {
     choose64<T, V>(p, row, top, lane, chosen);
     mine = lane < p.k ? chosen[lane] : -1;
     __syncwarp();
+  } else {  // many equal logits, or a large k: one after the other
+    for (int i = 0; i < p.k; ++i) {
+      uint32_t key;
+      int e;
+      if (!choice.best(lane, key, e)) break;
+      if (lane == i) mine = e;
+      choice.take(lane, e);
+    }
   }
   if (lane >= p.k) mine = -1;
   // weights: lane i's
