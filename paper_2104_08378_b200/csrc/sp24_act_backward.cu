@@ -165,6 +165,9 @@ __device__ __forceinline__ int expert_of_row(const ActGradParams& p, int64_t r) 
   return lo;
 }
 
+// dz is rounded to the operands' 16 bits, because what reads it are two products of 16-bit tensor-core operands (kept in FP32 it would be TF32 ones at half the rate, over
+// twice the bytes): dX and dW are off by the roundings of dz as well as by their own (bf16 8192 rows of 8 experts 4096 x 2048, against FP64: 0.0023, 0.0017 without).
+// The sums are of the values before it.
 // dz, and the bias's gradient of each expert's rows: tile i of kTile rows has a partial sum of its own for every expert that it meets, in row i + (expert) of
 // `partial`, which no other tile and expert share.  16-bit types, rows of whole vectors at 16-byte boundaries.  The tile's values go through shared memory in FP32, where a
 // column's sum may end at any row.  Bound by HBM and the arithmetic of the slope: us, device, bf16 8192 x 4096 in 8 experts, GELU 46, SiLU 44, without the sums 35 (floor 31);

@@ -89,8 +89,8 @@ TileShape choose_expert_tile(const sp24_expert_desc* d, bool has_c, bool has_pre
 
 // The same for dense weights (D and dX): M features of the result, K of the contraction.  Pairs of CTAs whatever the rows, if there are features for them; what a column
 // of a tile costs next to its 256 rows was set so that up to 160 columns, with which the ring has four stages (three from 192 on), are taken where there are a few rounds of
-// tiles and 256 where there are many.  Us, device, bf16 dX, widths 96, 128, 160, 256 and today's: 8 experts 2816 x 2048, 128 rows each 24, 25, 18, 20; 528: 60, 50, 54, 62;
-// 1024: 93, 86, 73, 90; 50 of 2336 x 1760, 16 rows 55, 56, 56, 58, 1024 479, 420, 422, 391.
+// tiles and 256 where there are many.  Us, device, bf16 dX, widths 96, 128, 160, 256 and as chosen: 8 experts 2816 x 2048, 128 rows each 23, 17, 17, 19, 19; 528: 51, 48, 46, 54, 49;
+// 1024: 95, 75, 78, 75, 75; 50 of 2336 x 1760, 16 rows 65, 65, 65, 68, 66, 1024 434, 405, 352, 363, 360.
 TileShape choose_dense_tile(const sp24_expert_desc* d, int64_t M, int64_t K) {
   const int64_t mean = mean_rows(d), met = d->E < d->rows ? d->E : d->rows;
   const int es = elem_bytes(d->ab_type), ctas = M > 128 ? 2 : 1, most = ctas == 2 ? 256 : 128;
